@@ -440,6 +440,109 @@ int randes_retrieve_static(const randes_plan_t* plan, uint32_t task_id, float la
                            randes_dtype_t out_dtype, const void* const* base, const void* M,
                            void* const* out, void* stream);
 
+/*
+ * Weights in four bits with group scales
+ * --------------------------------------
+ * (The paper has no counterpart: it keeps W_0 and M in the weights' own type.  A model that answers token by token
+ * reads every weight once per token, so the bytes per weight are the time per token.)
+ * A row is cut into groups of `group` columns (32, 64 or 128; the last may be shorter).  With a = max |w| of a group,
+ *     s = bf16( a / 7 )  (0 when that is below 2^-100),   q = rint( w / s ) in [-7, 7],   the four bits stand for q * s
+ * (both quotients rounded once in fp32, ties of rint to even).  A group that holds a NaN or an infinity gets s = NaN and
+ * reads back as NaN.  A packed matrix is one opaque buffer of randes_packed_bytes(), 16-byte aligned, device memory of
+ * the caller's; the library never keeps anything else about it.
+ */
+typedef struct {
+    void* data;              /* device; [rows, cols], fp32 or bf16, element-aligned */
+    uint32_t rows, cols;
+    uint64_t stride;         /* elements between rows, >= cols */
+} randes_matrix_t;
+
+/* Bytes of a packed [rows, cols] matrix; 0 on invalid arguments or an empty matrix.  Host-only. */
+size_t randes_packed_bytes(uint32_t rows, uint32_t cols, uint32_t group);
+
+/*
+ * Pack n matrices (one kernel launch per 32).
+ *   w[n]        HOST array; data is read only.  All of one element type `dtype`
+ *   packed[n]   HOST array of device pointers; must not overlap w
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, CUDA_ERROR.
+ */
+int randes_pack(const randes_matrix_t* w, uint32_t n, randes_dtype_t dtype, uint32_t group, void* const* packed, void* stream);
+
+/* The values the four bits stand for: exact in fp32, rounded once (nearest even) for bf16.  out[n] as w[n] above, written. */
+int randes_unpack(const void* const* packed, uint32_t n, uint32_t group, const randes_matrix_t* out, randes_dtype_t out_dtype,
+                  void* stream);
+
+/*
+ * retrieve straight into four bits: packs What_t[layers[i]] = fma(lambda, s_t M[sigma_t^-1], W_0) -- the fp32 values
+ * that randes_retrieve writes -- without storing them (Section 4, second display).
+ *   layers[n]          HOST array of layer indices
+ *   base[n_layers], M  as for randes_retrieve (only the named layers of base are used)
+ *   packed[n]          HOST array of device pointers, one per named layer
+ * Needs no workspace (the plan may have been built without one).  One kernel launch per 32 layers.
+ * Errors: those of randes_pack, plus UNKNOWN_TASK.
+ */
+int randes_retrieve_packed(const randes_plan_t* plan, uint32_t task_id, float lambda, const uint32_t* layers, uint32_t n,
+                           const void* const* base, const void* M, uint32_t group, void* const* packed, void* stream);
+
+/*
+ * A few tokens through a packed matrix:  y[b][r] = sum_c x[b][c] * q[r][c] s[r][c / group].
+ *   x, x_dtype, x_stride   device [n_tokens, cols], fp32 or bf16, x_stride elements between tokens (>= cols)
+ *   y, y_dtype, y_stride   device [n_tokens, rows] likewise; must not overlap the inputs
+ * Products are exact (an fp32 activation is taken as the sum of three bf16 terms), sums run in fp32 in a fixed order, a
+ * bf16 y is rounded once.  The matrix is read once per 64 tokens (one kernel launch each); meant for few tokens -- for many,
+ * retrieve the weight and use a dense product.  16-byte aligned tokens are read fastest.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, CUDA_ERROR.
+ */
+int randes_packed_linear(const void* packed, uint32_t rows, uint32_t cols, uint32_t group, const void* x, randes_dtype_t x_dtype,
+                         uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream);
+
+/*
+ * A few tokens, each of its own task, through one layer kept as packed base and packed superposition (Section 4, second
+ * display, inside y = x What^T, for several models at once):
+ *   y[b][r] = sum_c x[b][c] W_0q[p][r,c] + lambda * sum_c s_t(l,c) x[b][c] Mq[l][r,c],   t = task_ids[b], l = sigma_t^-1(p)
+ * The base is read once for all tokens and each distinct slot once for the tokens whose task keeps this layer there.
+ *   task_ids[n_tokens]   HOST array, copied; ids may repeat
+ *   packed_base          layer p of W_0 packed with `group`
+ *   packed_m[n_layers]   HOST array: slot l of M packed with `group` (entries of slots that no token uses may be NULL)
+ * Otherwise as randes_packed_linear.  Needs no workspace.  Errors: those of randes_packed_linear, plus UNKNOWN_TASK.
+ */
+int randes_packed_linear_tasks(const randes_plan_t* plan, float lambda, uint32_t layer, uint32_t group, const uint32_t* task_ids,
+                               uint32_t n_tokens, const void* x, randes_dtype_t x_dtype, uint64_t x_stride, const void* packed_base,
+                               const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream);
+
+/*
+ * What a model answers: log probabilities of given tokens, entropy, and the top alternatives (the paper's language models
+ * are scored by the probability of label words).  With u = scale * logits[row] (scale = one over the temperature):
+ *   logprob[row]      u[target] - logsumexp(u)
+ *   entropy[row]      -sum_j p_j log p_j,  p = softmax(u)
+ *   stats[2][row]     max of the logits; log sum_j exp(u_j - scale * max): what the backward call needs
+ *   top_ids, top_logprobs[row][top_k]   the top_k largest logits, best first, equal ones by index
+ * A logit of -inf is a masked token: probability 0, never among the top alternatives (missing entries: id -1, -inf).  A row
+ * with nothing left: logprob -inf, entropy 0.  A NaN or +inf among a row's logits: NaN, ids -1.
+ *   logits     device [n_rows, vocab], fp32 or bf16, `stride` elements between rows (>= vocab), element-aligned
+ *   targets    device int64 [n_rows], or NULL (logprob is then not written).  Negative: the row is not scored
+ *              (logprob 0, no gradient through it).  >= vocab: NaN
+ *   top_k      0 .. 64 (0: top_ids and top_logprobs are not written); scale in [1e-6, 1e6]
+ * One pass over the logits, sums in fp32, one kernel launch; results do not depend on timing.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, CUDA_ERROR.
+ */
+int randes_token_scores(const void* logits, randes_dtype_t dtype, uint32_t n_rows, uint32_t vocab, uint64_t stride,
+                        const int64_t* targets, float scale, uint32_t top_k, float* logprob, float* entropy, float* stats,
+                        int64_t* top_ids, float* top_logprobs, void* stream);
+
+/*
+ * Gradient of sum_row g_logprob logprob + g_entropy entropy with respect to the logits:
+ *   grad[row][j] = scale * ( g_logprob (1[j = target] - p_j) - g_entropy p_j (log p_j + entropy) )
+ *   stats, entropy          of randes_token_scores on the same logits and scale
+ *   g_logprob, g_entropy    device fp32 [n_rows]; either may be NULL (zero).  g_logprob needs targets
+ *   grad                    device [n_rows, vocab] of the logits' type, grad_stride elements between rows; may be the
+ *                           logits' own memory with the same stride
+ * One read, one write, one kernel launch.  Errors: as randes_token_scores.
+ */
+int randes_token_scores_backward(const void* logits, randes_dtype_t dtype, uint32_t n_rows, uint32_t vocab, uint64_t stride,
+                                 const int64_t* targets, float scale, const float* stats, const float* entropy,
+                                 const float* g_logprob, const float* g_entropy, void* grad, uint64_t grad_stride, void* stream);
+
 /* Number of kernels this library has launched in this process (all plans). */
 uint64_t randes_launch_count(void);
 

@@ -1486,3 +1486,429 @@ int randes_retrieve_static(const randes_plan_t* plan, uint32_t task_id, float la
 }
 
 }  // extern "C"
+
+// ---- weights in four bits, products with them, token scores ------------------------------------
+namespace {
+
+int check_dtype(int dtype, const char* what)
+{
+    if (dtype != RANDES_F32 && dtype != RANDES_BF16) return fail(RANDES_UNSUPPORTED_DTYPE, "%s dtype %d is not supported", what, dtype);
+    return RANDES_OK;
+}
+
+int check_group(uint32_t group)
+{
+    if (group != 32 && group != 64 && group != 128) return fail(RANDES_INVALID_ARGUMENT, "group = %u is not 32, 64 or 128", group);
+    return RANDES_OK;
+}
+
+int check_packed(const void* p, const char* what)
+{
+    if (!p) return fail(RANDES_INVALID_ARGUMENT, "%s is NULL", what);
+    if (reinterpret_cast<uintptr_t>(p) % 16) return fail(RANDES_MISALIGNED, "%s = %p is not 16-byte aligned", what, p);
+    return RANDES_OK;
+}
+
+// Bytes from the first to one past the last element of [rows, cols] with a row stride.
+uint64_t span_bytes(uint64_t rows, uint64_t cols, uint64_t stride, size_t elem) { return rows && cols ? ((rows - 1) * stride + cols) * elem : 0; }
+
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
+}
+
+// A strided [rows, cols] tensor of the caller's.
+int check_tensor(const void* p, uint64_t rows, uint64_t cols, uint64_t stride, size_t elem, const char* what)
+{
+    if (rows == 0 || cols == 0) return RANDES_OK;
+    if (!p) return fail(RANDES_INVALID_ARGUMENT, "%s is NULL", what);
+    if (reinterpret_cast<uintptr_t>(p) % elem) return fail(RANDES_MISALIGNED, "%s = %p is not aligned to its element size", what, p);
+    if (stride < cols && rows > 1) return fail(RANDES_INVALID_ARGUMENT, "%s: stride %llu is smaller than %llu columns", what,
+                                               static_cast<unsigned long long>(stride), static_cast<unsigned long long>(cols));
+    if (stride > (1ull << 40)) return fail(RANDES_INVALID_ARGUMENT, "%s: stride %llu is beyond 2^40", what, static_cast<unsigned long long>(stride));
+    return RANDES_OK;
+}
+
+// Whether every row of the tensor starts on a 16-byte boundary.
+bool rows_aligned(const void* p, uint64_t rows, uint64_t stride, size_t elem)
+{
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (stride * elem) % 16 == 0);
+}
+
+int current_sm_count(int* sms)
+{
+    static std::atomic<int> known[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev < 64 && known[dev].load(std::memory_order_relaxed)) {
+        *sms = known[dev].load(std::memory_order_relaxed);
+        return RANDES_OK;
+    }
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return fail_cuda(e, "query of the current device");
+    if (dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
+    return RANDES_OK;
+}
+
+DevTask dev_task(const TaskEntry& t)
+{
+    DevTask d;
+    d.id = t.id;
+    d.key0 = static_cast<uint32_t>(t.seed);
+    d.key1 = static_cast<uint32_t>(t.seed >> 32);
+    d.pad = 0;
+    return d;
+}
+
+int check_matrix(const randes_matrix_t& m, uint32_t i, size_t elem, uint32_t group, const void* packed)
+{
+    int rc;
+    char what[32];
+    snprintf(what, sizeof what, "matrix %u", i);
+    if ((rc = check_tensor(m.data, m.rows, m.cols, m.stride, elem, what))) return rc;
+    if (m.rows == 0 || m.cols == 0) return RANDES_OK;
+    if (static_cast<uint64_t>(m.rows) * m.cols > 0xFFFFFFFFull) return fail(RANDES_INVALID_ARGUMENT, "matrix %u has 2^32 elements or more", i);
+    snprintf(what, sizeof what, "packed[%u]", i);
+    if ((rc = check_packed(packed, what))) return rc;
+    if (overlap(m.data, span_bytes(m.rows, m.cols, m.stride, elem), packed, randes_packed_bytes(m.rows, m.cols, group)))
+        return fail(RANDES_INVALID_ARGUMENT, "packed[%u] overlaps its matrix", i);
+    return RANDES_OK;
+}
+
+int randes_pack_impl(const randes_matrix_t* w, uint32_t n, randes_dtype_t dtype, uint32_t group, void* const* packed, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(dtype, "weight")) || (rc = check_group(group))) return rc;
+    if (n == 0) return RANDES_OK;
+    if (!w || !packed) return fail(RANDES_INVALID_ARGUMENT, "w or packed is NULL");
+    const size_t elem = elem_size(dtype);
+    for (uint32_t i = 0; i < n; ++i)
+        if ((rc = check_matrix(w[i], i, elem, group, packed[i]))) return rc;
+    for (uint32_t first = 0; first < n;) {
+        PackArgs a;
+        a.n = 0;
+        a.group = group;
+        a.lambda = 0.f;
+        a.task = DevTask{0, 0, 0, 0};
+        for (; first < n && a.n < kPackBatch; ++first) {
+            const randes_matrix_t& m = w[first];
+            if (m.rows == 0 || m.cols == 0) continue;
+            PackMatrix& d = a.mat[a.n++];
+            d = PackMatrix{m.data, nullptr, packed[first], m.stride, m.rows, m.cols, 0, 0, rows_aligned(m.data, m.rows, m.stride, elem) ? 1u : 0u, 0};
+        }
+        if (a.n == 0) break;
+        const int e = launch_pack(dtype, dtype, false, a, stream);
+        if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the pack kernel");
+        ++g_launches;
+    }
+    return RANDES_OK;
+}
+
+int randes_unpack_impl(const void* const* packed, uint32_t n, uint32_t group, const randes_matrix_t* out, randes_dtype_t out_dtype, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(out_dtype, "output")) || (rc = check_group(group))) return rc;
+    if (n == 0) return RANDES_OK;
+    if (!out || !packed) return fail(RANDES_INVALID_ARGUMENT, "out or packed is NULL");
+    const size_t elem = elem_size(out_dtype);
+    for (uint32_t i = 0; i < n; ++i)
+        if ((rc = check_matrix(out[i], i, elem, group, packed[i]))) return rc;
+    for (uint32_t first = 0; first < n;) {
+        UnpackArgs a;
+        a.n = 0;
+        a.group = group;
+        for (; first < n && a.n < kPackBatch; ++first) {
+            const randes_matrix_t& m = out[first];
+            if (m.rows == 0 || m.cols == 0) continue;
+            a.mat[a.n++] = UnpackMatrix{packed[first], m.data, m.stride, m.rows, m.cols, rows_aligned(m.data, m.rows, m.stride, elem) ? 1u : 0u, 0};
+        }
+        if (a.n == 0) break;
+        const int e = launch_unpack(out_dtype, a, stream);
+        if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the unpack kernel");
+        ++g_launches;
+    }
+    return RANDES_OK;
+}
+
+int randes_retrieve_packed_impl(const randes_plan_t* plan, uint32_t task_id, float lambda, const uint32_t* layers, uint32_t n,
+                                const void* const* base, const void* M, uint32_t group, void* const* packed, void* stream)
+{
+    if (!plan) return fail(RANDES_INVALID_ARGUMENT, "plan is NULL");
+    if (plan->has_gauss) return fail(RANDES_INVALID_ARGUMENT, "not offered for plans with a RANDES_GAUSS group");
+    int rc;
+    if ((rc = check_group(group)) || (rc = check_m(M))) return rc;
+    const int row = find_task(*plan, task_id);
+    if (row < 0) return fail(RANDES_UNKNOWN_TASK, "task id %u is not registered", task_id);
+    if (n == 0) return RANDES_OK;
+    if (!layers || !base || !packed) return fail(RANDES_INVALID_ARGUMENT, "layers, base or packed is NULL");
+    const size_t elem = elem_size(plan->storage), m_elem = elem_size(plan->m_dtype);
+    for (uint32_t i = 0; i < n; ++i) {
+        if (layers[i] >= plan->n_layers) return fail(RANDES_INVALID_ARGUMENT, "layer %u out of range (n_layers = %u)", layers[i], plan->n_layers);
+        const randes_layer_t& l = plan->layers[layers[i]];
+        if ((rc = check_matrix(randes_matrix_t{const_cast<void*>(base[layers[i]]), l.rows, l.cols, l.cols}, i, elem, group, packed[i]))) return rc;
+        if (overlap(M, plan->m_bytes, packed[i], randes_packed_bytes(l.rows, l.cols, group)))
+            return fail(RANDES_INVALID_ARGUMENT, "packed[%u] overlaps M", i);
+    }
+    const TaskEntry& t = plan->tasks[row];
+    for (uint32_t first = 0; first < n;) {
+        PackArgs a;
+        a.n = 0;
+        a.group = group;
+        a.lambda = lambda;
+        a.task = dev_task(t);
+        for (; first < n && a.n < kPackBatch; ++first) {
+            const uint32_t p = layers[first], slot = t.slot_of_pos[p];
+            const randes_layer_t& l = plan->layers[p];
+            if (l.rows == 0 || l.cols == 0) continue;
+            const char* m = static_cast<const char*>(M) + plan->m_off_bytes[slot];
+            const uint32_t vec = (rows_aligned(base[p], l.rows, l.cols, elem) ? 1u : 0u) | (rows_aligned(m, l.rows, l.cols, m_elem) ? 2u : 0u);
+            a.mat[a.n++] = PackMatrix{base[p], m, packed[first], l.cols, l.rows, l.cols, slot, plan->dev_layers[slot].flags & kFlagFlip ? 1u : 0u, vec, 0};
+        }
+        if (a.n == 0) break;
+        const int e = launch_pack(plan->storage, plan->m_dtype, true, a, stream);
+        if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the retrieve-and-pack kernel");
+        ++g_launches;
+    }
+    return RANDES_OK;
+}
+
+// What both products check, and their token blocks of 64. `fill(a, first)` sets the segments of the tokens first .. .
+template <typename Fill>
+int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, int x_dtype, uint64_t x_stride, uint32_t n_tokens, void* y,
+                  int y_dtype, uint64_t y_stride, float lambda, void* stream, Fill&& fill)
+{
+    int rc;
+    const size_t xe = elem_size(x_dtype), ye = elem_size(y_dtype);
+    if ((rc = check_tensor(x, n_tokens, cols, x_stride, xe, "x")) || (rc = check_tensor(y, n_tokens, rows, y_stride, ye, "y"))) return rc;
+    // (strided tensors may interleave without sharing an element; dense ones are compared)
+    if ((n_tokens == 1 || (x_stride == cols && y_stride == rows)) &&
+        overlap(x, span_bytes(n_tokens, cols, x_stride, xe), y, span_bytes(n_tokens, rows, y_stride, ye)))
+        return fail(RANDES_INVALID_ARGUMENT, "y overlaps x");
+    int sms = 0;
+    if ((rc = current_sm_count(&sms))) return rc;
+    PackedLinearArgs a;
+    a.x_stride = x_stride;
+    a.y_stride = y_stride;
+    a.rows = rows;
+    a.cols = cols;
+    a.group = group;
+    a.x_vec = rows_aligned(x, n_tokens, x_stride, xe);
+    a.y_bf16 = y_dtype == RANDES_BF16;
+    a.lambda = lambda;
+    for (uint32_t first = 0; first < n_tokens; first += kPackedTokens) {
+        a.x = static_cast<const char*>(x) + first * x_stride * xe;
+        a.y = static_cast<char*>(y) + first * y_stride * ye;
+        a.n_tokens = std::min(kPackedTokens, n_tokens - first);
+        fill(a, first);
+        const int e = launch_packed_linear(a, x_dtype == RANDES_BF16, sms, stream);
+        if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the packed linear kernel");
+        ++g_launches;
+    }
+    return RANDES_OK;
+}
+
+int randes_packed_linear_impl(const void* packed, uint32_t rows, uint32_t cols, uint32_t group, const void* x, randes_dtype_t x_dtype,
+                              uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(x_dtype, "activation")) || (rc = check_dtype(y_dtype, "output")) || (rc = check_group(group))) return rc;
+    if (static_cast<uint64_t>(rows) * cols > 0xFFFFFFFFull) return fail(RANDES_INVALID_ARGUMENT, "the matrix has 2^32 elements or more");
+    if (n_tokens == 0 || rows == 0) return RANDES_OK;
+    if (cols && (rc = check_packed(packed, "packed"))) return rc;
+    if (overlap(packed, randes_packed_bytes(rows, cols, group), y, span_bytes(n_tokens, rows, y_stride, elem_size(y_dtype))))
+        return fail(RANDES_INVALID_ARGUMENT, "y overlaps packed");
+    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, 0.f, stream, [&](PackedLinearArgs& a, uint32_t) {
+        a.n_seg = 1;
+        a.seg[0] = PackedSegment{packed, 0, a.n_tokens, 0, 0};
+        for (uint32_t b = 0; b < a.n_tokens; ++b) a.token[b] = static_cast<uint8_t>(b);
+    });
+}
+
+int randes_packed_linear_tasks_impl(const randes_plan_t* plan, float lambda, uint32_t layer, uint32_t group, const uint32_t* task_ids,
+                                    uint32_t n_tokens, const void* x, randes_dtype_t x_dtype, uint64_t x_stride, const void* packed_base,
+                                    const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream)
+{
+    if (!plan) return fail(RANDES_INVALID_ARGUMENT, "plan is NULL");
+    if (plan->has_gauss) return fail(RANDES_INVALID_ARGUMENT, "not offered for plans with a RANDES_GAUSS group");
+    int rc;
+    if ((rc = check_dtype(x_dtype, "activation")) || (rc = check_dtype(y_dtype, "output")) || (rc = check_group(group))) return rc;
+    if (layer >= plan->n_layers) return fail(RANDES_INVALID_ARGUMENT, "layer %u out of range (n_layers = %u)", layer, plan->n_layers);
+    const uint32_t rows = plan->layers[layer].rows, cols = plan->layers[layer].cols;
+    if (n_tokens == 0) return RANDES_OK;
+    if (!task_ids) return fail(RANDES_INVALID_ARGUMENT, "task_ids is NULL");
+    std::vector<int> task_row(n_tokens);      // registry entry of every token
+    for (uint32_t b = 0; b < n_tokens; ++b) {
+        task_row[b] = b && task_ids[b] == task_ids[b - 1] ? task_row[b - 1] : find_task(*plan, task_ids[b]);
+        if (task_row[b] < 0) return fail(RANDES_UNKNOWN_TASK, "task id %u is not registered", task_ids[b]);
+    }
+    if (rows == 0) return RANDES_OK;
+    const uint64_t y_bytes = span_bytes(n_tokens, rows, y_stride, elem_size(y_dtype)), p_bytes = randes_packed_bytes(rows, cols, group);
+    if (cols) {
+        if ((rc = check_packed(packed_base, "packed_base"))) return rc;
+        if (!packed_m) return fail(RANDES_INVALID_ARGUMENT, "packed_m is NULL");
+        if (overlap(packed_base, p_bytes, y, y_bytes)) return fail(RANDES_INVALID_ARGUMENT, "y overlaps packed_base");
+        for (uint32_t b = 0; b < n_tokens; ++b) {
+            if (b && task_row[b] == task_row[b - 1]) continue;
+            const uint32_t slot = plan->tasks[task_row[b]].slot_of_pos[layer];
+            if ((rc = check_packed(packed_m[slot], "packed_m of a slot in use"))) return rc;
+            if (overlap(packed_m[slot], p_bytes, y, y_bytes)) return fail(RANDES_INVALID_ARGUMENT, "y overlaps packed_m[%u]", slot);
+        }
+    }
+    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, lambda, stream, [&](PackedLinearArgs& a, uint32_t first) {
+        const uint32_t n = a.n_tokens;
+        a.seg[0] = PackedSegment{packed_base, 0, n, 0, 0};
+        uint32_t n_task = 0, slot_of[kPackedTokens];
+        int row_of[kPackedTokens];
+        for (uint32_t b = 0; b < n; ++b) {
+            uint32_t k = 0;
+            while (k < n_task && row_of[k] != task_row[first + b]) ++k;
+            if (k == n_task) {
+                row_of[n_task++] = task_row[first + b];
+                a.task[k] = dev_task(plan->tasks[task_row[first + b]]);
+            }
+            a.token[b] = static_cast<uint8_t>(b);
+            a.token_task[b] = static_cast<uint8_t>(k);
+            slot_of[b] = plan->tasks[task_row[first + b]].slot_of_pos[layer];
+        }
+        // tokens of one slot next to one another, slots in the order in which tokens first need them
+        uint32_t at = n;
+        a.n_seg = 1;
+        for (uint32_t b = 0; b < n; ++b) {
+            bool seen = false;
+            for (uint32_t k = 1; k < a.n_seg && !seen; ++k) seen = a.seg[k].slot == slot_of[b];
+            if (seen) continue;
+            PackedSegment& s = a.seg[a.n_seg++];
+            s = PackedSegment{cols ? packed_m[slot_of[b]] : nullptr, at, 0, slot_of[b], plan->dev_layers[slot_of[b]].flags & kFlagFlip ? 1u : 0u};
+            for (uint32_t i = b; i < n; ++i)
+                if (slot_of[i] == slot_of[b]) {
+                    a.token[at] = static_cast<uint8_t>(i);
+                    a.token_task[at] = a.token_task[i];
+                    a.pos_of_token[i] = static_cast<uint8_t>(at++);
+                    ++s.count;
+                }
+        }
+    });
+}
+
+int check_scores(const void* logits, int dtype, uint32_t n_rows, uint32_t vocab, uint64_t stride, const int64_t* targets, float scale)
+{
+    int rc;
+    if ((rc = check_dtype(dtype, "logits"))) return rc;
+    if (!(scale >= 1e-6f && scale <= 1e6f)) return fail(RANDES_INVALID_ARGUMENT, "scale = %g is not in [1e-6, 1e6]", static_cast<double>(scale));
+    if (vocab > 0x7FFFFFFFu || n_rows > 0x07FFFFFFu) return fail(RANDES_INVALID_ARGUMENT, "%u rows x %u logits exceed the supported 134217727 x 2147483647", n_rows, vocab);
+    if (reinterpret_cast<uintptr_t>(targets) % 8) return fail(RANDES_MISALIGNED, "targets = %p is not 8-byte aligned", (const void*)targets);
+    return check_tensor(logits, n_rows, vocab, stride, elem_size(dtype), "logits");
+}
+
+int randes_token_scores_impl(const void* logits, randes_dtype_t dtype, uint32_t n_rows, uint32_t vocab, uint64_t stride, const int64_t* targets,
+                             float scale, uint32_t top_k, float* logprob, float* entropy, float* stats, int64_t* top_ids,
+                             float* top_logprobs, void* stream)
+{
+    int rc;
+    if ((rc = check_scores(logits, dtype, n_rows, vocab, stride, targets, scale))) return rc;
+    if (top_k > kMaxTop) return fail(RANDES_INVALID_ARGUMENT, "top_k = %u exceeds the supported %u", top_k, kMaxTop);
+    if (n_rows == 0) return RANDES_OK;
+    if (!entropy || !stats || (targets && !logprob)) return fail(RANDES_INVALID_ARGUMENT, "logprob, entropy or stats is NULL");
+    if (top_k && (!top_ids || !top_logprobs)) return fail(RANDES_INVALID_ARGUMENT, "top_ids or top_logprobs is NULL");
+    if ((reinterpret_cast<uintptr_t>(logprob) | reinterpret_cast<uintptr_t>(entropy) | reinterpret_cast<uintptr_t>(stats) |
+         reinterpret_cast<uintptr_t>(top_logprobs)) % 4 || reinterpret_cast<uintptr_t>(top_ids) % 8)
+        return fail(RANDES_MISALIGNED, "an output is not aligned to its element size");
+    int sms = 0;
+    if ((rc = current_sm_count(&sms))) return rc;
+    const ScoreArgs a{logits, targets, stride, n_rows, vocab, top_k, scale, logprob, entropy, stats, top_ids, top_logprobs};
+    const int e = launch_scores(dtype, a, sms, stream);
+    if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the token score kernel");
+    ++g_launches;
+    return RANDES_OK;
+}
+
+int randes_token_scores_backward_impl(const void* logits, randes_dtype_t dtype, uint32_t n_rows, uint32_t vocab, uint64_t stride,
+                                      const int64_t* targets, float scale, const float* stats, const float* entropy, const float* g_logprob,
+                                      const float* g_entropy, void* grad, uint64_t grad_stride, void* stream)
+{
+    int rc;
+    const size_t elem = elem_size(dtype);
+    if ((rc = check_scores(logits, dtype, n_rows, vocab, stride, targets, scale))) return rc;
+    if ((rc = check_tensor(grad, n_rows, vocab, grad_stride, elem, "grad"))) return rc;
+    if (n_rows == 0 || vocab == 0) return RANDES_OK;
+    if (!stats || !entropy) return fail(RANDES_INVALID_ARGUMENT, "stats or entropy is NULL");
+    if (g_logprob && !targets) return fail(RANDES_INVALID_ARGUMENT, "g_logprob without targets");
+    if ((reinterpret_cast<uintptr_t>(stats) | reinterpret_cast<uintptr_t>(entropy) | reinterpret_cast<uintptr_t>(g_logprob) |
+         reinterpret_cast<uintptr_t>(g_entropy)) % 4)
+        return fail(RANDES_MISALIGNED, "an input is not aligned to its element size");
+    if (!(grad == logits && (grad_stride == stride || n_rows == 1)) && (n_rows == 1 || (stride == vocab && grad_stride == vocab)) &&
+        overlap(logits, span_bytes(n_rows, vocab, stride, elem), grad, span_bytes(n_rows, vocab, grad_stride, elem)))
+        return fail(RANDES_INVALID_ARGUMENT, "grad overlaps the logits without being the same tensor");
+    const ScoreGradArgs a{logits, grad, targets, stats, entropy, g_logprob, g_entropy, stride, grad_stride, n_rows, vocab, scale};
+    const int e = launch_score_grad(dtype, a, stream);
+    if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the token score gradient kernel");
+    ++g_launches;
+    return RANDES_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t randes_packed_bytes(uint32_t rows, uint32_t cols, uint32_t group)
+{
+    if ((group != 32 && group != 64 && group != 128) || rows == 0 || cols == 0 || static_cast<uint64_t>(rows) * cols > 0xFFFFFFFFull) return 0;
+    return packed_codes_bytes(rows, cols) + (static_cast<size_t>(rows) + 15) / 16 * packed_groups(cols, group) * 32;
+}
+
+int randes_pack(const randes_matrix_t* w, uint32_t n, randes_dtype_t dtype, uint32_t group, void* const* packed, void* stream)
+{
+    return guarded("randes_pack", [&] { return randes_pack_impl(w, n, dtype, group, packed, stream); });
+}
+
+int randes_unpack(const void* const* packed, uint32_t n, uint32_t group, const randes_matrix_t* out, randes_dtype_t out_dtype, void* stream)
+{
+    return guarded("randes_unpack", [&] { return randes_unpack_impl(packed, n, group, out, out_dtype, stream); });
+}
+
+int randes_retrieve_packed(const randes_plan_t* plan, uint32_t task_id, float lambda, const uint32_t* layers, uint32_t n,
+                           const void* const* base, const void* M, uint32_t group, void* const* packed, void* stream)
+{
+    return guarded("randes_retrieve_packed", [&] { return randes_retrieve_packed_impl(plan, task_id, lambda, layers, n, base, M, group, packed, stream); });
+}
+
+int randes_packed_linear(const void* packed, uint32_t rows, uint32_t cols, uint32_t group, const void* x, randes_dtype_t x_dtype,
+                         uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream)
+{
+    return guarded("randes_packed_linear", [&] {
+        return randes_packed_linear_impl(packed, rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, stream);
+    });
+}
+
+int randes_packed_linear_tasks(const randes_plan_t* plan, float lambda, uint32_t layer, uint32_t group, const uint32_t* task_ids,
+                               uint32_t n_tokens, const void* x, randes_dtype_t x_dtype, uint64_t x_stride, const void* packed_base,
+                               const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream)
+{
+    return guarded("randes_packed_linear_tasks", [&] {
+        return randes_packed_linear_tasks_impl(plan, lambda, layer, group, task_ids, n_tokens, x, x_dtype, x_stride, packed_base, packed_m, y,
+                                               y_dtype, y_stride, stream);
+    });
+}
+
+int randes_token_scores(const void* logits, randes_dtype_t dtype, uint32_t n_rows, uint32_t vocab, uint64_t stride, const int64_t* targets,
+                        float scale, uint32_t top_k, float* logprob, float* entropy, float* stats, int64_t* top_ids, float* top_logprobs,
+                        void* stream)
+{
+    return guarded("randes_token_scores", [&] {
+        return randes_token_scores_impl(logits, dtype, n_rows, vocab, stride, targets, scale, top_k, logprob, entropy, stats, top_ids,
+                                        top_logprobs, stream);
+    });
+}
+
+int randes_token_scores_backward(const void* logits, randes_dtype_t dtype, uint32_t n_rows, uint32_t vocab, uint64_t stride,
+                                 const int64_t* targets, float scale, const float* stats, const float* entropy, const float* g_logprob,
+                                 const float* g_entropy, void* grad, uint64_t grad_stride, void* stream)
+{
+    return guarded("randes_token_scores_backward", [&] {
+        return randes_token_scores_backward_impl(logits, dtype, n_rows, vocab, stride, targets, scale, stats, entropy, g_logprob, g_entropy,
+                                                 grad, grad_stride, stream);
+    });
+}
+
+}  // extern "C"

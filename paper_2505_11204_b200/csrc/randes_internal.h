@@ -208,6 +208,99 @@ int launch_linear(const void* x, uint32_t n_tokens, const void* w0, const void* 
                   unsigned long long wait_ns, void* stream, int* n_launched);   // gate: NULL or a device word to wait on; wait_ns: 0 = one second
 int linear_giveups(unsigned int* count);   // CTAs that gave up on a bounded wait since the library was loaded (synchronises)
 
+// randes_packed.cu: weights in four bits with group scales (the layout is described there).
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+constexpr size_t packed_codes_bytes(uint32_t rows, uint32_t cols)
+{
+    return ((static_cast<size_t>(rows) + 15) / 16) * ((static_cast<size_t>(cols) + 63) / 64) * 512;
+}
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline uint32_t packed_groups(uint32_t cols, uint32_t group) { return cols / group + (cols % group ? 1u : 0u); }
+constexpr uint32_t kPackBatch = 32;       // matrices per launch of pack and unpack
+struct PackMatrix {
+    const void* src;              // weight (retrieve: W_0)
+    const void* m;                // retrieve: the slot of the superposition, rows x cols without padding
+    void* dst;
+    uint64_t stride;              // elements between rows of src
+    uint32_t rows, cols;
+    uint32_t slot, flip;
+    uint32_t vec;                 // bit 0: rows of src are 16-byte aligned; bit 1: rows of m
+    uint32_t first_cta;           // set by the launcher
+};
+struct PackArgs {
+    PackMatrix mat[kPackBatch];
+    uint32_t n, group;
+    float lambda;
+    DevTask task;
+};
+struct UnpackMatrix {
+    const void* src;
+    void* dst;
+    uint64_t stride;
+    uint32_t rows, cols, vec, first_cta;
+};
+struct UnpackArgs {
+    UnpackMatrix mat[kPackBatch];
+    uint32_t n, group;
+};
+constexpr uint32_t kPackedTokens = 64;    // tokens per launch of the product
+// One packed matrix and the tokens that go through it: positions first .. first + count - 1 of the token lists.
+struct PackedSegment {
+    const void* packed;
+    uint32_t first, count, slot, flip;
+};
+struct PackedLinearArgs {
+    const void* x;
+    void* y;
+    uint64_t x_stride, y_stride;  // elements between tokens
+    uint32_t rows, cols, group, n_tokens;
+    uint32_t n_seg, split;        // split: set by the launcher
+    uint32_t x_vec, y_bf16;
+    float lambda;
+    uint8_t token[2 * kPackedTokens];        // per position: the token
+    uint8_t token_task[2 * kPackedTokens];   // per position: its entry in `task`
+    uint8_t pos_of_token[kPackedTokens];     // the token's position in its slot's list
+    DevTask task[kPackedTokens];             // the distinct tasks of the launch
+    PackedSegment seg[1 + kPackedTokens];    // the base, then each distinct slot
+};
+// All return a cudaError_t as int.
+int launch_pack(int w_dtype, int m_dtype, bool retrieve, PackArgs& a, void* stream);
+int launch_unpack(int out_dtype, UnpackArgs& a, void* stream);
+int launch_packed_linear(PackedLinearArgs& a, bool x_bf16, int sm_count, void* stream);
+
+// randes_scores.cu: log probabilities, entropy and top alternatives of logits, and their gradient.
+constexpr uint32_t kMaxTop = 64;
+struct ScoreArgs {
+    const void* logits;
+    const int64_t* targets;       // or NULL
+    uint64_t stride;
+    uint32_t n_rows, vocab, top_k;
+    float scale;
+    float* logprob;               // NULL when targets is
+    float* entropy;
+    float* stats;                 // [2][n_rows]: greatest logit; log of the sum of exponentials relative to it
+    int64_t* top_ids;             // [n_rows][top_k]
+    float* top_logprobs;
+};
+struct ScoreGradArgs {
+    const void* logits;
+    void* grad;
+    const int64_t* targets;
+    const float* stats;
+    const float* entropy;
+    const float* g_logprob;       // either may be NULL
+    const float* g_entropy;
+    uint64_t stride, grad_stride;
+    uint32_t n_rows, vocab;
+    float scale;
+};
+int launch_scores(int dtype, const ScoreArgs& a, int sm_count, void* stream);
+int launch_score_grad(int dtype, const ScoreGradArgs& a, void* stream);
+
 // Retrieve with its tables in a fixed device array inside the library (no workspace).
 // Returns a cudaError_t as int, or -1 when the tables exceed kStaticScratchBytes.
 constexpr size_t kStaticScratchBytes = 1u << 20;

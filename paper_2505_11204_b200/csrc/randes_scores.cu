@@ -1,0 +1,433 @@
+// Log probabilities of given tokens, entropy and the top alternatives out of logits, in one pass; and their gradient.
+//
+// With u = scale * z (scale = one over the temperature), M = max z, d = z - M, S = sum exp(scale d), T = sum exp(scale d) d:
+//     log p_j = scale * d_j - ln S        H = -sum p log p = ln S - scale * T / S
+//     dz_j = scale * ( g_lp (1[j = target] - p_j) - g_H p_j (log p_j + H) )
+// The differences to the maximum are taken before anything is scaled, so no term carries the rounding of a large
+// exponent; each thread keeps (M, S, T) of what it has read and rescales them when its maximum rises.
+//
+// Top alternatives without sorting: a group of four threads knows the greatest of the elements it read; the k-th largest
+// of those group maxima cannot be above the k-th largest element, so only the groups that reach it are read again (about
+// k of 128), and what reaches it is ranked. Equal logits are ordered by index.
+//
+// A row may be shared by a cluster of CTAs (few rows); their sums and top lists meet in the first CTA through distributed
+// shared memory.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <cooperative_groups.h>
+
+#include <cfloat>
+
+#include "randes_device.cuh"
+#include "randes_internal.h"
+
+namespace cg = cooperative_groups;
+
+namespace randes {
+namespace {
+
+using namespace device;
+
+constexpr int kScoreThreads = 512;
+constexpr int kScoreWarps = kScoreThreads / 32;
+constexpr int kGroups = kScoreThreads / 4;      // groups of four threads; more than kMaxTop
+constexpr int kCandidates = 1024;
+constexpr int kMaxCluster = 8;
+static_assert(kGroups > static_cast<int>(kMaxTop), "the threshold is the k-th largest group maximum");
+
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// what one has read: greatest logit, sum of exp(scale (z - m)), sum of exp(scale (z - m)) (z - m)
+struct Sums { float m, s, t; };
+
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c)
+{
+    Sums r;
+    r.m = max_nan(a.m, b.m);
+    r.s = r.t = 0.f;
+    if (r.m == -INFINITY) return r;
+    if (a.m != -INFINITY) {
+        const float d = a.m - r.m, f = ex2(d * c);
+        r.s = f * a.s;
+        r.t = f * __fmaf_rn(a.s, d, a.t);
+        if (f == 0.f) r.s = r.t = 0.f;      // d may be infinite (the type's lowest value against a large one)
+    }
+    if (b.m != -INFINITY) {
+        const float d = b.m - r.m, f = ex2(d * c);
+        if (f != 0.f) {
+            r.s += f * b.s;
+            r.t += f * __fmaf_rn(b.s, d, b.t);
+        }
+    }
+    return r;
+}
+
+// order of (logit, index): larger logit first, then lower index; -0 counts as +0
+__device__ __forceinline__ unsigned long long key_of(float z, uint32_t idx)
+{
+    const uint32_t b = __float_as_uint(z + 0.f);
+    const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
+    return (static_cast<unsigned long long>(o) << 32) | (0xFFFFFFFFu - idx);
+}
+__device__ __forceinline__ float value_of(unsigned long long key)
+{
+    const uint32_t o = static_cast<uint32_t>(key >> 32);
+    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+__device__ __forceinline__ uint32_t index_of(unsigned long long key) { return 0xFFFFFFFFu - static_cast<uint32_t>(key); }
+
+// A CTA's share of a row: vectors [v0, v1) of the row's 16-byte aligned middle, and up to CPL - 1 single elements at
+// either end (given to the first and the last CTA).
+template <typename T> struct Share {
+    static constexpr int CPL = Store<T>::CPL;
+    const T* row;
+    uint32_t lead;            // elements before the aligned middle
+    uint32_t v0, v1;
+    uint32_t head, tail0, tail;   // single elements: 0 .. head - 1, tail0 .. tail0 + tail - 1
+    __device__ __forceinline__ Share(const T* r, uint32_t vocab, uint32_t rank, uint32_t ranks) : row(r)
+    {
+        const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(r) & 15) / sizeof(T);
+        lead = min(off ? CPL - off : 0u, vocab);
+        const uint32_t n = (vocab - lead) / CPL;
+        v0 = static_cast<uint32_t>(static_cast<uint64_t>(n) * rank / ranks);
+        v1 = static_cast<uint32_t>(static_cast<uint64_t>(n) * (rank + 1) / ranks);
+        head = rank == 0 ? lead : 0u;
+        tail0 = lead + n * CPL;
+        tail = rank == ranks - 1 ? vocab - tail0 : 0u;
+    }
+    __device__ __forceinline__ uint4 load(uint32_t v) const { return __ldg(reinterpret_cast<const uint4*>(row + lead) + v); }
+    // single element e (0 .. 2 CPL - 1) of this CTA: its index, or false
+    __device__ __forceinline__ bool single(uint32_t e, uint32_t& idx) const
+    {
+        if (e < static_cast<uint32_t>(CPL)) { idx = e; return e < head; }
+        idx = tail0 + e - CPL;
+        return e - CPL < tail;
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_constant__ ScoreArgs a)
+{
+    constexpr int CPL = Store<T>::CPL, U = 4;
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t ranks = cluster.num_blocks(), rank = cluster.block_rank();
+    const uint32_t row = blockIdx.x / ranks;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    __shared__ Sums s_warp[kScoreWarps];
+    __shared__ Sums s_cta;
+    __shared__ float s_group[kGroups];
+    __shared__ float s_tau;
+    __shared__ unsigned int s_count;
+    __shared__ unsigned long long s_cand[kCandidates];
+    __shared__ unsigned long long s_top[kMaxTop];          // this CTA's top list, best first; 0 = no element
+    __shared__ unsigned long long s_best[kScoreWarps];
+
+    const Share<T> sh(static_cast<const T*>(a.logits) + row * a.stride, a.vocab, rank, ranks);
+    const float c = a.scale * kLog2e;
+    Sums me = {-INFINITY, 0.f, 0.f};
+    auto take = [&](const float* z, int n, float top) {
+        const float m = max_nan(me.m, top);
+        if (m == -INFINITY) return;
+        if (m != me.m) {                     // also when m is NaN
+            const Sums old = me;
+            me.m = m;
+            me.s = me.t = 0.f;
+            if (old.m != -INFINITY) {
+                const float d = old.m - m, f = ex2(d * c);
+                if (f != 0.f) { me.s = f * old.s; me.t = f * __fmaf_rn(old.s, d, old.t); }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+            const float d = max_nan(z[e] - m, -1e30f);      // a masked element: exp gives 0, and 0 times this is 0
+            const float x = ex2(d * c);
+            me.s += x;
+            me.t = __fmaf_rn(x, d, me.t);
+        }
+    };
+    for (uint32_t v = sh.v0 + tid; v < sh.v1; v += kScoreThreads * U) {
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v + u * kScoreThreads < sh.v1) raw[u] = sh.load(v + u * kScoreThreads);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (v + u * kScoreThreads < sh.v1) {
+                float z[CPL];
+                Store<T>::widen(raw[u], z);
+                float top = z[0];
+#pragma unroll
+                for (int e = 1; e < CPL; ++e) top = max_nan(top, z[e]);
+                take(z, CPL, top);
+            }
+    }
+    uint32_t idx;
+    if (tid < 2 * CPL && sh.single(tid, idx)) {
+        const float z = Store<T>::load1(sh.row + idx);
+        take(&z, 1, z);
+    }
+    const float own_max = me.m;
+    // ---- sums of the CTA
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const Sums b = {__shfl_down_sync(~0u, me.m, o), __shfl_down_sync(~0u, me.s, o), __shfl_down_sync(~0u, me.t, o)};
+        me = join(me, b, c);
+    }
+    if (lane == 0) s_warp[warp] = me;
+    if (a.top_k) {
+        float gm = max_nan(own_max, __shfl_xor_sync(~0u, own_max, 1));
+        gm = max_nan(gm, __shfl_xor_sync(~0u, gm, 2));
+        if ((tid & 3) == 0) s_group[tid >> 2] = gm;
+        if (tid == 0) { s_count = 0; s_tau = -INFINITY; }
+    }
+    __syncthreads();
+    if (warp == 0) {
+        me = lane < kScoreWarps ? s_warp[lane] : Sums{-INFINITY, 0.f, 0.f};
+#pragma unroll
+        for (int o = kScoreWarps / 2; o > 0; o >>= 1) {
+            const Sums b = {__shfl_down_sync(~0u, me.m, o), __shfl_down_sync(~0u, me.s, o), __shfl_down_sync(~0u, me.t, o)};
+            me = join(me, b, c);
+        }
+        if (lane == 0) s_cta = me;
+    }
+    // ---- top list of the CTA
+    if (a.top_k) {
+        if (tid < kGroups) {
+            const float mine = s_group[tid];
+            uint32_t before = 0;
+            for (int j = 0; j < kGroups; ++j) {
+                const float o = s_group[j];
+                before += o > mine || (o == mine && j < tid);
+            }
+            if (before == a.top_k - 1) s_tau = mine;
+        }
+        __syncthreads();
+        const float tau = s_tau;
+        auto offer = [&](float z, uint32_t i) {
+            if (z >= tau && z > -INFINITY) {
+                const unsigned int at = atomicAdd(&s_count, 1u);
+                if (at < kCandidates) s_cand[at] = key_of(z, i);
+            }
+        };
+        for (int q = warp; q < kGroups; q += kScoreWarps) {
+            const float gm = s_group[q];
+            if (!(gm >= tau) || gm == -INFINITY) continue;
+            for (uint32_t v = sh.v0 + 4 * q + (lane & 3) + kScoreThreads * (lane >> 2); v < sh.v1; v += kScoreThreads * 8) {
+                float z[CPL];
+                Store<T>::widen(sh.load(v), z);
+#pragma unroll
+                for (int e = 0; e < CPL; ++e) offer(z[e], sh.lead + v * CPL + e);
+            }
+        }
+        if (tid < 2 * CPL && sh.single(tid, idx)) offer(Store<T>::load1(sh.row + idx), idx);
+        if (tid < static_cast<int>(kMaxTop)) s_top[tid] = 0ull;
+        __syncthreads();
+        const unsigned int n = s_count;
+        if (n <= kCandidates) {
+            for (unsigned int i = tid; i < n; i += kScoreThreads) {
+                const unsigned long long mine = s_cand[i];
+                unsigned int before = 0;
+                for (unsigned int j = 0; j < n; ++j) before += s_cand[j] > mine;
+                if (before < a.top_k) s_top[before] = mine;
+            }
+        } else {
+            // more equal (or nearly equal) logits than the list holds: the best below the last, k times over
+            unsigned long long last = ~0ull;
+            for (uint32_t k = 0; k < a.top_k; ++k) {
+                unsigned long long best = 0;
+                auto look = [&](float z, uint32_t i) {
+                    const unsigned long long key = z > -INFINITY ? key_of(z, i) : 0ull;
+                    if (key < last && key > best) best = key;
+                };
+                for (uint32_t v = sh.v0 + tid; v < sh.v1; v += kScoreThreads) {
+                    float z[CPL];
+                    Store<T>::widen(sh.load(v), z);
+#pragma unroll
+                    for (int e = 0; e < CPL; ++e) look(z[e], sh.lead + v * CPL + e);
+                }
+                if (tid < 2 * CPL && sh.single(tid, idx)) look(Store<T>::load1(sh.row + idx), idx);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    const unsigned long long b = __shfl_xor_sync(~0u, best, o);
+                    if (b > best) best = b;
+                }
+                if (lane == 0) s_best[warp] = best;
+                __syncthreads();
+                best = s_best[0];
+                for (int w = 1; w < kScoreWarps; ++w)
+                    if (s_best[w] > best) best = s_best[w];
+                if (tid == 0) s_top[k] = best;
+                last = best;
+                __syncthreads();
+                if (!best) break;            // the same in every thread
+            }
+        }
+    }
+    // ---- the row: sums and top lists of the cluster's CTAs meet in the first one
+    if (ranks > 1) cluster.sync(); else __syncthreads();
+    if (rank == 0) {
+        Sums all = s_cta;
+        for (uint32_t r = 1; r < ranks; ++r) all = join(all, *cluster.map_shared_rank(&s_cta, r), c);
+        const bool none = all.m == -INFINITY;
+        const float ln = none ? -INFINITY : logf(all.s);
+        const bool bad = !none && !(all.s < INFINITY);       // a NaN or +inf among the logits: NaN sum
+        if (tid == 0) {
+            a.stats[row] = all.m;
+            a.stats[static_cast<size_t>(a.n_rows) + row] = ln;
+            a.entropy[row] = none ? 0.f : __fmaf_rn(-a.scale, all.t / all.s, ln);
+            if (a.targets) {
+                const long long tk = a.targets[row];
+                float lp;
+                if (tk < 0) lp = 0.f;
+                else if (tk >= static_cast<long long>(a.vocab)) lp = NAN;
+                else if (none) lp = -INFINITY;
+                else lp = __fmaf_rn(a.scale, Store<T>::load1(sh.row + tk) - all.m, -ln);
+                a.logprob[row] = lp;
+            }
+        }
+        if (a.top_k) {
+            if (ranks > 1) {
+                // the other CTAs' lists join this one's; k * ranks entries, ranked like the candidates
+                const unsigned int n = a.top_k * ranks;
+                for (unsigned int i = tid; i < n; i += kScoreThreads) s_cand[i] = cluster.map_shared_rank(s_top, i / a.top_k)[i % a.top_k];
+                __syncthreads();
+                if (tid < static_cast<int>(kMaxTop)) s_top[tid] = 0ull;
+                __syncthreads();
+                for (unsigned int i = tid; i < n; i += kScoreThreads) {
+                    const unsigned long long mine = s_cand[i];
+                    unsigned int before = 0;
+                    for (unsigned int j = 0; j < n; ++j) before += s_cand[j] > mine;
+                    if (mine && before < a.top_k) s_top[before] = mine;
+                }
+                __syncthreads();
+            }
+            if (tid < static_cast<int>(a.top_k)) {
+                const unsigned long long key = bad ? 0ull : s_top[tid];
+                const size_t at = static_cast<size_t>(row) * a.top_k + tid;
+                a.top_ids[at] = key ? static_cast<long long>(index_of(key)) : -1;
+                a.top_logprobs[at] = bad ? NAN : (key ? __fmaf_rn(a.scale, value_of(key) - all.m, -ln) : -INFINITY);
+            }
+        }
+    }
+    if (ranks > 1) cluster.sync();           // nobody leaves while its shared memory may still be read
+}
+
+// ---- gradient ---------------------------------------------------------------------------------
+constexpr int kGradThreads = 256;
+constexpr int kGradVectors = 4;       // per thread
+
+// p and log p come back from the row's stats; one exponential per element, one read, one write.
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_constant__ ScoreGradArgs a, uint32_t chunks)
+{
+    constexpr int CPL = Store<T>::CPL;
+    const uint32_t row = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
+    const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+    T* dz = static_cast<T*>(a.grad) + row * a.grad_stride;
+    const float m = a.stats[row], ln = a.stats[static_cast<size_t>(a.n_rows) + row];
+    const long long tk = a.targets && a.g_logprob ? a.targets[row] : -1;
+    float gl = tk >= 0 ? a.g_logprob[row] : 0.f;
+    if (tk >= static_cast<long long>(a.vocab)) gl = NAN;
+    const float gh = a.g_entropy ? a.g_entropy[row] : 0.f;
+    const float h = a.entropy[row];
+    const bool none = m == -INFINITY;
+    const float a_p = -a.scale * __fmaf_rn(gh, h, gl), a_pl = -a.scale * gh, c = a.scale * kLog2e;
+    // dz = p (a_p + a_pl log p) [+ scale g_lp at the target]
+    auto grad = [&](float x, uint32_t j) {
+        if (none) return 0.f;
+        const float d = max_nan(x - m, -1e30f);
+        const float lp = __fmaf_rn(a.scale, d, -ln);
+        const float p = ex2(__fmaf_rn(d, c, -ln * kLog2e));
+        float r = p * __fmaf_rn(a_pl, lp, a_p);
+        if (static_cast<long long>(j) == tk) r = __fmaf_rn(a.scale, gl, r);
+        return r;
+    };
+    const uint32_t per = kGradThreads * kGradVectors * CPL;
+    const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T);
+    const uint32_t lead = min(off ? CPL - off : 0u, a.vocab);
+    // rows of the two tensors that sit alike in their 16-byte words go word by word, others element by element
+    if ((reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z) & 15)) {
+        const uint32_t n = (a.vocab - lead) / CPL;
+        uint4 raw[kGradVectors];
+        const uint32_t v0 = chunk * (kGradThreads * kGradVectors) + threadIdx.x;
+#pragma unroll
+        for (int u = 0; u < kGradVectors; ++u)
+            if (v0 + u * kGradThreads < n) raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + lead) + v0 + u * kGradThreads);
+#pragma unroll
+        for (int u = 0; u < kGradVectors; ++u) {
+            const uint32_t v = v0 + u * kGradThreads;
+            if (v >= n) break;
+            float x[CPL];
+            Store<T>::widen(raw[u], x);
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) x[e] = grad(x[e], lead + v * CPL + e);
+            Out<T>::template store<CPL>(dz + lead + v * CPL, x);
+        }
+        if (chunk == 0 && threadIdx.x < 2 * CPL) {
+            const uint32_t e = threadIdx.x, tail0 = lead + n * CPL;
+            const uint32_t j = e < static_cast<uint32_t>(CPL) ? e : tail0 + e - CPL;
+            if (e < static_cast<uint32_t>(CPL) ? e < lead : j < a.vocab) Out<T>::store1(dz + j, grad(Store<T>::load1(z + j), j));
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < per; i += kGradThreads) {
+            const uint64_t j = static_cast<uint64_t>(chunk) * per + i;
+            if (j < a.vocab) Out<T>::store1(dz + j, grad(Store<T>::load1(z + j), static_cast<uint32_t>(j)));
+        }
+    }
+}
+
+template <typename T> cudaError_t launch_scores_t(const ScoreArgs& a, int sm_count, cudaStream_t s)
+{
+    // a cluster shares a row while the rows alone do not fill the SMs and a share still is a few thousand elements
+    uint32_t ranks = 1;
+    while (ranks < kMaxCluster && static_cast<uint64_t>(a.n_rows) * ranks * 2 <= static_cast<uint64_t>(sm_count) && a.vocab / (ranks * 2) >= 2048) ranks *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.n_rows * ranks);
+    cfg.blockDim = dim3(kScoreThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ranks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, score_kernel<T>, a);
+}
+
+template <typename T> cudaError_t launch_grad_t(const ScoreGradArgs& a, cudaStream_t s)
+{
+    constexpr uint32_t per = kGradThreads * kGradVectors * Store<T>::CPL;
+    const uint32_t chunks = (a.vocab + per - 1) / per;
+    if (!chunks) return cudaSuccess;
+    score_grad_kernel<T><<<static_cast<unsigned>(chunks * a.n_rows), kGradThreads, 0, s>>>(a, chunks);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+int launch_scores(int dtype, const ScoreArgs& a, int sm_count, void* stream)
+{
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return static_cast<int>(dtype == 1 ? launch_scores_t<bf16>(a, sm_count, s) : launch_scores_t<float>(a, sm_count, s));
+}
+
+int launch_score_grad(int dtype, const ScoreGradArgs& a, void* stream)
+{
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return static_cast<int>(dtype == 1 ? launch_grad_t<bf16>(a, s) : launch_grad_t<float>(a, s));
+}
+
+}  // namespace randes

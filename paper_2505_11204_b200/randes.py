@@ -15,7 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import List, Optional, Sequence
+from typing import Any, List, NamedTuple, Optional, Sequence
 
 F32 = 0
 BF16 = 1
@@ -58,6 +58,10 @@ class Layer(ctypes.Structure):
 
 class Group(ctypes.Structure):
     _fields_ = [("flags", ctypes.c_uint32)]
+
+
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_uint32), ("cols", ctypes.c_uint32), ("stride", ctypes.c_uint64)]
 
 
 def lib():
@@ -129,6 +133,23 @@ def lib():
         L.randes_linear_gated.restype = ctypes.c_int
         L.randes_linear_giveups.argtypes = [ctypes.POINTER(ctypes.c_uint)]
         L.randes_linear_giveups.restype = ctypes.c_int
+        f32, dt = ctypes.c_float, ctypes.c_int
+        L.randes_packed_bytes.argtypes = [u32, u32, u32]
+        L.randes_packed_bytes.restype = sz
+        L.randes_pack.argtypes = [vp, u32, dt, u32, vp, vp]
+        L.randes_pack.restype = ctypes.c_int
+        L.randes_unpack.argtypes = [vp, u32, u32, vp, dt, vp]
+        L.randes_unpack.restype = ctypes.c_int
+        L.randes_retrieve_packed.argtypes = [vp, u32, f32, vp, u32, vp, vp, u32, vp, vp]
+        L.randes_retrieve_packed.restype = ctypes.c_int
+        L.randes_packed_linear.argtypes = [vp, u32, u32, u32, vp, dt, u64, u32, vp, dt, u64, vp]
+        L.randes_packed_linear.restype = ctypes.c_int
+        L.randes_packed_linear_tasks.argtypes = [vp, f32, u32, u32, vp, u32, vp, dt, u64, vp, vp, vp, dt, u64, vp]
+        L.randes_packed_linear_tasks.restype = ctypes.c_int
+        L.randes_token_scores.argtypes = [vp, dt, u32, u32, u64, vp, f32, u32, vp, vp, vp, vp, vp, vp]
+        L.randes_token_scores.restype = ctypes.c_int
+        L.randes_token_scores_backward.argtypes = [vp, dt, u32, u32, u64, vp, f32, vp, vp, vp, vp, vp, u64, vp]
+        L.randes_token_scores_backward.restype = ctypes.c_int
         L.randes_launch_count.argtypes = []
         L.randes_launch_count.restype = u64
         L.randes_last_error.argtypes = []
@@ -142,6 +163,8 @@ EXPORTS = [
     "randes_layer_offset", "randes_num_layers", "randes_num_tasks", "randes_task_list",
     "randes_task_tables", "randes_plan_serialize", "randes_plan_workspace_needed", "randes_plan_deserialize", "randes_compress", "randes_add_model", "randes_add_models", "randes_remove_model",
     "randes_retrieve", "randes_delta_gram_scratch_bytes", "randes_delta_gram", "randes_interference_norm", "randes_pairwise_cosines", "randes_retrieve_batch", "randes_retrieve_static", "randes_linear", "randes_linear_gated", "randes_linear_giveups", "randes_launch_count", "randes_last_error",
+    "randes_packed_bytes", "randes_pack", "randes_unpack", "randes_retrieve_packed", "randes_packed_linear", "randes_packed_linear_tasks",
+    "randes_token_scores", "randes_token_scores_backward",
 ]
 
 
@@ -304,6 +327,48 @@ def randes_linear_giveups() -> int:
     return int(n.value)
 
 
+def randes_packed_bytes(rows: int, cols: int, group: int) -> int:
+    """Bytes of a [rows, cols] matrix in four bits with scales for groups of `group` columns (0 on bad arguments)."""
+    return int(lib().randes_packed_bytes(rows, cols, group))
+
+
+def randes_pack(matrices, n: int, dtype: int, group: int, packed, stream) -> None:
+    """Pack `n` matrices (a ctypes array of Matrix) into the buffers whose addresses `packed` holds."""
+    _check(lib().randes_pack(_addr(matrices), n, dtype, group, _addr(packed), stream))
+
+
+def randes_unpack(packed, n: int, group: int, matrices, out_dtype: int, stream) -> None:
+    _check(lib().randes_unpack(_addr(packed), n, group, _addr(matrices), out_dtype, stream))
+
+
+def randes_retrieve_packed(plan, task_id, lam, layers, n, base, M, group, packed, stream) -> None:
+    """Pack the retrieved weight of the `n` named layers without storing it in its own type."""
+    _check(lib().randes_retrieve_packed(plan, task_id, lam, _addr(layers), n, _addr(base), _addr(M), group, _addr(packed), stream))
+
+
+def randes_packed_linear(packed, rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, stream) -> None:
+    _check(lib().randes_packed_linear(_addr(packed), rows, cols, group, _addr(x), x_dtype, x_stride, n_tokens, _addr(y), y_dtype, y_stride,
+                                      stream))
+
+
+def randes_packed_linear_tasks(plan, lam, layer, group, task_ids, n_tokens, x, x_dtype, x_stride, packed_base, packed_m, y, y_dtype, y_stride,
+                               stream) -> None:
+    _check(lib().randes_packed_linear_tasks(plan, lam, layer, group, _addr(task_ids), n_tokens, _addr(x), x_dtype, x_stride,
+                                            _addr(packed_base), _addr(packed_m), _addr(y), y_dtype, y_stride, stream))
+
+
+def randes_token_scores(logits, dtype, n_rows, vocab, stride, targets, scale, top_k, logprob, entropy, stats, top_ids, top_logprobs,
+                        stream) -> None:
+    _check(lib().randes_token_scores(_addr(logits), dtype, n_rows, vocab, stride, _addr(targets), scale, top_k, _addr(logprob),
+                                     _addr(entropy), _addr(stats), _addr(top_ids), _addr(top_logprobs), stream))
+
+
+def randes_token_scores_backward(logits, dtype, n_rows, vocab, stride, targets, scale, stats, entropy, g_logprob, g_entropy, grad, grad_stride,
+                                 stream) -> None:
+    _check(lib().randes_token_scores_backward(_addr(logits), dtype, n_rows, vocab, stride, _addr(targets), scale, _addr(stats),
+                                              _addr(entropy), _addr(g_logprob), _addr(g_entropy), _addr(grad), grad_stride, stream))
+
+
 def randes_launch_count() -> int:
     return int(lib().randes_launch_count())
 
@@ -354,6 +419,180 @@ def randes_pairwise_cosines(gram, exclude: int = -1):
     _check(lib().randes_pairwise_cosines(ctypes.addressof(g), n, -1 if exclude is None else int(exclude), ctypes.addressof(cos),
                                          ctypes.byref(mean)))
     return [[float(cos[j * n + l]) for l in range(n)] for j in range(n)], float(mean.value)
+
+
+# ---- weights in four bits and token scores on torch tensors ----------------------------------
+def _refuse(message: str):
+    raise RandesError(INVALID_ARGUMENT, message)
+
+
+def _matrix_dtype(t, what: str) -> int:
+    """Element type of a 2-D CUDA tensor whose rows may be strided; refuses anything the library would misread."""
+    import torch
+
+    code = {torch.float32: F32, torch.bfloat16: BF16}.get(t.dtype)
+    if code is None:
+        raise RandesError(UNSUPPORTED_DTYPE, "%s is %s: float32 or bfloat16 is wanted" % (what, t.dtype))
+    if t.dim() != 2 or not t.is_cuda:
+        _refuse("%s must be a 2-D CUDA tensor" % what)
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        _refuse("%s must have neighbouring columns (its last stride is %d)" % (what, t.stride(1)))
+    return code
+
+
+def _row_stride(t) -> int:
+    s = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if s < 0 or (s < t.shape[1] and t.shape[0] > 1):
+        _refuse("rows overlap (row stride %d, %d columns)" % (s, t.shape[1]))
+    return s
+
+
+def _raw_stream(device) -> int:
+    import torch
+
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+class PackedMatrix:
+    """A [rows, cols] weight in four bits with a scale per group of columns (see include/randes.h): one device buffer."""
+
+    __slots__ = ("rows", "cols", "group", "data", "address")
+
+    def __init__(self, rows: int, cols: int, group: int, data):
+        self.rows, self.cols, self.group, self.data = rows, cols, group, data
+        self.address = data.data_ptr()
+
+    @property
+    def nbytes(self) -> int:
+        return self.data.numel()
+
+    def unpack(self, out_dtype: int = F32, out=None):
+        """The [rows, cols] values that the four bits stand for."""
+        import torch
+
+        if out is None:
+            out = torch.empty(self.rows, self.cols, dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=self.data.device)
+        else:
+            out_dtype = _matrix_dtype(out, "out")
+            if tuple(out.shape) != (self.rows, self.cols):
+                _refuse("out is %s, the matrix [%d, %d]" % (list(out.shape), self.rows, self.cols))
+        randes_unpack((ctypes.c_void_p * 1)(self.address), 1, self.group, (Matrix * 1)(Matrix(out.data_ptr(), self.rows, self.cols, _row_stride(out))),
+                      out_dtype, _raw_stream(out.device))
+        return out
+
+
+def _new_packed(shapes, group: int, device):
+    """PackedMatrix objects for [(rows, cols)]."""
+    import torch
+
+    if group not in (32, 64, 128):
+        _refuse("group = %r is not 32, 64 or 128" % (group,))
+    made = []
+    for r, c in shapes:
+        nbytes = randes_packed_bytes(r, c, group)
+        if nbytes == 0 and r * c != 0:
+            _refuse("a matrix of [%d, %d] cannot be packed" % (r, c))
+        made.append(PackedMatrix(r, c, group, torch.empty(nbytes, dtype=torch.uint8, device=device)))
+    return made
+
+
+def pack(weights, group: int = 64):
+    """Four-bit form of a weight, or of a list of weights of one type (2-D CUDA tensors, fp32 or bf16; rows may be strided)."""
+    if not isinstance(weights, (list, tuple)):
+        return pack([weights], group)[0]
+    if not weights:
+        return []
+    dtypes = {_matrix_dtype(w, "a weight") for w in weights}
+    if len(dtypes) != 1 or len({w.device for w in weights}) != 1:
+        _refuse("the weights of one call have one type and one device")
+    made = _new_packed([tuple(w.shape) for w in weights], group, weights[0].device)
+    n = len(weights)
+    mats = (Matrix * n)(*[Matrix(w.data_ptr(), w.shape[0], w.shape[1], _row_stride(w)) for w in weights])
+    randes_pack(mats, n, dtypes.pop(), group, (ctypes.c_void_p * n)(*[p.address for p in made]), _raw_stream(weights[0].device))
+    return made
+
+
+def _linear_output(x, rows: int, cols: int, y, y_dtype: int):
+    """(y, x's type, y's type) of a product of x [n_tokens, cols] with a [rows, cols] weight."""
+    import torch
+
+    x_dtype = _matrix_dtype(x, "x")
+    if x.shape[1] != cols:
+        _refuse("x has %d columns, the weight %d" % (x.shape[1], cols))
+    if y is None:
+        return torch.empty((x.shape[0], rows), dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=x.device), x_dtype, y_dtype
+    y_dtype = _matrix_dtype(y, "y")
+    if tuple(y.shape) != (x.shape[0], rows) or y.device != x.device:
+        _refuse("y is %s on %s, [%d, %d] on %s is wanted" % (list(y.shape), y.device, x.shape[0], rows, x.device))
+    return y, x_dtype, y_dtype
+
+
+def packed_linear(x, w: PackedMatrix, y=None, y_dtype: int = F32):
+    """x: [n_tokens, cols] fp32 or bf16 CUDA tensor (rows may be strided); returns y = x W^T [n_tokens, rows]."""
+    y, x_dtype, y_dtype = _linear_output(x, w.rows, w.cols, y, y_dtype)
+    randes_packed_linear(w.address, w.rows, w.cols, w.group, x, x_dtype, _row_stride(x), x.shape[0], y, y_dtype, _row_stride(y),
+                         _raw_stream(x.device))
+    return y
+
+
+class TokenScores(NamedTuple):
+    """What token_scores returns; `stats` is what the backward call needs (row 0: greatest logit, row 1: log sum above it)."""
+
+    logprob: Any
+    entropy: Any
+    stats: Any
+    top_ids: Any
+    top_logprobs: Any
+
+
+def _check_targets(targets, n: int, device):
+    import torch
+
+    if targets is not None and (targets.dtype != torch.int64 or tuple(targets.shape) != (n,) or not targets.is_contiguous() or targets.device != device):
+        _refuse("targets must be a contiguous int64 tensor [%d] on %s" % (n, device))
+
+
+def token_scores(logits, targets=None, top_k: int = 0, scale: float = 1.0) -> TokenScores:
+    """Log probability of `targets`, entropy, and the `top_k` best tokens of every row of logits * scale (see include/randes.h).
+
+    logits: [n, vocab] fp32 or bf16 CUDA tensor (rows may be strided); targets: int64 [n], negative = not scored."""
+    import torch
+
+    dtype = _matrix_dtype(logits, "logits")
+    n, vocab = logits.shape
+    _check_targets(targets, n, logits.device)
+    if not 0 <= top_k <= 64:
+        _refuse("top_k = %d is not in 0 .. 64" % top_k)
+    sums = torch.empty((4, n), dtype=torch.float32, device=logits.device)
+    at = sums.data_ptr()
+    ids = tops = None
+    if top_k:
+        ids = torch.empty((n, top_k), dtype=torch.int64, device=logits.device)
+        tops = torch.empty((n, top_k), dtype=torch.float32, device=logits.device)
+    randes_token_scores(logits, dtype, n, vocab, _row_stride(logits), targets, scale, top_k, at if targets is not None else None, at + 4 * n,
+                        at + 8 * n, ids, tops, _raw_stream(logits.device))
+    return TokenScores(sums[0] if targets is not None else None, sums[1], sums[2:], ids, tops)
+
+
+def token_scores_backward(logits, targets, scores: TokenScores, g_logprob=None, g_entropy=None, scale: float = 1.0, out=None):
+    """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect to the logits; `out` may be the logits themselves."""
+    import torch
+
+    dtype = _matrix_dtype(logits, "logits")
+    n, vocab = logits.shape
+    _check_targets(targets, n, logits.device)
+    for g, what in ((g_logprob, "g_logprob"), (g_entropy, "g_entropy"), (scores.entropy, "entropy")):
+        if g is not None and (g.dtype != torch.float32 or tuple(g.shape) != (n,) or not g.is_contiguous() or g.device != logits.device):
+            _refuse("%s must be a contiguous float32 tensor [%d] on %s" % (what, n, logits.device))
+    if tuple(scores.stats.shape) != (2, n) or not scores.stats.is_contiguous():
+        _refuse("stats are not those of %d rows" % n)
+    if out is None:
+        out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+    elif _matrix_dtype(out, "out") != dtype or out.shape != logits.shape or out.device != logits.device:
+        _refuse("out must have the logits' shape, type and device")
+    randes_token_scores_backward(logits, dtype, n, vocab, _row_stride(logits), targets, scale, scores.stats, scores.entropy, g_logprob, g_entropy,
+                                 out, _row_stride(out), _raw_stream(logits.device))
+    return out
 
 
 # ---- convenience object over torch tensors --------------------------------------------------
@@ -520,3 +759,59 @@ class Plan:
             out_list = out
         randes_retrieve(self.handle, task_id, lam, out_dtype, _as_ptrs(base), M, _as_ptrs(out), self._stream())
         return out_list
+
+    # -- four-bit weights (see PackedMatrix)
+    def _layer(self, layer) -> int:
+        if not 0 <= int(layer) < self.n_layers:
+            _refuse("layer %d out of range (n_layers = %d)" % (int(layer), self.n_layers))
+        return int(layer)
+
+    def pack_superposition(self, M, group: int = 64, slots=None):
+        """Four-bit form of the slots of M, a list by slot (None for slots not named)."""
+        slots = list(range(self.n_layers)) if slots is None else [self._layer(l) for l in slots]
+        made = pack([self.slot(M, l) for l in slots], group)
+        out = [None] * self.n_layers
+        for l, p in zip(slots, made):
+            out[l] = p
+        return out
+
+    def retrieve_packed(self, task_id: int, lam: float, base, M, group: int = 64, layers=None):
+        """Four-bit form of one retrieved model, its own type never stored; a list, one entry per named layer (default: all).
+
+        ``base`` is the list of all layers' weights; only the named ones are read."""
+        layers = list(range(self.n_layers)) if layers is None else [self._layer(l) for l in layers]
+        n = len(layers)
+        made = _new_packed([(self.rows[l], self.cols[l]) for l in layers], group, self.device)
+        randes_retrieve_packed(self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, _as_ptrs(base), M, group,
+                               (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]), self._stream())
+        return made
+
+    def packed_linear(self, task_ids, lam: float, layer: int, x, packed_base: PackedMatrix, packed_m, y=None, y_dtype: int = F32):
+        """One layer applied to a few tokens, token b with the retrieved weight of task_ids[b].
+
+        ``packed_base`` is the layer's W_0, ``packed_m`` the slots of M by slot (pack_superposition), all packed with one
+        group size; x: [n_tokens, cols] fp32 or bf16; returns y [n_tokens, rows]."""
+        layer = self._layer(layer)
+        rows, cols, group = self.rows[layer], self.cols[layer], packed_base.group
+        if (packed_base.rows, packed_base.cols) != (rows, cols):
+            _refuse("packed_base is [%d, %d], layer %d is [%d, %d]" % (packed_base.rows, packed_base.cols, layer, rows, cols))
+        if not isinstance(packed_m, ctypes.Array):
+            if len(packed_m) != self.n_layers:
+                _refuse("packed_m has %d entries, the plan %d slots" % (len(packed_m), self.n_layers))
+            slots = (ctypes.c_void_p * max(self.n_layers, 1))()
+            for l, p in enumerate(packed_m):
+                if p is None or (p.rows, p.cols) != (rows, cols):
+                    continue      # not a slot this layer can lie in
+                if p.group != group:
+                    _refuse("slot %d has groups of %d columns, the base of %d" % (l, p.group, group))
+                slots[l] = p.address
+            packed_m = slots
+        y, x_dtype, y_dtype = _linear_output(x, rows, cols, y, y_dtype)
+        n = x.shape[0]
+        if len(task_ids) != n:
+            _refuse("%d task ids for %d tokens" % (len(task_ids), n))
+        if not isinstance(task_ids, ctypes.Array):
+            task_ids = (ctypes.c_uint32 * max(n, 1))(*task_ids)
+        randes_packed_linear_tasks(self.handle, lam, layer, group, task_ids, n, x, x_dtype, _row_stride(x), packed_base.address, packed_m, y,
+                                   y_dtype, _row_stride(y), self._stream())
+        return y
