@@ -1316,8 +1316,11 @@ int randes_linear_gated(const randes_plan_t* plan, uint32_t task_id, float lambd
 int randes_linear_giveups(unsigned int* count)
 {
     if (!count) return fail(RANDES_INVALID_ARGUMENT, "count is NULL");
-    const int e = linear_giveups(count);
+    unsigned int packed = 0;
+    int e = linear_giveups(count);
+    if (!e) e = packed_giveups(&packed);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "read of the give-up counter");
+    *count += packed;
     return RANDES_OK;
 }
 
@@ -1536,18 +1539,18 @@ bool rows_aligned(const void* p, uint64_t rows, uint64_t stride, size_t elem)
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (stride * elem) % 16 == 0);
 }
 
-int current_sm_count(int* sms)
+struct Device { int index, sms; };
+
+int current_device(Device* d)
 {
     static std::atomic<int> known[64];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess && dev < 64 && known[dev].load(std::memory_order_relaxed)) {
-        *sms = known[dev].load(std::memory_order_relaxed);
-        return RANDES_OK;
-    }
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+    cudaError_t e = cudaGetDevice(&d->index);
     if (e != cudaSuccess) return fail_cuda(e, "query of the current device");
-    if (dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
+    d->sms = d->index < 64 ? known[d->index].load(std::memory_order_relaxed) : 0;
+    if (d->sms) return RANDES_OK;
+    e = cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, d->index);
+    if (e != cudaSuccess) return fail_cuda(e, "query of the current device");
+    if (d->index < 64) known[d->index].store(d->sms, std::memory_order_relaxed);
     return RANDES_OK;
 }
 
@@ -1685,8 +1688,8 @@ int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, i
     if ((n_tokens == 1 || (x_stride == cols && y_stride == rows)) &&
         overlap(x, span_bytes(n_tokens, cols, x_stride, xe), y, span_bytes(n_tokens, rows, y_stride, ye)))
         return fail(RANDES_INVALID_ARGUMENT, "y overlaps x");
-    int sms = 0;
-    if ((rc = current_sm_count(&sms))) return rc;
+    Device dev;
+    if ((rc = current_device(&dev))) return rc;
     PackedLinearArgs a;
     a.x_stride = x_stride;
     a.y_stride = y_stride;
@@ -1701,7 +1704,7 @@ int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, i
         a.y = static_cast<char*>(y) + first * y_stride * ye;
         a.n_tokens = std::min(kPackedTokens, n_tokens - first);
         fill(a, first);
-        const int e = launch_packed_linear(a, x_dtype == RANDES_BF16, sms, stream);
+        const int e = launch_packed_linear(a, x_dtype == RANDES_BF16, dev.sms, dev.index, stream);
         if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the packed linear kernel");
         ++g_launches;
     }
@@ -1814,10 +1817,10 @@ int randes_token_scores_impl(const void* logits, randes_dtype_t dtype, uint32_t 
     if ((reinterpret_cast<uintptr_t>(logprob) | reinterpret_cast<uintptr_t>(entropy) | reinterpret_cast<uintptr_t>(stats) |
          reinterpret_cast<uintptr_t>(top_logprobs)) % 4 || reinterpret_cast<uintptr_t>(top_ids) % 8)
         return fail(RANDES_MISALIGNED, "an output is not aligned to its element size");
-    int sms = 0;
-    if ((rc = current_sm_count(&sms))) return rc;
+    Device dev;
+    if ((rc = current_device(&dev))) return rc;
     const ScoreArgs a{logits, targets, stride, n_rows, vocab, top_k, scale, logprob, entropy, stats, top_ids, top_logprobs};
-    const int e = launch_scores(dtype, a, sms, stream);
+    const int e = launch_scores(dtype, a, dev.sms, stream);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the token score kernel");
     ++g_launches;
     return RANDES_OK;
@@ -1854,7 +1857,7 @@ extern "C" {
 size_t randes_packed_bytes(uint32_t rows, uint32_t cols, uint32_t group)
 {
     if ((group != 32 && group != 64 && group != 128) || rows == 0 || cols == 0 || static_cast<uint64_t>(rows) * cols > 0xFFFFFFFFull) return 0;
-    return packed_codes_bytes(rows, cols) + (static_cast<size_t>(rows) + 15) / 16 * packed_groups(cols, group) * 32;
+    return PackedLayout(rows, cols, group).total;
 }
 
 int randes_pack(const randes_matrix_t* w, uint32_t n, randes_dtype_t dtype, uint32_t group, void* const* packed, void* stream)

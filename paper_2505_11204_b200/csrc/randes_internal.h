@@ -210,16 +210,27 @@ int linear_giveups(unsigned int* count);   // CTAs that gave up on a bounded wai
 
 // randes_packed.cu: weights in four bits with group scales (the layout is described there).
 #ifdef __CUDACC__
-__host__ __device__
+#define RANDES_BOTH __host__ __device__
+#else
+#define RANDES_BOTH
 #endif
-constexpr size_t packed_codes_bytes(uint32_t rows, uint32_t cols)
-{
-    return ((static_cast<size_t>(rows) + 15) / 16) * ((static_cast<size_t>(cols) + 63) / 64) * 512;
-}
-#ifdef __CUDACC__
-__host__ __device__
-#endif
-inline uint32_t packed_groups(uint32_t cols, uint32_t group) { return cols / group + (cols % group ? 1u : 0u); }
+struct PackedLayout {
+    uint32_t tiles, record, col_blocks, quarters;     // per record: column tiles, bytes; records per row block; 32-column quarters per group
+    size_t total;
+    RANDES_BOTH PackedLayout(uint32_t rows, uint32_t cols, uint32_t group)
+    {
+        tiles = group == 128 ? 2 : 1;
+        record = tiles * 2048 + (group == 32 ? 256 : 128);
+        col_blocks = cols / (64 * tiles) + (cols % (64 * tiles) ? 1 : 0);
+        quarters = group / 32;
+        total = (static_cast<size_t>(rows) + 63) / 64 * col_blocks * record;
+    }
+    // byte offsets of row tile rt (16 rows): codes of column tile kt (64 columns), scales of the group that holds 32-column quarter q
+    RANDES_BOTH size_t at(uint32_t rt, uint32_t kt) const { return (static_cast<size_t>(rt / 4) * col_blocks + kt / tiles) * record; }
+    RANDES_BOTH size_t codes(uint32_t rt, uint32_t kt) const { return at(rt, kt) + (kt % tiles * 4 + rt % 4) * 512; }
+    RANDES_BOTH size_t scales(uint32_t rt, uint32_t q) const { return at(rt, q / 2) + tiles * 2048 + ((q % (2 * tiles)) / quarters * 4 + rt % 4) * 32; }
+    RANDES_BOTH bool has_tile(uint32_t kt) const { return kt < col_blocks * tiles; }
+};
 constexpr uint32_t kPackBatch = 32;       // matrices per launch of pack and unpack
 struct PackMatrix {
     const void* src;              // weight (retrieve: W_0)
@@ -247,7 +258,7 @@ struct UnpackArgs {
     UnpackMatrix mat[kPackBatch];
     uint32_t n, group;
 };
-constexpr uint32_t kPackedTokens = 64;    // tokens per launch of the product
+constexpr uint32_t kPackedTokens = 8;    // tokens per launch of the product
 // One packed matrix and the tokens that go through it: positions first .. first + count - 1 of the token lists.
 struct PackedSegment {
     const void* packed;
@@ -258,7 +269,9 @@ struct PackedLinearArgs {
     void* y;
     uint64_t x_stride, y_stride;  // elements between tokens
     uint32_t rows, cols, group, n_tokens;
-    uint32_t n_seg, split;        // split: set by the launcher
+    uint32_t n_seg;
+    uint32_t log_split, log_ranks;               // set by the launcher: warps of a CTA and CTAs of a cluster that share rows
+    uint32_t ring_at;                            // and where the rings start in shared memory
     uint32_t x_vec, y_bf16;
     float lambda;
     uint8_t token[2 * kPackedTokens];        // per position: the token
@@ -270,7 +283,8 @@ struct PackedLinearArgs {
 // All return a cudaError_t as int.
 int launch_pack(int w_dtype, int m_dtype, bool retrieve, PackArgs& a, void* stream);
 int launch_unpack(int out_dtype, UnpackArgs& a, void* stream);
-int launch_packed_linear(PackedLinearArgs& a, bool x_bf16, int sm_count, void* stream);
+int packed_giveups(unsigned int* count);   // warps of the product that gave up on a bounded wait (synchronises)
+int launch_packed_linear(PackedLinearArgs& a, bool x_bf16, int sm_count, int device, void* stream);
 
 // randes_scores.cu: log probabilities, entropy and top alternatives of logits, and their gradient.
 constexpr uint32_t kMaxTop = 64;

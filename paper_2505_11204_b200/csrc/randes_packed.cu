@@ -9,21 +9,32 @@
 // and q is taken against the rounded scale, so the rounding costs no accuracy of its own. The clamp of the definition
 // never acts for the reason given above.
 //
-// Layout: tiles of 16 rows x 64 columns, 512 bytes = 16 bytes per lane, ordered [row tile][column tile][lane], so that
-// one 16-byte load per lane brings the A operands of four m16n8k16 products in the order the tensor core wants them.
+// Layout: records of 64 rows x 64 columns (128 columns for groups of 128), [row block][column block], each
+//     codes   [tile of 64 columns][row tile of 16][lane] 16 bytes
+//     scales  [group][row tile][lane / 4] one word: rows g (low half) and g + 8 (high half) of the row tile
+// so that the columns one warp works through are one contiguous run of memory -- one bulk copy per stage -- and one
+// 16-byte load per lane brings the A operands of four m16n8k16 products in the order the tensor core wants them.
 // Lane (g = lane / 4, t = lane % 4) holds rows g and g + 8. Its 32-bit word j holds the four columns
 //     c(j, e) = 32 (j / 2) + 8 t + 4 (j % 2) + e,    e = 0 .. 3
 // of both rows, code + 8 in nibble order (g,0) (g+8,0) (g,2) (g+8,2) (g,1) (g+8,1) (g,3) (g+8,3): shifting the word by
 // 4 i and masking with 0x000F000F leaves operand register i. The columns a lane owns are 8 neighbours in each half of
-// the tile, so that the activations it multiplies are two 16-byte loads. After the codes come the scales,
-// [row tile][group][g], one word per lane row: rows g (low half) and g + 8 (high half).
+// the tile, so that the activations it multiplies are two 16-byte loads.
 #include <cuda_bf16.h>
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
+
+#include <atomic>
+#include <cstring>
 
 #include "randes_device.cuh"
 #include "randes_internal.h"
 
+namespace cg = cooperative_groups;
+
 namespace randes {
+
+static __device__ unsigned int g_packed_giveups;   // warps that gave up waiting for a copy (0 in a healthy run)
+
 namespace {
 
 using namespace device;
@@ -41,27 +52,54 @@ __device__ __forceinline__ float quotient(float w, float s, float inv)
     return __fmaf_rn(__fmaf_rn(-q, s, w), inv, q);
 }
 
-// eight neighbouring columns of one row, zero beyond the row's end
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, uint32_t c, uint32_t cols, bool vec, float (&v)[8])
+// The four operand registers of one word of codes, as q / 64. A code left in the low byte of a bf16 is a number too: bf16
+// counts in steps of 2^-133 through its whole first two binades, so bits 0-3 read u 2^-133 and bits 4-7 read 16 u 2^-133
+// (u = q + 8). One exact multiply-add brings either to u / 64 - 1/8. So a word takes one shift instead of three, and no
+// bias has to be put in. Parts of 1/64, not units: a product with an activation cannot overflow where the weight itself
+// (q s, with s << 1) would not; the factor comes back with the partial sums.
+constexpr float kCodeUnit = 64.f;
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c)
 {
-    if (vec && c + 8 <= cols) {
-        if (sizeof(T) == 4) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ void decode(uint32_t word, uint32_t (&a)[4])
+{
+    constexpr uint32_t k127 = 0x7F007F00u, k123 = 0x7D007D00u, kOff = 0xBE00BE00u;    // 2^127, 2^123, -1/8, twice each
+    const uint32_t high = word >> 8;
+    a[0] = fma_bf16x2(word & 0x000F000Fu, k127, kOff);
+    a[1] = fma_bf16x2(word & 0x00F000F0u, k123, kOff);
+    a[2] = fma_bf16x2(high & 0x000F000Fu, k127, kOff);
+    a[3] = fma_bf16x2(high & 0x00F000F0u, k123, kOff);
+}
+
+// Eight neighbouring columns of one row as they lie in memory.
+template <typename T> struct Eight { uint4 w[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ Eight<T> load8(const T* p)
+{
+    Eight<T> v;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint4 r = __ldcs(reinterpret_cast<const uint4*>(row + c) + h);
-                v[4 * h] = __uint_as_float(r.x); v[4 * h + 1] = __uint_as_float(r.y);
-                v[4 * h + 2] = __uint_as_float(r.z); v[4 * h + 3] = __uint_as_float(r.w);
-            }
-        } else {
-            float u[Store<T>::CPL];
-            Store<T>::widen(__ldcs(reinterpret_cast<const uint4*>(row + c)), u);
+    for (int h = 0; h < static_cast<int>(sizeof(T)) / 2; ++h) v.w[h] = __ldcs(reinterpret_cast<const uint4*>(p) + h);
+    return v;
+}
+template <typename T> __device__ __noinline__ Eight<T> gather8(const T* row, uint32_t c, uint32_t cols)      // zero beyond the row's end
+{
+    Eight<T> v;
+    T e[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = u[e % Store<T>::CPL];
-        }
-    } else {
+    for (int k = 0; k < 8; ++k) e[k] = c + k < cols ? row[c + k] : T(0.f);
+    memcpy(&v, e, sizeof v);
+    return v;
+}
+template <typename T> __device__ __forceinline__ void widen8(const Eight<T>& r, float (&v)[8])
+{
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? Store<T>::load1(row + c + e) : 0.f;
+    for (int h = 0; h < static_cast<int>(sizeof(T)) / 2; ++h) {
+        float u[Store<T>::CPL];
+        Store<T>::widen(r.w[h], u);
+#pragma unroll
+        for (int e = 0; e < Store<T>::CPL; ++e) v[h * Store<T>::CPL + e] = u[e];
     }
 }
 
@@ -71,112 +109,143 @@ template <typename Args> __device__ __forceinline__ bool find_unit(const Args& a
     uint32_t m = 0;
     while (m + 1 < a.n && blockIdx.x >= a.mat[m + 1].first_cta) ++m;
     which = m;
-    const uint32_t kus = (a.mat[m].cols + 127) / 128;
-    const uint64_t u = static_cast<uint64_t>(blockIdx.x - a.mat[m].first_cta) * kPackWarps + (threadIdx.x >> 5);
-    if (u >= static_cast<uint64_t>((a.mat[m].rows + 15) / 16) * kus) return false;
-    rt = static_cast<uint32_t>(u / kus);
-    ku = static_cast<uint32_t>(u % kus);
-    return true;
+    const uint32_t kus = (a.mat[m].cols + 127) / 128, tiles = (a.mat[m].rows + 63) / 64 * 4;     // fewer than 2^32 units: a matrix has fewer elements
+    const uint32_t u = (blockIdx.x - a.mat[m].first_cta) * kPackWarps + (threadIdx.x >> 5);
+    rt = u / kus;
+    ku = u - rt * kus;
+    return rt < tiles;
+}
+
+__device__ __forceinline__ float max3_abs_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Bits of the greatest magnitude of eight columns and of those of the neighbouring lanes (32 columns): compared as whole
+// numbers between lanes, so that a NaN is the greatest.
+__device__ __forceinline__ uint32_t top_of_lanes(uint32_t x)
+{
+    x = umax(x, __shfl_xor_sync(~0u, x, 1));
+    return umax(x, __shfl_xor_sync(~0u, x, 2));
+}
+__device__ __forceinline__ uint32_t top_of(const float (&v)[8])
+{
+    const float m = max3_abs_nan(max3_abs_nan(v[0], v[1], v[2]), max3_abs_nan(v[3], v[4], v[5]), max3_abs_nan(v[6], v[7], 0.f));
+    return top_of_lanes(__float_as_uint(m) & 0x7FFFFFFFu);
+}
+__device__ __forceinline__ uint32_t top_of(const uint4& w)        // bf16 pairs
+{
+    constexpr uint32_t kAbs = 0x7FFF7FFFu;
+    const uint32_t m = max2_nan(max2_nan(w.x & kAbs, w.y & kAbs), max2_nan(w.z & kAbs, w.w & kAbs));
+    return top_of_lanes(umax(m << 16, m & 0xFFFF0000u));
 }
 
 // One warp turns 16 rows x 128 columns into two tiles. RETRIEVE: the weight is fma(lambda, s * M, W_0) with the sign
 // bits of the unit's 128 columns out of one Philox block -- the value retrieve writes in fp32, never stored.
 template <typename WT, typename MT, bool RETRIEVE>
-__global__ void __launch_bounds__(kPackWarps * 32) pack_kernel(const __grid_constant__ PackArgs a)
+__global__ void __launch_bounds__(kPackWarps * 32, 3) pack_kernel(const __grid_constant__ PackArgs a)
 {
     uint32_t which, rt, ku;
     if (!find_unit(a, which, rt, ku)) return;
     const PackMatrix& m = a.mat[which];
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const WT* w = static_cast<const WT*>(m.src);
-    const MT* sup = static_cast<const MT*>(m.m);
-    const bool vec_w = m.vec & 1u, vec_m = m.vec & 2u;
     const uint32_t cols = m.cols, c0 = ku * 128 + 8 * t;
+    const bool whole = ku * 128 + 128 <= cols && rt * 16 + 16 <= m.rows;       // the unit lies inside the matrix
+    const int per = a.group >> 5;     // 32-column quarters per group: 1, 2 or 4
 
     uint4 blk = make_uint4(0, 0, 0, 0);
     if (RETRIEVE && m.flip) blk = philox4x32_10(ku, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1);
-    float v[2][4][8];      // [row g / g + 8][32-column quarter][column]
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t r = rt * 16 + h * 8 + g;
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            if (r < m.rows) {
-                load8<WT>(w + r * m.stride, c0 + 32 * p, cols, vec_w, v[h][p]);
-                if (RETRIEVE) {
-                    float d[8];
-                    load8<MT>(sup + static_cast<size_t>(r) * cols, c0 + 32 * p, cols, vec_m, d);
-                    const uint32_t word = p == 0 ? blk.x : (p == 1 ? blk.y : (p == 2 ? blk.z : blk.w));
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[h][p][e] = __fmaf_rn(a.lambda, flip(d[e], (word >> (8 * t + e)) << 31), v[h][p][e]);
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[h][p][e] = 0.f;
-            }
-        }
-    }
-    uint32_t top[2][4];    // bits of the greatest magnitude per quarter: as integers, so that a NaN is the greatest
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            uint32_t x = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x = umax(x, __float_as_uint(v[h][p][e]) & 0x7FFFFFFFu);
-            x = umax(x, __shfl_xor_sync(~0u, x, 1));
-            top[h][p] = umax(x, __shfl_xor_sync(~0u, x, 2));
-        }
-    const int per = a.group >> 5;     // quarters per group: 1, 2 or 4
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (per >= 2) {
-            top[h][0] = top[h][1] = umax(top[h][0], top[h][1]);
-            top[h][2] = top[h][3] = umax(top[h][2], top[h][3]);
-        }
-        if (per == 4) top[h][0] = top[h][1] = top[h][2] = top[h][3] = umax(top[h][0], top[h][2]);
-    }
-    uint32_t scale_bits[2][4];
+    uint32_t scale_bits[2];           // of quarter t
+    // A word of codes is sum_i (q_i + 8) 16^i. Adding 1.5 * 2^23 to a quotient rounds it to the nearest integer (ties to
+    // even) and leaves kRound + q in its bits, so one integer multiply-add per code puts it in place; what the constants
+    // add up to is known beforehand.
+    constexpr uint32_t kRound = 0x4B400000u;
     uint32_t word[4][2];              // [quarter][word of the quarter]
 #pragma unroll
-    for (int p = 0; p < 4; ++p) word[p][0] = word[p][1] = 0;
+    for (int p = 0; p < 4; ++p) word[p][0] = word[p][1] = 0x88888888u - kRound * 0x11111111u;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {     // row g, row g + 8
+        const uint32_t r = rt * 16 + h * 8 + g;
+        const WT* w = static_cast<const WT*>(m.src) + r * m.stride;
+        const MT* sup = static_cast<const MT*>(m.m) + static_cast<size_t>(r) * cols;
+        Eight<WT> raw[4];
+        Eight<MT> add[4];
+        if (whole && (m.vec & 1u)) {
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
-            const bool finite = top[h][p] < 0x7F800000u;
-            const float s7 = __fdiv_rn(__uint_as_float(top[h][p]), 7.f);
-            const uint32_t sb = __bfloat16_as_ushort(__float2bfloat16_rn(s7));
-            float s = __uint_as_float(sb << 16);
-            if (!(s >= kMinScale)) s = 0.f;
-            scale_bits[h][p] = finite ? __float_as_uint(s) >> 16 : 0x7FC0u;
-            const float inv = finite && s > 0.f ? __frcp_rn(s) : 0.f;
-            // a group that is all NaN or all zero keeps code 0: its values are cleared here, not in the quotient
-            const bool live = inv != 0.f;
+            for (int p = 0; p < 4; ++p) raw[p] = load8<WT>(w + c0 + 32 * p);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float q = live ? quotient(v[h][p][e], s, inv) : 0.f;
-                // adding 1.5 * 2^23 rounds to the nearest integer (ties to even) and leaves it in the low bits
-                const uint32_t code = __float_as_uint(q + (12582912.f + 8.f)) & 15u;
-                // nibble of (row half h, column e % 4) in word e / 4: see the layout above
-                const int pos = ((e >> 1) & 1) * 2 + h + (e & 1) * 4;
-                word[p][e >> 2] |= code << (4 * pos);
+            for (int p = 0; p < 4; ++p) raw[p] = gather8<WT>(w, c0 + 32 * p, r < m.rows ? cols : 0u);
+        }
+        if (RETRIEVE) {
+            if (whole && (m.vec & 2u)) {
+#pragma unroll
+                for (int p = 0; p < 4; ++p) add[p] = load8<MT>(sup + c0 + 32 * p);
+            } else {
+#pragma unroll
+                for (int p = 0; p < 4; ++p) add[p] = gather8<MT>(sup, c0 + 32 * p, r < m.rows ? cols : 0u);
             }
         }
-    const uint32_t kts = (cols + 63) / 64, n_groups = packed_groups(cols, a.group);
-    uint4* codes = static_cast<uint4*>(m.dst) + (static_cast<size_t>(rt) * kts + 2 * ku) * 32 + lane;
-    codes[0] = make_uint4(word[0][0], word[0][1], word[1][0], word[1][1]);
-    if (2 * ku + 1 < kts) codes[32] = make_uint4(word[2][0], word[2][1], word[3][0], word[3][1]);
-    uint32_t* scales = reinterpret_cast<uint32_t*>(static_cast<char*>(m.dst) + packed_codes_bytes(m.rows, cols)) +
-                       static_cast<size_t>(rt) * n_groups * 8;
-    if (t == 0) {
+        float v[4][8];
+        uint32_t top[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const uint32_t grp = ku * (4 / per) + p / per;
-            if (p % per == 0 && grp < n_groups) scales[static_cast<size_t>(grp) * 8 + g] = scale_bits[0][p] | (scale_bits[1][p] << 16);
+            if (sizeof(WT) == 2 && !RETRIEVE) {
+                top[p] = top_of(raw[p].w[0]);            // widened below, where it is divided
+            } else {
+                widen8<WT>(raw[p], v[p]);
+                if (RETRIEVE) {
+                    float d[8];
+                    widen8<MT>(add[p], d);
+                    const uint32_t bits = p == 0 ? blk.x : (p == 1 ? blk.y : (p == 2 ? blk.z : blk.w));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[p][e] = __fmaf_rn(a.lambda, flip(d[e], (bits >> (8 * t + e)) << 31), v[p][e]);
+                }
+                top[p] = top_of(v[p]);
+            }
+        }
+        if (per >= 2) {
+            top[0] = top[1] = umax(top[0], top[1]);
+            top[2] = top[3] = umax(top[2], top[3]);
+        }
+        if (per == 4) top[0] = top[1] = top[2] = top[3] = umax(top[0], top[2]);
+        // The four lanes of a row share the divisions: lane t makes the scale of quarter t.
+        const uint32_t mine = t == 0 ? top[0] : (t == 1 ? top[1] : (t == 2 ? top[2] : top[3]));
+        const bool finite = mine < 0x7F800000u;
+        float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__uint_as_float(mine), 7.f)));
+        if (!(finite && s >= kMinScale)) s = 0.f;             // too small for a scale (or not a number): code 0
+        const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
+        scale_bits[h] = finite ? __float_as_uint(s) >> 16 : 0x7FC0u;
+        const bool spoilt = __any_sync(~0u, !finite);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const float sp = __shfl_sync(~0u, s, (lane & ~3) | p), ip = __shfl_sync(~0u, inv, (lane & ~3) | p);
+            if (sizeof(WT) == 2 && !RETRIEVE) widen8<WT>(raw[p], v[p]);
+            if (spoilt && sp == 0.f) {                        // a NaN would reach the other row's codes
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[p][e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int pos = ((e >> 1) & 1) * 2 + h + (e & 1) * 4;      // nibble of (row half, column): see the layout above
+                word[p][e >> 2] += __float_as_uint(quotient(v[p][e], sp, ip) + __uint_as_float(kRound)) * (1u << (4 * pos));
+            }
         }
     }
+    const PackedLayout lay(m.rows, cols, a.group);
+    char* dst = static_cast<char*>(m.dst);
+    *reinterpret_cast<uint4*>(dst + lay.codes(rt, 2 * ku) + lane * 16) = make_uint4(word[0][0], word[0][1], word[1][0], word[1][1]);
+    if (lay.has_tile(2 * ku + 1))
+        *reinterpret_cast<uint4*>(dst + lay.codes(rt, 2 * ku + 1) + lane * 16) = make_uint4(word[2][0], word[2][1], word[3][0], word[3][1]);
+    if (t % per == 0 && lay.has_tile(2 * ku + t / 2))
+        *reinterpret_cast<uint32_t*>(dst + lay.scales(rt, 4 * ku + t) + g * 4) = scale_bits[0] | (scale_bits[1] << 16);
 }
 
 template <typename OT> __device__ __forceinline__ void store8(OT* row, uint32_t c, uint32_t cols, bool vec, const float (&v)[8])
@@ -197,21 +266,21 @@ template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack
     if (!find_unit(a, which, rt, ku)) return;
     const UnpackMatrix& m = a.mat[which];
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const uint32_t cols = m.cols, kts = (cols + 63) / 64, n_groups = packed_groups(cols, a.group);
-    const uint4* codes = static_cast<const uint4*>(m.src) + (static_cast<size_t>(rt) * kts + 2 * ku) * 32 + lane;
+    const uint32_t cols = m.cols;
+    const PackedLayout lay(m.rows, cols, a.group);
+    const char* src = static_cast<const char*>(m.src);
     uint4 w[2];
-    w[0] = __ldcs(codes);
-    w[1] = 2 * ku + 1 < kts ? __ldcs(codes + 32) : make_uint4(0, 0, 0, 0);
-    const uint32_t* scales = reinterpret_cast<const uint32_t*>(static_cast<const char*>(m.src) + packed_codes_bytes(m.rows, cols)) +
-                             static_cast<size_t>(rt) * n_groups * 8;
-    const int per = a.group >> 5;
+    w[0] = __ldcs(reinterpret_cast<const uint4*>(src + lay.codes(rt, 2 * ku) + lane * 16));
+    w[1] = lay.has_tile(2 * ku + 1) ? __ldcs(reinterpret_cast<const uint4*>(src + lay.codes(rt, 2 * ku + 1) + lane * 16)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const uint32_t grp = ku * (4 / per) + p / per;
         const uint32_t c = ku * 128 + 32 * p + 8 * t;
-        if (grp >= n_groups || c >= cols) continue;
-        const uint32_t sb = __ldg(scales + static_cast<size_t>(grp) * 8 + g);
+        if (c >= cols) continue;
+        const uint32_t sb = __ldg(reinterpret_cast<const uint32_t*>(src + lay.scales(rt, 4 * ku + p) + g * 4));
         const uint32_t words[2] = {p & 1 ? w[p >> 1].z : w[p >> 1].x, p & 1 ? w[p >> 1].w : w[p >> 1].y};
+        uint32_t q[2][4];                // operand registers of the two words: [i] holds row half i % 2, column pair i / 2
+        decode(words[0], q[0]);
+        decode(words[1], q[1]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint32_t r = rt * 16 + h * 8 + g;
@@ -220,8 +289,8 @@ template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int pos = ((e >> 1) & 1) * 2 + h + (e & 1) * 4;
-                v[e] = (static_cast<float>((words[e >> 2] >> (4 * pos)) & 15u) - 8.f) * s;
+                const uint32_t pair = q[e >> 2][((e >> 1) & 1) * 2 + h];
+                v[e] = kCodeUnit * __uint_as_float(e & 1 ? pair & 0xFFFF0000u : pair << 16) * s;
             }
             store8<OT>(static_cast<OT*>(m.dst) + r * m.stride, c, cols, m.vec, v);
         }
@@ -230,248 +299,376 @@ template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack
 
 // ---- products with a few tokens -----------------------------------------------------------------
 constexpr int kMulWarps = 8;
+constexpr int kDevices = 64;
+
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-
-// Operand register i of one word of codes, as q / 16. 0x4100 is 8 in bf16 with a last place of 1/16, so the nibble dropped
-// into its mantissa reads 8 + (q + 8) / 16; taking 8.5 away is exact. Sixteenths, not units: a product with an activation
-// then cannot overflow where the weight itself (q * s, s << 1) would not; the factor comes back with the partial sums.
-constexpr float kCodeUnit = 16.f;
-__device__ __forceinline__ uint32_t decode2(uint32_t word, int i)
+__device__ __forceinline__ void mma_16816_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    const uint32_t biased = ((word >> (4 * i)) & 0x000F000Fu) | 0x41004100u;
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(biased), "r"(0x41084108u));
-    return r;
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-// Activations: a lane's eight neighbouring columns of one token as four words of bf16 pairs. An fp32 activation becomes
-// three bf16 terms by truncation (8 + 8 + 8 bits: their sum is the fp32 value exactly, down to where the last term
-// underflows), so that products and sums keep fp32's accuracy on the bf16 tensor core.
+// Activations: a lane's eight neighbouring columns of one token, as loaded and as four words of bf16 pairs. An fp32
+// activation becomes three bf16 terms by truncation (8 + 8 + 8 bits: their sum is the fp32 value exactly, down to where the
+// last term underflows), so that products and sums keep fp32's accuracy on the bf16 tensor core.
 template <typename XT> struct Acts;
 template <> struct Acts<bf16> {
     static constexpr int kTerms = 1;
-    uint32_t w[1][4];
-    __device__ __forceinline__ void load(const bf16* p, uint32_t c, uint32_t cols, bool vec)
+    struct Raw { uint4 r[1]; };
+    static __device__ __forceinline__ Raw words(const bf16* p) { return Raw{{__ldg(reinterpret_cast<const uint4*>(p))}}; }
+    static __device__ __noinline__ Raw gather(const bf16* p, uint32_t c, uint32_t cols)      // element by element
     {
-        if (vec && c + 8 <= cols) {
-            const uint4 r = __ldg(reinterpret_cast<const uint4*>(p + c));
-            w[0][0] = r.x; w[0][1] = r.y; w[0][2] = r.z; w[0][3] = r.w;
-        } else {
-            const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+        const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+        uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t lo = c + 2 * e < cols ? __ldg(q + c + 2 * e) : 0u, hi = c + 2 * e + 1 < cols ? __ldg(q + c + 2 * e + 1) : 0u;
-                w[0][e] = lo | (hi << 16);
-            }
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t lo = c + 2 * e < cols ? __ldg(q + c + 2 * e) : 0u, hi = c + 2 * e + 1 < cols ? __ldg(q + c + 2 * e + 1) : 0u;
+            w[e] = lo | (hi << 16);
         }
+        return Raw{{make_uint4(w[0], w[1], w[2], w[3])}};
+    }
+    static __device__ __forceinline__ Raw zero() { return Raw{{make_uint4(0, 0, 0, 0)}}; }
+    static __device__ __forceinline__ void terms(const Raw& v, uint32_t (&w)[1][4])
+    {
+        w[0][0] = v.r[0].x; w[0][1] = v.r[0].y; w[0][2] = v.r[0].z; w[0][3] = v.r[0].w;
     }
 };
 template <> struct Acts<float> {
     static constexpr int kTerms = 3;
-    uint32_t w[3][4];
-    __device__ __forceinline__ void load(const float* p, uint32_t c, uint32_t cols, bool vec)
+    struct Raw { uint4 r[2]; };
+    static __device__ __forceinline__ Raw words(const float* p)
     {
-        float v[8];
-        if (vec && c + 8 <= cols) {
+        return Raw{{__ldg(reinterpret_cast<const uint4*>(p)), __ldg(reinterpret_cast<const uint4*>(p) + 1)}};
+    }
+    static __device__ __noinline__ Raw gather(const float* p, uint32_t c, uint32_t cols)
+    {
+        uint32_t w[8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float4 r = __ldg(reinterpret_cast<const float4*>(p + c) + h);
-                v[4 * h] = r.x; v[4 * h + 1] = r.y; v[4 * h + 2] = r.z; v[4 * h + 3] = r.w;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? __ldg(p + c + e) : 0.f;
-        }
+        for (int e = 0; e < 8; ++e) w[e] = c + e < cols ? __float_as_uint(__ldg(p + c + e)) : 0u;
+        return Raw{{make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7])}};
+    }
+    static __device__ __forceinline__ Raw zero() { return Raw{{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}}; }
+    static __device__ __forceinline__ void terms(const Raw& v, uint32_t (&w)[3][4])
+    {
+        float f[8] = {__uint_as_float(v.r[0].x), __uint_as_float(v.r[0].y), __uint_as_float(v.r[0].z), __uint_as_float(v.r[0].w),
+                      __uint_as_float(v.r[1].x), __uint_as_float(v.r[1].y), __uint_as_float(v.r[1].z), __uint_as_float(v.r[1].w)};
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float a = v[2 * e], b = v[2 * e + 1];
+                const float a = f[2 * e], b = f[2 * e + 1];
                 w[k][e] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
                 const float ta = __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), tb = __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
-                v[2 * e] = a == ta ? 0.f : a - ta;           // the comparison keeps an infinity out of the lower terms
-                v[2 * e + 1] = b == tb ? 0.f : b - tb;
+                f[2 * e] = a == ta ? 0.f : a - ta;           // the comparison keeps an infinity out of the lower terms
+                f[2 * e + 1] = b == tb ? 0.f : b - tb;
             }
         }
     }
 };
 
-// NB blocks of 8 tokens per pass. HALF: groups of 32 columns (two scales per tile and row) instead of 64 or 128.
-//
-// A CTA's eight warps are `split` parts of the columns x (8 / split) tiles of 16 rows. A segment is one packed matrix with
-// the tokens that go through it: the base with every token, then each slot of the superposition with the tokens whose
-// task keeps this layer there. Partial sums of all parts and segments meet in shared memory and are added in a fixed
-// order, so results do not depend on timing.
-template <int NB, typename XT, bool HALF>
-__global__ void __launch_bounds__(kMulWarps * 32) packed_linear_kernel(const __grid_constant__ PackedLinearArgs a)
+// ---- the ring of bulk copies
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
 {
-    extern __shared__ float part[];      // [row tile of the CTA][part][position in the token lists][16 rows]
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_init(uint32_t bar) { asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+constexpr uint32_t kWaitLimit = 1u << 22;       // tries (each may sleep): seconds, far beyond any copy
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity)
+{
+    for (uint32_t i = 0; i < kWaitLimit; ++i)
+        if (bar_try(bar, parity)) return true;
+    return false;
+}
+
+constexpr int kTiles = 2;                        // column tiles per stage
+constexpr int kDepth = 2;                        // stages of a warp's ring
+constexpr int kRowTiles = 4;                     // row tiles a warp takes along: one row block
+constexpr int kRows = 16 * kRowTiles;
+
+// A segment is one packed matrix with the tokens that go through it: the base with every token, then each slot of the
+// superposition with the tokens whose task keeps this layer there.
+//
+// The column blocks of all segments, one after the other, are dealt in equal contiguous runs to 2^log_split warps of a CTA
+// times the CTAs of a cluster; the other warps of the CTA do the same for other row blocks. A warp takes 64 rows along:
+// what it does per tile of activations (three-way split, signs) is paid once for four tiles of codes. Each warp feeds
+// itself: codes and scales through a ring of two stages, one bulk copy per stage, activations one tile ahead in registers;
+// no warp waits for another until the end. Its sums of one segment stay in registers until its run leaves the segment. All partial sums meet in shared memory, those of a cluster's CTAs through distributed
+// shared memory, and are added in a fixed order: results do not depend on timing.
+template <typename XT, int GROUP>
+__global__ void __launch_bounds__(kMulWarps * 32, 2) packed_linear_kernel(const __grid_constant__ PackedLinearArgs a)
+{
+    typedef Acts<XT> Act;
+    constexpr bool HALF = GROUP == 32;
+    constexpr uint32_t kBlockTiles = GROUP == 128 ? 2 : 1;                       // column tiles per record
+    constexpr uint32_t kCodeBytes = kBlockTiles * kRowTiles * 512, kRecord = kCodeBytes + (HALF ? 2 : 1) * kRowTiles * 32;
+    constexpr uint32_t kBlocks = kTiles / kBlockTiles;                           // records per stage
+    constexpr uint32_t kStage = kBlocks * kRecord;
+    extern __shared__ float part[];      // [row block of the CTA][part][position in the token lists][kRows]
+    cg::cluster_group cluster = cg::this_cluster();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const uint32_t split = a.split, kp = warp % split, wr = warp / split, tiles_cta = kMulWarps / split;
-    const uint32_t rt = blockIdx.x * tiles_cta + wr;
-    const uint32_t kts = (a.cols + 63) / 64, rts = (a.rows + 15) / 16;
-    const uint32_t k0 = static_cast<uint32_t>(static_cast<uint64_t>(kts) * kp / split), k1 = static_cast<uint32_t>(static_cast<uint64_t>(kts) * (kp + 1) / split);
+    const uint32_t ls = a.log_split, kp = warp & ((1u << ls) - 1), wr = warp >> ls, split = 1u << ls, blocks_cta = kMulWarps >> ls;
+    const uint32_t lr = a.log_ranks, ranks = 1u << lr, rank = blockIdx.x & (ranks - 1);
+    const uint32_t first_block = (blockIdx.x >> lr) * blocks_cta, rb = first_block + wr;
+    const uint32_t kbs = (a.cols + 64 * kBlockTiles - 1) / (64 * kBlockTiles), rbs = (a.rows + kRows - 1) / kRows;
     const uint32_t n_pos = a.seg[a.n_seg - 1].first + a.seg[a.n_seg - 1].count;
+    const uint64_t total = static_cast<uint64_t>(kbs) * a.n_seg;
     const XT* x = static_cast<const XT*>(a.x);
-    const uint32_t n_groups = packed_groups(a.cols, a.group);
-    if (rt < rts) {
-        for (uint32_t sgi = 0; sgi < a.n_seg; ++sgi) {
-            const PackedSegment& sg = a.seg[sgi];
-            const uint4* codes = static_cast<const uint4*>(sg.packed) + static_cast<size_t>(rt) * kts * 32 + lane;
-            const uint32_t* scales = reinterpret_cast<const uint32_t*>(static_cast<const char*>(sg.packed) + packed_codes_bytes(a.rows, a.cols)) +
-                                     static_cast<size_t>(rt) * n_groups * 8 + g;
-            const XT* xr[NB];
-            float tot[NB][4];
-            uint4 blk[NB];
-            DevTask task[NB];
+    float* mine = part + static_cast<size_t>(wr * split + kp) * n_pos * kRows;
+
+    const uint32_t lo = static_cast<uint32_t>(total * (rank * split + kp) >> (ls + lr));
+    const uint32_t hi = rb < rbs ? static_cast<uint32_t>(total * (rank * split + kp + 1) >> (ls + lr)) : lo;
+
+    const uint32_t smem = static_cast<uint32_t>(__cvta_generic_to_shared(part));
+    const uint32_t bars = smem + a.ring_at + warp * kDepth * 8;
+    const uint32_t ring = smem + a.ring_at + kMulWarps * kDepth * 8 + warp * kDepth * kStage;
+    if (lane == 0) {
+        for (uint32_t d = 0; d < kDepth; ++d) bar_init(bars + d * 8);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncwarp();
+
+    uint32_t left = hi - lo, fseg = lo / max(kbs, 1u), fkb = lo - fseg * kbs, fstage = 0;      // what is fetched next
+    auto fetch = [&]() {
+        if (!left) return;
+        const uint32_t n = min(min(kBlocks, kbs - fkb), left);
+        if (lane == 0) {
+            const uint32_t bar = bars + fstage * 8;
+            bar_expect(bar, n * kRecord);
+            bulk_copy(ring + fstage * kStage, static_cast<const char*>(a.seg[fseg].packed) + (static_cast<size_t>(rb) * kbs + fkb) * kRecord, n * kRecord, bar);
+        }
+        fstage ^= 1u;
+        left -= n;
+        fkb += n;
+        if (fkb == kbs) { fkb = 0; ++fseg; }
+    };
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const uint32_t i = b * 8 + g;
-                const bool on = i < sg.count;
-                const uint32_t pos = sg.first + (on ? i : 0);
-                xr[b] = on ? x + a.token[pos] * a.x_stride : nullptr;
-                if (sg.flip) task[b] = a.task[a.token_task[pos]];
-                tot[b][0] = tot[b][1] = tot[b][2] = tot[b][3] = 0.f;
-                blk[b] = make_uint4(0, 0, 0, 0);
+    for (int d = 0; d < kDepth; ++d) fetch();
+    for (uint32_t i = lane; i < n_pos * (kRows / 4); i += 32) reinterpret_cast<float4*>(mine)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    __syncwarp();
+
+    uint32_t u = lo, useg = lo / max(kbs, 1u), ukb = lo - useg * kbs, stage = 0, parity = 0;
+    bool ok = true;
+    while (u < hi && ok) {
+        const uint32_t k0 = ukb, k1 = min(kbs, k0 + (hi - u));
+        const PackedSegment& sg = a.seg[useg++];
+        u += k1 - k0;
+        ukb = 0;
+        const uint32_t count = sg.count, tok = min(static_cast<uint32_t>(g), count - 1);
+        const bool signs = sg.flip != 0;
+        // Columns n of a product do not meet: what the lanes without a token hold (the last token's activations) goes nowhere.
+        const XT* xt = x + a.token[sg.first + tok] * a.x_stride;
+        const uint32_t whole = a.x_vec ? a.cols / 64 : 0u;        // column tiles whose activations are whole 16-byte words
+        typename Act::Raw raw[2];
+        auto load = [&](uint32_t kt) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const uint32_t c = kt * 64 + 32 * p + 8 * t;
+                if (kt < whole) raw[p] = Act::words(xt + c);
+                else raw[p] = c < a.cols ? Act::gather(xt, c, a.cols) : Act::zero();
             }
-            uint32_t blk0 = ~0u;         // first of the four sign blocks that the lanes of a token hold
-            for (uint32_t kt = k0; kt < k1; ++kt) {
-                const uint4 cw = __ldg(codes + static_cast<size_t>(kt) * 32);
-                const uint32_t sc0 = __ldg(scales + static_cast<size_t>(HALF ? 2 * kt : kt * 64 / a.group) * 8);
-                const uint32_t sc1 = HALF && 2 * kt + 1 < n_groups ? __ldg(scales + static_cast<size_t>(2 * kt + 1) * 8) : 0u;
-                if (sg.flip && (blk0 == ~0u || (kt >> 1) - blk0 >= 4)) {
-                    blk0 = kt >> 1;      // lane t of a token makes the block of columns 128 (blk0 + t) ..
+        };
+        const uint32_t kt1 = min(k1 * kBlockTiles, (a.cols + 63) / 64);
+        load(k0 * kBlockTiles);
+        DevTask task = {0, 0, 0, 0};
+        if (signs) task = a.task[a.token_task[sg.first + tok]];
+        float tot[kRowTiles][4];
 #pragma unroll
-                    for (int b = 0; b < NB; ++b)
-                        blk[b] = philox4x32_10(blk0 + t, sg.slot, kTagSign, task[b].id, task[b].key0, task[b].key1);
-                }
-                uint32_t am[4][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    am[0][i] = decode2(cw.x, i); am[1][i] = decode2(cw.y, i);
-                    am[2][i] = decode2(cw.z, i); am[3][i] = decode2(cw.w, i);
-                }
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    if (static_cast<uint32_t>(b * 8) >= sg.count) break;
-                    Acts<XT> xa[2];
+        for (int r = 0; r < kRowTiles; ++r) tot[r][0] = tot[r][1] = tot[r][2] = tot[r][3] = 0.f;
+        uint4 blk = make_uint4(0, 0, 0, 0);
+        uint32_t blk0 = ~0u;         // first of the four sign blocks that the lanes of a token hold
+        for (uint32_t kb = k0; kb < k1; kb += kBlocks) {
+            const uint32_t st = ring + stage * kStage;
+            ok = bar_wait(bars + stage * 8, parity);
+            if (!ok) break;
+            const uint32_t kt0 = kb * kBlockTiles, nt = min(static_cast<uint32_t>(kTiles), kt1 - kt0);
+#pragma unroll 1
+            for (uint32_t i = 0; i < nt; ++i) {
+                const uint32_t kt = kt0 + i;
+                uint32_t xa[2][Act::kTerms][4];
+                Act::terms(raw[0], xa[0]);
+                Act::terms(raw[1], xa[1]);
+                if (kt + 1 < kt1) load(kt + 1);
+                if (signs) {
+                    if (blk0 == ~0u || (kt >> 1) - blk0 >= 4) {
+                        blk0 = kt >> 1;      // lane t of a token makes the block of columns 128 (blk0 + t) ..
+                        blk = philox4x32_10(blk0 + t, sg.slot, kTagSign, task.id, task.key0, task.key1);
+                    }
+                    const int src = (lane & ~3) | static_cast<int>((kt >> 1) - blk0);
+                    const uint32_t w0 = __shfl_sync(~0u, kt & 1 ? blk.z : blk.x, src), w1 = __shfl_sync(~0u, kt & 1 ? blk.w : blk.y, src);
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
-                        if (xr[b]) {
-                            xa[p].load(xr[b], kt * 64 + 32 * p + 8 * t, a.cols, a.x_vec);
-                        } else {
+                        const uint32_t bits = ((p ? w1 : w0) >> (8 * t)) & 0xFFu;
 #pragma unroll
-                            for (int k = 0; k < Acts<XT>::kTerms; ++k)
+                        for (int e = 0; e < 4; ++e) {
+                            // bit 2e of the byte lands on bit 15, bit 2e + 1 on bit 31; the two copies do not overlap
+                            const uint32_t mask = (bits * ((1u << (15 - 2 * e)) + (1u << (30 - 2 * e)))) & 0x80008000u;
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) xa[p].w[k][e] = 0u;
+                            for (int k = 0; k < Act::kTerms; ++k) xa[p][k][e] ^= mask;
                         }
                     }
-                    if (sg.flip) {
-                        const int src = (lane & ~3) | static_cast<int>((kt >> 1) - blk0);
-                        const uint32_t w0 = __shfl_sync(~0u, kt & 1 ? blk[b].z : blk[b].x, src), w1 = __shfl_sync(~0u, kt & 1 ? blk[b].w : blk[b].y, src);
+                }
+                // word by word across the row tiles, so that a product does not wait for the one before it
+                const uint32_t rec = st + (kBlockTiles == 1 ? i * kRecord : 0u);
+                const uint32_t cat = rec + (kBlockTiles == 2 ? i * (kRowTiles * 512) : 0u) + lane * 16, sat = rec + kCodeBytes + g * 4;
+                uint4 cw[kRowTiles];
 #pragma unroll
-                        for (int p = 0; p < 2; ++p) {
-                            const uint32_t bits = ((p ? w1 : w0) >> (8 * t)) & 0xFFu;
+                for (int r = 0; r < kRowTiles; ++r) cw[r] = lds128(cat + r * 512);
+                float acc[kRowTiles][4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                // bit 2e of the byte lands on bit 15, bit 2e + 1 on bit 31; the two copies do not overlap
-                                const uint32_t mask = (bits * ((1u << (15 - 2 * e)) + (1u << (30 - 2 * e)))) & 0x80008000u;
+                for (int j = 0; j < 4; ++j) {
 #pragma unroll
-                                for (int k = 0; k < Acts<XT>::kTerms; ++k) xa[p].w[k][e] ^= mask;
-                            }
+                    for (int r = 0; r < kRowTiles; ++r) {
+                        uint32_t am[4];
+                        decode(j == 0 ? cw[r].x : (j == 1 ? cw[r].y : (j == 2 ? cw[r].z : cw[r].w)), am);
+#pragma unroll
+                        for (int k = 0; k < Act::kTerms; ++k) {
+                            const uint32_t b0 = xa[j >> 1][k][2 * (j & 1)], b1 = xa[j >> 1][k][2 * (j & 1) + 1];
+                            if (k == 0 && (j == 0 || (HALF && j == 2))) mma_16816_first(acc[r], am, b0, b1);
+                            else mma_16816(acc[r], am, b0, b1);
                         }
                     }
-                    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                    if ((HALF && j == 1) || j == 3) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-                        for (int k = 0; k < Acts<XT>::kTerms; ++k)
-                            mma_16816(acc, am[j], xa[j >> 1].w[k][2 * (j & 1)], xa[j >> 1].w[k][2 * (j & 1) + 1]);
-                        if ((HALF && j == 1) || j == 3) {
-                            const uint32_t sc = HALF && j == 3 ? sc1 : sc0;
-                            const float lo = __uint_as_float(sc << 16), hi = __uint_as_float(sc & 0xFFFF0000u);
-                            tot[b][0] = __fmaf_rn(lo, acc[0], tot[b][0]);
-                            tot[b][1] = __fmaf_rn(lo, acc[1], tot[b][1]);
-                            tot[b][2] = __fmaf_rn(hi, acc[2], tot[b][2]);
-                            tot[b][3] = __fmaf_rn(hi, acc[3], tot[b][3]);
-                            acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+                        for (int r = 0; r < kRowTiles; ++r) {
+                            const uint32_t s2 = lds_u32(sat + r * 32 + (HALF && j == 3 ? kRowTiles * 32 : 0));
+                            const float s_lo = __uint_as_float(s2 << 16), s_hi = __uint_as_float(s2 & 0xFFFF0000u);
+                            tot[r][0] = __fmaf_rn(s_lo, acc[r][0], tot[r][0]);
+                            tot[r][1] = __fmaf_rn(s_lo, acc[r][1], tot[r][1]);
+                            tot[r][2] = __fmaf_rn(s_hi, acc[r][2], tot[r][2]);
+                            tot[r][3] = __fmaf_rn(s_hi, acc[r][3], tot[r][3]);
                         }
                     }
                 }
             }
-            float* mine = part + (static_cast<size_t>(wr * split + kp) * n_pos + sg.first) * 16;
+            __syncwarp();                // every lane has read the stage: it may be filled again
+            fetch();
+            stage ^= 1u;
+            parity ^= stage ^ 1u;
+        }
+        {
+            const uint32_t i = 2 * t;
+            float* to = mine + (sg.first + i) * kRows + g;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const uint32_t i = b * 8 + 2 * t;
-                if (i < sg.count) { mine[i * 16 + g] = kCodeUnit * tot[b][0]; mine[i * 16 + g + 8] = kCodeUnit * tot[b][2]; }
-                if (i + 1 < sg.count) { mine[(i + 1) * 16 + g] = kCodeUnit * tot[b][1]; mine[(i + 1) * 16 + g + 8] = kCodeUnit * tot[b][3]; }
+            for (int r = 0; r < kRowTiles; ++r) {
+                if (i < count) { to[r * 16] = kCodeUnit * tot[r][0]; to[r * 16 + 8] = kCodeUnit * tot[r][2]; }
+                if (i + 1 < count) { to[kRows + r * 16] = kCodeUnit * tot[r][1]; to[kRows + r * 16 + 8] = kCodeUnit * tot[r][3]; }
             }
         }
     }
+    if (!ok) {                           // a copy that never arrived: count it, give the others time, spoil the sums
+        if (lane == 0) atomicAdd(&g_packed_giveups, 1u);
+        for (uint32_t d = 0; d < kDepth; ++d) (void)bar_wait(bars + d * 8, d < stage ? parity ^ 1u : parity);
+        for (uint32_t i = lane; i < n_pos * kRows; i += 32) mine[i] = NAN;
+    }
     __syncthreads();
-    // y = (sum of the base's parts) + lambda * (sum of the slot's parts), each sum in part order
-    const uint32_t n_out = tiles_cta * 16 * a.n_tokens;
-    for (uint32_t o = threadIdx.x; o < n_out; o += kMulWarps * 32) {
-        const uint32_t r = o % (tiles_cta * 16), tok = o / (tiles_cta * 16);
-        const uint64_t row = static_cast<uint64_t>(blockIdx.x) * tiles_cta * 16 + r;
-        if (row >= a.rows) continue;
-        const float* p = part + static_cast<size_t>(r >> 4) * split * n_pos * 16 + (r & 15);
-        float y = 0.f, d = 0.f;
-        for (uint32_t k = 0; k < split; ++k) y += p[(k * n_pos + tok) * 16];
-        if (a.n_seg > 1) {
-            const uint32_t pos = a.pos_of_token[tok];
-            for (uint32_t k = 0; k < split; ++k) d += p[(k * n_pos + pos) * 16];
-            y = __fmaf_rn(a.lambda, d, y);
-        }
-        const size_t at = tok * a.y_stride + row;
+    // the CTA's y = (sum of the base's parts) + lambda * (sum of the slot's parts), each sum in part order
+    const uint32_t rows_cta = blocks_cta * kRows, n_out = rows_cta * a.n_tokens;
+    float* sums = part + static_cast<size_t>(kMulWarps) * n_pos * kRows;      // [token][row of the CTA], only with a cluster
+    const uint64_t row0 = static_cast<uint64_t>(first_block) * kRows;
+    auto store = [&](uint32_t tok, uint32_t r, float y) {
+        if (row0 + r >= a.rows) return;
+        const size_t at = tok * a.y_stride + row0 + r;
         if (a.y_bf16) static_cast<bf16*>(a.y)[at] = __float2bfloat16_rn(y);
         else static_cast<float*>(a.y)[at] = y;
+    };
+    for (uint32_t o = threadIdx.x; o < n_out; o += kMulWarps * 32) {
+        const uint32_t r = o % rows_cta, tok = o / rows_cta;
+        const float* p = part + static_cast<size_t>(r / kRows) * split * n_pos * kRows + r % kRows;
+        float y = 0.f, d = 0.f;
+        for (uint32_t k = 0; k < split; ++k) y += p[(k * n_pos + tok) * kRows];
+        if (a.n_seg > 1) {
+            const uint32_t pos = a.pos_of_token[tok];
+            for (uint32_t k = 0; k < split; ++k) d += p[(k * n_pos + pos) * kRows];
+            y = __fmaf_rn(a.lambda, d, y);
+        }
+        if (ranks == 1) store(tok, r, y);
+        else sums[o] = y;
+    }
+    if (ranks > 1) {
+        cluster.sync();
+        for (uint32_t o = rank * (kMulWarps * 32) + threadIdx.x; o < n_out; o += ranks * kMulWarps * 32) {
+            float y = 0.f;
+            for (uint32_t k = 0; k < ranks; ++k) y += cluster.map_shared_rank(sums, k)[o];
+            store(o / rows_cta, o % rows_cta, y);
+        }
+        cluster.sync();          // nobody leaves while its sums may still be read
     }
 }
 
-template <int NB, typename XT, bool HALF> cudaError_t launch_mul(const PackedLinearArgs& a, unsigned grid, size_t smem, cudaStream_t s)
+template <typename XT, int GROUP> cudaError_t launch_mul(PackedLinearArgs& a, int sm_count, int device, cudaStream_t s)
 {
-    if (smem > 48 * 1024) {   // beyond this a kernel has to opt in, per device
-        const cudaError_t e = cudaFuncSetAttribute(packed_linear_kernel<NB, XT, HALF>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    const PackedLayout lay(a.rows, a.cols, a.group);
+    const uint64_t total = static_cast<uint64_t>(lay.col_blocks) * a.n_seg, blocks = (a.rows + kRows - 1) / kRows;
+    // two CTAs of eight warps per SM, as long as every warp has a record: first the warps of a CTA share rows, then CTAs do
+    const uint64_t want = static_cast<uint64_t>(sm_count) * 2 * kMulWarps;
+    a.log_split = a.log_ranks = 0;
+    while (a.log_split < 3 && (blocks << a.log_split) < want && (2u << a.log_split) <= total) ++a.log_split;
+    while (a.log_split == 3 && a.log_ranks < 3 && (blocks << (4 + a.log_ranks)) <= want && (16ull << a.log_ranks) <= total) ++a.log_ranks;
+    const uint32_t blocks_cta = kMulWarps >> a.log_split, ranks = 1u << a.log_ranks;
+    const uint32_t n_pos = a.seg[a.n_seg - 1].first + a.seg[a.n_seg - 1].count;
+    a.ring_at = (kMulWarps * n_pos + (ranks > 1 ? blocks_cta * a.n_tokens : 0)) * kRows * static_cast<uint32_t>(sizeof(float));
+    const size_t smem = a.ring_at + static_cast<size_t>(kMulWarps) * kDepth * (kTiles / lay.tiles * lay.record + 8);
+    static std::atomic<size_t> granted[kDevices];      // a kernel has to opt in beyond 48 KiB, per device
+    if (smem > 48 * 1024 && (device >= kDevices || smem > granted[device].load(std::memory_order_relaxed))) {
+        const cudaError_t e = cudaFuncSetAttribute(packed_linear_kernel<XT, GROUP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
         if (e != cudaSuccess) return e;
+        if (device < kDevices) granted[device].store(smem, std::memory_order_relaxed);
     }
-    packed_linear_kernel<NB, XT, HALF><<<grid, kMulWarps * 32, smem, s>>>(a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>((blocks + blocks_cta - 1) / blocks_cta * ranks));
+    cfg.blockDim = dim3(kMulWarps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ranks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = ranks > 1;
+    return cudaLaunchKernelEx(&cfg, packed_linear_kernel<XT, GROUP>, a);
 }
 
-template <typename XT, bool HALF> cudaError_t launch_nb(const PackedLinearArgs& a, unsigned grid, size_t smem, cudaStream_t s)
+template <typename XT> cudaError_t launch_group(PackedLinearArgs& a, int sm_count, int device, cudaStream_t s)
 {
-    if (a.n_tokens <= 8) return launch_mul<1, XT, HALF>(a, grid, smem, s);
-    if (a.n_tokens <= 16) return launch_mul<2, XT, HALF>(a, grid, smem, s);
-    if (a.n_tokens <= 32) return launch_mul<4, XT, HALF>(a, grid, smem, s);
-    return launch_mul<8, XT, HALF>(a, grid, smem, s);
+    if (a.group == 32) return launch_mul<XT, 32>(a, sm_count, device, s);
+    if (a.group == 64) return launch_mul<XT, 64>(a, sm_count, device, s);
+    return launch_mul<XT, 128>(a, sm_count, device, s);
 }
 
 }  // namespace
 
-int launch_packed_linear(PackedLinearArgs& a, bool x_bf16, int sm_count, void* stream)
+int launch_packed_linear(PackedLinearArgs& a, bool x_bf16, int sm_count, int device, void* stream)
 {
-    const uint32_t rts = (a.rows + 15) / 16, kts = (a.cols + 63) / 64;
-    uint32_t split = 1;
-    // enough warps to keep about sixteen per SM loading, as long as every part has a tile
-    while (split < kMulWarps && static_cast<uint64_t>(rts) * split < static_cast<uint64_t>(sm_count) * 16 && split * 2 <= kts) split *= 2;
-    a.split = split;
-    const uint32_t tiles_cta = kMulWarps / split;
-    const uint32_t n_pos = a.seg[a.n_seg - 1].first + a.seg[a.n_seg - 1].count;
-    const size_t smem = static_cast<size_t>(kMulWarps) * n_pos * 16 * sizeof(float);
-    const unsigned grid = (rts + tiles_cta - 1) / tiles_cta;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool half = a.group == 32;
-    cudaError_t e;
-    if (x_bf16) e = half ? launch_nb<bf16, true>(a, grid, smem, s) : launch_nb<bf16, false>(a, grid, smem, s);
-    else e = half ? launch_nb<float, true>(a, grid, smem, s) : launch_nb<float, false>(a, grid, smem, s);
-    return static_cast<int>(e);
+    return static_cast<int>(x_bf16 ? launch_group<bf16>(a, sm_count, device, s) : launch_group<float>(a, sm_count, device, s));
+}
+
+int packed_giveups(unsigned int* count)
+{
+    return static_cast<int>(cudaMemcpyFromSymbol(count, g_packed_giveups, sizeof(unsigned int)));
 }
 
 namespace {
@@ -480,7 +677,7 @@ template <typename M> unsigned deal_ctas(M* mat, uint32_t n)
     uint64_t at = 0;
     for (uint32_t i = 0; i < n; ++i) {
         mat[i].first_cta = static_cast<uint32_t>(at);
-        at += (static_cast<uint64_t>((mat[i].rows + 15) / 16) * ((mat[i].cols + 127) / 128) + kPackWarps - 1) / kPackWarps;
+        at += (static_cast<uint64_t>((mat[i].rows + 63) / 64) * 4 * ((mat[i].cols + 127) / 128) + kPackWarps - 1) / kPackWarps;
     }
     return static_cast<unsigned>(at);
 }

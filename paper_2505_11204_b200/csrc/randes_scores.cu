@@ -6,9 +6,9 @@
 // The differences to the maximum are taken before anything is scaled, so no term carries the rounding of a large
 // exponent; each thread keeps (M, S, T) of what it has read and rescales them when its maximum rises.
 //
-// Top alternatives without sorting: a group of four threads knows the greatest of the elements it read; the k-th largest
-// of those group maxima cannot be above the k-th largest element, so only the groups that reach it are read again (about
-// k of 128), and what reaches it is ranked. Equal logits are ordered by index.
+// Top alternatives without sorting: a pair of threads knows the greatest of the elements it read; the k-th largest of
+// those maxima cannot be above the k-th largest element, so only the pairs that reach it are read again (about k of 128),
+// and what reaches it is ranked. Equal logits are ordered by index.
 //
 // A row may be shared by a cluster of CTAs (few rows); their sums and top lists meet in the first CTA through distributed
 // shared memory.
@@ -28,12 +28,13 @@ namespace {
 
 using namespace device;
 
-constexpr int kScoreThreads = 512;
+constexpr int kScoreThreads = 256;
 constexpr int kScoreWarps = kScoreThreads / 32;
-constexpr int kGroups = kScoreThreads / 4;      // groups of four threads; more than kMaxTop
-constexpr int kCandidates = 1024;
+constexpr int kGroups = kScoreThreads / 2;      // pairs of threads; at least kMaxTop
+constexpr int kCandidates = 768;
 constexpr int kMaxCluster = 8;
-static_assert(kGroups > static_cast<int>(kMaxTop), "the threshold is the k-th largest group maximum");
+static_assert(kGroups >= static_cast<int>(kMaxTop), "the threshold is the k-th largest group maximum");
+static_assert(kCandidates >= kMaxCluster * static_cast<int>(kMaxTop), "the lists of a cluster are ranked together");
 
 __device__ __forceinline__ float max_nan(float a, float b)
 {
@@ -76,18 +77,57 @@ __device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c)
 }
 
 // order of (logit, index): larger logit first, then lower index; -0 counts as +0
-__device__ __forceinline__ unsigned long long key_of(float z, uint32_t idx)
+__device__ __forceinline__ uint32_t order_of(float z)
 {
     const uint32_t b = __float_as_uint(z + 0.f);
-    const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
-    return (static_cast<unsigned long long>(o) << 32) | (0xFFFFFFFFu - idx);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(unsigned long long key)
+__device__ __forceinline__ float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
+__device__ __forceinline__ unsigned long long key_of(float z, uint32_t idx)
 {
-    const uint32_t o = static_cast<uint32_t>(key >> 32);
-    return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+    return (static_cast<unsigned long long>(order_of(z)) << 32) | (0xFFFFFFFFu - idx);
 }
+__device__ __forceinline__ float value_of(unsigned long long key) { return value_of(static_cast<uint32_t>(key >> 32)); }
 __device__ __forceinline__ uint32_t index_of(unsigned long long key) { return 0xFFFFFFFFu - static_cast<uint32_t>(key); }
+
+// greatest and least of a lane's 16 bytes (a NaN wins both)
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t min2_nan(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float r;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+template <typename T> __device__ __forceinline__ void extremes(const uint4& w, float& top, float& low);
+template <> __device__ __forceinline__ void extremes<float>(const uint4& w, float& top, float& low)
+{
+    const float a = __uint_as_float(w.x), b = __uint_as_float(w.y), c = __uint_as_float(w.z), d = __uint_as_float(w.w);
+    top = max_nan(max3_nan(a, b, c), d);
+    low = fminf(min3(a, b, c), d);
+}
+template <> __device__ __forceinline__ void extremes<bf16>(const uint4& w, float& top, float& low)
+{
+    const uint32_t hi = max2_nan(max2_nan(w.x, w.y), max2_nan(w.z, w.w)), lo = min2_nan(min2_nan(w.x, w.y), min2_nan(w.z, w.w));
+    top = max_nan(__uint_as_float(hi << 16), __uint_as_float(hi & 0xFFFF0000u));
+    low = fminf(__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u));
+}
 
 // A CTA's share of a row: vectors [v0, v1) of the row's 16-byte aligned middle, and up to CPL - 1 single elements at
 // either end (given to the first and the last CTA).
@@ -119,43 +159,65 @@ template <typename T> struct Share {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_constant__ ScoreArgs a)
+__global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_constant__ ScoreArgs a, uint32_t ranks)
 {
     constexpr int CPL = Store<T>::CPL, U = 4;
     cg::cluster_group cluster = cg::this_cluster();
-    const uint32_t ranks = cluster.num_blocks(), rank = cluster.block_rank();
-    const uint32_t row = blockIdx.x / ranks;
+    const uint32_t row = blockIdx.x / ranks, rank = blockIdx.x - row * ranks;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     __shared__ Sums s_warp[kScoreWarps];
     __shared__ Sums s_cta;
-    __shared__ float s_group[kGroups];
+    __shared__ __align__(16) uint32_t s_group[kGroups];
+    __shared__ uint32_t s_picked[kGroups];
     __shared__ float s_tau;
-    __shared__ unsigned int s_count;
+    __shared__ unsigned int s_count, s_n_picked;
     __shared__ unsigned long long s_cand[kCandidates];
     __shared__ unsigned long long s_top[kMaxTop];          // this CTA's top list, best first; 0 = no element
     __shared__ unsigned long long s_best[kScoreWarps];
 
     const Share<T> sh(static_cast<const T*>(a.logits) + row * a.stride, a.vocab, rank, ranks);
     const float c = a.scale * kLog2e;
-    Sums me = {-INFINITY, 0.f, 0.f};
-    auto take = [&](const float* z, int n, float top) {
-        const float m = max_nan(me.m, top);
-        if (m == -INFINITY) return;
-        if (m != me.m) {                     // also when m is NaN
-            const Sums old = me;
-            me.m = m;
-            me.s = me.t = 0.f;
-            if (old.m != -INFINITY) {
-                const float d = old.m - m, f = ex2(d * c);
-                if (f != 0.f) { me.s = f * old.s; me.t = f * __fmaf_rn(old.s, d, old.t); }
-            }
+    const f32x2 c2 = pack2(__float_as_uint(c), __float_as_uint(c));
+    float m = -INFINITY;
+    f32x2 s2 = 0, t2 = 0;                    // two partial sums each
+    auto raise = [&](float to) {             // a new maximum (or a NaN)
+        const float d = m - to;
+        float f = ex2(d * c), fd = f * d;
+        if (f == 0.f) fd = 0.f;              // (also from m = -inf: nothing was summed yet)
+        m = to;
+        const f32x2 f2 = pack2(__float_as_uint(f), __float_as_uint(f)), g2 = pack2(__float_as_uint(fd), __float_as_uint(fd));
+        t2 = fma2(s2, g2, mul2(t2, f2));     // sum e^(c (z - to)) (z - to) = f (t + s d)
+        s2 = mul2(s2, f2);
+    };
+    auto add = [&](f32x2 z) {                // two logits, relative to m
+        const f32x2 d = z;
+        float a0, a1;
+        unpack2(mul2(d, c2), a0, a1);
+        const f32x2 e = pack2(__float_as_uint(ex2(a0)), __float_as_uint(ex2(a1)));
+        s2 = add2(s2, e);
+        t2 = fma2(e, d, t2);
+    };
+    auto take = [&](const uint4& raw) {
+        float top, low;
+        extremes<T>(raw, top, low);
+        if (!(top <= m)) {
+            if (top == -INFINITY) return;
+            raise(max_nan(m, top));
         }
+        if (m == -INFINITY) return;
+        const f32x2 neg = pack2(__float_as_uint(-m), __float_as_uint(-m));
+        f32x2 z[CPL / 2];
+        Store<T>::widen2(raw, z);
+        if (low > -1e30f) {
 #pragma unroll
-        for (int e = 0; e < n; ++e) {
-            const float d = max_nan(z[e] - m, -1e30f);      // a masked element: exp gives 0, and 0 times this is 0
-            const float x = ex2(d * c);
-            me.s += x;
-            me.t = __fmaf_rn(x, d, me.t);
+            for (int e = 0; e < CPL / 2; ++e) add(add2(z[e], neg));
+        } else {                             // masked logits: exp gives 0, and 0 times a finite number is 0
+#pragma unroll
+            for (int e = 0; e < CPL / 2; ++e) {
+                float a0, a1;
+                unpack2(add2(z[e], neg), a0, a1);
+                add(pack2(__float_as_uint(max_nan(a0, -1e30f)), __float_as_uint(max_nan(a1, -1e30f))));
+            }
         }
     };
     for (uint32_t v = sh.v0 + tid; v < sh.v1; v += kScoreThreads * U) {
@@ -165,21 +227,26 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
             if (v + u * kScoreThreads < sh.v1) raw[u] = sh.load(v + u * kScoreThreads);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (v + u * kScoreThreads < sh.v1) {
-                float z[CPL];
-                Store<T>::widen(raw[u], z);
-                float top = z[0];
-#pragma unroll
-                for (int e = 1; e < CPL; ++e) top = max_nan(top, z[e]);
-                take(z, CPL, top);
-            }
+            if (v + u * kScoreThreads < sh.v1) take(raw[u]);
     }
     uint32_t idx;
     if (tid < 2 * CPL && sh.single(tid, idx)) {
         const float z = Store<T>::load1(sh.row + idx);
-        take(&z, 1, z);
+        if (!(z <= m) && z != -INFINITY) raise(max_nan(m, z));
+        if (m != -INFINITY) {                // the second of the pair is masked
+            float d = max_nan(z - m, -1e30f);
+            add(pack2(__float_as_uint(d), __float_as_uint(-1e30f)));
+        }
     }
-    const float own_max = me.m;
+    Sums me;
+    {
+        float s0, s1, t0, t1;
+        unpack2(s2, s0, s1);
+        unpack2(t2, t0, t1);
+        me.m = m;
+        me.s = s0 + s1;
+        me.t = t0 + t1;
+    }
     // ---- sums of the CTA
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -188,10 +255,11 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
     }
     if (lane == 0) s_warp[warp] = me;
     if (a.top_k) {
-        float gm = max_nan(own_max, __shfl_xor_sync(~0u, own_max, 1));
-        gm = max_nan(gm, __shfl_xor_sync(~0u, gm, 2));
-        if ((tid & 3) == 0) s_group[tid >> 2] = gm;
-        if (tid == 0) { s_count = 0; s_tau = -INFINITY; }
+        // a pair's maximum as a whole number in the logits' order; the last bits hold the pair, so that no two are equal
+        const float pm = max_nan(m, __shfl_xor_sync(~0u, m, 1));
+        if ((tid & 1) == 0) s_group[tid >> 1] = (order_of(pm) & ~(kGroups - 1u)) | (tid >> 1);
+        if (tid == 0) { s_count = 0; s_n_picked = 0; }
+        if (tid < static_cast<int>(kMaxTop)) s_top[tid] = 0ull;
     }
     __syncthreads();
     if (warp == 0) {
@@ -205,43 +273,53 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
     }
     // ---- top list of the CTA
     if (a.top_k) {
-        if (tid < kGroups) {
-            const float mine = s_group[tid];
-            uint32_t before = 0;
-            for (int j = 0; j < kGroups; ++j) {
-                const float o = s_group[j];
-                before += o > mine || (o == mine && j < tid);
-            }
-            if (before == a.top_k - 1) s_tau = mine;
+        const uint32_t mine = s_group[tid >> 1];
+        uint32_t before = 0;                 // pairs in front of this one; each thread of a pair counts in one half
+#pragma unroll 4
+        for (int j = 0; j < kGroups / 8; ++j) {
+            const uint4 o = reinterpret_cast<const uint4*>(s_group)[(tid & 1) * (kGroups / 8) + j];
+            before += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+        }
+        before += __shfl_xor_sync(~0u, before, 1);
+        if (before < a.top_k && (tid & 1) == 0) {
+            s_picked[atomicAdd(&s_n_picked, 1u)] = tid >> 1;
+            // (below the order of the lowest finite number there is only -inf)
+            if (before == a.top_k - 1) s_tau = mine < 0x00800000u ? -INFINITY : value_of(mine & ~(kGroups - 1u));
         }
         __syncthreads();
+        // Pairs that the cut-off last bits put behind the k-th although their maximum equals it may still hold one of the
+        // best: they are looked for among all pairs.
         const float tau = s_tau;
+        if ((tid & 1) == 0 && before >= a.top_k && (mine & ~(kGroups - 1u)) == order_of(tau)) s_picked[atomicAdd(&s_n_picked, 1u)] = tid >> 1;
+        __syncthreads();
         auto offer = [&](float z, uint32_t i) {
             if (z >= tau && z > -INFINITY) {
                 const unsigned int at = atomicAdd(&s_count, 1u);
                 if (at < kCandidates) s_cand[at] = key_of(z, i);
             }
         };
-        for (int q = warp; q < kGroups; q += kScoreWarps) {
-            const float gm = s_group[q];
-            if (!(gm >= tau) || gm == -INFINITY) continue;
-            for (uint32_t v = sh.v0 + 4 * q + (lane & 3) + kScoreThreads * (lane >> 2); v < sh.v1; v += kScoreThreads * 8) {
-                float z[CPL];
-                Store<T>::widen(sh.load(v), z);
+        const uint32_t trips = (sh.v1 - sh.v0 + kScoreThreads - 1) / kScoreThreads, again = s_n_picked * trips * 2;
+        for (uint32_t i = tid; i < again; i += kScoreThreads) {
+            const uint32_t v = sh.v0 + 2 * s_picked[i / (2 * trips)] + (i & 1) + kScoreThreads * (i % (2 * trips) / 2);
+            if (v >= sh.v1) continue;
+            const uint4 raw = sh.load(v);
+            float top, low;
+            extremes<T>(raw, top, low);
+            if (!(top >= tau)) continue;
+            float z[CPL];
+            Store<T>::widen(raw, z);
 #pragma unroll
-                for (int e = 0; e < CPL; ++e) offer(z[e], sh.lead + v * CPL + e);
-            }
+            for (int e = 0; e < CPL; ++e) offer(z[e], sh.lead + v * CPL + e);
         }
         if (tid < 2 * CPL && sh.single(tid, idx)) offer(Store<T>::load1(sh.row + idx), idx);
-        if (tid < static_cast<int>(kMaxTop)) s_top[tid] = 0ull;
         __syncthreads();
         const unsigned int n = s_count;
         if (n <= kCandidates) {
             for (unsigned int i = tid; i < n; i += kScoreThreads) {
-                const unsigned long long mine = s_cand[i];
-                unsigned int before = 0;
-                for (unsigned int j = 0; j < n; ++j) before += s_cand[j] > mine;
-                if (before < a.top_k) s_top[before] = mine;
+                const unsigned long long key = s_cand[i];
+                unsigned int ahead = 0;
+                for (unsigned int j = 0; j < n; ++j) ahead += s_cand[j] > key;
+                if (ahead < a.top_k) s_top[ahead] = key;
             }
         } else {
             // more equal (or nearly equal) logits than the list holds: the best below the last, k times over
@@ -346,15 +424,14 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
     const bool none = m == -INFINITY;
     const float a_p = -a.scale * __fmaf_rn(gh, h, gl), a_pl = -a.scale * gh, c = a.scale * kLog2e;
     // dz = p (a_p + a_pl log p) [+ scale g_lp at the target]
-    auto grad = [&](float x, uint32_t j) {
+    const float ln2 = -ln * kLog2e;
+    auto grad = [&](float x) {
         if (none) return 0.f;
         const float d = max_nan(x - m, -1e30f);
         const float lp = __fmaf_rn(a.scale, d, -ln);
-        const float p = ex2(__fmaf_rn(d, c, -ln * kLog2e));
-        float r = p * __fmaf_rn(a_pl, lp, a_p);
-        if (static_cast<long long>(j) == tk) r = __fmaf_rn(a.scale, gl, r);
-        return r;
+        return ex2(__fmaf_rn(d, c, ln2)) * __fmaf_rn(a_pl, lp, a_p);
     };
+    const float at_target = none ? 0.f : a.scale * gl;
     const uint32_t per = kGradThreads * kGradVectors * CPL;
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T);
     const uint32_t lead = min(off ? CPL - off : 0u, a.vocab);
@@ -373,18 +450,24 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
             float x[CPL];
             Store<T>::widen(raw[u], x);
 #pragma unroll
-            for (int e = 0; e < CPL; ++e) x[e] = grad(x[e], lead + v * CPL + e);
+            for (int e = 0; e < CPL; ++e) x[e] = grad(x[e]);
+            const uint64_t at = static_cast<uint64_t>(tk) - (lead + v * CPL);      // beyond CPL also when there is no target
+            if (at < CPL) {
+#pragma unroll
+                for (int e = 0; e < CPL; ++e)
+                    if (e == static_cast<int>(at)) x[e] += at_target;
+            }
             Out<T>::template store<CPL>(dz + lead + v * CPL, x);
         }
         if (chunk == 0 && threadIdx.x < 2 * CPL) {
             const uint32_t e = threadIdx.x, tail0 = lead + n * CPL;
             const uint32_t j = e < static_cast<uint32_t>(CPL) ? e : tail0 + e - CPL;
-            if (e < static_cast<uint32_t>(CPL) ? e < lead : j < a.vocab) Out<T>::store1(dz + j, grad(Store<T>::load1(z + j), j));
+            if (e < static_cast<uint32_t>(CPL) ? e < lead : j < a.vocab) Out<T>::store1(dz + j, grad(Store<T>::load1(z + j)) + (static_cast<long long>(j) == tk ? at_target : 0.f));
         }
     } else {
         for (uint32_t i = threadIdx.x; i < per; i += kGradThreads) {
             const uint64_t j = static_cast<uint64_t>(chunk) * per + i;
-            if (j < a.vocab) Out<T>::store1(dz + j, grad(Store<T>::load1(z + j), static_cast<uint32_t>(j)));
+            if (j < a.vocab) Out<T>::store1(dz + j, grad(Store<T>::load1(z + j)) + (static_cast<int64_t>(j) == tk ? at_target : 0.f));
         }
     }
 }
@@ -393,7 +476,7 @@ template <typename T> cudaError_t launch_scores_t(const ScoreArgs& a, int sm_cou
 {
     // a cluster shares a row while the rows alone do not fill the SMs and a share still is a few thousand elements
     uint32_t ranks = 1;
-    while (ranks < kMaxCluster && static_cast<uint64_t>(a.n_rows) * ranks * 2 <= static_cast<uint64_t>(sm_count) && a.vocab / (ranks * 2) >= 2048) ranks *= 2;
+    while (ranks < kMaxCluster && static_cast<uint64_t>(a.n_rows) * ranks * 2 <= static_cast<uint64_t>(sm_count) * 4 && a.vocab / (ranks * 2) >= 2048) ranks *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.n_rows * ranks);
     cfg.blockDim = dim3(kScoreThreads);
@@ -403,8 +486,8 @@ template <typename T> cudaError_t launch_scores_t(const ScoreArgs& a, int sm_cou
     at[0].val.clusterDim.x = ranks;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, score_kernel<T>, a);
+    cfg.numAttrs = ranks > 1;
+    return cudaLaunchKernelEx(&cfg, score_kernel<T>, a, ranks);
 }
 
 template <typename T> cudaError_t launch_grad_t(const ScoreGradArgs& a, cudaStream_t s)

@@ -14,6 +14,7 @@ Two levels:
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Any, List, NamedTuple, Optional, Sequence
 
@@ -426,31 +427,54 @@ def _refuse(message: str):
     raise RandesError(INVALID_ARGUMENT, message)
 
 
-def _matrix_dtype(t, what: str) -> int:
-    """Element type of a 2-D CUDA tensor whose rows may be strided; refuses anything the library would misread."""
+def _rows_of(t, what: str):
+    """(element type, rows, columns, elements between rows) of a 2-D CUDA tensor whose rows may be strided; refuses anything
+    the library would misread."""
     import torch
 
-    code = {torch.float32: F32, torch.bfloat16: BF16}.get(t.dtype)
-    if code is None:
-        raise RandesError(UNSUPPORTED_DTYPE, "%s is %s: float32 or bfloat16 is wanted" % (what, t.dtype))
+    dtype = t.dtype
+    if dtype is torch.bfloat16:
+        code = BF16
+    elif dtype is torch.float32:
+        code = F32
+    else:
+        raise RandesError(UNSUPPORTED_DTYPE, "%s is %s: float32 or bfloat16 is wanted" % (what, dtype))
     if t.dim() != 2 or not t.is_cuda:
         _refuse("%s must be a 2-D CUDA tensor" % what)
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        _refuse("%s must have neighbouring columns (its last stride is %d)" % (what, t.stride(1)))
-    return code
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
+        _refuse("%s must have neighbouring columns (its last stride is %d)" % (what, step))
+    if rows <= 1:
+        stride = cols
+    elif stride < cols:
+        _refuse("the rows of %s overlap (row stride %d, %d columns)" % (what, stride, cols))
+    return code, rows, cols, stride
 
 
-def _row_stride(t) -> int:
-    s = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if s < 0 or (s < t.shape[1] and t.shape[0] > 1):
-        _refuse("rows overlap (row stride %d, %d columns)" % (s, t.shape[1]))
-    return s
-
-
-def _raw_stream(device) -> int:
+def _stream_of(t) -> int:
+    """The current stream of a CUDA tensor's device."""
     import torch
 
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _call(rc: int) -> None:
+    if rc:
+        raise RandesError(rc, randes_last_error())
+
+
+@functools.lru_cache(maxsize=4096)
+def _packed_size(rows: int, cols: int, group: int) -> int:
+    if group not in (32, 64, 128):
+        _refuse("group = %r is not 32, 64 or 128" % (group,))
+    nbytes = randes_packed_bytes(rows, cols, group)
+    if nbytes == 0 and rows * cols != 0:
+        _refuse("a matrix of [%d, %d] cannot be packed" % (rows, cols))
+    return nbytes
+
+
+_MatrixOne, _PtrOne = Matrix * 1, ctypes.c_void_p * 1
 
 
 class PackedMatrix:
@@ -470,73 +494,71 @@ class PackedMatrix:
         """The [rows, cols] values that the four bits stand for."""
         import torch
 
+        rows, cols = self.rows, self.cols
         if out is None:
-            out = torch.empty(self.rows, self.cols, dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=self.data.device)
+            out = torch.empty((rows, cols), dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=self.data.device)
+            stride = cols
         else:
-            out_dtype = _matrix_dtype(out, "out")
-            if tuple(out.shape) != (self.rows, self.cols):
-                _refuse("out is %s, the matrix [%d, %d]" % (list(out.shape), self.rows, self.cols))
-        randes_unpack((ctypes.c_void_p * 1)(self.address), 1, self.group, (Matrix * 1)(Matrix(out.data_ptr(), self.rows, self.cols, _row_stride(out))),
-                      out_dtype, _raw_stream(out.device))
+            out_dtype, r, c, stride = _rows_of(out, "out")
+            if (r, c) != (rows, cols):
+                _refuse("out is [%d, %d], the matrix [%d, %d]" % (r, c, rows, cols))
+        _call(lib().randes_unpack(_PtrOne(self.address), 1, self.group, _MatrixOne((out.data_ptr(), rows, cols, stride)), out_dtype,
+                                  _stream_of(out)))
         return out
 
 
-def _new_packed(shapes, group: int, device):
-    """PackedMatrix objects for [(rows, cols)]."""
+def _new_packed(rows: int, cols: int, group: int, device) -> PackedMatrix:
     import torch
 
-    if group not in (32, 64, 128):
-        _refuse("group = %r is not 32, 64 or 128" % (group,))
-    made = []
-    for r, c in shapes:
-        nbytes = randes_packed_bytes(r, c, group)
-        if nbytes == 0 and r * c != 0:
-            _refuse("a matrix of [%d, %d] cannot be packed" % (r, c))
-        made.append(PackedMatrix(r, c, group, torch.empty(nbytes, dtype=torch.uint8, device=device)))
-    return made
+    return PackedMatrix(rows, cols, group, torch.empty(_packed_size(rows, cols, group), dtype=torch.uint8, device=device))
 
 
 def pack(weights, group: int = 64):
     """Four-bit form of a weight, or of a list of weights of one type (2-D CUDA tensors, fp32 or bf16; rows may be strided)."""
     if not isinstance(weights, (list, tuple)):
-        return pack([weights], group)[0]
+        dtype, rows, cols, stride = _rows_of(weights, "the weight")
+        p = _new_packed(rows, cols, group, weights.device)
+        _call(lib().randes_pack(_MatrixOne((weights.data_ptr(), rows, cols, stride)), 1, dtype, group, _PtrOne(p.address), _stream_of(weights)))
+        return p
     if not weights:
         return []
-    dtypes = {_matrix_dtype(w, "a weight") for w in weights}
-    if len(dtypes) != 1 or len({w.device for w in weights}) != 1:
+    device, n = weights[0].device, len(weights)
+    shapes = [_rows_of(w, "a weight") for w in weights]
+    if len({s[0] for s in shapes}) != 1 or any(w.device != device for w in weights):
         _refuse("the weights of one call have one type and one device")
-    made = _new_packed([tuple(w.shape) for w in weights], group, weights[0].device)
-    n = len(weights)
-    mats = (Matrix * n)(*[Matrix(w.data_ptr(), w.shape[0], w.shape[1], _row_stride(w)) for w in weights])
-    randes_pack(mats, n, dtypes.pop(), group, (ctypes.c_void_p * n)(*[p.address for p in made]), _raw_stream(weights[0].device))
+    made = [_new_packed(r, c, group, device) for _, r, c, _ in shapes]
+    mats = (Matrix * n)(*[(w.data_ptr(), r, c, s) for w, (_, r, c, s) in zip(weights, shapes)])
+    randes_pack(mats, n, shapes[0][0], group, (ctypes.c_void_p * n)(*[p.address for p in made]), _stream_of(weights[0]))
     return made
 
 
-def _linear_output(x, rows: int, cols: int, y, y_dtype: int):
-    """(y, x's type, y's type) of a product of x [n_tokens, cols] with a [rows, cols] weight."""
+def _linear_tensors(x, rows: int, cols: int, y, y_dtype: int):
+    """(n_tokens, x's type and row stride, y, y's type and row stride) of a product of x [n_tokens, cols] with a [rows, cols] weight."""
     import torch
 
-    x_dtype = _matrix_dtype(x, "x")
-    if x.shape[1] != cols:
-        _refuse("x has %d columns, the weight %d" % (x.shape[1], cols))
+    x_dtype, n, c, x_stride = _rows_of(x, "x")
+    if c != cols:
+        _refuse("x has %d columns, the weight %d" % (c, cols))
     if y is None:
-        return torch.empty((x.shape[0], rows), dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=x.device), x_dtype, y_dtype
-    y_dtype = _matrix_dtype(y, "y")
-    if tuple(y.shape) != (x.shape[0], rows) or y.device != x.device:
-        _refuse("y is %s on %s, [%d, %d] on %s is wanted" % (list(y.shape), y.device, x.shape[0], rows, x.device))
-    return y, x_dtype, y_dtype
+        return n, x_dtype, x_stride, torch.empty((n, rows), dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=x.device), y_dtype, rows
+    y_dtype, yn, yr, y_stride = _rows_of(y, "y")
+    if (yn, yr) != (n, rows) or y.device != x.device:
+        _refuse("y is [%d, %d] on %s, [%d, %d] on %s is wanted" % (yn, yr, y.device, n, rows, x.device))
+    return n, x_dtype, x_stride, y, y_dtype, y_stride
 
 
 def packed_linear(x, w: PackedMatrix, y=None, y_dtype: int = F32):
     """x: [n_tokens, cols] fp32 or bf16 CUDA tensor (rows may be strided); returns y = x W^T [n_tokens, rows]."""
-    y, x_dtype, y_dtype = _linear_output(x, w.rows, w.cols, y, y_dtype)
-    randes_packed_linear(w.address, w.rows, w.cols, w.group, x, x_dtype, _row_stride(x), x.shape[0], y, y_dtype, _row_stride(y),
-                         _raw_stream(x.device))
+    rows, cols = w.rows, w.cols
+    n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, rows, cols, y, y_dtype)
+    _call(lib().randes_packed_linear(w.address, rows, cols, w.group, x.data_ptr(), x_dtype, x_stride, n, y.data_ptr(), y_dtype, y_stride,
+                                     _stream_of(x)))
     return y
 
 
 class TokenScores(NamedTuple):
-    """What token_scores returns; `stats` is what the backward call needs (row 0: greatest logit, row 1: log sum above it)."""
+    """What token_scores returns. ``stats`` [4, n] is what the backward call needs: rows logprob, entropy, greatest logit, log
+    of the sum of exponentials relative to it (of scale * logits)."""
 
     logprob: Any
     entropy: Any
@@ -545,11 +567,14 @@ class TokenScores(NamedTuple):
     top_logprobs: Any
 
 
-def _check_targets(targets, n: int, device):
+def _target_address(targets, n: int, device):
     import torch
 
-    if targets is not None and (targets.dtype != torch.int64 or tuple(targets.shape) != (n,) or not targets.is_contiguous() or targets.device != device):
+    if targets is None:
+        return None
+    if targets.dtype is not torch.int64 or targets.shape != (n,) or not targets.is_contiguous() or targets.device != device:
         _refuse("targets must be a contiguous int64 tensor [%d] on %s" % (n, device))
+    return targets.data_ptr()
 
 
 def token_scores(logits, targets=None, top_k: int = 0, scale: float = 1.0) -> TokenScores:
@@ -558,40 +583,51 @@ def token_scores(logits, targets=None, top_k: int = 0, scale: float = 1.0) -> To
     logits: [n, vocab] fp32 or bf16 CUDA tensor (rows may be strided); targets: int64 [n], negative = not scored."""
     import torch
 
-    dtype = _matrix_dtype(logits, "logits")
-    n, vocab = logits.shape
-    _check_targets(targets, n, logits.device)
+    dtype, n, vocab, stride = _rows_of(logits, "logits")
+    device = logits.device
+    target = _target_address(targets, n, device)
     if not 0 <= top_k <= 64:
         _refuse("top_k = %d is not in 0 .. 64" % top_k)
-    sums = torch.empty((4, n), dtype=torch.float32, device=logits.device)
-    at = sums.data_ptr()
+    stats = torch.empty((4, n), dtype=torch.float32, device=device)
+    at = stats.data_ptr()
     ids = tops = None
     if top_k:
-        ids = torch.empty((n, top_k), dtype=torch.int64, device=logits.device)
-        tops = torch.empty((n, top_k), dtype=torch.float32, device=logits.device)
-    randes_token_scores(logits, dtype, n, vocab, _row_stride(logits), targets, scale, top_k, at if targets is not None else None, at + 4 * n,
-                        at + 8 * n, ids, tops, _raw_stream(logits.device))
-    return TokenScores(sums[0] if targets is not None else None, sums[1], sums[2:], ids, tops)
+        ids = torch.empty((n, top_k), dtype=torch.int64, device=device)
+        tops = torch.empty((n, top_k), dtype=torch.float32, device=device)
+    _call(lib().randes_token_scores(logits.data_ptr(), dtype, n, vocab, stride, target, scale, top_k, at if target is not None else None, at + 4 * n,
+                                    at + 8 * n, ids.data_ptr() if top_k else None, tops.data_ptr() if top_k else None, _stream_of(logits)))
+    return TokenScores(stats.select(0, 0) if targets is not None else None, stats.select(0, 1), stats, ids, tops)
+
+
+def _row_gradient(g, what: str, n: int, device):
+    import torch
+
+    if g is None:
+        return None
+    if g.dtype is not torch.float32 or g.shape != (n,) or not g.is_contiguous() or g.device != device:
+        _refuse("%s must be a contiguous float32 tensor [%d] on %s" % (what, n, device))
+    return g.data_ptr()
 
 
 def token_scores_backward(logits, targets, scores: TokenScores, g_logprob=None, g_entropy=None, scale: float = 1.0, out=None):
     """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect to the logits; `out` may be the logits themselves."""
     import torch
 
-    dtype = _matrix_dtype(logits, "logits")
-    n, vocab = logits.shape
-    _check_targets(targets, n, logits.device)
-    for g, what in ((g_logprob, "g_logprob"), (g_entropy, "g_entropy"), (scores.entropy, "entropy")):
-        if g is not None and (g.dtype != torch.float32 or tuple(g.shape) != (n,) or not g.is_contiguous() or g.device != logits.device):
-            _refuse("%s must be a contiguous float32 tensor [%d] on %s" % (what, n, logits.device))
-    if tuple(scores.stats.shape) != (2, n) or not scores.stats.is_contiguous():
-        _refuse("stats are not those of %d rows" % n)
+    dtype, n, vocab, stride = _rows_of(logits, "logits")
+    device, stats = logits.device, scores.stats
+    target = _target_address(targets, n, device)
+    g_lp, g_h = _row_gradient(g_logprob, "g_logprob", n, device), _row_gradient(g_entropy, "g_entropy", n, device)
+    if stats.dtype is not torch.float32 or stats.shape != (4, n) or not stats.is_contiguous() or stats.device != device:
+        _refuse("the scores are not those of %d rows on %s" % (n, device))
     if out is None:
-        out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
-    elif _matrix_dtype(out, "out") != dtype or out.shape != logits.shape or out.device != logits.device:
-        _refuse("out must have the logits' shape, type and device")
-    randes_token_scores_backward(logits, dtype, n, vocab, _row_stride(logits), targets, scale, scores.stats, scores.entropy, g_logprob, g_entropy,
-                                 out, _row_stride(out), _raw_stream(logits.device))
+        out, out_stride = torch.empty((n, vocab), dtype=logits.dtype, device=device), vocab
+    else:
+        out_dtype, on, ov, out_stride = _rows_of(out, "out")
+        if (out_dtype, on, ov) != (dtype, n, vocab) or out.device != device:
+            _refuse("out must have the logits' shape, type and device")
+    at = stats.data_ptr()
+    _call(lib().randes_token_scores_backward(logits.data_ptr(), dtype, n, vocab, stride, target, scale, at + 8 * n, at + 4 * n, g_lp, g_h,
+                                             out.data_ptr(), out_stride, _stream_of(logits)))
     return out
 
 
@@ -781,9 +817,9 @@ class Plan:
         ``base`` is the list of all layers' weights; only the named ones are read."""
         layers = list(range(self.n_layers)) if layers is None else [self._layer(l) for l in layers]
         n = len(layers)
-        made = _new_packed([(self.rows[l], self.cols[l]) for l in layers], group, self.device)
+        made = [_new_packed(self.rows[l], self.cols[l], group, M.device) for l in layers]
         randes_retrieve_packed(self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, _as_ptrs(base), M, group,
-                               (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]), self._stream())
+                               (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]), _stream_of(M))
         return made
 
     def packed_linear(self, task_ids, lam: float, layer: int, x, packed_base: PackedMatrix, packed_m, y=None, y_dtype: int = F32):
@@ -806,12 +842,11 @@ class Plan:
                     _refuse("slot %d has groups of %d columns, the base of %d" % (l, p.group, group))
                 slots[l] = p.address
             packed_m = slots
-        y, x_dtype, y_dtype = _linear_output(x, rows, cols, y, y_dtype)
-        n = x.shape[0]
+        n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, rows, cols, y, y_dtype)
         if len(task_ids) != n:
             _refuse("%d task ids for %d tokens" % (len(task_ids), n))
         if not isinstance(task_ids, ctypes.Array):
             task_ids = (ctypes.c_uint32 * max(n, 1))(*task_ids)
-        randes_packed_linear_tasks(self.handle, lam, layer, group, task_ids, n, x, x_dtype, _row_stride(x), packed_base.address, packed_m, y,
-                                   y_dtype, _row_stride(y), self._stream())
+        _call(lib().randes_packed_linear_tasks(self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride, packed_base.address,
+                                               packed_m, y.data_ptr(), y_dtype, y_stride, _stream_of(x)))
         return y
