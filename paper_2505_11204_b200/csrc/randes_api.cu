@@ -1316,11 +1316,12 @@ int randes_linear_gated(const randes_plan_t* plan, uint32_t task_id, float lambd
 int randes_linear_giveups(unsigned int* count)
 {
     if (!count) return fail(RANDES_INVALID_ARGUMENT, "count is NULL");
-    unsigned int packed = 0;
+    unsigned int packed = 0, wide = 0;
     int e = linear_giveups(count);
     if (!e) e = packed_giveups(&packed);
+    if (!e) e = packed_wide_giveups(&wide);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "read of the give-up counter");
-    *count += packed;
+    *count += packed + wide;
     return RANDES_OK;
 }
 
@@ -1676,7 +1677,10 @@ int randes_retrieve_packed_impl(const randes_plan_t* plan, uint32_t task_id, flo
     return RANDES_OK;
 }
 
-// What both products check, and their token blocks of 64. `fill(a, first)` sets the segments of the tokens first .. .
+int launch(PackedLinearArgs<kNarrowTokens>& a, bool x_bf16, const Device& d, void* stream) { return launch_packed_linear(a, x_bf16, d.sms, d.index, stream); }
+int launch(PackedLinearArgs<kWideTokens>& a, bool x_bf16, const Device& d, void* stream) { return launch_packed_wide(a, x_bf16, d.sms, d.index, stream); }
+
+// What both products check, and their token blocks. `fill(a, first)` sets the segments of the tokens first .. .
 template <typename Fill>
 int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, int x_dtype, uint64_t x_stride, uint32_t n_tokens, void* y,
                   int y_dtype, uint64_t y_stride, float lambda, void* stream, Fill&& fill)
@@ -1690,23 +1694,34 @@ int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, i
         return fail(RANDES_INVALID_ARGUMENT, "y overlaps x");
     Device dev;
     if ((rc = current_device(&dev))) return rc;
-    PackedLinearArgs a;
-    a.x_stride = x_stride;
-    a.y_stride = y_stride;
-    a.rows = rows;
-    a.cols = cols;
-    a.group = group;
-    a.x_vec = rows_aligned(x, n_tokens, x_stride, xe);
-    a.y_bf16 = y_dtype == RANDES_BF16;
-    a.lambda = lambda;
-    for (uint32_t first = 0; first < n_tokens; first += kPackedTokens) {
+    auto run = [&](auto& a, uint32_t first, uint32_t n) {
         a.x = static_cast<const char*>(x) + first * x_stride * xe;
         a.y = static_cast<char*>(y) + first * y_stride * ye;
-        a.n_tokens = std::min(kPackedTokens, n_tokens - first);
+        a.x_stride = x_stride;
+        a.y_stride = y_stride;
+        a.rows = rows;
+        a.cols = cols;
+        a.group = group;
+        a.n_tokens = n;
+        a.x_vec = rows_aligned(x, n_tokens, x_stride, xe);
+        a.y_bf16 = y_dtype == RANDES_BF16;
+        a.lambda = lambda;
         fill(a, first);
-        const int e = launch_packed_linear(a, x_dtype == RANDES_BF16, dev.sms, dev.index, stream);
+        const int e = launch(a, x_dtype == RANDES_BF16, dev, stream);
         if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the packed linear kernel");
         ++g_launches;
+        return static_cast<int>(RANDES_OK);
+    };
+    for (uint32_t first = 0, n; first < n_tokens; first += n) {
+        n = std::min(kWideTokens, n_tokens - first);
+        if (n > kNarrowTokens) {
+            PackedLinearArgs<kWideTokens> a;
+            rc = run(a, first, n);
+        } else {
+            PackedLinearArgs<kNarrowTokens> a;
+            rc = run(a, first, n);
+        }
+        if (rc) return rc;
     }
     return RANDES_OK;
 }
@@ -1721,7 +1736,7 @@ int randes_packed_linear_impl(const void* packed, uint32_t rows, uint32_t cols, 
     if (cols && (rc = check_packed(packed, "packed"))) return rc;
     if (overlap(packed, randes_packed_bytes(rows, cols, group), y, span_bytes(n_tokens, rows, y_stride, elem_size(y_dtype))))
         return fail(RANDES_INVALID_ARGUMENT, "y overlaps packed");
-    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, 0.f, stream, [&](PackedLinearArgs& a, uint32_t) {
+    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, 0.f, stream, [&](auto& a, uint32_t) {
         a.n_seg = 1;
         a.seg[0] = PackedSegment{packed, 0, a.n_tokens, 0, 0};
         for (uint32_t b = 0; b < a.n_tokens; ++b) a.token[b] = static_cast<uint8_t>(b);
@@ -1758,11 +1773,11 @@ int randes_packed_linear_tasks_impl(const randes_plan_t* plan, float lambda, uin
             if (overlap(packed_m[slot], p_bytes, y, y_bytes)) return fail(RANDES_INVALID_ARGUMENT, "y overlaps packed_m[%u]", slot);
         }
     }
-    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, lambda, stream, [&](PackedLinearArgs& a, uint32_t first) {
+    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, lambda, stream, [&](auto& a, uint32_t first) {
         const uint32_t n = a.n_tokens;
         a.seg[0] = PackedSegment{packed_base, 0, n, 0, 0};
-        uint32_t n_task = 0, slot_of[kPackedTokens];
-        int row_of[kPackedTokens];
+        uint32_t n_task = 0, slot_of[kWideTokens];
+        int row_of[kWideTokens];
         for (uint32_t b = 0; b < n; ++b) {
             uint32_t k = 0;
             while (k < n_task && row_of[k] != task_row[first + b]) ++k;

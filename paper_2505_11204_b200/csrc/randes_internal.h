@@ -258,13 +258,15 @@ struct UnpackArgs {
     UnpackMatrix mat[kPackBatch];
     uint32_t n, group;
 };
-constexpr uint32_t kPackedTokens = 8;    // tokens per launch of the product
 // One packed matrix and the tokens that go through it: positions first .. first + count - 1 of the token lists.
 struct PackedSegment {
     const void* packed;
     uint32_t first, count, slot, flip;
 };
-struct PackedLinearArgs {
+// Tokens per launch of the two product kernels: sums per warp on the small tensor-core instruction (few tokens), or tiles of
+// 128 rows with accumulators in tensor memory.
+constexpr uint32_t kNarrowTokens = 8, kWideTokens = 64;
+template <uint32_t TOKENS> struct PackedLinearArgs {
     const void* x;
     void* y;
     uint64_t x_stride, y_stride;  // elements between tokens
@@ -274,17 +276,20 @@ struct PackedLinearArgs {
     uint32_t ring_at;                            // and where the rings start in shared memory
     uint32_t x_vec, y_bf16;
     float lambda;
-    uint8_t token[2 * kPackedTokens];        // per position: the token
-    uint8_t token_task[2 * kPackedTokens];   // per position: its entry in `task`
-    uint8_t pos_of_token[kPackedTokens];     // the token's position in its slot's list
-    DevTask task[kPackedTokens];             // the distinct tasks of the launch
-    PackedSegment seg[1 + kPackedTokens];    // the base, then each distinct slot
+    uint8_t token[2 * TOKENS];        // per position: the token
+    uint8_t token_task[2 * TOKENS];   // per position: its entry in `task`
+    uint8_t pos_of_token[TOKENS];     // the token's position in its slot's list
+    DevTask task[TOKENS];             // the distinct tasks of the launch
+    PackedSegment seg[1 + TOKENS];    // the base, then each distinct slot
 };
 // All return a cudaError_t as int.
 int launch_pack(int w_dtype, int m_dtype, bool retrieve, PackArgs& a, void* stream);
 int launch_unpack(int out_dtype, UnpackArgs& a, void* stream);
 int packed_giveups(unsigned int* count);   // warps of the product that gave up on a bounded wait (synchronises)
-int launch_packed_linear(PackedLinearArgs& a, bool x_bf16, int sm_count, int device, void* stream);
+int launch_packed_linear(PackedLinearArgs<kNarrowTokens>& a, bool x_bf16, int sm_count, int device, void* stream);
+// randes_packed_wide.cu
+int launch_packed_wide(PackedLinearArgs<kWideTokens>& a, bool x_bf16, int sm_count, int device, void* stream);
+int packed_wide_giveups(unsigned int* count);
 
 // randes_scores.cu: log probabilities, entropy and top alternatives of logits, and their gradient.
 constexpr uint32_t kMaxTop = 64;

@@ -26,8 +26,7 @@
 #include <atomic>
 #include <cstring>
 
-#include "randes_device.cuh"
-#include "randes_internal.h"
+#include "randes_packed.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -50,28 +49,6 @@ __device__ __forceinline__ float quotient(float w, float s, float inv)
 {
     const float q = w * inv;
     return __fmaf_rn(__fmaf_rn(-q, s, w), inv, q);
-}
-
-// The four operand registers of one word of codes, as q / 64. A code left in the low byte of a bf16 is a number too: bf16
-// counts in steps of 2^-133 through its whole first two binades, so bits 0-3 read u 2^-133 and bits 4-7 read 16 u 2^-133
-// (u = q + 8). One exact multiply-add brings either to u / 64 - 1/8. So a word takes one shift instead of three, and no
-// bias has to be put in. Parts of 1/64, not units: a product with an activation cannot overflow where the weight itself
-// (q s, with s << 1) would not; the factor comes back with the partial sums.
-constexpr float kCodeUnit = 64.f;
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c)
-{
-    uint32_t r;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
-__device__ __forceinline__ void decode(uint32_t word, uint32_t (&a)[4])
-{
-    constexpr uint32_t k127 = 0x7F007F00u, k123 = 0x7D007D00u, kOff = 0xBE00BE00u;    // 2^127, 2^123, -1/8, twice each
-    const uint32_t high = word >> 8;
-    a[0] = fma_bf16x2(word & 0x000F000Fu, k127, kOff);
-    a[1] = fma_bf16x2(word & 0x00F000F0u, k123, kOff);
-    a[2] = fma_bf16x2(high & 0x000F000Fu, k127, kOff);
-    a[3] = fma_bf16x2(high & 0x00F000F0u, k123, kOff);
 }
 
 // Eight neighbouring columns of one row as they lie in memory.
@@ -315,93 +292,6 @@ __device__ __forceinline__ void mma_16816_first(float (&d)[4], const uint32_t (&
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
-// Activations: a lane's eight neighbouring columns of one token, as loaded and as four words of bf16 pairs. An fp32
-// activation becomes three bf16 terms by truncation (8 + 8 + 8 bits: their sum is the fp32 value exactly, down to where the
-// last term underflows), so that products and sums keep fp32's accuracy on the bf16 tensor core.
-template <typename XT> struct Acts;
-template <> struct Acts<bf16> {
-    static constexpr int kTerms = 1;
-    struct Raw { uint4 r[1]; };
-    static __device__ __forceinline__ Raw words(const bf16* p) { return Raw{{__ldg(reinterpret_cast<const uint4*>(p))}}; }
-    static __device__ __noinline__ Raw gather(const bf16* p, uint32_t c, uint32_t cols)      // element by element
-    {
-        const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t lo = c + 2 * e < cols ? __ldg(q + c + 2 * e) : 0u, hi = c + 2 * e + 1 < cols ? __ldg(q + c + 2 * e + 1) : 0u;
-            w[e] = lo | (hi << 16);
-        }
-        return Raw{{make_uint4(w[0], w[1], w[2], w[3])}};
-    }
-    static __device__ __forceinline__ Raw zero() { return Raw{{make_uint4(0, 0, 0, 0)}}; }
-    static __device__ __forceinline__ void terms(const Raw& v, uint32_t (&w)[1][4])
-    {
-        w[0][0] = v.r[0].x; w[0][1] = v.r[0].y; w[0][2] = v.r[0].z; w[0][3] = v.r[0].w;
-    }
-};
-template <> struct Acts<float> {
-    static constexpr int kTerms = 3;
-    struct Raw { uint4 r[2]; };
-    static __device__ __forceinline__ Raw words(const float* p)
-    {
-        return Raw{{__ldg(reinterpret_cast<const uint4*>(p)), __ldg(reinterpret_cast<const uint4*>(p) + 1)}};
-    }
-    static __device__ __noinline__ Raw gather(const float* p, uint32_t c, uint32_t cols)
-    {
-        uint32_t w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = c + e < cols ? __float_as_uint(__ldg(p + c + e)) : 0u;
-        return Raw{{make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7])}};
-    }
-    static __device__ __forceinline__ Raw zero() { return Raw{{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)}}; }
-    static __device__ __forceinline__ void terms(const Raw& v, uint32_t (&w)[3][4])
-    {
-        float f[8] = {__uint_as_float(v.r[0].x), __uint_as_float(v.r[0].y), __uint_as_float(v.r[0].z), __uint_as_float(v.r[0].w),
-                      __uint_as_float(v.r[1].x), __uint_as_float(v.r[1].y), __uint_as_float(v.r[1].z), __uint_as_float(v.r[1].w)};
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float a = f[2 * e], b = f[2 * e + 1];
-                w[k][e] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-                const float ta = __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), tb = __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
-                f[2 * e] = a == ta ? 0.f : a - ta;           // the comparison keeps an infinity out of the lower terms
-                f[2 * e + 1] = b == tb ? 0.f : b - tb;
-            }
-        }
-    }
-};
-
-// ---- the ring of bulk copies
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-__device__ __forceinline__ void bar_init(uint32_t bar) { asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-constexpr uint32_t kWaitLimit = 1u << 22;       // tries (each may sleep): seconds, far beyond any copy
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity)
-{
-    for (uint32_t i = 0; i < kWaitLimit; ++i)
-        if (bar_try(bar, parity)) return true;
-    return false;
-}
-
 constexpr int kTiles = 2;                        // column tiles per stage
 constexpr int kDepth = 2;                        // stages of a warp's ring
 constexpr int kRowTiles = 4;                     // row tiles a warp takes along: one row block
@@ -417,7 +307,7 @@ constexpr int kRows = 16 * kRowTiles;
 // no warp waits for another until the end. Its sums of one segment stay in registers until its run leaves the segment. All partial sums meet in shared memory, those of a cluster's CTAs through distributed
 // shared memory, and are added in a fixed order: results do not depend on timing.
 template <typename XT, int GROUP>
-__global__ void __launch_bounds__(kMulWarps * 32, 2) packed_linear_kernel(const __grid_constant__ PackedLinearArgs a)
+__global__ void __launch_bounds__(kMulWarps * 32, 2) packed_linear_kernel(const __grid_constant__ PackedLinearArgs<kNarrowTokens> a)
 {
     typedef Acts<XT> Act;
     constexpr bool HALF = GROUP == 32;
@@ -618,7 +508,7 @@ __global__ void __launch_bounds__(kMulWarps * 32, 2) packed_linear_kernel(const 
     }
 }
 
-template <typename XT, int GROUP> cudaError_t launch_mul(PackedLinearArgs& a, int sm_count, int device, cudaStream_t s)
+template <typename XT, int GROUP> cudaError_t launch_mul(PackedLinearArgs<kNarrowTokens>& a, int sm_count, int device, cudaStream_t s)
 {
     const PackedLayout lay(a.rows, a.cols, a.group);
     const uint64_t total = static_cast<uint64_t>(lay.col_blocks) * a.n_seg, blocks = (a.rows + kRows - 1) / kRows;
@@ -651,7 +541,7 @@ template <typename XT, int GROUP> cudaError_t launch_mul(PackedLinearArgs& a, in
     return cudaLaunchKernelEx(&cfg, packed_linear_kernel<XT, GROUP>, a);
 }
 
-template <typename XT> cudaError_t launch_group(PackedLinearArgs& a, int sm_count, int device, cudaStream_t s)
+template <typename XT> cudaError_t launch_group(PackedLinearArgs<kNarrowTokens>& a, int sm_count, int device, cudaStream_t s)
 {
     if (a.group == 32) return launch_mul<XT, 32>(a, sm_count, device, s);
     if (a.group == 64) return launch_mul<XT, 64>(a, sm_count, device, s);
@@ -660,7 +550,7 @@ template <typename XT> cudaError_t launch_group(PackedLinearArgs& a, int sm_coun
 
 }  // namespace
 
-int launch_packed_linear(PackedLinearArgs& a, bool x_bf16, int sm_count, int device, void* stream)
+int launch_packed_linear(PackedLinearArgs<kNarrowTokens>& a, bool x_bf16, int sm_count, int device, void* stream)
 {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return static_cast<int>(x_bf16 ? launch_group<bf16>(a, sm_count, device, s) : launch_group<float>(a, sm_count, device, s));
