@@ -488,13 +488,17 @@ int randes_retrieve_packed(const randes_plan_t* plan, uint32_t task_id, float la
  * A few tokens through a packed matrix:  y[b][r] = sum_c x[b][c] * q[r][c] s[r][c / group].
  *   x, x_dtype, x_stride   device [n_tokens, cols], fp32 or bf16, x_stride elements between tokens (>= cols)
  *   y, y_dtype, y_stride   device [n_tokens, rows] likewise; must not overlap the inputs
+ *   workspace, workspace_bytes   device memory, 16-byte aligned, at least randes_packed_linear_workspace() bytes: none for up
+ *                 to 8 tokens; for more, the activations laid out for the tensor core.  Free again when the call's work is done
  * Products are exact (an fp32 activation is taken as the sum of three bf16 terms), sums run in fp32 in a fixed order, a
- * bf16 y is rounded once.  The matrix is read once per 64 tokens (one kernel launch each); meant for few tokens -- for many,
- * retrieve the weight and use a dense product.  16-byte aligned tokens are read fastest.
- * Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, CUDA_ERROR.
+ * bf16 y is rounded once.  The matrix is read once per 64 tokens; one kernel launch for up to 8 tokens, two per 64 beyond.
+ * Meant for few tokens -- for many, retrieve the weight and use a dense product.  16-byte aligned tokens are read fastest.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, WORKSPACE_TOO_SMALL, CUDA_ERROR.
  */
+size_t randes_packed_linear_workspace(uint32_t cols, randes_dtype_t x_dtype, uint32_t n_tokens, int with_tasks);   /* host-only */
 int randes_packed_linear(const void* packed, uint32_t rows, uint32_t cols, uint32_t group, const void* x, randes_dtype_t x_dtype,
-                         uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream);
+                         uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 /*
  * A few tokens, each of its own task, through one layer kept as packed base and packed superposition (Section 4, second
@@ -504,11 +508,13 @@ int randes_packed_linear(const void* packed, uint32_t rows, uint32_t cols, uint3
  *   task_ids[n_tokens]   HOST array, copied; ids may repeat
  *   packed_base          layer p of W_0 packed with `group`
  *   packed_m[n_layers]   HOST array: slot l of M packed with `group` (entries of slots that no token uses may be NULL)
- * Otherwise as randes_packed_linear.  Needs no workspace.  Errors: those of randes_packed_linear, plus UNKNOWN_TASK.
+ * Otherwise as randes_packed_linear (with_tasks = 1 for its workspace; the plan itself may have been built without one).
+ * Errors: those of randes_packed_linear, plus UNKNOWN_TASK.
  */
 int randes_packed_linear_tasks(const randes_plan_t* plan, float lambda, uint32_t layer, uint32_t group, const uint32_t* task_ids,
                                uint32_t n_tokens, const void* x, randes_dtype_t x_dtype, uint64_t x_stride, const void* packed_base,
-                               const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream);
+                               const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* workspace,
+                               size_t workspace_bytes, void* stream);
 
 /*
  * What a model answers: log probabilities of given tokens, entropy, and the top alternatives (the paper's language models

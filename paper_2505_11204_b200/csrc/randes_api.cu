@@ -1677,15 +1677,29 @@ int randes_retrieve_packed_impl(const randes_plan_t* plan, uint32_t task_id, flo
     return RANDES_OK;
 }
 
-int launch(PackedLinearArgs<kNarrowTokens>& a, bool x_bf16, const Device& d, void* stream) { return launch_packed_linear(a, x_bf16, d.sms, d.index, stream); }
-int launch(PackedLinearArgs<kWideTokens>& a, bool x_bf16, const Device& d, void* stream) { return launch_packed_wide(a, x_bf16, d.sms, d.index, stream); }
+int launch(PackedLinearArgs<kNarrowTokens>& a, bool x_bf16, const Device& d, int* launched, void* stream)
+{
+    const int e = launch_packed_linear(a, x_bf16, d.sms, d.index, stream);
+    *launched = e ? 0 : 1;
+    return e;
+}
+int launch(PackedLinearArgs<kWideTokens>& a, bool x_bf16, const Device& d, int* launched, void* stream)
+{
+    return launch_packed_wide(a, x_bf16, d.sms, d.index, launched, stream);
+}
 
 // What both products check, and their token blocks. `fill(a, first)` sets the segments of the tokens first .. .
 template <typename Fill>
 int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, int x_dtype, uint64_t x_stride, uint32_t n_tokens, void* y,
-                  int y_dtype, uint64_t y_stride, float lambda, void* stream, Fill&& fill)
+                  int y_dtype, uint64_t y_stride, float lambda, bool tasks, void* workspace, size_t workspace_bytes, void* stream, Fill&& fill)
 {
     int rc;
+    const size_t need = packed_wide_workspace(cols, x_dtype == RANDES_BF16, n_tokens, tasks);
+    if (need) {
+        if (!workspace || workspace_bytes < need)
+            return fail(RANDES_WORKSPACE_TOO_SMALL, "%u tokens of %u columns need a workspace of %zu bytes, got %zu", n_tokens, cols, need, workspace ? workspace_bytes : 0);
+        if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(RANDES_MISALIGNED, "workspace = %p is not 16-byte aligned", workspace);
+    }
     const size_t xe = elem_size(x_dtype), ye = elem_size(y_dtype);
     if ((rc = check_tensor(x, n_tokens, cols, x_stride, xe, "x")) || (rc = check_tensor(y, n_tokens, rows, y_stride, ye, "y"))) return rc;
     // (strided tensors may interleave without sharing an element; dense ones are compared)
@@ -1707,9 +1721,11 @@ int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, i
         a.y_bf16 = y_dtype == RANDES_BF16;
         a.lambda = lambda;
         fill(a, first);
-        const int e = launch(a, x_dtype == RANDES_BF16, dev, stream);
+        int launched = 0;
+        a.operands = workspace;
+        const int e = launch(a, x_dtype == RANDES_BF16, dev, &launched, stream);
+        g_launches += launched;
         if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the packed linear kernel");
-        ++g_launches;
         return static_cast<int>(RANDES_OK);
     };
     for (uint32_t first = 0, n; first < n_tokens; first += n) {
@@ -1727,7 +1743,8 @@ int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, i
 }
 
 int randes_packed_linear_impl(const void* packed, uint32_t rows, uint32_t cols, uint32_t group, const void* x, randes_dtype_t x_dtype,
-                              uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream)
+                              uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* workspace,
+                              size_t workspace_bytes, void* stream)
 {
     int rc;
     if ((rc = check_dtype(x_dtype, "activation")) || (rc = check_dtype(y_dtype, "output")) || (rc = check_group(group))) return rc;
@@ -1736,7 +1753,7 @@ int randes_packed_linear_impl(const void* packed, uint32_t rows, uint32_t cols, 
     if (cols && (rc = check_packed(packed, "packed"))) return rc;
     if (overlap(packed, randes_packed_bytes(rows, cols, group), y, span_bytes(n_tokens, rows, y_stride, elem_size(y_dtype))))
         return fail(RANDES_INVALID_ARGUMENT, "y overlaps packed");
-    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, 0.f, stream, [&](auto& a, uint32_t) {
+    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, 0.f, false, workspace, workspace_bytes, stream, [&](auto& a, uint32_t) {
         a.n_seg = 1;
         a.seg[0] = PackedSegment{packed, 0, a.n_tokens, 0, 0};
         for (uint32_t b = 0; b < a.n_tokens; ++b) a.token[b] = static_cast<uint8_t>(b);
@@ -1745,7 +1762,8 @@ int randes_packed_linear_impl(const void* packed, uint32_t rows, uint32_t cols, 
 
 int randes_packed_linear_tasks_impl(const randes_plan_t* plan, float lambda, uint32_t layer, uint32_t group, const uint32_t* task_ids,
                                     uint32_t n_tokens, const void* x, randes_dtype_t x_dtype, uint64_t x_stride, const void* packed_base,
-                                    const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream)
+                                    const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* workspace,
+                                    size_t workspace_bytes, void* stream)
 {
     if (!plan) return fail(RANDES_INVALID_ARGUMENT, "plan is NULL");
     if (plan->has_gauss) return fail(RANDES_INVALID_ARGUMENT, "not offered for plans with a RANDES_GAUSS group");
@@ -1773,7 +1791,7 @@ int randes_packed_linear_tasks_impl(const randes_plan_t* plan, float lambda, uin
             if (overlap(packed_m[slot], p_bytes, y, y_bytes)) return fail(RANDES_INVALID_ARGUMENT, "y overlaps packed_m[%u]", slot);
         }
     }
-    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, lambda, stream, [&](auto& a, uint32_t first) {
+    return packed_linear(rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, lambda, true, workspace, workspace_bytes, stream, [&](auto& a, uint32_t first) {
         const uint32_t n = a.n_tokens;
         a.seg[0] = PackedSegment{packed_base, 0, n, 0, 0};
         uint32_t n_task = 0, slot_of[kWideTokens];
@@ -1891,21 +1909,28 @@ int randes_retrieve_packed(const randes_plan_t* plan, uint32_t task_id, float la
     return guarded("randes_retrieve_packed", [&] { return randes_retrieve_packed_impl(plan, task_id, lambda, layers, n, base, M, group, packed, stream); });
 }
 
+size_t randes_packed_linear_workspace(uint32_t cols, randes_dtype_t x_dtype, uint32_t n_tokens, int with_tasks)
+{
+    return packed_wide_workspace(cols, x_dtype == RANDES_BF16, n_tokens, with_tasks != 0);
+}
+
 int randes_packed_linear(const void* packed, uint32_t rows, uint32_t cols, uint32_t group, const void* x, randes_dtype_t x_dtype,
-                         uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream)
+                         uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* workspace,
+                         size_t workspace_bytes, void* stream)
 {
     return guarded("randes_packed_linear", [&] {
-        return randes_packed_linear_impl(packed, rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, stream);
+        return randes_packed_linear_impl(packed, rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, workspace, workspace_bytes, stream);
     });
 }
 
 int randes_packed_linear_tasks(const randes_plan_t* plan, float lambda, uint32_t layer, uint32_t group, const uint32_t* task_ids,
                                uint32_t n_tokens, const void* x, randes_dtype_t x_dtype, uint64_t x_stride, const void* packed_base,
-                               const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* stream)
+                               const void* const* packed_m, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* workspace,
+                               size_t workspace_bytes, void* stream)
 {
     return guarded("randes_packed_linear_tasks", [&] {
         return randes_packed_linear_tasks_impl(plan, lambda, layer, group, task_ids, n_tokens, x, x_dtype, x_stride, packed_base, packed_m, y,
-                                               y_dtype, y_stride, stream);
+                                               y_dtype, y_stride, workspace, workspace_bytes, stream);
     });
 }
 

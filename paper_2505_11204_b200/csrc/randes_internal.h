@@ -281,6 +281,8 @@ template <uint32_t TOKENS> struct PackedLinearArgs {
     uint8_t pos_of_token[TOKENS];     // the token's position in its slot's list
     DevTask task[TOKENS];             // the distinct tasks of the launch
     PackedSegment seg[1 + TOKENS];    // the base, then each distinct slot
+    void* operands;                   // wide form only: the activations as operand tiles, in the caller's workspace
+    uint16_t operand_at[1 + TOKENS];  // per segment: rows of operand tiles before it (set by the launcher)
 };
 // All return a cudaError_t as int.
 int launch_pack(int w_dtype, int m_dtype, bool retrieve, PackArgs& a, void* stream);
@@ -288,7 +290,8 @@ int launch_unpack(int out_dtype, UnpackArgs& a, void* stream);
 int packed_giveups(unsigned int* count);   // warps of the product that gave up on a bounded wait (synchronises)
 int launch_packed_linear(PackedLinearArgs<kNarrowTokens>& a, bool x_bf16, int sm_count, int device, void* stream);
 // randes_packed_wide.cu
-int launch_packed_wide(PackedLinearArgs<kWideTokens>& a, bool x_bf16, int sm_count, int device, void* stream);
+size_t packed_wide_workspace(uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks);     // bytes for calls of that many tokens
+int launch_packed_wide(PackedLinearArgs<kWideTokens>& a, bool x_bf16, int sm_count, int device, int* launched, void* stream);
 int packed_wide_giveups(unsigned int* count);
 
 // randes_scores.cu: log probabilities, entropy and top alternatives of logits, and their gradient.

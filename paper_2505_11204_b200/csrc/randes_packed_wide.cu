@@ -6,12 +6,15 @@
 // rows and a contiguous run of column blocks over all segments (see randes_packed.cu for segments); the CTAs of a cluster
 // share the rows and meet through distributed shared memory.
 //
-//   warps 0-7  workers. Per tile of 64 columns a warp decodes 16 rows of codes into the A operand (K-major, 128-byte
-//              swizzle), all of them bring the tokens' activations into the B operand (signs applied; an fp32 activation
-//              as three bf16 terms), then they take the group sums of the tile before out of tensor memory: a thread owns
-//              one row and half the tokens.
-//   warp 8     copies the records (one lane, bulk copies, two stages of 128 columns), owns tensor memory.
-//   warp 9     issues tcgen05.mma (one lane): M = 128 rows, N = tokens of the segment rounded up to 16.
+// The activations are the same for every block of rows, so a first kernel lays them out once as operand B in the caller's
+// workspace (signs applied; an fp32 activation as three bf16 terms), one tile of 64 columns after the other, swizzled as
+// the tensor core wants them. The product kernel has one CTA per SM, whose warps keep to one task each:
+//   warps 0-7    group sums: a thread owns one row and half the tokens
+//   warps 8-15   operand A: codes to bf16 (K-major, 128-byte swizzle), 16 rows each
+//   warp 16      copies records (one lane, bulk copies), owns tensor memory
+//   warp 17      issues tcgen05.mma (one lane): M = 128 rows, N = tokens of the segment rounded up to 16
+//   warp 18      copies operand B (one lane, bulk copies)
+// A hand-over between roles costs hundreds of cycles however little it hands over, so a stage is 128 columns.
 //
 // Every wait is bounded; a CTA whose wait runs out raises a flag, all roles leave, what is in flight is waited for, tensor
 // memory is freed, its sums become NaN and a device counter records the event.
@@ -32,10 +35,10 @@ namespace {
 
 using namespace device;
 
-constexpr int kWorkers = 8;                        // warps
-constexpr int kThreads = (kWorkers + 2) * 32;
+constexpr int kSumWarps = 8, kAWarps = 8;
+constexpr int kAFirst = kSumWarps, kCopyWarp = kAFirst + kAWarps, kMmaWarp = kCopyWarp + 1, kCopyBWarp = kMmaWarp + 1;
+constexpr int kThreads = (kCopyBWarp + 1) * 32;
 constexpr uint32_t kTileRows = 128;
-constexpr uint32_t kRecStages = 2, kOpStages = 2, kAccs = 4;
 constexpr uint32_t kATile = kTileRows * 128;       // 128 rows x 64 bf16
 
 // ---- mbarriers with any count, bounded waits that also end when the CTA has given up
@@ -74,6 +77,12 @@ __device__ __forceinline__ void tc_load16(uint32_t addr, uint32_t* v)
           "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(addr) : "memory");
 }
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 // K-major operand of 64 bf16 columns (128 bytes) per row with the 128-byte swizzle: 16-byte chunk c of row r lies at
 // chunk c ^ (r % 8) of its row; groups of eight rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr)
@@ -89,21 +98,61 @@ template <int NT, typename XT, int GROUP> struct Wide {
     static constexpr uint32_t kCodeBytes = kBlockTiles * 4 * 512, kRecord = kCodeBytes + (HALF ? 256 : 128);
     static constexpr uint32_t kUnitBytes = 2 / kBlockTiles * kRecord;       // 64 rows x 128 columns
     static constexpr uint32_t kBTile = NT * 128;
-    static constexpr uint32_t kOpBytes = kATile + kTerms * kBTile;
+    static constexpr uint32_t kBAt = 2 * kATile;                            // a stage: two tiles of A, then two of B
+    static constexpr uint32_t kOpBytes = kBAt + 2 * kTerms * kBTile;
+    static constexpr uint32_t kOpStages = kTerms == 3 ? 2 : 3, kRecStages = kTerms == 3 && NT == 64 ? 2 : 3;
+    static constexpr uint32_t kAccs = 256 / NT;
     static constexpr uint32_t kOpsAt = 0;                                   // 1024-byte aligned operands first
     static constexpr uint32_t kRecAt = kOpsAt + kOpStages * kOpBytes;
     static constexpr uint32_t kBarsAt = kRecAt + kRecStages * 2 * kUnitBytes;
     static constexpr uint32_t kYAt = kBarsAt + 256;
-    static constexpr uint32_t kTmem = kAccs * NT;
+    static_assert(kYAt + NT * kTileRows * 4 + 1024 <= 227 * 1024, "shared memory of a CTA");
+    static constexpr uint32_t kTmem = 256;
     static size_t smem(uint32_t n_tokens) { return 1024 + kYAt + static_cast<size_t>(n_tokens) * kTileRows * sizeof(float); }
 };
 
+// Rows of operand B that a segment with that many tokens takes up: whole groups of eight, the swizzle's period. (Rows that
+// no token fills are whatever was there: their columns of the product go nowhere.)
+__host__ __device__ constexpr uint32_t operand_rows(uint32_t count) { return (count + 7) / 8 * 8; }
+
+// One thread per position of the token lists and eight columns.
+template <typename XT>
+__global__ void __launch_bounds__(256) operand_kernel(const __grid_constant__ PackedLinearArgs<kWideTokens> a)
+{
+    typedef Acts<XT> Act;
+    const uint32_t kts = (a.cols + 63) / 64, chunk = blockIdx.x * 256 + threadIdx.x, pos = blockIdx.y;
+    if (chunk >= kts * 8) return;
+    uint32_t seg = 0;
+    while (pos >= a.seg[seg].first + a.seg[seg].count) ++seg;
+    const uint32_t row = pos - a.seg[seg].first, rows = operand_rows(a.seg[seg].count), c = chunk * 8;
+    const XT* x = static_cast<const XT*>(a.x) + a.token[pos] * a.x_stride;
+    typename Act::Raw raw;
+    if (a.x_vec && c + 8 <= a.cols) raw = Act::words(x + c);
+    else raw = c < a.cols ? Act::gather(x, c, a.cols) : Act::zero();
+    uint32_t w[Act::kTerms][4];
+    Act::terms(raw, w);
+    if (a.seg[seg].flip) {
+        const DevTask task = a.task[a.token_task[pos]];
+        const uint4 blk = philox4x32_10(c >> 7, a.seg[seg].slot, kTagSign, task.id, task.key0, task.key1);
+        const uint32_t q = (c >> 5) & 3u, word = q == 0 ? blk.x : (q == 1 ? blk.y : (q == 2 ? blk.z : blk.w)), byte = (word >> (c & 31)) & 0xFFu;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t mask = (byte * ((1u << (15 - 2 * e)) + (1u << (30 - 2 * e)))) & 0x80008000u;
+#pragma unroll
+            for (int k = 0; k < Act::kTerms; ++k) w[k][e] ^= mask;
+        }
+    }
+    char* to = static_cast<char*>(a.operands) + a.operand_at[seg] * (static_cast<size_t>(kts) * 128 * Act::kTerms) +
+               static_cast<size_t>(chunk >> 3) * rows * 128 * Act::kTerms + row * 128 + (((chunk & 7) ^ (row & 7)) * 16);
+#pragma unroll
+    for (int k = 0; k < Act::kTerms; ++k) *reinterpret_cast<uint4*>(to + static_cast<size_t>(k) * rows * 128) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+}
+
 template <int NT, typename XT, int GROUP>
-__global__ void __launch_bounds__(kThreads, 2) packed_wide_kernel(const __grid_constant__ PackedLinearArgs<kWideTokens> a)
+__global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_constant__ PackedLinearArgs<kWideTokens> a)
 {
     typedef Wide<NT, XT, GROUP> W;
-    typedef Acts<XT> Act;
-    constexpr uint32_t kLanes = 256 / NT, kCols = NT / 4, kChunks = kCols / 8;    // threads per token; columns and 16-byte chunks of each
+    constexpr uint32_t kOpStages = W::kOpStages, kRecStages = W::kRecStages, kAccs = W::kAccs;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw_at = static_cast<uint32_t>(__cvta_generic_to_shared(smem_raw));
     const uint32_t base = (raw_at + 1023u) & ~1023u;
@@ -111,11 +160,12 @@ __global__ void __launch_bounds__(kThreads, 2) packed_wide_kernel(const __grid_c
     float* ysum = reinterpret_cast<float*>(gbase + W::kYAt);                      // [token][row]
     const uint32_t bars = base + W::kBarsAt;
     auto rec_full = [&](uint32_t s) { return bars + 8 * s; };
-    auto rec_free = [&](uint32_t s) { return bars + 16 + 8 * s; };
-    auto op_full = [&](uint32_t s) { return bars + 32 + 8 * s; };
-    auto op_done = [&](uint32_t s) { return bars + 48 + 8 * s; };
-    auto acc_free = [&](uint32_t s) { return bars + 64 + 8 * s; };
-    volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(gbase + W::kBarsAt + 128);
+    auto rec_free = [&](uint32_t s) { return bars + 24 + 8 * s; };
+    auto op_full = [&](uint32_t s) { return bars + 48 + 8 * s; };
+    auto op_done = [&](uint32_t s) { return bars + 72 + 8 * s; };
+    auto acc_full = [&](uint32_t s) { return bars + 96 + 8 * s; };
+    auto acc_free = [&](uint32_t s) { return bars + 160 + 8 * s; };
+    volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(gbase + W::kBarsAt + 224);
     volatile uint32_t* gone = tmem_ptr + 1;
 
     cg::cluster_group cluster = cg::this_cluster();
@@ -129,19 +179,24 @@ __global__ void __launch_bounds__(kThreads, 2) packed_wide_kernel(const __grid_c
     const uint32_t lo = static_cast<uint32_t>(total * rank >> lr), hi = static_cast<uint32_t>(total * (rank + 1) >> lr);
 
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < 2; ++s) {
+        for (uint32_t s = 0; s < kRecStages; ++s) {
             bar_init_n(rec_full(s), 1);
-            bar_init_n(rec_free(s), kWorkers);
-            bar_init_n(op_full(s), kWorkers);
+            bar_init_n(rec_free(s), kAWarps + kSumWarps);
+        }
+        for (uint32_t s = 0; s < kOpStages; ++s) {
+            bar_init_n(op_full(s), kAWarps + 1);
             bar_init_n(op_done(s), 1);
         }
-        for (uint32_t s = 0; s < kAccs; ++s) bar_init_n(acc_free(s), kWorkers);
+        for (uint32_t s = 0; s < kAccs; ++s) {
+            bar_init_n(acc_full(s), 1);
+            bar_init_n(acc_free(s), kSumWarps);
+        }
         *gone = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == kWorkers) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + W::kBarsAt + 128), "r"(W::kTmem) : "memory");
+    if (warp == kCopyWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + W::kBarsAt + 224), "r"(W::kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     for (uint32_t i = threadIdx.x; i < a.n_tokens * kTileRows; i += kThreads) ysum[i] = 0.f;
@@ -150,8 +205,8 @@ __global__ void __launch_bounds__(kThreads, 2) packed_wide_kernel(const __grid_c
     tc_after();
     const uint32_t tmem = *tmem_ptr;
 
-    if (warp == kWorkers) {
-        // ---- records
+    if (warp == kCopyWarp) {
+        // ---- records, in stages of 128 columns
         if (lane == 0) {
             uint32_t seg = lo / units, unit = lo - seg * units, n_issued = 0;
             for (uint32_t u = lo; u < hi; ++u, ++n_issued) {
@@ -170,190 +225,155 @@ __global__ void __launch_bounds__(kThreads, 2) packed_wide_kernel(const __grid_c
                 for (uint32_t k = n_issued > kRecStages ? n_issued - kRecStages : 0; k < n_issued; ++k)
                     (void)bar_wait(rec_full(k % kRecStages), (k / kRecStages) & 1u);
         }
-    } else if (warp == kWorkers + 1) {
-        // ---- products
+    } else if (warp == kCopyBWarp) {
+        // ---- operand B
         if (lane == 0) {
-            uint32_t seg = lo / units, unit = lo - seg * units, it = 0, acc = 0;
-            bool ok = true;
-            for (uint32_t u = lo; u < hi && ok; ++u) {
-                const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (((a.seg[seg].count + 15) / 16 * 16 >> 3) << 17) | ((kTileRows >> 4) << 24);
-                const uint32_t nt = min(2u, kts - 2 * unit);
-                for (uint32_t i = 0; i < nt && ok; ++i, ++it) {
-                    const uint32_t s = it % kOpStages;
-                    ok = wait_or_leave(op_full(s), (it / kOpStages) & 1u, gone);
-                    if (!ok) break;
-                    tc_after();
-                    const uint32_t op = base + W::kOpsAt + s * W::kOpBytes;
-                    const uint64_t da = operand_desc(op);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const bool fresh = k == 0 ? (GROUP != 128 || i == 0) : (W::HALF && k == 2);
-                        if (fresh) {
-                            ok = wait_or_leave(acc_free(acc % kAccs), ((acc / kAccs) & 1u) ^ 1u, gone);
-                            if (!ok) break;
-                            tc_after();
-                            ++acc;
-                        }
-                        const uint32_t d = tmem + (acc - 1) % kAccs * NT;
-#pragma unroll
-                        for (uint32_t term = 0; term < W::kTerms; ++term)
-                            tc_mma(d, da + 2 * k, operand_desc(op + kATile + term * W::kBTile) + 2 * k, idesc, !(fresh && term == 0));
-                    }
-                    tc_commit(op_done(s));
-                }
+            uint32_t seg = lo / units, unit = lo - seg * units, it = 0;
+            for (uint32_t u = lo; u < hi; ++u, ++it) {
+                const uint32_t os = it % kOpStages, bytes = operand_rows(a.seg[seg].count) * 128 * W::kTerms, all = min(2u, kts - 2 * unit) * bytes;
+                if (!wait_or_leave(op_done(os), ((it / kOpStages) & 1u) ^ 1u, gone)) break;      // the products have read the stage
+                bar_expect(op_full(os), all);
+                bulk_copy(base + W::kOpsAt + os * W::kOpBytes + W::kBAt,
+                          static_cast<const char*>(a.operands) + a.operand_at[seg] * (static_cast<size_t>(kts) * 128 * W::kTerms) +
+                              static_cast<size_t>(2 * unit) * bytes, all, op_full(os));
                 if (++unit == units) { unit = 0; ++seg; }
             }
-            if (!ok) {      // what was issued ends before tensor memory is freed: one more commit on a barrier that nobody waits for now
-                tc_commit(op_done(it % kOpStages));
-                (void)bar_wait(op_done(it % kOpStages), (it / kOpStages) & 1u);
+            if (*gone) {    // these copies end on a barrier that needs other arrivals too: give them time instead (10 ms)
+                const long long until = clock64() + 20000000ll;
+                while (clock64() < until) __nanosleep(1000);
             }
         }
+    } else if (warp == kMmaWarp) {
+        // ---- products. The whole warp walks the loop, so that descriptors stay in uniform registers; one lane issues.
+        uint32_t seg = lo / units, unit = lo - seg * units, stage = 0, parity = 0, acc = 0, acc_parity = 1;
+        const bool leader = elect_one();
+        const uint64_t desc0 = operand_desc(base + W::kOpsAt);
+        bool ok = true;
+        for (uint32_t u = lo; u < hi; ++u) {
+            const uint32_t rows = operand_rows(a.seg[seg].count), nt = min(2u, kts - 2 * unit), term = rows * 128 / 16;
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((rows + 8) / 16 << 18) | ((kTileRows >> 4) << 24);     // N = rows rounded up to 16
+            ok = wait_or_leave(op_full(stage), parity, gone);
+            if (!ok) break;
+            const uint64_t da = desc0 + stage * (W::kOpBytes / 16), db = da + W::kBAt / 16;
+            // a sum of products per group: kSteps steps of 16 columns
+            constexpr uint32_t kSteps = GROUP / 16;
+#pragma unroll
+            for (uint32_t first = 0; first < 8; first += kSteps) {
+                if (first / 4 >= nt) break;
+                ok = wait_or_leave(acc_free(acc), acc_parity, gone);
+                if (!ok) break;
+                tc_after();
+                if (leader) {
+                    const uint32_t d = tmem + acc * NT;
+#pragma unroll
+                    for (uint32_t k = first; k < first + kSteps; ++k)
+                        if (k / 4 < nt) {
+#pragma unroll
+                            for (uint32_t h = 0; h < W::kTerms; ++h)
+                                tc_mma(d, da + (k / 4) * (kATile / 16) + 2 * (k % 4), db + (k / 4) * W::kTerms * term + h * term + 2 * (k % 4), idesc, !(k == first && h == 0));
+                        }
+                    tc_commit(acc_full(acc));
+                }
+                if (++acc == kAccs) { acc = 0; acc_parity ^= 1u; }
+            }
+            if (!ok) break;
+            if (leader) tc_commit(op_done(stage));
+            if (++stage == kOpStages) { stage = 0; parity ^= 1u; }
+            if (++unit == units) { unit = 0; ++seg; }
+            __syncwarp();
+        }
+        if (!ok && leader) {    // what was issued ends before tensor memory is freed: one more commit on a barrier that nobody waits for now
+            tc_commit(op_done(stage));
+            (void)bar_wait(op_done(stage), parity);
+        }
+        __syncwarp();
+    } else if (warp >= kAFirst) {
+        // ---- operand A: this warp's row tile
+        const uint32_t g = lane >> 2, t = lane & 3, tile = warp - kAFirst;
+        const bool odd = g & 1;
+        const uint32_t from = base + W::kRecAt + (tile >> 2) * W::kUnitBytes + (tile & 3) * 512 + lane * 16;
+        const uint32_t to = base + W::kOpsAt + (tile * 16 + g) * 128;
+        uint32_t unit = lo % units, rs = 0, rec_parity = 0, os = 0, op_parity = 1;
+        for (uint32_t u = lo; u < hi; ++u) {
+            if (!__all_sync(~0u, wait_or_leave(rec_full(rs), rec_parity, gone))) break;
+            const uint32_t rec = from + rs * 2 * W::kUnitBytes;
+            const bool two = 2 * unit + 1 < kts;
+            const uint4 c0 = lds128(rec), c1 = lds128(rec + (W::kBlockTiles == 2 ? 2048 : W::kRecord));   // (a second tile that does not exist: not used)
+            if (!__all_sync(~0u, wait_or_leave(op_done(os), op_parity, gone))) break;       // the products have read the stage
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (i == 1 && !two) break;
+                const uint4 cw = i ? c1 : c0;
+                // lanes with odd g take the right half of the tile first, so that the stores of eight lanes fall into different banks
+                const uint32_t w[4] = {odd ? cw.z : cw.x, odd ? cw.w : cw.y, odd ? cw.x : cw.z, odd ? cw.y : cw.w};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t q0[4], q1[4];
+                    decode(w[2 * h], q0);
+                    decode(w[2 * h + 1], q1);
+                    const uint32_t at = to + os * W::kOpBytes + i * kATile + ((((h ^ (g & 1)) * 4 + t) ^ g) * 16);
+                    sts128(at, make_uint4(q0[0], q0[2], q1[0], q1[2]));
+                    sts128(at + 1024, make_uint4(q0[1], q0[3], q1[1], q1[3]));
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the tensor core reads through the async proxy
+            __syncwarp();
+            if (lane == 0) {
+                bar_arrive(op_full(os));
+                bar_arrive(rec_free(rs));
+            }
+            if (++rs == kRecStages) { rs = 0; rec_parity ^= 1u; }
+            if (++os == kOpStages) { os = 0; op_parity ^= 1u; }
+            if (++unit == units) unit = 0;
+        }
     } else {
-        // ---- workers
-        const int g = lane >> 2, t = lane & 3, tid = threadIdx.x;
-        const uint32_t token = tid / kLanes, tl = tid % kLanes;
+        // ---- group sums
         const uint32_t quadrant = warp & 3, half = warp >> 2, trow = quadrant * 32 + lane;      // this thread's row and half of the tokens
         const uint32_t own_scale = (trow >> 6) * W::kUnitBytes + W::kCodeBytes + ((trow & 63) >> 4) * 32 + (trow & 7) * 4 + ((trow >> 3) & 1) * 2;
-        const XT* x = static_cast<const XT*>(a.x);
-        const uint32_t whole = a.x_vec ? a.cols / 64 : 0u;
-        float tot[NT / 2];
-        uint32_t seg = lo / units, unit = lo - seg * units, it = 0, acc = 0, n_rec = 0;
-        bool ok = true, pending = false;
-        float ps0 = 0.f, ps1 = 0.f;          // scale(s) of the group(s) that wait to be added up
-        uint32_t p_it = 0;
-        uint32_t count = 0;
-        auto drain_one = [&](float scale) {
-            const uint32_t b = acc % kAccs;
-            const uint32_t at = tmem + (quadrant << 21) + b * NT + half * (NT / 2);
-#pragma unroll
-            for (int c = 0; c < NT / 2; c += 16) {
-                if (half * (NT / 2) + c < count) {
-                    uint32_t v[16];
-                    tc_load16(at + c, v);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) tot[c + j] = __fmaf_rn(scale, __uint_as_float(v[j]), tot[c + j]);
-                }
-            }
-            tc_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(acc_free(b));
-            ++acc;
-        };
-        auto drain = [&]() {
-            if (!pending) return;
-            pending = false;
-            ok = wait_or_leave(op_done(p_it % kOpStages), (p_it / kOpStages) & 1u, gone);
-            ok = __all_sync(~0u, ok);
-            if (!ok) return;
-            tc_after();
-            drain_one(ps0);
-            if (W::HALF) drain_one(ps1);
-        };
-        while (lo + n_rec < hi && ok) {
-            // ---- one segment's part of the run
+        uint32_t seg = lo / units, unit = lo - seg * units, acc = 0, n_rec = 0;
+        bool ok = true;
+        for (uint32_t u = lo; u < hi && ok; unit = 0, ++seg) {
             const PackedSegment& sg = a.seg[seg];
-            count = sg.count;
-            const bool on = token < count, signs = sg.flip != 0;
-            const uint32_t pos = sg.first + (on ? token : 0);
-            const XT* xt = x + a.token[pos] * a.x_stride + tl * kCols;
-            DevTask task = {0, 0, 0, 0};
-            if (signs) task = a.task[a.token_task[pos]];
+            const uint32_t count = sg.count;
+            float tot[NT / 2];
 #pragma unroll
             for (int j = 0; j < NT / 2; ++j) tot[j] = 0.f;
-            uint4 blk = make_uint4(0, 0, 0, 0);
-            uint32_t blk0 = ~0u;
-            typename Act::Raw raw[kChunks];
-            auto load = [&](uint32_t kt) {
-#pragma unroll
-                for (uint32_t h = 0; h < kChunks; ++h) {
-                    const uint32_t c = kt * 64 + tl * kCols + h * 8;
-                    if (kt < whole) raw[h] = Act::words(xt + kt * 64 + h * 8);
-                    else raw[h] = c < a.cols ? Act::gather(xt - tl * kCols, c, a.cols) : Act::zero();
-                }
-            };
-            const uint32_t kt_end = min(kts, 2 * (unit + (hi - lo - n_rec)));
-            load(2 * unit);
-            for (; unit < units && lo + n_rec < hi && ok; ++unit, ++n_rec) {
-                const uint32_t rs = n_rec % kRecStages, rec = base + W::kRecAt + rs * 2 * W::kUnitBytes;
+            for (; unit < units && u < hi && ok; ++unit, ++u, ++n_rec) {
+                const uint32_t rs = n_rec % kRecStages, sat = base + W::kRecAt + rs * 2 * W::kUnitBytes + own_scale;
                 ok = __all_sync(~0u, wait_or_leave(rec_full(rs), (n_rec / kRecStages) & 1u, gone));
-                const uint32_t nt = min(2u, kts - 2 * unit);
-#pragma unroll 1
-                for (uint32_t i = 0; i < nt && ok; ++i, ++it) {
-                    const uint32_t kt = 2 * unit + i, os = it % kOpStages, op = base + W::kOpsAt + os * W::kOpBytes;
-                    // the stage's products of two tiles ago have read it
-                    if (it >= kOpStages) ok = __all_sync(~0u, wait_or_leave(op_done(os), ((it / kOpStages) & 1u) ^ 1u, gone));
+                if (!ok) break;
+                const uint32_t nt = min(2u, kts - 2 * unit), n_sums = GROUP == 128 ? 1 : (W::HALF ? 2 * nt : nt);
+                float scale[W::HALF ? 4 : 2];
+#pragma unroll
+                for (int k = 0; k < (GROUP == 128 ? 1 : (W::HALF ? 4 : 2)); ++k)      // (a tile that does not exist: never used)
+                    scale[k] = __uint_as_float(lds_u16(sat + (W::HALF ? (k >> 1) * W::kRecord + (k & 1) * 128 : k * W::kRecord)) << 16);
+                __syncwarp();
+                if (lane == 0) bar_arrive(rec_free(rs));
+#pragma unroll
+                for (uint32_t k = 0; k < (GROUP == 128 ? 1 : (W::HALF ? 4 : 2)); ++k) {
+                    if (k >= n_sums) break;
+                    const uint32_t b = acc % kAccs;
+                    ok = __all_sync(~0u, wait_or_leave(acc_full(b), (acc / kAccs) & 1u, gone));
                     if (!ok) break;
-                    // A: 16 rows of codes. Lanes with odd g take the right half of the tile first, so that eight lanes' stores
-                    // fall into different banks.
-                    {
-                        const uint32_t tile = rec + (warp >> 2) * W::kUnitBytes + (W::kBlockTiles == 2 ? i * 2048 : i * W::kRecord) + (warp & 3) * 512 + lane * 16;
-                        const uint4 cw = lds128(tile);
-                        const bool odd = g & 1;
-                        const uint32_t w[4] = {odd ? cw.z : cw.x, odd ? cw.w : cw.y, odd ? cw.x : cw.z, odd ? cw.y : cw.w};
+                    tc_after();
+                    const uint32_t at = tmem + (quadrant << 21) + b * NT + half * (NT / 2);
+                    uint32_t v[NT / 2];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t q0[4], q1[4];
-                            decode(w[2 * h], q0);
-                            decode(w[2 * h + 1], q1);
-                            const uint32_t chunk = ((h ^ (g & 1)) * 4 + t) ^ g;
-                            const uint32_t to = op + (warp * 16 + g) * 128 + chunk * 16;
-                            sts128(to, make_uint4(q0[0], q0[2], q1[0], q1[2]));
-                            sts128(to + 8 * 128, make_uint4(q0[1], q0[3], q1[1], q1[3]));
+                    for (int c = 0; c < NT / 2; c += 16)
+                        if (half * (NT / 2) + c < count) tc_load16(at + c, v + c);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int c = 0; c < NT / 2; c += 16)
+                        if (half * (NT / 2) + c < count) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) tot[c + j] = __fmaf_rn(scale[k], __uint_as_float(v[c + j]), tot[c + j]);
                         }
-                    }
-                    // B: this thread's columns of its token
-                    if (signs) {
-                        if (blk0 == ~0u || (kt >> 1) - blk0 >= kLanes) {
-                            blk0 = kt >> 1;      // lane tl of a token makes the block of columns 128 (blk0 + tl) ..
-                            blk = philox4x32_10(blk0 + tl, sg.slot, kTagSign, task.id, task.key0, task.key1);
-                        }
-                        const int src = static_cast<int>((lane & ~(kLanes - 1)) | ((kt >> 1) - blk0));
-                        const uint32_t w0 = __shfl_sync(~0u, kt & 1 ? blk.z : blk.x, src), w1 = __shfl_sync(~0u, kt & 1 ? blk.w : blk.y, src);
-                        const uint32_t bits = (tl * kCols >= 32 ? w1 : w0) >> (tl * kCols & 31);
-#pragma unroll
-                        for (uint32_t h = 0; h < kChunks; ++h) {
-                            uint32_t wt[Act::kTerms][4];
-                            Act::terms(raw[h], wt);
-                            const uint32_t byte = (bits >> (8 * h)) & 0xFFu, chunk = (tl * kChunks + h) ^ (token & 7);
-#pragma unroll
-                            for (int k = 0; k < Act::kTerms; ++k) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) wt[k][e] ^= (byte * ((1u << (15 - 2 * e)) + (1u << (30 - 2 * e)))) & 0x80008000u;
-                                if (on) sts128(op + kATile + k * W::kBTile + token * 128 + chunk * 16, make_uint4(wt[k][0], wt[k][1], wt[k][2], wt[k][3]));
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (uint32_t h = 0; h < kChunks; ++h) {
-                            uint32_t wt[Act::kTerms][4];
-                            Act::terms(raw[h], wt);
-                            const uint32_t chunk = (tl * kChunks + h) ^ (token & 7);
-#pragma unroll
-                            for (int k = 0; k < Act::kTerms; ++k)
-                                if (on) sts128(op + kATile + k * W::kBTile + token * 128 + chunk * 16, make_uint4(wt[k][0], wt[k][1], wt[k][2], wt[k][3]));
-                        }
-                    }
-                    if (kt + 1 < kt_end) load(kt + 1);
-                    const uint32_t sat = rec + own_scale + (W::kBlockTiles == 1 ? i * W::kRecord : 0u);
-                    const float s0 = __uint_as_float(lds_u16(sat) << 16);
-                    const float s1 = W::HALF ? __uint_as_float(lds_u16(sat + 128) << 16) : 0.f;
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the tensor core reads through the async proxy
+                    tc_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        bar_arrive(op_full(os));
-                        if (i + 1 == nt) bar_arrive(rec_free(rs));
-                    }
-                    drain();                      // the tile before
-                    if (GROUP != 128 || i + 1 == nt) {
-                        pending = true;
-                        p_it = it;
-                        ps0 = s0;
-                        ps1 = s1;
-                    }
+                    if (lane == 0) bar_arrive(acc_free(b));
+                    ++acc;
                 }
             }
-            if (ok) drain();
             if (!ok) break;
             // this segment's sums: at most two (base and slot) meet in an element, so their order does not matter
             const float factor = seg ? kCodeUnit * a.lambda : kCodeUnit;
@@ -362,13 +382,11 @@ __global__ void __launch_bounds__(kThreads, 2) packed_wide_kernel(const __grid_c
                 const uint32_t i = half * (NT / 2) + j;
                 if (i < count) atomicAdd(ysum + a.token[sg.first + i] * kTileRows + trow, factor * tot[j]);
             }
-            unit = 0;
-            ++seg;
         }
     }
     tc_before();
     __syncthreads();
-    if (warp == kWorkers) {
+    if (warp == kCopyWarp) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(W::kTmem) : "memory");
     }
@@ -399,14 +417,14 @@ __global__ void __launch_bounds__(kThreads, 2) packed_wide_kernel(const __grid_c
 
 constexpr int kDevices = 64;
 
-template <int NT, typename XT, int GROUP> cudaError_t launch_wide(PackedLinearArgs<kWideTokens>& a, int sm_count, int device, cudaStream_t s)
+template <int NT, typename XT, int GROUP> cudaError_t launch_wide(PackedLinearArgs<kWideTokens>& a, int sm_count, int device, int* launched, cudaStream_t s)
 {
     typedef Wide<NT, XT, GROUP> W;
     const uint64_t blocks = (static_cast<uint64_t>(a.rows) + kTileRows - 1) / kTileRows;
     const uint64_t units = ((a.cols + 63ull) / 64 + 1) / 2 * a.n_seg;
-    // two CTAs per SM, as long as each has a few units to itself
+    // one CTA per SM, as long as each has a few units to itself
     a.log_ranks = 0;
-    while (a.log_ranks < 3 && (blocks << (a.log_ranks + 1)) <= static_cast<uint64_t>(sm_count) * 2 && (4ull << a.log_ranks) <= units) ++a.log_ranks;
+    while (a.log_ranks < 3 && (blocks << (a.log_ranks + 1)) <= static_cast<uint64_t>(sm_count) && (4ull << a.log_ranks) <= units) ++a.log_ranks;
     const uint32_t ranks = 1u << a.log_ranks;
     const size_t smem = W::smem(a.n_tokens);
     static std::atomic<size_t> granted[kDevices];      // a kernel has to opt in beyond 48 KiB, per device
@@ -414,6 +432,18 @@ template <int NT, typename XT, int GROUP> cudaError_t launch_wide(PackedLinearAr
         const cudaError_t e = cudaFuncSetAttribute(packed_wide_kernel<NT, XT, GROUP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(W::smem(NT)));
         if (e != cudaSuccess) return e;
         if (device < kDevices) granted[device].store(W::smem(NT), std::memory_order_relaxed);
+    }
+    uint32_t rows = 0;
+    for (uint32_t k = 0; k < a.n_seg; ++k) {
+        a.operand_at[k] = static_cast<uint16_t>(rows);
+        rows += operand_rows(a.seg[k].count);
+    }
+    const uint32_t kts = (a.cols + 63) / 64;
+    if (kts) {
+        operand_kernel<XT><<<dim3((kts * 8 + 255) / 256, a.seg[a.n_seg - 1].first + a.seg[a.n_seg - 1].count), 256, 0, s>>>(a);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        ++*launched;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks * ranks));
@@ -426,23 +456,34 @@ template <int NT, typename XT, int GROUP> cudaError_t launch_wide(PackedLinearAr
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = ranks > 1;
-    return cudaLaunchKernelEx(&cfg, packed_wide_kernel<NT, XT, GROUP>, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, packed_wide_kernel<NT, XT, GROUP>, a);
+    if (e == cudaSuccess) ++*launched;
+    return e;
 }
 
-template <int NT, typename XT> cudaError_t launch_group(PackedLinearArgs<kWideTokens>& a, int sm_count, int device, cudaStream_t s)
+template <int NT, typename XT> cudaError_t launch_group(PackedLinearArgs<kWideTokens>& a, int sm_count, int device, int* launched, cudaStream_t s)
 {
-    if (a.group == 32) return launch_wide<NT, XT, 32>(a, sm_count, device, s);
-    if (a.group == 64) return launch_wide<NT, XT, 64>(a, sm_count, device, s);
-    return launch_wide<NT, XT, 128>(a, sm_count, device, s);
+    if (a.group == 32) return launch_wide<NT, XT, 32>(a, sm_count, device, launched, s);
+    if (a.group == 64) return launch_wide<NT, XT, 64>(a, sm_count, device, launched, s);
+    return launch_wide<NT, XT, 128>(a, sm_count, device, launched, s);
 }
 
 }  // namespace
 
-int launch_packed_wide(PackedLinearArgs<kWideTokens>& a, bool x_bf16, int sm_count, int device, void* stream)
+size_t packed_wide_workspace(uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks)
+{
+    const uint32_t n = n_tokens < kWideTokens ? n_tokens : kWideTokens;
+    if (n_tokens <= kNarrowTokens) return 0;
+    // the base with every token; at worst every token has a slot of its own
+    const size_t rows = operand_rows(n) + (tasks ? 8u * n : 0u);
+    return rows * ((static_cast<size_t>(cols) + 63) / 64) * 128 * (x_bf16 ? 1 : 3);
+}
+
+int launch_packed_wide(PackedLinearArgs<kWideTokens>& a, bool x_bf16, int sm_count, int device, int* launched, void* stream)
 {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a.n_tokens <= 32) return static_cast<int>(x_bf16 ? launch_group<32, bf16>(a, sm_count, device, s) : launch_group<32, float>(a, sm_count, device, s));
-    return static_cast<int>(x_bf16 ? launch_group<64, bf16>(a, sm_count, device, s) : launch_group<64, float>(a, sm_count, device, s));
+    if (a.n_tokens <= 32) return static_cast<int>(x_bf16 ? launch_group<32, bf16>(a, sm_count, device, launched, s) : launch_group<32, float>(a, sm_count, device, launched, s));
+    return static_cast<int>(x_bf16 ? launch_group<64, bf16>(a, sm_count, device, launched, s) : launch_group<64, float>(a, sm_count, device, launched, s));
 }
 
 int packed_wide_giveups(unsigned int* count)

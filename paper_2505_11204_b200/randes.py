@@ -143,9 +143,11 @@ def lib():
         L.randes_unpack.restype = ctypes.c_int
         L.randes_retrieve_packed.argtypes = [vp, u32, f32, vp, u32, vp, vp, u32, vp, vp]
         L.randes_retrieve_packed.restype = ctypes.c_int
-        L.randes_packed_linear.argtypes = [vp, u32, u32, u32, vp, dt, u64, u32, vp, dt, u64, vp]
+        L.randes_packed_linear_workspace.argtypes = [u32, dt, u32, ctypes.c_int]
+        L.randes_packed_linear_workspace.restype = sz
+        L.randes_packed_linear.argtypes = [vp, u32, u32, u32, vp, dt, u64, u32, vp, dt, u64, vp, sz, vp]
         L.randes_packed_linear.restype = ctypes.c_int
-        L.randes_packed_linear_tasks.argtypes = [vp, f32, u32, u32, vp, u32, vp, dt, u64, vp, vp, vp, dt, u64, vp]
+        L.randes_packed_linear_tasks.argtypes = [vp, f32, u32, u32, vp, u32, vp, dt, u64, vp, vp, vp, dt, u64, vp, sz, vp]
         L.randes_packed_linear_tasks.restype = ctypes.c_int
         L.randes_token_scores.argtypes = [vp, dt, u32, u32, u64, vp, f32, u32, vp, vp, vp, vp, vp, vp]
         L.randes_token_scores.restype = ctypes.c_int
@@ -164,7 +166,7 @@ EXPORTS = [
     "randes_layer_offset", "randes_num_layers", "randes_num_tasks", "randes_task_list",
     "randes_task_tables", "randes_plan_serialize", "randes_plan_workspace_needed", "randes_plan_deserialize", "randes_compress", "randes_add_model", "randes_add_models", "randes_remove_model",
     "randes_retrieve", "randes_delta_gram_scratch_bytes", "randes_delta_gram", "randes_interference_norm", "randes_pairwise_cosines", "randes_retrieve_batch", "randes_retrieve_static", "randes_linear", "randes_linear_gated", "randes_linear_giveups", "randes_launch_count", "randes_last_error",
-    "randes_packed_bytes", "randes_pack", "randes_unpack", "randes_retrieve_packed", "randes_packed_linear", "randes_packed_linear_tasks",
+    "randes_packed_bytes", "randes_pack", "randes_unpack", "randes_retrieve_packed", "randes_packed_linear_workspace", "randes_packed_linear", "randes_packed_linear_tasks",
     "randes_token_scores", "randes_token_scores_backward",
 ]
 
@@ -347,15 +349,22 @@ def randes_retrieve_packed(plan, task_id, lam, layers, n, base, M, group, packed
     _check(lib().randes_retrieve_packed(plan, task_id, lam, _addr(layers), n, _addr(base), _addr(M), group, _addr(packed), stream))
 
 
-def randes_packed_linear(packed, rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, stream) -> None:
+def randes_packed_linear_workspace(cols: int, x_dtype: int, n_tokens: int, with_tasks: bool) -> int:
+    """Bytes of device workspace the two calls below need (0 for up to 8 tokens)."""
+    return int(lib().randes_packed_linear_workspace(cols, x_dtype, n_tokens, int(with_tasks)))
+
+
+def randes_packed_linear(packed, rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, stream, workspace=None,
+                         workspace_bytes: int = 0) -> None:
     _check(lib().randes_packed_linear(_addr(packed), rows, cols, group, _addr(x), x_dtype, x_stride, n_tokens, _addr(y), y_dtype, y_stride,
-                                      stream))
+                                      _addr(workspace), workspace_bytes, stream))
 
 
 def randes_packed_linear_tasks(plan, lam, layer, group, task_ids, n_tokens, x, x_dtype, x_stride, packed_base, packed_m, y, y_dtype, y_stride,
-                               stream) -> None:
+                               stream, workspace=None, workspace_bytes: int = 0) -> None:
     _check(lib().randes_packed_linear_tasks(plan, lam, layer, group, _addr(task_ids), n_tokens, _addr(x), x_dtype, x_stride,
-                                            _addr(packed_base), _addr(packed_m), _addr(y), y_dtype, y_stride, stream))
+                                            _addr(packed_base), _addr(packed_m), _addr(y), y_dtype, y_stride, _addr(workspace), workspace_bytes,
+                                            stream))
 
 
 def randes_token_scores(logits, dtype, n_rows, vocab, stride, targets, scale, top_k, logprob, entropy, stats, top_ids, top_logprobs,
@@ -547,12 +556,24 @@ def _linear_tensors(x, rows: int, cols: int, y, y_dtype: int):
     return n, x_dtype, x_stride, y, y_dtype, y_stride
 
 
+def _linear_workspace(x, cols: int, x_dtype: int, n: int, with_tasks: bool):
+    """(tensor or None, its address, its bytes): what a product of more than 8 tokens lays its activations out in."""
+    import torch
+
+    if n <= 8:
+        return None, None, 0
+    nbytes = randes_packed_linear_workspace(cols, x_dtype, n, with_tasks)
+    t = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    return t, t.data_ptr(), nbytes
+
+
 def packed_linear(x, w: PackedMatrix, y=None, y_dtype: int = F32):
     """x: [n_tokens, cols] fp32 or bf16 CUDA tensor (rows may be strided); returns y = x W^T [n_tokens, rows]."""
     rows, cols = w.rows, w.cols
     n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, rows, cols, y, y_dtype)
+    workspace, ws_at, ws_bytes = _linear_workspace(x, cols, x_dtype, n, False)
     _call(lib().randes_packed_linear(w.address, rows, cols, w.group, x.data_ptr(), x_dtype, x_stride, n, y.data_ptr(), y_dtype, y_stride,
-                                     _stream_of(x)))
+                                     ws_at, ws_bytes, _stream_of(x)))
     return y
 
 
@@ -847,6 +868,7 @@ class Plan:
             _refuse("%d task ids for %d tokens" % (len(task_ids), n))
         if not isinstance(task_ids, ctypes.Array):
             task_ids = (ctypes.c_uint32 * max(n, 1))(*task_ids)
+        workspace, ws_at, ws_bytes = _linear_workspace(x, cols, x_dtype, n, True)
         _call(lib().randes_packed_linear_tasks(self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride, packed_base.address,
-                                               packed_m, y.data_ptr(), y_dtype, y_stride, _stream_of(x)))
+                                               packed_m, y.data_ptr(), y_dtype, y_stride, ws_at, ws_bytes, _stream_of(x)))
         return y
