@@ -14,7 +14,11 @@
 //   warp 16      copies records (one lane, bulk copies), owns tensor memory
 //   warp 17      issues tcgen05.mma (one lane): M = 128 rows, N = tokens of the segment rounded up to 16
 //   warp 18      copies operand B (one lane, bulk copies)
-// A hand-over between roles costs hundreds of cycles however little it hands over, so a stage is 128 columns.
+// A hand-over between roles costs hundreds of cycles however little it hands over, so a stage is 128 columns (64: 69 us
+// against 51 us for an 8192 x 8192 base and superposition with 64 tokens; warps that do all of the work in turn: 86 us).
+// What bounds it there is shared memory: per stage of 128 rows x 128 columns the codes come in (8 KiB), go out as bf16
+// (32 KiB), are read by the tensor core (32 KiB) next to operand B (16 KiB in, 16 KiB out) -- 112 KiB or 900 cycles at 128
+// bytes a cycle, against 370 cycles of HBM time. More stages (4 and 6 of records, 5 of B) change nothing.
 //
 // Every wait is bounded; a CTA whose wait runs out raises a flag, all roles leave, what is in flight is waited for, tensor
 // memory is freed, its sums become NaN and a device counter records the event.
@@ -98,14 +102,16 @@ template <int NT, typename XT, int GROUP> struct Wide {
     static constexpr uint32_t kCodeBytes = kBlockTiles * 4 * 512, kRecord = kCodeBytes + (HALF ? 256 : 128);
     static constexpr uint32_t kUnitBytes = 2 / kBlockTiles * kRecord;       // 64 rows x 128 columns
     static constexpr uint32_t kBTile = NT * 128;
-    static constexpr uint32_t kBAt = 2 * kATile;                            // a stage: two tiles of A, then two of B
-    static constexpr uint32_t kOpBytes = kBAt + 2 * kTerms * kBTile;
-    static constexpr uint32_t kOpStages = kTerms == 3 ? 2 : 3, kRecStages = kTerms == 3 && NT == 64 ? 2 : 3;
+    // Stages of 128 columns: operand A, operand B, records. What limits them is shared memory; what they hide is one hand-over
+    // for A, an L2 latency for B, an HBM latency for the records.
+    static constexpr uint32_t kABytes = 2 * kATile, kBBytes = 2 * kTerms * kBTile;
+    static constexpr uint32_t kAStages = kTerms == 1 ? 3 : 2, kBStages = kTerms == 3 && NT == 64 ? 2 : 4;
+    static constexpr uint32_t kRecStages = NT == 32 ? 4 : (kTerms == 1 ? 3 : 2);
     static constexpr uint32_t kAccs = 256 / NT;
-    static constexpr uint32_t kOpsAt = 0;                                   // 1024-byte aligned operands first
-    static constexpr uint32_t kRecAt = kOpsAt + kOpStages * kOpBytes;
+    static constexpr uint32_t kAAt = 0, kBAt = kAStages * kABytes;          // 1024-byte aligned operands first
+    static constexpr uint32_t kRecAt = kBAt + kBStages * kBBytes;
     static constexpr uint32_t kBarsAt = kRecAt + kRecStages * 2 * kUnitBytes;
-    static constexpr uint32_t kYAt = kBarsAt + 256;
+    static constexpr uint32_t kYAt = kBarsAt + 512;
     static_assert(kYAt + NT * kTileRows * 4 + 1024 <= 227 * 1024, "shared memory of a CTA");
     static constexpr uint32_t kTmem = 256;
     static size_t smem(uint32_t n_tokens) { return 1024 + kYAt + static_cast<size_t>(n_tokens) * kTileRows * sizeof(float); }
@@ -152,7 +158,7 @@ template <int NT, typename XT, int GROUP>
 __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_constant__ PackedLinearArgs<kWideTokens> a)
 {
     typedef Wide<NT, XT, GROUP> W;
-    constexpr uint32_t kOpStages = W::kOpStages, kRecStages = W::kRecStages, kAccs = W::kAccs;
+    constexpr uint32_t kAStages = W::kAStages, kBStages = W::kBStages, kRecStages = W::kRecStages, kAccs = W::kAccs;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw_at = static_cast<uint32_t>(__cvta_generic_to_shared(smem_raw));
     const uint32_t base = (raw_at + 1023u) & ~1023u;
@@ -160,12 +166,15 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
     float* ysum = reinterpret_cast<float*>(gbase + W::kYAt);                      // [token][row]
     const uint32_t bars = base + W::kBarsAt;
     auto rec_full = [&](uint32_t s) { return bars + 8 * s; };
-    auto rec_free = [&](uint32_t s) { return bars + 24 + 8 * s; };
-    auto op_full = [&](uint32_t s) { return bars + 48 + 8 * s; };
-    auto op_done = [&](uint32_t s) { return bars + 72 + 8 * s; };
-    auto acc_full = [&](uint32_t s) { return bars + 96 + 8 * s; };
-    auto acc_free = [&](uint32_t s) { return bars + 160 + 8 * s; };
-    volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(gbase + W::kBarsAt + 224);
+    auto rec_free = [&](uint32_t s) { return bars + 64 + 8 * s; };
+    auto a_full = [&](uint32_t s) { return bars + 128 + 8 * s; };
+    auto a_free = [&](uint32_t s) { return bars + 160 + 8 * s; };
+    auto b_full = [&](uint32_t s) { return bars + 192 + 8 * s; };
+    auto b_free = [&](uint32_t s) { return bars + 256 + 8 * s; };
+    auto acc_full = [&](uint32_t s) { return bars + 320 + 8 * s; };
+    auto acc_free = [&](uint32_t s) { return bars + 384 + 8 * s; };
+    const uint32_t flushed = bars + 448;
+    volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(gbase + W::kBarsAt + 456);
     volatile uint32_t* gone = tmem_ptr + 1;
 
     cg::cluster_group cluster = cg::this_cluster();
@@ -183,20 +192,25 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
             bar_init_n(rec_full(s), 1);
             bar_init_n(rec_free(s), kAWarps + kSumWarps);
         }
-        for (uint32_t s = 0; s < kOpStages; ++s) {
-            bar_init_n(op_full(s), kAWarps + 1);
-            bar_init_n(op_done(s), 1);
+        for (uint32_t s = 0; s < kAStages; ++s) {
+            bar_init_n(a_full(s), kAWarps);
+            bar_init_n(a_free(s), 1);
+        }
+        for (uint32_t s = 0; s < kBStages; ++s) {
+            bar_init_n(b_full(s), 1);
+            bar_init_n(b_free(s), 1);
         }
         for (uint32_t s = 0; s < kAccs; ++s) {
             bar_init_n(acc_full(s), 1);
             bar_init_n(acc_free(s), kSumWarps);
         }
+        bar_init_n(flushed, kSumWarps);
         *gone = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == kCopyWarp) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + W::kBarsAt + 224), "r"(W::kTmem) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + W::kBarsAt + 456), "r"(W::kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     for (uint32_t i = threadIdx.x; i < a.n_tokens * kTileRows; i += kThreads) ysum[i] = 0.f;
@@ -228,33 +242,32 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
     } else if (warp == kCopyBWarp) {
         // ---- operand B
         if (lane == 0) {
-            uint32_t seg = lo / units, unit = lo - seg * units, it = 0;
-            for (uint32_t u = lo; u < hi; ++u, ++it) {
-                const uint32_t os = it % kOpStages, bytes = operand_rows(a.seg[seg].count) * 128 * W::kTerms, all = min(2u, kts - 2 * unit) * bytes;
-                if (!wait_or_leave(op_done(os), ((it / kOpStages) & 1u) ^ 1u, gone)) break;      // the products have read the stage
-                bar_expect(op_full(os), all);
-                bulk_copy(base + W::kOpsAt + os * W::kOpBytes + W::kBAt,
+            uint32_t seg = lo / units, unit = lo - seg * units, n_issued = 0;
+            for (uint32_t u = lo; u < hi; ++u, ++n_issued) {
+                const uint32_t s = n_issued % kBStages, bytes = operand_rows(a.seg[seg].count) * 128 * W::kTerms, all = min(2u, kts - 2 * unit) * bytes;
+                if (!wait_or_leave(b_free(s), ((n_issued / kBStages) & 1u) ^ 1u, gone)) break;
+                bar_expect(b_full(s), all);
+                bulk_copy(base + W::kBAt + s * W::kBBytes,
                           static_cast<const char*>(a.operands) + a.operand_at[seg] * (static_cast<size_t>(kts) * 128 * W::kTerms) +
-                              static_cast<size_t>(2 * unit) * bytes, all, op_full(os));
+                              static_cast<size_t>(2 * unit) * bytes, all, b_full(s));
                 if (++unit == units) { unit = 0; ++seg; }
             }
-            if (*gone) {    // these copies end on a barrier that needs other arrivals too: give them time instead (10 ms)
-                const long long until = clock64() + 20000000ll;
-                while (clock64() < until) __nanosleep(1000);
-            }
+            if (*gone)      // let what was issued land
+                for (uint32_t k = n_issued > kBStages ? n_issued - kBStages : 0; k < n_issued; ++k)
+                    (void)bar_wait(b_full(k % kBStages), (k / kBStages) & 1u);
         }
     } else if (warp == kMmaWarp) {
         // ---- products. The whole warp walks the loop, so that descriptors stay in uniform registers; one lane issues.
-        uint32_t seg = lo / units, unit = lo - seg * units, stage = 0, parity = 0, acc = 0, acc_parity = 1;
+        uint32_t seg = lo / units, unit = lo - seg * units, sa = 0, a_parity = 0, sb = 0, b_parity = 0, acc = 0, acc_parity = 1;
         const bool leader = elect_one();
-        const uint64_t desc0 = operand_desc(base + W::kOpsAt);
+        const uint64_t desc_a = operand_desc(base + W::kAAt), desc_b = operand_desc(base + W::kBAt);
         bool ok = true;
         for (uint32_t u = lo; u < hi; ++u) {
             const uint32_t rows = operand_rows(a.seg[seg].count), nt = min(2u, kts - 2 * unit), term = rows * 128 / 16;
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((rows + 8) / 16 << 18) | ((kTileRows >> 4) << 24);     // N = rows rounded up to 16
-            ok = wait_or_leave(op_full(stage), parity, gone);
+            ok = wait_or_leave(b_full(sb), b_parity, gone) && wait_or_leave(a_full(sa), a_parity, gone);
             if (!ok) break;
-            const uint64_t da = desc0 + stage * (W::kOpBytes / 16), db = da + W::kBAt / 16;
+            const uint64_t da = desc_a + sa * (W::kABytes / 16), db = desc_b + sb * (W::kBBytes / 16);
             // a sum of products per group: kSteps steps of 16 columns
             constexpr uint32_t kSteps = GROUP / 16;
 #pragma unroll
@@ -277,14 +290,18 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
                 if (++acc == kAccs) { acc = 0; acc_parity ^= 1u; }
             }
             if (!ok) break;
-            if (leader) tc_commit(op_done(stage));
-            if (++stage == kOpStages) { stage = 0; parity ^= 1u; }
+            if (leader) {
+                tc_commit(a_free(sa));
+                tc_commit(b_free(sb));
+            }
+            if (++sa == kAStages) { sa = 0; a_parity ^= 1u; }
+            if (++sb == kBStages) { sb = 0; b_parity ^= 1u; }
             if (++unit == units) { unit = 0; ++seg; }
             __syncwarp();
         }
         if (!ok && leader) {    // what was issued ends before tensor memory is freed: one more commit on a barrier that nobody waits for now
-            tc_commit(op_done(stage));
-            (void)bar_wait(op_done(stage), parity);
+            tc_commit(a_free(sa));
+            (void)bar_wait(a_free(sa), a_parity);
         }
         __syncwarp();
     } else if (warp >= kAFirst) {
@@ -292,14 +309,14 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
         const uint32_t g = lane >> 2, t = lane & 3, tile = warp - kAFirst;
         const bool odd = g & 1;
         const uint32_t from = base + W::kRecAt + (tile >> 2) * W::kUnitBytes + (tile & 3) * 512 + lane * 16;
-        const uint32_t to = base + W::kOpsAt + (tile * 16 + g) * 128;
-        uint32_t unit = lo % units, rs = 0, rec_parity = 0, os = 0, op_parity = 1;
+        const uint32_t to = base + W::kAAt + (tile * 16 + g) * 128;
+        uint32_t unit = lo % units, rs = 0, rec_parity = 0, sa = 0, a_parity = 1;
         for (uint32_t u = lo; u < hi; ++u) {
             if (!__all_sync(~0u, wait_or_leave(rec_full(rs), rec_parity, gone))) break;
             const uint32_t rec = from + rs * 2 * W::kUnitBytes;
             const bool two = 2 * unit + 1 < kts;
             const uint4 c0 = lds128(rec), c1 = lds128(rec + (W::kBlockTiles == 2 ? 2048 : W::kRecord));   // (a second tile that does not exist: not used)
-            if (!__all_sync(~0u, wait_or_leave(op_done(os), op_parity, gone))) break;       // the products have read the stage
+            if (!__all_sync(~0u, wait_or_leave(a_free(sa), a_parity, gone))) break;       // the products have read the stage
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 if (i == 1 && !two) break;
@@ -311,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
                     uint32_t q0[4], q1[4];
                     decode(w[2 * h], q0);
                     decode(w[2 * h + 1], q1);
-                    const uint32_t at = to + os * W::kOpBytes + i * kATile + ((((h ^ (g & 1)) * 4 + t) ^ g) * 16);
+                    const uint32_t at = to + sa * W::kABytes + i * kATile + ((((h ^ (g & 1)) * 4 + t) ^ g) * 16);
                     sts128(at, make_uint4(q0[0], q0[2], q1[0], q1[2]));
                     sts128(at + 1024, make_uint4(q0[1], q0[3], q1[1], q1[3]));
                 }
@@ -319,18 +336,18 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the tensor core reads through the async proxy
             __syncwarp();
             if (lane == 0) {
-                bar_arrive(op_full(os));
+                bar_arrive(a_full(sa));
                 bar_arrive(rec_free(rs));
             }
             if (++rs == kRecStages) { rs = 0; rec_parity ^= 1u; }
-            if (++os == kOpStages) { os = 0; op_parity ^= 1u; }
+            if (++sa == kAStages) { sa = 0; a_parity ^= 1u; }
             if (++unit == units) unit = 0;
         }
     } else {
         // ---- group sums
         const uint32_t quadrant = warp & 3, half = warp >> 2, trow = quadrant * 32 + lane;      // this thread's row and half of the tokens
         const uint32_t own_scale = (trow >> 6) * W::kUnitBytes + W::kCodeBytes + ((trow & 63) >> 4) * 32 + (trow & 7) * 4 + ((trow >> 3) & 1) * 2;
-        uint32_t seg = lo / units, unit = lo - seg * units, acc = 0, n_rec = 0;
+        uint32_t seg = lo / units, unit = lo - seg * units, acc = 0, n_rec = 0, n_flush = 0;
         bool ok = true;
         for (uint32_t u = lo; u < hi && ok; unit = 0, ++seg) {
             const PackedSegment& sg = a.seg[seg];
@@ -375,13 +392,18 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
                 }
             }
             if (!ok) break;
-            // this segment's sums: at most two (base and slot) meet in an element, so their order does not matter
+            // This segment's sums join the others' (an element gets one from the base and one from its token's slot, perhaps
+            // from another warp): one segment after the other.
+            if (n_flush && !__all_sync(~0u, wait_or_leave(flushed, (n_flush & 1u) ^ 1u, gone))) break;
+            ++n_flush;
             const float factor = seg ? kCodeUnit * a.lambda : kCodeUnit;
 #pragma unroll
             for (uint32_t j = 0; j < NT / 2; ++j) {
                 const uint32_t i = half * (NT / 2) + j;
-                if (i < count) atomicAdd(ysum + a.token[sg.first + i] * kTileRows + trow, factor * tot[j]);
+                if (i < count) ysum[a.token[sg.first + i] * kTileRows + trow] += factor * tot[j];
             }
+            __syncwarp();
+            if (lane == 0) bar_arrive(flushed);
         }
     }
     tc_before();
@@ -422,9 +444,10 @@ template <int NT, typename XT, int GROUP> cudaError_t launch_wide(PackedLinearAr
     typedef Wide<NT, XT, GROUP> W;
     const uint64_t blocks = (static_cast<uint64_t>(a.rows) + kTileRows - 1) / kTileRows;
     const uint64_t units = ((a.cols + 63ull) / 64 + 1) / 2 * a.n_seg;
-    // one CTA per SM, as long as each has a few units to itself
+    // One CTA per SM, as long as each has a few units to itself. Clusters of four: not all those of eight that 128 CTAs make
+    // fit the processor clusters at once (2000 x 2000, 24 tokens: 17.4 us against 11.8 us).
     a.log_ranks = 0;
-    while (a.log_ranks < 3 && (blocks << (a.log_ranks + 1)) <= static_cast<uint64_t>(sm_count) && (4ull << a.log_ranks) <= units) ++a.log_ranks;
+    while (a.log_ranks < 2 && (blocks << (a.log_ranks + 1)) <= static_cast<uint64_t>(sm_count) && (4ull << a.log_ranks) <= units) ++a.log_ranks;
     const uint32_t ranks = 1u << a.log_ranks;
     const size_t smem = W::smem(a.n_tokens);
     static std::atomic<size_t> granted[kDevices];      // a kernel has to opt in beyond 48 KiB, per device
@@ -439,7 +462,13 @@ template <int NT, typename XT, int GROUP> cudaError_t launch_wide(PackedLinearAr
         rows += operand_rows(a.seg[k].count);
     }
     const uint32_t kts = (a.cols + 63) / 64;
+    static std::atomic<int> same_split[kDevices];
     if (kts) {
+        if (device >= kDevices || !same_split[device].exchange(1, std::memory_order_relaxed)) {
+            // the same division of L1 and shared memory as the kernel that follows: changing it costs microseconds
+            const cudaError_t e = cudaFuncSetAttribute(operand_kernel<XT>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+            if (e != cudaSuccess) return e;
+        }
         operand_kernel<XT><<<dim3((kts * 8 + 255) / 256, a.seg[a.n_seg - 1].first + a.seg[a.n_seg - 1].count), 256, 0, s>>>(a);
         const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;

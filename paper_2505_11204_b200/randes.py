@@ -556,13 +556,16 @@ def _linear_tensors(x, rows: int, cols: int, y, y_dtype: int):
     return n, x_dtype, x_stride, y, y_dtype, y_stride
 
 
+_linear_workspace_bytes = functools.lru_cache(maxsize=4096)(randes_packed_linear_workspace)
+
+
 def _linear_workspace(x, cols: int, x_dtype: int, n: int, with_tasks: bool):
     """(tensor or None, its address, its bytes): what a product of more than 8 tokens lays its activations out in."""
     import torch
 
     if n <= 8:
         return None, None, 0
-    nbytes = randes_packed_linear_workspace(cols, x_dtype, n, with_tasks)
+    nbytes = _linear_workspace_bytes(cols, x_dtype, n, with_tasks)
     t = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
     return t, t.data_ptr(), nbytes
 
