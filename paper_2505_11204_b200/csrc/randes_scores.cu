@@ -3,12 +3,16 @@
 // With u = scale * z (scale = one over the temperature), M = max z, d = z - M, S = sum exp(scale d), T = sum exp(scale d) d:
 //     log p_j = scale * d_j - ln S        H = -sum p log p = ln S - scale * T / S
 //     dz_j = scale * ( g_lp (1[j = target] - p_j) - g_H p_j (log p_j + H) )
-// The differences to the maximum are taken before anything is scaled, so no term carries the rounding of a large
-// exponent; each thread keeps (M, S, T) of what it has read and rescales them when its maximum rises.
+// Everything is kept in powers of two: with c = scale log2 e an element counts 2^a, a = (z - m) c, m the greatest logit a thread
+// has read. The difference is taken before anything is scaled, so no term carries the rounding of a large exponent, and a row
+// that is sure of one token gets log probability 0 (one multiply-add z c - m c in place of the two steps would not give
+// that). Each thread keeps (m, S = sum 2^a, T = sum 2^a a) and rescales S and T when its maximum rises.
 //
-// Top alternatives without sorting: a pair of threads knows the greatest of the elements it read; the k-th largest of
-// those maxima cannot be above the k-th largest element, so only the pairs that reach it are read again (about k of 128),
-// and what reaches it is ranked. Equal logits are ordered by index.
+// Top alternatives without sorting: four threads know the greatest of the elements they read; the k-th largest of those 64
+// maxima cannot be above the k-th largest element. What reaches it is ranked, and to find that almost nothing is read again:
+// a thread remembers which batch of loads held its maximum and the greatest of its other batches, so a thread whose maximum
+// reaches the threshold (about k of 256) reads one batch again, or everything if a second batch reaches it too. Equal
+// logits are ordered by index.
 //
 // A row may be shared by a cluster of CTAs (few rows); their sums and top lists meet in the first CTA through distributed
 // shared memory.
@@ -30,7 +34,7 @@ using namespace device;
 
 constexpr int kScoreThreads = 256;
 constexpr int kScoreWarps = kScoreThreads / 32;
-constexpr int kGroups = kScoreThreads / 2;      // pairs of threads; at least kMaxTop
+constexpr int kGroups = kScoreThreads / 4;      // at least kMaxTop
 constexpr int kCandidates = 768;
 constexpr int kMaxCluster = 8;
 static_assert(kGroups >= static_cast<int>(kMaxTop), "the threshold is the k-th largest group maximum");
@@ -49,31 +53,41 @@ __device__ __forceinline__ float ex2(float x)
     return r;
 }
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// what one has read: greatest logit, sum of exp(scale (z - m)), sum of exp(scale (z - m)) (z - m)
+// what one has read: greatest logit m, S = sum 2^a, T = sum 2^a a with a = (z - m) c
 struct Sums { float m, s, t; };
 
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c)
+// S and T relative to another maximum (at least the own one): 2^(a + x) (a + x) = 2^x (2^a a + x 2^a)
+__device__ __forceinline__ void rebase(Sums& v, float m, float c)
 {
-    Sums r;
-    r.m = max_nan(a.m, b.m);
-    r.s = r.t = 0.f;
-    if (r.m == -INFINITY) return r;
-    if (a.m != -INFINITY) {
-        const float d = a.m - r.m, f = ex2(d * c);
-        r.s = f * a.s;
-        r.t = f * __fmaf_rn(a.s, d, a.t);
-        if (f == 0.f) r.s = r.t = 0.f;      // d may be infinite (the type's lowest value against a large one)
+    if (v.m == m) return;
+    const float x = (v.m - m) * c, f = ex2(x);
+    const float fx = f == 0.f ? 0.f : f * x;          // also from m = -inf: nothing was summed yet
+    v.t = f == 0.f ? 0.f : __fmaf_rn(v.s, fx, v.t * f);
+    v.s = f == 0.f ? 0.f : v.s * f;
+    v.m = m;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c)
+{
+    const float m = max_nan(a.m, b.m);
+    rebase(a, m, c);
+    rebase(b, m, c);
+    return Sums{m, a.s + b.s, a.t + b.t};
+}
+// the sums of N lanes (a power of two), in every one of them
+template <int N> __device__ __forceinline__ Sums join_lanes(Sums v, float c)
+{
+    float m = v.m;
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
+    rebase(v, m, c);
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) {
+        v.s += __shfl_xor_sync(~0u, v.s, o);
+        v.t += __shfl_xor_sync(~0u, v.t, o);
     }
-    if (b.m != -INFINITY) {
-        const float d = b.m - r.m, f = ex2(d * c);
-        if (f != 0.f) {
-            r.s += f * b.s;
-            r.t += f * __fmaf_rn(b.s, d, b.t);
-        }
-    }
-    return r;
+    return v;
 }
 
 // order of (logit, index): larger logit first, then lower index; -0 counts as +0
@@ -115,18 +129,28 @@ __device__ __forceinline__ float min3(float a, float b, float c)
     asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-template <typename T> __device__ __forceinline__ void extremes(const uint4& w, float& top, float& low);
-template <> __device__ __forceinline__ void extremes<float>(const uint4& w, float& top, float& low)
+template <typename T, int N> __device__ __forceinline__ void extremes(const uint4 (&w)[N], float& top, float& low)
 {
-    const float a = __uint_as_float(w.x), b = __uint_as_float(w.y), c = __uint_as_float(w.z), d = __uint_as_float(w.w);
-    top = max_nan(max3_nan(a, b, c), d);
-    low = fminf(min3(a, b, c), d);
-}
-template <> __device__ __forceinline__ void extremes<bf16>(const uint4& w, float& top, float& low)
-{
-    const uint32_t hi = max2_nan(max2_nan(w.x, w.y), max2_nan(w.z, w.w)), lo = min2_nan(min2_nan(w.x, w.y), min2_nan(w.z, w.w));
-    top = max_nan(__uint_as_float(hi << 16), __uint_as_float(hi & 0xFFFF0000u));
-    low = fminf(__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u));
+    if (sizeof(T) == 4) {
+        top = -INFINITY;
+        low = INFINITY;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const float a = __uint_as_float(w[u].x), b = __uint_as_float(w[u].y), c = __uint_as_float(w[u].z), d = __uint_as_float(w[u].w);
+            top = max3_nan(top, a, max3_nan(b, c, d));
+            low = min3(low, a, min3(b, c, d));
+        }
+    } else {
+        uint32_t hi = w[0].x, lo = w[0].x;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            if (u) { hi = max2_nan(hi, w[u].x); lo = min2_nan(lo, w[u].x); }
+            hi = max2_nan(hi, max2_nan(w[u].y, max2_nan(w[u].z, w[u].w)));
+            lo = min2_nan(lo, min2_nan(w[u].y, min2_nan(w[u].z, w[u].w)));
+        }
+        top = max_nan(__uint_as_float(hi << 16), __uint_as_float(hi & 0xFFFF0000u));
+        low = fminf(__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u));
+    }
 }
 
 // A CTA's share of a row: vectors [v0, v1) of the row's 16-byte aligned middle, and up to CPL - 1 single elements at
@@ -161,136 +185,154 @@ template <typename T> struct Share {
 template <typename T>
 __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_constant__ ScoreArgs a, uint32_t ranks)
 {
-    constexpr int CPL = Store<T>::CPL, U = 4;
+    constexpr int CPL = Store<T>::CPL, U = 6;
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t row = blockIdx.x / ranks, rank = blockIdx.x - row * ranks;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     __shared__ Sums s_warp[kScoreWarps];
     __shared__ Sums s_cta;
     __shared__ __align__(16) uint32_t s_group[kGroups];
-    __shared__ uint32_t s_picked[kGroups];
+    __shared__ uint32_t s_batch[kScoreThreads], s_all[kScoreThreads];     // what is read again: batches (8 v + loads), threads
     __shared__ float s_tau;
-    __shared__ unsigned int s_count, s_n_picked;
+    __shared__ unsigned int s_count, s_n_batch, s_n_all;
     __shared__ unsigned long long s_cand[kCandidates];
     __shared__ unsigned long long s_top[kMaxTop];          // this CTA's top list, best first; 0 = no element
     __shared__ unsigned long long s_best[kScoreWarps];
 
     const Share<T> sh(static_cast<const T*>(a.logits) + row * a.stride, a.vocab, rank, ranks);
+    // the target's logit is wanted at the very end: its two dependent loads start here
+    long long target = -1;
+    float target_logit = 0.f;
+    if (rank == 0 && tid == 0 && a.targets) {
+        target = a.targets[row];
+        if (target >= 0 && target < static_cast<long long>(a.vocab)) target_logit = Store<T>::load1(sh.row + target);
+    }
     const float c = a.scale * kLog2e;
     const f32x2 c2 = pack2(__float_as_uint(c), __float_as_uint(c));
     float m = -INFINITY;
     f32x2 s2 = 0, t2 = 0;                    // two partial sums each
     auto raise = [&](float to) {             // a new maximum (or a NaN)
-        const float d = m - to;
-        float f = ex2(d * c), fd = f * d;
-        if (f == 0.f) fd = 0.f;              // (also from m = -inf: nothing was summed yet)
+        const float x = (m - to) * c, f = ex2(x);
+        const float fx = f == 0.f ? 0.f : f * x;      // (also from m = -inf: nothing was summed yet)
         m = to;
-        const f32x2 f2 = pack2(__float_as_uint(f), __float_as_uint(f)), g2 = pack2(__float_as_uint(fd), __float_as_uint(fd));
-        t2 = fma2(s2, g2, mul2(t2, f2));     // sum e^(c (z - to)) (z - to) = f (t + s d)
+        const f32x2 f2 = pack2(__float_as_uint(f), __float_as_uint(f)), g2 = pack2(__float_as_uint(fx), __float_as_uint(fx));
+        t2 = fma2(s2, g2, mul2(t2, f2));
         s2 = mul2(s2, f2);
     };
-    auto add = [&](f32x2 z) {                // two logits, relative to m
-        const f32x2 d = z;
+    auto add = [&](f32x2 a2) {               // two elements 2^a
         float a0, a1;
-        unpack2(mul2(d, c2), a0, a1);
+        unpack2(a2, a0, a1);
         const f32x2 e = pack2(__float_as_uint(ex2(a0)), __float_as_uint(ex2(a1)));
         s2 = add2(s2, e);
-        t2 = fma2(e, d, t2);
+        t2 = fma2(e, a2, t2);
     };
-    auto take = [&](const uint4& raw) {
+    auto exponent = [&](float z) { return max_nan((z - m) * c, -1e30f); };      // masked logits: 2^a is 0, and 0 times a finite number is 0
+    float second = -INFINITY;                // greatest element outside the batch that holds the maximum
+    uint32_t best = 0;
+    auto take = [&](const auto& raw, uint32_t v) {       // N words of 16 bytes, from vector v on
+        constexpr int N = sizeof(raw) / 16;
         float top, low;
-        extremes<T>(raw, top, low);
+        extremes<T, N>(raw, top, low);
         if (!(top <= m)) {
-            if (top == -INFINITY) return;
+            second = m;
+            best = 8 * v + N;
             raise(max_nan(m, top));
+        } else {
+            second = fmaxf(second, top);
         }
         if (m == -INFINITY) return;
         const f32x2 neg = pack2(__float_as_uint(-m), __float_as_uint(-m));
-        f32x2 z[CPL / 2];
-        Store<T>::widen2(raw, z);
-        if (low > -1e30f) {
+        if (low > -1e30f) {                  // (times c, at most 1.5e6, that is a finite number)
 #pragma unroll
-            for (int e = 0; e < CPL / 2; ++e) add(add2(z[e], neg));
-        } else {                             // masked logits: exp gives 0, and 0 times a finite number is 0
+            for (int u = 0; u < N; ++u) {
+                f32x2 z[CPL / 2];
+                Store<T>::widen2(raw[u], z);
 #pragma unroll
-            for (int e = 0; e < CPL / 2; ++e) {
-                float a0, a1;
-                unpack2(add2(z[e], neg), a0, a1);
-                add(pack2(__float_as_uint(max_nan(a0, -1e30f)), __float_as_uint(max_nan(a1, -1e30f))));
+                for (int e = 0; e < CPL / 2; ++e) add(mul2(add2(z[e], neg), c2));
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                f32x2 z[CPL / 2];
+                Store<T>::widen2(raw[u], z);
+#pragma unroll
+                for (int e = 0; e < CPL / 2; ++e) {
+                    float z0, z1;
+                    unpack2(z[e], z0, z1);
+                    add(pack2(__float_as_uint(exponent(z0)), __float_as_uint(exponent(z1))));
+                }
             }
         }
     };
-    for (uint32_t v = sh.v0 + tid; v < sh.v1; v += kScoreThreads * U) {
+    uint32_t v = sh.v0 + tid;
+    for (; v + (U - 1) * kScoreThreads < sh.v1; v += kScoreThreads * U) {
         uint4 raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v + u * kScoreThreads < sh.v1) raw[u] = sh.load(v + u * kScoreThreads);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (v + u * kScoreThreads < sh.v1) take(raw[u]);
+        for (int u = 0; u < U; ++u) raw[u] = sh.load(v + u * kScoreThreads);
+        take(raw, v);
     }
+    // what is left, fewer than U: all loads first, then four, two and one of them at a time
+    const uint32_t left = v < sh.v1 ? (sh.v1 - v + kScoreThreads - 1) / kScoreThreads : 0u;
+    static_assert(U <= 8, "the rest is three bits");
+    uint4 four[4], two[2], one[1];
+#pragma unroll
+    for (uint32_t u = 0; u < 4; ++u)
+        if (left & 4u) four[u] = sh.load(v + u * kScoreThreads);
+#pragma unroll
+    for (uint32_t u = 0; u < 2; ++u)
+        if (left & 2u) two[u] = sh.load(v + ((left & 4u) + u) * kScoreThreads);
+    if (left & 1u) one[0] = sh.load(v + (left & 6u) * kScoreThreads);
+    if (left & 4u) take(four, v);
+    if (left & 2u) take(two, v + (left & 4u) * kScoreThreads);
+    if (left & 1u) take(one, v + (left & 6u) * kScoreThreads);
+    const float own_max = m;                 // of the vectors: single elements are offered one by one
     uint32_t idx;
     if (tid < 2 * CPL && sh.single(tid, idx)) {
         const float z = Store<T>::load1(sh.row + idx);
-        if (!(z <= m) && z != -INFINITY) raise(max_nan(m, z));
-        if (m != -INFINITY) {                // the second of the pair is masked
-            float d = max_nan(z - m, -1e30f);
-            add(pack2(__float_as_uint(d), __float_as_uint(-1e30f)));
-        }
+        if (!(z <= m)) raise(max_nan(m, z));
+        if (m != -INFINITY)                  // the second of the pair counts 0
+            add(pack2(__float_as_uint(exponent(z)), __float_as_uint(-1e30f)));
     }
     Sums me;
     {
         float s0, s1, t0, t1;
         unpack2(s2, s0, s1);
         unpack2(t2, t0, t1);
-        me.m = m;
-        me.s = s0 + s1;
-        me.t = t0 + t1;
-    }
-    // ---- sums of the CTA
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const Sums b = {__shfl_down_sync(~0u, me.m, o), __shfl_down_sync(~0u, me.s, o), __shfl_down_sync(~0u, me.t, o)};
-        me = join(me, b, c);
+        me = join_lanes<32>(Sums{m, s0 + s1, t0 + t1}, c);
     }
     if (lane == 0) s_warp[warp] = me;
     if (a.top_k) {
-        // a pair's maximum as a whole number in the logits' order; the last bits hold the pair, so that no two are equal
-        const float pm = max_nan(m, __shfl_xor_sync(~0u, m, 1));
-        if ((tid & 1) == 0) s_group[tid >> 1] = (order_of(pm) & ~(kGroups - 1u)) | (tid >> 1);
-        if (tid == 0) { s_count = 0; s_n_picked = 0; }
+        // four threads' maximum as a whole number in the logits' order; the last bits hold the group, so that no two are equal
+        float gm = max_nan(m, __shfl_xor_sync(~0u, m, 1));
+        gm = max_nan(gm, __shfl_xor_sync(~0u, gm, 2));
+        if ((tid & 3) == 0) s_group[tid >> 2] = (order_of(gm) & ~(kGroups - 1u)) | (tid >> 2);
+        if (tid == 0) s_count = s_n_batch = s_n_all = 0;
         if (tid < static_cast<int>(kMaxTop)) s_top[tid] = 0ull;
     }
     __syncthreads();
     if (warp == 0) {
-        me = lane < kScoreWarps ? s_warp[lane] : Sums{-INFINITY, 0.f, 0.f};
-#pragma unroll
-        for (int o = kScoreWarps / 2; o > 0; o >>= 1) {
-            const Sums b = {__shfl_down_sync(~0u, me.m, o), __shfl_down_sync(~0u, me.s, o), __shfl_down_sync(~0u, me.t, o)};
-            me = join(me, b, c);
-        }
+        me = join_lanes<kScoreWarps>(s_warp[lane % kScoreWarps], c);
         if (lane == 0) s_cta = me;
     }
     // ---- top list of the CTA
     if (a.top_k) {
-        const uint32_t mine = s_group[tid >> 1];
-        uint32_t before = 0;                 // pairs in front of this one; each thread of a pair counts in one half
-#pragma unroll 4
-        for (int j = 0; j < kGroups / 8; ++j) {
-            const uint4 o = reinterpret_cast<const uint4*>(s_group)[(tid & 1) * (kGroups / 8) + j];
+        const uint32_t mine = s_group[tid >> 2];
+        uint32_t before = 0;                 // groups in front of this one; each of its threads counts in a quarter
+#pragma unroll
+        for (int j = 0; j < kGroups / 16; ++j) {
+            const uint4 o = reinterpret_cast<const uint4*>(s_group)[(tid & 3) * (kGroups / 16) + j];
             before += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
         }
         before += __shfl_xor_sync(~0u, before, 1);
-        if (before < a.top_k && (tid & 1) == 0) {
-            s_picked[atomicAdd(&s_n_picked, 1u)] = tid >> 1;
-            // (below the order of the lowest finite number there is only -inf)
-            if (before == a.top_k - 1) s_tau = mine < 0x00800000u ? -INFINITY : value_of(mine & ~(kGroups - 1u));
-        }
+        before += __shfl_xor_sync(~0u, before, 2);
+        // (the group's number cut off: at most the maximum itself; below the order of the lowest finite number there is only -inf)
+        if (before == a.top_k - 1 && (tid & 3) == 0) s_tau = mine < 0x00800000u ? -INFINITY : value_of(mine & ~(kGroups - 1u));
         __syncthreads();
-        // Pairs that the cut-off last bits put behind the k-th although their maximum equals it may still hold one of the
-        // best: they are looked for among all pairs.
         const float tau = s_tau;
-        if ((tid & 1) == 0 && before >= a.top_k && (mine & ~(kGroups - 1u)) == order_of(tau)) s_picked[atomicAdd(&s_n_picked, 1u)] = tid >> 1;
+        if (own_max >= tau && own_max > -INFINITY) {
+            if (second < tau) s_batch[atomicAdd(&s_n_batch, 1u)] = best;
+            else s_all[atomicAdd(&s_n_all, 1u)] = tid;
+        }
         __syncthreads();
         auto offer = [&](float z, uint32_t i) {
             if (z >= tau && z > -INFINITY) {
@@ -298,19 +340,22 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
                 if (at < kCandidates) s_cand[at] = key_of(z, i);
             }
         };
-        const uint32_t trips = (sh.v1 - sh.v0 + kScoreThreads - 1) / kScoreThreads, again = s_n_picked * trips * 2;
-        for (uint32_t i = tid; i < again; i += kScoreThreads) {
-            const uint32_t v = sh.v0 + 2 * s_picked[i / (2 * trips)] + (i & 1) + kScoreThreads * (i % (2 * trips) / 2);
-            if (v >= sh.v1) continue;
-            const uint4 raw = sh.load(v);
+        auto look_again = [&](uint32_t v) {
+            const uint4 raw[1] = {sh.load(v)};
             float top, low;
-            extremes<T>(raw, top, low);
-            if (!(top >= tau)) continue;
+            extremes<T, 1>(raw, top, low);
+            if (!(top >= tau)) return;
             float z[CPL];
-            Store<T>::widen(raw, z);
+            Store<T>::widen(raw[0], z);
 #pragma unroll
             for (int e = 0; e < CPL; ++e) offer(z[e], sh.lead + v * CPL + e);
+        };
+        for (uint32_t i = tid; i < 8 * s_n_batch; i += kScoreThreads) {
+            const uint32_t b = s_batch[i >> 3];
+            if ((i & 7u) < (b & 7u)) look_again((b >> 3) + (i & 7u) * kScoreThreads);
         }
+        for (uint32_t w = warp; w < s_n_all; w += kScoreWarps)
+            for (uint32_t v = sh.v0 + s_all[w] + lane * kScoreThreads; v < sh.v1; v += 32 * kScoreThreads) look_again(v);
         if (tid < 2 * CPL && sh.single(tid, idx)) offer(Store<T>::load1(sh.row + idx), idx);
         __syncthreads();
         const unsigned int n = s_count;
@@ -365,14 +410,13 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         if (tid == 0) {
             a.stats[row] = all.m;
             a.stats[static_cast<size_t>(a.n_rows) + row] = ln;
-            a.entropy[row] = none ? 0.f : __fmaf_rn(-a.scale, all.t / all.s, ln);
+            a.entropy[row] = none ? 0.f : __fmaf_rn(-kLn2, all.t / all.s, ln);
             if (a.targets) {
-                const long long tk = a.targets[row];
                 float lp;
-                if (tk < 0) lp = 0.f;
-                else if (tk >= static_cast<long long>(a.vocab)) lp = NAN;
+                if (target < 0) lp = 0.f;
+                else if (target >= static_cast<long long>(a.vocab)) lp = NAN;
                 else if (none) lp = -INFINITY;
-                else lp = __fmaf_rn(a.scale, Store<T>::load1(sh.row + tk) - all.m, -ln);
+                else lp = __fmaf_rn(a.scale, target_logit - all.m, -ln);
                 a.logprob[row] = lp;
             }
         }
