@@ -1534,10 +1534,10 @@ int check_tensor(const void* p, uint64_t rows, uint64_t cols, uint64_t stride, s
     return RANDES_OK;
 }
 
-// Whether every row of the tensor starts on a 16-byte boundary.
-bool rows_aligned(const void* p, uint64_t rows, uint64_t stride, size_t elem)
+// Whether every row of the tensor starts on such a boundary.
+bool rows_aligned(const void* p, uint64_t rows, uint64_t stride, size_t elem, uint64_t boundary = 16)
 {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || (stride * elem) % 16 == 0);
+    return reinterpret_cast<uintptr_t>(p) % boundary == 0 && (rows <= 1 || (stride * elem) % boundary == 0);
 }
 
 struct Device { int index, sms; };
@@ -1625,7 +1625,8 @@ int randes_unpack_impl(const void* const* packed, uint32_t n, uint32_t group, co
         for (; first < n && a.n < kPackBatch; ++first) {
             const randes_matrix_t& m = out[first];
             if (m.rows == 0 || m.cols == 0) continue;
-            a.mat[a.n++] = UnpackMatrix{packed[first], m.data, m.stride, m.rows, m.cols, rows_aligned(m.data, m.rows, m.stride, elem) ? 1u : 0u, 0};
+            const uint32_t vec = rows_aligned(m.data, m.rows, m.stride, elem, 32) ? 2u : (rows_aligned(m.data, m.rows, m.stride, elem) ? 1u : 0u);
+            a.mat[a.n++] = UnpackMatrix{packed[first], m.data, m.stride, m.rows, m.cols, vec, 0};
         }
         if (a.n == 0) break;
         const int e = launch_unpack(out_dtype, a, stream);

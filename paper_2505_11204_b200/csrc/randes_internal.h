@@ -252,7 +252,9 @@ struct UnpackMatrix {
     const void* src;
     void* dst;
     uint64_t stride;
-    uint32_t rows, cols, vec, first_cta;
+    uint32_t rows, cols;
+    uint32_t vec;                 // rows of dst start on boundaries of: 0 an element, 1 16 bytes, 2 32 bytes
+    uint32_t first_cta;
 };
 struct UnpackArgs {
     UnpackMatrix mat[kPackBatch];

@@ -38,7 +38,7 @@ namespace {
 
 using namespace device;
 
-constexpr int kPackWarps = 8;                 // warps per CTA of the pack and unpack kernels
+constexpr int kPackWarps = 4;                 // warps per CTA of the pack and unpack kernels (8: up to a tenth slower)
 constexpr float kMinScale = 0x1p-100f;        // far enough from the subnormals for the quotient below to be exact
 
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
@@ -126,8 +126,12 @@ __device__ __forceinline__ uint32_t top_of(const uint4& w)        // bf16 pairs
 
 // One warp turns 16 rows x 128 columns into two tiles. RETRIEVE: the weight is fma(lambda, s * M, W_0) with the sign
 // bits of the unit's 128 columns out of one Philox block -- the value retrieve writes in fp32, never stored.
+//
+// Warps per SM, measured at 16384 x 4096 fp32 and 50257 x 768 bf16: a plain pack wants 32 of them (64 registers) and to keep its
+// 16-byte loads coming (fp32 41.7 us at 32 warps, 44.1 at 24; bf16 22.4 and 24.3). A retrieve holds two tensors' words: with
+// fp32 on either side 16 warps and no spills (80 us; 24 warps 98, 32 warps 118), with bf16 on both 24 (36.2 us; 38.8 at 32).
 template <typename WT, typename MT, bool RETRIEVE>
-__global__ void __launch_bounds__(kPackWarps * 32, 3) pack_kernel(const __grid_constant__ PackArgs a)
+__global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) + sizeof(MT) == 4 ? 6 : 4)) pack_kernel(const __grid_constant__ PackArgs a)
 {
     uint32_t which, rt, ku;
     if (!find_unit(a, which, rt, ku)) return;
@@ -225,9 +229,14 @@ __global__ void __launch_bounds__(kPackWarps * 32, 3) pack_kernel(const __grid_c
         *reinterpret_cast<uint32_t*>(dst + lay.scales(rt, 4 * ku + t) + g * 4) = scale_bits[0] | (scale_bits[1] << 16);
 }
 
-template <typename OT> __device__ __forceinline__ void store8(OT* row, uint32_t c, uint32_t cols, bool vec, const float (&v)[8])
+// `vec`: 0 element by element, 1 in words of 16 bytes, 2 (fp32) in words of 32 bytes: a lane's eight columns in one store, so
+// that every store fills whole sectors (16384 x 4096: 53 us against 69).
+template <typename OT> __device__ __forceinline__ void store8(OT* row, uint32_t c, uint32_t cols, uint32_t vec, const float (&v)[8])
 {
-    if (vec && c + 8 <= cols) {
+    if (sizeof(OT) == 4 && vec == 2 && c + 8 <= cols) {
+        asm volatile("st.global.cs.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(row + c), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+    } else if (vec && c + 8 <= cols) {
         Out<OT>::template store<8>(row + c, v);
     } else {
 #pragma unroll
