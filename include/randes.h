@@ -339,6 +339,8 @@ int randes_linear_gated(const randes_plan_t* plan, uint32_t task_id, float lambd
  * Every wait inside the randes_linear kernel is bounded; a thread block whose wait runs out
  * skips its tile and counts itself here.  *count = number of such blocks since the library was
  * loaded on the current device (0 in a healthy run).  Synchronises with the device.
+ * The kernels of randes_packed_linear and randes_packed_linear_tasks wait likewise and are counted here too (per warp or
+ * per block); what such a warp or block was to add up comes out as NaN.
  */
 int randes_linear_giveups(unsigned int* count);
 
@@ -489,9 +491,11 @@ int randes_retrieve_packed(const randes_plan_t* plan, uint32_t task_id, float la
  *   x, x_dtype, x_stride   device [n_tokens, cols], fp32 or bf16, x_stride elements between tokens (>= cols)
  *   y, y_dtype, y_stride   device [n_tokens, rows] likewise; must not overlap the inputs
  *   workspace, workspace_bytes   device memory, 16-byte aligned, at least randes_packed_linear_workspace() bytes: none for up
- *                 to 8 tokens; for more, the activations laid out for the tensor core.  Free again when the call's work is done
+ *                 to 8 fp32 or 16 bf16 tokens; for more, the activations laid out for the tensor core.  Free again when the
+ *                 call's work is done
  * Products are exact (an fp32 activation is taken as the sum of three bf16 terms), sums run in fp32 in a fixed order, a
- * bf16 y is rounded once.  The matrix is read once per 64 tokens; one kernel launch for up to 8 tokens, two per 64 beyond.
+ * bf16 y is rounded once.  The matrix is read once per 64 tokens, or per 8 where no workspace is needed; one kernel launch
+ * per 8 tokens there, two per 64 beyond.
  * Meant for few tokens -- for many, retrieve the weight and use a dense product.  16-byte aligned tokens are read fastest.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, WORKSPACE_TOO_SMALL, CUDA_ERROR.
  */

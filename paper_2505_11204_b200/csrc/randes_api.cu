@@ -1731,10 +1731,11 @@ int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, i
     };
     for (uint32_t first = 0, n; first < n_tokens; first += n) {
         n = std::min(kWideTokens, n_tokens - first);
-        if (n > kNarrowTokens) {
+        if (packed_is_wide(x_dtype == RANDES_BF16, n)) {
             PackedLinearArgs<kWideTokens> a;
             rc = run(a, first, n);
         } else {
+            n = std::min(kNarrowTokens, n);
             PackedLinearArgs<kNarrowTokens> a;
             rc = run(a, first, n);
         }

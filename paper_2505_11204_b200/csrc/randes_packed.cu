@@ -403,8 +403,9 @@ __global__ void __launch_bounds__(kMulWarps * 32, 2) packed_linear_kernel(const 
             ok = bar_wait(bars + stage * 8, parity);
             if (!ok) break;
             const uint32_t kt0 = kb * kBlockTiles, nt = min(static_cast<uint32_t>(kTiles), kt1 - kt0);
-#pragma unroll 1
-            for (uint32_t i = 0; i < nt; ++i) {
+#pragma unroll
+            for (uint32_t i = 0; i < static_cast<uint32_t>(kTiles); ++i) {
+                if (i >= nt) break;
                 const uint32_t kt = kt0 + i;
                 uint32_t xa[2][Act::kTerms][4];
                 Act::terms(raw[0], xa[0]);

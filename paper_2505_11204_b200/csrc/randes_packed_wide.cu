@@ -1,4 +1,4 @@
-// Products of 9 to 64 tokens with packed weights, on the fifth-generation tensor cores.
+// Products of more than a few tokens (up to 64 a launch) with packed weights, on the fifth-generation tensor cores.
 //
 // The scale of a weight belongs to a row and a group of columns, so the tensor core can only add up within a group: codes
 // (q / 64, exact in bf16) x activations over the columns of one group, in tensor memory; the group's sums then come back
@@ -499,10 +499,16 @@ template <int NT, typename XT> cudaError_t launch_group(PackedLinearArgs<kWideTo
 
 }  // namespace
 
+// The other form takes 8 tokens a launch. It reads the matrix once per launch, but two launches of it are still faster for
+// bf16 tokens (16 tokens, 16384 x 16384: 70 us against 81 us; 4096 x 4096 base and superposition: 18.2 and 18.5) three
+// are not (24 tokens: 105 against 81). fp32 tokens cost it three products each: 16 of them on
+// 4096 x 4096 base and superposition take 28.5 us against 22.5.
+bool packed_is_wide(bool x_bf16, uint32_t n_tokens) { return n_tokens > (x_bf16 ? 2 * kNarrowTokens : kNarrowTokens); }
+
 size_t packed_wide_workspace(uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks)
 {
     const uint32_t n = n_tokens < kWideTokens ? n_tokens : kWideTokens;
-    if (n_tokens <= kNarrowTokens) return 0;
+    if (!packed_is_wide(x_bf16, n_tokens)) return 0;
     // the base with every token; at worst every token has a slot of its own
     const size_t rows = operand_rows(n) + (tasks ? 8u * n : 0u);
     return rows * ((static_cast<size_t>(cols) + 63) / 64) * 128 * (x_bf16 ? 1 : 3);

@@ -539,6 +539,7 @@ template <typename T> cudaError_t launch_grad_t(const ScoreGradArgs& a, cudaStre
     constexpr uint32_t per = kGradThreads * kGradVectors * Store<T>::CPL;
     const uint32_t chunks = (a.vocab + per - 1) / per;
     if (!chunks) return cudaSuccess;
+    if (static_cast<uint64_t>(chunks) * a.n_rows > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
     score_grad_kernel<T><<<static_cast<unsigned>(chunks * a.n_rows), kGradThreads, 0, s>>>(a, chunks);
     return cudaGetLastError();
 }

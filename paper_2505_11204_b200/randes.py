@@ -350,7 +350,7 @@ def randes_retrieve_packed(plan, task_id, lam, layers, n, base, M, group, packed
 
 
 def randes_packed_linear_workspace(cols: int, x_dtype: int, n_tokens: int, with_tasks: bool) -> int:
-    """Bytes of device workspace the two calls below need (0 for up to 8 tokens)."""
+    """Bytes of device workspace the two calls below need (0 for up to 8 fp32 or 16 bf16 tokens)."""
     return int(lib().randes_packed_linear_workspace(cols, x_dtype, n_tokens, int(with_tasks)))
 
 
@@ -560,12 +560,12 @@ _linear_workspace_bytes = functools.lru_cache(maxsize=4096)(randes_packed_linear
 
 
 def _linear_workspace(x, cols: int, x_dtype: int, n: int, with_tasks: bool):
-    """(tensor or None, its address, its bytes): what a product of more than 8 tokens lays its activations out in."""
+    """(tensor or None, its address, its bytes): what a product of many tokens lays its activations out in."""
     import torch
 
-    if n <= 8:
+    nbytes = _linear_workspace_bytes(cols, x_dtype, n, with_tasks) if n > 8 else 0
+    if nbytes == 0:
         return None, None, 0
-    nbytes = _linear_workspace_bytes(cols, x_dtype, n, with_tasks)
     t = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
     return t, t.data_ptr(), nbytes
 

@@ -35,8 +35,8 @@ def test_packed_sizes():
 
 def test_workspace_sizes():
     f = randes.randes_packed_linear_workspace
-    assert f(4096, randes.F32, 0, True) == f(4096, randes.BF16, 8, True) == 0
-    assert f(4096, randes.BF16, 9, False) == 16 * 4096 * 2                  # whole groups of eight rows
+    assert f(4096, randes.F32, 0, True) == f(4096, randes.F32, 8, True) == f(4096, randes.BF16, 16, True) == 0
+    assert f(4096, randes.BF16, 17, False) == 24 * 4096 * 2                 # whole groups of eight rows
     assert f(4100, randes.F32, 64, False) == 64 * 4160 * 2 * 3              # whole tiles of columns, three terms
     assert f(4096, randes.BF16, 1000, False) == f(4096, randes.BF16, 64, False)
     assert f(4096, randes.BF16, 64, True) > f(4096, randes.BF16, 64, False)
