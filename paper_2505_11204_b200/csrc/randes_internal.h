@@ -245,6 +245,7 @@ struct PackMatrix {
 struct PackArgs {
     PackMatrix mat[kPackBatch];
     uint32_t n, group;
+    uint32_t tile_bytes;          // shared memory per warp, set by the launcher
     float lambda;
     DevTask task;
 };
@@ -259,6 +260,7 @@ struct UnpackMatrix {
 struct UnpackArgs {
     UnpackMatrix mat[kPackBatch];
     uint32_t n, group;
+    uint32_t tile_bytes;          // shared memory per warp, set by the launcher
 };
 // One packed matrix and the tokens that go through it: positions first .. first + count - 1 of the token lists.
 struct PackedSegment {

@@ -80,6 +80,64 @@ template <typename T> __device__ __forceinline__ void widen8(const Eight<T>& r, 
     }
 }
 
+// Rows that do not start on 16-byte boundaries go through shared memory, element by element but neighbours together: a warp's
+// 16 x 128 tile, rows a little apart so that the lanes' 16-byte accesses fall into different banks. (Each lane touching its
+// own eight columns in memory took 71 us instead of 12 to unpack 4001 x 4001 bf16, retrieve-and-pack 43 instead of 27.)
+template <typename T> struct Tile {
+    static constexpr uint32_t kPitch = 128 * sizeof(T) + 16;
+    static constexpr uint32_t kBytes = 16 * kPitch;
+};
+template <typename T>
+__device__ __forceinline__ void tile_in(unsigned char* tile, const T* m, uint64_t stride, uint32_t rt, uint32_t ku, uint32_t rows, uint32_t cols, int lane)
+{
+#pragma unroll 4
+    for (uint32_t i = 0; i < 16; ++i) {
+        const uint32_t r = rt * 16 + i;
+        const T* from = m + r * stride;
+        T* to = reinterpret_cast<T*>(tile + i * Tile<T>::kPitch);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t c = ku * 128 + j * 32 + lane;
+            to[j * 32 + lane] = r < rows && c < cols ? from[c] : T(0.f);
+        }
+    }
+    __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void tile_out(const unsigned char* tile, T* m, uint64_t stride, uint32_t rt, uint32_t ku, uint32_t rows, uint32_t cols, int lane)
+{
+    __syncwarp();
+#pragma unroll 4
+    for (uint32_t i = 0; i < 16; ++i) {
+        const uint32_t r = rt * 16 + i;
+        if (r >= rows) break;
+        T* to = m + r * stride;
+        const T* from = reinterpret_cast<const T*>(tile + i * Tile<T>::kPitch);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t c = ku * 128 + j * 32 + lane;
+            if (c < cols) to[c] = from[j * 32 + lane];
+        }
+    }
+}
+template <typename T> __device__ __forceinline__ Eight<T> from_tile(const unsigned char* tile, uint32_t row, uint32_t c)
+{
+    Eight<T> v;
+#pragma unroll
+    for (int h = 0; h < static_cast<int>(sizeof(T)) / 2; ++h) v.w[h] = *reinterpret_cast<const uint4*>(tile + row * Tile<T>::kPitch + c * sizeof(T) + h * 16);
+    return v;
+}
+
+__device__ __forceinline__ void to_tile(float* at, const float (&v)[8])
+{
+    reinterpret_cast<float4*>(at)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(at)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void to_tile(bf16* at, const float (&v)[8])
+{
+    *reinterpret_cast<uint4*>(at) = make_uint4(Out<bf16>::pack(v[0], v[1]), Out<bf16>::pack(v[2], v[3]), Out<bf16>::pack(v[4], v[5]), Out<bf16>::pack(v[6], v[7]));
+}
+
 // Which matrix of the launch a CTA works on, and the warp's 16-row x 128-column unit in it.
 template <typename Args> __device__ __forceinline__ bool find_unit(const Args& a, uint32_t& which, uint32_t& rt, uint32_t& ku)
 {
@@ -141,6 +199,9 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
     const bool whole = ku * 128 + 128 <= cols && rt * 16 + 16 <= m.rows;       // the unit lies inside the matrix
     const int per = a.group >> 5;     // 32-column quarters per group: 1, 2 or 4
 
+    extern __shared__ __align__(16) unsigned char tiles[];        // only where a matrix of the launch needs it
+    unsigned char* tile = tiles + (threadIdx.x >> 5) * a.tile_bytes;
+
     uint4 blk = make_uint4(0, 0, 0, 0);
     if (RETRIEVE && m.flip) blk = philox4x32_10(ku, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1);
     uint32_t scale_bits[2];           // of quarter t
@@ -161,6 +222,10 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
         if (whole && (m.vec & 1u)) {
 #pragma unroll
             for (int p = 0; p < 4; ++p) raw[p] = load8<WT>(w + c0 + 32 * p);
+        } else if (!(m.vec & 1u)) {
+            if (h == 0) tile_in<WT>(tile, static_cast<const WT*>(m.src), m.stride, rt, ku, m.rows, cols, lane);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) raw[p] = from_tile<WT>(tile, h * 8 + g, 32 * p + 8 * t);
         } else {
 #pragma unroll
             for (int p = 0; p < 4; ++p) raw[p] = gather8<WT>(w, c0 + 32 * p, r < m.rows ? cols : 0u);
@@ -169,6 +234,11 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
             if (whole && (m.vec & 2u)) {
 #pragma unroll
                 for (int p = 0; p < 4; ++p) add[p] = load8<MT>(sup + c0 + 32 * p);
+            } else if (!(m.vec & 2u)) {
+                unsigned char* second = tile + Tile<WT>::kBytes;
+                if (h == 0) tile_in<MT>(second, static_cast<const MT*>(m.m), cols, rt, ku, m.rows, cols, lane);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) add[p] = from_tile<MT>(second, h * 8 + g, 32 * p + 8 * t);
             } else {
 #pragma unroll
                 for (int p = 0; p < 4; ++p) add[p] = gather8<MT>(sup, c0 + 32 * p, r < m.rows ? cols : 0u);
@@ -229,14 +299,14 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
         *reinterpret_cast<uint32_t*>(dst + lay.scales(rt, 4 * ku + t) + g * 4) = scale_bits[0] | (scale_bits[1] << 16);
 }
 
-// `vec`: 0 element by element, 1 in words of 16 bytes, 2 (fp32) in words of 32 bytes: a lane's eight columns in one store, so
+// `vec`: 1 in words of 16 bytes, 2 (fp32) in words of 32 bytes: a lane's eight columns in one store, so
 // that every store fills whole sectors (16384 x 4096: 53 us against 69).
 template <typename OT> __device__ __forceinline__ void store8(OT* row, uint32_t c, uint32_t cols, uint32_t vec, const float (&v)[8])
 {
     if (sizeof(OT) == 4 && vec == 2 && c + 8 <= cols) {
         asm volatile("st.global.cs.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                      ::"l"(row + c), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
-    } else if (vec && c + 8 <= cols) {
+    } else if (c + 8 <= cols) {
         Out<OT>::template store<8>(row + c, v);
     } else {
 #pragma unroll
@@ -255,6 +325,8 @@ template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack
     const uint32_t cols = m.cols;
     const PackedLayout lay(m.rows, cols, a.group);
     const char* src = static_cast<const char*>(m.src);
+    extern __shared__ __align__(16) unsigned char tiles[];
+    unsigned char* tile = tiles + (threadIdx.x >> 5) * a.tile_bytes;
     uint4 w[2];
     w[0] = __ldcs(reinterpret_cast<const uint4*>(src + lay.codes(rt, 2 * ku) + lane * 16));
     w[1] = lay.has_tile(2 * ku + 1) ? __ldcs(reinterpret_cast<const uint4*>(src + lay.codes(rt, 2 * ku + 1) + lane * 16)) : make_uint4(0, 0, 0, 0);
@@ -270,7 +342,7 @@ template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint32_t r = rt * 16 + h * 8 + g;
-            if (r >= m.rows) continue;
+            if (m.vec && r >= m.rows) continue;
             const float s = __uint_as_float(h ? sb & 0xFFFF0000u : sb << 16);
             float v[8];
 #pragma unroll
@@ -278,15 +350,16 @@ template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack
                 const uint32_t pair = q[e >> 2][((e >> 1) & 1) * 2 + h];
                 v[e] = kCodeUnit * __uint_as_float(e & 1 ? pair & 0xFFFF0000u : pair << 16) * s;
             }
-            store8<OT>(static_cast<OT*>(m.dst) + r * m.stride, c, cols, m.vec, v);
+            if (m.vec) store8<OT>(static_cast<OT*>(m.dst) + r * m.stride, c, cols, m.vec, v);
+            else to_tile(reinterpret_cast<OT*>(tile + (h * 8 + g) * Tile<OT>::kPitch) + 32 * p + 8 * t, v);
         }
     }
+    if (!m.vec) tile_out<OT>(tile, static_cast<OT*>(m.dst), m.stride, rt, ku, m.rows, cols, lane);
 }
 
 // ---- products with a few tokens -----------------------------------------------------------------
 constexpr int kMulWarps = 8;
 constexpr int kDevices = 64;
-
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
@@ -313,8 +386,9 @@ constexpr int kRows = 16 * kRowTiles;
 // times the CTAs of a cluster; the other warps of the CTA do the same for other row blocks. A warp takes 64 rows along:
 // what it does per tile of activations (three-way split, signs) is paid once for four tiles of codes. Each warp feeds
 // itself: codes and scales through a ring of two stages, one bulk copy per stage, activations one tile ahead in registers;
-// no warp waits for another until the end. Its sums of one segment stay in registers until its run leaves the segment. All partial sums meet in shared memory, those of a cluster's CTAs through distributed
-// shared memory, and are added in a fixed order: results do not depend on timing.
+// no warp waits for another until the end. Its sums of one segment stay in registers until its run leaves the segment. All
+// partial sums meet in shared memory, those of a cluster's CTAs through distributed shared memory, and are added in a fixed
+// order: results do not depend on timing.
 template <typename XT, int GROUP>
 __global__ void __launch_bounds__(kMulWarps * 32, 2) packed_linear_kernel(const __grid_constant__ PackedLinearArgs<kNarrowTokens> a)
 {
@@ -522,11 +596,12 @@ template <typename XT, int GROUP> cudaError_t launch_mul(PackedLinearArgs<kNarro
 {
     const PackedLayout lay(a.rows, a.cols, a.group);
     const uint64_t total = static_cast<uint64_t>(lay.col_blocks) * a.n_seg, blocks = (a.rows + kRows - 1) / kRows;
-    // two CTAs of eight warps per SM, as long as every warp has a record: first the warps of a CTA share rows, then CTAs do
-    const uint64_t want = static_cast<uint64_t>(sm_count) * 2 * kMulWarps;
+    // As many warps to a row block as still fit the SMs at once (two CTAs each), as long as every warp has a record: first the
+    // warps of a CTA share rows, then the CTAs of a cluster do. (One and a third rounds of CTAs instead of one: no faster.)
+    const uint64_t slots = static_cast<uint64_t>(sm_count) * 2;
     a.log_split = a.log_ranks = 0;
-    while (a.log_split < 3 && (blocks << a.log_split) < want && (2u << a.log_split) <= total) ++a.log_split;
-    while (a.log_split == 3 && a.log_ranks < 3 && (blocks << (4 + a.log_ranks)) <= want && (16ull << a.log_ranks) <= total) ++a.log_ranks;
+    while (a.log_split < 3 && ((blocks << (a.log_split + 1)) + kMulWarps - 1) / kMulWarps <= slots && (2u << a.log_split) <= total) ++a.log_split;
+    while (a.log_split == 3 && a.log_ranks < 3 && (blocks << (a.log_ranks + 1)) <= slots && (16ull << a.log_ranks) <= total) ++a.log_ranks;
     const uint32_t blocks_cta = kMulWarps >> a.log_split, ranks = 1u << a.log_ranks;
     const uint32_t n_pos = a.seg[a.n_seg - 1].first + a.seg[a.n_seg - 1].count;
     a.ring_at = (kMulWarps * n_pos + (ranks > 1 ? blocks_cta * a.n_tokens : 0)) * kRows * static_cast<uint32_t>(sizeof(float));
@@ -589,25 +664,35 @@ int launch_pack(int w_dtype, int m_dtype, bool retrieve, PackArgs& a, void* stre
     if (!grid) return 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     constexpr int kThreads = kPackWarps * 32;
-    if (!retrieve) {
-        if (w_dtype == 1) pack_kernel<bf16, bf16, false><<<grid, kThreads, 0, s>>>(a);
-        else pack_kernel<float, float, false><<<grid, kThreads, 0, s>>>(a);
-    } else if (w_dtype == 1) {
-        if (m_dtype == 1) pack_kernel<bf16, bf16, true><<<grid, kThreads, 0, s>>>(a);
-        else pack_kernel<bf16, float, true><<<grid, kThreads, 0, s>>>(a);
-    } else {
-        if (m_dtype == 1) pack_kernel<float, bf16, true><<<grid, kThreads, 0, s>>>(a);
-        else pack_kernel<float, float, true><<<grid, kThreads, 0, s>>>(a);
-    }
-    return static_cast<int>(cudaGetLastError());
+    const uint32_t all = retrieve ? 3u : 1u;
+    a.tile_bytes = 0;
+    for (uint32_t i = 0; i < a.n; ++i)
+        if ((a.mat[i].vec & all) != all)
+            a.tile_bytes = (w_dtype == 1 ? Tile<bf16>::kBytes : Tile<float>::kBytes) + (retrieve ? (m_dtype == 1 ? Tile<bf16>::kBytes : Tile<float>::kBytes) : 0u);
+    const size_t smem = static_cast<size_t>(kPackWarps) * a.tile_bytes;
+    auto run = [&](auto kernel) {
+        if (smem > 48 * 1024) {
+            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+            if (e != cudaSuccess) return static_cast<int>(e);
+        }
+        kernel<<<grid, kThreads, smem, s>>>(a);
+        return static_cast<int>(cudaGetLastError());
+    };
+    if (!retrieve) return w_dtype == 1 ? run(pack_kernel<bf16, bf16, false>) : run(pack_kernel<float, float, false>);
+    if (w_dtype == 1) return m_dtype == 1 ? run(pack_kernel<bf16, bf16, true>) : run(pack_kernel<bf16, float, true>);
+    return m_dtype == 1 ? run(pack_kernel<float, bf16, true>) : run(pack_kernel<float, float, true>);
 }
 
 int launch_unpack(int out_dtype, UnpackArgs& a, void* stream)
 {
     const unsigned grid = deal_ctas(a.mat, a.n);
     if (!grid) return 0;
-    if (out_dtype == 1) unpack_kernel<bf16><<<grid, kPackWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    else unpack_kernel<float><<<grid, kPackWarps * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    a.tile_bytes = 0;
+    for (uint32_t i = 0; i < a.n; ++i)
+        if (!a.mat[i].vec) a.tile_bytes = out_dtype == 1 ? Tile<bf16>::kBytes : Tile<float>::kBytes;
+    const size_t smem = static_cast<size_t>(kPackWarps) * a.tile_bytes;
+    if (out_dtype == 1) unpack_kernel<bf16><<<grid, kPackWarps * 32, smem, static_cast<cudaStream_t>(stream)>>>(a);
+    else unpack_kernel<float><<<grid, kPackWarps * 32, smem, static_cast<cudaStream_t>(stream)>>>(a);
     return static_cast<int>(cudaGetLastError());
 }
 
