@@ -10,15 +10,13 @@
 // workspace (signs applied; an fp32 activation as three bf16 terms), one tile of 64 columns after the other, swizzled as
 // the tensor core wants them. The product kernel has one CTA per SM, whose warps keep to one task each:
 //   warps 0-7    group sums: a thread owns one row and half the tokens
-//   warps 8-15   operand A: codes to bf16 (K-major, 128-byte swizzle), 16 rows each
+//   warps 8-15   operand A: codes to bf16, 16 rows each, straight into tensor memory (by way of shared memory: a fifth slower)
 //   warp 16      copies records (one lane, bulk copies), owns tensor memory
 //   warp 17      issues tcgen05.mma (one lane): M = 128 rows, N = tokens of the segment rounded up to 16
 //   warp 18      copies operand B (one lane, bulk copies)
-// A hand-over between roles costs hundreds of cycles however little it hands over, so a stage is 128 columns (64: 69 us
-// against 51 us for an 8192 x 8192 base and superposition with 64 tokens; warps that do all of the work in turn: 86 us).
-// What bounds it there is shared memory: per stage of 128 rows x 128 columns the codes come in (8 KiB), go out as bf16
-// (32 KiB), are read by the tensor core (32 KiB) next to operand B (16 KiB in, 16 KiB out) -- 112 KiB or 900 cycles at 128
-// bytes a cycle, against 370 cycles of HBM time. More stages (4 and 6 of records, 5 of B) change nothing.
+// The order of the columns in a product step is the one in which the lanes hold the codes (operand B is laid out alike), so
+// that a decoded word is four registers of operand A as they are. A hand-over between roles costs hundreds of cycles however
+// little it hands over: stages are 128 columns, and one hand-over per stage passes on all its sums and frees what came before.
 //
 // Every wait is bounded; a CTA whose wait runs out raises a flag, all roles leave, what is in flight is waited for, tensor
 // memory is freed, its sums become NaN and a device counter records the event.
@@ -43,9 +41,9 @@ constexpr int kSumWarps = 8, kAWarps = 8;
 constexpr int kAFirst = kSumWarps, kCopyWarp = kAFirst + kAWarps, kMmaWarp = kCopyWarp + 1, kCopyBWarp = kMmaWarp + 1;
 constexpr int kThreads = (kCopyBWarp + 1) * 32;
 constexpr uint32_t kTileRows = 128;
-constexpr uint32_t kATile = kTileRows * 128;       // 128 rows x 64 bf16
 
-// ---- mbarriers with any count, bounded waits that also end when the CTA has given up
+// ---- mbarriers with any count, bounded waits that also end when the CTA has given up: of one lane, and of a whole warp (every
+// lane asks and the warp votes, so that no branch diverges: 20 cycles where nothing has to be waited for, a loop per lane takes 80)
 __device__ __forceinline__ void bar_init_n(uint32_t bar, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ bool wait_or_leave(uint32_t bar, uint32_t parity, volatile uint32_t* gone)
@@ -58,6 +56,17 @@ __device__ __forceinline__ bool wait_or_leave(uint32_t bar, uint32_t parity, vol
     return false;
 }
 
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gone)
+{
+    for (uint32_t i = 0; i < kWaitLimit; ++i) {
+        if (__all_sync(~0u, bar_try(bar, parity))) return true;
+        if ((i & 63u) == 63u && __any_sync(~0u, *gone != 0)) return false;
+    }
+    if ((threadIdx.x & 31) == 0 && atomicExch(const_cast<uint32_t*>(gone), 1u) == 0u) atomicAdd(&g_wide_giveups, 1u);
+    __syncwarp();
+    return false;
+}
+
 // ---- tcgen05
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -65,13 +74,13 @@ __device__ __forceinline__ void tc_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)      // A in tensor memory
 {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void tc_load16(uint32_t addr, uint32_t* v)
 {
@@ -80,6 +89,15 @@ __device__ __forceinline__ void tc_load16(uint32_t addr, uint32_t* v)
         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
           "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(addr) : "memory");
+}
+// 16 rows x 32 words: lane 4 g + t holds words 4 i + t of rows g (v[2 i]) and g + 8 (v[2 i + 1])
+__device__ __forceinline__ void tc_store16x32(uint32_t addr, const uint32_t* v)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+          "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
 }
 __device__ __forceinline__ bool elect_one()
 {
@@ -102,18 +120,22 @@ template <int NT, typename XT, int GROUP> struct Wide {
     static constexpr uint32_t kCodeBytes = kBlockTiles * 4 * 512, kRecord = kCodeBytes + (HALF ? 256 : 128);
     static constexpr uint32_t kUnitBytes = 2 / kBlockTiles * kRecord;       // 64 rows x 128 columns
     static constexpr uint32_t kBTile = NT * 128;
-    // Stages of 128 columns: operand A, operand B, records. What limits them is shared memory; what they hide is one hand-over
-    // for A, an L2 latency for B, an HBM latency for the records.
-    static constexpr uint32_t kABytes = 2 * kATile, kBBytes = 2 * kTerms * kBTile;
-    static constexpr uint32_t kAStages = kTerms == 1 ? 3 : 2, kBStages = kTerms == 3 && NT == 64 ? 2 : 4;
-    static constexpr uint32_t kRecStages = NT == 32 ? 4 : (kTerms == 1 ? 3 : 2);
-    static constexpr uint32_t kAccs = 256 / NT;
-    static constexpr uint32_t kAAt = 0, kBAt = kAStages * kABytes;          // 1024-byte aligned operands first
-    static constexpr uint32_t kRecAt = kBAt + kBStages * kBBytes;
+    // Stages of 128 columns: operand A (half of tensor memory), operand B and records (as shared memory allows). What they
+    // hide is one hand-over for A, an L2 latency for B, an HBM latency for the records.
+    static constexpr uint32_t kAWords = 64, kBBytes = 2 * kTerms * kBTile;
+    static constexpr uint32_t kAStages = 4, kBStages = kTerms == 3 ? (NT == 64 ? 3 : 4) : 6;
+    static constexpr uint32_t kRecStages = kTerms == 3 && NT == 64 ? 5 : 8;
+    // The sums of a stage's groups go over to the other warps together -- in two batches where they take more than 128 columns
+    // of tensor memory --, and the hand-over also says that operands A and B of what came before are free.
+    static constexpr uint32_t kGroups = 128 / GROUP, kBatches = kGroups * NT > 128 ? 2 : 1, kPer = kGroups / kBatches;
+    static constexpr uint32_t kRing = 256 / (kPer * NT);                    // batches of sums in tensor memory
+    static constexpr uint32_t kDone = 16;                                   // barriers that batches complete in turn
+    static_assert(kDone >= kBatches * kBStages && kDone >= kBatches * kAStages && kDone >= kBatches * kRecStages && kDone >= kRing, "nobody may miss a whole turn");
+    static constexpr uint32_t kBAt = 0, kRecAt = kBStages * kBBytes;        // 1024-byte aligned operand first
     static constexpr uint32_t kBarsAt = kRecAt + kRecStages * 2 * kUnitBytes;
     static constexpr uint32_t kYAt = kBarsAt + 512;
     static_assert(kYAt + NT * kTileRows * 4 + 1024 <= 227 * 1024, "shared memory of a CTA");
-    static constexpr uint32_t kTmem = 256;
+    static constexpr uint32_t kTmem = 512, kTmemA = 256;                    // sums, operand A
     static size_t smem(uint32_t n_tokens) { return 1024 + kYAt + static_cast<size_t>(n_tokens) * kTileRows * sizeof(float); }
 };
 
@@ -148,17 +170,22 @@ __global__ void __launch_bounds__(256) operand_kernel(const __grid_constant__ Pa
             for (int k = 0; k < Act::kTerms; ++k) w[k][e] ^= mask;
         }
     }
+    // pair e of this lane's eight columns (t of the tile's half h) goes where operand A has it: word t of 16-byte chunk 4 h + e
     char* to = static_cast<char*>(a.operands) + a.operand_at[seg] * (static_cast<size_t>(kts) * 128 * Act::kTerms) +
-               static_cast<size_t>(chunk >> 3) * rows * 128 * Act::kTerms + row * 128 + (((chunk & 7) ^ (row & 7)) * 16);
+               static_cast<size_t>(chunk >> 3) * rows * 128 * Act::kTerms + row * 128 + (chunk & 3) * 4;
 #pragma unroll
-    for (int k = 0; k < Act::kTerms; ++k) *reinterpret_cast<uint4*>(to + static_cast<size_t>(k) * rows * 128) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t at = (((chunk & 4) + e) ^ (row & 7)) * 16;
+#pragma unroll
+        for (int k = 0; k < Act::kTerms; ++k) *reinterpret_cast<uint32_t*>(to + static_cast<size_t>(k) * rows * 128 + at) = w[k][e];
+    }
 }
 
 template <int NT, typename XT, int GROUP>
 __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_constant__ PackedLinearArgs<kWideTokens> a)
 {
     typedef Wide<NT, XT, GROUP> W;
-    constexpr uint32_t kAStages = W::kAStages, kBStages = W::kBStages, kRecStages = W::kRecStages, kAccs = W::kAccs;
+    constexpr uint32_t kAStages = W::kAStages, kBStages = W::kBStages, kRecStages = W::kRecStages, kRing = W::kRing;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw_at = static_cast<uint32_t>(__cvta_generic_to_shared(smem_raw));
     const uint32_t base = (raw_at + 1023u) & ~1023u;
@@ -166,16 +193,14 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
     float* ysum = reinterpret_cast<float*>(gbase + W::kYAt);                      // [token][row]
     const uint32_t bars = base + W::kBarsAt;
     auto rec_full = [&](uint32_t s) { return bars + 8 * s; };
-    auto rec_free = [&](uint32_t s) { return bars + 64 + 8 * s; };
+    auto b_full = [&](uint32_t s) { return bars + 64 + 8 * s; };
     auto a_full = [&](uint32_t s) { return bars + 128 + 8 * s; };
-    auto a_free = [&](uint32_t s) { return bars + 160 + 8 * s; };
-    auto b_full = [&](uint32_t s) { return bars + 192 + 8 * s; };
-    auto b_free = [&](uint32_t s) { return bars + 256 + 8 * s; };
-    auto acc_full = [&](uint32_t s) { return bars + 320 + 8 * s; };
-    auto acc_free = [&](uint32_t s) { return bars + 384 + 8 * s; };
-    const uint32_t flushed = bars + 448;
-    volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(gbase + W::kBarsAt + 456);
+    auto done = [&](uint32_t n) { return bars + 160 + 8 * (n % W::kDone); };      // batch n of sums is in tensor memory
+    auto summed = [&](uint32_t n) { return bars + 288 + 8 * (n % W::kDone); };    // and has been read
+    const uint32_t flushed = bars + 416, drained = bars + 424;
+    volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(gbase + W::kBarsAt + 432);
     volatile uint32_t* gone = tmem_ptr + 1;
+    auto last_batch = [&](uint32_t i) { return i * W::kBatches + W::kBatches - 1; };      // of the CTA's i-th stage
 
     cg::cluster_group cluster = cg::this_cluster();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -188,29 +213,21 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
     const uint32_t lo = static_cast<uint32_t>(total * rank >> lr), hi = static_cast<uint32_t>(total * (rank + 1) >> lr);
 
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < kRecStages; ++s) {
-            bar_init_n(rec_full(s), 1);
-            bar_init_n(rec_free(s), kAWarps + kSumWarps);
+        for (uint32_t s = 0; s < kRecStages; ++s) bar_init_n(rec_full(s), 1);
+        for (uint32_t s = 0; s < kBStages; ++s) bar_init_n(b_full(s), 1);
+        for (uint32_t s = 0; s < kAStages; ++s) bar_init_n(a_full(s), kAWarps);
+        for (uint32_t s = 0; s < W::kDone; ++s) {
+            bar_init_n(done(s), 1);
+            bar_init_n(summed(s), kSumWarps);
         }
-        for (uint32_t s = 0; s < kAStages; ++s) {
-            bar_init_n(a_full(s), kAWarps);
-            bar_init_n(a_free(s), 1);
-        }
-        for (uint32_t s = 0; s < kBStages; ++s) {
-            bar_init_n(b_full(s), 1);
-            bar_init_n(b_free(s), 1);
-        }
-        for (uint32_t s = 0; s < kAccs; ++s) {
-            bar_init_n(acc_full(s), 1);
-            bar_init_n(acc_free(s), kSumWarps);
-        }
+        bar_init_n(drained, 1);
         bar_init_n(flushed, kSumWarps);
         *gone = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == kCopyWarp) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + W::kBarsAt + 456), "r"(W::kTmem) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + W::kBarsAt + 432), "r"(W::kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     for (uint32_t i = threadIdx.x; i < a.n_tokens * kTileRows; i += kThreads) ysum[i] = 0.f;
@@ -225,7 +242,10 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
             uint32_t seg = lo / units, unit = lo - seg * units, n_issued = 0;
             for (uint32_t u = lo; u < hi; ++u, ++n_issued) {
                 const uint32_t s = n_issued % kRecStages;
-                if (!wait_or_leave(rec_free(s), ((n_issued / kRecStages) & 1u) ^ 1u, gone)) break;
+                if (n_issued >= kRecStages) {      // whose codes went into products that have been read, and whose scales with them
+                    const uint32_t n = last_batch(n_issued - kRecStages);
+                    if (!wait_or_leave(summed(n), (n / W::kDone) & 1u, gone)) break;
+                }
                 const uint32_t kb = W::kBlockTiles == 2 ? unit : 2 * unit;
                 const uint32_t bytes = min(2 / W::kBlockTiles, kbs - kb) * W::kRecord;
                 const char* src = static_cast<const char*>(a.seg[seg].packed) + (static_cast<size_t>(2 * block) * kbs + kb) * W::kRecord;
@@ -245,7 +265,10 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
             uint32_t seg = lo / units, unit = lo - seg * units, n_issued = 0;
             for (uint32_t u = lo; u < hi; ++u, ++n_issued) {
                 const uint32_t s = n_issued % kBStages, bytes = operand_rows(a.seg[seg].count) * 128 * W::kTerms, all = min(2u, kts - 2 * unit) * bytes;
-                if (!wait_or_leave(b_free(s), ((n_issued / kBStages) & 1u) ^ 1u, gone)) break;
+                if (n_issued >= kBStages) {
+                    const uint32_t n = last_batch(n_issued - kBStages);
+                    if (!wait_or_leave(done(n), (n / W::kDone) & 1u, gone)) break;
+                }
                 bar_expect(b_full(s), all);
                 bulk_copy(base + W::kBAt + s * W::kBBytes,
                           static_cast<const char*>(a.operands) + a.operand_at[seg] * (static_cast<size_t>(kts) * 128 * W::kTerms) +
@@ -258,149 +281,146 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
         }
     } else if (warp == kMmaWarp) {
         // ---- products. The whole warp walks the loop, so that descriptors stay in uniform registers; one lane issues.
-        uint32_t seg = lo / units, unit = lo - seg * units, sa = 0, a_parity = 0, sb = 0, b_parity = 0, acc = 0, acc_parity = 1;
+        uint32_t seg = lo / units, unit = lo - seg * units, sa = 0, a_parity = 0, sb = 0, b_parity = 0, batch = 0, slot = 0;
         const bool leader = elect_one();
-        const uint64_t desc_a = operand_desc(base + W::kAAt), desc_b = operand_desc(base + W::kBAt);
+        const uint64_t desc_b = operand_desc(base + W::kBAt);
         bool ok = true;
         for (uint32_t u = lo; u < hi; ++u) {
             const uint32_t rows = operand_rows(a.seg[seg].count), nt = min(2u, kts - 2 * unit), term = rows * 128 / 16;
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((rows + 8) / 16 << 18) | ((kTileRows >> 4) << 24);     // N = rows rounded up to 16
-            ok = wait_or_leave(b_full(sb), b_parity, gone) && wait_or_leave(a_full(sa), a_parity, gone);
+            ok = warp_wait(b_full(sb), b_parity, gone) && warp_wait(a_full(sa), a_parity, gone);
             if (!ok) break;
-            const uint64_t da = desc_a + sa * (W::kABytes / 16), db = desc_b + sb * (W::kBBytes / 16);
-            // a sum of products per group: kSteps steps of 16 columns
-            constexpr uint32_t kSteps = GROUP / 16;
+            const uint32_t at_a = tmem + W::kTmemA + sa * W::kAWords;
+            const uint64_t db = desc_b + sb * (W::kBBytes / 16);
+            constexpr uint32_t kSteps = GROUP / 16;       // product steps of 16 columns per group
 #pragma unroll
-            for (uint32_t first = 0; first < 8; first += kSteps) {
-                if (first / 4 >= nt) break;
-                ok = wait_or_leave(acc_free(acc), acc_parity, gone);
+            for (uint32_t b = 0; b < W::kBatches; ++b) {
+                if (batch >= kRing) ok = warp_wait(summed(batch - kRing), ((batch - kRing) / W::kDone) & 1u, gone);
                 if (!ok) break;
                 tc_after();
                 if (leader) {
-                    const uint32_t d = tmem + acc * NT;
 #pragma unroll
-                    for (uint32_t k = first; k < first + kSteps; ++k)
+                    for (uint32_t k = b * W::kPer * kSteps; k < (b + 1) * W::kPer * kSteps; ++k)
                         if (k / 4 < nt) {
+                            const uint32_t d = tmem + (slot * W::kPer + (k / kSteps) % W::kPer) * NT;
 #pragma unroll
                             for (uint32_t h = 0; h < W::kTerms; ++h)
-                                tc_mma(d, da + (k / 4) * (kATile / 16) + 2 * (k % 4), db + (k / 4) * W::kTerms * term + h * term + 2 * (k % 4), idesc, !(k == first && h == 0));
+                                tc_mma(d, at_a + 8 * k, db + (k / 4) * W::kTerms * term + h * term + 2 * (k % 4), idesc, !(k % kSteps == 0 && h == 0));
                         }
-                    tc_commit(acc_full(acc));
+                    tc_commit(done(batch));
                 }
-                if (++acc == kAccs) { acc = 0; acc_parity ^= 1u; }
+                ++batch;
+                if (++slot == kRing) slot = 0;
             }
             if (!ok) break;
-            if (leader) {
-                tc_commit(a_free(sa));
-                tc_commit(b_free(sb));
-            }
             if (++sa == kAStages) { sa = 0; a_parity ^= 1u; }
             if (++sb == kBStages) { sb = 0; b_parity ^= 1u; }
             if (++unit == units) { unit = 0; ++seg; }
             __syncwarp();
         }
-        if (!ok && leader) {    // what was issued ends before tensor memory is freed: one more commit on a barrier that nobody waits for now
-            tc_commit(a_free(sa));
-            (void)bar_wait(a_free(sa), a_parity);
+        if (!ok && leader) {    // what was issued ends before tensor memory is freed
+            tc_commit(drained);
+            (void)bar_wait(drained, 0u);
         }
         __syncwarp();
     } else if (warp >= kAFirst) {
-        // ---- operand A: this warp's row tile
-        const uint32_t g = lane >> 2, t = lane & 3, tile = warp - kAFirst;
-        const bool odd = g & 1;
+        // ---- operand A: one row tile. A warp reaches the quarter of tensor memory that its number modulo four names.
+        const uint32_t tile = (warp & 3) * 2 + ((warp >> 2) & 1);
         const uint32_t from = base + W::kRecAt + (tile >> 2) * W::kUnitBytes + (tile & 3) * 512 + lane * 16;
-        const uint32_t to = base + W::kAAt + (tile * 16 + g) * 128;
-        uint32_t unit = lo % units, rs = 0, rec_parity = 0, sa = 0, a_parity = 1;
+        const uint32_t to = tmem + W::kTmemA + (tile << 20);
+        uint32_t unit = lo % units, rs = 0, rec_parity = 0, sa = 0;
         for (uint32_t u = lo; u < hi; ++u) {
-            if (!__all_sync(~0u, wait_or_leave(rec_full(rs), rec_parity, gone))) break;
+            if (!warp_wait(rec_full(rs), rec_parity, gone)) break;
             const uint32_t rec = from + rs * 2 * W::kUnitBytes;
             const bool two = 2 * unit + 1 < kts;
             const uint4 c0 = lds128(rec), c1 = lds128(rec + (W::kBlockTiles == 2 ? 2048 : W::kRecord));   // (a second tile that does not exist: not used)
-            if (!__all_sync(~0u, wait_or_leave(a_free(sa), a_parity, gone))) break;       // the products have read the stage
+            if (u - lo >= kAStages) {        // the products have read the stage
+                const uint32_t n = last_batch(u - lo - kAStages);
+                if (!warp_wait(done(n), (n / W::kDone) & 1u, gone)) break;
+                tc_after();
+            }
+            __syncwarp();
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 if (i == 1 && !two) break;
                 const uint4 cw = i ? c1 : c0;
-                // lanes with odd g take the right half of the tile first, so that the stores of eight lanes fall into different banks
-                const uint32_t w[4] = {odd ? cw.z : cw.x, odd ? cw.w : cw.y, odd ? cw.x : cw.z, odd ? cw.y : cw.w};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t q0[4], q1[4];
-                    decode(w[2 * h], q0);
-                    decode(w[2 * h + 1], q1);
-                    const uint32_t at = to + sa * W::kABytes + i * kATile + ((((h ^ (g & 1)) * 4 + t) ^ g) * 16);
-                    sts128(at, make_uint4(q0[0], q0[2], q1[0], q1[2]));
-                    sts128(at + 1024, make_uint4(q0[1], q0[3], q1[1], q1[3]));
-                }
+                uint32_t q[4][4];          // word j: operand registers, the 16 columns of product step 4 i + j
+                decode(cw.x, q[0]);
+                decode(cw.y, q[1]);
+                decode(cw.z, q[2]);
+                decode(cw.w, q[3]);
+                tc_store16x32(to + sa * W::kAWords + 32 * i, &q[0][0]);
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // the tensor core reads through the async proxy
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            tc_before();
             __syncwarp();
-            if (lane == 0) {
-                bar_arrive(a_full(sa));
-                bar_arrive(rec_free(rs));
-            }
+            if (lane == 0) bar_arrive(a_full(sa));
             if (++rs == kRecStages) { rs = 0; rec_parity ^= 1u; }
-            if (++sa == kAStages) { sa = 0; a_parity ^= 1u; }
+            if (++sa == kAStages) sa = 0;
             if (++unit == units) unit = 0;
         }
     } else {
         // ---- group sums
         const uint32_t quadrant = warp & 3, half = warp >> 2, trow = quadrant * 32 + lane;      // this thread's row and half of the tokens
         const uint32_t own_scale = (trow >> 6) * W::kUnitBytes + W::kCodeBytes + ((trow & 63) >> 4) * 32 + (trow & 7) * 4 + ((trow >> 3) & 1) * 2;
-        uint32_t seg = lo / units, unit = lo - seg * units, acc = 0, n_rec = 0, n_flush = 0;
+        uint32_t seg = lo / units, unit = lo - seg * units, batch = 0, n_rec = 0, n_flush = 0;
         bool ok = true;
         for (uint32_t u = lo; u < hi && ok; unit = 0, ++seg) {
             const PackedSegment& sg = a.seg[seg];
             const uint32_t count = sg.count;
-            float tot[NT / 2];
+            f32x2 tot[NT / 4];             // two tokens each
 #pragma unroll
-            for (int j = 0; j < NT / 2; ++j) tot[j] = 0.f;
+            for (int j = 0; j < NT / 4; ++j) tot[j] = 0;
             for (; unit < units && u < hi && ok; ++unit, ++u, ++n_rec) {
                 const uint32_t rs = n_rec % kRecStages, sat = base + W::kRecAt + rs * 2 * W::kUnitBytes + own_scale;
-                ok = __all_sync(~0u, wait_or_leave(rec_full(rs), (n_rec / kRecStages) & 1u, gone));
+                ok = warp_wait(rec_full(rs), (n_rec / kRecStages) & 1u, gone);
                 if (!ok) break;
-                const uint32_t nt = min(2u, kts - 2 * unit), n_sums = GROUP == 128 ? 1 : (W::HALF ? 2 * nt : nt);
-                float scale[W::HALF ? 4 : 2];
+                const uint32_t nt = min(2u, kts - 2 * unit);
+                float scale[W::kGroups];
 #pragma unroll
-                for (int k = 0; k < (GROUP == 128 ? 1 : (W::HALF ? 4 : 2)); ++k)      // (a tile that does not exist: never used)
+                for (int k = 0; k < static_cast<int>(W::kGroups); ++k)      // (a tile that does not exist: never used)
                     scale[k] = __uint_as_float(lds_u16(sat + (W::HALF ? (k >> 1) * W::kRecord + (k & 1) * 128 : k * W::kRecord)) << 16);
-                __syncwarp();
-                if (lane == 0) bar_arrive(rec_free(rs));
 #pragma unroll
-                for (uint32_t k = 0; k < (GROUP == 128 ? 1 : (W::HALF ? 4 : 2)); ++k) {
-                    if (k >= n_sums) break;
-                    const uint32_t b = acc % kAccs;
-                    ok = __all_sync(~0u, wait_or_leave(acc_full(b), (acc / kAccs) & 1u, gone));
+                for (uint32_t b = 0; b < W::kBatches; ++b, ++batch) {
+                    ok = warp_wait(done(batch), (batch / W::kDone) & 1u, gone);
                     if (!ok) break;
                     tc_after();
-                    const uint32_t at = tmem + (quadrant << 21) + b * NT + half * (NT / 2);
-                    uint32_t v[NT / 2];
+                    __syncwarp();
+                    const uint32_t slot = batch % kRing;
 #pragma unroll
-                    for (int c = 0; c < NT / 2; c += 16)
-                        if (half * (NT / 2) + c < count) tc_load16(at + c, v + c);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    for (uint32_t k = b * W::kPer; k < (b + 1) * W::kPer; ++k) {
+                        if (k * GROUP / 64 >= nt) break;
+                        const uint32_t at = tmem + (quadrant << 21) + (slot * W::kPer + k % W::kPer) * NT + half * (NT / 2);
+                        const f32x2 scale2 = pack2(__float_as_uint(scale[k]), __float_as_uint(scale[k]));
+                        uint32_t v[NT / 2];
 #pragma unroll
-                    for (int c = 0; c < NT / 2; c += 16)
-                        if (half * (NT / 2) + c < count) {
+                        for (int c = 0; c < NT / 2; c += 16)
+                            if (half * (NT / 2) + c < count) tc_load16(at + c, v + c);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) tot[c + j] = __fmaf_rn(scale[k], __uint_as_float(v[c + j]), tot[c + j]);
-                        }
+                        for (int c = 0; c < NT / 2; c += 16)
+                            if (half * (NT / 2) + c < count) {
+#pragma unroll
+                                for (int j = 0; j < 16; j += 2) tot[(c + j) / 2] = fma2(pack2(v[c + j], v[c + j + 1]), scale2, tot[(c + j) / 2]);
+                            }
+                    }
                     tc_before();
                     __syncwarp();
-                    if (lane == 0) bar_arrive(acc_free(b));
-                    ++acc;
+                    if (lane == 0) bar_arrive(summed(batch));
                 }
             }
             if (!ok) break;
             // This segment's sums join the others' (an element gets one from the base and one from its token's slot, perhaps
             // from another warp): one segment after the other.
-            if (n_flush && !__all_sync(~0u, wait_or_leave(flushed, (n_flush & 1u) ^ 1u, gone))) break;
+            if (n_flush && !warp_wait(flushed, (n_flush & 1u) ^ 1u, gone)) break;
             ++n_flush;
             const float factor = seg ? kCodeUnit * a.lambda : kCodeUnit;
 #pragma unroll
             for (uint32_t j = 0; j < NT / 2; ++j) {
                 const uint32_t i = half * (NT / 2) + j;
-                if (i < count) ysum[a.token[sg.first + i] * kTileRows + trow] += factor * tot[j];
+                float even, odd;
+                unpack2(tot[j / 2], even, odd);
+                if (i < count) ysum[a.token[sg.first + i] * kTileRows + trow] += factor * (j & 1 ? odd : even);
             }
             __syncwarp();
             if (lane == 0) bar_arrive(flushed);
