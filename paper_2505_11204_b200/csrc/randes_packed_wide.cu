@@ -16,7 +16,7 @@
 //   warp 18      copies operand B (one lane, bulk copies)
 // The order of the columns in a product step is the one in which the lanes hold the codes (operand B is laid out alike), so
 // that a decoded word is four registers of operand A as they are. A hand-over between roles costs hundreds of cycles however
-// little it hands over: stages are 128 columns, and one hand-over per stage passes on all its sums and frees what came before.
+// little it hands over: stages are 128 or 256 columns, and what is passed on also frees what came before.
 //
 // Every wait is bounded; a CTA whose wait runs out raises a flag, all roles leave, what is in flight is waited for, tensor
 // memory is freed, its sums become NaN and a device counter records the event.
@@ -118,16 +118,19 @@ template <int NT, typename XT, int GROUP> struct Wide {
     static constexpr uint32_t kTerms = sizeof(XT) == 4 ? 3 : 1;
     static constexpr uint32_t kBlockTiles = GROUP == 128 ? 2 : 1;
     static constexpr uint32_t kCodeBytes = kBlockTiles * 4 * 512, kRecord = kCodeBytes + (HALF ? 256 : 128);
-    static constexpr uint32_t kUnitBytes = 2 / kBlockTiles * kRecord;       // 64 rows x 128 columns
+    // Column tiles per stage: as many as shared memory allows with a second stage behind it, since what a warp does per stage
+    // besides its work costs as much as the work (64 tokens, 16384 x 16384: 53 us, 73 with half of that)
+    static constexpr uint32_t kTiles = kTerms == 3 && NT == 64 ? 2 : 4;
+    static constexpr uint32_t kUnitBytes = kTiles / kBlockTiles * kRecord;  // 64 rows
     static constexpr uint32_t kBTile = NT * 128;
-    // Stages of 128 columns: operand A (half of tensor memory), operand B and records (as shared memory allows). What they
-    // hide is one hand-over for A, an L2 latency for B, an HBM latency for the records.
-    static constexpr uint32_t kAWords = 64, kBBytes = 2 * kTerms * kBTile;
-    static constexpr uint32_t kAStages = 4, kBStages = kTerms == 3 ? (NT == 64 ? 3 : 4) : 6;
-    static constexpr uint32_t kRecStages = kTerms == 3 && NT == 64 ? 5 : 8;
-    // The sums of a stage's groups go over to the other warps together -- in two batches where they take more than 128 columns
+    // Stages: operand A (half of tensor memory), operand B and records (as shared memory allows). What they hide is one
+    // hand-over for A, an L2 latency for B, an HBM latency for the records.
+    static constexpr uint32_t kAWords = kTiles * 32, kBBytes = kTiles * kTerms * kBTile;
+    static constexpr uint32_t kAStages = 256 / kAWords, kBStages = kTerms == 3 ? (NT == 64 ? 3 : 2) : 3;
+    static constexpr uint32_t kRecStages = kTiles == 2 ? 5 : 4;
+    // The sums of a stage's groups go over to the other warps together -- in batches where they take more than 128 columns
     // of tensor memory --, and the hand-over also says that operands A and B of what came before are free.
-    static constexpr uint32_t kGroups = 128 / GROUP, kBatches = kGroups * NT > 128 ? 2 : 1, kPer = kGroups / kBatches;
+    static constexpr uint32_t kGroups = kTiles * 64 / GROUP, kBatches = kGroups * NT > 128 ? kGroups * NT / 128 : 1, kPer = kGroups / kBatches;
     static constexpr uint32_t kRing = 256 / (kPer * NT);                    // batches of sums in tensor memory
     static constexpr uint32_t kDone = 16;                                   // barriers that batches complete in turn
     static_assert(kDone >= kBatches * kBStages && kDone >= kBatches * kAStages && kDone >= kBatches * kRecStages && kDone >= kRing, "nobody may miss a whole turn");
@@ -206,8 +209,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t lr = a.log_ranks, ranks = 1u << lr, rank = blockIdx.x & (ranks - 1);
     const uint32_t block = blockIdx.x >> lr;                                      // 128 rows = row blocks 2 block, 2 block + 1
-    const uint32_t kts = (a.cols + 63) / 64, units = max((kts + 1) / 2, 1u);
-    const uint32_t kbs = W::kBlockTiles == 2 ? units : kts;                       // records per row block
+    const uint32_t kts = (a.cols + 63) / 64, units = max((kts + W::kTiles - 1) / W::kTiles, 1u);
+    const uint32_t kbs = (kts + W::kBlockTiles - 1) / W::kBlockTiles;                       // records per row block
     const bool second = (2 * block + 1) * 64 < a.rows;                            // the second row block exists
     const uint64_t total = kts ? static_cast<uint64_t>(units) * a.n_seg : 0u;
     const uint32_t lo = static_cast<uint32_t>(total * rank >> lr), hi = static_cast<uint32_t>(total * (rank + 1) >> lr);
@@ -237,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
     const uint32_t tmem = *tmem_ptr;
 
     if (warp == kCopyWarp) {
-        // ---- records, in stages of 128 columns
+        // ---- records
         if (lane == 0) {
             uint32_t seg = lo / units, unit = lo - seg * units, n_issued = 0;
             for (uint32_t u = lo; u < hi; ++u, ++n_issued) {
@@ -246,8 +249,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
                     const uint32_t n = last_batch(n_issued - kRecStages);
                     if (!wait_or_leave(summed(n), (n / W::kDone) & 1u, gone)) break;
                 }
-                const uint32_t kb = W::kBlockTiles == 2 ? unit : 2 * unit;
-                const uint32_t bytes = min(2 / W::kBlockTiles, kbs - kb) * W::kRecord;
+                const uint32_t kb = unit * (W::kTiles / W::kBlockTiles);
+                const uint32_t bytes = min(W::kTiles / W::kBlockTiles, kbs - kb) * W::kRecord;
                 const char* src = static_cast<const char*>(a.seg[seg].packed) + (static_cast<size_t>(2 * block) * kbs + kb) * W::kRecord;
                 const uint32_t to = base + W::kRecAt + s * 2 * W::kUnitBytes;
                 bar_expect(rec_full(s), second ? 2 * bytes : bytes);
@@ -264,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
         if (lane == 0) {
             uint32_t seg = lo / units, unit = lo - seg * units, n_issued = 0;
             for (uint32_t u = lo; u < hi; ++u, ++n_issued) {
-                const uint32_t s = n_issued % kBStages, bytes = operand_rows(a.seg[seg].count) * 128 * W::kTerms, all = min(2u, kts - 2 * unit) * bytes;
+                const uint32_t s = n_issued % kBStages, bytes = operand_rows(a.seg[seg].count) * 128 * W::kTerms, all = min(W::kTiles, kts - W::kTiles * unit) * bytes;
                 if (n_issued >= kBStages) {
                     const uint32_t n = last_batch(n_issued - kBStages);
                     if (!wait_or_leave(done(n), (n / W::kDone) & 1u, gone)) break;
@@ -272,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
                 bar_expect(b_full(s), all);
                 bulk_copy(base + W::kBAt + s * W::kBBytes,
                           static_cast<const char*>(a.operands) + a.operand_at[seg] * (static_cast<size_t>(kts) * 128 * W::kTerms) +
-                              static_cast<size_t>(2 * unit) * bytes, all, b_full(s));
+                              static_cast<size_t>(W::kTiles * unit) * bytes, all, b_full(s));
                 if (++unit == units) { unit = 0; ++seg; }
             }
             if (*gone)      // let what was issued land
@@ -286,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
         const uint64_t desc_b = operand_desc(base + W::kBAt);
         bool ok = true;
         for (uint32_t u = lo; u < hi; ++u) {
-            const uint32_t rows = operand_rows(a.seg[seg].count), nt = min(2u, kts - 2 * unit), term = rows * 128 / 16;
+            const uint32_t rows = operand_rows(a.seg[seg].count), nt = min(W::kTiles, kts - W::kTiles * unit), term = rows * 128 / 16;
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((rows + 8) / 16 << 18) | ((kTileRows >> 4) << 24);     // N = rows rounded up to 16
             ok = warp_wait(b_full(sb), b_parity, gone) && warp_wait(a_full(sa), a_parity, gone);
             if (!ok) break;
@@ -332,8 +335,11 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
         for (uint32_t u = lo; u < hi; ++u) {
             if (!warp_wait(rec_full(rs), rec_parity, gone)) break;
             const uint32_t rec = from + rs * 2 * W::kUnitBytes;
-            const bool two = 2 * unit + 1 < kts;
-            const uint4 c0 = lds128(rec), c1 = lds128(rec + (W::kBlockTiles == 2 ? 2048 : W::kRecord));   // (a second tile that does not exist: not used)
+            const uint32_t nt = min(W::kTiles, kts - W::kTiles * unit);
+            uint4 c[W::kTiles];
+#pragma unroll
+            for (uint32_t i = 0; i < W::kTiles; ++i)       // (a tile that does not exist: not used)
+                c[i] = lds128(rec + i / W::kBlockTiles * W::kRecord + i % W::kBlockTiles * 2048);
             if (u - lo >= kAStages) {        // the products have read the stage
                 const uint32_t n = last_batch(u - lo - kAStages);
                 if (!warp_wait(done(n), (n / W::kDone) & 1u, gone)) break;
@@ -341,14 +347,13 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
             }
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (i == 1 && !two) break;
-                const uint4 cw = i ? c1 : c0;
+            for (uint32_t i = 0; i < W::kTiles; ++i) {
+                if (i >= nt) break;
                 uint32_t q[4][4];          // word j: operand registers, the 16 columns of product step 4 i + j
-                decode(cw.x, q[0]);
-                decode(cw.y, q[1]);
-                decode(cw.z, q[2]);
-                decode(cw.w, q[3]);
+                decode(c[i].x, q[0]);
+                decode(c[i].y, q[1]);
+                decode(c[i].z, q[2]);
+                decode(c[i].w, q[3]);
                 tc_store16x32(to + sa * W::kAWords + 32 * i, &q[0][0]);
             }
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
                 const uint32_t rs = n_rec % kRecStages, sat = base + W::kRecAt + rs * 2 * W::kUnitBytes + own_scale;
                 ok = warp_wait(rec_full(rs), (n_rec / kRecStages) & 1u, gone);
                 if (!ok) break;
-                const uint32_t nt = min(2u, kts - 2 * unit);
+                const uint32_t nt = min(W::kTiles, kts - W::kTiles * unit);
                 float scale[W::kGroups];
 #pragma unroll
                 for (int k = 0; k < static_cast<int>(W::kGroups); ++k)      // (a tile that does not exist: never used)
@@ -463,11 +468,11 @@ template <int NT, typename XT, int GROUP> cudaError_t launch_wide(PackedLinearAr
 {
     typedef Wide<NT, XT, GROUP> W;
     const uint64_t blocks = (static_cast<uint64_t>(a.rows) + kTileRows - 1) / kTileRows;
-    const uint64_t units = ((a.cols + 63ull) / 64 + 1) / 2 * a.n_seg;
+    const uint64_t tiles = (a.cols + 63ull) / 64 * a.n_seg;
     // One CTA per SM, as long as each has a few units to itself. Clusters of four: not all those of eight that 128 CTAs make
     // fit the processor clusters at once (2000 x 2000, 24 tokens: 17.4 us against 11.8 us).
     a.log_ranks = 0;
-    while (a.log_ranks < 2 && (blocks << (a.log_ranks + 1)) <= static_cast<uint64_t>(sm_count) && (4ull << a.log_ranks) <= units) ++a.log_ranks;
+    while (a.log_ranks < 2 && (blocks << (a.log_ranks + 1)) <= static_cast<uint64_t>(sm_count) && (8ull << a.log_ranks) <= tiles) ++a.log_ranks;
     const uint32_t ranks = 1u << a.log_ranks;
     const size_t smem = W::smem(a.n_tokens);
     static std::atomic<size_t> granted[kDevices];      // a kernel has to opt in beyond 48 KiB, per device
