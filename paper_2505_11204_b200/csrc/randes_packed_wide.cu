@@ -151,6 +151,7 @@ template <typename XT>
 __global__ void __launch_bounds__(256) operand_kernel(const __grid_constant__ PackedLinearArgs<kWideTokens> a)
 {
     typedef Acts<XT> Act;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the product kernel sets itself up meanwhile
     const uint32_t kts = (a.cols + 63) / 64, chunk = blockIdx.x * 256 + threadIdx.x, pos = blockIdx.y;
     if (chunk >= kts * 8) return;
     uint32_t seg = 0;
@@ -265,6 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
     } else if (warp == kCopyBWarp) {
         // ---- operand B
         if (lane == 0) {
+            asm volatile("griddepcontrol.wait;" ::: "memory");       // for the kernel that lays it out
             uint32_t seg = lo / units, unit = lo - seg * units, n_issued = 0;
             for (uint32_t u = lo; u < hi; ++u, ++n_issued) {
                 const uint32_t s = n_issued % kBStages, bytes = operand_rows(a.seg[seg].count) * 128 * W::kTerms, all = min(W::kTiles, kts - W::kTiles * unit) * bytes;
@@ -504,12 +506,15 @@ template <int NT, typename XT, int GROUP> cudaError_t launch_wide(PackedLinearAr
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = ranks;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    // The kernel may start while the one that lays out operand B (launched the ordinary way, behind everything before it) runs
+    at[ranks > 1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[ranks > 1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = ranks > 1;
+    cfg.numAttrs = (ranks > 1) + (kts > 0);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, packed_wide_kernel<NT, XT, GROUP>, a);
     if (e == cudaSuccess) ++*launched;
     return e;
