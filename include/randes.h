@@ -491,15 +491,15 @@ int randes_retrieve_packed(const randes_plan_t* plan, uint32_t task_id, float la
  *   x, x_dtype, x_stride   device [n_tokens, cols], fp32 or bf16, x_stride elements between tokens (>= cols)
  *   y, y_dtype, y_stride   device [n_tokens, rows] likewise; must not overlap the inputs
  *   workspace, workspace_bytes   device memory, 16-byte aligned, at least randes_packed_linear_workspace() bytes: none for up
- *                 to 8 fp32 or 16 bf16 tokens; for more, the activations laid out for the tensor core.  Free again when the
- *                 call's work is done
+ *                 to 8 bf16 tokens, nor for up to 8 fp32 tokens unless the matrix is large; otherwise the activations laid out
+ *                 for the tensor core.  Free again when the call's work is done
  * Products are exact (an fp32 activation is taken as the sum of three bf16 terms), sums run in fp32 in a fixed order, a
- * bf16 y is rounded once.  The matrix is read once per 64 tokens, or per 8 where no workspace is needed; one kernel launch
- * per 8 tokens there, two per 64 beyond.
+ * bf16 y is rounded once.  The matrix is read once per 64 tokens; two kernel launches per 64 tokens, one where no workspace is
+ * needed.
  * Meant for few tokens -- for many, retrieve the weight and use a dense product.  16-byte aligned tokens are read fastest.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, WORKSPACE_TOO_SMALL, CUDA_ERROR.
  */
-size_t randes_packed_linear_workspace(uint32_t cols, randes_dtype_t x_dtype, uint32_t n_tokens, int with_tasks);   /* host-only */
+size_t randes_packed_linear_workspace(uint32_t rows, uint32_t cols, randes_dtype_t x_dtype, uint32_t n_tokens, int with_tasks);   /* host-only */
 int randes_packed_linear(const void* packed, uint32_t rows, uint32_t cols, uint32_t group, const void* x, randes_dtype_t x_dtype,
                          uint64_t x_stride, uint32_t n_tokens, void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* workspace,
                          size_t workspace_bytes, void* stream);

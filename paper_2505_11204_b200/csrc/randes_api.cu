@@ -1695,10 +1695,10 @@ int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, i
                   int y_dtype, uint64_t y_stride, float lambda, bool tasks, void* workspace, size_t workspace_bytes, void* stream, Fill&& fill)
 {
     int rc;
-    const size_t need = packed_wide_workspace(cols, x_dtype == RANDES_BF16, n_tokens, tasks);
+    const size_t need = packed_wide_workspace(rows, cols, x_dtype == RANDES_BF16, n_tokens, tasks);
     if (need) {
         if (!workspace || workspace_bytes < need)
-            return fail(RANDES_WORKSPACE_TOO_SMALL, "%u tokens of %u columns need a workspace of %zu bytes, got %zu", n_tokens, cols, need, workspace ? workspace_bytes : 0);
+            return fail(RANDES_WORKSPACE_TOO_SMALL, "%u tokens on %u x %u need a workspace of %zu bytes, got %zu", n_tokens, rows, cols, need, workspace ? workspace_bytes : 0);
         if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(RANDES_MISALIGNED, "workspace = %p is not 16-byte aligned", workspace);
     }
     const size_t xe = elem_size(x_dtype), ye = elem_size(y_dtype);
@@ -1731,7 +1731,7 @@ int packed_linear(uint32_t rows, uint32_t cols, uint32_t group, const void* x, i
     };
     for (uint32_t first = 0, n; first < n_tokens; first += n) {
         n = std::min(kWideTokens, n_tokens - first);
-        if (packed_is_wide(x_dtype == RANDES_BF16, n)) {
+        if (packed_is_wide(rows, cols, x_dtype == RANDES_BF16, n, tasks)) {
             PackedLinearArgs<kWideTokens> a;
             rc = run(a, first, n);
         } else {
@@ -1911,9 +1911,9 @@ int randes_retrieve_packed(const randes_plan_t* plan, uint32_t task_id, float la
     return guarded("randes_retrieve_packed", [&] { return randes_retrieve_packed_impl(plan, task_id, lambda, layers, n, base, M, group, packed, stream); });
 }
 
-size_t randes_packed_linear_workspace(uint32_t cols, randes_dtype_t x_dtype, uint32_t n_tokens, int with_tasks)
+size_t randes_packed_linear_workspace(uint32_t rows, uint32_t cols, randes_dtype_t x_dtype, uint32_t n_tokens, int with_tasks)
 {
-    return packed_wide_workspace(cols, x_dtype == RANDES_BF16, n_tokens, with_tasks != 0);
+    return packed_wide_workspace(rows, cols, x_dtype == RANDES_BF16, n_tokens, with_tasks != 0);
 }
 
 int randes_packed_linear(const void* packed, uint32_t rows, uint32_t cols, uint32_t group, const void* x, randes_dtype_t x_dtype,

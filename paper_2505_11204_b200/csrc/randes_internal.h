@@ -294,8 +294,8 @@ int launch_unpack(int out_dtype, UnpackArgs& a, void* stream);
 int packed_giveups(unsigned int* count);   // warps of the product that gave up on a bounded wait (synchronises)
 int launch_packed_linear(PackedLinearArgs<kNarrowTokens>& a, bool x_bf16, int sm_count, int device, void* stream);
 // randes_packed_wide.cu
-bool packed_is_wide(bool x_bf16, uint32_t n_tokens);         // which of the two forms takes that many tokens
-size_t packed_wide_workspace(uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks);     // bytes for calls of that many tokens
+bool packed_is_wide(uint32_t rows, uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks);      // which of the two forms takes a call
+size_t packed_wide_workspace(uint32_t rows, uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks);     // bytes for calls of that many tokens
 int launch_packed_wide(PackedLinearArgs<kWideTokens>& a, bool x_bf16, int sm_count, int device, int* launched, void* stream);
 int packed_wide_giveups(unsigned int* count);
 

@@ -529,19 +529,25 @@ template <int NT, typename XT> cudaError_t launch_group(PackedLinearArgs<kWideTo
 
 }  // namespace
 
-// The other form takes 8 tokens a launch. It reads the matrix once per launch, but two launches of it are still faster for
-// bf16 tokens (16 tokens, 16384 x 16384: 70 us against 81 us; 4096 x 4096 base and superposition: 18.2 and 18.5) three
-// are not (24 tokens: 105 against 81). fp32 tokens cost it three products each: 16 of them on
-// 4096 x 4096 base and superposition take 28.5 us against 22.5.
-bool packed_is_wide(bool x_bf16, uint32_t n_tokens) { return n_tokens > (x_bf16 ? 2 * kNarrowTokens : kNarrowTokens); }
+// The other form takes 8 tokens a launch and needs no second kernel, which small matrices notice most: 8 bf16 tokens on
+// 2000 x 2000 take 4.9 us against 8.3, on 16384 x 8192 20 against 26. Two launches of it are slower nearly everywhere (16
+// tokens: 9.6 against 8.9 and 38 against 27 us). fp32 tokens cost it three products and the splitting of the activations for
+// every row block: it loses them where the matrix is large (one token, 16384 x 8192: 35 us against 29; with a superposition
+// 67 against 52; 4096 x 4096: 7.6 against 8.9 and 13.0 against 12.1), unless the rows are short, so that a CTA of this form has little to
+// do once it has set itself up (50257 x 768: 14.4 against 17.7; with a superposition, so with twice the columns, 28.7 against 27.9).
+bool packed_is_wide(uint32_t rows, uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks)
+{
+    const uint64_t columns = static_cast<uint64_t>(cols) << tasks;       // base, and one slot of the superposition
+    return n_tokens > kNarrowTokens || (!x_bf16 && n_tokens && columns >= 1536 && rows * columns >= (1u << 25));
+}
 
-size_t packed_wide_workspace(uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks)
+size_t packed_wide_workspace(uint32_t rows, uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks)
 {
     const uint32_t n = n_tokens < kWideTokens ? n_tokens : kWideTokens;
-    if (!packed_is_wide(x_bf16, n_tokens)) return 0;
+    if (!packed_is_wide(rows, cols, x_bf16, n_tokens, tasks)) return 0;
     // the base with every token; at worst every token has a slot of its own
-    const size_t rows = operand_rows(n) + (tasks ? 8u * n : 0u);
-    return rows * ((static_cast<size_t>(cols) + 63) / 64) * 128 * (x_bf16 ? 1 : 3);
+    const size_t lines = operand_rows(n) + (tasks ? 8u * n : 0u);
+    return lines * ((static_cast<size_t>(cols) + 63) / 64) * 128 * (x_bf16 ? 1 : 3);
 }
 
 int launch_packed_wide(PackedLinearArgs<kWideTokens>& a, bool x_bf16, int sm_count, int device, int* launched, void* stream)

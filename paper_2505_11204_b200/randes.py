@@ -143,7 +143,7 @@ def lib():
         L.randes_unpack.restype = ctypes.c_int
         L.randes_retrieve_packed.argtypes = [vp, u32, f32, vp, u32, vp, vp, u32, vp, vp]
         L.randes_retrieve_packed.restype = ctypes.c_int
-        L.randes_packed_linear_workspace.argtypes = [u32, dt, u32, ctypes.c_int]
+        L.randes_packed_linear_workspace.argtypes = [u32, u32, dt, u32, ctypes.c_int]
         L.randes_packed_linear_workspace.restype = sz
         L.randes_packed_linear.argtypes = [vp, u32, u32, u32, vp, dt, u64, u32, vp, dt, u64, vp, sz, vp]
         L.randes_packed_linear.restype = ctypes.c_int
@@ -349,9 +349,9 @@ def randes_retrieve_packed(plan, task_id, lam, layers, n, base, M, group, packed
     _check(lib().randes_retrieve_packed(plan, task_id, lam, _addr(layers), n, _addr(base), _addr(M), group, _addr(packed), stream))
 
 
-def randes_packed_linear_workspace(cols: int, x_dtype: int, n_tokens: int, with_tasks: bool) -> int:
-    """Bytes of device workspace the two calls below need (0 for up to 8 fp32 or 16 bf16 tokens)."""
-    return int(lib().randes_packed_linear_workspace(cols, x_dtype, n_tokens, int(with_tasks)))
+def randes_packed_linear_workspace(rows: int, cols: int, x_dtype: int, n_tokens: int, with_tasks: bool) -> int:
+    """Bytes of device workspace the two calls below need (0 for up to 8 tokens, unless they are fp32 and the matrix is large)."""
+    return int(lib().randes_packed_linear_workspace(rows, cols, x_dtype, n_tokens, int(with_tasks)))
 
 
 def randes_packed_linear(packed, rows, cols, group, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, stream, workspace=None,
@@ -559,11 +559,11 @@ def _linear_tensors(x, rows: int, cols: int, y, y_dtype: int):
 _linear_workspace_bytes = functools.lru_cache(maxsize=4096)(randes_packed_linear_workspace)
 
 
-def _linear_workspace(x, cols: int, x_dtype: int, n: int, with_tasks: bool):
+def _linear_workspace(x, rows: int, cols: int, x_dtype: int, n: int, with_tasks: bool):
     """(tensor or None, its address, its bytes): what a product of many tokens lays its activations out in."""
     import torch
 
-    nbytes = _linear_workspace_bytes(cols, x_dtype, n, with_tasks) if n > 8 else 0
+    nbytes = _linear_workspace_bytes(rows, cols, x_dtype, n, with_tasks)
     if nbytes == 0:
         return None, None, 0
     t = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
@@ -574,7 +574,7 @@ def packed_linear(x, w: PackedMatrix, y=None, y_dtype: int = F32):
     """x: [n_tokens, cols] fp32 or bf16 CUDA tensor (rows may be strided); returns y = x W^T [n_tokens, rows]."""
     rows, cols = w.rows, w.cols
     n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, rows, cols, y, y_dtype)
-    workspace, ws_at, ws_bytes = _linear_workspace(x, cols, x_dtype, n, False)
+    workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, False)
     _call(lib().randes_packed_linear(w.address, rows, cols, w.group, x.data_ptr(), x_dtype, x_stride, n, y.data_ptr(), y_dtype, y_stride,
                                      ws_at, ws_bytes, _stream_of(x)))
     return y
@@ -871,7 +871,7 @@ class Plan:
             _refuse("%d task ids for %d tokens" % (len(task_ids), n))
         if not isinstance(task_ids, ctypes.Array):
             task_ids = (ctypes.c_uint32 * max(n, 1))(*task_ids)
-        workspace, ws_at, ws_bytes = _linear_workspace(x, cols, x_dtype, n, True)
+        workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, True)
         _call(lib().randes_packed_linear_tasks(self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride, packed_base.address,
                                                packed_m, y.data_ptr(), y_dtype, y_stride, ws_at, ws_bytes, _stream_of(x)))
         return y

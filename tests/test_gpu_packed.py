@@ -251,6 +251,22 @@ def test_linear_on_gaussian_inputs(rows, cols, group, x_dtype):
         assert torch.equal(randes.packed_linear(on_gpu(x, x_dtype), p), y)      # the same bits every time
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_few_tokens_on_a_large_matrix(group):
+    """Sizes on either side of where fp32 activations change over to the other form; a superposition counts as well."""
+    rng = np.random.default_rng(12)
+    for rows, cols in ((8192, 4096), (8191, 4096), (4100, 8193)):
+        p = randes.pack(on_gpu(weight(rng, rows, cols, wl.F32), wl.F32), group=group)
+        w = p.unpack().double()
+        for n in (1, 3, 8):
+            x = rng.standard_normal((n, cols)).astype(np.float32)
+            for dtype in (wl.F32, wl.BF16):
+                xt = on_gpu(x, dtype)
+                y = randes.packed_linear(xt, p)
+                want, y_abs = xt.double() @ w.T, xt.double().abs() @ w.abs().T
+                assert ((y.double() - want).abs() <= np.sqrt(2.0 * cols + 2.0) * 2.0 ** -24 * y_abs).all(), (rows, cols, n, dtype)
+
+
 def test_linear_with_extreme_activations():
     rng = np.random.default_rng(8)
     rows, cols = 32, 128

@@ -85,8 +85,8 @@ def test_the_command_runs():
 def test_products_of_many_tokens_need_their_workspace():
     p = randes.pack(torch.randn(64, 256, device="cuda"))
     x, y = torch.randn(20, 256, device="cuda"), torch.empty(20, 64, device="cuda")
-    need = randes.randes_packed_linear_workspace(256, randes.F32, 20, False)
-    assert need > 0 and randes.randes_packed_linear_workspace(256, randes.F32, 8, True) == 0
+    need = randes.randes_packed_linear_workspace(64, 256, randes.F32, 20, False)
+    assert need > 0 and randes.randes_packed_linear_workspace(64, 256, randes.F32, 8, True) == 0
     ws = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
     s = torch.cuda.current_stream().cuda_stream
     call = lambda at, n: randes.randes_packed_linear(p.address, 64, 256, 64, x, 0, 256, 20, y, 0, 64, s, at, n)

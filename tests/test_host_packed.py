@@ -35,11 +35,15 @@ def test_packed_sizes():
 
 def test_workspace_sizes():
     f = randes.randes_packed_linear_workspace
-    assert f(4096, randes.F32, 0, True) == f(4096, randes.F32, 8, True) == f(4096, randes.BF16, 16, True) == 0
-    assert f(4096, randes.BF16, 17, False) == 24 * 4096 * 2                 # whole groups of eight rows
-    assert f(4100, randes.F32, 64, False) == 64 * 4160 * 2 * 3              # whole tiles of columns, three terms
-    assert f(4096, randes.BF16, 1000, False) == f(4096, randes.BF16, 64, False)
-    assert f(4096, randes.BF16, 64, True) > f(4096, randes.BF16, 64, False)
+    assert f(512, 4096, randes.F32, 0, True) == f(512, 4096, randes.F32, 8, True) == f(1 << 16, 1 << 15, randes.BF16, 8, True) == 0
+    assert f(512, 4096, randes.BF16, 17, False) == 24 * 4096 * 2            # whole groups of eight rows
+    assert f(512, 4100, randes.F32, 64, False) == 64 * 4160 * 2 * 3         # whole tiles of columns, three terms
+    assert f(512, 4096, randes.BF16, 1000, False) == f(512, 4096, randes.BF16, 64, False)
+    assert f(512, 4096, randes.BF16, 64, True) > f(512, 4096, randes.BF16, 64, False)
+    # few fp32 tokens need one where the matrix (with a superposition: both matrices) is large
+    assert f(1 << 13, 1 << 12, randes.F32, 1, False) == 8 * 4096 * 2 * 3
+    assert f(1 << 13, (1 << 12) - 1, randes.F32, 1, False) == 0 < f(1 << 13, (1 << 12) - 1, randes.F32, 1, True)
+    assert f(50257, 768, randes.F32, 1, False) == f(50257, 767, randes.F32, 1, True) == 0
 
 
 def test_pack_arguments():
