@@ -505,7 +505,7 @@ class PackedMatrix:
 
         rows, cols = self.rows, self.cols
         if out is None:
-            out = torch.empty((rows, cols), dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=self.data.device)
+            out = torch.empty(rows, cols, dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=self.data.device)
             stride = cols
         else:
             out_dtype, r, c, stride = _rows_of(out, "out")
@@ -549,7 +549,7 @@ def _linear_tensors(x, rows: int, cols: int, y, y_dtype: int):
     if c != cols:
         _refuse("x has %d columns, the weight %d" % (c, cols))
     if y is None:
-        return n, x_dtype, x_stride, torch.empty((n, rows), dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=x.device), y_dtype, rows
+        return n, x_dtype, x_stride, torch.empty(n, rows, dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=x.device), y_dtype, rows
     y_dtype, yn, yr, y_stride = _rows_of(y, "y")
     if (yn, yr) != (n, rows) or y.device != x.device:
         _refuse("y is [%d, %d] on %s, [%d, %d] on %s is wanted" % (yn, yr, y.device, n, rows, x.device))
@@ -612,15 +612,15 @@ def token_scores(logits, targets=None, top_k: int = 0, scale: float = 1.0) -> To
     target = _target_address(targets, n, device)
     if not 0 <= top_k <= 64:
         _refuse("top_k = %d is not in 0 .. 64" % top_k)
-    stats = torch.empty((4, n), dtype=torch.float32, device=device)
+    stats = torch.empty(4, n, dtype=torch.float32, device=device)
     at = stats.data_ptr()
     ids = tops = None
     if top_k:
-        ids = torch.empty((n, top_k), dtype=torch.int64, device=device)
-        tops = torch.empty((n, top_k), dtype=torch.float32, device=device)
+        ids = torch.empty(n, top_k, dtype=torch.int64, device=device)
+        tops = torch.empty(n, top_k, dtype=torch.float32, device=device)
     _call(lib().randes_token_scores(logits.data_ptr(), dtype, n, vocab, stride, target, scale, top_k, at if target is not None else None, at + 4 * n,
                                     at + 8 * n, ids.data_ptr() if top_k else None, tops.data_ptr() if top_k else None, _stream_of(logits)))
-    return TokenScores(stats.select(0, 0) if targets is not None else None, stats.select(0, 1), stats, ids, tops)
+    return TokenScores(stats[0] if targets is not None else None, stats[1], stats, ids, tops)
 
 
 def _row_gradient(g, what: str, n: int, device):
@@ -644,7 +644,7 @@ def token_scores_backward(logits, targets, scores: TokenScores, g_logprob=None, 
     if stats.dtype is not torch.float32 or stats.shape != (4, n) or not stats.is_contiguous() or stats.device != device:
         _refuse("the scores are not those of %d rows on %s" % (n, device))
     if out is None:
-        out, out_stride = torch.empty((n, vocab), dtype=logits.dtype, device=device), vocab
+        out, out_stride = torch.empty(n, vocab, dtype=logits.dtype, device=device), vocab
     else:
         out_dtype, on, ov, out_stride = _rows_of(out, "out")
         if (out_dtype, on, ov) != (dtype, n, vocab) or out.device != device:
