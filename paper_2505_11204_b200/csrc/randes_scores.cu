@@ -68,19 +68,22 @@ __device__ __forceinline__ void rebase(Sums& v, float m, float c)
     v.s = f == 0.f ? 0.f : v.s * f;
     v.m = m;
 }
-__device__ __forceinline__ Sums join(Sums a, Sums b, float c)
+// order of (logit, index): larger logit first, then lower index; -0 counts as +0
+__device__ __forceinline__ uint32_t order_of(float z)
 {
-    const float m = max_nan(a.m, b.m);
-    rebase(a, m, c);
-    rebase(b, m, c);
-    return Sums{m, a.s + b.s, a.t + b.t};
+    const uint32_t b = __float_as_uint(z + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
+
 // the sums of N lanes (a power of two), in every one of them
 template <int N> __device__ __forceinline__ Sums join_lanes(Sums v, float c)
 {
     float m = v.m;
+    if (N == 32) m = value_of(__reduce_max_sync(~0u, order_of(m)));        // (a NaN out of max_nan has the greatest order)
+    else
 #pragma unroll
-    for (int o = N / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
+        for (int o = N / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
     rebase(v, m, c);
 #pragma unroll
     for (int o = N / 2; o > 0; o >>= 1) {
@@ -90,13 +93,6 @@ template <int N> __device__ __forceinline__ Sums join_lanes(Sums v, float c)
     return v;
 }
 
-// order of (logit, index): larger logit first, then lower index; -0 counts as +0
-__device__ __forceinline__ uint32_t order_of(float z)
-{
-    const uint32_t b = __float_as_uint(z + 0.f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
 __device__ __forceinline__ unsigned long long key_of(float z, uint32_t idx)
 {
     return (static_cast<unsigned long long>(order_of(z)) << 32) | (0xFFFFFFFFu - idx);
@@ -192,18 +188,19 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     __shared__ Sums s_warp[kScoreWarps];
     __shared__ Sums s_cta;
     __shared__ __align__(16) uint32_t s_group[kGroups];
-    __shared__ uint32_t s_batch[kScoreThreads], s_all[kScoreThreads];     // what is read again: batches (8 v + loads), threads
-    __shared__ float s_tau;
-    __shared__ unsigned int s_count, s_n_batch, s_n_all;
+    __shared__ float s_tau, s_log;
+    __shared__ unsigned int s_count;
     __shared__ unsigned long long s_cand[kCandidates];
     __shared__ unsigned long long s_top[kMaxTop];          // this CTA's top list, best first; 0 = no element
     __shared__ unsigned long long s_best[kScoreWarps];
+    // The last warp joins the sums and writes the row, while the others still order the list. The target's logit is wanted
+    // at the very end: its two dependent loads start here.
+    const bool writer = tid == kScoreThreads - 32;
 
     const Share<T> sh(static_cast<const T*>(a.logits) + row * a.stride, a.vocab, rank, ranks);
-    // the target's logit is wanted at the very end: its two dependent loads start here
     long long target = -1;
     float target_logit = 0.f;
-    if (rank == 0 && tid == 0 && a.targets) {
+    if (rank == 0 && writer && a.targets) {
         target = a.targets[row];
         if (target >= 0 && target < static_cast<long long>(a.vocab)) target_logit = Store<T>::load1(sh.row + target);
     }
@@ -282,16 +279,18 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     for (uint32_t u = 0; u < 2; ++u)
         if (left & 2u) two[u] = sh.load(v + ((left & 4u) + u) * kScoreThreads);
     if (left & 1u) one[0] = sh.load(v + (left & 6u) * kScoreThreads);
+    uint32_t idx = 0;
+    float edge = -INFINITY;                  // this thread's single element
+    const bool has_edge = tid < 2 * CPL && sh.single(tid, idx);
+    if (has_edge) edge = Store<T>::load1(sh.row + idx);
     if (left & 4u) take(four, v);
     if (left & 2u) take(two, v + (left & 4u) * kScoreThreads);
     if (left & 1u) take(one, v + (left & 6u) * kScoreThreads);
     const float own_max = m;                 // of the vectors: single elements are offered one by one
-    uint32_t idx;
-    if (tid < 2 * CPL && sh.single(tid, idx)) {
-        const float z = Store<T>::load1(sh.row + idx);
-        if (!(z <= m)) raise(max_nan(m, z));
+    if (has_edge) {
+        if (!(edge <= m)) raise(max_nan(m, edge));
         if (m != -INFINITY)                  // the second of the pair counts 0
-            add(pack2(__float_as_uint(exponent(z)), __float_as_uint(-1e30f)));
+            add(pack2(__float_as_uint(exponent(edge)), __float_as_uint(-1e30f)));
     }
     Sums me;
     {
@@ -306,14 +305,33 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         float gm = max_nan(m, __shfl_xor_sync(~0u, m, 1));
         gm = max_nan(gm, __shfl_xor_sync(~0u, gm, 2));
         if ((tid & 3) == 0) s_group[tid >> 2] = (order_of(gm) & ~(kGroups - 1u)) | (tid >> 2);
-        if (tid == 0) s_count = s_n_batch = s_n_all = 0;
+        if (tid == 0) s_count = 0;
         if (tid < static_cast<int>(kMaxTop)) s_top[tid] = 0ull;
     }
     __syncthreads();
-    if (warp == 0) {
-        me = join_lanes<kScoreWarps>(s_warp[lane % kScoreWarps], c);
-        if (lane == 0) s_cta = me;
-    }
+    auto log_sum = [](const Sums& all) { return all.m == -INFINITY ? -INFINITY : logf(all.s); };
+    auto write_row = [&](const Sums& all, float ln) {        // by the thread that holds the target
+        const bool none = all.m == -INFINITY;
+        a.stats[row] = all.m;
+        a.stats[static_cast<size_t>(a.n_rows) + row] = ln;
+        a.entropy[row] = none ? 0.f : __fmaf_rn(-kLn2, all.t / all.s, ln);
+        if (a.targets) {
+            float lp;
+            if (target < 0) lp = 0.f;
+            else if (target >= static_cast<long long>(a.vocab)) lp = NAN;
+            else if (none) lp = -INFINITY;
+            else lp = __fmaf_rn(a.scale, target_logit - all.m, -ln);
+            a.logprob[row] = lp;
+        }
+    };
+    auto finish_sums = [&] {
+        if (warp != kScoreWarps - 1) return;
+        const Sums all = join_lanes<kScoreWarps>(s_warp[lane % kScoreWarps], c);
+        if (!writer) return;
+        s_cta = all;
+        if (ranks == 1) write_row(all, s_log = log_sum(all));
+    };
+    if (!a.top_k) finish_sums();
     // ---- top list of the CTA
     if (a.top_k) {
         const uint32_t mine = s_group[tid >> 2];
@@ -329,11 +347,6 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         if (before == a.top_k - 1 && (tid & 3) == 0) s_tau = mine < 0x00800000u ? -INFINITY : value_of(mine & ~(kGroups - 1u));
         __syncthreads();
         const float tau = s_tau;
-        if (own_max >= tau && own_max > -INFINITY) {
-            if (second < tau) s_batch[atomicAdd(&s_n_batch, 1u)] = best;
-            else s_all[atomicAdd(&s_n_all, 1u)] = tid;
-        }
-        __syncthreads();
         auto offer = [&](float z, uint32_t i) {
             if (z >= tau && z > -INFINITY) {
                 const unsigned int at = atomicAdd(&s_count, 1u);
@@ -347,24 +360,43 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
             if (!(top >= tau)) return;
             float z[CPL];
             Store<T>::widen(raw[0], z);
+            uint32_t found = 0;
 #pragma unroll
-            for (int e = 0; e < CPL; ++e) offer(z[e], sh.lead + v * CPL + e);
+            for (int e = 0; e < CPL; ++e) found |= (z[e] >= tau ? 1u : 0u) << e;
+            for (; found; found &= found - 1) {
+                const uint32_t i = sh.lead + v * CPL + __ffs(found) - 1;
+                offer(Store<T>::load1(sh.row + i), i);
+            }
         };
-        for (uint32_t i = tid; i < 8 * s_n_batch; i += kScoreThreads) {
-            const uint32_t b = s_batch[i >> 3];
-            if ((i & 7u) < (b & 7u)) look_again((b >> 3) + (i & 7u) * kScoreThreads);
+        // each warp reads again for its own threads: eight lanes for one's batch, or all of them for everything one has read
+        const bool hot = own_max >= tau && own_max > -INFINITY;
+        for (uint32_t some = __ballot_sync(~0u, hot && second < tau); some;) {
+            int src = -1;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (lane >> 3 == q) src = __ffs(some) - 1;
+                some &= some - 1;            // (0 stays 0)
+            }
+            const uint32_t b = __shfl_sync(~0u, best, src < 0 ? 0 : src);
+            if (src >= 0 && (lane & 7u) < (b & 7u)) look_again((b >> 3) + (lane & 7u) * kScoreThreads);
         }
-        for (uint32_t w = warp; w < s_n_all; w += kScoreWarps)
-            for (uint32_t v = sh.v0 + s_all[w] + lane * kScoreThreads; v < sh.v1; v += 32 * kScoreThreads) look_again(v);
-        if (tid < 2 * CPL && sh.single(tid, idx)) offer(Store<T>::load1(sh.row + idx), idx);
+        for (uint32_t some = __ballot_sync(~0u, hot && !(second < tau)); some; some &= some - 1)
+            for (uint32_t v = sh.v0 + warp * 32 + __ffs(some) - 1 + lane * kScoreThreads; v < sh.v1; v += 32 * kScoreThreads) look_again(v);
+        offer(edge, idx);
         __syncthreads();
+        finish_sums();
         const unsigned int n = s_count;
         if (n <= kCandidates) {
-            for (unsigned int i = tid; i < n; i += kScoreThreads) {
-                const unsigned long long key = s_cand[i];
+            for (unsigned int first = 0; first < n; first += kScoreThreads / 8) {        // eight threads rank a candidate
+                const unsigned int i = first + (tid >> 3);
+                const unsigned long long key = i < n ? s_cand[i] : ~0ull;
                 unsigned int ahead = 0;
-                for (unsigned int j = 0; j < n; ++j) ahead += s_cand[j] > key;
-                if (ahead < a.top_k) s_top[ahead] = key;
+#pragma unroll 4
+                for (unsigned int j = tid & 7; j < n; j += 8) ahead += s_cand[j] > key;
+                ahead += __shfl_xor_sync(~0u, ahead, 1);
+                ahead += __shfl_xor_sync(~0u, ahead, 2);
+                ahead += __shfl_xor_sync(~0u, ahead, 4);
+                if (i < n && ahead < a.top_k && (tid & 7) == 0) s_top[ahead] = key;
             }
         } else {
             // more equal (or nearly equal) logits than the list holds: the best below the last, k times over
@@ -381,7 +413,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
 #pragma unroll
                     for (int e = 0; e < CPL; ++e) look(z[e], sh.lead + v * CPL + e);
                 }
-                if (tid < 2 * CPL && sh.single(tid, idx)) look(Store<T>::load1(sh.row + idx), idx);
+                look(edge, idx);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
                     const unsigned long long b = __shfl_xor_sync(~0u, best, o);
@@ -403,23 +435,13 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
     if (ranks > 1) cluster.sync(); else __syncthreads();
     if (rank == 0) {
         Sums all = s_cta;
-        for (uint32_t r = 1; r < ranks; ++r) all = join(all, *cluster.map_shared_rank(&s_cta, r), c);
-        const bool none = all.m == -INFINITY;
-        const float ln = none ? -INFINITY : logf(all.s);
-        const bool bad = !none && !(all.s < INFINITY);       // a NaN or +inf among the logits: NaN sum
-        if (tid == 0) {
-            a.stats[row] = all.m;
-            a.stats[static_cast<size_t>(a.n_rows) + row] = ln;
-            a.entropy[row] = none ? 0.f : __fmaf_rn(-kLn2, all.t / all.s, ln);
-            if (a.targets) {
-                float lp;
-                if (target < 0) lp = 0.f;
-                else if (target >= static_cast<long long>(a.vocab)) lp = NAN;
-                else if (none) lp = -INFINITY;
-                else lp = __fmaf_rn(a.scale, target_logit - all.m, -ln);
-                a.logprob[row] = lp;
-            }
+        if (ranks > 1) {
+            const uint32_t r = lane % kMaxCluster;
+            all = join_lanes<kMaxCluster>(r < ranks ? *cluster.map_shared_rank(&s_cta, r) : Sums{-INFINITY, 0.f, 0.f}, c);
         }
+        const float ln = ranks == 1 ? s_log : log_sum(all);
+        const bool bad = all.m != -INFINITY && !(all.s < INFINITY);       // a NaN or +inf among the logits: NaN sum
+        if (ranks > 1 && writer) write_row(all, ln);
         if (a.top_k) {
             if (ranks > 1) {
                 // the other CTAs' lists join this one's; k * ranks entries, ranked like the candidates
@@ -428,11 +450,18 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
                 __syncthreads();
                 if (tid < static_cast<int>(kMaxTop)) s_top[tid] = 0ull;
                 __syncthreads();
-                for (unsigned int i = tid; i < n; i += kScoreThreads) {
-                    const unsigned long long mine = s_cand[i];
-                    unsigned int before = 0;
-                    for (unsigned int j = 0; j < n; ++j) before += s_cand[j] > mine;
-                    if (mine && before < a.top_k) s_top[before] = mine;
+                // each list is in order: `ranks` lanes (a power of two) look up one entry's place in each of them
+                for (unsigned int first = 0; first < n * ranks; first += kScoreThreads) {
+                    const unsigned int i = (first + tid) / ranks, list = (first + tid) % ranks;
+                    const unsigned long long mine = i < n ? s_cand[i] : 0ull;
+                    unsigned int lo = 0, hi = a.top_k;           // entries before lo are greater, those from hi on are not
+                    while (lo < hi) {
+                        const unsigned int mid = (lo + hi) / 2;
+                        if (s_cand[list * a.top_k + mid] > mine) lo = mid + 1;
+                        else hi = mid;
+                    }
+                    for (uint32_t o = 1; o < ranks; o *= 2) lo += __shfl_xor_sync(~0u, lo, o);
+                    if (mine && lo < a.top_k && list == 0) s_top[lo] = mine;
                 }
                 __syncthreads();
             }
