@@ -16,6 +16,11 @@
 //
 // A row may be shared by a cluster of CTAs (few rows); their sums and top lists meet in the first CTA through distributed
 // shared memory.
+//
+// What bounds it: fp32 logits HBM (512 x 50257: 18 us, 5.7 TB/s); bf16 logits the special-function unit -- one exponential per
+// two bytes, 25 us of it for 2048 x 50257 --, and between the last load of a row and its results some 5000 cycles in which
+// the other rows of the SM go on (4096 x 32128: 52 us, 5.0 TB/s; with 20 alternatives 68 us). Fetching the next rows
+// into L2 meanwhile gains nothing.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cooperative_groups.h>
@@ -480,7 +485,8 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
 constexpr int kGradThreads = 256;
 constexpr int kGradVectors = 4;       // per thread
 
-// p and log p come back from the row's stats; one exponential per element, one read, one write.
+// p and log p come back from the row's stats; one exponential per element, one read, one write. Bound by HBM: 4096 x 32128 bf16
+// 83 us, 6.3 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_constant__ ScoreGradArgs a, uint32_t chunks)
 {
