@@ -50,6 +50,12 @@ __device__ __forceinline__ float quotient(float w, float s, float inv)
     const float q = w * inv;
     return __fmaf_rn(__fmaf_rn(-q, s, w), inv, q);
 }
+__device__ __forceinline__ f32x2 quotient2(f32x2 w, f32x2 neg_s, f32x2 inv)
+{
+    const f32x2 q = mul2(w, inv);
+    return fma2(fma2(q, neg_s, w), inv, q);
+}
+__device__ __forceinline__ f32x2 twice(float x) { return pack2(__float_as_uint(x), __float_as_uint(x)); }
 
 // Eight neighbouring columns of one row as they lie in memory.
 template <typename T> struct Eight { uint4 w[sizeof(T) / 2]; };
@@ -128,14 +134,10 @@ template <typename T> __device__ __forceinline__ Eight<T> from_tile(const unsign
     return v;
 }
 
-__device__ __forceinline__ void to_tile(float* at, const float (&v)[8])
+template <typename T> __device__ __forceinline__ void to_tile(unsigned char* tile, uint32_t row, uint32_t c, const Eight<T>& v)
 {
-    reinterpret_cast<float4*>(at)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(at)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void to_tile(bf16* at, const float (&v)[8])
-{
-    *reinterpret_cast<uint4*>(at) = make_uint4(Out<bf16>::pack(v[0], v[1]), Out<bf16>::pack(v[2], v[3]), Out<bf16>::pack(v[4], v[5]), Out<bf16>::pack(v[6], v[7]));
+#pragma unroll
+    for (int h = 0; h < static_cast<int>(sizeof(T)) / 2; ++h) *reinterpret_cast<uint4*>(tile + row * Tile<T>::kPitch + c * sizeof(T) + h * 16) = v.w[h];
 }
 
 // Which matrix of the launch a CTA works on, and the warp's 16-row x 128-column unit in it.
@@ -182,9 +184,9 @@ __device__ __forceinline__ uint32_t top_of(const uint4& w)        // bf16 pairs
     return top_of_lanes(umax(m << 16, m & 0xFFFF0000u));
 }
 
-// One warp turns 16 rows x 128 columns into two tiles. Bound by HBM as far as the loads keep coming (16384 x 4096 fp32: 41.7 us,
-// the rate of a copy; 50257 x 768 bf16, where there are half the bytes per code: 22.4 us, 4.4 TB/s). RETRIEVE: the weight is fma(lambda, s * M, W_0) with the sign
-// bits of the unit's 128 columns out of one Philox block -- the value retrieve writes in fp32, never stored.
+// One warp turns 16 rows x 128 columns into two tiles. RETRIEVE: the weight is fma(lambda, s * M, W_0) with the sign bits of the
+// unit's 128 columns out of one Philox block -- the value retrieve writes in fp32, never stored. Bound by HBM for fp32 (16384 x
+// 4096: 42 us, the rate of a copy) and by instruction issue for bf16, with half the bytes per code (50257 x 768: 22.1 us, 4.4 TB/s).
 //
 // Warps per SM, measured at 16384 x 4096 fp32 and 50257 x 768 bf16: a plain pack wants 32 of them (64 registers) and to keep its
 // 16-byte loads coming (fp32 41.7 us at 32 warps, 44.1 at 24; bf16 22.4 and 24.3). A retrieve holds two tensors' words: with
@@ -271,7 +273,7 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
         // The four lanes of a row share the divisions: lane t makes the scale of quarter t.
         const uint32_t mine = t == 0 ? top[0] : (t == 1 ? top[1] : (t == 2 ? top[2] : top[3]));
         const bool finite = mine < 0x7F800000u;
-        float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__uint_as_float(mine), 7.f)));
+        float s = __bfloat162float(__float2bfloat16_rn(quotient(__uint_as_float(mine), 7.f, 1.f / 7.f)));       // (of use from 2^-100 on)
         if (!(finite && s >= kMinScale)) s = 0.f;             // too small for a scale (or not a number): code 0
         const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
         scale_bits[h] = finite ? __float_as_uint(s) >> 16 : 0x7FC0u;
@@ -284,10 +286,20 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[p][e] = 0.f;
             }
+            if (sizeof(WT) == 4 && !RETRIEVE) {               // two at a time is no faster where HBM bounds it (42.0 us, 43.1)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int pos = ((e >> 1) & 1) * 2 + h + (e & 1) * 4;      // nibble of (row half, column): see the layout above
-                word[p][e >> 2] += __float_as_uint(quotient(v[p][e], sp, ip) + __uint_as_float(kRound)) * (1u << (4 * pos));
+                for (int e = 0; e < 8; ++e) {
+                    const int pos = ((e >> 1) & 1) * 2 + h + (e & 1) * 4;      // nibble of (row half, column): see the layout above
+                    word[p][e >> 2] += __float_as_uint(quotient(v[p][e], sp, ip) + __uint_as_float(kRound)) * (1u << (4 * pos));
+                }
+                continue;
+            }
+            const f32x2 neg_s = twice(-sp), inv2 = twice(ip), round2 = twice(__uint_as_float(kRound));
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const f32x2 q = add2(quotient2(pack2(__float_as_uint(v[p][e]), __float_as_uint(v[p][e + 1])), neg_s, inv2), round2);
+                const int pos = ((e >> 1) & 1) * 2 + h;      // and the next column's nibble four further
+                word[p][e >> 2] += static_cast<uint32_t>(q) * (1u << (4 * pos)) + static_cast<uint32_t>(q >> 32) * (1u << (4 * pos + 16));
             }
         }
     }
@@ -302,22 +314,51 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
 
 // `vec`: 1 in words of 16 bytes, 2 (fp32) in words of 32 bytes: a lane's eight columns in one store, so
 // that every store fills whole sectors (16384 x 4096: 53 us against 69).
-template <typename OT> __device__ __forceinline__ void store8(OT* row, uint32_t c, uint32_t cols, uint32_t vec, const float (&v)[8])
+template <typename OT> __device__ __forceinline__ void store8(OT* row, uint32_t c, uint32_t cols, uint32_t vec, const Eight<OT>& v)
 {
-    if (sizeof(OT) == 4 && vec == 2 && c + 8 <= cols) {
-        asm volatile("st.global.cs.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                     ::"l"(row + c), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+    constexpr int W = sizeof(OT) / 2;
+    if (W == 2 && vec == 2 && c + 8 <= cols) {
+        asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(row + c), "r"(v.w[0].x), "r"(v.w[0].y), "r"(v.w[0].z), "r"(v.w[0].w), "r"(v.w[W - 1].x), "r"(v.w[W - 1].y), "r"(v.w[W - 1].z), "r"(v.w[W - 1].w) : "memory");
     } else if (c + 8 <= cols) {
-        Out<OT>::template store<8>(row + c, v);
-    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c + e < cols) Out<OT>::store1(row + c + e, v[e]);
+        for (int h = 0; h < W; ++h) __stcs(reinterpret_cast<uint4*>(row + c) + h, v.w[h]);
+    } else {
+        OT e[8];
+        memcpy(e, &v, sizeof e);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (c + k < cols) row[c + k] = e[k];
     }
 }
 
-// The values that the four bits stand for: q * s is exact in fp32 (3 + 8 bits), rounded once for bf16. Bound by its stores
-// (16384 x 4096 fp32: 53 us, 5.7 TB/s).
+// Eight values out of the operand registers (q / 64) of two words, for row half h: see the layout above. Both products by 64 and
+// the fp32 ones by the scale are exact; a bf16 value is rounded once, in the second product.
+template <typename OT> __device__ __forceinline__ Eight<OT> values8(const uint32_t (&q)[2][4], int h, uint32_t scale);      // scale: bf16 bits
+template <> __device__ __forceinline__ Eight<bf16> values8(const uint32_t (&q)[2][4], int h, uint32_t scale)
+{
+    const uint32_t s2 = __byte_perm(scale, scale, 0x1010), unit = __float_as_uint(kCodeUnit) | (__float_as_uint(kCodeUnit) >> 16);
+    uint32_t v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = mul_bf16x2(mul_bf16x2(q[e >> 1][(e & 1) * 2 + h], unit), s2);
+    return Eight<bf16>{{make_uint4(v[0], v[1], v[2], v[3])}};
+}
+template <> __device__ __forceinline__ Eight<float> values8(const uint32_t (&q)[2][4], int h, uint32_t scale)
+{
+    const f32x2 s2 = twice(__uint_as_float(scale << 16)), unit = twice(kCodeUnit);
+    f32x2 v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t pair = q[e >> 1][(e & 1) * 2 + h];
+        v[e] = mul2(mul2(pack2(pair << 16, pair & 0xFFFF0000u), unit), s2);
+    }
+    Eight<float> r;
+    memcpy(&r, v, sizeof r);
+    return r;
+}
+
+// The values that the four bits stand for. Bound by its stores (16384 x 4096 fp32: 53 us, 5.7 TB/s; 50257 x 768 bf16: 16.7 us, 5.8
+// TB/s).
 template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack_kernel(const __grid_constant__ UnpackArgs a)
 {
     uint32_t which, rt, ku;
@@ -345,15 +386,9 @@ template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack
         for (int h = 0; h < 2; ++h) {
             const uint32_t r = rt * 16 + h * 8 + g;
             if (m.vec && r >= m.rows) continue;
-            const float s = __uint_as_float(h ? sb & 0xFFFF0000u : sb << 16);
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t pair = q[e >> 2][((e >> 1) & 1) * 2 + h];
-                v[e] = kCodeUnit * __uint_as_float(e & 1 ? pair & 0xFFFF0000u : pair << 16) * s;
-            }
+            const Eight<OT> v = values8<OT>(q, h, h ? sb >> 16 : sb & 0xFFFFu);
             if (m.vec) store8<OT>(static_cast<OT*>(m.dst) + r * m.stride, c, cols, m.vec, v);
-            else to_tile(reinterpret_cast<OT*>(tile + (h * 8 + g) * Tile<OT>::kPitch) + 32 * p + 8 * t, v);
+            else to_tile<OT>(tile, h * 8 + g, 32 * p + 8 * t, v);
         }
     }
     if (!m.vec) tile_out<OT>(tile, static_cast<OT*>(m.dst), m.stride, rt, ku, m.rows, cols, lane);

@@ -23,6 +23,12 @@ __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t 
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 __device__ __forceinline__ void decode(uint32_t word, uint32_t (&a)[4])
 {
     constexpr uint32_t k127 = 0x7F007F00u, k123 = 0x7D007D00u, kOff = 0xBE00BE00u;    // 2^127, 2^123, -1/8, twice each
