@@ -215,21 +215,25 @@ int linear_giveups(unsigned int* count);   // CTAs that gave up on a bounded wai
 #define RANDES_BOTH
 #endif
 struct PackedLayout {
-    uint32_t tiles, record, col_blocks, quarters;     // per record: column tiles, bytes; records per row block; 32-column quarters per group
+    uint32_t log_tiles, record, col_blocks, log_quarters;     // per record: column tiles, bytes; records per row block; 32-column quarters per group
     size_t total;
     RANDES_BOTH PackedLayout(uint32_t rows, uint32_t cols, uint32_t group)
     {
-        tiles = group == 128 ? 2 : 1;
-        record = tiles * 2048 + (group == 32 ? 256 : 128);
-        col_blocks = cols / (64 * tiles) + (cols % (64 * tiles) ? 1 : 0);
-        quarters = group / 32;
+        log_tiles = group == 128;
+        record = (2048u << log_tiles) + (group == 32 ? 256 : 128);
+        const uint32_t width = 64u << log_tiles;
+        col_blocks = (cols >> (6 + log_tiles)) + ((cols & (width - 1)) != 0);
+        log_quarters = group >> 6;
         total = (static_cast<size_t>(rows) + 63) / 64 * col_blocks * record;
     }
     // byte offsets of row tile rt (16 rows): codes of column tile kt (64 columns), scales of the group that holds 32-column quarter q
-    RANDES_BOTH size_t at(uint32_t rt, uint32_t kt) const { return (static_cast<size_t>(rt / 4) * col_blocks + kt / tiles) * record; }
-    RANDES_BOTH size_t codes(uint32_t rt, uint32_t kt) const { return at(rt, kt) + (kt % tiles * 4 + rt % 4) * 512; }
-    RANDES_BOTH size_t scales(uint32_t rt, uint32_t q) const { return at(rt, q / 2) + tiles * 2048 + ((q % (2 * tiles)) / quarters * 4 + rt % 4) * 32; }
-    RANDES_BOTH bool has_tile(uint32_t kt) const { return kt < col_blocks * tiles; }
+    RANDES_BOTH size_t at(uint32_t rt, uint32_t kt) const { return (static_cast<size_t>(rt / 4) * col_blocks + (kt >> log_tiles)) * record; }
+    RANDES_BOTH size_t codes(uint32_t rt, uint32_t kt) const { return at(rt, kt) + ((kt & log_tiles) * 4 + rt % 4) * 512; }
+    RANDES_BOTH size_t scales(uint32_t rt, uint32_t q) const
+    {
+        return at(rt, q / 2) + (2048u << log_tiles) + (((q & ((2u << log_tiles) - 1)) >> log_quarters) * 4 + rt % 4) * 32;
+    }
+    RANDES_BOTH bool has_tile(uint32_t kt) const { return kt < col_blocks << log_tiles; }
 };
 constexpr uint32_t kPackBatch = 32;       // matrices per launch of pack and unpack
 struct PackMatrix {

@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
     *reinterpret_cast<uint4*>(dst + lay.codes(rt, 2 * ku) + lane * 16) = make_uint4(word[0][0], word[0][1], word[1][0], word[1][1]);
     if (lay.has_tile(2 * ku + 1))
         *reinterpret_cast<uint4*>(dst + lay.codes(rt, 2 * ku + 1) + lane * 16) = make_uint4(word[2][0], word[2][1], word[3][0], word[3][1]);
-    if (t % per == 0 && lay.has_tile(2 * ku + t / 2))
+    if ((t & (per - 1)) == 0 && lay.has_tile(2 * ku + t / 2))
         *reinterpret_cast<uint32_t*>(dst + lay.scales(rt, 4 * ku + t) + g * 4) = scale_bits[0] | (scale_bits[1] << 16);
 }
 
@@ -646,7 +646,7 @@ template <typename XT, int GROUP> cudaError_t launch_mul(PackedLinearArgs<kNarro
     const uint32_t blocks_cta = kMulWarps >> a.log_split, ranks = 1u << a.log_ranks;
     const uint32_t n_pos = a.seg[a.n_seg - 1].first + a.seg[a.n_seg - 1].count;
     a.ring_at = (kMulWarps * n_pos + (ranks > 1 ? blocks_cta * a.n_tokens : 0)) * kRows * static_cast<uint32_t>(sizeof(float));
-    const size_t smem = a.ring_at + static_cast<size_t>(kMulWarps) * kDepth * (kTiles / lay.tiles * lay.record + 8);
+    const size_t smem = a.ring_at + static_cast<size_t>(kMulWarps) * kDepth * ((kTiles >> lay.log_tiles) * lay.record + 8);
     static std::atomic<size_t> granted[kDevices];      // a kernel has to opt in beyond 48 KiB, per device
     if (smem > 48 * 1024 && (device >= kDevices || smem > granted[device].load(std::memory_order_relaxed))) {
         const cudaError_t e = cudaFuncSetAttribute(packed_linear_kernel<XT, GROUP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
