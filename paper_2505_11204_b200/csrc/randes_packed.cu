@@ -186,7 +186,8 @@ __device__ __forceinline__ uint32_t top_of(const uint4& w)        // bf16 pairs
 
 // One warp turns 16 rows x 128 columns into two tiles. RETRIEVE: the weight is fma(lambda, s * M, W_0) with the sign bits of the
 // unit's 128 columns out of one Philox block -- the value retrieve writes in fp32, never stored. Bound by HBM for fp32 (16384 x
-// 4096: 42 us, the rate of a copy) and by instruction issue for bf16, with half the bytes per code (50257 x 768: 22.1 us, 4.4 TB/s).
+// 4096: 42 us, the rate of a copy) and by instruction issue for bf16, with half the bytes per code (50257 x 768: 21.1 us, 4.6
+// TB/s; both rows' loads at once change nothing).
 //
 // Warps per SM, measured at 16384 x 4096 fp32 and 50257 x 768 bf16: a plain pack wants 32 of them (64 registers) and to keep its
 // 16-byte loads coming (fp32 41.7 us at 32 warps, 44.1 at 24; bf16 22.4 and 24.3). A retrieve holds two tensors' words: with
@@ -357,7 +358,7 @@ template <> __device__ __forceinline__ Eight<float> values8(const uint32_t (&q)[
     return r;
 }
 
-// The values that the four bits stand for. Bound by its stores (16384 x 4096 fp32: 53 us, 5.7 TB/s; 50257 x 768 bf16: 16.7 us, 5.8
+// The values that the four bits stand for. Bound by its stores (16384 x 4096 fp32: 53 us, 5.7 TB/s; 50257 x 768 bf16: 15.9 us, 6.1
 // TB/s).
 template <typename OT> __global__ void __launch_bounds__(kPackWarps * 32) unpack_kernel(const __grid_constant__ UnpackArgs a)
 {
