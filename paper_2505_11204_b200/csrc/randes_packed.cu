@@ -88,7 +88,7 @@ template <typename T> __device__ __forceinline__ void widen8(const Eight<T>& r, 
 
 // Rows that do not start on 16-byte boundaries go through shared memory, element by element but neighbours together: a warp's
 // 16 x 128 tile, rows a little apart so that the lanes' 16-byte accesses fall into different banks. (Each lane touching its
-// own eight columns in memory took 71 us instead of 12 to unpack 4001 x 4001 bf16, retrieve-and-pack 43 instead of 27.)
+// own eight columns in memory took 71 us instead of 12 to unpack 4001 x 4001 bf16, retrieve-and-pack 43 instead of 25.)
 template <typename T> struct Tile {
     static constexpr uint32_t kPitch = 128 * sizeof(T) + 16;
     static constexpr uint32_t kBytes = 16 * kPitch;
@@ -191,7 +191,8 @@ __device__ __forceinline__ uint32_t top_of(const uint4& w)        // bf16 pairs
 //
 // Warps per SM, measured at 16384 x 4096 fp32 and 50257 x 768 bf16: a plain pack wants 32 of them (64 registers) and to keep its
 // 16-byte loads coming (fp32 41.7 us at 32 warps, 44.1 at 24; bf16 22.4 and 24.3). A retrieve holds two tensors' words: with
-// fp32 on either side 16 warps and no spills (80 us; 24 warps 98, 32 warps 118), with bf16 on both 24 (36.2 us; 38.8 at 32).
+// fp32 on either side 16 warps and no spills (80 us; 24 warps 98, 32 warps 118), with bf16 on both 24 (36.2 us, 38.8 at 32; 33.1 since two
+// elements share their instructions).
 template <typename WT, typename MT, bool RETRIEVE>
 __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) + sizeof(MT) == 4 ? 6 : 4)) pack_kernel(const __grid_constant__ PackArgs a)
 {
@@ -257,11 +258,25 @@ __global__ void __launch_bounds__(kPackWarps * 32, !RETRIEVE ? 8 : (sizeof(WT) +
             } else {
                 widen8<WT>(raw[p], v[p]);
                 if (RETRIEVE) {
+                    // this lane's eight signs; in a pair of bf16 bit 2 e goes to bit 15, bit 2 e + 1 to bit 31 (the two copies of the
+                    // byte do not overlap)
+                    const uint32_t byte = ((p == 0 ? blk.x : (p == 1 ? blk.y : (p == 2 ? blk.z : blk.w))) >> (8 * t)) & 0xFFu;
+                    auto pair = [&](int e) { return (byte * ((1u << (15 - 2 * e)) + (1u << (30 - 2 * e)))) & 0x80008000u; };
+                    if (sizeof(MT) == 2) {
+                        uint4& x = add[p].w[0];
+                        x = make_uint4(x.x ^ pair(0), x.y ^ pair(1), x.z ^ pair(2), x.w ^ pair(3));
+                    }
                     float d[8];
                     widen8<MT>(add[p], d);
-                    const uint32_t bits = p == 0 ? blk.x : (p == 1 ? blk.y : (p == 2 ? blk.z : blk.w));
+                    const f32x2 lambda2 = twice(a.lambda);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[p][e] = __fmaf_rn(a.lambda, flip(d[e], (bits >> (8 * t + e)) << 31), v[p][e]);
+                    for (int e = 0; e < 8; e += 2) {
+                        if (sizeof(MT) == 4) {
+                            d[e] = flip(d[e], (byte << (31 - e)) & 0x80000000u);
+                            d[e + 1] = flip(d[e + 1], (byte << (30 - e)) & 0x80000000u);
+                        }
+                        unpack2(fma2(lambda2, pack2(__float_as_uint(d[e]), __float_as_uint(d[e + 1])), pack2(__float_as_uint(v[p][e]), __float_as_uint(v[p][e + 1]))), v[p][e], v[p][e + 1]);
+                    }
                 }
                 top[p] = top_of(v[p]);
             }
