@@ -503,16 +503,25 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
     if (m == -INFINITY) m = ln = gl = gh = 0.f;           // nothing left in the row: the gradient is 0
     const uint32_t target = tk >= 0 && tk < static_cast<long long>(a.vocab) ? static_cast<uint32_t>(tk) : ~0u;
     const float h = a.entropy[row], a_p = -a.scale * __fmaf_rn(gh, h, gl), a_pl = -a.scale * gh, c = a.scale * kLog2e, at_target = a.scale * gl;
-    // dz = p (a_p + a_pl log p) [+ scale g_lp at the target], two at a time
+    // dz = p (a_p + a_pl log p) [+ scale g_lp at the target], two at a time. A p of 0 has to give 0, so the bracket has to be a
+    // number there: scale d stops at -1000, where p is 0 for certain (ln S >= 0), also for masked logits; and where the given
+    // gradients alone may overflow the bracket, p is asked.
+    const float least = -1000.f / a.scale;
+    const bool overflows = fabsf(a_p) + 1100.f * fabsf(a_pl) == INFINITY;          // log p >= -1000 - ln S, ln S <= ln 2^31
     auto both = [](float x) { return pack2(__float_as_uint(x), __float_as_uint(x)); };
     const f32x2 neg_m = both(-m), scale2 = both(a.scale), neg_ln = both(-ln), c2 = both(c), ln2 = both(-ln * kLog2e), a_p2 = both(a_p), a_pl2 = both(a_pl);
     auto grad2 = [&](f32x2 x) {
         float d0, d1, e0, e1;
         unpack2(add2(x, neg_m), d0, d1);
-        const f32x2 d = pack2(__float_as_uint(max_nan(d0, -1e30f)), __float_as_uint(max_nan(d1, -1e30f)));
+        const f32x2 d = pack2(__float_as_uint(max_nan(d0, least)), __float_as_uint(max_nan(d1, least)));
         const f32x2 lp = fma2(scale2, d, neg_ln);
         unpack2(fma2(d, c2, ln2), e0, e1);
-        return mul2(pack2(__float_as_uint(ex2(e0)), __float_as_uint(ex2(e1))), fma2(a_pl2, lp, a_p2));
+        const float p0 = ex2(e0), p1 = ex2(e1);
+        const f32x2 bracket = fma2(a_pl2, lp, a_p2), y = mul2(pack2(__float_as_uint(p0), __float_as_uint(p1)), bracket);
+        if (!overflows) return y;
+        float y0, y1;
+        unpack2(y, y0, y1);
+        return pack2(__float_as_uint(p0 == 0.f ? 0.f : y0), __float_as_uint(p1 == 0.f ? 0.f : y1));
     };
     auto grad = [&](float x) {
         float y, other;

@@ -290,3 +290,47 @@ def test_refusals():
     big = torch.randn(5, 100, device="cuda")
     refused(inv, lambda: randes.randes_token_scores_backward(big, 0, 4, 100, 100, t, 1.0, st, g, g, None, big.data_ptr() + 400, 100, s))
     assert randes.randes_launch_count() == before
+
+
+def range_tolerance(z, t, scale, g_lp, g_h, dtype):
+    """grad_tolerance where u spans more than fp32's exponentials: a p below 2^-126 may come out as 0, and what multiplies it
+    is the bracket of the formula."""
+    u, lp, p, h, m, ln = definition(z, t, scale)
+    a = np.abs(np.where(p > 0, lp, 0))
+    flushed = float(np.float32(scale)) * 2.0 ** -126 * (np.abs(g_lp)[:, None] + np.abs(g_h)[:, None] * (a + h[:, None]))
+    return grad_tolerance(z, t, scale, g_lp, g_h, dtype) + flushed
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1e-6, 1.0, 2e4, 1e6])
+@pytest.mark.parametrize("mask", ["-inf", "lowest"])
+def test_gradient_at_masked_logits_for_every_scale(mask, scale, dtype):
+    rng = np.random.default_rng(7)
+    n, vocab = 5, 3001
+    z, _, t, td = make(rng, n, vocab, dtype)
+    value = -np.inf if mask == "-inf" else float(torch.finfo(TYPES[dtype]).min)
+    masked = rng.random((n, vocab)) < 0.3
+    masked[np.arange(n), t] = False
+    masked[4] = True                                       # one token left
+    masked[4, t[4]] = False
+    z[masked] = value
+    zd = torch.from_numpy(z).to(TYPES[dtype]).cuda()
+    z = zd.float().cpu().numpy()
+    r = randes.token_scores(zd, td, scale=scale)
+    zero = torch.from_numpy(masked).cuda()
+    with np.errstate(invalid="ignore"):
+        for loss_scale in (1.0, 65536.0):
+            g_lp, g_h = (loss_scale * rng.standard_normal(n).astype(np.float32) for _ in range(2))
+            got = randes.token_scores_backward(zd, td, r, torch.from_numpy(g_lp).cuda(), torch.from_numpy(g_h).cuda(), scale=scale).float()
+            assert torch.isfinite(got).all(), "%d of %d elements are no numbers" % (int((~torch.isfinite(got)).sum()), got.numel())
+            a, b = g_lp.astype(np.float64), g_h.astype(np.float64)
+            err, tol = np.abs(got.cpu().numpy() - grad_definition(z, t, scale, a, b)), range_tolerance(z, t, scale, a, b, dtype)
+            assert (err <= tol).all(), "worst %.3g x tolerance" % float((err / tol).max())
+            if mask == "-inf" or scale * -value > 1e9:     # (lowest value times 1e-6 is masked as well)
+                assert (got[zero] == 0).all()
+    # whatever the gradients: nothing comes back through a token of probability 0
+    for big in (3e38, -3e38):
+        g = torch.full((n,), big, device="cuda")
+        for pair in ((g, g), (g, None), (None, g)):
+            got = randes.token_scores_backward(zd, td, r, *pair, scale=scale)
+            assert (got[zero] == 0).all(), "%d of %d masked elements are not 0" % (int((got[zero] != 0).sum()), int(zero.sum()))
