@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kScoreThreads, 5) score_kernel(const __grid_co
         }
         if (m == -INFINITY) return;
         const f32x2 neg = pack2(__float_as_uint(-m), __float_as_uint(-m));
-        if (low > -1e30f) {                  // (times c, at most 1.5e6, that is a finite number)
+        if ((low - m) * c > -1e30f) {        // no exponent of the batch leaves fp32's range, at either end of the logits
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 f32x2 z[CPL / 2];

@@ -334,3 +334,34 @@ def test_gradient_at_masked_logits_for_every_scale(mask, scale, dtype):
         for pair in ((g, g), (g, None), (None, g)):
             got = randes.token_scores_backward(zd, td, r, *pair, scale=scale)
             assert (got[zero] == 0).all(), "%d of %d masked elements are not 0" % (int((got[zero] != 0).sum()), int(zero.sum()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1e-6, 0.5, 1.0, 3.0, 1e6])
+@pytest.mark.parametrize("vocab", [37, 5000, 40001])
+def test_one_logit_near_the_greatest_number(vocab, scale, dtype):
+    rng = np.random.default_rng(8)
+    n = 6
+    z, _, t, _ = make(rng, n, vocab, dtype, sharp=False)
+    top = rng.integers(0, vocab, size=n)
+    z[np.arange(n), top] = [3e38, 2.5e38, float(torch.finfo(TYPES[dtype]).max), 1e38, 1e33, 2e30]      # (a token that is forced)
+    t[::2] = top[::2]
+    zd, td = torch.from_numpy(z).to(TYPES[dtype]).cuda(), torch.from_numpy(t).cuda()
+    z = zd.float().cpu().numpy()
+    r = randes.token_scores(zd, td, top_k=3, scale=scale)
+    u, lp, p, h, m, ln = definition(z, t, scale)
+    assert (p[np.arange(n), top] == 1).all()
+    assert (r.entropy == 0).all(), r.entropy
+    want = lp[np.arange(n), t]
+    with np.errstate(over="ignore"):
+        want32 = want.astype(np.float32)                   # -inf where fp32 has no such number
+    got, tol = r.logprob.cpu().numpy(), 2.0 ** -21 * (np.abs(want) + 1)
+    assert ((np.abs(got - want) <= tol) | (np.isinf(want32) & (got == want32))).all(), (got, want)
+    assert np.array_equal(r.top_ids.cpu().numpy(), np.argsort(-z, axis=1, kind="stable")[:, :3]) and (r.top_logprobs[:, 0] == 0).all()
+    g_lp, g_h = (rng.standard_normal(n).astype(np.float32) for _ in range(2))
+    gl, gh = torch.from_numpy(g_lp).cuda(), torch.from_numpy(g_h).cuda()
+    for a, b in ((gl, gh), (gl, None), (None, gh)):
+        x, y = (np.zeros(n) if g is None else g.double().cpu().numpy() for g in (a, b))
+        grad = randes.token_scores_backward(zd, td, r, a, b, scale=scale).float().cpu().numpy()
+        err, tol = np.abs(grad - grad_definition(z, t, scale, x, y)), range_tolerance(z, t, scale, x, y, dtype)
+        assert (err <= tol).all(), "worst %.3g x tolerance" % float(np.nanmax(err / tol))
