@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
     float gh = a.g_entropy ? a.g_entropy[row] : 0.f;
     if (m == -INFINITY) m = ln = gl = gh = 0.f;           // nothing left in the row: the gradient is 0
     const uint32_t target = tk >= 0 && tk < static_cast<long long>(a.vocab) ? static_cast<uint32_t>(tk) : ~0u;
-    const float h = a.entropy[row], a_p = -a.scale * __fmaf_rn(gh, h, gl), a_pl = -a.scale * gh, c = a.scale * kLog2e, at_target = a.scale * gl;
+    const float h = a.g_entropy ? a.entropy[row] : 0.f, a_p = -a.scale * __fmaf_rn(gh, h, gl), a_pl = -a.scale * gh, c = a.scale * kLog2e, at_target = a.scale * gl;
     // dz = p (a_p + a_pl log p) [+ scale g_lp at the target], two at a time. A p of 0 has to give 0, so the bracket has to be a
     // number there: scale d stops at -1000, where p is 0 for certain (ln S >= 0), also for masked logits; and where the given
     // gradients alone may overflow the bracket, p is asked.

@@ -365,3 +365,15 @@ def test_one_logit_near_the_greatest_number(vocab, scale, dtype):
         grad = randes.token_scores_backward(zd, td, r, a, b, scale=scale).float().cpu().numpy()
         err, tol = np.abs(grad - grad_definition(z, t, scale, x, y)), range_tolerance(z, t, scale, x, y, dtype)
         assert (err <= tol).all(), "worst %.3g x tolerance" % float(np.nanmax(err / tol))
+
+
+def test_the_entropy_is_not_read_without_its_gradient():
+    rng = np.random.default_rng(9)
+    z, zd, t, td = make(rng, 4, 300, "f32")
+    r = randes.token_scores(zd, td)
+    g = torch.ones(4, device="cuda")
+    want = randes.token_scores_backward(zd, td, r, g, None)
+    stats = r.stats.clone()
+    stats[1] = float("nan")
+    spoilt = randes.TokenScores(stats[0], stats[1], stats, None, None)
+    assert torch.equal(randes.token_scores_backward(zd, td, spoilt, g, None), want) and torch.isfinite(want).all()
