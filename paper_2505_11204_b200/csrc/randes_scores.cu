@@ -495,6 +495,17 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
     const uint32_t row = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
     T* dz = static_cast<T*>(a.grad) + row * a.grad_stride;
+    const uint32_t per = kGradThreads * kGradVectors * CPL;
+    const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T);
+    const uint32_t lead = min(off ? CPL - off : 0u, a.vocab);
+    // Rows of the two tensors that sit alike in their 16-byte words go word by word, others element by element. The words are
+    // asked for first, then what the row's factors are made of.
+    const bool alike = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z) & 15);
+    const uint32_t n = alike ? (a.vocab - lead) / CPL : 0u, v0 = chunk * (kGradThreads * kGradVectors) + threadIdx.x;
+    uint4 raw[kGradVectors];
+#pragma unroll
+    for (int u = 0; u < kGradVectors; ++u)
+        if (v0 + u * kGradThreads < n) raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + lead) + v0 + u * kGradThreads);
     float m = a.stats[row], ln = a.stats[static_cast<size_t>(a.n_rows) + row];
     const long long tk = a.targets && a.g_logprob ? a.targets[row] : -1;
     float gl = tk >= 0 ? a.g_logprob[row] : 0.f;
@@ -502,43 +513,31 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
     float gh = a.g_entropy ? a.g_entropy[row] : 0.f;
     if (m == -INFINITY) m = ln = gl = gh = 0.f;           // nothing left in the row: the gradient is 0
     const uint32_t target = tk >= 0 && tk < static_cast<long long>(a.vocab) ? static_cast<uint32_t>(tk) : ~0u;
-    const float h = a.g_entropy ? a.entropy[row] : 0.f, a_p = -a.scale * __fmaf_rn(gh, h, gl), a_pl = -a.scale * gh, c = a.scale * kLog2e, at_target = a.scale * gl;
     // dz = p (a_p + a_pl log p) [+ scale g_lp at the target], two at a time. A p of 0 has to give 0, so the bracket has to be a
-    // number there: scale d stops at -1000, where p is 0 for certain (ln S >= 0), also for masked logits; and where the given
-    // gradients alone may overflow the bracket, p is asked.
-    const float least = -1000.f / a.scale;
-    const bool overflows = fabsf(a_p) + 1100.f * fabsf(a_pl) == INFINITY;          // log p >= -1000 - ln S, ln S <= ln 2^31
+    // number there. For masked logits scale d stops at -1000 (a.least), where p is 0 for certain (ln S >= 0); and gradients that
+    // may overflow the bracket are taken in parts of 2^64, for which p counts 2^64 (2^-64 is exact, and log p >= -1000 - ln 2^31).
+    const float h = a.g_entropy ? a.entropy[row] : 0.f, at_target = a.scale * gl, c = a.scale * kLog2e;
+    const bool parts = a.scale * (fabsf(gl) + fabsf(gh) * (h + 1100.f)) == INFINITY;
+    const float part = parts ? 0x1p-64f : 1.f;
+    gl *= part;
+    gh *= part;
+    const float a_p = -a.scale * __fmaf_rn(gh, h, gl), a_pl = -a.scale * gh;
     auto both = [](float x) { return pack2(__float_as_uint(x), __float_as_uint(x)); };
-    const f32x2 neg_m = both(-m), scale2 = both(a.scale), neg_ln = both(-ln), c2 = both(c), ln2 = both(-ln * kLog2e), a_p2 = both(a_p), a_pl2 = both(a_pl);
+    const f32x2 neg_m = both(-m), scale2 = both(a.scale), neg_ln = both(-ln), c2 = both(c), ln2 = both(-ln * kLog2e + (parts ? 64.f : 0.f)), a_p2 = both(a_p), a_pl2 = both(a_pl);
     auto grad2 = [&](f32x2 x) {
         float d0, d1, e0, e1;
         unpack2(add2(x, neg_m), d0, d1);
-        const f32x2 d = pack2(__float_as_uint(max_nan(d0, least)), __float_as_uint(max_nan(d1, least)));
+        const f32x2 d = pack2(__float_as_uint(max_nan(d0, a.least)), __float_as_uint(max_nan(d1, a.least)));
         const f32x2 lp = fma2(scale2, d, neg_ln);
         unpack2(fma2(d, c2, ln2), e0, e1);
-        const float p0 = ex2(e0), p1 = ex2(e1);
-        const f32x2 bracket = fma2(a_pl2, lp, a_p2), y = mul2(pack2(__float_as_uint(p0), __float_as_uint(p1)), bracket);
-        if (!overflows) return y;
-        float y0, y1;
-        unpack2(y, y0, y1);
-        return pack2(__float_as_uint(p0 == 0.f ? 0.f : y0), __float_as_uint(p1 == 0.f ? 0.f : y1));
+        return mul2(pack2(__float_as_uint(ex2(e0)), __float_as_uint(ex2(e1))), fma2(a_pl2, lp, a_p2));
     };
     auto grad = [&](float x) {
         float y, other;
         unpack2(grad2(both(x)), y, other);
         return y;
     };
-    const uint32_t per = kGradThreads * kGradVectors * CPL;
-    const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T);
-    const uint32_t lead = min(off ? CPL - off : 0u, a.vocab);
-    // rows of the two tensors that sit alike in their 16-byte words go word by word, others element by element
-    if ((reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z) & 15)) {
-        const uint32_t n = (a.vocab - lead) / CPL;
-        uint4 raw[kGradVectors];
-        const uint32_t v0 = chunk * (kGradThreads * kGradVectors) + threadIdx.x;
-#pragma unroll
-        for (int u = 0; u < kGradVectors; ++u)
-            if (v0 + u * kGradThreads < n) raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + lead) + v0 + u * kGradThreads);
+    if (alike) {
 #pragma unroll
         for (int u = 0; u < kGradVectors; ++u) {
             const uint32_t v = v0 + u * kGradThreads;
