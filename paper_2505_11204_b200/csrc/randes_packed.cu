@@ -663,11 +663,17 @@ template <typename XT, int GROUP> cudaError_t launch_mul(PackedLinearArgs<kNarro
     const uint32_t n_pos = a.seg[a.n_seg - 1].first + a.seg[a.n_seg - 1].count;
     a.ring_at = (kMulWarps * n_pos + (ranks > 1 ? blocks_cta * a.n_tokens : 0)) * kRows * static_cast<uint32_t>(sizeof(float));
     const size_t smem = a.ring_at + static_cast<size_t>(kMulWarps) * kDepth * ((kTiles >> lay.log_tiles) * lay.record + 8);
-    static std::atomic<size_t> granted[kDevices];      // a kernel has to opt in beyond 48 KiB, per device
-    if (smem > 48 * 1024 && (device >= kDevices || smem > granted[device].load(std::memory_order_relaxed))) {
-        const cudaError_t e = cudaFuncSetAttribute(packed_linear_kernel<XT, GROUP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    // A kernel has to opt in beyond 48 KiB, per device: once, to the most that any call can want (every token a slot of its own, a
+    // cluster; a limit of each call's own size could be lowered again by another thread before the launch).
+    constexpr uint32_t kRecords = GROUP == 128 ? kTiles / 2 : kTiles, kRecord = GROUP == 128 ? 4224 : (GROUP == 32 ? 2304 : 2176);
+    constexpr size_t kMost = (kMulWarps * 2 * kNarrowTokens + kNarrowTokens) * kRows * sizeof(float) + kMulWarps * kDepth * (kRecords * kRecord + 8);
+    static_assert(kMost <= 113 * 1024, "two CTAs per SM");
+    if (smem > kMost) return cudaErrorInvalidValue;
+    static std::atomic<bool> granted[kDevices];
+    if (device >= kDevices || !granted[device].load(std::memory_order_relaxed)) {
+        const cudaError_t e = cudaFuncSetAttribute(packed_linear_kernel<XT, GROUP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMost));
         if (e != cudaSuccess) return e;
-        if (device < kDevices) granted[device].store(smem, std::memory_order_relaxed);
+        if (device < kDevices) granted[device].store(true, std::memory_order_relaxed);
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>((blocks + blocks_cta - 1) / blocks_cta * ranks));

@@ -10,6 +10,9 @@ products of a few tokens with packed matrices, against plain numpy implementatio
   random-walk form sqrt(2 n + 2) * 2^-24 * y_abs, n the number of products of one output and y_abs the sum of their
   magnitudes: n roundings of 2^-24 of partial sums that stay near y_abs / sqrt(n)."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -21,6 +24,7 @@ from oracle import randes_oracle as ro                              # noqa: E402
 from paper_2505_11204_b200 import build, randes, workloads as wl    # noqa: E402
 from gpu_util import model_to_dev, to_dev                           # noqa: E402
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 S, F = wl.SHUFFLE, wl.FLIP
 TYPES = {wl.F32: torch.float32, wl.BF16: torch.bfloat16}
 
@@ -488,3 +492,52 @@ def test_side_stream_and_graph_replay():
         graph.replay()
         torch.cuda.synchronize()
         same_values(y.cpu().numpy(), new.astype(np.float64) @ w.astype(np.float64).T)
+
+
+_TWO_THREADS = """
+import sys, threading
+sys.path.insert(0, {root!r})
+import torch
+from paper_2505_11204_b200 import randes
+torch.cuda.init()
+torch.manual_seed({seed})
+failed = []
+for dtype in (torch.float32, torch.bfloat16):
+    for group in (32, 64, 128):
+        # more rows, fewer CTAs to a row block: every size wants another amount of shared memory
+        packed = [randes.pack(torch.randn(rows, 1024, device="cuda"), group=group) for rows in (64, 2048, 16384, 40000)]
+        xs = [torch.randn(n, 1024, device="cuda").to(dtype) for n in range(1, 9)]
+        torch.cuda.synchronize()
+        for p in packed:
+            start = threading.Barrier(len(xs))
+
+            def work(x):
+                try:
+                    torch.cuda.current_stream()
+                    start.wait()
+                    for _ in range(3):
+                        randes.packed_linear(x, p)
+                except Exception as e:
+                    failed.append((str(dtype), group, p.rows, x.shape[0], str(e)))
+
+            threads = [threading.Thread(target=work, args=(x,)) for x in xs]
+            for t in threads: t.start()
+            for t in threads: t.join()
+            for x in xs[::-1]:
+                try:
+                    y = randes.packed_linear(x, p)
+                    assert torch.equal(y, randes.packed_linear(x, p))
+                except Exception as e:
+                    failed.append(("after", str(dtype), group, p.rows, x.shape[0], str(e)))
+torch.cuda.synchronize()
+print(len(failed), failed[:3])
+sys.exit(1 if failed else 0)
+"""
+
+
+def test_first_calls_from_several_threads_at_once():
+    """Threads whose calls want different amounts of shared memory, each kernel's first calls among them (so in processes of
+    their own)."""
+    for seed in range(4):
+        r = subprocess.run([sys.executable, "-c", _TWO_THREADS.format(root=ROOT, seed=seed)], cwd=ROOT, capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, (seed, r.stdout[-2000:], r.stderr[-2000:])
