@@ -397,6 +397,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
+        __syncwarp();   // the products were one lane's; what follows is the whole warp's
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Geo::kTmemCols) : "memory");
     }

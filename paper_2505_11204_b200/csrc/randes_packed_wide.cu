@@ -441,6 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_wide_kernel(const __grid_c
     tc_before();
     __syncthreads();
     if (warp == kCopyWarp) {
+        __syncwarp();            // the copies were one lane's; what follows is the whole warp's
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(W::kTmem) : "memory");
     }
