@@ -468,7 +468,16 @@ def _stream_of(t) -> int:
     return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
-def _call(rc: int) -> None:
+def _call(device, function, *args) -> None:
+    """function(*args) with the tensors' device current (as torch's own operators run: the library launches on the current one);
+    raises what it reports."""
+    import torch
+
+    if device.index == torch._C._cuda_getDevice():
+        rc = function(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = function(*args)
     if rc:
         raise RandesError(rc, randes_last_error())
 
@@ -511,8 +520,8 @@ class PackedMatrix:
             out_dtype, r, c, stride = _rows_of(out, "out")
             if (r, c) != (rows, cols):
                 _refuse("out is [%d, %d], the matrix [%d, %d]" % (r, c, rows, cols))
-        _call(lib().randes_unpack(_PtrOne(self.address), 1, self.group, _MatrixOne((out.data_ptr(), rows, cols, stride)), out_dtype,
-                                  _stream_of(out)))
+        _call(out.device, lib().randes_unpack, _PtrOne(self.address), 1, self.group, _MatrixOne((out.data_ptr(), rows, cols, stride)), out_dtype,
+              _stream_of(out))
         return out
 
 
@@ -527,7 +536,8 @@ def pack(weights, group: int = 64):
     if not isinstance(weights, (list, tuple)):
         dtype, rows, cols, stride = _rows_of(weights, "the weight")
         p = _new_packed(rows, cols, group, weights.device)
-        _call(lib().randes_pack(_MatrixOne((weights.data_ptr(), rows, cols, stride)), 1, dtype, group, _PtrOne(p.address), _stream_of(weights)))
+        _call(weights.device, lib().randes_pack, _MatrixOne((weights.data_ptr(), rows, cols, stride)), 1, dtype, group, _PtrOne(p.address),
+              _stream_of(weights))
         return p
     if not weights:
         return []
@@ -537,7 +547,7 @@ def pack(weights, group: int = 64):
         _refuse("the weights of one call have one type and one device")
     made = [_new_packed(r, c, group, device) for _, r, c, _ in shapes]
     mats = (Matrix * n)(*[(w.data_ptr(), r, c, s) for w, (_, r, c, s) in zip(weights, shapes)])
-    randes_pack(mats, n, shapes[0][0], group, (ctypes.c_void_p * n)(*[p.address for p in made]), _stream_of(weights[0]))
+    _call(device, lib().randes_pack, mats, n, shapes[0][0], group, (ctypes.c_void_p * n)(*[p.address for p in made]), _stream_of(weights[0]))
     return made
 
 
@@ -575,8 +585,8 @@ def packed_linear(x, w: PackedMatrix, y=None, y_dtype: int = F32):
     rows, cols = w.rows, w.cols
     n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, rows, cols, y, y_dtype)
     workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, False)
-    _call(lib().randes_packed_linear(w.address, rows, cols, w.group, x.data_ptr(), x_dtype, x_stride, n, y.data_ptr(), y_dtype, y_stride,
-                                     ws_at, ws_bytes, _stream_of(x)))
+    _call(x.device, lib().randes_packed_linear, w.address, rows, cols, w.group, x.data_ptr(), x_dtype, x_stride, n, y.data_ptr(), y_dtype,
+          y_stride, ws_at, ws_bytes, _stream_of(x))
     return y
 
 
@@ -618,8 +628,8 @@ def token_scores(logits, targets=None, top_k: int = 0, scale: float = 1.0) -> To
     if top_k:
         ids = torch.empty(n, top_k, dtype=torch.int64, device=device)
         tops = torch.empty(n, top_k, dtype=torch.float32, device=device)
-    _call(lib().randes_token_scores(logits.data_ptr(), dtype, n, vocab, stride, target, scale, top_k, at if target is not None else None, at + 4 * n,
-                                    at + 8 * n, ids.data_ptr() if top_k else None, tops.data_ptr() if top_k else None, _stream_of(logits)))
+    _call(device, lib().randes_token_scores, logits.data_ptr(), dtype, n, vocab, stride, target, scale, top_k, at if target is not None else None,
+          at + 4 * n, at + 8 * n, ids.data_ptr() if top_k else None, tops.data_ptr() if top_k else None, _stream_of(logits))
     return TokenScores(stats[0] if targets is not None else None, stats[1], stats, ids, tops)
 
 
@@ -650,8 +660,8 @@ def token_scores_backward(logits, targets, scores: TokenScores, g_logprob=None, 
         if (out_dtype, on, ov) != (dtype, n, vocab) or out.device != device:
             _refuse("out must have the logits' shape, type and device")
     at = stats.data_ptr()
-    _call(lib().randes_token_scores_backward(logits.data_ptr(), dtype, n, vocab, stride, target, scale, at + 8 * n, at + 4 * n, g_lp, g_h,
-                                             out.data_ptr(), out_stride, _stream_of(logits)))
+    _call(device, lib().randes_token_scores_backward, logits.data_ptr(), dtype, n, vocab, stride, target, scale, at + 8 * n, at + 4 * n, g_lp,
+          g_h, out.data_ptr(), out_stride, _stream_of(logits))
     return out
 
 
@@ -842,8 +852,8 @@ class Plan:
         layers = list(range(self.n_layers)) if layers is None else [self._layer(l) for l in layers]
         n = len(layers)
         made = [_new_packed(self.rows[l], self.cols[l], group, M.device) for l in layers]
-        randes_retrieve_packed(self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, _as_ptrs(base), M, group,
-                               (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]), _stream_of(M))
+        _call(M.device, lib().randes_retrieve_packed, self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, _as_ptrs(base),
+              M.data_ptr(), group, (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]), _stream_of(M))
         return made
 
     def packed_linear(self, task_ids, lam: float, layer: int, x, packed_base: PackedMatrix, packed_m, y=None, y_dtype: int = F32):
@@ -872,6 +882,6 @@ class Plan:
         if not isinstance(task_ids, ctypes.Array):
             task_ids = (ctypes.c_uint32 * max(n, 1))(*task_ids)
         workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, True)
-        _call(lib().randes_packed_linear_tasks(self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride, packed_base.address,
-                                               packed_m, y.data_ptr(), y_dtype, y_stride, ws_at, ws_bytes, _stream_of(x)))
+        _call(x.device, lib().randes_packed_linear_tasks, self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride,
+              packed_base.address, packed_m, y.data_ptr(), y_dtype, y_stride, ws_at, ws_bytes, _stream_of(x))
         return y

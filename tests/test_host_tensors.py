@@ -1,0 +1,120 @@
+"""The calls on torch tensors, without a GPU: tensors that only say where they are, and a library that only notes which device
+is current when it is called."""
+import contextlib
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2505_11204_b200 import build, randes    # noqa: E402
+
+
+class Fake:
+    """What the binding asks of a CUDA tensor."""
+
+    def __init__(self, shape, dtype=torch.float32, device=0, stride=None, address=0x10000000):
+        self.shape, self.dtype, self.device, self.is_cuda, self.address = tuple(shape), dtype, torch.device("cuda", device), True, address
+        self._stride = stride or tuple(int(torch.tensor(self.shape[i + 1:]).prod()) for i in range(len(self.shape)))
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        return self._stride
+
+    def data_ptr(self):
+        return self.address
+
+    def numel(self):
+        return int(torch.tensor(self.shape).prod())
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return self._stride == Fake(self.shape)._stride
+
+    def __getitem__(self, row):      # a row of the statistics
+        return Fake(self.shape[1:], self.dtype, self.device.index)
+
+
+class Library:
+    """The real library for what runs on the host alone; the rest notes the current device."""
+
+    LAUNCHING = ("randes_pack", "randes_unpack", "randes_retrieve_packed", "randes_packed_linear", "randes_packed_linear_tasks",
+                 "randes_token_scores", "randes_token_scores_backward")
+
+    def __init__(self, real, current):
+        self.real, self.current, self.calls = real, current, []
+
+    def __getattr__(self, name):
+        if name not in self.LAUNCHING:
+            return getattr(self.real, name)
+
+        def noted(*args):
+            self.calls.append((name, self.current[0], args))
+            return 0
+        return noted
+
+
+@pytest.fixture
+def fake(monkeypatch):
+    build.build_library()
+    current = [0]
+
+    @contextlib.contextmanager
+    def device(d):
+        before, current[0] = current[0], d if isinstance(d, int) else d.index
+        yield
+        current[0] = before
+
+    library = Library(randes.lib(), current)
+    monkeypatch.setattr(randes, "lib", lambda: library)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0])
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 1000 + index)
+    monkeypatch.setattr(torch, "empty", lambda *shape, dtype=torch.float32, device=None: Fake(shape, dtype, torch.device(device).index))
+    return library
+
+
+def _plan(**kw):
+    return randes.Plan([64, 64], [128, 128], [0, 0], [randes.SHUFFLE | randes.FLIP], task_ids=[5], seeds=[1], host_only=True, **kw)
+
+
+def _refused(code, fn):
+    with pytest.raises(randes.RandesError) as e:
+        fn()
+    assert e.value.code == code, (e.value.code, str(e.value))
+
+
+@pytest.mark.parametrize("where", [0, 1, 3])
+def test_the_library_runs_with_the_tensors_device_current(fake, where):
+    w, x = Fake((64, 128), device=where), Fake((3, 128), torch.bfloat16, where)
+    p = randes.pack(w)
+    packed = randes.pack([w, w])
+    p.unpack()
+    randes.packed_linear(x, p)
+    randes.packed_linear(Fake((12, 128), device=where), p)      # with a workspace
+    plan = _plan()
+    M = Fake((plan.m_bytes // 4,), device=where)
+    plan.retrieve_packed(5, 1.0, [w, w], M)
+    plan.packed_linear([5, 5, 5], 1.0, 0, x, p, packed)
+    z, t, g = Fake((3, 100), device=where), Fake((3,), torch.int64, where), Fake((3,), device=where)
+    r = randes.token_scores(z, t, top_k=4)
+    randes.token_scores_backward(z, t, r, g, g)
+    assert [c[0] for c in fake.calls] == ["randes_pack", "randes_pack", "randes_unpack", "randes_packed_linear", "randes_packed_linear",
+                                          "randes_retrieve_packed", "randes_packed_linear_tasks", "randes_token_scores",
+                                          "randes_token_scores_backward"]
+    for name, current, args in fake.calls:
+        assert current == where, name
+        assert args[-1] == 1000 + where, "%s: stream" % name
+    assert fake.current[0] == 0                                 # as the caller left it
+    plan.close()
+
+
+def test_the_callers_device_comes_back_after_an_error(fake):
+    failing = lambda *a: 7
+    with pytest.raises(randes.RandesError):
+        randes._call(torch.device("cuda", 2), failing)
+    assert fake.current[0] == 0
