@@ -518,8 +518,8 @@ class PackedMatrix:
             stride = cols
         else:
             out_dtype, r, c, stride = _rows_of(out, "out")
-            if (r, c) != (rows, cols):
-                _refuse("out is [%d, %d], the matrix [%d, %d]" % (r, c, rows, cols))
+            if (r, c) != (rows, cols) or out.device != self.data.device:
+                _refuse("out is [%d, %d] on %s, the matrix [%d, %d] on %s" % (r, c, out.device, rows, cols, self.data.device))
         _call(out.device, lib().randes_unpack, _PtrOne(self.address), 1, self.group, _MatrixOne((out.data_ptr(), rows, cols, stride)), out_dtype,
               _stream_of(out))
         return out
@@ -551,13 +551,16 @@ def pack(weights, group: int = 64):
     return made
 
 
-def _linear_tensors(x, rows: int, cols: int, y, y_dtype: int):
+def _linear_tensors(x, w: PackedMatrix, y, y_dtype: int):
     """(n_tokens, x's type and row stride, y, y's type and row stride) of a product of x [n_tokens, cols] with a [rows, cols] weight."""
     import torch
 
+    rows, cols = w.rows, w.cols
     x_dtype, n, c, x_stride = _rows_of(x, "x")
     if c != cols:
         _refuse("x has %d columns, the weight %d" % (c, cols))
+    if x.device != w.data.device:
+        _refuse("x is on %s, the weight on %s" % (x.device, w.data.device))
     if y is None:
         return n, x_dtype, x_stride, torch.empty(n, rows, dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=x.device), y_dtype, rows
     y_dtype, yn, yr, y_stride = _rows_of(y, "y")
@@ -583,7 +586,7 @@ def _linear_workspace(x, rows: int, cols: int, x_dtype: int, n: int, with_tasks:
 def packed_linear(x, w: PackedMatrix, y=None, y_dtype: int = F32):
     """x: [n_tokens, cols] fp32 or bf16 CUDA tensor (rows may be strided); returns y = x W^T [n_tokens, rows]."""
     rows, cols = w.rows, w.cols
-    n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, rows, cols, y, y_dtype)
+    n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, w, y, y_dtype)
     workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, False)
     _call(x.device, lib().randes_packed_linear, w.address, rows, cols, w.group, x.data_ptr(), x_dtype, x_stride, n, y.data_ptr(), y_dtype,
           y_stride, ws_at, ws_bytes, _stream_of(x))
@@ -872,11 +875,11 @@ class Plan:
             for l, p in enumerate(packed_m):
                 if p is None or (p.rows, p.cols) != (rows, cols):
                     continue      # not a slot this layer can lie in
-                if p.group != group:
-                    _refuse("slot %d has groups of %d columns, the base of %d" % (l, p.group, group))
+                if p.group != group or p.data.device != packed_base.data.device:
+                    _refuse("slot %d has groups of %d columns on %s, the base of %d on %s" % (l, p.group, p.data.device, group, packed_base.data.device))
                 slots[l] = p.address
             packed_m = slots
-        n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, rows, cols, y, y_dtype)
+        n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, packed_base, y, y_dtype)
         if len(task_ids) != n:
             _refuse("%d task ids for %d tokens" % (len(task_ids), n))
         if not isinstance(task_ids, ctypes.Array):

@@ -118,3 +118,29 @@ def test_the_callers_device_comes_back_after_an_error(fake):
     with pytest.raises(randes.RandesError):
         randes._call(torch.device("cuda", 2), failing)
     assert fake.current[0] == 0
+
+
+def test_tensors_of_two_devices_are_refused(fake):
+    inv = randes.INVALID_ARGUMENT
+    w, other = Fake((64, 128)), Fake((64, 128), device=1)
+    p, q = randes.pack(w), randes.pack(other)
+    x, y = Fake((3, 128)), Fake((3, 64))
+    plan = _plan()
+    del fake.calls[:]
+    _refused(inv, lambda: randes.pack([w, other]))
+    _refused(inv, lambda: p.unpack(out=other))
+    _refused(inv, lambda: randes.packed_linear(x, q))
+    _refused(inv, lambda: randes.packed_linear(x, p, y=Fake((3, 64), device=1)))
+    _refused(inv, lambda: plan.packed_linear([5] * 3, 1.0, 0, x, q, [p, p]))
+    _refused(inv, lambda: plan.packed_linear([5] * 3, 1.0, 0, x, p, [p, q]))
+    _refused(inv, lambda: plan.packed_linear([5] * 3, 1.0, 0, x, p, [p, p], y=Fake((3, 64), device=1)))
+    z, t, g = Fake((3, 100)), Fake((3,), torch.int64), Fake((3,))
+    _refused(inv, lambda: randes.token_scores(z, Fake((3,), torch.int64, 1)))
+    r = randes.token_scores(z, t)
+    _refused(inv, lambda: randes.token_scores_backward(Fake((3, 100), device=1), Fake((3,), torch.int64, 1), r, None))
+    _refused(inv, lambda: randes.token_scores_backward(z, t, r, Fake((3,), device=1)))
+    _refused(inv, lambda: randes.token_scores_backward(z, t, r, g, out=Fake((3, 100), device=1)))
+    assert [c[0] for c in fake.calls] == ["randes_token_scores"]
+    randes.packed_linear(x, p, y=y)
+    plan.packed_linear([5] * 3, 1.0, 0, x, p, [p, None])
+    plan.close()
