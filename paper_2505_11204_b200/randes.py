@@ -498,11 +498,11 @@ _MatrixOne, _PtrOne = Matrix * 1, ctypes.c_void_p * 1
 class PackedMatrix:
     """A [rows, cols] weight in four bits with a scale per group of columns (see include/randes.h): one device buffer."""
 
-    __slots__ = ("rows", "cols", "group", "data", "address")
+    __slots__ = ("rows", "cols", "group", "data", "address", "device")
 
     def __init__(self, rows: int, cols: int, group: int, data):
         self.rows, self.cols, self.group, self.data = rows, cols, group, data
-        self.address = data.data_ptr()
+        self.address, self.device = data.data_ptr(), data.device
 
     @property
     def nbytes(self) -> int:
@@ -514,12 +514,12 @@ class PackedMatrix:
 
         rows, cols = self.rows, self.cols
         if out is None:
-            out = torch.empty(rows, cols, dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=self.data.device)
+            out = torch.empty(rows, cols, dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=self.device)
             stride = cols
         else:
             out_dtype, r, c, stride = _rows_of(out, "out")
-            if (r, c) != (rows, cols) or out.device != self.data.device:
-                _refuse("out is [%d, %d] on %s, the matrix [%d, %d] on %s" % (r, c, out.device, rows, cols, self.data.device))
+            if (r, c) != (rows, cols) or out.device != self.device:
+                _refuse("out is [%d, %d] on %s, the matrix [%d, %d] on %s" % (r, c, out.device, rows, cols, self.device))
         _call(out.device, lib().randes_unpack, _PtrOne(self.address), 1, self.group, _MatrixOne((out.data_ptr(), rows, cols, stride)), out_dtype,
               _stream_of(out))
         return out
@@ -559,8 +559,8 @@ def _linear_tensors(x, w: PackedMatrix, y, y_dtype: int):
     x_dtype, n, c, x_stride = _rows_of(x, "x")
     if c != cols:
         _refuse("x has %d columns, the weight %d" % (c, cols))
-    if x.device != w.data.device:
-        _refuse("x is on %s, the weight on %s" % (x.device, w.data.device))
+    if x.device != w.device:
+        _refuse("x is on %s, the weight on %s" % (x.device, w.device))
     if y is None:
         return n, x_dtype, x_stride, torch.empty(n, rows, dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=x.device), y_dtype, rows
     y_dtype, yn, yr, y_stride = _rows_of(y, "y")
@@ -865,20 +865,23 @@ class Plan:
         ``packed_base`` is the layer's W_0, ``packed_m`` the slots of M by slot (pack_superposition), all packed with one
         group size; x: [n_tokens, cols] fp32 or bf16; returns y [n_tokens, rows]."""
         layer = self._layer(layer)
-        rows, cols, group = self.rows[layer], self.cols[layer], packed_base.group
+        if not isinstance(packed_base, PackedMatrix):
+            _refuse("packed_base is no PackedMatrix")
+        rows, cols, group, device = self.rows[layer], self.cols[layer], packed_base.group, packed_base.device
         if (packed_base.rows, packed_base.cols) != (rows, cols):
             _refuse("packed_base is [%d, %d], layer %d is [%d, %d]" % (packed_base.rows, packed_base.cols, layer, rows, cols))
-        if not isinstance(packed_m, ctypes.Array):
-            if len(packed_m) != self.n_layers:
-                _refuse("packed_m has %d entries, the plan %d slots" % (len(packed_m), self.n_layers))
-            slots = (ctypes.c_void_p * max(self.n_layers, 1))()
+        if len(packed_m) != self.n_layers:
+            _refuse("packed_m has %d entries, the plan %d slots" % (len(packed_m), self.n_layers))
+        slots = (ctypes.c_void_p * max(self.n_layers, 1))()
+        try:
             for l, p in enumerate(packed_m):
                 if p is None or (p.rows, p.cols) != (rows, cols):
                     continue      # not a slot this layer can lie in
-                if p.group != group or p.data.device != packed_base.data.device:
-                    _refuse("slot %d has groups of %d columns on %s, the base of %d on %s" % (l, p.group, p.data.device, group, packed_base.data.device))
+                if p.group != group or p.device != device:
+                    _refuse("slot %d has groups of %d columns on %s, the base of %d on %s" % (l, p.group, p.device, group, device))
                 slots[l] = p.address
-            packed_m = slots
+        except AttributeError:
+            _refuse("packed_m holds something that is no PackedMatrix")
         n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, packed_base, y, y_dtype)
         if len(task_ids) != n:
             _refuse("%d task ids for %d tokens" % (len(task_ids), n))
@@ -886,5 +889,5 @@ class Plan:
             task_ids = (ctypes.c_uint32 * max(n, 1))(*task_ids)
         workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, True)
         _call(x.device, lib().randes_packed_linear_tasks, self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride,
-              packed_base.address, packed_m, y.data_ptr(), y_dtype, y_stride, ws_at, ws_bytes, _stream_of(x))
+              packed_base.address, slots, y.data_ptr(), y_dtype, y_stride, ws_at, ws_bytes, _stream_of(x))
         return y

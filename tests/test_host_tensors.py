@@ -144,3 +144,14 @@ def test_tensors_of_two_devices_are_refused(fake):
     randes.packed_linear(x, p, y=y)
     plan.packed_linear([5] * 3, 1.0, 0, x, p, [p, None])
     plan.close()
+
+
+def test_slots_are_packed_matrices_not_addresses(fake):
+    """An array of addresses says neither how many slots it names nor what they hold."""
+    p, x, plan = randes.pack(Fake((64, 128))), Fake((2, 128)), _plan()
+    for n in (1, 2, 5):
+        _refused(randes.INVALID_ARGUMENT, lambda: plan.packed_linear([5, 5], 1.0, 0, x, p, (ctypes.c_void_p * n)(*[p.address] * n)))
+    _refused(randes.INVALID_ARGUMENT, lambda: plan.packed_linear([5, 5], 1.0, 0, x, p, [p, p.address]))
+    _refused(randes.INVALID_ARGUMENT, lambda: plan.packed_linear([5, 5], 1.0, 0, x, p.address, [p, p]))
+    plan.packed_linear([5, 5], 1.0, 0, x, p, (p, p))
+    plan.close()
