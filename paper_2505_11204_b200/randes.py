@@ -885,7 +885,7 @@ class Plan:
         n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, packed_base, y, y_dtype)
         if len(task_ids) != n:
             _refuse("%d task ids for %d tokens" % (len(task_ids), n))
-        if not isinstance(task_ids, ctypes.Array):
+        if not (isinstance(task_ids, ctypes.Array) and task_ids._type_ is ctypes.c_uint32):
             task_ids = (ctypes.c_uint32 * max(n, 1))(*task_ids)
         workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, True)
         _call(x.device, lib().randes_packed_linear_tasks, self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride,

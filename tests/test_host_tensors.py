@@ -155,3 +155,13 @@ def test_slots_are_packed_matrices_not_addresses(fake):
     _refused(randes.INVALID_ARGUMENT, lambda: plan.packed_linear([5, 5], 1.0, 0, x, p.address, [p, p]))
     plan.packed_linear([5, 5], 1.0, 0, x, p, (p, p))
     plan.close()
+
+
+def test_task_ids_of_any_integer_array_are_read_as_numbers(fake):
+    p, x, plan = randes.pack(Fake((64, 128))), Fake((3, 128)), _plan()
+    for ids in ([5, 6, 7], (5, 6, 7), (ctypes.c_uint32 * 3)(5, 6, 7), (ctypes.c_uint8 * 3)(5, 6, 7), (ctypes.c_uint64 * 3)(5, 6, 7),
+                torch.tensor([5, 6, 7])):
+        plan.packed_linear(ids, 1.0, 0, x, p, [p, p])
+        passed = fake.calls[-1][2][4]
+        assert passed._type_ is ctypes.c_uint32 and list(passed) == [5, 6, 7], type(ids)
+    plan.close()
