@@ -501,12 +501,22 @@ class PackedMatrix:
     __slots__ = ("rows", "cols", "group", "data", "address", "device")
 
     def __init__(self, rows: int, cols: int, group: int, data):
+        """Around a buffer that holds such a matrix: `data` of a PackedMatrix of the same shape and group, or a copy of it."""
+        need, have = _packed_size(rows, cols, group), data.numel() * data.element_size()
+        if not data.is_cuda or not data.is_contiguous() or have < need:
+            _refuse("a packed [%d, %d] matrix in groups of %d columns is a contiguous CUDA tensor of %d bytes, not one of %d on %s"
+                    % (rows, cols, group, need, have, data.device))
+        if data.data_ptr() % 16:
+            raise RandesError(MISALIGNED, "the buffer of a packed matrix starts on a 16-byte boundary")
+        self._hold(rows, cols, group, data)
+
+    def _hold(self, rows: int, cols: int, group: int, data):
         self.rows, self.cols, self.group, self.data = rows, cols, group, data
         self.address, self.device = data.data_ptr(), data.device
 
     @property
     def nbytes(self) -> int:
-        return self.data.numel()
+        return self.data.numel() * self.data.element_size()
 
     def unpack(self, out_dtype: int = F32, out=None):
         """The [rows, cols] values that the four bits stand for."""
@@ -528,7 +538,9 @@ class PackedMatrix:
 def _new_packed(rows: int, cols: int, group: int, device) -> PackedMatrix:
     import torch
 
-    return PackedMatrix(rows, cols, group, torch.empty(_packed_size(rows, cols, group), dtype=torch.uint8, device=device))
+    p = PackedMatrix.__new__(PackedMatrix)      # (the size is right)
+    p._hold(rows, cols, group, torch.empty(_packed_size(rows, cols, group), dtype=torch.uint8, device=device))
+    return p
 
 
 def pack(weights, group: int = 64):

@@ -165,3 +165,22 @@ def test_task_ids_of_any_integer_array_are_read_as_numbers(fake):
         passed = fake.calls[-1][2][4]
         assert passed._type_ is ctypes.c_uint32 and list(passed) == [5, 6, 7], type(ids)
     plan.close()
+
+
+def test_a_packed_matrix_checks_the_buffer_it_is_made_of(fake):
+    inv = randes.INVALID_ARGUMENT
+    need = randes.randes_packed_bytes(64, 128, 64)
+    buffer = lambda n, **kw: Fake((n,), kw.pop("dtype", torch.uint8), **kw)
+    p = randes.PackedMatrix(64, 128, 64, buffer(need))           # as read back from a file
+    assert p.nbytes == need and randes.pack(Fake((64, 128))).nbytes == need
+    randes.PackedMatrix(64, 128, 64, buffer(need + 16))
+    randes.PackedMatrix(0, 128, 64, buffer(0))
+    randes.PackedMatrix(64, 128, 64, buffer(need // 4, dtype=torch.int32))
+    _refused(inv, lambda: randes.PackedMatrix(64, 128, 64, buffer(need - 1)))
+    _refused(inv, lambda: randes.PackedMatrix(64, 128, 32, buffer(need)))
+    _refused(inv, lambda: randes.PackedMatrix(65, 128, 64, buffer(need)))
+    _refused(inv, lambda: randes.PackedMatrix(64, 128, 48, buffer(need)))
+    _refused(inv, lambda: randes.PackedMatrix(70000, 70000, 64, buffer(need)))
+    _refused(inv, lambda: randes.PackedMatrix(64, 128, 64, buffer(need, stride=(2,))))
+    _refused(inv, lambda: randes.PackedMatrix(64, 128, 64, torch.zeros(need, dtype=torch.uint8)))       # host memory
+    _refused(randes.MISALIGNED, lambda: randes.PackedMatrix(64, 128, 64, buffer(need, address=0x10000008)))
