@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 from typing import Any, List, NamedTuple, Optional, Sequence
 
@@ -851,8 +852,45 @@ class Plan:
             _refuse("layer %d out of range (n_layers = %d)" % (int(layer), self.n_layers))
         return int(layer)
 
+    @staticmethod
+    def _stored(t, what: str, dtype: int, shape, device, at_least: bool = False) -> int:
+        """Address of a tensor that the library reads as so many dense elements of this type; refuses any other."""
+        import torch
+
+        if not hasattr(t, "data_ptr"):
+            _refuse("%s is no tensor" % what)
+        want = torch.bfloat16 if dtype == BF16 else torch.float32
+        if t.dtype is not want:
+            raise RandesError(UNSUPPORTED_DTYPE, "%s is %s: this plan keeps it in %s" % (what, t.dtype, want))
+        n, have = math.prod(shape), t.numel()
+        if (have < n if at_least else have != n) or (t.dim() == 2 and not at_least and tuple(t.shape) != tuple(shape)):
+            _refuse("%s is %s, %s is wanted" % (what, list(t.shape), list(shape)))
+        if not t.is_cuda or not t.is_contiguous() or (device is not None and t.device != device):
+            _refuse("%s must be a contiguous tensor on %s" % (what, "a CUDA device" if device is None else device))
+        return t.data_ptr()
+
+    def _arena(self, M):
+        """M after the checks that a tensor has to pass before the library reads it as this plan's superposition."""
+        self._stored(M, "M", self.m_dtype, (self.m_bytes // (2 if self.m_dtype == BF16 else 4),), None, at_least=True)
+        return M
+
+    def _weights(self, base, layers, device):
+        """Host array of the weights' addresses; the named ones are checked. Addresses (a ctypes array, or numbers in the list)
+        are taken at the caller's word, as the other methods take them."""
+        have, top = len(base), max(layers, default=-1)
+        if have <= top or (isinstance(base, ctypes.Array) and base._type_ is not ctypes.c_void_p):
+            _refuse("base has %d weights, layer %d is named" % (have, top))
+        if isinstance(base, ctypes.Array):
+            return base
+        out = (ctypes.c_void_p * max(self.n_layers, 1))()
+        for l in layers:
+            w = base[l]
+            out[l] = w if isinstance(w, int) else self._stored(w, "base[%d]" % l, self.storage, (self.rows[l], self.cols[l]), device)
+        return out
+
     def pack_superposition(self, M, group: int = 64, slots=None):
         """Four-bit form of the slots of M, a list by slot (None for slots not named)."""
+        self._arena(M)
         slots = list(range(self.n_layers)) if slots is None else [self._layer(l) for l in slots]
         made = pack([self.slot(M, l) for l in slots], group)
         out = [None] * self.n_layers
@@ -863,11 +901,13 @@ class Plan:
     def retrieve_packed(self, task_id: int, lam: float, base, M, group: int = 64, layers=None):
         """Four-bit form of one retrieved model, its own type never stored; a list, one entry per named layer (default: all).
 
-        ``base`` is the list of all layers' weights; only the named ones are read."""
+        ``base`` is the list of all layers' weights, dense and in the plan's type; only the named ones are read."""
+        self._arena(M)
         layers = list(range(self.n_layers)) if layers is None else [self._layer(l) for l in layers]
         n = len(layers)
+        weights = self._weights(base, layers, M.device)
         made = [_new_packed(self.rows[l], self.cols[l], group, M.device) for l in layers]
-        _call(M.device, lib().randes_retrieve_packed, self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, _as_ptrs(base),
+        _call(M.device, lib().randes_retrieve_packed, self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, weights,
               M.data_ptr(), group, (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]), _stream_of(M))
         return made
 

@@ -184,3 +184,41 @@ def test_a_packed_matrix_checks_the_buffer_it_is_made_of(fake):
     _refused(inv, lambda: randes.PackedMatrix(64, 128, 64, buffer(need, stride=(2,))))
     _refused(inv, lambda: randes.PackedMatrix(64, 128, 64, torch.zeros(need, dtype=torch.uint8)))       # host memory
     _refused(randes.MISALIGNED, lambda: randes.PackedMatrix(64, 128, 64, buffer(need, address=0x10000008)))
+
+
+@pytest.mark.parametrize("storage,m_dtype", [(randes.F32, randes.F32), (randes.BF16, randes.F32), (randes.F32, randes.BF16)])
+def test_retrieve_packed_checks_the_weights_and_the_superposition(fake, storage, m_dtype):
+    inv, dt = randes.INVALID_ARGUMENT, randes.UNSUPPORTED_DTYPE
+    types = {randes.F32: torch.float32, randes.BF16: torch.bfloat16}
+    wt, mt, wrong = types[storage], types[m_dtype], {torch.float32: torch.bfloat16, torch.bfloat16: torch.float32}
+    plan = _plan(storage=storage, m_dtype=m_dtype)
+    n = plan.m_bytes // mt.itemsize
+    w, M = Fake((64, 128), wt), Fake((n,), mt)
+    call = lambda base=(w, w), m=M, **kw: plan.retrieve_packed(5, 1.0, base, m, **kw)
+    _refused(dt, lambda: call((w, Fake((64, 128), wrong[wt]))))
+    _refused(dt, lambda: call((Fake((64, 128), torch.float16), w)))
+    _refused(inv, lambda: call((w, Fake((64, 128), wt, stride=(136, 1)))))     # rows apart: the library reads them as dense
+    _refused(inv, lambda: call((w, Fake((128, 64), wt))))
+    _refused(inv, lambda: call((w, Fake((64, 127), wt))))
+    _refused(inv, lambda: call((w, Fake((64, 128), wt, device=1))))
+    _refused(inv, lambda: call((w, torch.zeros(64, 128, dtype=wt))))           # host memory
+    _refused(inv, lambda: call((w, None)))
+    _refused(inv, lambda: call((w,)))
+    _refused(inv, lambda: call((w,), layers=[1]))
+    _refused(inv, lambda: call((ctypes.c_void_p * 1)(0x10000)))
+    _refused(inv, lambda: call((ctypes.c_uint32 * 2)(0x10000, 0x20000)))
+    _refused(dt, lambda: call(m=Fake((2 * n,), wrong[mt])))
+    _refused(inv, lambda: call(m=Fake((n - 1,), mt)))
+    _refused(inv, lambda: call(m=Fake((n,), mt, stride=(2,))))
+    _refused(inv, lambda: call(m=torch.zeros(n, dtype=mt)))
+    _refused(dt, lambda: plan.pack_superposition(Fake((2 * n,), wrong[mt])))
+    _refused(inv, lambda: plan.pack_superposition(Fake((n - 1,), mt)))
+    assert not fake.calls
+    call()
+    call((w,), layers=[0])                                                     # only the named ones are read
+    call((w, None), layers=[0])
+    call((Fake((64 * 128,), wt), Fake((64, 2, 64), wt)))
+    call((ctypes.c_void_p * 2)(0x10000, 0x20000))                              # addresses, as the other methods take them
+    call((), layers=[])
+    assert len(fake.calls) == 6
+    plan.close()
