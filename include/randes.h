@@ -459,7 +459,8 @@ typedef struct {
     uint64_t stride;         /* elements between rows, >= cols */
 } randes_matrix_t;
 
-/* Bytes of a packed [rows, cols] matrix; 0 on invalid arguments or an empty matrix.  Host-only. */
+/* Bytes of a packed [rows, cols] matrix; 0 on invalid arguments, an empty matrix, or one of 2^32 elements or more (rows and
+ * cols: at most 2^32 - 256).  Host-only. */
 size_t randes_packed_bytes(uint32_t rows, uint32_t cols, uint32_t group);
 
 /*

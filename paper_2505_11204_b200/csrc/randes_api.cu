@@ -1506,6 +1506,12 @@ int check_group(uint32_t group)
     return RANDES_OK;
 }
 
+// Sizes that the packed operators count in 32 bits: elements, and rows and columns rounded up to whole records.
+bool packable(uint32_t rows, uint32_t cols)
+{
+    return rows <= 0xFFFFFF00u && cols <= 0xFFFFFF00u && static_cast<uint64_t>(rows) * cols <= 0xFFFFFFFFull;
+}
+
 int check_packed(const void* p, const char* what)
 {
     if (!p) return fail(RANDES_INVALID_ARGUMENT, "%s is NULL", what);
@@ -1572,7 +1578,7 @@ int check_matrix(const randes_matrix_t& m, uint32_t i, size_t elem, uint32_t gro
     snprintf(what, sizeof what, "matrix %u", i);
     if ((rc = check_tensor(m.data, m.rows, m.cols, m.stride, elem, what))) return rc;
     if (m.rows == 0 || m.cols == 0) return RANDES_OK;
-    if (static_cast<uint64_t>(m.rows) * m.cols > 0xFFFFFFFFull) return fail(RANDES_INVALID_ARGUMENT, "matrix %u has 2^32 elements or more", i);
+    if (!packable(m.rows, m.cols)) return fail(RANDES_INVALID_ARGUMENT, "matrix %u: %u x %u is too large to be packed", i, m.rows, m.cols);
     snprintf(what, sizeof what, "packed[%u]", i);
     if ((rc = check_packed(packed, what))) return rc;
     if (overlap(m.data, span_bytes(m.rows, m.cols, m.stride, elem), packed, randes_packed_bytes(m.rows, m.cols, group)))
@@ -1750,8 +1756,8 @@ int randes_packed_linear_impl(const void* packed, uint32_t rows, uint32_t cols, 
 {
     int rc;
     if ((rc = check_dtype(x_dtype, "activation")) || (rc = check_dtype(y_dtype, "output")) || (rc = check_group(group))) return rc;
-    if (static_cast<uint64_t>(rows) * cols > 0xFFFFFFFFull) return fail(RANDES_INVALID_ARGUMENT, "the matrix has 2^32 elements or more");
     if (n_tokens == 0 || rows == 0) return RANDES_OK;
+    if (!packable(rows, cols)) return fail(RANDES_INVALID_ARGUMENT, "a packed matrix of %u x %u is not supported", rows, cols);
     if (cols && (rc = check_packed(packed, "packed"))) return rc;
     if (overlap(packed, randes_packed_bytes(rows, cols, group), y, span_bytes(n_tokens, rows, y_stride, elem_size(y_dtype))))
         return fail(RANDES_INVALID_ARGUMENT, "y overlaps packed");
@@ -1781,6 +1787,7 @@ int randes_packed_linear_tasks_impl(const randes_plan_t* plan, float lambda, uin
         if (task_row[b] < 0) return fail(RANDES_UNKNOWN_TASK, "task id %u is not registered", task_ids[b]);
     }
     if (rows == 0) return RANDES_OK;
+    if (!packable(rows, cols)) return fail(RANDES_INVALID_ARGUMENT, "a packed matrix of %u x %u is not supported", rows, cols);
     const uint64_t y_bytes = span_bytes(n_tokens, rows, y_stride, elem_size(y_dtype)), p_bytes = randes_packed_bytes(rows, cols, group);
     if (cols) {
         if ((rc = check_packed(packed_base, "packed_base"))) return rc;
@@ -1891,7 +1898,7 @@ extern "C" {
 
 size_t randes_packed_bytes(uint32_t rows, uint32_t cols, uint32_t group)
 {
-    if ((group != 32 && group != 64 && group != 128) || rows == 0 || cols == 0 || static_cast<uint64_t>(rows) * cols > 0xFFFFFFFFull) return 0;
+    if ((group != 32 && group != 64 && group != 128) || rows == 0 || cols == 0 || !packable(rows, cols)) return 0;
     return PackedLayout(rows, cols, group).total;
 }
 

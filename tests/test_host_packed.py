@@ -132,3 +132,17 @@ def test_score_arguments():
     _refused(INV, lambda: back(gs=50))
     _refused(INV, lambda: back(st=None))
     _refused(INV, lambda: back(grad=z + 400))                               # the logits one row further
+
+
+def test_sizes_next_to_the_end_of_32_bits_are_refused():
+    """Rows and columns are rounded up to whole records in 32 bits."""
+    arr = lambda *a: (ctypes.c_void_p * len(a))(*a)
+    for rows, cols in ((1, 0xFFFFFFFF), (1, 0xFFFFFF81), (0xFFFFFFFF, 1), (0xFFFFFFC1, 1)):
+        assert randes.randes_packed_bytes(rows, cols, 64) == 0
+        m = (randes.Matrix * 1)((0x10000, rows, cols, cols))
+        for dtype in (randes.F32, randes.BF16):
+            _refused(INV, lambda: randes.randes_pack(m, 1, dtype, 64, arr(0x1000000000000), None))
+            _refused(INV, lambda: randes.randes_unpack(arr(0x1000000000000), 1, 64, m, dtype, None))
+        _refused(INV, lambda: randes.randes_packed_linear(0x1000000000000, rows, cols, 64, 0x10000, 0, cols, 1, 0x2000000000000, 0, rows, None))
+    for rows, cols in ((1, 0xFFFFFF00), (0xFFFFFF00, 1), (65535, 65537)):
+        assert randes.randes_packed_bytes(rows, cols, 128) == -(-rows // 64) * -(-cols // 128) * 4224
