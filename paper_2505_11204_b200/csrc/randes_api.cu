@@ -1885,7 +1885,7 @@ int randes_token_scores_backward_impl(const void* logits, randes_dtype_t dtype, 
     if (!(grad == logits && (grad_stride == stride || n_rows == 1)) && (n_rows == 1 || (stride == vocab && grad_stride == vocab)) &&
         overlap(logits, span_bytes(n_rows, vocab, stride, elem), grad, span_bytes(n_rows, vocab, grad_stride, elem)))
         return fail(RANDES_INVALID_ARGUMENT, "grad overlaps the logits without being the same tensor");
-    const ScoreGradArgs a{logits, grad, targets, stats, entropy, g_logprob, g_entropy, stride, grad_stride, n_rows, vocab, scale, -1000.f / scale};
+    const ScoreGradArgs a{logits, grad, targets, stats, entropy, g_logprob, g_entropy, stride, grad_stride, n_rows, vocab, scale};
     const int e = launch_score_grad(dtype, a, stream);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the token score gradient kernel");
     ++g_launches;

@@ -328,7 +328,6 @@ struct ScoreGradArgs {
     uint64_t stride, grad_stride;
     uint32_t n_rows, vocab;
     float scale;
-    float least;                  // -1000 / scale: a logit that far below the greatest has probability 0
 };
 int launch_scores(int dtype, const ScoreArgs& a, int sm_count, void* stream);
 int launch_score_grad(int dtype, const ScoreGradArgs& a, void* stream);

@@ -486,8 +486,9 @@ constexpr int kGradThreads = 256;
 constexpr int kGradVectors = 4;       // per thread
 
 // p and log p come back from the row's stats; one exponential per element, one read, one write. Bound by HBM, now that two
-// elements share their instructions: 4096 x 32128 bf16 79 us, 6.7 TB/s (one at a time: 83; rows off 16-byte boundaries, 2048 x
-// 50257, 63 against 70; together with the forward pass, on cold logits, 132 against 152).
+// elements share their instructions: 4096 x 32128 bf16 80.6 us, 6.5 TB/s; rows off 16-byte boundaries, 2048 x 50257, 66 us (one
+// element at a time: a twentieth and a ninth slower). It takes 32 registers, eight CTAs per SM: the same work in 34 (six CTAs)
+// 83.5 and 69.7 us.
 template <typename T>
 __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_constant__ ScoreGradArgs a, uint32_t chunks)
 {
@@ -498,14 +499,9 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
     const uint32_t per = kGradThreads * kGradVectors * CPL;
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T);
     const uint32_t lead = min(off ? CPL - off : 0u, a.vocab);
-    // Rows of the two tensors that sit alike in their 16-byte words go word by word, others element by element. The words are
-    // asked for first, then what the row's factors are made of.
+    // rows of the two tensors that sit alike in their 16-byte words go word by word, others element by element
     const bool alike = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z) & 15);
     const uint32_t n = alike ? (a.vocab - lead) / CPL : 0u, v0 = chunk * (kGradThreads * kGradVectors) + threadIdx.x;
-    uint4 raw[kGradVectors];
-#pragma unroll
-    for (int u = 0; u < kGradVectors; ++u)
-        if (v0 + u * kGradThreads < n) raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + lead) + v0 + u * kGradThreads);
     float m = a.stats[row], ln = a.stats[static_cast<size_t>(a.n_rows) + row];
     const long long tk = a.targets && a.g_logprob ? a.targets[row] : -1;
     float gl = tk >= 0 ? a.g_logprob[row] : 0.f;
@@ -514,8 +510,8 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
     if (m == -INFINITY) m = ln = gl = gh = 0.f;           // nothing left in the row: the gradient is 0
     const uint32_t target = tk >= 0 && tk < static_cast<long long>(a.vocab) ? static_cast<uint32_t>(tk) : ~0u;
     // dz = p (a_p + a_pl log p) [+ scale g_lp at the target], two at a time. A p of 0 has to give 0, so the bracket has to be a
-    // number there. For masked logits scale d stops at -1000 (a.least), where p is 0 for certain (ln S >= 0); and gradients that
-    // may overflow the bracket are taken in parts of 2^64, for which p counts 2^64 (2^-64 is exact, and log p >= -1000 - ln 2^31).
+    // number there. For masked logits log p stops at -1000, where p has long been 0; and gradients that may overflow the bracket
+    // are taken in parts of 2^64, for which p counts 2^64 (2^-64 is exact).
     const float h = a.g_entropy ? a.entropy[row] : 0.f, at_target = a.scale * gl, c = a.scale * kLog2e;
     const bool parts = a.scale * (fabsf(gl) + fabsf(gh) * (h + 1100.f)) == INFINITY;
     const float part = parts ? 0x1p-64f : 1.f;
@@ -525,10 +521,10 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
     auto both = [](float x) { return pack2(__float_as_uint(x), __float_as_uint(x)); };
     const f32x2 neg_m = both(-m), scale2 = both(a.scale), neg_ln = both(-ln), c2 = both(c), ln2 = both(-ln * kLog2e + (parts ? 64.f : 0.f)), a_p2 = both(a_p), a_pl2 = both(a_pl);
     auto grad2 = [&](f32x2 x) {
-        float d0, d1, e0, e1;
-        unpack2(add2(x, neg_m), d0, d1);
-        const f32x2 d = pack2(__float_as_uint(max_nan(d0, a.least)), __float_as_uint(max_nan(d1, a.least)));
-        const f32x2 lp = fma2(scale2, d, neg_ln);
+        const f32x2 d = add2(x, neg_m);
+        float l0, l1, e0, e1;
+        unpack2(fma2(scale2, d, neg_ln), l0, l1);
+        const f32x2 lp = pack2(__float_as_uint(max_nan(l0, -1000.f)), __float_as_uint(max_nan(l1, -1000.f)));
         unpack2(fma2(d, c2, ln2), e0, e1);
         return mul2(pack2(__float_as_uint(ex2(e0)), __float_as_uint(ex2(e1))), fma2(a_pl2, lp, a_p2));
     };
@@ -538,6 +534,10 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_c
         return y;
     };
     if (alike) {
+        uint4 raw[kGradVectors];
+#pragma unroll
+        for (int u = 0; u < kGradVectors; ++u)
+            if (v0 + u * kGradThreads < n) raw[u] = __ldcs(reinterpret_cast<const uint4*>(z + lead) + v0 + u * kGradThreads);
 #pragma unroll
         for (int u = 0; u < kGradVectors; ++u) {
             const uint32_t v = v0 + u * kGradThreads;
