@@ -541,3 +541,134 @@ def test_first_calls_from_several_threads_at_once():
     for seed in range(4):
         r = subprocess.run([sys.executable, "-c", _TWO_THREADS.format(root=ROOT, seed=seed)], cwd=ROOT, capture_output=True, text=True, timeout=300)
         assert r.returncode == 0, (seed, r.stdout[-2000:], r.stderr[-2000:])
+
+
+@pytest.mark.parametrize("rows,cols", [(4096, 4096), (4096, 4095), (16384, 1024)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_few_tokens_on_a_large_superposition(rows, cols, group):
+    """Sizes on either side of where fp32 activations change over to the other form, the superposition's columns counted; the
+    workspace is of the size that is asked for and no larger."""
+    plan, spec, ids, seeds = _plan(rows, cols, 5, S | F, wl.BF16, wl.BF16, ids=[3, 0, 8, 77], seeds=[42, 43, 2 ** 35 + 1, 9])
+    rng = np.random.default_rng(21)
+    pb = randes.pack(on_gpu(weight(rng, rows, cols, wl.F32), wl.F32), group=group)
+    pm = randes.pack([torch.randn(rows, cols, device="cuda") * 3e-3 for _ in range(5)], group=group)
+    base, m = pb.unpack().double(), [p.unpack().double() for p in pm]
+    lam = float(np.float32(0.3))
+    for n in (1, 3, 8):
+        tasks = [ids[(3 * b + 1) % 4] for b in range(n)]
+        slots = [int(ro.task_tables(spec, seeds[ids.index(t)], t)[1][2]) for t in tasks]
+        assert n < 3 or len(set(slots)) > 1
+        x = torch.randn(n, cols, device="cuda")
+        need = randes.randes_packed_linear_workspace(rows, cols, wl.F32, n, True)
+        assert (need > 0) == ((rows, cols) != (4096, 4095))
+        ws = torch.full((need + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+        y = torch.full((n, rows), float("nan"), device="cuda")
+        addresses = (ctypes.c_void_p * 5)(*[p.address for p in pm])
+        randes.randes_packed_linear_tasks(plan.handle, 0.3, 2, group, (ctypes.c_uint32 * n)(*tasks), n, x, 0, cols, pb.address, addresses, y, 0, rows,
+                                          torch.cuda.current_stream().cuda_stream, ws, need)
+        assert (ws[need:] == 0xA5).all()
+        assert torch.equal(y, plan.packed_linear(tasks, 0.3, 2, x, pb, pm))
+        for b in range(n):
+            sign = torch.from_numpy(_signs(spec, seeds[ids.index(tasks[b])], tasks[b], slots[b], cols)).cuda()
+            xd = x[b].double()
+            want = base @ xd + lam * (m[slots[b]] @ (xd * sign))
+            y_abs = base.abs() @ xd.abs() + lam * (m[slots[b]].abs() @ xd.abs())
+            assert ((y[b].double() - want).abs() <= np.sqrt(4.0 * cols + 2.0) * 2.0 ** -24 * y_abs).all(), (n, b)
+    plan.close()
+
+
+@pytest.mark.parametrize("x_dtype", [wl.F32, wl.BF16])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_many_tokens_on_a_large_matrix(group, x_dtype):
+    rng = np.random.default_rng(22)
+    rows, cols = 8200, 4100
+    p = randes.pack(on_gpu(weight(rng, rows, cols, wl.F32), wl.F32), group=group)
+    w = p.unpack().double()
+    for n in (33, 64):
+        x = torch.randn(n, cols, device="cuda").to(TYPES[x_dtype])
+        y = randes.packed_linear(x, p)
+        want, y_abs = x.double() @ w.T, x.double().abs() @ w.abs().T
+        assert ((y.double() - want).abs() <= np.sqrt(2.0 * cols + 2.0) * 2.0 ** -24 * y_abs).all(), n
+
+
+@pytest.mark.parametrize("n,rows,cols", [(12, 200, 128), (40, 200, 320), (64, 2100, 192)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_many_tokens_with_extreme_activations(group, n, rows, cols):
+    rng = np.random.default_rng(23)
+    w = dyadic_weight(rng, rows, cols, group)
+    w[w == 0] = np.float32(2.0 ** -7)                      # few zero codes: an infinity times zero is a NaN
+    p = randes.pack(on_gpu(w, wl.F32), group=group)
+    v = p.unpack().cpu().numpy().astype(np.float64)
+    x = rng.standard_normal((n, cols)).astype(np.float32)
+    x[:3] = 0
+    x[0, 5] = 3e38
+    x[1, 9] = 1e-30
+    x[2, 7] = np.float32(1) + np.float32(2.0 ** -23)
+    x[4] = 0
+    x[4, 3] = np.inf
+    x[5, 3] = np.nan
+    x[n - 1] = 0
+    x[n - 1, cols - 1] = -np.inf
+    for dtype in (wl.F32, wl.BF16):
+        xt = on_gpu(x, dtype)
+        xs = xt.double().cpu().numpy()
+        y = randes.packed_linear(xt, p).cpu().numpy()
+        ordinary = [b for b in range(n) if np.isfinite(xs[b]).all()]
+        assert set(ordinary) >= {1, 2, 3, 6}
+        want, y_abs = xs[ordinary] @ v.T, np.abs(xs[ordinary]) @ np.abs(v).T
+        assert (np.abs(y[ordinary] - want) <= np.sqrt(2.0 * cols + 2.0) * 2.0 ** -24 * y_abs).all()
+        for b, c, sign in ((4, 3, 1), (n - 1, cols - 1, -1)):
+            live = v[:, c] != 0
+            assert np.array_equal(y[b][live], sign * np.sign(v[live, c]) * np.inf) and np.isnan(y[b][~live]).all()
+        assert np.isnan(y[5]).all()
+        # tokens do not see one another: zeros in place of the extreme ones leave the others' bits as they are
+        calm = xt.clone()
+        calm[[0, 4, 5, n - 1]] = 0
+        rest = [b for b in range(n) if b not in (0, 4, 5, n - 1)]
+        assert np.array_equal(y[rest], randes.packed_linear(calm, p).cpu().numpy()[rest])
+
+
+@pytest.mark.parametrize("n", [3, 20, 64, 130])
+@pytest.mark.parametrize("x_dtype", [wl.F32, wl.BF16])
+def test_tasks_and_products_on_a_side_stream_and_in_a_graph(x_dtype, n):
+    rows, cols, lam = 600, 512, 0.25
+    plan, spec, ids, seeds = _plan(rows, cols, 5, S | F, wl.BF16, wl.BF16, ids=[3, 0, 8, 77], seeds=[42, 43, 2 ** 35 + 1, 9])
+    rng = np.random.default_rng(24)
+    base, m = dyadic_weight(rng, rows, cols, 64), [dyadic_weight(rng, rows, cols, 64) for _ in range(5)]
+    pb, pm = randes.pack(on_gpu(base, wl.F32)), randes.pack([on_gpu(v, wl.F32) for v in m])
+    tasks = [ids[int(k)] for k in rng.integers(0, 4, size=n)]
+    before = randes.randes_linear_giveups()
+    x = on_gpu(np.zeros((n, cols)), x_dtype)
+    y, plain = torch.full((n, rows), float("nan"), device="cuda"), torch.full((n, rows), float("nan"), device="cuda")
+
+    def both():
+        plan.packed_linear(tasks, lam, 3, x, pb, pm, y=y)
+        randes.packed_linear(x, pb, y=plain)
+
+    def right(acts, what):
+        want, _ = _tasks_reference(spec, ids, seeds, tasks, lam, 3, acts, base.astype(np.float64), [v.astype(np.float64) for v in m])
+        same_values(y.cpu().numpy(), want, what)
+        same_values(plain.cpu().numpy(), acts.astype(np.float64) @ base.astype(np.float64).T, what)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(4):                                 # the activations arrive on the stream, right before the calls
+            acts = dyadic_acts(rng, n, cols)
+            x.copy_(on_gpu(acts, x_dtype))
+            both()
+    side.synchronize()
+    right(acts, "side stream")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(3):
+        acts = dyadic_acts(rng, n, cols)
+        x.copy_(on_gpu(acts, x_dtype))
+        y.fill_(float("nan"))
+        plain.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        right(acts, "graph")
+    assert randes.randes_linear_giveups() == before
+    plan.close()
