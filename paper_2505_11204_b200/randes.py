@@ -437,15 +437,19 @@ def _refuse(message: str):
     raise RandesError(INVALID_ARGUMENT, message)
 
 
+_torch = None      # the module, once a call on tensors has been made: importing this file does not need it
+
+
 def _rows_of(t, what: str):
     """(element type, rows, columns, elements between rows) of a 2-D CUDA tensor whose rows may be strided; refuses anything
     the library would misread."""
-    import torch
-
+    global _torch
+    if _torch is None:
+        import torch as _torch
     dtype = t.dtype
-    if dtype is torch.bfloat16:
+    if dtype is _torch.bfloat16:
         code = BF16
-    elif dtype is torch.float32:
+    elif dtype is _torch.float32:
         code = F32
     else:
         raise RandesError(UNSUPPORTED_DTYPE, "%s is %s: float32 or bfloat16 is wanted" % (what, dtype))
@@ -462,23 +466,19 @@ def _rows_of(t, what: str):
     return code, rows, cols, stride
 
 
-def _stream_of(t) -> int:
-    """The current stream of a CUDA tensor's device."""
-    import torch
-
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
-
-
 def _call(device, function, *args) -> None:
-    """function(*args) with the tensors' device current (as torch's own operators run: the library launches on the current one);
-    raises what it reports."""
-    import torch
-
-    if device.index == torch._C._cuda_getDevice():
-        rc = function(*args)
+    """function(*args, stream) with the tensors' device current (as torch's own operators run: the library launches on the
+    current one) and its current stream; raises what the library reports."""
+    global _torch
+    if _torch is None:
+        import torch as _torch
+    c, index = _torch._C, device.index
+    stream = c._cuda_getCurrentRawStream(index)
+    if index == c._cuda_getDevice():
+        rc = function(*args, stream)
     else:
-        with torch.cuda.device(device):
-            rc = function(*args)
+        with _torch.cuda.device(device):
+            rc = function(*args, stream)
     if rc:
         raise RandesError(rc, randes_last_error())
 
@@ -531,8 +531,7 @@ class PackedMatrix:
             out_dtype, r, c, stride = _rows_of(out, "out")
             if (r, c) != (rows, cols) or out.device != self.device:
                 _refuse("out is [%d, %d] on %s, the matrix [%d, %d] on %s" % (r, c, out.device, rows, cols, self.device))
-        _call(out.device, lib().randes_unpack, _PtrOne(self.address), 1, self.group, _MatrixOne((out.data_ptr(), rows, cols, stride)), out_dtype,
-              _stream_of(out))
+        _call(self.device, lib().randes_unpack, _PtrOne(self.address), 1, self.group, _MatrixOne((out.data_ptr(), rows, cols, stride)), out_dtype)
         return out
 
 
@@ -549,8 +548,7 @@ def pack(weights, group: int = 64):
     if not isinstance(weights, (list, tuple)):
         dtype, rows, cols, stride = _rows_of(weights, "the weight")
         p = _new_packed(rows, cols, group, weights.device)
-        _call(weights.device, lib().randes_pack, _MatrixOne((weights.data_ptr(), rows, cols, stride)), 1, dtype, group, _PtrOne(p.address),
-              _stream_of(weights))
+        _call(p.device, lib().randes_pack, _MatrixOne((weights.data_ptr(), rows, cols, stride)), 1, dtype, group, _PtrOne(p.address))
         return p
     if not weights:
         return []
@@ -560,39 +558,36 @@ def pack(weights, group: int = 64):
         _refuse("the weights of one call have one type and one device")
     made = [_new_packed(r, c, group, device) for _, r, c, _ in shapes]
     mats = (Matrix * n)(*[(w.data_ptr(), r, c, s) for w, (_, r, c, s) in zip(weights, shapes)])
-    _call(device, lib().randes_pack, mats, n, shapes[0][0], group, (ctypes.c_void_p * n)(*[p.address for p in made]), _stream_of(weights[0]))
+    _call(device, lib().randes_pack, mats, n, shapes[0][0], group, (ctypes.c_void_p * n)(*[p.address for p in made]))
     return made
 
 
 def _linear_tensors(x, w: PackedMatrix, y, y_dtype: int):
     """(n_tokens, x's type and row stride, y, y's type and row stride) of a product of x [n_tokens, cols] with a [rows, cols] weight."""
-    import torch
-
     rows, cols = w.rows, w.cols
     x_dtype, n, c, x_stride = _rows_of(x, "x")
     if c != cols:
         _refuse("x has %d columns, the weight %d" % (c, cols))
-    if x.device != w.device:
-        _refuse("x is on %s, the weight on %s" % (x.device, w.device))
+    device = w.device
+    if x.device != device:
+        _refuse("x is on %s, the weight on %s" % (x.device, device))
     if y is None:
-        return n, x_dtype, x_stride, torch.empty(n, rows, dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=x.device), y_dtype, rows
+        return n, x_dtype, x_stride, _torch.empty(n, rows, dtype=_torch.bfloat16 if y_dtype == BF16 else _torch.float32, device=device), y_dtype, rows
     y_dtype, yn, yr, y_stride = _rows_of(y, "y")
-    if (yn, yr) != (n, rows) or y.device != x.device:
-        _refuse("y is [%d, %d] on %s, [%d, %d] on %s is wanted" % (yn, yr, y.device, n, rows, x.device))
+    if (yn, yr) != (n, rows) or y.device != device:
+        _refuse("y is [%d, %d] on %s, [%d, %d] on %s is wanted" % (yn, yr, y.device, n, rows, device))
     return n, x_dtype, x_stride, y, y_dtype, y_stride
 
 
 _linear_workspace_bytes = functools.lru_cache(maxsize=4096)(randes_packed_linear_workspace)
 
 
-def _linear_workspace(x, rows: int, cols: int, x_dtype: int, n: int, with_tasks: bool):
+def _linear_workspace(device, rows: int, cols: int, x_dtype: int, n: int, with_tasks: bool):
     """(tensor or None, its address, its bytes): what a product of many tokens lays its activations out in."""
-    import torch
-
     nbytes = _linear_workspace_bytes(rows, cols, x_dtype, n, with_tasks)
     if nbytes == 0:
         return None, None, 0
-    t = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    t = _torch.empty(nbytes, dtype=_torch.uint8, device=device)
     return t, t.data_ptr(), nbytes
 
 
@@ -600,9 +595,9 @@ def packed_linear(x, w: PackedMatrix, y=None, y_dtype: int = F32):
     """x: [n_tokens, cols] fp32 or bf16 CUDA tensor (rows may be strided); returns y = x W^T [n_tokens, rows]."""
     rows, cols = w.rows, w.cols
     n, x_dtype, x_stride, y, y_dtype, y_stride = _linear_tensors(x, w, y, y_dtype)
-    workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, False)
-    _call(x.device, lib().randes_packed_linear, w.address, rows, cols, w.group, x.data_ptr(), x_dtype, x_stride, n, y.data_ptr(), y_dtype,
-          y_stride, ws_at, ws_bytes, _stream_of(x))
+    workspace, ws_at, ws_bytes = _linear_workspace(w.device, rows, cols, x_dtype, n, False)
+    _call(w.device, lib().randes_packed_linear, w.address, rows, cols, w.group, x.data_ptr(), x_dtype, x_stride, n, y.data_ptr(), y_dtype,
+          y_stride, ws_at, ws_bytes)
     return y
 
 
@@ -618,11 +613,9 @@ class TokenScores(NamedTuple):
 
 
 def _target_address(targets, n: int, device):
-    import torch
-
     if targets is None:
         return None
-    if targets.dtype is not torch.int64 or targets.shape != (n,) or not targets.is_contiguous() or targets.device != device:
+    if targets.dtype is not _torch.int64 or targets.shape != (n,) or not targets.is_contiguous() or targets.device != device:
         _refuse("targets must be a contiguous int64 tensor [%d] on %s" % (n, device))
     return targets.data_ptr()
 
@@ -631,53 +624,47 @@ def token_scores(logits, targets=None, top_k: int = 0, scale: float = 1.0) -> To
     """Log probability of `targets`, entropy, and the `top_k` best tokens of every row of logits * scale (see include/randes.h).
 
     logits: [n, vocab] fp32 or bf16 CUDA tensor (rows may be strided); targets: int64 [n], negative = not scored."""
-    import torch
-
     dtype, n, vocab, stride = _rows_of(logits, "logits")
     device = logits.device
     target = _target_address(targets, n, device)
     if not 0 <= top_k <= 64:
         _refuse("top_k = %d is not in 0 .. 64" % top_k)
-    stats = torch.empty(4, n, dtype=torch.float32, device=device)
+    stats = _torch.empty(4, n, dtype=_torch.float32, device=device)
     at = stats.data_ptr()
     ids = tops = None
     if top_k:
-        ids = torch.empty(n, top_k, dtype=torch.int64, device=device)
-        tops = torch.empty(n, top_k, dtype=torch.float32, device=device)
+        ids = _torch.empty(n, top_k, dtype=_torch.int64, device=device)
+        tops = _torch.empty(n, top_k, dtype=_torch.float32, device=device)
     _call(device, lib().randes_token_scores, logits.data_ptr(), dtype, n, vocab, stride, target, scale, top_k, at if target is not None else None,
-          at + 4 * n, at + 8 * n, ids.data_ptr() if top_k else None, tops.data_ptr() if top_k else None, _stream_of(logits))
+          at + 4 * n, at + 8 * n, ids.data_ptr() if top_k else None, tops.data_ptr() if top_k else None)
     return TokenScores(stats[0] if targets is not None else None, stats[1], stats, ids, tops)
 
 
 def _row_gradient(g, what: str, n: int, device):
-    import torch
-
     if g is None:
         return None
-    if g.dtype is not torch.float32 or g.shape != (n,) or not g.is_contiguous() or g.device != device:
+    if g.dtype is not _torch.float32 or g.shape != (n,) or not g.is_contiguous() or g.device != device:
         _refuse("%s must be a contiguous float32 tensor [%d] on %s" % (what, n, device))
     return g.data_ptr()
 
 
 def token_scores_backward(logits, targets, scores: TokenScores, g_logprob=None, g_entropy=None, scale: float = 1.0, out=None):
     """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect to the logits; `out` may be the logits themselves."""
-    import torch
-
     dtype, n, vocab, stride = _rows_of(logits, "logits")
     device, stats = logits.device, scores.stats
     target = _target_address(targets, n, device)
     g_lp, g_h = _row_gradient(g_logprob, "g_logprob", n, device), _row_gradient(g_entropy, "g_entropy", n, device)
-    if stats.dtype is not torch.float32 or stats.shape != (4, n) or not stats.is_contiguous() or stats.device != device:
+    if stats.dtype is not _torch.float32 or stats.shape != (4, n) or not stats.is_contiguous() or stats.device != device:
         _refuse("the scores are not those of %d rows on %s" % (n, device))
     if out is None:
-        out, out_stride = torch.empty(n, vocab, dtype=logits.dtype, device=device), vocab
+        out, out_stride = _torch.empty(n, vocab, dtype=logits.dtype, device=device), vocab
     else:
         out_dtype, on, ov, out_stride = _rows_of(out, "out")
         if (out_dtype, on, ov) != (dtype, n, vocab) or out.device != device:
             _refuse("out must have the logits' shape, type and device")
     at = stats.data_ptr()
     _call(device, lib().randes_token_scores_backward, logits.data_ptr(), dtype, n, vocab, stride, target, scale, at + 8 * n, at + 4 * n, g_lp,
-          g_h, out.data_ptr(), out_stride, _stream_of(logits))
+          g_h, out.data_ptr(), out_stride)
     return out
 
 
@@ -862,17 +849,17 @@ class Plan:
         want = torch.bfloat16 if dtype == BF16 else torch.float32
         if t.dtype is not want:
             raise RandesError(UNSUPPORTED_DTYPE, "%s is %s: this plan keeps it in %s" % (what, t.dtype, want))
-        n, have = math.prod(shape), t.numel()
-        if (have < n if at_least else have != n) or (t.dim() == 2 and not at_least and tuple(t.shape) != tuple(shape)):
-            _refuse("%s is %s, %s is wanted" % (what, list(t.shape), list(shape)))
-        if not t.is_cuda or not t.is_contiguous() or (device is not None and t.device != device):
+        if t.shape != shape:
+            n, have = math.prod(shape), t.numel()
+            if (have < n if at_least else have != n) or (t.dim() == 2 and not at_least):
+                _refuse("%s is %s, %s is wanted" % (what, list(t.shape), list(shape)))
+        if not t.is_contiguous() or (not t.is_cuda if device is None else t.device != device):
             _refuse("%s must be a contiguous tensor on %s" % (what, "a CUDA device" if device is None else device))
         return t.data_ptr()
 
-    def _arena(self, M):
-        """M after the checks that a tensor has to pass before the library reads it as this plan's superposition."""
-        self._stored(M, "M", self.m_dtype, (self.m_bytes // (2 if self.m_dtype == BF16 else 4),), None, at_least=True)
-        return M
+    def _arena(self, M) -> int:
+        """Address of M, after the checks that a tensor has to pass before the library reads it as this plan's superposition."""
+        return self._stored(M, "M", self.m_dtype, (self.m_bytes // (2 if self.m_dtype == BF16 else 4),), None, at_least=True)
 
     def _weights(self, base, layers, device):
         """Host array of the weights' addresses; the named ones are checked. Addresses (a ctypes array, or numbers in the list)
@@ -902,13 +889,14 @@ class Plan:
         """Four-bit form of one retrieved model, its own type never stored; a list, one entry per named layer (default: all).
 
         ``base`` is the list of all layers' weights, dense and in the plan's type; only the named ones are read."""
-        self._arena(M)
+        m = self._arena(M)
+        device = M.device
         layers = list(range(self.n_layers)) if layers is None else [self._layer(l) for l in layers]
         n = len(layers)
-        weights = self._weights(base, layers, M.device)
-        made = [_new_packed(self.rows[l], self.cols[l], group, M.device) for l in layers]
-        _call(M.device, lib().randes_retrieve_packed, self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, weights,
-              M.data_ptr(), group, (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]), _stream_of(M))
+        weights = self._weights(base, layers, device)
+        made = [_new_packed(self.rows[l], self.cols[l], group, device) for l in layers]
+        _call(device, lib().randes_retrieve_packed, self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, weights, m, group,
+              (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]))
         return made
 
     def packed_linear(self, task_ids, lam: float, layer: int, x, packed_base: PackedMatrix, packed_m, y=None, y_dtype: int = F32):
@@ -939,7 +927,7 @@ class Plan:
             _refuse("%d task ids for %d tokens" % (len(task_ids), n))
         if not (isinstance(task_ids, ctypes.Array) and task_ids._type_ is ctypes.c_uint32):
             task_ids = (ctypes.c_uint32 * max(n, 1))(*task_ids)
-        workspace, ws_at, ws_bytes = _linear_workspace(x, rows, cols, x_dtype, n, True)
-        _call(x.device, lib().randes_packed_linear_tasks, self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride,
-              packed_base.address, slots, y.data_ptr(), y_dtype, y_stride, ws_at, ws_bytes, _stream_of(x))
+        workspace, ws_at, ws_bytes = _linear_workspace(device, rows, cols, x_dtype, n, True)
+        _call(device, lib().randes_packed_linear_tasks, self.handle, lam, layer, group, task_ids, n, x.data_ptr(), x_dtype, x_stride,
+              packed_base.address, slots, y.data_ptr(), y_dtype, y_stride, ws_at, ws_bytes)
         return y
