@@ -544,7 +544,8 @@ int randes_token_scores(const void* logits, randes_dtype_t dtype, uint32_t n_row
 /*
  * Gradient of sum_row g_logprob logprob + g_entropy entropy with respect to the logits:
  *   grad[row][j] = scale * ( g_logprob (1[j = target] - p_j) - g_entropy p_j (log p_j + entropy) )
- *   stats, entropy          of randes_token_scores on the same logits and scale
+ * A token of probability 0 (a masked one among them) gets gradient 0, whatever finite gradients are given.
+ *   stats, entropy          of randes_token_scores on the same logits and scale (entropy is read only with g_entropy)
  *   g_logprob, g_entropy    device fp32 [n_rows]; either may be NULL (zero).  g_logprob needs targets
  *   grad                    device [n_rows, vocab] of the logits' type, grad_stride elements between rows; may be the
  *                           logits' own memory with the same stride

@@ -443,9 +443,10 @@ constexpr int kRows = 16 * kRowTiles;
 // partial sums meet in shared memory, those of a cluster's CTAs through distributed shared memory, and are added in a fixed
 // order: results do not depend on timing.
 //
-// What bounds it: instruction issue, about 80 instructions per tile of 16 x 64 codes (decoding, four products, scales), the
-// three-way split and the signs of the activations on top. 16384 x 16384: 33 us with one bf16 token, 34 with eight, that is 4.2
-// TB/s, where the ring alone streams 6.05; small matrices: launch and latencies (768 x 768: 3.5 us).
+// What bounds it: some 6 us that do not depend on the columns (start, first loads, the join), then 5.2 TB/s, where the ring
+// alone streams 6.05: 16384 rows and 4096, 8192, 16384, 32768 columns take 11.3, 18.8, 32.9, 60.1 us with one bf16 token (eight: at most
+// 1.1 more). At 16384 x 8192 no unit is full (issue 0.54 of the slots, about 80 instructions per tile of 16 x 64 codes; HBM 0.40,
+// tensor pipe 0.24): below that size the 6 us are the larger part. 768 x 768: 3.9 us.
 template <typename XT, int GROUP>
 __global__ void __launch_bounds__(kMulWarps * 32, 2) packed_linear_kernel(const __grid_constant__ PackedLinearArgs<kNarrowTokens> a)
 {

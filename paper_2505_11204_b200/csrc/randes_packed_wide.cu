@@ -19,9 +19,12 @@
 // that a decoded word is four registers of operand A as they are. A hand-over between roles costs hundreds of cycles however
 // little it hands over: stages are 128 or 256 columns, and what is passed on also frees what came before.
 //
-// What bounds it: instruction issue (0.6 of the slots, most of them decoding and handing over) and, with many fp32 tokens,
-// operand B out of L2. 16384 x 16384, groups of 128: 17 to 64 bf16 tokens 47 to 51 us, 2.9 to 2.7 TB/s of packed weights; 64 fp32
-// tokens 99 us. Smaller groups hand over more sums: 64 tokens 73 us in groups of 64, 118 in groups of 32.
+// What bounds it: about 8 to 10 us that do not depend on the columns (two launches, set-up, first hand-overs, the join), then the
+// chain of hand-overs. In groups of 128 a stage of 256 columns costs 0.60 us with 16 bf16 tokens and 0.64 with 64 (from 16384 to
+// 32768 columns at 16384 rows: 46.4 -> 85.0 and 51.2 -> 92.5 us, 3.4 TB/s of packed weights), and no unit is full at 64 tokens
+// (issue 0.60 of the slots, waiting warps' questions included; tensor pipe 0.33, HBM 0.27): operand A has two stages, and
+// each goes record, decode, tensor memory, products, free again. 64 fp32 tokens pay for their three products, 1.4 us per 256
+// columns (16384 x 16384: 99.7 us). Smaller groups hand over more sums: 64 tokens 73 us in groups of 64, 118 in groups of 32.
 //
 // Every wait is bounded; a CTA whose wait runs out raises a flag, all roles leave, what is in flight is waited for, tensor
 // memory is freed, its sums become NaN and a device counter records the event.
@@ -541,6 +544,8 @@ template <int NT, typename XT> cudaError_t launch_group(PackedLinearArgs<kWideTo
 // every row block: it loses them where the matrix is large (one token, 16384 x 8192: 35 us against 29; with a superposition
 // 67 against 52; 4096 x 4096: 7.6 against 8.9 and 13.0 against 12.1), unless the rows are short, so that a CTA of this form has little to
 // do once it has set itself up (50257 x 768: 14.4 against 17.7; with a superposition, so with twice the columns, 28.7 against 27.9).
+// Nothing was measured between 2^24 and 2^25 codes; and a superposition counts as one slot, however many the tokens use (the
+// workspace is asked for before their tasks are known).
 bool packed_is_wide(uint32_t rows, uint32_t cols, bool x_bf16, uint32_t n_tokens, bool tasks)
 {
     const uint64_t columns = static_cast<uint64_t>(cols) << tasks;       // base, and one slot of the superposition

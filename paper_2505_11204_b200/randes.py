@@ -603,7 +603,8 @@ def packed_linear(x, w: PackedMatrix, y=None, y_dtype: int = F32):
 
 class TokenScores(NamedTuple):
     """What token_scores returns. ``stats`` [4, n] is what the backward call needs: rows logprob, entropy, greatest logit, log
-    of the sum of exponentials relative to it (of scale * logits)."""
+    of the sum of exponentials relative to it (of scale * logits). ``logprob`` and ``entropy`` are views of its first two rows:
+    clone them before changing them in place, an entropy that has changed changes the entropy's gradient."""
 
     logprob: Any
     entropy: Any
@@ -649,7 +650,9 @@ def _row_gradient(g, what: str, n: int, device):
 
 
 def token_scores_backward(logits, targets, scores: TokenScores, g_logprob=None, g_entropy=None, scale: float = 1.0, out=None):
-    """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect to the logits; `out` may be the logits themselves."""
+    """Gradient of sum(g_logprob * logprob + g_entropy * entropy) with respect to the logits; `out` may be the logits themselves.
+
+    Reads ``scores.stats`` (of token_scores on the same logits and scale), the entropy in it only with ``g_entropy``."""
     dtype, n, vocab, stride = _rows_of(logits, "logits")
     device, stats = logits.device, scores.stats
     target = _target_address(targets, n, device)

@@ -21,7 +21,7 @@ from .scoring import token_log_probs
 
 
 def build(width: int, blocks: int, vocab: int, n_tasks: int, seed: int = 0):
-    """(plan, base, deltas, M): `blocks` layers [width, width] of one shuffled group and a head [vocab, width]."""
+    """(plan, base, models, M): `blocks` layers [width, width] of one shuffled group and a head [vocab, width]."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
     rows, cols = [width] * blocks + [vocab], [width] * (blocks + 1)
     plan = randes.Plan(rows, cols, [0] * blocks + [1], [randes.SHUFFLE | randes.FLIP, randes.FLIP], task_ids=range(n_tasks),
