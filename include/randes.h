@@ -339,8 +339,8 @@ int randes_linear_gated(const randes_plan_t* plan, uint32_t task_id, float lambd
  * Every wait inside the randes_linear kernel is bounded; a thread block whose wait runs out
  * skips its tile and counts itself here.  *count = number of such blocks since the library was
  * loaded on the current device (0 in a healthy run).  Synchronises with the device.
- * The kernels of randes_packed_linear and randes_packed_linear_tasks wait likewise and are counted here too (per warp or
- * per block); what such a warp or block was to add up comes out as NaN.
+ * The kernels of randes_packed_linear, randes_packed_linear_tasks and randes_packed_eight_linear wait likewise and are counted here
+ * too (per warp or per block); what such a warp or block was to add up comes out as NaN.
  */
 int randes_linear_giveups(unsigned int* count);
 
@@ -554,6 +554,112 @@ int randes_token_scores(const void* logits, randes_dtype_t dtype, uint32_t n_row
 int randes_token_scores_backward(const void* logits, randes_dtype_t dtype, uint32_t n_rows, uint32_t vocab, uint64_t stride,
                                  const int64_t* targets, float scale, const float* stats, const float* entropy,
                                  const float* g_logprob, const float* g_entropy, void* grad, uint64_t grad_stride, void* stream);
+
+/*
+ * Weights and activations in eight bits
+ * -------------------------------------
+ * (The paper has no counterpart: a prompt of many tokens, or a training step, is bound by the tensor cores, which multiply eight-bit
+ * numbers at twice bf16's rate.)  A row is cut into blocks of 128 columns (the last may be shorter).  With a = max |w| of a block,
+ *     e = the least integer, -100 at least, with a <= 448 * 2^e,   code = e4m3( w * 2^-e ) (nearest even),   it stands for code * 2^e
+ * A block that holds a NaN or an infinity reads back as NaN; a value that rounds to 2^128 (the last 1/64 of fp32's range) as an
+ * infinity.  A matrix in eight bits is one opaque buffer of
+ * randes_packed_eight_bytes(), 16-byte aligned, device memory of the caller's; it is kept in tiles of 128 rows x 128 columns, so
+ * that a few rows take the memory of 128.
+ */
+/* Bytes of a [rows, cols] matrix in eight bits; 0 on an empty matrix or one of more than 2^24 tiles.  Host-only. */
+size_t randes_packed_eight_bytes(uint32_t rows, uint32_t cols);
+
+/* Eight-bit form of n matrices (one kernel launch per 32); arguments and errors as randes_pack. */
+int randes_pack_eight(const randes_matrix_t* w, uint32_t n, randes_dtype_t dtype, void* const* packed, void* stream);
+
+/* The values the eight bits stand for: exact in fp32 and in bf16 (below bf16's normal range: rounded).  As randes_unpack. */
+int randes_unpack_eight(const void* const* packed, uint32_t n, const randes_matrix_t* out, randes_dtype_t out_dtype, void* stream);
+
+/*
+ * Eight-bit form of a matrix's transpose, [w.cols, w.rows] in blocks of 128 ROWS of w; and with packed != NULL that of the matrix
+ * itself out of the same read.  What a training step needs: y = x W^T has dx = dy W, a product with (W^T), and
+ * dW = dy^T x, a product of (dy^T) with (x^T).  One kernel launch.  Errors: as randes_pack.
+ */
+int randes_pack_eight_transposed(const randes_matrix_t* w, randes_dtype_t dtype, void* packed, void* transposed, void* stream);
+
+/*
+ * The same of a [rows, cols] matrix that is in eight bits already (an activation kept for the backward pass).  Scales are powers
+ * of two, so values stay what they are; only those below 2^-6 of the new block's unit lose bits.  One kernel launch.
+ */
+int randes_transpose_eight(const void* packed, uint32_t rows, uint32_t cols, void* transposed, void* stream);
+
+/* retrieve straight into eight bits: arguments and errors as randes_retrieve_packed. */
+int randes_retrieve_packed_eight(const randes_plan_t* plan, uint32_t task_id, float lambda, const uint32_t* layers, uint32_t n,
+                            const void* const* base, const void* M, void* const* packed, void* stream);
+
+/*
+ * Product of two matrices in eight bits:  y[t][r] = sum_c x[t][c] w[r][c].
+ *   w [rows, cols], x [n_tokens, cols]   in eight bits
+ *   y, y_dtype, y_stride                 device [n_tokens, rows], y_stride elements between tokens (>= rows); must not overlap x or w
+ * Products are exact, sums run in the tensor core's fp32 in a fixed order, a bf16 y is rounded once.  From one token to millions.
+ * One kernel launch.  Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, CUDA_ERROR.  Its waits are bounded and counted by
+ * randes_linear_giveups().
+ */
+int randes_packed_eight_linear(const void* w, uint32_t rows, uint32_t cols, const void* x, uint32_t n_tokens, void* y, randes_dtype_t y_dtype,
+                          uint64_t y_stride, void* stream);
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition in front:
+ *     h = x + residual, rounded to dtype (without residual: x)       rstd = 1 / sqrt( mean h^2 + eps )       y = h rstd gain
+ *   x, residual, h, y    device [rows, cols] of `dtype`, strides in elements; residual, h, y may be NULL.  h may be x's or the
+ *                        residual's own memory (with the same stride), y may be x's or the residual's unless h is; else apart
+ *   gain                 device [cols], fp32 or bf16 (gain_dtype); NULL: ones
+ *   y8                   y in eight bits (randes_packed_eight_bytes(rows, cols)) or NULL: what a product takes, and what its backward
+ *                        pass takes as the checkpoint of its input
+ *   kept8                h in eight bits or NULL: the checkpoint that randes_rms_norm_backward reads
+ *   rstd                 device fp32 [rows] or NULL
+ *   rows, cols           1 <= cols <= 32768;  eps in [1e-20, 1]
+ * One pass, sums in fp32 in a fixed order (again in fp64 where fp32 overflows), one kernel launch.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, CUDA_ERROR.
+ */
+typedef struct {
+    const void* x;
+    const void* residual;
+    const void* gain;
+    void* h;
+    void* y;
+    void* y8;
+    void* kept8;
+    float* rstd;
+    uint64_t x_stride, residual_stride, h_stride, y_stride;
+    uint32_t rows, cols;
+    randes_dtype_t dtype, gain_dtype;
+    float eps;
+} randes_rms_norm_t;
+int randes_rms_norm(const randes_rms_norm_t* norm, void* stream);
+
+/*
+ * Its gradient.  With n = h rstd and g = dy gain:
+ *     dx = rstd ( g - n mean(g n) ) + dh        dgain = sum over rows of dy n
+ * dx is the gradient of x and of the residual alike.
+ *   dy, h, dh, dx     device [rows, cols] of `dtype`, strides in elements; dh (the gradient that reaches h past the norm) may be
+ *                     NULL; dx may be the own memory of dy, h or dh (with the same stride)
+ *   kept8             in place of h (which is NULL then): h in eight bits
+ *   rstd              of the forward call
+ *   dgain             device fp32 [cols] or NULL
+ *   workspace         device memory, 16-byte aligned, at least randes_rms_norm_backward_workspace(rows, cols) bytes with dgain
+ * Sums in fp32 in a fixed order; one kernel launch, two with dgain.  Errors: as above, WORKSPACE_TOO_SMALL.
+ */
+typedef struct {
+    const void* dy;
+    const void* h;
+    const void* kept8;
+    const float* rstd;
+    const void* gain;
+    const void* dh;
+    void* dx;
+    float* dgain;
+    uint64_t dy_stride, h_stride, dh_stride, dx_stride;
+    uint32_t rows, cols;
+    randes_dtype_t dtype, gain_dtype;
+} randes_rms_norm_backward_t;
+size_t randes_rms_norm_backward_workspace(uint32_t rows, uint32_t cols);      /* host-only */
+int randes_rms_norm_backward(const randes_rms_norm_backward_t* grad, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Number of kernels this library has launched in this process (all plans). */
 uint64_t randes_launch_count(void);

@@ -18,8 +18,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librandes.so")
-SOURCES = ["randes_api.cu", "randes_kernels.cu", "randes_group.cu", "randes_linear.cu", "randes_context.cu", "randes_batch.cu", "randes_diag.cu", "randes_packed.cu", "randes_packed_wide.cu", "randes_scores.cu"]
-HEADERS = [os.path.join(CSRC, "randes_internal.h"), os.path.join(CSRC, "randes_device.cuh"), os.path.join(CSRC, "randes_packed.cuh"), os.path.join(os.path.dirname(HERE), "include", "randes.h")]
+SOURCES = ["randes_api.cu", "randes_kernels.cu", "randes_group.cu", "randes_linear.cu", "randes_context.cu", "randes_batch.cu", "randes_diag.cu", "randes_packed.cu", "randes_packed_wide.cu", "randes_scores.cu", "randes_packed8.cu", "randes_linear8.cu", "randes_norm.cu"]
+HEADERS = [os.path.join(CSRC, "randes_internal.h"), os.path.join(CSRC, "randes_device.cuh"), os.path.join(CSRC, "randes_packed.cuh"), os.path.join(CSRC, "randes_packed8.cuh"), os.path.join(os.path.dirname(HERE), "include", "randes.h")]
 
 
 def _stale() -> bool:

@@ -9,6 +9,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <string>
 #include <vector>
@@ -1316,12 +1317,13 @@ int randes_linear_gated(const randes_plan_t* plan, uint32_t task_id, float lambd
 int randes_linear_giveups(unsigned int* count)
 {
     if (!count) return fail(RANDES_INVALID_ARGUMENT, "count is NULL");
-    unsigned int packed = 0, wide = 0;
+    unsigned int packed = 0, wide = 0, eight = 0;
     int e = linear_giveups(count);
     if (!e) e = packed_giveups(&packed);
     if (!e) e = packed_wide_giveups(&wide);
+    if (!e) e = linear8_giveups(&eight);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "read of the give-up counter");
-    *count += packed + wide;
+    *count += packed + wide + eight;
     return RANDES_OK;
 }
 
@@ -1892,9 +1894,347 @@ int randes_token_scores_backward_impl(const void* logits, randes_dtype_t dtype, 
     return RANDES_OK;
 }
 
+// ---- eight bits, their products, the norm -----------------------------------------------------
+// Sizes that the eight-bit operators serve: tiles of 128 x 128 are counted in 32 bits (2^24 of them are 256 GiB).
+bool packable8(uint32_t rows, uint32_t cols)
+{
+    return (static_cast<uint64_t>(rows) + 127) / 128 * ((static_cast<uint64_t>(cols) + 127) / 128) <= (1u << 24);
+}
+
+int check_matrix8(const void* data, uint32_t rows, uint32_t cols, uint64_t stride, uint32_t i, size_t elem, const void* packed)
+{
+    int rc;
+    char what[32];
+    snprintf(what, sizeof what, "matrix %u", i);
+    if ((rc = check_tensor(data, rows, cols, stride, elem, what))) return rc;
+    if (rows == 0 || cols == 0) return RANDES_OK;
+    if (!packable8(rows, cols)) return fail(RANDES_INVALID_ARGUMENT, "matrix %u: %u x %u is too large to be packed", i, rows, cols);
+    snprintf(what, sizeof what, "packed[%u]", i);
+    if ((rc = check_packed(packed, what))) return rc;
+    if (overlap(data, span_bytes(rows, cols, stride, elem), packed, randes_packed_eight_bytes(rows, cols)))
+        return fail(RANDES_INVALID_ARGUMENT, "packed[%u] overlaps its matrix", i);
+    return RANDES_OK;
+}
+
+int randes_pack_eight_impl(const randes_matrix_t* w, uint32_t n, randes_dtype_t dtype, void* const* packed, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(dtype, "weight"))) return rc;
+    if (n == 0) return RANDES_OK;
+    if (!w || !packed) return fail(RANDES_INVALID_ARGUMENT, "w or packed is NULL");
+    const size_t elem = elem_size(dtype);
+    for (uint32_t i = 0; i < n; ++i)
+        if ((rc = check_matrix8(w[i].data, w[i].rows, w[i].cols, w[i].stride, i, elem, packed[i]))) return rc;
+    for (uint32_t first = 0; first < n;) {
+        Pack8Args a;
+        a.n = 0;
+        a.lambda = 0.f;
+        a.task = DevTask{0, 0, 0, 0};
+        for (; first < n && a.n < kPackBatch; ++first) {
+            const randes_matrix_t& m = w[first];
+            if (m.rows == 0 || m.cols == 0) continue;
+            a.mat[a.n++] = Pack8Matrix{m.data, nullptr, packed[first], m.stride, m.rows, m.cols, 0, 0, rows_aligned(m.data, m.rows, m.stride, elem) ? 1u : 0u, 0};
+        }
+        if (a.n == 0) break;
+        const int e = launch_pack8(dtype, dtype, false, a, stream);
+        if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit pack kernel");
+        ++g_launches;
+    }
+    return RANDES_OK;
+}
+
+int randes_unpack_eight_impl(const void* const* packed, uint32_t n, const randes_matrix_t* out, randes_dtype_t out_dtype, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(out_dtype, "output"))) return rc;
+    if (n == 0) return RANDES_OK;
+    if (!out || !packed) return fail(RANDES_INVALID_ARGUMENT, "out or packed is NULL");
+    const size_t elem = elem_size(out_dtype);
+    for (uint32_t i = 0; i < n; ++i)
+        if ((rc = check_matrix8(out[i].data, out[i].rows, out[i].cols, out[i].stride, i, elem, packed[i]))) return rc;
+    for (uint32_t first = 0; first < n;) {
+        Unpack8Args a;
+        a.n = 0;
+        for (; first < n && a.n < kPackBatch; ++first) {
+            const randes_matrix_t& m = out[first];
+            if (m.rows == 0 || m.cols == 0) continue;
+            a.mat[a.n++] = Unpack8Matrix{packed[first], m.data, m.stride, m.rows, m.cols, rows_aligned(m.data, m.rows, m.stride, elem) ? 1u : 0u, 0};
+        }
+        if (a.n == 0) break;
+        const int e = launch_unpack8(out_dtype, a, stream);
+        if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit unpack kernel");
+        ++g_launches;
+    }
+    return RANDES_OK;
+}
+
+int turn8(int src_dtype, const void* src, uint32_t rows, uint32_t cols, uint64_t stride, bool vec, void* packed, void* transposed, void* stream)
+{
+    const int e = launch_turn8(src_dtype, Turn8Args{src, packed, transposed, stride, rows, cols, vec ? 1u : 0u}, stream);
+    if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit transpose kernel");
+    ++g_launches;
+    return RANDES_OK;
+}
+
+int randes_pack_eight_transposed_impl(const randes_matrix_t* w, randes_dtype_t dtype, void* packed, void* transposed, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(dtype, "weight"))) return rc;
+    if (!w) return fail(RANDES_INVALID_ARGUMENT, "w is NULL");
+    const size_t elem = elem_size(dtype);
+    if ((rc = check_matrix8(w->data, w->rows, w->cols, w->stride, 0, elem, packed ? packed : transposed))) return rc;
+    if (w->rows == 0 || w->cols == 0) return RANDES_OK;
+    if ((rc = check_packed(transposed, "transposed"))) return rc;
+    const size_t bytes = randes_packed_eight_bytes(w->rows, w->cols), turned = randes_packed_eight_bytes(w->cols, w->rows);
+    if (overlap(w->data, span_bytes(w->rows, w->cols, w->stride, elem), transposed, turned) || (packed && overlap(packed, bytes, transposed, turned)))
+        return fail(RANDES_INVALID_ARGUMENT, "transposed overlaps the matrix or its packed form");
+    return turn8(dtype, w->data, w->rows, w->cols, w->stride, rows_aligned(w->data, w->rows, w->stride, elem), packed, transposed, stream);
+}
+
+int randes_transpose_eight_impl(const void* packed, uint32_t rows, uint32_t cols, void* transposed, void* stream)
+{
+    int rc;
+    if (rows == 0 || cols == 0) return RANDES_OK;
+    if (!packable8(rows, cols)) return fail(RANDES_INVALID_ARGUMENT, "a packed matrix of %u x %u is not supported", rows, cols);
+    if ((rc = check_packed(packed, "packed")) || (rc = check_packed(transposed, "transposed"))) return rc;
+    if (overlap(packed, randes_packed_eight_bytes(rows, cols), transposed, randes_packed_eight_bytes(cols, rows)))
+        return fail(RANDES_INVALID_ARGUMENT, "transposed overlaps packed");
+    return turn8(-1, packed, rows, cols, 0, true, nullptr, transposed, stream);
+}
+
+int randes_retrieve_packed_eight_impl(const randes_plan_t* plan, uint32_t task_id, float lambda, const uint32_t* layers, uint32_t n,
+                                 const void* const* base, const void* M, void* const* packed, void* stream)
+{
+    if (!plan) return fail(RANDES_INVALID_ARGUMENT, "plan is NULL");
+    if (plan->has_gauss) return fail(RANDES_INVALID_ARGUMENT, "not offered for plans with a RANDES_GAUSS group");
+    int rc;
+    if ((rc = check_m(M))) return rc;
+    const int row = find_task(*plan, task_id);
+    if (row < 0) return fail(RANDES_UNKNOWN_TASK, "task id %u is not registered", task_id);
+    if (n == 0) return RANDES_OK;
+    if (!layers || !base || !packed) return fail(RANDES_INVALID_ARGUMENT, "layers, base or packed is NULL");
+    const size_t elem = elem_size(plan->storage), m_elem = elem_size(plan->m_dtype);
+    for (uint32_t i = 0; i < n; ++i) {
+        if (layers[i] >= plan->n_layers) return fail(RANDES_INVALID_ARGUMENT, "layer %u out of range (n_layers = %u)", layers[i], plan->n_layers);
+        const randes_layer_t& l = plan->layers[layers[i]];
+        if ((rc = check_matrix8(base[layers[i]], l.rows, l.cols, l.cols, i, elem, packed[i]))) return rc;
+        if (overlap(M, plan->m_bytes, packed[i], randes_packed_eight_bytes(l.rows, l.cols)))
+            return fail(RANDES_INVALID_ARGUMENT, "packed[%u] overlaps M", i);
+    }
+    const TaskEntry& t = plan->tasks[row];
+    for (uint32_t first = 0; first < n;) {
+        Pack8Args a;
+        a.n = 0;
+        a.lambda = lambda;
+        a.task = dev_task(t);
+        for (; first < n && a.n < kPackBatch; ++first) {
+            const uint32_t p = layers[first], slot = t.slot_of_pos[p];
+            const randes_layer_t& l = plan->layers[p];
+            if (l.rows == 0 || l.cols == 0) continue;
+            const char* m = static_cast<const char*>(M) + plan->m_off_bytes[slot];
+            const uint32_t vec = (rows_aligned(base[p], l.rows, l.cols, elem) ? 1u : 0u) | (rows_aligned(m, l.rows, l.cols, m_elem) ? 2u : 0u);
+            a.mat[a.n++] = Pack8Matrix{base[p], m, packed[first], l.cols, l.rows, l.cols, slot, plan->dev_layers[slot].flags & kFlagFlip ? 1u : 0u, vec, 0};
+        }
+        if (a.n == 0) break;
+        const int e = launch_pack8(plan->storage, plan->m_dtype, true, a, stream);
+        if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit retrieve-and-pack kernel");
+        ++g_launches;
+    }
+    return RANDES_OK;
+}
+
+int randes_packed_eight_linear_impl(const void* w, uint32_t rows, uint32_t cols, const void* x, uint32_t n_tokens, void* y, randes_dtype_t y_dtype,
+                               uint64_t y_stride, void* stream)
+{
+    int rc;
+    if ((rc = check_dtype(y_dtype, "output"))) return rc;
+    if (n_tokens == 0 || rows == 0) return RANDES_OK;
+    const size_t ye = elem_size(y_dtype);
+    if ((rc = check_tensor(y, n_tokens, rows, y_stride, ye, "y"))) return rc;
+    if (cols == 0) {      // a sum over nothing
+        const cudaError_t e = n_tokens == 1 ? cudaMemsetAsync(y, 0, rows * ye, static_cast<cudaStream_t>(stream))
+                                            : cudaMemset2DAsync(y, y_stride * ye, 0, rows * ye, n_tokens, static_cast<cudaStream_t>(stream));
+        return e == cudaSuccess ? static_cast<int>(RANDES_OK) : fail_cuda(e, "clearing y");
+    }
+    if (!packable8(rows, cols) || !packable8(n_tokens, cols) || !packable8(rows, n_tokens))
+        return fail(RANDES_INVALID_ARGUMENT, "a product of %u tokens with %u x %u is not supported", n_tokens, rows, cols);
+    if ((rc = check_packed(w, "w")) || (rc = check_packed(x, "x"))) return rc;
+    const uint64_t span = span_bytes(n_tokens, rows, y_stride, ye);
+    if (overlap(w, randes_packed_eight_bytes(rows, cols), y, span) || overlap(x, randes_packed_eight_bytes(n_tokens, cols), y, span))
+        return fail(RANDES_INVALID_ARGUMENT, "y overlaps w or x");
+    Device dev;
+    if ((rc = current_device(&dev))) return rc;
+    Linear8Args a{w, x, y, y_stride, rows, cols, n_tokens, y_dtype == RANDES_BF16 ? 1u : 0u, 0};
+    const int e = launch_linear8(a, dev.sms, dev.index, stream);
+    if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit product");
+    ++g_launches;
+    return RANDES_OK;
+}
+
+// A tensor that a norm writes may be the very memory of one it reads; other overlaps of dense tensors are refused (strided ones may
+// interleave without sharing an element).
+struct NormTensor {
+    const void* p;
+    uint64_t stride;
+    const char* name;
+};
+int check_apart(const NormTensor& out, std::initializer_list<NormTensor> others, uint32_t rows, uint32_t cols, size_t elem, bool may_be_same)
+{
+    if (!out.p) return RANDES_OK;
+    for (const NormTensor& o : others) {
+        if (!o.p || (may_be_same && o.p == out.p && (rows == 1 || o.stride == out.stride))) continue;
+        if (rows > 1 && (o.stride != cols || out.stride != cols) && o.p != out.p) continue;
+        if (overlap(out.p, span_bytes(rows, cols, out.stride, elem), o.p, span_bytes(rows, cols, o.stride, elem)))
+            return fail(RANDES_INVALID_ARGUMENT, "%s overlaps %s", out.name, o.name);
+    }
+    return RANDES_OK;
+}
+int check_norm(uint32_t rows, uint32_t cols, int dtype, const void* gain, int gain_dtype)
+{
+    int rc;
+    if ((rc = check_dtype(dtype, "activation")) || (gain && (rc = check_dtype(gain_dtype, "gain")))) return rc;
+    if (cols == 0 || cols > kNormMaxCols) return fail(RANDES_INVALID_ARGUMENT, "%u columns are not in 1 .. %u", cols, kNormMaxCols);
+    if (rows > 0x7FFFFFFFu || !packable8(rows, cols)) return fail(RANDES_INVALID_ARGUMENT, "%u rows of %u columns are not supported", rows, cols);
+    if (gain && reinterpret_cast<uintptr_t>(gain) % elem_size(gain_dtype)) return fail(RANDES_MISALIGNED, "gain is not aligned to its element size");
+    return RANDES_OK;
+}
+int check_words(const void* p, const char* what)
+{
+    if (reinterpret_cast<uintptr_t>(p) % 4) return fail(RANDES_MISALIGNED, "%s is not aligned to its element size", what);
+    return RANDES_OK;
+}
+
+int randes_rms_norm_impl(const randes_rms_norm_t* p, void* stream)
+{
+    if (!p) return fail(RANDES_INVALID_ARGUMENT, "norm is NULL");
+    const randes_rms_norm_t& a = *p;
+    int rc;
+    if ((rc = check_norm(a.rows, a.cols, a.dtype, a.gain, a.gain_dtype))) return rc;
+    if (!(a.eps >= 1e-20f && a.eps <= 1.f)) return fail(RANDES_INVALID_ARGUMENT, "eps = %g is not in [1e-20, 1]", static_cast<double>(a.eps));
+    if (a.rows == 0) return RANDES_OK;
+    const size_t elem = elem_size(a.dtype), bytes8 = randes_packed_eight_bytes(a.rows, a.cols);
+    const NormTensor x{a.x, a.x_stride, "x"}, res{a.residual, a.residual_stride, "the residual"}, h{a.h, a.h_stride, "h"}, y{a.y, a.y_stride, "y"};
+    bool vec = true;
+    for (const NormTensor* t : {&x, &res, &h, &y}) {
+        if (!t->p && t != &x) continue;
+        if ((rc = check_tensor(t->p, a.rows, a.cols, t->stride, elem, t->name))) return rc;
+        vec = vec && rows_aligned(t->p, a.rows, t->stride, elem);
+    }
+    if ((rc = check_apart(h, {x, res}, a.rows, a.cols, elem, true)) || (rc = check_apart(y, {x, res}, a.rows, a.cols, elem, true)) ||
+        (rc = check_apart(y, {h}, a.rows, a.cols, elem, false)))
+        return rc;
+    for (const void* q : {static_cast<const void*>(a.y8), static_cast<const void*>(a.kept8)}) {
+        if (!q) continue;
+        if ((rc = check_packed(q, q == a.y8 ? "y8" : "kept8"))) return rc;
+        for (const NormTensor* t : {&x, &res, &h, &y})
+            if (t->p && overlap(q, bytes8, t->p, span_bytes(a.rows, a.cols, t->stride, elem)))
+                return fail(RANDES_INVALID_ARGUMENT, "an eight-bit output overlaps %s", t->name);
+    }
+    if (a.y8 && a.kept8 && overlap(a.y8, bytes8, a.kept8, bytes8)) return fail(RANDES_INVALID_ARGUMENT, "y8 overlaps kept8");
+    if ((rc = check_words(a.rstd, "rstd"))) return rc;
+    const NormArgs n{a.x, a.residual, a.gain, a.h, a.y, a.y8, a.kept8, a.rstd, a.x_stride, a.residual_stride, a.h_stride, a.y_stride,
+                     a.rows, a.cols, vec ? 1u : 0u, a.gain && a.gain_dtype == RANDES_BF16 ? 1u : 0u, a.eps};
+    const int e = launch_norm(a.dtype, n, stream);
+    if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the norm kernel");
+    ++g_launches;
+    return RANDES_OK;
+}
+
+int randes_rms_norm_backward_impl(const randes_rms_norm_backward_t* p, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!p) return fail(RANDES_INVALID_ARGUMENT, "grad is NULL");
+    const randes_rms_norm_backward_t& a = *p;
+    int rc;
+    if ((rc = check_norm(a.rows, a.cols, a.dtype, a.gain, a.gain_dtype))) return rc;
+    if ((rc = check_words(a.rstd, "rstd")) || (rc = check_words(a.dgain, "dgain"))) return rc;
+    if (a.rows == 0) {      // a sum over no rows
+        if (!a.dgain) return RANDES_OK;
+        const cudaError_t e = cudaMemsetAsync(a.dgain, 0, a.cols * sizeof(float), static_cast<cudaStream_t>(stream));
+        return e == cudaSuccess ? static_cast<int>(RANDES_OK) : fail_cuda(e, "clearing dgain");
+    }
+    if (!a.rstd || !a.dx) return fail(RANDES_INVALID_ARGUMENT, "rstd or dx is NULL");
+    if (!a.h == !a.kept8) return fail(RANDES_INVALID_ARGUMENT, "either h or kept8 is wanted");
+    const size_t elem = elem_size(a.dtype);
+    const NormTensor dy{a.dy, a.dy_stride, "dy"}, h{a.h, a.h_stride, "h"}, dh{a.dh, a.dh_stride, "dh"}, dx{a.dx, a.dx_stride, "dx"};
+    bool vec = true;
+    for (const NormTensor* t : {&dy, &h, &dh, &dx}) {
+        if (!t->p && t != &dy) continue;
+        if ((rc = check_tensor(t->p, a.rows, a.cols, t->stride, elem, t->name))) return rc;
+        vec = vec && rows_aligned(t->p, a.rows, t->stride, elem);
+    }
+    if ((rc = check_apart(dx, {dy, h, dh}, a.rows, a.cols, elem, true))) return rc;
+    if (a.kept8) {
+        if ((rc = check_packed(a.kept8, "kept8"))) return rc;
+        if (overlap(a.kept8, randes_packed_eight_bytes(a.rows, a.cols), a.dx, span_bytes(a.rows, a.cols, a.dx_stride, elem)))
+            return fail(RANDES_INVALID_ARGUMENT, "dx overlaps kept8");
+    }
+    const size_t need = a.dgain ? randes_rms_norm_backward_workspace(a.rows, a.cols) : 0;
+    if (need) {
+        if (!workspace || workspace_bytes < need)
+            return fail(RANDES_WORKSPACE_TOO_SMALL, "the gradient of the gain needs a workspace of %zu bytes, got %zu", need, workspace ? workspace_bytes : 0);
+        if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(RANDES_MISALIGNED, "workspace = %p is not 16-byte aligned", workspace);
+    }
+    const NormGradArgs n{a.dy, a.h, a.kept8, a.rstd, a.gain, a.dh, a.dx, a.dgain, static_cast<float*>(workspace), a.dy_stride, a.h_stride, a.dh_stride,
+                         a.dx_stride, a.rows, a.cols, vec ? 1u : 0u, a.gain && a.gain_dtype == RANDES_BF16 ? 1u : 0u};
+    int launched = 0;
+    const int e = launch_norm_grad(a.dtype, n, &launched, stream);
+    g_launches += launched;
+    if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the norm's gradient");
+    return RANDES_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t randes_packed_eight_bytes(uint32_t rows, uint32_t cols)
+{
+    return rows == 0 || cols == 0 || !packable8(rows, cols) ? 0 : Packed8Layout(rows, cols).total;
+}
+
+int randes_pack_eight(const randes_matrix_t* w, uint32_t n, randes_dtype_t dtype, void* const* packed, void* stream)
+{
+    return guarded("randes_pack_eight", [&] { return randes_pack_eight_impl(w, n, dtype, packed, stream); });
+}
+
+int randes_unpack_eight(const void* const* packed, uint32_t n, const randes_matrix_t* out, randes_dtype_t out_dtype, void* stream)
+{
+    return guarded("randes_unpack_eight", [&] { return randes_unpack_eight_impl(packed, n, out, out_dtype, stream); });
+}
+
+int randes_pack_eight_transposed(const randes_matrix_t* w, randes_dtype_t dtype, void* packed, void* transposed, void* stream)
+{
+    return guarded("randes_pack_eight_transposed", [&] { return randes_pack_eight_transposed_impl(w, dtype, packed, transposed, stream); });
+}
+
+int randes_transpose_eight(const void* packed, uint32_t rows, uint32_t cols, void* transposed, void* stream)
+{
+    return guarded("randes_transpose_eight", [&] { return randes_transpose_eight_impl(packed, rows, cols, transposed, stream); });
+}
+
+int randes_retrieve_packed_eight(const randes_plan_t* plan, uint32_t task_id, float lambda, const uint32_t* layers, uint32_t n,
+                            const void* const* base, const void* M, void* const* packed, void* stream)
+{
+    return guarded("randes_retrieve_packed_eight", [&] { return randes_retrieve_packed_eight_impl(plan, task_id, lambda, layers, n, base, M, packed, stream); });
+}
+
+int randes_packed_eight_linear(const void* w, uint32_t rows, uint32_t cols, const void* x, uint32_t n_tokens, void* y, randes_dtype_t y_dtype,
+                          uint64_t y_stride, void* stream)
+{
+    return guarded("randes_packed_eight_linear", [&] { return randes_packed_eight_linear_impl(w, rows, cols, x, n_tokens, y, y_dtype, y_stride, stream); });
+}
+
+int randes_rms_norm(const randes_rms_norm_t* norm, void* stream)
+{
+    return guarded("randes_rms_norm", [&] { return randes_rms_norm_impl(norm, stream); });
+}
+
+size_t randes_rms_norm_backward_workspace(uint32_t rows, uint32_t cols) { return norm_grad_workspace(rows, cols); }
+
+int randes_rms_norm_backward(const randes_rms_norm_backward_t* grad, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return guarded("randes_rms_norm_backward", [&] { return randes_rms_norm_backward_impl(grad, workspace, workspace_bytes, stream); });
+}
 
 size_t randes_packed_bytes(uint32_t rows, uint32_t cols, uint32_t group)
 {

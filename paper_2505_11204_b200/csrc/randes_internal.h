@@ -303,6 +303,110 @@ size_t packed_wide_workspace(uint32_t rows, uint32_t cols, bool x_bf16, uint32_t
 int launch_packed_wide(PackedLinearArgs<kWideTokens>& a, bool x_bf16, int sm_count, int device, int* launched, void* stream);
 int packed_wide_giveups(unsigned int* count);
 
+// randes_packed8.cu: weights and activations in eight bits, a power-of-two scale per block of 128 columns of a row (the
+// layout is described there).
+struct Packed8Layout {
+    uint32_t row_tiles, col_blocks, groups;      // tiles of 128 rows, blocks of 128 columns, groups of four blocks
+    size_t codes, total;                         // bytes of the codes, of everything
+    RANDES_BOTH Packed8Layout(uint32_t rows, uint32_t cols)
+    {
+        row_tiles = (rows >> 7) + ((rows & 127) != 0);
+        col_blocks = (cols >> 7) + ((cols & 127) != 0);
+        groups = (col_blocks + 3) / 4;
+        codes = static_cast<size_t>(row_tiles) * col_blocks * 16384;
+        total = codes + static_cast<size_t>(row_tiles) * groups * 512;
+    }
+    // byte offsets: tile of 128 x 128 codes; word of the scales of a row's four blocks
+    RANDES_BOTH size_t tile(uint32_t rt, uint32_t kb) const { return (static_cast<size_t>(rt) * col_blocks + kb) * 16384; }
+    RANDES_BOTH size_t scales(uint32_t rt, uint32_t g) const { return codes + (static_cast<size_t>(rt) * groups + g) * 512; }
+    static RANDES_BOTH uint32_t scale_word(uint32_t r) { return (r & 31) * 16 + ((r >> 5) & 3) * 4; }      // inside the 512 bytes of a group
+};
+struct Pack8Matrix {
+    const void* src;              // weight (retrieve: W_0)
+    const void* m;                // retrieve: the slot of the superposition, rows x cols without padding
+    void* dst;
+    uint64_t stride;              // elements between rows of src
+    uint32_t rows, cols;
+    uint32_t slot, flip;
+    uint32_t vec;                 // bit 0: rows of src are 16-byte aligned; bit 1: rows of m
+    uint32_t first_cta;           // set by the launcher
+};
+struct Pack8Args {
+    Pack8Matrix mat[kPackBatch];
+    uint32_t n;
+    float lambda;
+    DevTask task;
+};
+struct Unpack8Matrix {
+    const void* src;
+    void* dst;
+    uint64_t stride;
+    uint32_t rows, cols;
+    uint32_t vec;                 // rows of dst are 16-byte aligned
+    uint32_t first_cta;
+};
+struct Unpack8Args {
+    Unpack8Matrix mat[kPackBatch];
+    uint32_t n;
+};
+struct Turn8Args {
+    const void* src;              // [rows, cols] fp32 or bf16, or a matrix in eight bits
+    void* dst;                    // the same rows in eight bits, or NULL
+    void* turned;                 // [cols, rows] in eight bits
+    uint64_t stride;
+    uint32_t rows, cols, vec;
+};
+int launch_pack8(int w_dtype, int m_dtype, bool retrieve, Pack8Args& a, void* stream);
+int launch_unpack8(int out_dtype, Unpack8Args& a, void* stream);
+int launch_turn8(int src_dtype, const Turn8Args& a, void* stream);       // src_dtype -1: eight bits
+
+// randes_linear8.cu: products of two matrices in eight bits
+struct Linear8Args {
+    const void* w;                // [rows, cols] in eight bits
+    const void* x;                // [n_tokens, cols] in eight bits
+    void* y;
+    uint64_t y_stride;
+    uint32_t rows, cols, n_tokens;
+    uint32_t y_bf16;
+    uint32_t log_ranks;           // set by the launcher: CTAs of a cluster that share a tile's columns
+};
+int launch_linear8(Linear8Args& a, int sm_count, int device, void* stream);
+int linear8_giveups(unsigned int* count);
+
+// randes_norm.cu: root-mean-square norm with the residual's addition, and its gradient
+struct NormArgs {
+    const void* x;
+    const void* residual;         // or NULL
+    const void* gain;             // or NULL; fp32 or bf16
+    void* h;                      // x + residual, or NULL
+    void* y;                      // the activations' type, or NULL
+    void* y8;                     // eight bits, or NULL
+    void* kept8;                  // h in eight bits, or NULL
+    float* rstd;                  // or NULL
+    uint64_t x_stride, residual_stride, h_stride, y_stride;
+    uint32_t rows, cols;
+    uint32_t vec;                 // rows of x, residual, h and y are 16-byte aligned
+    uint32_t gain_bf16;
+    float eps;
+};
+struct NormGradArgs {
+    const void* dy;
+    const void* h;                // the activations' type, or NULL
+    const void* kept8;            // in its place, eight bits
+    const float* rstd;
+    const void* gain;             // or NULL; fp32 or bf16
+    const void* dh;               // or NULL
+    void* dx;
+    float* dgain;                 // or NULL
+    float* partial;               // [ctas][cols], in the caller's workspace
+    uint64_t dy_stride, h_stride, dh_stride, dx_stride;
+    uint32_t rows, cols, vec, gain_bf16;
+};
+constexpr uint32_t kNormMaxCols = 32768;
+int launch_norm(int dtype, const NormArgs& a, void* stream);
+size_t norm_grad_workspace(uint32_t rows, uint32_t cols);
+int launch_norm_grad(int dtype, const NormGradArgs& a, int* launched, void* stream);
+
 // randes_scores.cu: log probabilities, entropy and top alternatives of logits, and their gradient.
 constexpr uint32_t kMaxTop = 64;
 struct ScoreArgs {

@@ -66,6 +66,22 @@ class Matrix(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_uint32), ("cols", ctypes.c_uint32), ("stride", ctypes.c_uint64)]
 
 
+class RmsNorm(ctypes.Structure):
+    """randes_rms_norm_t"""
+
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("x", "residual", "gain", "h", "y", "y8", "kept8", "rstd")]
+                + [(n, ctypes.c_uint64) for n in ("x_stride", "residual_stride", "h_stride", "y_stride")]
+                + [("rows", ctypes.c_uint32), ("cols", ctypes.c_uint32), ("dtype", ctypes.c_int), ("gain_dtype", ctypes.c_int), ("eps", ctypes.c_float)])
+
+
+class RmsNormBackward(ctypes.Structure):
+    """randes_rms_norm_backward_t"""
+
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("dy", "h", "kept8", "rstd", "gain", "dh", "dx", "dgain")]
+                + [(n, ctypes.c_uint64) for n in ("dy_stride", "h_stride", "dh_stride", "dx_stride")]
+                + [("rows", ctypes.c_uint32), ("cols", ctypes.c_uint32), ("dtype", ctypes.c_int), ("gain_dtype", ctypes.c_int)])
+
+
 def lib():
     """The loaded shared library; raises if it has not been built."""
     global _lib
@@ -154,6 +170,26 @@ def lib():
         L.randes_token_scores.restype = ctypes.c_int
         L.randes_token_scores_backward.argtypes = [vp, dt, u32, u32, u64, vp, f32, vp, vp, vp, vp, vp, u64, vp]
         L.randes_token_scores_backward.restype = ctypes.c_int
+        L.randes_packed_eight_bytes.argtypes = [u32, u32]
+        L.randes_packed_eight_bytes.restype = sz
+        L.randes_pack_eight.argtypes = [vp, u32, dt, vp, vp]
+        L.randes_pack_eight.restype = ctypes.c_int
+        L.randes_unpack_eight.argtypes = [vp, u32, vp, dt, vp]
+        L.randes_unpack_eight.restype = ctypes.c_int
+        L.randes_pack_eight_transposed.argtypes = [vp, dt, vp, vp, vp]
+        L.randes_pack_eight_transposed.restype = ctypes.c_int
+        L.randes_transpose_eight.argtypes = [vp, u32, u32, vp, vp]
+        L.randes_transpose_eight.restype = ctypes.c_int
+        L.randes_retrieve_packed_eight.argtypes = [vp, u32, f32, vp, u32, vp, vp, vp, vp]
+        L.randes_retrieve_packed_eight.restype = ctypes.c_int
+        L.randes_packed_eight_linear.argtypes = [vp, u32, u32, vp, u32, vp, dt, u64, vp]
+        L.randes_packed_eight_linear.restype = ctypes.c_int
+        L.randes_rms_norm.argtypes = [vp, vp]
+        L.randes_rms_norm.restype = ctypes.c_int
+        L.randes_rms_norm_backward_workspace.argtypes = [u32, u32]
+        L.randes_rms_norm_backward_workspace.restype = sz
+        L.randes_rms_norm_backward.argtypes = [vp, vp, sz, vp]
+        L.randes_rms_norm_backward.restype = ctypes.c_int
         L.randes_launch_count.argtypes = []
         L.randes_launch_count.restype = u64
         L.randes_last_error.argtypes = []
@@ -169,6 +205,8 @@ EXPORTS = [
     "randes_retrieve", "randes_delta_gram_scratch_bytes", "randes_delta_gram", "randes_interference_norm", "randes_pairwise_cosines", "randes_retrieve_batch", "randes_retrieve_static", "randes_linear", "randes_linear_gated", "randes_linear_giveups", "randes_launch_count", "randes_last_error",
     "randes_packed_bytes", "randes_pack", "randes_unpack", "randes_retrieve_packed", "randes_packed_linear_workspace", "randes_packed_linear", "randes_packed_linear_tasks",
     "randes_token_scores", "randes_token_scores_backward",
+    "randes_packed_eight_bytes", "randes_pack_eight", "randes_unpack_eight", "randes_pack_eight_transposed", "randes_transpose_eight", "randes_retrieve_packed_eight",
+    "randes_packed_eight_linear", "randes_rms_norm", "randes_rms_norm_backward_workspace", "randes_rms_norm_backward",
 ]
 
 
@@ -382,6 +420,52 @@ def randes_token_scores_backward(logits, dtype, n_rows, vocab, stride, targets, 
 
 def randes_launch_count() -> int:
     return int(lib().randes_launch_count())
+
+
+def randes_packed_eight_bytes(rows: int, cols: int) -> int:
+    """Bytes of a [rows, cols] matrix in eight bits with a scale per 128 columns (0 on bad arguments)."""
+    return int(lib().randes_packed_eight_bytes(rows, cols))
+
+
+def randes_pack_eight(matrices, n: int, dtype: int, packed, stream) -> None:
+    """Eight-bit form of `n` matrices (a ctypes array of Matrix) in the buffers whose addresses `packed` holds."""
+    _check(lib().randes_pack_eight(_addr(matrices), n, dtype, _addr(packed), stream))
+
+
+def randes_unpack_eight(packed, n: int, matrices, out_dtype: int, stream) -> None:
+    _check(lib().randes_unpack_eight(_addr(packed), n, _addr(matrices), out_dtype, stream))
+
+
+def randes_pack_eight_transposed(matrix, dtype: int, packed, transposed, stream) -> None:
+    """Eight-bit form of a matrix's transpose, and with `packed` of the matrix itself."""
+    _check(lib().randes_pack_eight_transposed(_addr(matrix), dtype, _addr(packed), _addr(transposed), stream))
+
+
+def randes_transpose_eight(packed, rows: int, cols: int, transposed, stream) -> None:
+    _check(lib().randes_transpose_eight(_addr(packed), rows, cols, _addr(transposed), stream))
+
+
+def randes_retrieve_packed_eight(plan, task_id, lam, layers, n, base, M, packed, stream) -> None:
+    """Eight-bit form of the retrieved weight of the `n` named layers, its own type never stored."""
+    _check(lib().randes_retrieve_packed_eight(plan, task_id, lam, _addr(layers), n, _addr(base), _addr(M), _addr(packed), stream))
+
+
+def randes_packed_eight_linear(w, rows, cols, x, n_tokens, y, y_dtype, y_stride, stream) -> None:
+    """y = x W^T of two matrices in eight bits."""
+    _check(lib().randes_packed_eight_linear(_addr(w), rows, cols, _addr(x), n_tokens, _addr(y), y_dtype, y_stride, stream))
+
+
+def randes_rms_norm(norm: RmsNorm, stream) -> None:
+    _check(lib().randes_rms_norm(ctypes.addressof(norm), stream))
+
+
+def randes_rms_norm_backward_workspace(rows: int, cols: int) -> int:
+    """Bytes of device workspace the call below needs for the gradient of the gain."""
+    return int(lib().randes_rms_norm_backward_workspace(rows, cols))
+
+
+def randes_rms_norm_backward(grad: RmsNormBackward, workspace, workspace_bytes: int, stream) -> None:
+    _check(lib().randes_rms_norm_backward(ctypes.addressof(grad), _addr(workspace), workspace_bytes, stream))
 
 
 def ptr_array(tensors: Sequence) -> ctypes.Array:
@@ -671,6 +755,222 @@ def token_scores_backward(logits, targets, scores: TokenScores, g_logprob=None, 
     return out
 
 
+# ---- eight bits, their products and the norm on torch tensors -----------------------------------
+@functools.lru_cache(maxsize=4096)
+def _packed8_size(rows: int, cols: int) -> int:
+    nbytes = randes_packed_eight_bytes(rows, cols)
+    if nbytes == 0 and rows * cols != 0:
+        _refuse("a matrix of [%d, %d] cannot be packed" % (rows, cols))
+    return nbytes
+
+
+class Packed8Matrix:
+    """A [rows, cols] weight or activation in eight bits with a scale per 128 columns (see include/randes.h): one device buffer."""
+
+    __slots__ = ("rows", "cols", "data", "address", "device")
+
+    def __init__(self, rows: int, cols: int, data):
+        """Around a buffer that holds such a matrix: `data` of a Packed8Matrix of the same shape, or a copy of it."""
+        need, have = _packed8_size(rows, cols), data.numel() * data.element_size()
+        if not data.is_cuda or not data.is_contiguous() or have < need:
+            _refuse("an eight-bit [%d, %d] matrix is a contiguous CUDA tensor of %d bytes, not one of %d on %s" % (rows, cols, need, have, data.device))
+        if data.data_ptr() % 16:
+            raise RandesError(MISALIGNED, "the buffer of an eight-bit matrix starts on a 16-byte boundary")
+        self._hold(rows, cols, data)
+
+    def _hold(self, rows: int, cols: int, data):
+        self.rows, self.cols, self.data = rows, cols, data
+        self.address, self.device = data.data_ptr(), data.device
+
+    @property
+    def nbytes(self) -> int:
+        return self.data.numel() * self.data.element_size()
+
+    def unpack(self, out_dtype: int = F32, out=None):
+        """The [rows, cols] values that the eight bits stand for."""
+        import torch
+
+        rows, cols = self.rows, self.cols
+        if out is None:
+            out = torch.empty(rows, cols, dtype=torch.bfloat16 if out_dtype == BF16 else torch.float32, device=self.device)
+            stride = cols
+        else:
+            out_dtype, r, c, stride = _rows_of(out, "out")
+            if (r, c) != (rows, cols) or out.device != self.device:
+                _refuse("out is [%d, %d] on %s, the matrix [%d, %d] on %s" % (r, c, out.device, rows, cols, self.device))
+        _call(self.device, lib().randes_unpack_eight, _PtrOne(self.address), 1, _MatrixOne((out.data_ptr(), rows, cols, stride)), out_dtype)
+        return out
+
+
+def _new_packed8(rows: int, cols: int, device) -> Packed8Matrix:
+    import torch
+
+    p = Packed8Matrix.__new__(Packed8Matrix)      # (the size is right)
+    p._hold(rows, cols, torch.empty(_packed8_size(rows, cols), dtype=_torch.uint8, device=device))
+    return p
+
+
+def pack8(weights):
+    """Eight-bit form of a matrix, or of a list of matrices of one type (2-D CUDA tensors, fp32 or bf16; rows may be strided)."""
+    if not isinstance(weights, (list, tuple)):
+        dtype, rows, cols, stride = _rows_of(weights, "the matrix")
+        p = _new_packed8(rows, cols, weights.device)
+        _call(p.device, lib().randes_pack_eight, _MatrixOne((weights.data_ptr(), rows, cols, stride)), 1, dtype, _PtrOne(p.address))
+        return p
+    if not weights:
+        return []
+    device, n = weights[0].device, len(weights)
+    shapes = [_rows_of(w, "a matrix") for w in weights]
+    if len({s[0] for s in shapes}) != 1 or any(w.device != device for w in weights):
+        _refuse("the matrices of one call have one type and one device")
+    made = [_new_packed8(r, c, device) for _, r, c, _ in shapes]
+    mats = (Matrix * n)(*[(w.data_ptr(), r, c, s) for w, (_, r, c, s) in zip(weights, shapes)])
+    _call(device, lib().randes_pack_eight, mats, n, shapes[0][0], (ctypes.c_void_p * n)(*[p.address for p in made]))
+    return made
+
+
+def _turned(x, both: bool):
+    dtype, rows, cols, stride = _rows_of(x, "the matrix")
+    device = x.device
+    p, t = _new_packed8(rows, cols, device) if both else None, _new_packed8(cols, rows, device)
+    _call(device, lib().randes_pack_eight_transposed, _MatrixOne((x.data_ptr(), rows, cols, stride)), dtype, p.address if both else None, t.address)
+    return p, t
+
+
+def pack8_transposed(x) -> Packed8Matrix:
+    """Eight-bit form of the transpose, in blocks along the rows of `x`: a 2-D CUDA tensor, or a Packed8Matrix (an activation kept
+    for the backward pass)."""
+    if not isinstance(x, Packed8Matrix):
+        return _turned(x, False)[1]
+    t = _new_packed8(x.cols, x.rows, x.device)
+    _call(x.device, lib().randes_transpose_eight, x.address, x.rows, x.cols, t.address)
+    return t
+
+
+def pack8_both(x):
+    """(eight-bit form of `x`, that of its transpose) out of one read: what the two products of a backward pass take."""
+    return _turned(x, True)
+
+
+def packed8_linear(x, w: Packed8Matrix, y=None, y_dtype: int = F32):
+    """x: [n_tokens, cols] Packed8Matrix, or an fp32 or bf16 CUDA tensor, which is packed first; returns y = x W^T [n_tokens, rows]."""
+    if not isinstance(w, Packed8Matrix):
+        _refuse("w is no Packed8Matrix")
+    if not isinstance(x, Packed8Matrix):
+        x = pack8(x)
+    n, rows, cols, device = x.rows, w.rows, w.cols, w.device
+    if x.cols != cols:
+        _refuse("x has %d columns, the weight %d" % (x.cols, cols))
+    if x.device != device:
+        _refuse("x is on %s, the weight on %s" % (x.device, device))
+    if y is None:
+        y, y_stride = _torch.empty(n, rows, dtype=_torch.bfloat16 if y_dtype == BF16 else _torch.float32, device=device), rows
+    else:
+        y_dtype, yn, yr, y_stride = _rows_of(y, "y")
+        if (yn, yr) != (n, rows) or y.device != device:
+            _refuse("y is [%d, %d] on %s, [%d, %d] on %s is wanted" % (yn, yr, y.device, n, rows, device))
+    _call(device, lib().randes_packed_eight_linear, w.address, rows, cols, x.address, n, y.data_ptr(), y_dtype, y_stride)
+    return y
+
+
+class Normed(NamedTuple):
+    """What rms_norm returns: the norm's output (a tensor, or a Packed8Matrix), the new residual (x itself without a residual), one
+    over the root mean square of every row [n] fp32, and the new residual in eight bits, if it was asked for."""
+
+    y: Any
+    h: Any
+    rstd: Any
+    kept: Any
+
+
+def _like_rows(t, what: str, dtype: int, n: int, cols: int, device):
+    """(address, row stride) of a tensor that has to match the activations."""
+    code, r, c, stride = _rows_of(t, what)
+    if (code, r, c) != (dtype, n, cols) or t.device != device:
+        _refuse("%s must have the activations' shape, type and device" % what)
+    return t.data_ptr(), stride
+
+
+def _gain(gain, cols: int, device):
+    if gain is None:
+        return None, F32
+    code = BF16 if gain.dtype is _torch.bfloat16 else F32
+    if (code == F32 and gain.dtype is not _torch.float32) or gain.shape != (cols,) or not gain.is_contiguous() or gain.device != device:
+        _refuse("gain must be a contiguous float32 or bfloat16 tensor [%d] on %s" % (cols, device))
+    return gain.data_ptr(), code
+
+
+def rms_norm(x, gain=None, residual=None, eps: float = 1e-6, packed: bool = False, checkpoint: bool = False, h=None, y=None) -> Normed:
+    """h = x + residual, y = h / sqrt(mean(h^2) + eps) * gain for every row (see include/randes.h).
+
+    x, residual: [n, cols] fp32 or bf16 CUDA tensors (rows may be strided); gain: fp32 or bf16 [cols].  ``packed``: y in eight
+    bits; ``checkpoint``: h in eight bits too, which rms_norm_backward takes in h's place.  ``h``, ``y``: where to write (h may be x
+    or the residual itself)."""
+    dtype, n, cols, x_stride = _rows_of(x, "x")
+    device = x.device
+    a = RmsNorm(x=x.data_ptr(), x_stride=x_stride, rows=n, cols=cols, dtype=dtype, eps=eps)
+    a.gain, a.gain_dtype = _gain(gain, cols, device)
+    if residual is not None:
+        a.residual, a.residual_stride = _like_rows(residual, "residual", dtype, n, cols, device)
+        if h is None:
+            h = _torch.empty(n, cols, dtype=x.dtype, device=device)
+    if h is not None:
+        a.h, a.h_stride = _like_rows(h, "h", dtype, n, cols, device)
+    if packed:
+        if y is not None:
+            _refuse("y is a tensor to write, packed asks for eight bits")
+        y = _new_packed8(n, cols, device)
+        a.y8 = y.address
+    else:
+        if y is None:
+            y = _torch.empty(n, cols, dtype=x.dtype, device=device)
+        a.y, a.y_stride = _like_rows(y, "y", dtype, n, cols, device)
+    kept = _new_packed8(n, cols, device) if checkpoint else None
+    if checkpoint:
+        a.kept8 = kept.address
+    rstd = _torch.empty(n, dtype=_torch.float32, device=device)
+    a.rstd = rstd.data_ptr()
+    _call(device, lib().randes_rms_norm, ctypes.addressof(a))
+    return Normed(y, x if h is None else h, rstd, kept)
+
+
+_norm_workspace_bytes = functools.lru_cache(maxsize=4096)(randes_rms_norm_backward_workspace)
+
+
+def rms_norm_backward(dy, h, rstd, gain=None, dh=None, out=None):
+    """(gradient of x and of the residual alike, gradient of the gain fp32 [cols], None without a gain) of rms_norm.
+
+    ``h``: the new residual, or its checkpoint (a Packed8Matrix); ``dh``: the gradient that reaches h past the norm; ``out`` may
+    be dy, h or dh itself."""
+    dtype, n, cols, dy_stride = _rows_of(dy, "dy")
+    device = dy.device
+    a = RmsNormBackward(dy=dy.data_ptr(), dy_stride=dy_stride, rows=n, cols=cols, dtype=dtype)
+    if isinstance(h, Packed8Matrix):
+        if (h.rows, h.cols) != (n, cols) or h.device != device:
+            _refuse("the checkpoint is [%d, %d] on %s, dy [%d, %d] on %s" % (h.rows, h.cols, h.device, n, cols, device))
+        a.kept8 = h.address
+    else:
+        a.h, a.h_stride = _like_rows(h, "h", dtype, n, cols, device)
+    if rstd.dtype is not _torch.float32 or rstd.shape != (n,) or not rstd.is_contiguous() or rstd.device != device:
+        _refuse("rstd must be a contiguous float32 tensor [%d] on %s" % (n, device))
+    a.rstd = rstd.data_ptr()
+    a.gain, a.gain_dtype = _gain(gain, cols, device)
+    if dh is not None:
+        a.dh, a.dh_stride = _like_rows(dh, "dh", dtype, n, cols, device)
+    if out is None:
+        out = _torch.empty(n, cols, dtype=dy.dtype, device=device)
+    a.dx, a.dx_stride = _like_rows(out, "out", dtype, n, cols, device)
+    dgain = workspace = None
+    nbytes = 0
+    if gain is not None:
+        dgain = _torch.empty(cols, dtype=_torch.float32, device=device)
+        a.dgain = dgain.data_ptr()
+        nbytes = _norm_workspace_bytes(n, cols)
+        workspace = _torch.empty(nbytes, dtype=_torch.uint8, device=device)
+    _call(device, lib().randes_rms_norm_backward, ctypes.addressof(a), workspace.data_ptr() if nbytes else None, nbytes)
+    return out, dgain
+
+
 # ---- convenience object over torch tensors --------------------------------------------------
 class Plan:
     """A plan plus the device workspace it lives in.
@@ -899,6 +1199,20 @@ class Plan:
         weights = self._weights(base, layers, device)
         made = [_new_packed(self.rows[l], self.cols[l], group, device) for l in layers]
         _call(device, lib().randes_retrieve_packed, self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, weights, m, group,
+              (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]))
+        return made
+
+    def retrieve_packed8(self, task_id: int, lam: float, base, M, layers=None):
+        """Eight-bit form of one retrieved model, its own type never stored; a list, one entry per named layer (default: all).
+
+        ``base`` is the list of all layers' weights, dense and in the plan's type; only the named ones are read."""
+        m = self._arena(M)
+        device = M.device
+        layers = list(range(self.n_layers)) if layers is None else [self._layer(l) for l in layers]
+        n = len(layers)
+        weights = self._weights(base, layers, device)
+        made = [_new_packed8(self.rows[l], self.cols[l], device) for l in layers]
+        _call(device, lib().randes_retrieve_packed_eight, self.handle, task_id, lam, (ctypes.c_uint32 * max(n, 1))(*layers), n, weights, m,
               (ctypes.c_void_p * max(n, 1))(*[p.address for p in made]))
         return made
 
