@@ -8,6 +8,7 @@
 // w is operand A (128 rows: tensor memory lanes), x operand B (16 to 128 tokens: columns): few tokens waste nothing, and a warp of
 // the epilogue writes 32 neighbouring outputs of a token whatever the row's alignment.
 #include <cooperative_groups.h>
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -52,6 +53,52 @@ __device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint64_t desc)
 {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
+// The same for a pair of CTAs: one product of 256 rows, each CTA holding half of either operand and the sums of its own 128 rows.
+__device__ __forceinline__ void pair_mma8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void pair_copy_scales(uint32_t tmem, uint64_t desc)
+{
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+// arrives at the same barrier of both CTAs once the products so far are done
+__device__ __forceinline__ void pair_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
+}
+// a box of the map into this CTA's shared memory, counted by the barrier of either CTA of the pair
+__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, uint32_t row)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(0), "r"(row) : "memory");
+}
+__device__ __forceinline__ uint32_t of_rank(uint32_t saddr, uint32_t rank)      // the other CTA's copy of a shared address
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void tc_load32(uint32_t t, uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(t)
+        : "memory");
+}
 __device__ __forceinline__ void tc_load16(uint32_t t, uint32_t (&v)[16])
 {
     asm volatile(
@@ -74,22 +121,66 @@ __device__ __forceinline__ uint64_t scales_desc(uint32_t saddr)
     return static_cast<uint64_t>((saddr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46);
 }
 
-// A wait that ends: when it runs out, or when another role of the CTA has given up, it says so.
+// One lane of a converged warp. What only it does is issued with operands that are the same for the warp; a loop that one lane runs
+// by itself takes some 60 cycles to issue a product, and then issuing, not the tensor core, is what a product of 2^13 rows waits for.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// A wait that ends, for a converged warp; when it runs out it says so.
 __device__ __forceinline__ bool wait8(uint32_t bar, uint32_t parity, volatile uint32_t* aborted)
 {
-    for (uint32_t i = 0; i < kWaitLimit; ++i) {
-        if (bar_try(bar, parity)) return true;
-        if ((i & 15u) == 15u && *aborted) return false;
-    }
-    if (atomicExch(const_cast<uint32_t*>(aborted), 1u) == 0u) atomicAdd(&g_linear8_giveups, 1u);
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
+        "mov.u32 n, %3;\n\t"
+        "AGAIN:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\t"
+        "setp.ne.u32 q, n, 0;\n\t"
+        "@q bra AGAIN;\n\t"
+        "DONE:\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "n"(kWaitLimit) : "memory");
+    if (__all_sync(~0u, ok)) return true;
+    if (elected() && atomicExch(const_cast<uint32_t*>(aborted), 1u) == 0u) atomicAdd(&g_linear8_giveups, 1u);
+    __syncwarp();
     return false;
 }
+// Where a role stands in the ring of S stages: the stage and the parity of its round.
+template <uint32_t S> struct Ring {
+    uint32_t s = 0, round = 0;
+    __device__ __forceinline__ void step()
+    {
+        if (++s == S) { s = 0; round ^= 1u; }
+    }
+};
 
-__device__ __forceinline__ void store_y(const Linear8Args& a, uint32_t token, uint32_t row, float v)
+__device__ __forceinline__ void store_y(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_y(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
+// One row's sums of N neighbouring tokens, of which n exist: a warp writes 32 neighbouring outputs of a token at a time.
+// (No branch between the stores: with one per output this took three times as long.)
+template <int N, typename T> __device__ __forceinline__ void store_tokens(const Linear8Args& a, uint32_t token, uint32_t n, uint32_t row, const uint32_t (&v)[N])
 {
-    const size_t at = static_cast<size_t>(token) * a.y_stride + row;
-    if (a.y_bf16) static_cast<bf16*>(a.y)[at] = __float2bfloat16_rn(v);
-    else static_cast<float*>(a.y)[at] = v;
+    if (row >= a.rows) return;
+    T* p = static_cast<T*>(a.y) + static_cast<size_t>(token) * a.y_stride + row;
+    if (n >= N) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) store_y(p + j * a.y_stride, __uint_as_float(v[j]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N - 1; ++j)
+            if (j < n) store_y(p + j * a.y_stride, __uint_as_float(v[j]));
+    }
+}
+template <int N> __device__ __forceinline__ void store_tokens(const Linear8Args& a, uint32_t token, uint32_t row, const uint32_t (&v)[N])
+{
+    if (token >= a.n_tokens) return;
+    if (a.y_bf16) store_tokens<N, bf16>(a, token, a.n_tokens - token, row, v);
+    else store_tokens<N, float>(a, token, a.n_tokens - token, row, v);
 }
 
 // N tokens to a tile.
@@ -100,7 +191,7 @@ template <int N> struct Geom8 {
     static constexpr uint32_t kTmem = 2 * N + 16 <= 64 ? 64 : (2 * N + 16 <= 128 ? 128 : (2 * N + 16 <= 256 ? 256 : 512));
     // instruction descriptor: e4m3 both, fp32 sums, scales as exponents; bits 4-5 and 29-30 will say which byte of the scale words of B and A
     static constexpr uint32_t kIdesc = (N >> 3 << 17) | (1u << 23) | (128 >> 4 << 24);
-    static constexpr uint32_t kBars = 2 * kStages + 7;                  // full, empty; scales free, sums full, sums free (two each); drained
+    static constexpr uint32_t kBars = 2 * kStages + 5;                  // full, empty; sums full, sums free (two each); drained
     static constexpr size_t kSmem = 1024 + static_cast<size_t>(kStages) * kStage + 8 * kBars + 16;
     static_assert(kStage % 1024 == 0 && 8 * kBars + 16 <= 512, "stages on the swizzle's boundary");
 };
@@ -116,10 +207,9 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
     const uint32_t bars = base + S * G::kStage;
     auto full = [&](uint32_t s) { return bars + 8 * s; };
     auto empty = [&](uint32_t s) { return bars + 8 * (S + s); };
-    auto scales_free = [&](uint32_t b) { return bars + 8 * (2 * S + b); };
-    auto sums_full = [&](uint32_t b) { return bars + 8 * (2 * S + 2 + b); };
-    auto sums_free = [&](uint32_t b) { return bars + 8 * (2 * S + 4 + b); };
-    const uint32_t drained = bars + 8 * (2 * S + 6);
+    auto sums_full = [&](uint32_t b) { return bars + 8 * (2 * S + b); };
+    auto sums_free = [&](uint32_t b) { return bars + 8 * (2 * S + 2 + b); };
+    const uint32_t drained = bars + 8 * (2 * S + 4);
     volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(gen + S * G::kStage + 8 * G::kBars);      // tensor memory's address, give-up flag
     volatile uint32_t* aborted = words + 1;
 
@@ -133,7 +223,7 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < S; ++s) { bar_init(full(s)); bar_init(empty(s)); }
-        for (uint32_t b = 0; b < 2; ++b) { bar_init(scales_free(b)); bar_init(sums_full(b)); bar_init_n(sums_free(b), 128); }
+        for (uint32_t b = 0; b < 2; ++b) { bar_init(sums_full(b)); bar_init_n(sums_free(b), 128); }
         bar_init(drained);
         *aborted = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -148,61 +238,69 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
     const uint32_t tmem = words[0];
 
     if (warp == 0) {
-        if (lane == 0) {
-            const char *w = static_cast<const char*>(a.w), *x = static_cast<const char*>(a.x);
-            uint32_t it = 0;
-            bool ok = true;
-            for (uint32_t tile = tile0; ok && tile < tiles; tile += tile_step) {
-                const uint32_t rt = tile / token_tiles, n0 = (tile - rt * token_tiles) * N, xt = n0 >> 7;
-                for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
-                    const uint32_t s = it % S, st = base + s * G::kStage;
-                    if (!(ok = wait8(empty(s), (it / S & 1u) ^ 1u, aborted))) break;
-                    const bool first = kb == k0 || (kb & 3u) == 0;
-                    bar_expect(full(s), kTile + N * 128 + (first ? 2 * kScales : 0));
-                    bulk_copy(st, w + lw.tile(rt, kb), kTile, full(s));
-                    bulk_copy(st + kTile, x + lx.tile(xt, kb) + (n0 & 127) * 128, N * 128, full(s));
+        const char *w = static_cast<const char*>(a.w), *x = static_cast<const char*>(a.x);
+        Ring<S> at;
+        uint32_t issued = 0;
+        bool ok = true;
+        for (uint32_t tile = tile0; ok && tile < tiles; tile += tile_step) {
+            const uint32_t rt = tile / token_tiles, n0 = (tile - rt * token_tiles) * N, xt = n0 >> 7;
+            for (uint32_t kb = k0; kb < k1; ++kb, at.step(), ++issued) {
+                const uint32_t st = base + at.s * G::kStage, bar = full(at.s);
+                if (!(ok = wait8(empty(at.s), at.round ^ 1u, aborted))) break;
+                const bool first = kb == k0 || (kb & 3u) == 0;
+                if (elected()) {
+                    bar_expect(bar, kTile + N * 128 + (first ? 2 * kScales : 0));
+                    bulk_copy(st, w + lw.tile(rt, kb), kTile, bar);
+                    bulk_copy(st + kTile, x + lx.tile(xt, kb) + (n0 & 127) * 128, N * 128, bar);
                     if (first) {
-                        bulk_copy(st + kTile + N * 128, w + lw.scales(rt, kb >> 2), kScales, full(s));
-                        bulk_copy(st + kTile + N * 128 + kScales, x + lx.scales(xt, kb >> 2), kScales, full(s));
+                        bulk_copy(st + kTile + N * 128, w + lw.scales(rt, kb >> 2), kScales, bar);
+                        bulk_copy(st + kTile + N * 128 + kScales, x + lx.scales(xt, kb >> 2), kScales, bar);
                     }
                 }
+                __syncwarp();
             }
-            if (*aborted)      // what is under way has to land before the CTA's shared memory is released
-                for (uint32_t i = it > S ? it - S : 0; i < it; ++i) bar_wait(full(i % S), i / S & 1u);
         }
+        if (!ok)      // what is under way has to land before the CTA's shared memory is released
+            for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) bar_wait(full(i % S), i / S & 1u);
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            uint32_t it = 0, group = 0, turn = 0;
-            bool ok = true;
-            for (uint32_t tile = tile0; ok && tile < tiles; tile += tile_step, ++turn) {
-                const uint32_t acc = tmem + (turn & 1u) * N;
-                if (!(ok = wait8(sums_free(turn & 1u), (turn >> 1 & 1u) ^ 1u, aborted))) break;
+        Ring<S> at;
+        uint32_t turn = 0, set = 0, last_stage[2] = {}, last_round[2] = {}, used = 0;      // of either set of scales: where its last product stood
+        bool ok = true;
+        for (uint32_t tile = tile0; ok && tile < tiles; tile += tile_step, ++turn) {
+            const uint32_t acc = tmem + (turn & 1u) * N;
+            if (!(ok = wait8(sums_free(turn & 1u), (turn >> 1 & 1u) ^ 1u, aborted))) break;
+            tc_after();
+            for (uint32_t kb = k0; kb < k1; ++kb, at.step()) {
+                const uint32_t st = base + at.s * G::kStage;
+                if (!(ok = wait8(full(at.s), at.round, aborted))) break;
                 tc_after();
-                for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
-                    const uint32_t s = it % S, st = base + s * G::kStage;
-                    if (!(ok = wait8(full(s), it / S & 1u, aborted))) break;
-                    tc_after();
-                    if (kb == k0 || (kb & 3u) == 0) {
-                        ++group;      // of scales; the set is free once the products of the group before last are done
-                        if (!(ok = wait8(scales_free(group & 1u), (group >> 1 & 1u) ^ (group & 1u), aborted))) break;
-                        const uint32_t to = tmem + G::kScaleCols + (group & 1u) * 8;
-                        tc_copy_scales(to, scales_desc(st + kTile + N * 128));
-                        tc_copy_scales(to + 4, scales_desc(st + kTile + N * 128 + kScales));
+                const bool first = kb == k0 || (kb & 3u) == 0;
+                if (first) {      // the other set, once the products that used it are done
+                    set ^= 1u;
+                    if (used >> set & 1u && !(ok = wait8(empty(set ? last_stage[1] : last_stage[0]), set ? last_round[1] : last_round[0], aborted))) break;
+                    used |= 1u << set;
+                }
+                const uint32_t sa = tmem + G::kScaleCols + set * 8, id = (kb & 3u) << 29 | (kb & 3u) << 4 | G::kIdesc;
+                const uint64_t da = operand_desc(st), db = operand_desc(st + kTile);
+                if (elected()) {
+                    if (first) {
+                        tc_copy_scales(sa, scales_desc(st + kTile + N * 128));
+                        tc_copy_scales(sa + 4, scales_desc(st + kTile + N * 128 + kScales));
                     }
-                    const uint32_t sa = tmem + G::kScaleCols + (group & 1u) * 8, id = (kb & 3u) << 29 | (kb & 3u) << 4 | G::kIdesc;
-                    const uint64_t da = operand_desc(st), db = operand_desc(st + kTile);
 #pragma unroll
                     for (uint32_t k = 0; k < 4; ++k) tc_mma8(acc, da + 2 * k, db + 2 * k, id, sa, sa + 4, kb > k0 || k ? 1u : 0u);
-                    tc_commit(empty(s));
-                    if ((kb & 3u) == 3u || kb + 1 == k1) tc_commit(scales_free(group & 1u));
+                    tc_commit(empty(at.s));
+                    if (kb + 1 == k1) tc_commit(sums_full(turn & 1u));
                 }
-                if (ok) tc_commit(sums_full(turn & 1u));
+                __syncwarp();
+                if (set) { last_stage[1] = at.s; last_round[1] = at.round; }
+                else { last_stage[0] = at.s; last_round[0] = at.round; }
             }
-            if (!ok) {
-                tc_commit(drained);
-                bar_wait(drained, 0);
-            }
+        }
+        if (!ok) {
+            if (elected()) tc_commit(drained);
+            bar_wait(drained, 0);
         }
         __syncwarp();
     } else {
@@ -212,7 +310,6 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
         for (uint32_t tile = tile0; tile < tiles; tile += tile_step, ++turn) {
             const uint32_t rt = tile / token_tiles, n0 = (tile - rt * token_tiles) * N, row = rt * 128 + quarter * 32 + lane;
             ok = ok && wait8(sums_full(turn & 1u), turn >> 1 & 1u, aborted);
-            ok = __all_sync(~0u, ok);
             tc_after();
 #pragma unroll 1
             for (uint32_t j0 = 0; j0 < N; j0 += 16) {
@@ -229,9 +326,7 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
 #pragma unroll
                     for (int j = 0; j < 16; ++j) part[(j0 + j) * 128 + quarter * 32 + lane] = __uint_as_float(v[j]);
                 } else {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (n0 + j0 + j < a.n_tokens && row < a.rows) store_y(a, n0 + j0 + j, row, __uint_as_float(v[j]));
+                    store_tokens<16>(a, n0 + j0, row, v);
                 }
             }
             tc_before();
@@ -250,7 +345,8 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
             for (uint32_t j = rank; j < N && n0 + j < a.n_tokens; j += ranks) {
                 float y = 0.f;
                 for (uint32_t k = 0; k < ranks; ++k) y += cluster.map_shared_rank(part, k)[j * 128 + threadIdx.x];
-                store_y(a, n0 + j, row, bad ? __uint_as_float(0x7FFFFFFFu) : y);
+                const uint32_t one[1] = {bad ? 0x7FFFFFFFu : __float_as_uint(y)};
+                store_tokens<1>(a, n0 + j, row, one);
             }
         }
         cluster.sync();      // nobody leaves while its sums may still be read
@@ -260,6 +356,184 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
     if (warp == 1) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::kTmem) : "memory");
+    }
+}
+
+// Many tokens: pairs of CTAs, 256 rows x 256 tokens to a tile, so that a byte brought into shared memory feeds twice the products of
+// the form above. Either CTA copies its 128 rows of w and its 128 tokens of x; the first one issues the products, on both tensor
+// cores. Persistent, with two accumulators: of tensor memory's 512 columns scales take 24 and the accumulators overlap in the 24
+// that are missing, which are read first when a tile is done.
+struct Pair8 {
+    static constexpr uint32_t kStage = 2 * kTile, kScaleSlot = 3 * kScales;      // w and x; scales of w, and of both halves of x
+    static constexpr int kStages = 6;
+    static constexpr uint32_t kScaleSet = 12, kScaleCols = 512 - 2 * kScaleSet, kShift = kScaleCols - 256;      // columns; the second accumulator's first
+    static constexpr uint32_t kIdesc = (256 >> 3 << 17) | (1u << 23) | (256 >> 4 << 24);
+    static constexpr uint32_t kBarsAt = kStages * (kStage + kScaleSlot), kBars = 2 * kStages + 4;      // full, empty; sums full (two); next, drained
+    static constexpr int kThreads = 320;                                            // warps 2-9 results, half a tile's tokens to four of them
+    static constexpr size_t kSmem = 1024 + kBarsAt + 8 * kBars + 16;
+    static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
+};
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Pair8::kThreads, 1)
+linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
+                    const __grid_constant__ CUtensorMap map_xs, const Linear8Args a)
+{
+    typedef Pair8 G;
+    constexpr int S = G::kStages;
+    extern __shared__ unsigned char smem_raw[];
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t raw = static_cast<uint32_t>(__cvta_generic_to_shared(smem_raw)), base = (raw + 1023u) & ~1023u;
+    unsigned char* gen = smem_raw + (base - raw);
+    const uint32_t scales = base + S * G::kStage, bars = base + G::kBarsAt;
+    auto full = [&](uint32_t s) { return bars + 8 * s; };                       // of the first CTA: the copies of both
+    auto empty = [&](uint32_t s) { return bars + 8 * (S + s); };
+    auto sums_full = [&](uint32_t b) { return bars + 8 * (2 * S + b); };
+    const uint32_t next = bars + 8 * (2 * S + 2), drained = bars + 8 * (2 * S + 3);
+    volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(gen + G::kBarsAt + 8 * G::kBars);
+    volatile uint32_t* aborted = words + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster.block_rank();
+    const Packed8Layout lw(a.rows, a.cols), lx(a.n_tokens, a.cols);
+    const uint32_t n_kb = lw.col_blocks, row_pairs = (lw.row_tiles + 1) / 2, token_pairs = (lx.row_tiles + 1) / 2, tiles = row_pairs * token_pairs;
+    const uint32_t tile0 = blockIdx.x >> 1, tile_step = gridDim.x >> 1;
+    // bands of 8 pairs of row tiles: the CTAs that run at a time share what they read
+    auto place = [&](uint32_t tile, uint32_t& rp, uint32_t& tp) {
+        const uint32_t band = tile / (8 * token_pairs), left = tile - band * 8 * token_pairs, high = min(8u, row_pairs - band * 8);
+        tp = left / high;
+        rp = band * 8 + left - tp * high;
+    };
+
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < S; ++s) { bar_init(full(s)); bar_init(empty(s)); }
+        for (uint32_t b = 0; b < 2; ++b) bar_init(sums_full(b));
+        bar_init_n(next, 16);
+        bar_init(drained);
+        *aborted = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(bars + 8 * G::kBars) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    cluster.sync();
+    tc_after();
+    const uint32_t tmem = words[0];
+
+    if (warp == 0) {
+        Ring<S> at;
+        uint32_t issued = 0;
+        bool ok = true;
+        for (uint32_t tile = tile0; ok && tile < tiles; tile += tile_step) {
+            uint32_t rp, tp;
+            place(tile, rp, tp);
+            // (a half that does not exist lies behind the map's end and reads zero)
+            const uint32_t w0 = (rp * 2 + rank) * n_kb, x0 = (tp * 2 + rank) * n_kb;
+            for (uint32_t kb = 0; kb < n_kb; ++kb, at.step(), ++issued) {
+                const uint32_t st = base + at.s * G::kStage, bar = of_rank(full(at.s), 0);
+                if (!(ok = wait8(empty(at.s), at.round ^ 1u, aborted))) break;
+                const bool first = (kb & 3u) == 0;
+                if (elected()) {
+                    if (rank == 0) bar_expect(full(at.s), 2 * (G::kStage + (first ? G::kScaleSlot : 0)));
+                    pair_load(st, &map_w, bar, (w0 + kb) * 128);
+                    pair_load(st + kTile, &map_x, bar, (x0 + kb) * 128);
+                    if (first) {
+                        const uint32_t sc = scales + at.s * G::kScaleSlot, g = kb >> 2;
+                        pair_load(sc, &map_ws, bar, (rp * 2 + rank) * lw.groups + g);
+                        pair_load(sc + kScales, &map_xs, bar, tp * 2 * lx.groups + g);
+                        pair_load(sc + 2 * kScales, &map_xs, bar, (tp * 2 + 1) * lx.groups + g);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        if (!ok) {      // what is under way has to land before either CTA's shared memory is released
+            if (rank == 0)
+                for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) bar_wait(full(i % S), i / S & 1u);
+            __nanosleep(1000000);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (rank == 0) {
+            Ring<S> at;
+            uint32_t turn = 0, set = 0, last_stage[2] = {}, last_round[2] = {}, used = 0;
+            bool ok = true;
+            for (uint32_t tile = tile0; ok && tile < tiles; tile += tile_step, ++turn) {
+                const uint32_t acc = tmem + (turn & 1u) * G::kShift;
+                // of the tile before, the shared columns have been read, and the one before that altogether
+                if (turn && !(ok = wait8(next, (turn & 1u) ^ 1u, aborted))) break;
+                tc_after();
+                for (uint32_t kb = 0; kb < n_kb; ++kb, at.step()) {
+                    const uint32_t st = base + at.s * G::kStage;
+                    if (!(ok = wait8(full(at.s), at.round, aborted))) break;
+                    tc_after();
+                    const bool first = (kb & 3u) == 0;
+                    if (first) {
+                        set ^= 1u;
+                        if (used >> set & 1u && !(ok = wait8(empty(set ? last_stage[1] : last_stage[0]), set ? last_round[1] : last_round[0], aborted))) break;
+                        used |= 1u << set;
+                    }
+                    const uint32_t sa = tmem + G::kScaleCols + set * G::kScaleSet, id = (kb & 3u) << 29 | (kb & 3u) << 4 | G::kIdesc;
+                    const uint64_t da = operand_desc(st), db = operand_desc(st + kTile);
+                    if (elected()) {
+                        if (first) {
+                            const uint32_t sc = scales + at.s * G::kScaleSlot;
+                            pair_copy_scales(sa, scales_desc(sc));
+                            pair_copy_scales(sa + 4, scales_desc(sc + kScales));
+                            pair_copy_scales(sa + 8, scales_desc(sc + 2 * kScales));
+                        }
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k) pair_mma8(acc, da + 2 * k, db + 2 * k, id, sa, sa + 4, kb || k ? 1u : 0u);
+                        pair_commit(empty(at.s));
+                        if (kb + 1 == n_kb) pair_commit(sums_full(turn & 1u));
+                    }
+                    __syncwarp();
+                    if (set) { last_stage[1] = at.s; last_round[1] = at.round; }
+                    else { last_stage[0] = at.s; last_round[0] = at.round; }
+                }
+            }
+            if (!ok) {
+                if (elected()) pair_commit(drained);
+                bar_wait(drained, 0);
+            }
+        }
+        __syncwarp();
+    } else {
+        const uint32_t quarter = warp & 3, half = (warp - 2) >> 2, lanes = quarter * 32 << 16, next0 = of_rank(next, 0);
+        uint32_t turn = 0;
+        bool ok = true;
+        for (uint32_t tile = tile0; tile < tiles; tile += tile_step, ++turn) {
+            uint32_t rp, tp;
+            place(tile, rp, tp);
+            const uint32_t row = (rp * 2 + rank) * 128 + quarter * 32 + lane, n0 = tp * 256;
+            ok = ok && wait8(sums_full(turn & 1u), turn >> 1 & 1u, aborted);
+            tc_after();
+#pragma unroll 1
+            for (uint32_t j = half; j < 8; j += 2) {
+                const uint32_t j0 = (turn & 1u ? j : 7 - j) * 32;      // the shared columns first: the first accumulator's last, the second's first
+                uint32_t v[32];
+                if (ok) {
+                    tc_load32(tmem + lanes + (turn & 1u) * G::kShift + j0, v);
+                    tc_wait_ld();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = 0x7FFFFFFFu;      // a sum that was not made is NaN
+                }
+                if (j == half) {
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) cluster_arrive(next0);
+                }
+                store_tokens<32>(a, n0 + j0, row, v);
+            }
+        }
+        tc_before();
+    }
+    cluster.sync();      // neither CTA leaves while the other's products read its shared memory
+    if (warp == 1) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     }
 }
 
@@ -293,6 +567,52 @@ template <int N> int run_linear8(Linear8Args& a, int sm_count, int device, cudaS
     return static_cast<int>(cudaLaunchKernelEx(&cfg, linear8_kernel<N>, a));
 }
 
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult st;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &st) != cudaSuccess || st != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+// `rows` rows of `words` 32-bit words one behind the other, in boxes of `box` rows; rows behind the end read zero
+bool map_rows(EncodeTiled enc, CUtensorMap* map, const void* p, uint32_t words, uint64_t rows, uint32_t box)
+{
+    const cuuint64_t dims[2] = {words, rows}, strides[1] = {words * 4ull};
+    const cuuint32_t boxes[2] = {words, box}, step[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(p), dims, strides, boxes, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int run_pairs(const Linear8Args& a, int sm_count, int device, cudaStream_t stream)
+{
+    static std::atomic<bool> granted[kDevices8];
+    if (device >= kDevices8 || !granted[device].load(std::memory_order_relaxed)) {
+        const cudaError_t e = cudaFuncSetAttribute(linear8_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Pair8::kSmem));
+        if (e != cudaSuccess) return static_cast<int>(e);
+        if (device < kDevices8) granted[device].store(true, std::memory_order_relaxed);
+    }
+    const EncodeTiled enc = encode_tiled();
+    if (!enc) return static_cast<int>(cudaErrorNotSupported);
+    const Packed8Layout lw(a.rows, a.cols), lx(a.n_tokens, a.cols);
+    CUtensorMap mw, mws, mx, mxs;
+    if (!map_rows(enc, &mw, a.w, 32, lw.codes / 128, 128) || !map_rows(enc, &mx, a.x, 32, lx.codes / 128, 128) ||
+        !map_rows(enc, &mws, static_cast<const char*>(a.w) + lw.codes, 128, static_cast<uint64_t>(lw.row_tiles) * lw.groups, 1) ||
+        !map_rows(enc, &mxs, static_cast<const char*>(a.x) + lx.codes, 128, static_cast<uint64_t>(lx.row_tiles) * lx.groups, 1))
+        return static_cast<int>(cudaErrorInvalidValue);
+    const uint64_t tiles = static_cast<uint64_t>((lw.row_tiles + 1) / 2) * ((lx.row_tiles + 1) / 2);
+    const unsigned grid = static_cast<unsigned>(std::min<uint64_t>(tiles, sm_count / 2) * 2);
+    linear8_pair_kernel<<<grid, Pair8::kThreads, Pair8::kSmem, stream>>>(mw, mws, mx, mxs, a);
+    return static_cast<int>(cudaGetLastError());
+}
+
 }  // namespace
 
 int launch_linear8(Linear8Args& a, int sm_count, int device, void* stream)
@@ -301,6 +621,7 @@ int launch_linear8(Linear8Args& a, int sm_count, int device, void* stream)
     if (a.n_tokens <= 16) return run_linear8<16>(a, sm_count, device, s);
     if (a.n_tokens <= 32) return run_linear8<32>(a, sm_count, device, s);
     if (a.n_tokens <= 64) return run_linear8<64>(a, sm_count, device, s);
+    if (a.n_tokens > 128) return run_pairs(a, sm_count, device, s);
     return run_linear8<128>(a, sm_count, device, s);
 }
 
