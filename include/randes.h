@@ -594,14 +594,20 @@ int randes_retrieve_packed_eight(const randes_plan_t* plan, uint32_t task_id, fl
 
 /*
  * Product of two matrices in eight bits:  y[t][r] = sum_c x[t][c] w[r][c].
- *   w [rows, cols], x [n_tokens, cols]   in eight bits
- *   y, y_dtype, y_stride                 device [n_tokens, rows], y_stride elements between tokens (>= rows); must not overlap x or w
+ *   w [rows, cols]           in eight bits
+ *   x [n_tokens, cols]       x_dtype RANDES_EIGHT_BITS: in eight bits (x_stride is not used); RANDES_F32 or RANDES_BF16: device,
+ *                            x_stride elements between tokens (>= cols), taken into eight bits by the call
+ *   y, y_dtype, y_stride     device [n_tokens, rows], y_stride elements between tokens (>= rows); must not overlap x or w
+ *   workspace                device memory, 16-byte aligned, at least randes_packed_eight_linear_workspace() bytes: none for tokens in
+ *                            eight bits and for up to 16 others
  * Products are exact, sums run in the tensor core's fp32 in a fixed order, a bf16 y is rounded once.  From one token to millions.
- * One kernel launch.  Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED, CUDA_ERROR.  Its waits are bounded and counted by
- * randes_linear_giveups().
+ * One kernel launch, two where a workspace is needed.  Errors: INVALID_ARGUMENT, UNSUPPORTED_DTYPE, MISALIGNED,
+ * WORKSPACE_TOO_SMALL, CUDA_ERROR.  Its waits are bounded and counted by randes_linear_giveups().
  */
-int randes_packed_eight_linear(const void* w, uint32_t rows, uint32_t cols, const void* x, uint32_t n_tokens, void* y, randes_dtype_t y_dtype,
-                          uint64_t y_stride, void* stream);
+#define RANDES_EIGHT_BITS 8
+size_t randes_packed_eight_linear_workspace(uint32_t cols, int x_dtype, uint32_t n_tokens);      /* host-only */
+int randes_packed_eight_linear(const void* w, uint32_t rows, uint32_t cols, const void* x, int x_dtype, uint64_t x_stride, uint32_t n_tokens,
+                               void* y, randes_dtype_t y_dtype, uint64_t y_stride, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Root-mean-square norm of rows, with the residual's addition in front:

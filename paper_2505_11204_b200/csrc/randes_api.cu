@@ -1904,13 +1904,10 @@ bool packable8(uint32_t rows, uint32_t cols)
 int check_matrix8(const void* data, uint32_t rows, uint32_t cols, uint64_t stride, uint32_t i, size_t elem, const void* packed)
 {
     int rc;
-    char what[32];
-    snprintf(what, sizeof what, "matrix %u", i);
-    if ((rc = check_tensor(data, rows, cols, stride, elem, what))) return rc;
+    if ((rc = check_tensor(data, rows, cols, stride, elem, "a matrix"))) return rc;
     if (rows == 0 || cols == 0) return RANDES_OK;
     if (!packable8(rows, cols)) return fail(RANDES_INVALID_ARGUMENT, "matrix %u: %u x %u is too large to be packed", i, rows, cols);
-    snprintf(what, sizeof what, "packed[%u]", i);
-    if ((rc = check_packed(packed, what))) return rc;
+    if ((rc = check_packed(packed, "the buffer of a packed matrix"))) return rc;
     if (overlap(data, span_bytes(rows, cols, stride, elem), packed, randes_packed_eight_bytes(rows, cols)))
         return fail(RANDES_INVALID_ARGUMENT, "packed[%u] overlaps its matrix", i);
     return RANDES_OK;
@@ -2043,13 +2040,14 @@ int randes_retrieve_packed_eight_impl(const randes_plan_t* plan, uint32_t task_i
     return RANDES_OK;
 }
 
-int randes_packed_eight_linear_impl(const void* w, uint32_t rows, uint32_t cols, const void* x, uint32_t n_tokens, void* y, randes_dtype_t y_dtype,
-                               uint64_t y_stride, void* stream)
+int randes_packed_eight_linear_impl(const void* w, uint32_t rows, uint32_t cols, const void* x, int x_dtype, uint64_t x_stride, uint32_t n_tokens, void* y,
+                                    randes_dtype_t y_dtype, uint64_t y_stride, void* workspace, size_t workspace_bytes, void* stream)
 {
     int rc;
-    if ((rc = check_dtype(y_dtype, "output"))) return rc;
+    const bool packed = x_dtype == RANDES_EIGHT_BITS;
+    if ((!packed && (rc = check_dtype(x_dtype, "activation"))) || (rc = check_dtype(y_dtype, "output"))) return rc;
     if (n_tokens == 0 || rows == 0) return RANDES_OK;
-    const size_t ye = elem_size(y_dtype);
+    const size_t xe = packed ? 1 : elem_size(x_dtype), ye = elem_size(y_dtype);
     if ((rc = check_tensor(y, n_tokens, rows, y_stride, ye, "y"))) return rc;
     if (cols == 0) {      // a sum over nothing
         const cudaError_t e = n_tokens == 1 ? cudaMemsetAsync(y, 0, rows * ye, static_cast<cudaStream_t>(stream))
@@ -2058,14 +2056,36 @@ int randes_packed_eight_linear_impl(const void* w, uint32_t rows, uint32_t cols,
     }
     if (!packable8(rows, cols) || !packable8(n_tokens, cols) || !packable8(rows, n_tokens))
         return fail(RANDES_INVALID_ARGUMENT, "a product of %u tokens with %u x %u is not supported", n_tokens, rows, cols);
-    if ((rc = check_packed(w, "w")) || (rc = check_packed(x, "x"))) return rc;
-    const uint64_t span = span_bytes(n_tokens, rows, y_stride, ye);
-    if (overlap(w, randes_packed_eight_bytes(rows, cols), y, span) || overlap(x, randes_packed_eight_bytes(n_tokens, cols), y, span))
-        return fail(RANDES_INVALID_ARGUMENT, "y overlaps w or x");
+    if ((rc = check_packed(w, "w")) || (rc = packed ? check_packed(x, "x") : check_tensor(x, n_tokens, cols, x_stride, xe, "x"))) return rc;
+    const uint64_t x_bytes = packed ? randes_packed_eight_bytes(n_tokens, cols) : span_bytes(n_tokens, cols, x_stride, xe);
+    const uint64_t y_bytes = span_bytes(n_tokens, rows, y_stride, ye);
+    if (overlap(w, randes_packed_eight_bytes(rows, cols), y, y_bytes)) return fail(RANDES_INVALID_ARGUMENT, "y overlaps w");
+    // (strided tensors may interleave without sharing an element; dense ones are compared)
+    if ((packed || n_tokens == 1 || (x_stride == cols && y_stride == rows)) && overlap(x, x_bytes, y, y_bytes))
+        return fail(RANDES_INVALID_ARGUMENT, "y overlaps x");
+    const size_t need = randes_packed_eight_linear_workspace(cols, x_dtype, n_tokens);
+    if (need) {
+        if (!workspace || workspace_bytes < need)
+            return fail(RANDES_WORKSPACE_TOO_SMALL, "%u tokens of %u columns need a workspace of %zu bytes, got %zu", n_tokens, cols, need, workspace ? workspace_bytes : 0);
+        if ((rc = check_packed(workspace, "workspace"))) return rc;
+        if (overlap(workspace, need, x, x_bytes) || overlap(workspace, need, y, y_bytes) || overlap(workspace, need, w, randes_packed_eight_bytes(rows, cols)))
+            return fail(RANDES_INVALID_ARGUMENT, "the workspace overlaps x, y or w");
+    }
     Device dev;
     if ((rc = current_device(&dev))) return rc;
-    Linear8Args a{w, x, y, y_stride, rows, cols, n_tokens, y_dtype == RANDES_BF16 ? 1u : 0u, 0};
-    const int e = launch_linear8(a, dev.sms, dev.index, stream);
+    const bool vec = !packed && rows_aligned(x, n_tokens, x_stride, xe);
+    if (need) {
+        Pack8Args p;
+        p.n = 1;
+        p.lambda = 0.f;
+        p.task = DevTask{0, 0, 0, 0};
+        p.mat[0] = Pack8Matrix{x, nullptr, workspace, x_stride, n_tokens, cols, 0, 0, vec ? 1u : 0u, 0};
+        const int e = launch_pack8(x_dtype, x_dtype, false, p, stream);
+        if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit pack kernel");
+        ++g_launches;
+    }
+    Linear8Args a{w, need ? workspace : x, y, x_stride, y_stride, rows, cols, n_tokens, vec ? 1u : 0u, y_dtype == RANDES_BF16 ? 1u : 0u, 0};
+    const int e = launch_linear8(a, packed || need ? -1 : x_dtype, dev.sms, dev.index, stream);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit product");
     ++g_launches;
     return RANDES_OK;
@@ -2218,10 +2238,17 @@ int randes_retrieve_packed_eight(const randes_plan_t* plan, uint32_t task_id, fl
     return guarded("randes_retrieve_packed_eight", [&] { return randes_retrieve_packed_eight_impl(plan, task_id, lambda, layers, n, base, M, packed, stream); });
 }
 
-int randes_packed_eight_linear(const void* w, uint32_t rows, uint32_t cols, const void* x, uint32_t n_tokens, void* y, randes_dtype_t y_dtype,
-                          uint64_t y_stride, void* stream)
+size_t randes_packed_eight_linear_workspace(uint32_t cols, int x_dtype, uint32_t n_tokens)
 {
-    return guarded("randes_packed_eight_linear", [&] { return randes_packed_eight_linear_impl(w, rows, cols, x, n_tokens, y, y_dtype, y_stride, stream); });
+    return x_dtype == RANDES_EIGHT_BITS || linear8_packs(n_tokens) ? 0 : randes_packed_eight_bytes(n_tokens, cols);
+}
+
+int randes_packed_eight_linear(const void* w, uint32_t rows, uint32_t cols, const void* x, int x_dtype, uint64_t x_stride, uint32_t n_tokens, void* y,
+                               randes_dtype_t y_dtype, uint64_t y_stride, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return guarded("randes_packed_eight_linear", [&] {
+        return randes_packed_eight_linear_impl(w, rows, cols, x, x_dtype, x_stride, n_tokens, y, y_dtype, y_stride, workspace, workspace_bytes, stream);
+    });
 }
 
 int randes_rms_norm(const randes_rms_norm_t* norm, void* stream)

@@ -331,12 +331,13 @@ struct Pack8Matrix {
     uint32_t vec;                 // bit 0: rows of src are 16-byte aligned; bit 1: rows of m
     uint32_t first_cta;           // set by the launcher
 };
-struct Pack8Args {
-    Pack8Matrix mat[kPackBatch];
+template <uint32_t BATCH> struct Pack8Batch {      // one matrix or many: a launch copies what it is given
+    Pack8Matrix mat[BATCH];
     uint32_t n;
     float lambda;
     DevTask task;
 };
+typedef Pack8Batch<kPackBatch> Pack8Args;
 struct Unpack8Matrix {
     const void* src;
     void* dst;
@@ -345,10 +346,11 @@ struct Unpack8Matrix {
     uint32_t vec;                 // rows of dst are 16-byte aligned
     uint32_t first_cta;
 };
-struct Unpack8Args {
-    Unpack8Matrix mat[kPackBatch];
+template <uint32_t BATCH> struct Unpack8Batch {
+    Unpack8Matrix mat[BATCH];
     uint32_t n;
 };
+typedef Unpack8Batch<kPackBatch> Unpack8Args;
 struct Turn8Args {
     const void* src;              // [rows, cols] fp32 or bf16, or a matrix in eight bits
     void* dst;                    // the same rows in eight bits, or NULL
@@ -363,14 +365,15 @@ int launch_turn8(int src_dtype, const Turn8Args& a, void* stream);       // src_
 // randes_linear8.cu: products of two matrices in eight bits
 struct Linear8Args {
     const void* w;                // [rows, cols] in eight bits
-    const void* x;                // [n_tokens, cols] in eight bits
+    const void* x;                // [n_tokens, cols] in eight bits, or of the type that the launcher is given
     void* y;
-    uint64_t y_stride;
+    uint64_t x_stride, y_stride;
     uint32_t rows, cols, n_tokens;
-    uint32_t y_bf16;
+    uint32_t x_vec, y_bf16;
     uint32_t log_ranks;           // set by the launcher: CTAs of a cluster that share a tile's columns
 };
-int launch_linear8(Linear8Args& a, int sm_count, int device, void* stream);
+bool linear8_packs(uint32_t n_tokens);      // whether so few tokens go into eight bits inside the product
+int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, int device, void* stream);      // x_dtype -1: eight bits
 int linear8_giveups(unsigned int* count);
 
 // randes_norm.cu: root-mean-square norm with the residual's addition, and its gradient

@@ -150,6 +150,11 @@ __device__ __forceinline__ bool wait8(uint32_t bar, uint32_t parity, volatile ui
     __syncwarp();
     return false;
 }
+// After giving up: a millisecond at most for the copies of a stage, which take microseconds.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity)
+{
+    for (uint32_t i = 0; i < 256 && !bar_try(bar, parity); ++i) {}
+}
 // Where a role stands in the ring of S stages: the stage and the parity of its round.
 template <uint32_t S> struct Ring {
     uint32_t s = 0, round = 0;
@@ -196,9 +201,54 @@ template <int N> struct Geom8 {
     static_assert(kStage % 1024 == 0 && 8 * kBars + 16 <= 512, "stages on the swizzle's boundary");
 };
 
-template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(const Linear8Args a)
+// Few tokens that are not in eight bits yet: a thread holds 16 columns of one token, eight threads a block, four blocks ahead.
+template <typename X> struct Sixteen {
+    static constexpr int kWords = sizeof(X);
+    uint4 w[kWords];
+    __device__ __forceinline__ void load(const X* row, uint32_t c, uint32_t cols, bool vec)
+    {
+        if (vec && c + 16 <= cols) {
+#pragma unroll
+            for (int h = 0; h < kWords; ++h) w[h] = __ldg(reinterpret_cast<const uint4*>(row + c) + h);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[8];
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) v[e] = c + 8 * h + e < cols ? Store<X>::load1(row + c + 8 * h + e) : 0.f;
+                const Octet<X> o = narrow<X>(v);
+#pragma unroll
+                for (int e = 0; e < kWords / 2; ++e) w[h * (kWords / 2) + e] = o.w[e];
+            }
+        }
+    }
+    __device__ __forceinline__ void half(int h, float (&v)[8]) const
+    {
+        Octet<X> o;
+#pragma unroll
+        for (int e = 0; e < kWords / 2; ++e) o.w[e] = w[h * (kWords / 2) + e];
+        widen(o, v);
+    }
+    __device__ __forceinline__ uint32_t top() const
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[8];
+            half(h, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max_bits(m, magnitude(v[e]));
+        }
+        return m;
+    }
+};
+
+// X: the type of x; uint8_t where it is in eight bits. Other types are for one tile of 16 tokens: the warps of the results lay the
+// tokens out themselves (which saves a launch and a pass; for more tokens every CTA would repeat too much of it).
+template <int N, typename X> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(const Linear8Args a)
 {
     typedef Geom8<N> G;
+    constexpr bool kPacks = sizeof(X) > 1;
     constexpr int S = G::kStages;
     extern __shared__ unsigned char smem_raw[];
     cg::cluster_group cluster = cg::this_cluster();
@@ -222,7 +272,7 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
     const uint32_t tile0 = blockIdx.x >> a.log_ranks, tile_step = gridDim.x >> a.log_ranks;
 
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < S; ++s) { bar_init(full(s)); bar_init(empty(s)); }
+        for (uint32_t s = 0; s < S; ++s) { bar_init_n(full(s), kPacks ? 5 : 1); bar_init(empty(s)); }
         for (uint32_t b = 0; b < 2; ++b) { bar_init(sums_full(b)); bar_init_n(sums_free(b), 128); }
         bar_init(drained);
         *aborted = 0;
@@ -249,19 +299,19 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
                 if (!(ok = wait8(empty(at.s), at.round ^ 1u, aborted))) break;
                 const bool first = kb == k0 || (kb & 3u) == 0;
                 if (elected()) {
-                    bar_expect(bar, kTile + N * 128 + (first ? 2 * kScales : 0));
+                    bar_expect(bar, kTile + (kPacks ? 0 : N * 128) + (first ? (kPacks ? 1 : 2) * kScales : 0));
                     bulk_copy(st, w + lw.tile(rt, kb), kTile, bar);
-                    bulk_copy(st + kTile, x + lx.tile(xt, kb) + (n0 & 127) * 128, N * 128, bar);
+                    if (!kPacks) bulk_copy(st + kTile, x + lx.tile(xt, kb) + (n0 & 127) * 128, N * 128, bar);
                     if (first) {
                         bulk_copy(st + kTile + N * 128, w + lw.scales(rt, kb >> 2), kScales, bar);
-                        bulk_copy(st + kTile + N * 128 + kScales, x + lx.scales(xt, kb >> 2), kScales, bar);
+                        if (!kPacks) bulk_copy(st + kTile + N * 128 + kScales, x + lx.scales(xt, kb >> 2), kScales, bar);
                     }
                 }
                 __syncwarp();
             }
         }
         if (!ok)      // what is under way has to land before the CTA's shared memory is released
-            for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) bar_wait(full(i % S), i / S & 1u);
+            for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) drain(full(i % S), i / S & 1u);
         __syncwarp();
     } else if (warp == 1) {
         Ring<S> at;
@@ -307,8 +357,50 @@ template <int N> __global__ void __launch_bounds__(kThreads8, 1) linear8_kernel(
         const uint32_t quarter = warp & 3, lanes = quarter * 32 << 16;
         uint32_t turn = 0;
         bool ok = true;
+        Ring<S> at;
         for (uint32_t tile = tile0; tile < tiles; tile += tile_step, ++turn) {
             const uint32_t rt = tile / token_tiles, n0 = (tile - rt * token_tiles) * N, row = rt * 128 + quarter * 32 + lane;
+            if constexpr (kPacks) {
+                const uint32_t t = quarter * 4 + (lane >> 3), piece = lane & 7;      // token; 16 columns of a block
+                const X* from = static_cast<const X*>(a.x) + min(t, a.n_tokens - 1) * a.x_stride;
+                for (uint32_t g0 = k0; ok && g0 < k1;) {
+                    const uint32_t g1 = min(k1, (g0 | 3u) + 1);
+                    Sixteen<X> v[4];
+                    uint32_t e[4], word = 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+                        if (g0 + i < g1) v[i].load(from, (g0 + i) * 128 + piece * 16, a.cols, a.x_vec);
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        uint32_t top = 0;
+                        if (g0 + i < g1) top = v[i].top();
+#pragma unroll
+                        for (int o = 1; o < 8; o <<= 1) top = max_bits(top, __shfl_xor_sync(~0u, top, o));
+                        e[i] = top;
+                        if (g0 + i < g1) word |= block_scale(top) << ((g0 + i & 3u) * 8);
+                    }
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        if (g0 + i >= g1 || !ok) break;
+                        if (!(ok = wait8(empty(at.s), at.round ^ 1u, aborted))) break;
+                        if (t < a.n_tokens) {
+                            unsigned char* stage = gen + at.s * G::kStage + kTile;
+                            float c[8];
+                            v[i].half(0, c);
+                            const uint2 lo = codes8(c, e[i], block_scale(e[i]));
+                            v[i].half(1, c);
+                            const uint2 hi = codes8(c, e[i], block_scale(e[i]));
+                            *reinterpret_cast<uint4*>(stage + code_at(t, piece * 16)) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                            if (i == 0 && piece == 0) *reinterpret_cast<uint32_t*>(stage + N * 128 + kScales + Packed8Layout::scale_word(t)) = word;
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tensor core reads it next
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(full(at.s));
+                        at.step();
+                    }
+                    g0 = g1;
+                }
+            }
             ok = ok && wait8(sums_full(turn & 1u), turn >> 1 & 1u, aborted);
             tc_after();
 #pragma unroll 1
@@ -450,7 +542,7 @@ linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         }
         if (!ok) {      // what is under way has to land before either CTA's shared memory is released
             if (rank == 0)
-                for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) bar_wait(full(i % S), i / S & 1u);
+                for (uint32_t i = issued > S ? issued - S : 0; i < issued; ++i) drain(full(i % S), i / S & 1u);
             __nanosleep(1000000);
         }
         __syncwarp();
@@ -539,12 +631,12 @@ linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 
 constexpr int kDevices8 = 64;
 
-template <int N> int run_linear8(Linear8Args& a, int sm_count, int device, cudaStream_t stream)
+template <int N, typename X> int run_linear8(Linear8Args& a, int sm_count, int device, cudaStream_t stream)
 {
     typedef Geom8<N> G;
     static std::atomic<bool> granted[kDevices8];
     if (device >= kDevices8 || !granted[device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(G::kSmem));
+        const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<N, X>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(G::kSmem));
         if (e != cudaSuccess) return static_cast<int>(e);
         if (device < kDevices8) granted[device].store(true, std::memory_order_relaxed);
     }
@@ -564,7 +656,7 @@ template <int N> int run_linear8(Linear8Args& a, int sm_count, int device, cudaS
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = a.log_ranks ? 1 : 0;
-    return static_cast<int>(cudaLaunchKernelEx(&cfg, linear8_kernel<N>, a));
+    return static_cast<int>(cudaLaunchKernelEx(&cfg, linear8_kernel<N, X>, a));
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -615,14 +707,18 @@ int run_pairs(const Linear8Args& a, int sm_count, int device, cudaStream_t strea
 
 }  // namespace
 
-int launch_linear8(Linear8Args& a, int sm_count, int device, void* stream)
+bool linear8_packs(uint32_t n_tokens) { return n_tokens <= 16; }
+
+int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, int device, void* stream)
 {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a.n_tokens <= 16) return run_linear8<16>(a, sm_count, device, s);
-    if (a.n_tokens <= 32) return run_linear8<32>(a, sm_count, device, s);
-    if (a.n_tokens <= 64) return run_linear8<64>(a, sm_count, device, s);
+    if (x_dtype == 0) return run_linear8<16, float>(a, sm_count, device, s);
+    if (x_dtype == 1) return run_linear8<16, bf16>(a, sm_count, device, s);
+    if (a.n_tokens <= 16) return run_linear8<16, uint8_t>(a, sm_count, device, s);
+    if (a.n_tokens <= 32) return run_linear8<32, uint8_t>(a, sm_count, device, s);
+    if (a.n_tokens <= 64) return run_linear8<64, uint8_t>(a, sm_count, device, s);
     if (a.n_tokens > 128) return run_pairs(a, sm_count, device, s);
-    return run_linear8<128>(a, sm_count, device, s);
+    return run_linear8<128, uint8_t>(a, sm_count, device, s);
 }
 
 int linear8_giveups(unsigned int* count)

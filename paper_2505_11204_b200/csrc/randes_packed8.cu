@@ -36,12 +36,12 @@ template <typename Args> __device__ __forceinline__ uint32_t matrix_of(const Arg
 }
 
 // A warp takes rows r0 .. r0 + 3 of 512 columns: two runs of 256, lane l holding columns 8 l .. 8 l + 7 of either.
-template <typename T, typename M, bool RETRIEVE>
-__global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_constant__ Pack8Args a)
+template <typename T, typename M, bool RETRIEVE, uint32_t BATCH>
+__global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_constant__ Pack8Batch<BATCH> a)
 {
     __shared__ __align__(16) float s_scratch[kWarps8][256];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Pack8Matrix& m = a.mat[matrix_of(a, blockIdx.x)];
+    const Pack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
     const Packed8Layout lay(m.rows, m.cols);
     const uint32_t cta = blockIdx.x - m.first_cta, rb = cta / lay.groups, g = cta - rb * lay.groups;
     const uint32_t r0 = rb * kCtaRows8 + warp * kRows8, cols = m.cols;
@@ -107,11 +107,11 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
             *reinterpret_cast<uint32_t*>(dst + lay.scales(r0 >> 7, g) + Packed8Layout::scale_word(r0 + i)) = word[i];
 }
 
-template <typename T> __global__ void __launch_bounds__(kWarps8 * 32) unpack8_kernel(const __grid_constant__ Unpack8Args a)
+template <typename T, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 * 32) unpack8_kernel(const __grid_constant__ Unpack8Batch<BATCH> a)
 {
     __shared__ __align__(16) float s_scratch[kWarps8][256];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Unpack8Matrix& m = a.mat[matrix_of(a, blockIdx.x)];
+    const Unpack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
     const Packed8Layout lay(m.rows, m.cols);
     const uint32_t cta = blockIdx.x - m.first_cta, rb = cta / lay.groups, g = cta - rb * lay.groups;
     const uint32_t r0 = rb * kCtaRows8 + warp * kRows8, cols = m.cols;
@@ -293,7 +293,18 @@ template <typename Args> uint32_t count_ctas(Args& a)
 
 template <typename T, typename M, bool RETRIEVE> int run_pack8(Pack8Args& a, void* stream)
 {
-    pack8_kernel<T, M, RETRIEVE><<<count_ctas(a), kWarps8 * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    const uint32_t ctas = count_ctas(a);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (a.n == 1) pack8_kernel<T, M, RETRIEVE, 1><<<ctas, kWarps8 * 32, 0, s>>>(Pack8Batch<1>{{a.mat[0]}, 1, a.lambda, a.task});
+    else pack8_kernel<T, M, RETRIEVE, kPackBatch><<<ctas, kWarps8 * 32, 0, s>>>(a);
+    return static_cast<int>(cudaGetLastError());
+}
+template <typename T> int run_unpack8(Unpack8Args& a, void* stream)
+{
+    const uint32_t ctas = count_ctas(a);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (a.n == 1) unpack8_kernel<T, 1><<<ctas, kWarps8 * 32, 0, s>>>(Unpack8Batch<1>{{a.mat[0]}, 1});
+    else unpack8_kernel<T, kPackBatch><<<ctas, kWarps8 * 32, 0, s>>>(a);
     return static_cast<int>(cudaGetLastError());
 }
 template <typename T> int run_turn8(const Turn8Args& a, void* stream)
@@ -320,10 +331,7 @@ int launch_pack8(int w_dtype, int m_dtype, bool retrieve, Pack8Args& a, void* st
 
 int launch_unpack8(int out_dtype, Unpack8Args& a, void* stream)
 {
-    const uint32_t ctas = count_ctas(a);
-    if (out_dtype) unpack8_kernel<bf16><<<ctas, kWarps8 * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    else unpack8_kernel<float><<<ctas, kWarps8 * 32, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    return static_cast<int>(cudaGetLastError());
+    return out_dtype ? run_unpack8<bf16>(a, stream) : run_unpack8<float>(a, stream);
 }
 
 int launch_turn8(int src_dtype, const Turn8Args& a, void* stream)

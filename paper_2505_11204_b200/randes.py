@@ -17,10 +17,12 @@ import ctypes
 import functools
 import math
 import os
+import struct
 from typing import Any, List, NamedTuple, Optional, Sequence
 
 F32 = 0
 BF16 = 1
+EIGHT_BITS = 8   # RANDES_EIGHT_BITS: activations that are in eight bits already
 SHUFFLE = 1
 FLIP = 2
 SHIFT = 4
@@ -182,7 +184,9 @@ def lib():
         L.randes_transpose_eight.restype = ctypes.c_int
         L.randes_retrieve_packed_eight.argtypes = [vp, u32, f32, vp, u32, vp, vp, vp, vp]
         L.randes_retrieve_packed_eight.restype = ctypes.c_int
-        L.randes_packed_eight_linear.argtypes = [vp, u32, u32, vp, u32, vp, dt, u64, vp]
+        L.randes_packed_eight_linear_workspace.argtypes = [u32, ctypes.c_int, u32]
+        L.randes_packed_eight_linear_workspace.restype = sz
+        L.randes_packed_eight_linear.argtypes = [vp, u32, u32, vp, ctypes.c_int, u64, u32, vp, dt, u64, vp, sz, vp]
         L.randes_packed_eight_linear.restype = ctypes.c_int
         L.randes_rms_norm.argtypes = [vp, vp]
         L.randes_rms_norm.restype = ctypes.c_int
@@ -206,7 +210,7 @@ EXPORTS = [
     "randes_packed_bytes", "randes_pack", "randes_unpack", "randes_retrieve_packed", "randes_packed_linear_workspace", "randes_packed_linear", "randes_packed_linear_tasks",
     "randes_token_scores", "randes_token_scores_backward",
     "randes_packed_eight_bytes", "randes_pack_eight", "randes_unpack_eight", "randes_pack_eight_transposed", "randes_transpose_eight", "randes_retrieve_packed_eight",
-    "randes_packed_eight_linear", "randes_rms_norm", "randes_rms_norm_backward_workspace", "randes_rms_norm_backward",
+    "randes_packed_eight_linear_workspace", "randes_packed_eight_linear", "randes_rms_norm", "randes_rms_norm_backward_workspace", "randes_rms_norm_backward",
 ]
 
 
@@ -450,9 +454,16 @@ def randes_retrieve_packed_eight(plan, task_id, lam, layers, n, base, M, packed,
     _check(lib().randes_retrieve_packed_eight(plan, task_id, lam, _addr(layers), n, _addr(base), _addr(M), _addr(packed), stream))
 
 
-def randes_packed_eight_linear(w, rows, cols, x, n_tokens, y, y_dtype, y_stride, stream) -> None:
-    """y = x W^T of two matrices in eight bits."""
-    _check(lib().randes_packed_eight_linear(_addr(w), rows, cols, _addr(x), n_tokens, _addr(y), y_dtype, y_stride, stream))
+def randes_packed_eight_linear_workspace(cols: int, x_dtype: int, n_tokens: int) -> int:
+    """Bytes of device workspace the call below needs (0 for tokens in eight bits, and for up to 16 others)."""
+    return int(lib().randes_packed_eight_linear_workspace(cols, x_dtype, n_tokens))
+
+
+def randes_packed_eight_linear(w, rows, cols, x, n_tokens, y, y_dtype, y_stride, stream, x_dtype: int = EIGHT_BITS, x_stride: int = 0, workspace=None,
+                               workspace_bytes: int = 0) -> None:
+    """y = x W^T of a matrix in eight bits with tokens in eight bits, fp32 or bf16."""
+    _check(lib().randes_packed_eight_linear(_addr(w), rows, cols, _addr(x), x_dtype, x_stride, n_tokens, _addr(y), y_dtype, y_stride, _addr(workspace),
+                                            workspace_bytes, stream))
 
 
 def randes_rms_norm(norm: RmsNorm, stream) -> None:
@@ -756,6 +767,11 @@ def token_scores_backward(logits, targets, scores: TokenScores, g_logprob=None, 
 
 
 # ---- eight bits, their products and the norm on torch tensors -----------------------------------
+# A structure that a call reads once goes as bytes: packing them takes a third of the time of filling a ctypes object.
+_ONE_MATRIX, _ONE_ADDRESS = struct.Struct("@P2IQ").pack, struct.Struct("@P").pack      # randes_matrix_t[1], void*[1]
+_NORM, _NORM_BACKWARD = struct.Struct("@8P4Q2I2if4x").pack, struct.Struct("@8P4Q2I2i").pack      # randes_rms_norm_t, randes_rms_norm_backward_t
+
+
 @functools.lru_cache(maxsize=4096)
 def _packed8_size(rows: int, cols: int) -> int:
     nbytes = randes_packed_eight_bytes(rows, cols)
@@ -815,7 +831,7 @@ def pack8(weights):
     if not isinstance(weights, (list, tuple)):
         dtype, rows, cols, stride = _rows_of(weights, "the matrix")
         p = _new_packed8(rows, cols, weights.device)
-        _call(p.device, lib().randes_pack_eight, _MatrixOne((weights.data_ptr(), rows, cols, stride)), 1, dtype, _PtrOne(p.address))
+        _call(p.device, lib().randes_pack_eight, _ONE_MATRIX(weights.data_ptr(), rows, cols, stride), 1, dtype, _ONE_ADDRESS(p.address))
         return p
     if not weights:
         return []
@@ -833,7 +849,7 @@ def _turned(x, both: bool):
     dtype, rows, cols, stride = _rows_of(x, "the matrix")
     device = x.device
     p, t = _new_packed8(rows, cols, device) if both else None, _new_packed8(cols, rows, device)
-    _call(device, lib().randes_pack_eight_transposed, _MatrixOne((x.data_ptr(), rows, cols, stride)), dtype, p.address if both else None, t.address)
+    _call(device, lib().randes_pack_eight_transposed, _ONE_MATRIX(x.data_ptr(), rows, cols, stride), dtype, p.address if both else None, t.address)
     return p, t
 
 
@@ -852,24 +868,42 @@ def pack8_both(x):
     return _turned(x, True)
 
 
+_eight_workspace_bytes = functools.lru_cache(maxsize=4096)(randes_packed_eight_linear_workspace)
+
+
 def packed8_linear(x, w: Packed8Matrix, y=None, y_dtype: int = F32):
-    """x: [n_tokens, cols] Packed8Matrix, or an fp32 or bf16 CUDA tensor, which is packed first; returns y = x W^T [n_tokens, rows]."""
+    """x: [n_tokens, cols] Packed8Matrix, or an fp32 or bf16 CUDA tensor (rows may be strided), which goes into eight bits on the way;
+    returns y = x W^T [n_tokens, rows]."""
     if not isinstance(w, Packed8Matrix):
         _refuse("w is no Packed8Matrix")
-    if not isinstance(x, Packed8Matrix):
-        x = pack8(x)
-    n, rows, cols, device = x.rows, w.rows, w.cols, w.device
-    if x.cols != cols:
-        _refuse("x has %d columns, the weight %d" % (x.cols, cols))
+    rows, cols, device = w.rows, w.cols, w.device
+    workspace = None
+    workspace_at = nbytes = x_stride = 0
+    if isinstance(x, Packed8Matrix):
+        x_dtype, n, c, x_at = EIGHT_BITS, x.rows, x.cols, x.address
+    else:
+        x_dtype, n, c, x_stride = _rows_of(x, "x")
+        x_at = x.data_ptr()
+        nbytes = _eight_workspace_bytes(c, x_dtype, n)
+    if c != cols:
+        _refuse("x has %d columns, the weight %d" % (c, cols))
     if x.device != device:
         _refuse("x is on %s, the weight on %s" % (x.device, device))
+    if _torch is None:
+        import torch
+    else:
+        torch = _torch
+    if nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        workspace_at = workspace.data_ptr()
     if y is None:
-        y, y_stride = _torch.empty(n, rows, dtype=_torch.bfloat16 if y_dtype == BF16 else _torch.float32, device=device), rows
+        y, y_stride = torch.empty(n, rows, dtype=torch.bfloat16 if y_dtype == BF16 else torch.float32, device=device), rows
     else:
         y_dtype, yn, yr, y_stride = _rows_of(y, "y")
         if (yn, yr) != (n, rows) or y.device != device:
             _refuse("y is [%d, %d] on %s, [%d, %d] on %s is wanted" % (yn, yr, y.device, n, rows, device))
-    _call(device, lib().randes_packed_eight_linear, w.address, rows, cols, x.address, n, y.data_ptr(), y_dtype, y_stride)
+    _call(device, lib().randes_packed_eight_linear, w.address, rows, cols, x_at, x_dtype, x_stride, n, y.data_ptr(), y_dtype, y_stride, workspace_at or None,
+          nbytes)
     return y
 
 
@@ -893,11 +927,11 @@ def _like_rows(t, what: str, dtype: int, n: int, cols: int, device):
 
 def _gain(gain, cols: int, device):
     if gain is None:
-        return None, F32
-    code = BF16 if gain.dtype is _torch.bfloat16 else F32
-    if (code == F32 and gain.dtype is not _torch.float32) or gain.shape != (cols,) or not gain.is_contiguous() or gain.device != device:
+        return 0, F32
+    dtype = gain.dtype
+    if (dtype is not _torch.float32 and dtype is not _torch.bfloat16) or gain.shape != (cols,) or not gain.is_contiguous() or gain.device != device:
         _refuse("gain must be a contiguous float32 or bfloat16 tensor [%d] on %s" % (cols, device))
-    return gain.data_ptr(), code
+    return gain.data_ptr(), BF16 if dtype is _torch.bfloat16 else F32
 
 
 def rms_norm(x, gain=None, residual=None, eps: float = 1e-6, packed: bool = False, checkpoint: bool = False, h=None, y=None) -> Normed:
@@ -908,30 +942,33 @@ def rms_norm(x, gain=None, residual=None, eps: float = 1e-6, packed: bool = Fals
     or the residual itself)."""
     dtype, n, cols, x_stride = _rows_of(x, "x")
     device = x.device
-    a = RmsNorm(x=x.data_ptr(), x_stride=x_stride, rows=n, cols=cols, dtype=dtype, eps=eps)
-    a.gain, a.gain_dtype = _gain(gain, cols, device)
+    gain_at, gain_type = _gain(gain, cols, device)
+    residual_at = residual_stride = h_at = h_stride = y_at = y_stride = y8_at = kept_at = 0
+    kept, new_h = None, h
     if residual is not None:
-        a.residual, a.residual_stride = _like_rows(residual, "residual", dtype, n, cols, device)
+        residual_at, residual_stride = _like_rows(residual, "residual", dtype, n, cols, device)
         if h is None:
-            h = _torch.empty(n, cols, dtype=x.dtype, device=device)
+            new_h = x.new_empty(n, cols)
+            h_at, h_stride = new_h.data_ptr(), cols
     if h is not None:
-        a.h, a.h_stride = _like_rows(h, "h", dtype, n, cols, device)
+        h_at, h_stride = _like_rows(h, "h", dtype, n, cols, device)
     if packed:
         if y is not None:
             _refuse("y is a tensor to write, packed asks for eight bits")
         y = _new_packed8(n, cols, device)
-        a.y8 = y.address
+        y8_at = y.address
+    elif y is None:
+        y = x.new_empty(n, cols)
+        y_at, y_stride = y.data_ptr(), cols
     else:
-        if y is None:
-            y = _torch.empty(n, cols, dtype=x.dtype, device=device)
-        a.y, a.y_stride = _like_rows(y, "y", dtype, n, cols, device)
-    kept = _new_packed8(n, cols, device) if checkpoint else None
+        y_at, y_stride = _like_rows(y, "y", dtype, n, cols, device)
     if checkpoint:
-        a.kept8 = kept.address
+        kept = _new_packed8(n, cols, device)
+        kept_at = kept.address
     rstd = _torch.empty(n, dtype=_torch.float32, device=device)
-    a.rstd = rstd.data_ptr()
-    _call(device, lib().randes_rms_norm, ctypes.addressof(a))
-    return Normed(y, x if h is None else h, rstd, kept)
+    _call(device, lib().randes_rms_norm, _NORM(x.data_ptr(), residual_at, gain_at, h_at, y_at, y8_at, kept_at, rstd.data_ptr(), x_stride, residual_stride,
+                                               h_stride, y_stride, n, cols, dtype, gain_type, eps))
+    return Normed(y, x if new_h is None else new_h, rstd, kept)
 
 
 _norm_workspace_bytes = functools.lru_cache(maxsize=4096)(randes_rms_norm_backward_workspace)
@@ -944,30 +981,33 @@ def rms_norm_backward(dy, h, rstd, gain=None, dh=None, out=None):
     be dy, h or dh itself."""
     dtype, n, cols, dy_stride = _rows_of(dy, "dy")
     device = dy.device
-    a = RmsNormBackward(dy=dy.data_ptr(), dy_stride=dy_stride, rows=n, cols=cols, dtype=dtype)
+    h_at = h_stride = kept_at = dh_at = dh_stride = dgain_at = workspace_at = nbytes = 0
     if isinstance(h, Packed8Matrix):
-        if (h.rows, h.cols) != (n, cols) or h.device != device:
+        if h.rows != n or h.cols != cols or h.device != device:
             _refuse("the checkpoint is [%d, %d] on %s, dy [%d, %d] on %s" % (h.rows, h.cols, h.device, n, cols, device))
-        a.kept8 = h.address
+        kept_at = h.address
     else:
-        a.h, a.h_stride = _like_rows(h, "h", dtype, n, cols, device)
+        h_at, h_stride = _like_rows(h, "h", dtype, n, cols, device)
     if rstd.dtype is not _torch.float32 or rstd.shape != (n,) or not rstd.is_contiguous() or rstd.device != device:
         _refuse("rstd must be a contiguous float32 tensor [%d] on %s" % (n, device))
-    a.rstd = rstd.data_ptr()
-    a.gain, a.gain_dtype = _gain(gain, cols, device)
+    gain_at, gain_type = _gain(gain, cols, device)
     if dh is not None:
-        a.dh, a.dh_stride = _like_rows(dh, "dh", dtype, n, cols, device)
+        dh_at, dh_stride = _like_rows(dh, "dh", dtype, n, cols, device)
     if out is None:
-        out = _torch.empty(n, cols, dtype=dy.dtype, device=device)
-    a.dx, a.dx_stride = _like_rows(out, "out", dtype, n, cols, device)
+        out = dy.new_empty(n, cols)
+        dx_at, dx_stride = out.data_ptr(), cols
+    else:
+        dx_at, dx_stride = _like_rows(out, "out", dtype, n, cols, device)
     dgain = workspace = None
-    nbytes = 0
     if gain is not None:
         dgain = _torch.empty(cols, dtype=_torch.float32, device=device)
-        a.dgain = dgain.data_ptr()
+        dgain_at = dgain.data_ptr()
         nbytes = _norm_workspace_bytes(n, cols)
-        workspace = _torch.empty(nbytes, dtype=_torch.uint8, device=device)
-    _call(device, lib().randes_rms_norm_backward, ctypes.addressof(a), workspace.data_ptr() if nbytes else None, nbytes)
+        if nbytes:
+            workspace = _torch.empty(nbytes, dtype=_torch.uint8, device=device)
+            workspace_at = workspace.data_ptr()
+    _call(device, lib().randes_rms_norm_backward, _NORM_BACKWARD(dy.data_ptr(), h_at, kept_at, rstd.data_ptr(), gain_at, dh_at, dx_at, dgain_at, dy_stride,
+                                                                 h_stride, dh_stride, dx_stride, n, cols, dtype, gain_type), workspace_at or None, nbytes)
     return out, dgain
 
 

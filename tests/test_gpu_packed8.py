@@ -175,9 +175,17 @@ def test_products(tokens, rows, cols, y_dtype):
     assert randes.randes_linear_giveups() == 0
 
 
-def test_a_tensor_is_packed_on_the_way():
-    x, w = weight(20, 300, torch.bfloat16, 1, 1.0), randes.pack8(weight(50, 300, torch.bfloat16))
-    assert torch.equal(randes.packed8_linear(x, w), randes.packed8_linear(randes.pack8(x), w))
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,rows,cols", [(1, 50, 1), (1, 4096, 1024), (1, 300, 129), (3, 130, 700), (9, 1000, 2050), (16, 128, 4096), (16, 20000, 520), (17, 200, 300),
+                                              (20, 50, 300), (200, 300, 400)])
+def test_a_tensor_is_packed_on_the_way(tokens, rows, cols, dtype):
+    w = randes.pack8(weight(rows, cols, torch.bfloat16))
+    for pad, first in ((0, 0), (3, 1), (8, 8)):
+        x = weight(tokens, cols + pad + first, dtype, 1, 1.0)[:, first:first + cols]
+        if tokens > 1 and cols > 128:
+            x[1, 3], x[0, cols - 1] = float("nan"), 0.0
+        a, b = randes.packed8_linear(x, w), randes.packed8_linear(randes.pack8(x), w)
+        assert same(a, b) and torch.isfinite(a[0]).all()
 
 
 @pytest.mark.parametrize("tokens", [1, 20, 150])
@@ -255,6 +263,9 @@ def test_refusals():
     s = torch.cuda.current_stream().cuda_stream
     call = lambda wa=w.address, xa=x8.address, ya=y, ydt=0, st=8, n=4, rows=8, cols=256: randes.randes_packed_eight_linear(wa, rows, cols, xa, n, ya, ydt, st, s)
     inv, mis = randes.INVALID_ARGUMENT, randes.MISALIGNED
+    many = torch.zeros(400, 256, device="cuda")
+    typed = lambda xa, n=4, dt=0, st=256, ws=None: randes.randes_packed_eight_linear(w.address, 8, 256, xa, n, y if n <= 4 else out, 0, 8, s, dt, st, ws, 1 << 17 if ws is not None else 0)
+    out = torch.empty(17, 8, device="cuda")
     inside = torch.empty(w.data.numel(), dtype=torch.uint8, device="cuda")
     cases = [(lambda: call(wa=None), inv), (lambda: call(xa=None), inv), (lambda: call(ya=None), inv), (lambda: call(wa=w.address + 8), mis),
              (lambda: call(xa=x8.address + 4), mis), (lambda: call(ya=y.data_ptr() + 2), mis), (lambda: call(st=7), inv), (lambda: call(ydt=2), randes.UNSUPPORTED_DTYPE),
@@ -264,7 +275,9 @@ def test_refusals():
              (lambda: randes.packed8_linear(x, w, y=y.t()), inv), (lambda: randes.Packed8Matrix(200, 256, inside), inv),
              (lambda: randes.Packed8Matrix(8, 100, inside[8:]), mis), (lambda: randes.Packed8Matrix(8, 100, inside.cpu()), inv),
              (lambda: w.unpack(out=torch.empty(8, 255, device="cuda")), inv),
-             (lambda: randes.randes_transpose_eight(w.address, 8, 256, w.address, s), inv)]
+             (lambda: randes.randes_transpose_eight(w.address, 8, 256, w.address, s), inv), (lambda: typed(x, st=255), inv), (lambda: typed(x.data_ptr() + 2), mis),
+             (lambda: typed(x, dt=3), randes.UNSUPPORTED_DTYPE), (lambda: typed(y, n=1), inv), (lambda: typed(many, n=17), randes.WORKSPACE_TOO_SMALL),
+             (lambda: typed(many, n=17, ws=many), inv)]
     for i, (f, code) in enumerate(cases):
         with pytest.raises(randes.RandesError) as e:
             f()
