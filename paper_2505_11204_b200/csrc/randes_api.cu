@@ -2134,7 +2134,7 @@ int randes_rms_norm_impl(const randes_rms_norm_t* p, void* stream)
     if (a.rows == 0) return RANDES_OK;
     const size_t elem = elem_size(a.dtype), bytes8 = randes_packed_eight_bytes(a.rows, a.cols);
     const NormTensor x{a.x, a.x_stride, "x"}, res{a.residual, a.residual_stride, "the residual"}, h{a.h, a.h_stride, "h"}, y{a.y, a.y_stride, "y"};
-    bool vec = true;
+    bool vec = reinterpret_cast<uintptr_t>(a.gain) % 16 == 0;
     for (const NormTensor* t : {&x, &res, &h, &y}) {
         if (!t->p && t != &x) continue;
         if ((rc = check_tensor(t->p, a.rows, a.cols, t->stride, elem, t->name))) return rc;

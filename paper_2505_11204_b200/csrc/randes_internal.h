@@ -388,7 +388,7 @@ struct NormArgs {
     float* rstd;                  // or NULL
     uint64_t x_stride, residual_stride, h_stride, y_stride;
     uint32_t rows, cols;
-    uint32_t vec;                 // rows of x, residual, h and y are 16-byte aligned
+    uint32_t vec;                 // rows of x, residual, h and y, and the gain, are 16-byte aligned
     uint32_t gain_bf16;
     float eps;
 };

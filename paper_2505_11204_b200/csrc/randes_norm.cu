@@ -6,12 +6,14 @@
 // gradient of x and of r alike, dh what reaches h past the norm. Sums run in fp32; a sum of squares that leaves fp32 is taken
 // again in fp64.
 //
-// One pass: a row stays in registers, eight neighbouring columns to a thread and step, between the loads and the sum's return,
-// so 16 neighbouring lanes hold a block of 128 columns and its scale in eight bits is four shuffles away.
+// Forward: a row stays in registers between the loads and the sum's return, eight columns to a thread and run -- neighbours
+// where rows start on 16-byte boundaries (OCTETS), so that 16 lanes hold a block of 128 columns; else 32 apart, so that a warp's
+// accesses are whole whatever the row's alignment.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "randes_packed8.cuh"
@@ -28,10 +30,28 @@ __device__ __forceinline__ float gain_at(const void* gain, bool bf, uint32_t c)
 {
     return bf ? Store<bf16>::load1(static_cast<const bf16*>(gain) + c) : __ldg(static_cast<const float*>(gain) + c);
 }
-__device__ __forceinline__ void load_gain(const void* gain, bool bf, uint32_t c, uint32_t cols, float (&v)[8])
+// the gain of a lane's columns of a run that starts at `first`; ones without a gain
+template <bool OCTETS> __device__ __forceinline__ void load_gain(const void* gain, bool bf, uint32_t first, uint32_t cols, int lane, float (&v)[8])
 {
+    const uint32_t c = first + 8 * lane;
+    if (OCTETS && gain && c + 8 <= cols) {
+        if (bf) {
+            Octet<bf16> o;
+            o.w[0] = __ldg(reinterpret_cast<const uint4*>(static_cast<const bf16*>(gain) + c));
+            widen(o, v);
+        } else {
+            Octet<float> o;
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) v[e] = gain && c + e < cols ? gain_at(gain, bf, c + e) : 1.f;
+            for (int h = 0; h < 2; ++h) o.w[h] = __ldg(reinterpret_cast<const uint4*>(static_cast<const float*>(gain) + c) + h);
+            widen(o, v);
+        }
+        return;
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+        const uint32_t at = OCTETS ? c + e : first + 32 * e + lane;
+        v[e] = gain && at < cols ? gain_at(gain, bf, at) : 1.f;
+    }
 }
 
 template <typename V> __device__ __forceinline__ V warp_sum(V v)
@@ -54,75 +74,69 @@ template <int THREADS, typename V> __device__ __forceinline__ V row_sum(V v, V* 
     return all;
 }
 
-// A row's columns 8 (k THREADS + t) .. + 7, k < CHUNKS, all loads before the first use.
-template <typename T, int THREADS, int CHUNKS>
-__device__ __forceinline__ void load_row(const T* row, bool vec, uint32_t cols, int t, float* scratch, float (&v)[CHUNKS][8])
-{
-    const int lane = t & 31;
-    if (vec) {
-        Octet<T> o[CHUNKS];
+// A row's runs first(k) = 8 (k THREADS + warp's first thread), all loads before the first use.
+template <typename T, int THREADS, int CHUNKS, bool OCTETS> struct Row {
+    Octet<T> o[OCTETS ? CHUNKS : 1];
+    float f[OCTETS ? 1 : CHUNKS][8];
+    __device__ __forceinline__ void load(const T* row, uint32_t cols, int t)
+    {
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) o[k] = load_octet(row, (k * THREADS + t) * 8, cols);
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) widen(o[k], v[k]);
-    } else {
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) load_loose(row, (k * THREADS + t) * 8, cols, lane, v[k]);
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) turn_in(v[k], scratch, lane);
+        for (int k = 0; k < CHUNKS; ++k) {
+            const uint32_t first = (k * THREADS + (t & ~31)) * 8;
+            if (OCTETS) o[OCTETS ? k : 0] = load_octet(row, first + 8 * (t & 31), cols);
+            else load_strided(row, first, cols, t & 31, f[OCTETS ? 0 : k]);
+        }
     }
-}
-template <typename T> __device__ __forceinline__ void store_chunk(T* row, bool vec, uint32_t c, uint32_t cols, const float (&v)[8], float* scratch, int lane)
-{
-    if (vec) store_octet(row, c, cols, v);
-    else store_loose(row, c, cols, v, scratch, lane);
-}
-// Eight columns into eight bits: the block's scale from its 16 lanes.
-__device__ __forceinline__ void store8(char* dst, const Packed8Layout& lay, uint32_t r, uint32_t c, const float (&v)[8], int lane)
-{
-    uint32_t amax = 0;
+    __device__ __forceinline__ void get(int k, float (&v)[8]) const
+    {
+        if (OCTETS) widen(o[OCTETS ? k : 0], v);
+        else
 #pragma unroll
-    for (int e = 0; e < 8; ++e) amax = max_bits(amax, magnitude(v[e]));
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) amax = max_bits(amax, __shfl_xor_sync(~0u, amax, o));
-    const uint32_t kb = c >> 7, e = block_scale(amax);
-    if (kb >= lay.col_blocks) return;
-    *reinterpret_cast<uint2*>(dst + lay.tile(r >> 7, kb) + code_at(r, c)) = codes8(v, amax, e);
-    if ((lane & 15) == 0) dst[lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)] = static_cast<char>(e);
+            for (int e = 0; e < 8; ++e) v[e] = f[OCTETS ? 0 : k][e];
+    }
+};
+template <bool OCTETS, typename T> __device__ __forceinline__ void store_run(T* row, uint32_t first, uint32_t cols, const float (&v)[8], int lane)
+{
+    if (OCTETS) store_octet(row, first + 8 * lane, cols, v);
+    else store_strided(row, first, cols, lane, v);
 }
 
-template <typename T, int THREADS, int CHUNKS>
+template <typename T, int THREADS, int CHUNKS, bool OCTETS>
 __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(const NormArgs a)
 {
     constexpr int kWarps = THREADS * kRowsPerCta<THREADS> / 32;
-    __shared__ __align__(16) float s_scratch[kWarps][256];
     __shared__ float s_part[THREADS == 32 ? 1 : kWarps];
     __shared__ double s_part64[THREADS == 32 ? 1 : kWarps];
     const int t = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x, lane = t & 31;
     const uint32_t r = THREADS == 32 ? blockIdx.x * kRowsPerCta<THREADS> + (threadIdx.x >> 5) : blockIdx.x;
     if (THREADS == 32 && r >= a.rows) return;
-    float* scratch = s_scratch[threadIdx.x >> 5];
     const uint32_t cols = a.cols;
     const Packed8Layout lay(a.rows, cols);
 
     float v[CHUNKS][8];
-    load_row<T, THREADS, CHUNKS>(static_cast<const T*>(a.x) + r * a.x_stride, a.vec, cols, t, scratch, v);
-    if (a.residual) {
-        float d[CHUNKS][8];
-        load_row<T, THREADS, CHUNKS>(static_cast<const T*>(a.residual) + r * a.residual_stride, a.vec, cols, t, scratch, d);
+    {
+        Row<T, THREADS, CHUNKS, OCTETS> x, d;
+        x.load(static_cast<const T*>(a.x) + r * a.x_stride, cols, t);
+        if (a.residual) d.load(static_cast<const T*>(a.residual) + r * a.residual_stride, cols, t);
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
+            x.get(k, v[k]);
+            if (a.residual) {
+                float u[8];
+                d.get(k, u);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[k][e] += d[k][e];
-            widen(narrow<T>(v[k]), v[k]);                   // what is stored is what is normed
+                for (int e = 0; e < 8; ++e) v[k][e] += u[e];
+                if (sizeof(T) == 2) widen(narrow<T>(v[k]), v[k]);      // what is stored is what is normed
+            }
         }
     }
     float ss = 0.f;
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
-        const uint32_t c = (k * THREADS + t) * 8;
-        if (a.h && c - 8 * lane < cols) store_chunk(static_cast<T*>(a.h) + r * a.h_stride, a.vec, c, cols, v[k], scratch, lane);
-        if (a.kept8) store8(static_cast<char*>(a.kept8), lay, r, c, v[k], lane);
+        const uint32_t first = (k * THREADS + (t & ~31)) * 8;
+        if (first >= cols) break;                           // the same for a warp
+        if (a.h) store_run<OCTETS>(static_cast<T*>(a.h) + r * a.h_stride, first, cols, v[k], lane);
+        if (a.kept8) store_scales(static_cast<char*>(a.kept8), lay, r, first, pack_run<OCTETS>(static_cast<char*>(a.kept8), lay, r, first, v[k], lane), lane);
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = __fmaf_rn(v[k][e], v[k][e], ss);
     }
@@ -139,33 +153,36 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
         s = __frsqrt_rn(ss / cols + a.eps);
     }
     if (a.rstd && t == 0) a.rstd[r] = s;
+    if (!a.y && !a.y8) return;
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
-        const uint32_t c = (k * THREADS + t) * 8;
-        if (c - 8 * lane >= cols) break;                    // the same for a warp
+        const uint32_t first = (k * THREADS + (t & ~31)) * 8;
+        if (first >= cols) break;
         float w[8];
-        load_gain(a.gain, a.gain_bf16, c, cols, w);
+        load_gain<OCTETS>(a.gain, a.gain_bf16, first, cols, lane, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = c + e < cols ? v[k][e] * s * w[e] : 0.f;      // (0 * NaN behind the row's end would spoil the block)
-        if (a.y) store_chunk(static_cast<T*>(a.y) + r * a.y_stride, a.vec, c, cols, w, scratch, lane);
-        if (a.y8) store8(static_cast<char*>(a.y8), lay, r, c, w, lane);
+        for (uint32_t e = 0; e < 8; ++e) {
+            w[e] = v[k][e] * s * w[e];
+            if (first + 256 > cols && first + (OCTETS ? 8 * lane + e : 32 * e + lane) >= cols) w[e] = 0.f;      // (0 * NaN behind the row's end would spoil the block)
+        }
+        if (a.y) store_run<OCTETS>(static_cast<T*>(a.y) + r * a.y_stride, first, cols, w, lane);
+        if (a.y8) store_scales(static_cast<char*>(a.y8), lay, r, first, pack_run<OCTETS>(static_cast<char*>(a.y8), lay, r, first, w, lane), lane);
     }
 }
 
 // A CTA walks rows and keeps its share of dgain in registers; the shares of all CTAs are added in a fixed order by a second kernel.
-template <typename T, int THREADS, int CHUNKS>
+template <typename T, int THREADS, int CHUNKS, bool OCTETS>
 __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_grad_kernel(const NormGradArgs a)
 {
     constexpr int kWarps = THREADS * kRowsPerCta<THREADS> / 32;
     constexpr int kSum = THREADS == 32 ? 256 * CHUNKS : 1;
-    __shared__ __align__(16) float s_scratch[kWarps][256];
     __shared__ float s_part[2][THREADS == 32 ? 1 : kWarps];
     __shared__ float s_sum[kSum];
     const int t = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x, lane = t & 31;
-    float* scratch = s_scratch[threadIdx.x >> 5];
     const uint32_t cols = a.cols;
     const Packed8Layout lay(a.rows, cols);
     const uint32_t step = gridDim.x * kRowsPerCta<THREADS>;
+    auto column = [&](int k, uint32_t e) { return (k * THREADS + (t & ~31)) * 8 + (OCTETS ? 8 * lane + e : 32 * e + lane); };
     float sum[CHUNKS][8] = {};
     uint32_t turn = 0;
     for (uint32_t r = blockIdx.x * kRowsPerCta<THREADS> + (THREADS == 32 ? threadIdx.x >> 5 : 0); r < a.rows; r += step, turn ^= 1) {
@@ -175,28 +192,52 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_grad_kerne
             const char* src = static_cast<const char*>(a.kept8);
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
-                const uint32_t c = (k * THREADS + t) * 8, kb = c >> 7;
-                uint2 w = make_uint2(0, 0);
-                uint32_t e = 0;
-                if (kb < lay.col_blocks) {
-                    w = __ldcs(reinterpret_cast<const uint2*>(src + lay.tile(r >> 7, kb) + code_at(r, c)));
-                    e = __ldg(reinterpret_cast<const unsigned char*>(src + lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)));
-                }
-                values4(w.x, block_unit(e), n[k]);
-                values4(w.y, block_unit(e), n[k] + 4);
-                if (c + 8 > cols)
+                const uint32_t first = (k * THREADS + (t & ~31)) * 8;
+                if (OCTETS) {
+                    const uint32_t c = first + 8 * lane, kb = c >> 7;
+                    uint2 w = make_uint2(0, 0);
+                    uint32_t e = 0;
+                    if (kb < lay.col_blocks) {
+                        w = __ldcs(reinterpret_cast<const uint2*>(src + lay.tile(r >> 7, kb) + code_at(r, c)));
+                        e = __ldg(reinterpret_cast<const unsigned char*>(src + lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)));
+                    }
+                    values4(w.x, block_unit(e), n[k]);
+                    values4(w.y, block_unit(e), n[k] + 4);
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) n[k][j] = c + j < cols ? n[k][j] : 0.f;      // (codes behind the row's end may be NaN)
+                    for (uint32_t b = 0; b < 2; ++b) {
+                        const uint32_t kb = (first >> 7) + b;
+                        uint32_t w = 0, e = 0;
+                        if (kb < lay.col_blocks) {
+                            const unsigned char* from = reinterpret_cast<const unsigned char*>(src) + lay.tile(r >> 7, kb) + (r & 127) * 128 + (lane & 15);
+#pragma unroll
+                            for (uint32_t j = 0; j < 4; ++j) w |= static_cast<uint32_t>(__ldg(from + (((2 * j + (lane >> 4)) ^ (r & 7)) << 4))) << (8 * j);
+                            e = __ldg(reinterpret_cast<const unsigned char*>(src + lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)));
+                        }
+                        values4(w, block_unit(e), n[k] + 4 * b);
+                    }
+                }
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e)
+                    if (first + 256 > cols && column(k, e) >= cols) n[k][e] = 0.f;      // (codes behind the row's end may be NaN)
             }
         } else {
-            load_row<T, THREADS, CHUNKS>(static_cast<const T*>(a.h) + r * a.h_stride, a.vec, cols, t, scratch, n);
+            Row<T, THREADS, CHUNKS, OCTETS> h;
+            h.load(static_cast<const T*>(a.h) + r * a.h_stride, cols, t);
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) h.get(k, n[k]);
         }
-        load_row<T, THREADS, CHUNKS>(static_cast<const T*>(a.dy) + r * a.dy_stride, a.vec, cols, t, scratch, g);
+        {
+            Row<T, THREADS, CHUNKS, OCTETS> dy;
+            dy.load(static_cast<const T*>(a.dy) + r * a.dy_stride, cols, t);
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) dy.get(k, g[k]);
+        }
         float inner = 0.f;
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
             float w[8];
-            load_gain(a.gain, a.gain_bf16, (k * THREADS + t) * 8, cols, w);
+            load_gain<OCTETS>(a.gain, a.gain_bf16, (k * THREADS + (t & ~31)) * 8, cols, lane, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 n[k][e] *= s;
@@ -208,24 +249,20 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_grad_kerne
         inner = row_sum<THREADS>(inner, s_part[turn], t) / cols;
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
-            const uint32_t c = (k * THREADS + t) * 8;
-            if (c - 8 * lane >= cols) break;
+            const uint32_t first = (k * THREADS + (t & ~31)) * 8;
+            if (first >= cols) break;
             float d[8];
             if (a.dh) {
                 const T* row = static_cast<const T*>(a.dh) + r * a.dh_stride;
-                if (a.vec) {
-                    widen(load_octet(row, c, cols), d);
-                } else {
-                    load_loose(row, c, cols, lane, d);
-                    turn_in(d, scratch, lane);
-                }
+                if (OCTETS) widen(load_octet(row, first + 8 * lane, cols), d);
+                else load_strided(row, first, cols, lane, d);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float v = s * __fmaf_rn(-n[k][e], inner, g[k][e]);
                 d[e] = a.dh ? v + d[e] : v;
             }
-            store_chunk(static_cast<T*>(a.dx) + r * a.dx_stride, a.vec, c, cols, d, scratch, lane);
+            store_run<OCTETS>(static_cast<T*>(a.dx) + r * a.dx_stride, first, cols, d, lane);
         }
     }
     if (!a.dgain) return;
@@ -238,21 +275,180 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_grad_kerne
             for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float& to = s_sum[e * 32 * CHUNKS + k * 32 + lane];
+                    float& to = s_sum[(e * CHUNKS + k) * 32 + lane];
                     to = w ? to + sum[k][e] : sum[k][e];
                 }
         }
         __syncthreads();
-        for (uint32_t c = threadIdx.x; c < cols; c += THREADS * kRowsPerCta<THREADS>)
-            out[c] = s_sum[(c & 7) * 32 * CHUNKS + (c >> 3)];
+        for (uint32_t c = threadIdx.x; c < cols; c += THREADS * kRowsPerCta<THREADS>) {
+            const uint32_t k = c >> 8, e = OCTETS ? c & 7 : (c >> 5) & 7, l = OCTETS ? (c >> 3) & 31 : c & 31;
+            out[c] = s_sum[(e * CHUNKS + k) * 32 + l];
+        }
     } else {
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t c = (k * THREADS + t) * 8 + e;
-                if (c < cols) out[c] = sum[k][e];
+            for (int e = 0; e < 8; ++e)
+                if (column(k, e) < cols) out[column(k, e)] = sum[k][e];
+    }
+}
+
+// The same where rows start on 16-byte boundaries and have up to 8192 columns. What bounds the form above is that a row's loads, its
+// sum and its stores follow one another; here the rows to come are on their way into shared memory meanwhile, each thread copying
+// what it will read itself (so that nothing has to be waited for but its own copies): 16 columns of dy, h and dh, the scales
+// and the root of the row. TEAM threads to a row.
+template <typename T, int TEAM> struct GradRing {
+    static constexpr int kThreads = TEAM < 256 ? 256 : TEAM, kRows = kThreads / TEAM;
+    static constexpr int kWords = sizeof(T);                                    // 16-byte words of 16 columns
+    static constexpr uint32_t kSlot = kThreads * 16;
+    static constexpr uint32_t kStage = 3 * kWords * kSlot + 2 * kThreads * 4;   // dy, h, dh; scales, rstd
+    static constexpr int kPerSm = kThreads == 256 ? 2 : 1;
+    static constexpr uint32_t kDepth = 220 * 1024 / kPerSm / kStage > 4 ? 4 : 220 * 1024 / kPerSm / kStage;
+    static constexpr size_t kSmem = kDepth * kStage;
+};
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, uint32_t bytes)      // the rest of the 16 bytes reads zero
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
+
+template <typename T, int TEAM>
+__global__ void __launch_bounds__(GradRing<T, TEAM>::kThreads, GradRing<T, TEAM>::kPerSm) norm_grad_ring_kernel(const NormGradArgs a)
+{
+    typedef GradRing<T, TEAM> G;
+    constexpr int kWarps = G::kThreads / 32;
+    extern __shared__ __align__(16) unsigned char s_ring[];
+    __shared__ float s_part[2][kWarps];
+    const int tid = threadIdx.x, t = tid % TEAM, team = tid / TEAM;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring));
+    const uint32_t cols = a.cols, c = t * 16, kb = c >> 7;
+    const Packed8Layout lay(a.rows, cols);
+    const bool kept = a.kept8 != nullptr, in = kb < lay.col_blocks;
+    const uint32_t step = gridDim.x * G::kRows;
+    auto bytes_at = [&](int w) {      // of a 16-byte word of the lane's columns, how many exist
+        const uint32_t at = c + w * (16 / sizeof(T));
+        return at < cols ? min(16u, (cols - at) * static_cast<uint32_t>(sizeof(T))) : 0u;
+    };
+    auto fetch = [&](uint32_t r, uint32_t slot) {
+        if (r < a.rows) {
+            const uint32_t at = ring + slot * G::kStage + tid * 16;
+            auto row = [&](const void* p, uint64_t stride, uint32_t first) {
+                const T* from = static_cast<const T*>(p) + r * stride;
+#pragma unroll
+                for (int w = 0; w < G::kWords; ++w) {
+                    const uint32_t n = bytes_at(w);
+                    copy16(at + (first + w) * G::kSlot, n ? from + c + w * (16 / sizeof(T)) : from, n);
+                }
+            };
+            row(a.dy, a.dy_stride, 0);
+            if (a.dh) row(a.dh, a.dh_stride, 2 * G::kWords);
+            const uint32_t word = ring + slot * G::kStage + 3 * G::kWords * G::kSlot + tid * 4;
+            if (kept) {
+                const char* src = static_cast<const char*>(a.kept8);
+                copy16(at + G::kWords * G::kSlot, in ? src + lay.tile(r >> 7, kb) + code_at(r, c) : src, in ? 16u : 0u);
+                if (in) copy4(word, src + lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r));
+            } else {
+                row(a.h, a.h_stride, G::kWords);
             }
+            copy4(word + G::kThreads * 4, a.rstd + r);
+        }
+        cp_async_commit();
+    };
+    auto words = [&](uint32_t slot, uint32_t first, float (&v)[16]) {
+        const uint32_t at = ring + slot * G::kStage + first * G::kSlot + tid * 16;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Octet<T> o;
+#pragma unroll
+            for (int w = 0; w < G::kWords / 2; ++w) o.w[w] = lds128(at + (h * (G::kWords / 2) + w) * G::kSlot);
+            float u[8];
+            widen(o, u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[8 * h + e] = u[e];
+        }
+    };
+
+    float gain[16], sum[16] = {};
+#pragma unroll
+    for (uint32_t e = 0; e < 16; ++e) gain[e] = a.gain && c + e < cols ? gain_at(a.gain, a.gain_bf16, c + e) : 1.f;
+    uint32_t r = blockIdx.x * G::kRows + team, slot = 0, turn = 0;
+#pragma unroll
+    for (uint32_t i = 0; i + 1 < G::kDepth; ++i) fetch(r + i * step, i);
+    // the rows of a CTA's teams end together or one apart: all teams of a CTA take part in its last round
+    for (uint32_t r0 = blockIdx.x * G::kRows; r0 < a.rows; r0 += step, r += step, turn ^= 1) {
+        fetch(r + (G::kDepth - 1) * step, slot == 0 ? G::kDepth - 1 : slot - 1);
+        cp_async_wait<static_cast<int>(G::kDepth) - 1>();
+        float n[16], g[16], inner = 0.f, s = 0.f;
+        if (r < a.rows) {
+            const uint32_t word = ring + slot * G::kStage + 3 * G::kWords * G::kSlot + tid * 4;
+            s = __uint_as_float(lds_u32(word + G::kThreads * 4));
+            if (kept) {
+                const uint4 w = lds128(ring + slot * G::kStage + G::kWords * G::kSlot + tid * 16);
+                const float unit = in ? block_unit((lds_u32(word) >> (8 * (kb & 3))) & 0xFFu) : 0.f;
+                values4(w.x, unit, n);
+                values4(w.y, unit, n + 4);
+                values4(w.z, unit, n + 8);
+                values4(w.w, unit, n + 12);
+                if (c + 16 > cols)
+#pragma unroll
+                    for (uint32_t e = 0; e < 16; ++e) n[e] = c + e < cols ? n[e] : 0.f;      // (codes behind the row's end may be NaN)
+            } else {
+                words(slot, G::kWords, n);
+            }
+            words(slot, 0, g);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                n[e] *= s;
+                sum[e] = __fmaf_rn(g[e], n[e], sum[e]);
+                g[e] *= gain[e];
+                inner = __fmaf_rn(g[e], n[e], inner);
+            }
+        }
+        inner = warp_sum(inner);
+        if (TEAM > 32) {
+            if ((tid & 31) == 0) s_part[turn][tid >> 5] = inner;
+            __syncthreads();
+            inner = 0.f;
+#pragma unroll
+            for (int w = 0; w < TEAM / 32; ++w) inner += s_part[turn][team * (TEAM / 32) + w];
+        }
+        inner /= cols;
+        if (r < a.rows) {
+            float d[16];
+            if (a.dh) words(slot, 2 * G::kWords, d);
+            T* row = static_cast<T*>(a.dx) + r * a.dx_stride;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = s * __fmaf_rn(-n[8 * h + e], inner, g[8 * h + e]);
+                    u[e] = a.dh ? v + d[8 * h + e] : v;
+                }
+                if (c + 8 * h < cols) store_octet(row, c + 8 * h, cols, u);
+            }
+        }
+        slot = slot + 1 == G::kDepth ? 0 : slot + 1;
+    }
+    if (!a.dgain) return;
+    cp_async_wait<0>();
+    float* out = a.partial + static_cast<size_t>(blockIdx.x) * cols;
+    float* shares = reinterpret_cast<float*>(s_ring);      // [team][column], 17 words to 16 columns
+    if (G::kRows > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) shares[tid * 17 + e] = sum[e];
+        __syncthreads();
+        for (uint32_t at = tid; at < cols; at += G::kThreads) {
+            float v = 0.f;
+#pragma unroll
+            for (int k = 0; k < G::kRows; ++k) v += shares[(k * TEAM + (at >> 4)) * 17 + (at & 15)];
+            out[at] = v;
+        }
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 16; ++e)
+            if (c + e < cols) out[c + e] = sum[e];
     }
 }
 
@@ -273,59 +469,101 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_gain_kernel(const float* p
     }
 }
 
-template <typename T, int THREADS, int CHUNKS> int run_norm(const NormArgs& a, cudaStream_t stream)
-{
-    constexpr uint32_t kRows = kRowsPerCta<THREADS>;
-    norm_kernel<T, THREADS, CHUNKS><<<(a.rows + kRows - 1) / kRows, THREADS * kRows, 0, stream>>>(a);
-    return static_cast<int>(cudaGetLastError());
-}
+template <int V> using Const = std::integral_constant<int, V>;
 // Calls f with the row's form: threads to a row and runs of 8 columns per thread.
 template <typename F> int by_width(uint32_t cols, F&& f)
 {
-    if (cols <= 256) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
-    if (cols <= 512) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 2>());
-    if (cols <= 1024) return f(std::integral_constant<int, 32>(), std::integral_constant<int, 4>());
-    if (cols <= 2048) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-    if (cols <= 4096) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-    if (cols <= 8192) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
-    if (cols <= 16384) return f(std::integral_constant<int, 512>(), std::integral_constant<int, 4>());
-    return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
+    if (cols <= 256) return f(Const<32>(), Const<1>());
+    if (cols <= 512) return f(Const<32>(), Const<2>());
+    if (cols <= 1024) return f(Const<32>(), Const<4>());
+    if (cols <= 2048) return f(Const<256>(), Const<1>());
+    if (cols <= 4096) return f(Const<256>(), Const<2>());
+    if (cols <= 8192) return f(Const<256>(), Const<4>());
+    if (cols <= 16384) return f(Const<512>(), Const<4>());
+    return f(Const<1024>(), Const<4>());
 }
 // CTAs that walk the rows of a backward pass: the rows, or what the 148 SMs hold at a time (a constant, so that sums are the same
 // on every device and the workspace is known without one).
+constexpr uint32_t kSms = 148;
 uint32_t grad_ctas(uint32_t rows, uint32_t cols)
 {
     const uint32_t per_sm = cols <= 1024 ? 8 : (cols <= 4096 ? 4 : (cols <= 8192 ? 2 : 1));
-    const uint32_t ctas = cols <= 1024 ? (rows + 3) / 4 : rows;
-    return std::min(ctas, per_sm * 148u);
+    return std::min(cols <= 1024 ? (rows + 3) / 4 : rows, per_sm * kSms);
+}
+constexpr uint32_t kRingCols = 8192;
+template <typename T, int TEAM> uint32_t ring_ctas(uint32_t rows)
+{
+    typedef GradRing<T, TEAM> G;
+    return std::min<uint32_t>((rows + G::kRows - 1) / G::kRows, G::kPerSm * kSms);
+}
+
+constexpr int kDevices = 64;
+template <typename T, int TEAM> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
+{
+    typedef GradRing<T, TEAM> G;
+    static std::atomic<bool> granted[kDevices];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return static_cast<int>(e);
+    if (device >= kDevices || !granted[device].load(std::memory_order_relaxed)) {
+        e = cudaFuncSetAttribute(norm_grad_ring_kernel<T, TEAM>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(G::kSmem));
+        if (e != cudaSuccess) return static_cast<int>(e);
+        if (device < kDevices) granted[device].store(true, std::memory_order_relaxed);
+    }
+    *ctas = ring_ctas<T, TEAM>(a.rows);
+    norm_grad_ring_kernel<T, TEAM><<<*ctas, G::kThreads, G::kSmem, stream>>>(a);
+    return static_cast<int>(cudaGetLastError());
+}
+template <typename T> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
+{
+    if (a.cols <= 512) return run_ring<T, 32>(a, ctas, stream);
+    if (a.cols <= 1024) return run_ring<T, 64>(a, ctas, stream);
+    if (a.cols <= 2048) return run_ring<T, 128>(a, ctas, stream);
+    if (a.cols <= 4096) return run_ring<T, 256>(a, ctas, stream);
+    return run_ring<T, 512>(a, ctas, stream);
+}
+
+template <bool OCTETS> int run_norm(int dtype, const NormArgs& a, cudaStream_t stream)
+{
+    return by_width(a.cols, [&](auto threads, auto chunks) {
+        constexpr int T = decltype(threads)::value, C = decltype(chunks)::value, R = kRowsPerCta<T>;
+        const uint32_t ctas = a.rows / R + (a.rows % R != 0);
+        if (dtype) norm_kernel<bf16, T, C, OCTETS><<<ctas, T * R, 0, stream>>>(a);
+        else norm_kernel<float, T, C, OCTETS><<<ctas, T * R, 0, stream>>>(a);
+        return static_cast<int>(cudaGetLastError());
+    });
+}
+template <bool OCTETS> int run_grad(int dtype, const NormGradArgs& a, uint32_t ctas, cudaStream_t stream)
+{
+    return by_width(a.cols, [&](auto threads, auto chunks) {
+        constexpr int T = decltype(threads)::value, C = decltype(chunks)::value;
+        if constexpr (!OCTETS || T >= 512) {      // (narrower rows on 16-byte boundaries take the ring)
+            if (dtype) norm_grad_kernel<bf16, T, C, OCTETS><<<ctas, T * kRowsPerCta<T>, 0, stream>>>(a);
+            else norm_grad_kernel<float, T, C, OCTETS><<<ctas, T * kRowsPerCta<T>, 0, stream>>>(a);
+        }
+        return static_cast<int>(cudaGetLastError());
+    });
 }
 
 }  // namespace
 
 int launch_norm(int dtype, const NormArgs& a, void* stream)
 {
-    return by_width(a.cols, [&](auto threads, auto chunks) {
-        constexpr int T = decltype(threads)::value, C = decltype(chunks)::value;
-        return dtype ? run_norm<bf16, T, C>(a, static_cast<cudaStream_t>(stream)) : run_norm<float, T, C>(a, static_cast<cudaStream_t>(stream));
-    });
+    return a.vec ? run_norm<true>(dtype, a, static_cast<cudaStream_t>(stream)) : run_norm<false>(dtype, a, static_cast<cudaStream_t>(stream));
 }
 
 size_t norm_grad_workspace(uint32_t rows, uint32_t cols)
 {
-    return static_cast<size_t>(grad_ctas(rows, cols)) * cols * sizeof(float);
+    return static_cast<size_t>(std::max(grad_ctas(rows, cols), std::min(rows, 2 * kSms))) * cols * sizeof(float);
 }
 
 int launch_norm_grad(int dtype, const NormGradArgs& a, int* launched, void* stream)
 {
     *launched = 0;
-    const uint32_t ctas = grad_ctas(a.rows, a.cols);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int e = by_width(a.cols, [&](auto threads, auto chunks) {
-        constexpr int T = decltype(threads)::value, C = decltype(chunks)::value;
-        if (dtype) norm_grad_kernel<bf16, T, C><<<ctas, T * kRowsPerCta<T>, 0, s>>>(a);
-        else norm_grad_kernel<float, T, C><<<ctas, T * kRowsPerCta<T>, 0, s>>>(a);
-        return static_cast<int>(cudaGetLastError());
-    });
+    uint32_t ctas = grad_ctas(a.rows, a.cols);
+    const int e = a.vec && a.cols <= kRingCols ? (dtype ? run_ring<bf16>(a, &ctas, s) : run_ring<float>(a, &ctas, s))
+                                               : (a.vec ? run_grad<true>(dtype, a, ctas, s) : run_grad<false>(dtype, a, ctas, s));
     if (e) return e;
     *launched = 1;
     if (!a.dgain) return 0;

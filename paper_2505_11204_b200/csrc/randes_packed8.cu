@@ -35,70 +35,84 @@ template <typename Args> __device__ __forceinline__ uint32_t matrix_of(const Arg
     return i;
 }
 
-// A warp takes rows r0 .. r0 + 3 of 512 columns: two runs of 256, lane l holding columns 8 l .. 8 l + 7 of either.
-template <typename T, typename M, bool RETRIEVE, uint32_t BATCH>
+// Four rows of a warp's run of 256 columns, every load before the first use. OCTETS: the rows start on 16-byte boundaries.
+template <typename T, bool OCTETS> struct Rows8 {
+    Octet<T> o[OCTETS ? kRows8 : 1];
+    float f[OCTETS ? 1 : kRows8][8];
+    __device__ __forceinline__ void load(const T* p, uint64_t stride, uint32_t n, uint32_t first, uint32_t cols, int lane)
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < kRows8; ++i)
+            if (i < n) {
+                if (OCTETS) o[OCTETS ? i : 0] = load_octet(p + i * stride, first + 8 * lane, cols);
+                else load_strided(p + i * stride, first, cols, lane, f[OCTETS ? 0 : i]);
+            }
+    }
+    __device__ __forceinline__ void get(uint32_t i, float (&v)[8]) const
+    {
+        if (OCTETS) widen(o[OCTETS ? i : 0], v);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = f[OCTETS ? 0 : i][e];
+    }
+};
+
+// A warp takes rows r0 .. r0 + 3 of 512 columns, two runs of 256; both are loaded at once where that takes 32 to 64 registers.
+template <typename T, typename M, bool RETRIEVE, bool OCTETS, uint32_t BATCH>
 __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_constant__ Pack8Batch<BATCH> a)
 {
-    __shared__ __align__(16) float s_scratch[kWarps8][256];
+    constexpr bool kBoth = OCTETS && sizeof(T) + (RETRIEVE ? sizeof(M) : 0) <= 4;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Pack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
     const Packed8Layout lay(m.rows, m.cols);
-    const uint32_t cta = blockIdx.x - m.first_cta, rb = cta / lay.groups, g = cta - rb * lay.groups;
-    const uint32_t r0 = rb * kCtaRows8 + warp * kRows8, cols = m.cols;
+    const uint32_t cta = blockIdx.x - m.first_cta, rb = cta / lay.groups, g = cta - rb * lay.groups, r0 = rb * kCtaRows8 + warp * kRows8;
     if (r0 >= m.rows) return;
-    const uint32_t n = min(kRows8, m.rows - r0);
+    const uint32_t n = min(kRows8, m.rows - r0), cols = m.cols;
     char* dst = static_cast<char*>(m.dst);
+    const T* src = static_cast<const T*>(m.src) + r0 * m.stride;
+    const M* add = RETRIEVE ? static_cast<const M*>(m.m) + static_cast<uint64_t>(r0) * cols : nullptr;
     uint32_t word[kRows8] = {};
+    Rows8<T, OCTETS> w[kBoth ? 2 : 1];
+    Rows8<M, OCTETS> d[RETRIEVE && kBoth ? 2 : 1];
+    auto load = [&](uint32_t half) {
+        const uint32_t first = g * 512 + half * 256;
+        if (first >= cols) return;
+        w[kBoth ? half : 0].load(src, m.stride, n, first, cols, lane);
+        if (RETRIEVE) d[kBoth ? half : 0].load(add, cols, n, first, cols, lane);
+    };
+    load(0);
+    if (kBoth) load(1);
 #pragma unroll
     for (uint32_t half = 0; half < 2; ++half) {
-        const uint32_t c = g * 512 + half * 256 + lane * 8, kb = c >> 7;
-        if (g * 512 + half * 256 >= cols) break;
-        float v[kRows8][8];
-        auto read = [&](const auto* p, uint64_t stride, bool vec, float (&to)[kRows8][8]) {
-            typedef typename std::remove_const<typename std::remove_pointer<decltype(p)>::type>::type E;
-            if (vec) {
-                Octet<E> o[kRows8];
-#pragma unroll
-                for (uint32_t i = 0; i < kRows8; ++i)
-                    if (i < n) o[i] = load_octet(p + (r0 + i) * stride, c, cols);
-#pragma unroll
-                for (uint32_t i = 0; i < kRows8; ++i)
-                    if (i < n) widen(o[i], to[i]);
+        const uint32_t first = g * 512 + half * 256;
+        if (first >= cols) break;
+        if (!kBoth && half) load(1);
+        uint32_t bits = 0;      // of the lane's eight columns
+        if (RETRIEVE && m.flip) {
+            if (OCTETS) {
+                const uint32_t c = first + 8 * lane, q = (c >> 5) & 3;
+                const uint4 blk = philox4x32_10(c >> 7, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1);
+                bits = (q == 0 ? blk.x : (q == 1 ? blk.y : (q == 2 ? blk.z : blk.w))) >> (c & 31);
             } else {
 #pragma unroll
-                for (uint32_t i = 0; i < kRows8; ++i)
-                    if (i < n) load_loose(p + (r0 + i) * stride, c, cols, lane, to[i]);
-#pragma unroll
-                for (uint32_t i = 0; i < kRows8; ++i)
-                    if (i < n) turn_in(to[i], s_scratch[warp], lane);
+                for (uint32_t b = 0; b < 2; ++b) {
+                    const uint4 blk = philox4x32_10((first >> 7) + b, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1);
+                    bits |= ((blk.x >> lane & 1u) | (blk.y >> lane & 1u) << 1 | (blk.z >> lane & 1u) << 2 | (blk.w >> lane & 1u) << 3) << (4 * b);
+                }
             }
-        };
-        read(static_cast<const T*>(m.src), m.stride, m.vec & 1u, v);
-        if (RETRIEVE) {
-            float d[kRows8][8];
-            read(static_cast<const M*>(m.m), cols, m.vec & 2u, d);
-            uint32_t bits = 0;
-            if (m.flip) {
-                const uint4 blk = philox4x32_10(kb, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1);
-                const uint32_t q = (c >> 5) & 3;
-                bits = (q == 0 ? blk.x : (q == 1 ? blk.y : (q == 2 ? blk.z : blk.w))) >> (c & 31);
-            }
-#pragma unroll
-            for (uint32_t i = 0; i < kRows8; ++i)
-#pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) v[i][e] = __fmaf_rn(a.lambda, flip(d[i][e], (bits >> e) << 31), v[i][e]);
         }
 #pragma unroll
         for (uint32_t i = 0; i < kRows8; ++i) {
             if (i >= n) break;
-            uint32_t amax = 0;
+            float v[8];
+            w[kBoth ? half : 0].get(i, v);
+            if (RETRIEVE) {
+                float e[8];
+                d[RETRIEVE && kBoth ? half : 0].get(i, e);
 #pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) amax = max_bits(amax, magnitude(v[i][e]));
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) amax = max_bits(amax, __shfl_xor_sync(~0u, amax, o));
-            const uint32_t e = block_scale(amax), r = r0 + i;
-            if (kb < lay.col_blocks) *reinterpret_cast<uint2*>(dst + lay.tile(r >> 7, kb) + code_at(r, c)) = codes8(v[i], amax, e);
-            word[i] |= (__shfl_sync(~0u, e, 0) | (__shfl_sync(~0u, e, 16) << 8)) << (16 * half);
+                for (uint32_t k = 0; k < 8; ++k) v[k] = __fmaf_rn(a.lambda, flip(e[k], (bits >> k) << 31), v[k]);
+            }
+            word[i] |= pack_run<OCTETS>(dst, lay, r0 + i, first, v, lane) << (16 * half);
         }
     }
 #pragma unroll
@@ -109,7 +123,6 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
 
 template <typename T, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 * 32) unpack8_kernel(const __grid_constant__ Unpack8Batch<BATCH> a)
 {
-    __shared__ __align__(16) float s_scratch[kWarps8][256];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Unpack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
     const Packed8Layout lay(m.rows, m.cols);
@@ -137,29 +150,42 @@ template <typename T, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 
         T* row = static_cast<T*>(m.dst) + (r0 + i) * m.stride;
 #pragma unroll
         for (uint32_t half = 0; half < 2; ++half) {
-            const uint32_t c = g * 512 + half * 256 + lane * 8;
-            if (g * 512 + half * 256 >= cols) break;
+            const uint32_t first = g * 512 + half * 256, c = first + lane * 8;
+            if (first >= cols) break;
             float v[8];
-            const float unit = block_unit((word[i] >> (8 * ((c >> 7) & 3))) & 0xFFu);
-            values4(codes[half][i].x, unit, v);
-            values4(codes[half][i].y, unit, v + 4);
-            if (m.vec) store_octet(row, c, cols, v);
-            else store_loose(row, c, cols, v, s_scratch[warp], lane);
+            if (m.vec) {
+                const float unit = block_unit((word[i] >> (8 * ((c >> 7) & 3))) & 0xFFu);
+                values4(codes[half][i].x, unit, v);
+                values4(codes[half][i].y, unit, v + 4);
+                store_octet(row, c, cols, v);
+            } else {
+                // column l + 32 k lies in lane 4 k + l / 8, whose eight codes are 8 (l / 8) .. + 7 of that run
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) {
+                    const uint32_t from = 4 * k + (lane >> 3);
+                    const uint32_t x = __shfl_sync(~0u, codes[half][i].x, from), y = __shfl_sync(~0u, codes[half][i].y, from);
+                    float u[4];
+                    values4((lane & 4 ? y : x) >> (8 * (lane & 3)), block_unit((word[i] >> (16 * half + 8 * (k >> 2))) & 0xFFu), u);
+                    v[k] = u[0];
+                }
+                store_strided(row, first, cols, lane, v);
+            }
         }
     }
 }
 
-// A tile of 128 x 128 in blocks along its columns, and with BOTH in blocks along its rows too, out of one read. A thread holds 8 rows
-// x 8 columns; the greatest magnitudes of the columns meet in shared memory; the codes of a column are turned there, 8-byte pieces
-// exchanged by the column's octet so that neither the writes nor the reads meet in a bank.
-template <typename T> __device__ __forceinline__ void load_sub(const Turn8Args& a, uint32_t r0, uint32_t c, float* scratch, int lane, float (&v)[8][8])
+// A tile of 128 x 128 in blocks along its columns, and with BOTH in blocks along its rows too, out of one read. A thread holds rows
+// 8 rg .. 8 rg + 7 of eight columns: 8 l .. 8 l + 7 where rows start on 16-byte boundaries (OCTETS), else l, l + 16 ..
+// l + 112. The greatest magnitudes of the columns meet in shared memory; the codes of a column are turned there, 8-byte pieces
+// exchanged by a number that differs between the 16 lanes that write at a time, so that they do not meet in a bank.
+template <typename T, bool OCTETS> __device__ __forceinline__ void load_sub(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, float (&v)[8][8])
 {
     const T* src = static_cast<const T*>(a.src);
-    if (a.vec) {
+    if (OCTETS) {
         Octet<T> o[8];
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
-            if (r0 + i < a.rows) o[i] = load_octet(src + (r0 + i) * a.stride, c, a.cols);
+            if (r0 + i < a.rows) o[i] = load_octet(src + (r0 + i) * a.stride, c0 + 8 * l, a.cols);
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
             if (r0 + i < a.rows) widen(o[i], v[i]);
@@ -168,32 +194,20 @@ template <typename T> __device__ __forceinline__ void load_sub(const Turn8Args& 
                 for (uint32_t e = 0; e < 8; ++e) v[i][e] = 0.f;
         }
     } else {
-        // half a warp reads a row's 128 columns: 16 neighbours at a time
-        const uint32_t l = lane & 15, first = c - 8 * l;
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
 #pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) {
-                const uint32_t at = first + 16 * k + l;
-                v[i][k] = r0 + i < a.rows && at < a.cols ? Store<T>::load1(src + (r0 + i) * a.stride + at) : 0.f;
+            for (uint32_t e = 0; e < 8; ++e) {
+                const uint32_t at = c0 + 16 * e + l;
+                v[i][e] = r0 + i < a.rows && at < a.cols ? Store<T>::load1(src + (r0 + i) * a.stride + at) : 0.f;
             }
-        float* mine = scratch + (lane >> 4) * 128;
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-#pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) mine[16 * k + l] = v[i][k];
-            __syncwarp();
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) v[i][e] = mine[8 * l + e];
-            __syncwarp();
-        }
     }
 }
-template <> __device__ __forceinline__ void load_sub<uint8_t>(const Turn8Args& a, uint32_t r0, uint32_t c, float*, int, float (&v)[8][8])
+template <> __device__ __forceinline__ void load_sub<uint8_t, true>(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, float (&v)[8][8])
 {
     const Packed8Layout lay(a.rows, a.cols);
     const char* src = static_cast<const char*>(a.src);
-    const uint32_t rt = r0 >> 7, kb = c >> 7;
+    const uint32_t rt = r0 >> 7, kb = c0 >> 7;
     uint2 w[8];
     uint32_t e[8];
 #pragma unroll
@@ -201,7 +215,7 @@ template <> __device__ __forceinline__ void load_sub<uint8_t>(const Turn8Args& a
         w[i] = make_uint2(0, 0);
         e[i] = 0;
         if (r0 + i < a.rows) {
-            w[i] = __ldcs(reinterpret_cast<const uint2*>(src + lay.tile(rt, kb) + code_at(r0 + i, c)));
+            w[i] = __ldcs(reinterpret_cast<const uint2*>(src + lay.tile(rt, kb) + code_at(r0 + i, c0 + 8 * l)));
             e[i] = __ldg(reinterpret_cast<const unsigned char*>(src + lay.scales(rt, kb >> 2) + Packed8Layout::scale_word(r0 + i) + (kb & 3)));
         }
     }
@@ -214,17 +228,17 @@ template <> __device__ __forceinline__ void load_sub<uint8_t>(const Turn8Args& a
 
 constexpr int kTurnThreads = 256;
 
-template <typename T, bool BOTH> __global__ void __launch_bounds__(kTurnThreads, 2) turn8_kernel(const Turn8Args a)
+template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(kTurnThreads, 2) turn8_kernel(const Turn8Args a)
 {
-    __shared__ __align__(16) float s_scratch[kTurnThreads / 32][256];
     __shared__ __align__(16) uint32_t s_max[kTurnThreads / 32][128];
     __shared__ __align__(16) unsigned char s_tile[128 * 128];
+    __shared__ __align__(16) unsigned char s_rows[BOTH && !OCTETS ? 128 * 128 : 16];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t blocks = (a.cols + 127) / 128, rt = blockIdx.x / blocks, kb = blockIdx.x - rt * blocks;
-    const uint32_t l = tid & 15, rg = tid >> 4;
-    const uint32_t r0 = rt * 128 + rg * 8, c = kb * 128 + l * 8;
+    const uint32_t l = tid & 15, rg = tid >> 4, r0 = rt * 128 + rg * 8, c0 = kb * 128;
+    auto column = [&](uint32_t e) { return OCTETS ? 8 * l + e : l + 16 * e; };
     float v[8][8];
-    load_sub<T>(a, r0, c, s_scratch[warp], lane, v);
+    load_sub<T, OCTETS>(a, r0, c0, l, v);
 
     uint32_t top[8] = {};
 #pragma unroll
@@ -233,9 +247,9 @@ template <typename T, bool BOTH> __global__ void __launch_bounds__(kTurnThreads,
         for (int e = 0; e < 8; ++e) top[e] = max_bits(top[e], magnitude(v[i][e]));
 #pragma unroll
     for (int e = 0; e < 8; ++e) top[e] = max_bits(top[e], __shfl_xor_sync(~0u, top[e], 16));
-    if (lane < 16) {
-        reinterpret_cast<uint4*>(s_max[warp])[2 * l] = make_uint4(top[0], top[1], top[2], top[3]);
-        reinterpret_cast<uint4*>(s_max[warp])[2 * l + 1] = make_uint4(top[4], top[5], top[6], top[7]);
+    if (lane < 16) {      // kept by lane, so that a lane reads its own columns back in two pieces
+        reinterpret_cast<uint4*>(s_max[warp])[l] = make_uint4(top[0], top[1], top[2], top[3]);
+        reinterpret_cast<uint4*>(s_max[warp])[16 + l] = make_uint4(top[4], top[5], top[6], top[7]);
     }
     if (BOTH) {
         const Packed8Layout lay(a.rows, a.cols);
@@ -248,8 +262,13 @@ template <typename T, bool BOTH> __global__ void __launch_bounds__(kTurnThreads,
 #pragma unroll
             for (int o = 1; o < 16; o <<= 1) amax = max_bits(amax, __shfl_xor_sync(~0u, amax, o));
             const uint32_t e = block_scale(amax), r = r0 + i;
+            const uint2 w = codes8(v[i], amax, e);
+            if (!OCTETS) {
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k) s_rows[(rg * 8 + i) * 128 + ((k ^ (r & 7)) << 4) + l] = static_cast<unsigned char>((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
+            }
             if (r < a.rows) {
-                *reinterpret_cast<uint2*>(dst + lay.tile(rt, kb) + code_at(r, c)) = codes8(v[i], amax, e);
+                if (OCTETS) *reinterpret_cast<uint2*>(dst + lay.tile(rt, kb) + code_at(r, c0 + 8 * l)) = w;
                 if (l == 0) dst[lay.scales(rt, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)] = static_cast<char>(e);
             }
         }
@@ -257,7 +276,7 @@ template <typename T, bool BOTH> __global__ void __launch_bounds__(kTurnThreads,
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kTurnThreads / 32; ++w) {
-        const uint4 p = reinterpret_cast<const uint4*>(s_max[w])[2 * l], q = reinterpret_cast<const uint4*>(s_max[w])[2 * l + 1];
+        const uint4 p = reinterpret_cast<const uint4*>(s_max[w])[l], q = reinterpret_cast<const uint4*>(s_max[w])[16 + l];
         top[0] = max_bits(top[0], p.x); top[1] = max_bits(top[1], p.y); top[2] = max_bits(top[2], p.z); top[3] = max_bits(top[3], p.w);
         top[4] = max_bits(top[4], q.x); top[5] = max_bits(top[5], q.y); top[6] = max_bits(top[6], q.z); top[7] = max_bits(top[7], q.w);
     }
@@ -267,17 +286,23 @@ template <typename T, bool BOTH> __global__ void __launch_bounds__(kTurnThreads,
     for (int e = 0; e < 8; ++e) {
         const uint32_t s = block_scale(top[e]);
         const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
-        *reinterpret_cast<uint2*>(s_tile + (l * 8 + e) * 128 + ((rg ^ l) << 3)) = codes8(col, top[e], s);
-        if (rg == 0 && c + e < a.cols) turned[lay.scales(kb, rt >> 2) + Packed8Layout::scale_word(l * 8 + e) + (rt & 3)] = static_cast<char>(s);
+        *reinterpret_cast<uint2*>(s_tile + column(e) * 128 + ((rg ^ l) << 3)) = codes8(col, top[e], s);
+        if (rg == 0 && c0 + column(e) < a.cols) turned[lay.scales(kb, rt >> 2) + Packed8Layout::scale_word(column(e)) + (rt & 3)] = static_cast<char>(s);
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const uint32_t at = k * kTurnThreads + tid, row = at >> 3, piece = at & 7, f = row >> 3;      // f: what the row's pieces were exchanged by
-        if (kb * 128 + row >= a.cols) break;
-        const uint4 w = *reinterpret_cast<const uint4*>(s_tile + row * 128 + ((piece ^ (f >> 1)) << 4));
-        const uint4 o = f & 1 ? make_uint4(w.z, w.w, w.x, w.y) : w;
-        *reinterpret_cast<uint4*>(turned + lay.tile(kb, rt) + row * 128 + ((piece ^ (row & 7)) << 4)) = o;
+        const uint32_t at = k * kTurnThreads + tid, row = at >> 3, piece = at & 7, f = OCTETS ? row >> 3 : row & 15;      // f: the lane that wrote the row
+        if (BOTH && !OCTETS) {
+            const Packed8Layout to(a.rows, a.cols);
+            if (rt * 128 + row < a.rows)
+                *reinterpret_cast<uint4*>(static_cast<char*>(a.dst) + to.tile(rt, kb) + at * 16) = *reinterpret_cast<const uint4*>(s_rows + at * 16);
+        }
+        if (c0 + row < a.cols) {
+            const uint4 w = *reinterpret_cast<const uint4*>(s_tile + row * 128 + ((piece ^ (f >> 1)) << 4));
+            const uint4 o = f & 1 ? make_uint4(w.z, w.w, w.x, w.y) : w;
+            *reinterpret_cast<uint4*>(turned + lay.tile(kb, rt) + row * 128 + ((piece ^ (row & 7)) << 4)) = o;
+        }
     }
 }
 
@@ -295,8 +320,15 @@ template <typename T, typename M, bool RETRIEVE> int run_pack8(Pack8Args& a, voi
 {
     const uint32_t ctas = count_ctas(a);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a.n == 1) pack8_kernel<T, M, RETRIEVE, 1><<<ctas, kWarps8 * 32, 0, s>>>(Pack8Batch<1>{{a.mat[0]}, 1, a.lambda, a.task});
-    else pack8_kernel<T, M, RETRIEVE, kPackBatch><<<ctas, kWarps8 * 32, 0, s>>>(a);
+    bool octets = true;
+    for (uint32_t i = 0; i < a.n; ++i) octets = octets && a.mat[i].vec == (RETRIEVE ? 3u : 1u);
+    auto run = [&](const auto& args, auto batch) {
+        constexpr uint32_t B = decltype(batch)::value;
+        if (octets) pack8_kernel<T, M, RETRIEVE, true, B><<<ctas, kWarps8 * 32, 0, s>>>(args);
+        else pack8_kernel<T, M, RETRIEVE, false, B><<<ctas, kWarps8 * 32, 0, s>>>(args);
+    };
+    if (a.n == 1) run(Pack8Batch<1>{{a.mat[0]}, 1, a.lambda, a.task}, std::integral_constant<uint32_t, 1>());
+    else run(a, std::integral_constant<uint32_t, kPackBatch>());
     return static_cast<int>(cudaGetLastError());
 }
 template <typename T> int run_unpack8(Unpack8Args& a, void* stream)
@@ -307,17 +339,16 @@ template <typename T> int run_unpack8(Unpack8Args& a, void* stream)
     else unpack8_kernel<T, kPackBatch><<<ctas, kWarps8 * 32, 0, s>>>(a);
     return static_cast<int>(cudaGetLastError());
 }
-template <typename T> int run_turn8(const Turn8Args& a, void* stream)
+template <typename T, bool BOTH, bool OCTETS> int run_turn8(const Turn8Args& a, void* stream)
 {
     const uint32_t ctas = ((a.rows + 127) / 128) * ((a.cols + 127) / 128);
-    if constexpr (sizeof(T) > 1) {      // (a checkpoint has its blocks along the rows already)
-        if (a.dst) {
-            turn8_kernel<T, true><<<ctas, kTurnThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
-            return static_cast<int>(cudaGetLastError());
-        }
-    }
-    turn8_kernel<T, false><<<ctas, kTurnThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    turn8_kernel<T, BOTH, OCTETS><<<ctas, kTurnThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
     return static_cast<int>(cudaGetLastError());
+}
+template <typename T> int run_turn8(const Turn8Args& a, void* stream)
+{
+    if (a.dst) return a.vec ? run_turn8<T, true, true>(a, stream) : run_turn8<T, true, false>(a, stream);
+    return a.vec ? run_turn8<T, false, true>(a, stream) : run_turn8<T, false, false>(a, stream);
 }
 
 }  // namespace
@@ -336,7 +367,7 @@ int launch_unpack8(int out_dtype, Unpack8Args& a, void* stream)
 
 int launch_turn8(int src_dtype, const Turn8Args& a, void* stream)
 {
-    if (src_dtype < 0) return run_turn8<uint8_t>(a, stream);
+    if (src_dtype < 0) return run_turn8<uint8_t, false, true>(a, stream);
     return src_dtype ? run_turn8<bf16>(a, stream) : run_turn8<float>(a, stream);
 }
 

@@ -106,38 +106,63 @@ template <typename T> __device__ __forceinline__ void store_octet(T* row, uint32
             if (c + e < cols) Out<T>::store1(row + c + e, v[e]);
     }
 }
-// The same for a warp whose row starts anywhere: its 256 columns, lane l holding 8 l .. 8 l + 7, go through shared memory,
-// so that memory is read and written by neighbours together. `scratch`: 256 words of the warp's own.
-template <typename T> __device__ __forceinline__ void load_loose(const T* row, uint32_t c, uint32_t cols, int lane, float (&raw)[8])
+// Rows that start anywhere: a warp's run of 256 columns, lane l holding columns l, l + 32 .. l + 224, so that memory is read and
+// written by neighbours together, one element to a lane and instruction.
+template <typename T> __device__ __forceinline__ void load_strided(const T* row, uint32_t first, uint32_t cols, int lane, float (&v)[8])
 {
-    const uint32_t first = c - 8 * lane;
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) {
         const uint32_t at = first + 32 * k + lane;
-        raw[k] = at < cols ? Store<T>::load1(row + at) : 0.f;
+        v[k] = at < cols ? Store<T>::load1(row + at) : 0.f;
     }
 }
-__device__ __forceinline__ void turn_in(float (&v)[8], float* scratch, int lane)
+template <typename T> __device__ __forceinline__ void store_strided(T* row, uint32_t first, uint32_t cols, int lane, const float (&v)[8])
 {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) scratch[32 * k + lane] = v[k];
-    __syncwarp();
-    const float4 a = reinterpret_cast<const float4*>(scratch)[2 * lane], b = reinterpret_cast<const float4*>(scratch)[2 * lane + 1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    __syncwarp();
-}
-template <typename T> __device__ __forceinline__ void store_loose(T* row, uint32_t c, uint32_t cols, const float (&v)[8], float* scratch, int lane)
-{
-    const uint32_t first = c - 8 * lane;
-    reinterpret_cast<float4*>(scratch)[2 * lane] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(scratch)[2 * lane + 1] = make_float4(v[4], v[5], v[6], v[7]);
-    __syncwarp();
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k) {
         const uint32_t at = first + 32 * k + lane;
-        if (at < cols) Out<T>::store1(row + at, scratch[32 * k + lane]);
+        if (at < cols) Out<T>::store1(row + at, v[k]);
     }
-    __syncwarp();
+}
+
+// A warp's 256 columns of row r, from column `first` on, into eight bits; returns the scales of its two blocks (the second in bits 8-15).
+// OCTETS: lane l holds columns 8 l .. 8 l + 7; otherwise l, l + 32 ...
+template <bool OCTETS> __device__ __forceinline__ uint32_t pack_run(char* dst, const Packed8Layout& lay, uint32_t r, uint32_t first, const float (&v)[8], int lane)
+{
+    if (OCTETS) {
+        uint32_t amax = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = max_bits(amax, magnitude(v[e]));
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) amax = max_bits(amax, __shfl_xor_sync(~0u, amax, o));
+        const uint32_t c = first + 8 * lane, kb = c >> 7, e = block_scale(amax);
+        if (kb < lay.col_blocks) *reinterpret_cast<uint2*>(dst + lay.tile(r >> 7, kb) + code_at(r, c)) = codes8(v, amax, e);
+        return __shfl_sync(~0u, e, 0) | (__shfl_sync(~0u, e, 16) << 8);
+    }
+    uint32_t scales = 0;
+#pragma unroll
+    for (uint32_t b = 0; b < 2; ++b) {
+        const uint32_t kb = (first >> 7) + b;
+        if (kb >= lay.col_blocks) break;
+        uint32_t amax = 0;
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) amax = max_bits(amax, magnitude(v[4 * b + e]));
+        amax = __reduce_max_sync(~0u, amax);
+        const uint32_t s = block_scale(amax);
+        const float inv = block_inverse(s);
+        const uint32_t w = amax >= kNotFinite ? kNanCodes : codes4(v[4 * b] * inv, v[4 * b + 1] * inv, v[4 * b + 2] * inv, v[4 * b + 3] * inv);
+        char* to = dst + lay.tile(r >> 7, kb) + (r & 127) * 128 + (lane & 15);
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) to[((2 * e + (lane >> 4)) ^ (r & 7)) << 4] = static_cast<char>(w >> (8 * e));
+        scales |= s << (8 * b);
+    }
+    return scales;
+}
+// and its scales, where no word of four blocks is at hand
+__device__ __forceinline__ void store_scales(char* dst, const Packed8Layout& lay, uint32_t r, uint32_t first, uint32_t scales, int lane)
+{
+    const uint32_t kb = (first >> 7) + lane;
+    if (lane < 2 && kb < lay.col_blocks) dst[lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)] = static_cast<char>(scales >> (8 * lane));
 }
 
 }  // namespace device
