@@ -2153,7 +2153,7 @@ int randes_rms_norm_impl(const randes_rms_norm_t* p, void* stream)
     if (a.y8 && a.kept8 && overlap(a.y8, bytes8, a.kept8, bytes8)) return fail(RANDES_INVALID_ARGUMENT, "y8 overlaps kept8");
     if ((rc = check_words(a.rstd, "rstd"))) return rc;
     const NormArgs n{a.x, a.residual, a.gain, a.h, a.y, a.y8, a.kept8, a.rstd, a.x_stride, a.residual_stride, a.h_stride, a.y_stride,
-                     a.rows, a.cols, vec ? 1u : 0u, a.gain && a.gain_dtype == RANDES_BF16 ? 1u : 0u, a.eps};
+                     a.rows, a.cols, vec ? 1u : 0u, a.gain && a.gain_dtype == RANDES_BF16 ? 1u : 0u, a.eps, 1.f / a.cols};
     const int e = launch_norm(a.dtype, n, stream);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the norm kernel");
     ++g_launches;

@@ -390,7 +390,7 @@ struct NormArgs {
     uint32_t rows, cols;
     uint32_t vec;                 // rows of x, residual, h and y, and the gain, are 16-byte aligned
     uint32_t gain_bf16;
-    float eps;
+    float eps, per_col;           // per_col: 1 / cols
 };
 struct NormGradArgs {
     const void* dy;

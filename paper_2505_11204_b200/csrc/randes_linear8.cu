@@ -229,17 +229,12 @@ template <typename X> struct Sixteen {
         for (int e = 0; e < kWords / 2; ++e) o.w[e] = w[h * (kWords / 2) + e];
         widen(o, v);
     }
-    __device__ __forceinline__ uint32_t top() const
+    __device__ __forceinline__ float top() const
     {
-        uint32_t m = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float v[8];
-            half(h, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) m = max_bits(m, magnitude(v[e]));
-        }
-        return m;
+        float v[8], u[8];
+        half(0, v);
+        half(1, u);
+        return top2(top8(v), top8(u));
     }
 };
 
@@ -366,18 +361,17 @@ template <int N, typename X> __global__ void __launch_bounds__(kThreads8, 1) lin
                 for (uint32_t g0 = k0; ok && g0 < k1;) {
                     const uint32_t g1 = min(k1, (g0 | 3u) + 1);
                     Sixteen<X> v[4];
-                    uint32_t e[4], word = 0;
+                    float top[4];
+                    uint32_t word = 0;
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i)
                         if (g0 + i < g1) v[i].load(from, (g0 + i) * 128 + piece * 16, a.cols, a.x_vec);
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i) {
-                        uint32_t top = 0;
-                        if (g0 + i < g1) top = v[i].top();
+                        top[i] = g0 + i < g1 ? v[i].top() : 0.f;
 #pragma unroll
-                        for (int o = 1; o < 8; o <<= 1) top = max_bits(top, __shfl_xor_sync(~0u, top, o));
-                        e[i] = top;
-                        if (g0 + i < g1) word |= block_scale(top) << ((g0 + i & 3u) * 8);
+                        for (int o = 1; o < 8; o <<= 1) top[i] = top2(top[i], __shfl_xor_sync(~0u, top[i], o));
+                        if (g0 + i < g1) word |= block_scale(top[i]) << ((g0 + i & 3u) * 8);
                     }
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i) {
@@ -387,9 +381,9 @@ template <int N, typename X> __global__ void __launch_bounds__(kThreads8, 1) lin
                             unsigned char* stage = gen + at.s * G::kStage + kTile;
                             float c[8];
                             v[i].half(0, c);
-                            const uint2 lo = codes8(c, e[i], block_scale(e[i]));
+                            const uint2 lo = codes8(c, top[i], block_scale(top[i]));
                             v[i].half(1, c);
-                            const uint2 hi = codes8(c, e[i], block_scale(e[i]));
+                            const uint2 hi = codes8(c, top[i], block_scale(top[i]));
                             *reinterpret_cast<uint4*>(stage + code_at(t, piece * 16)) = make_uint4(lo.x, lo.y, hi.x, hi.y);
                             if (i == 0 && piece == 0) *reinterpret_cast<uint32_t*>(stage + N * 128 + kScales + Packed8Layout::scale_word(t)) = word;
                         }

@@ -74,6 +74,14 @@ template <int THREADS, typename V> __device__ __forceinline__ V row_sum(V v, V* 
     return all;
 }
 
+// 1 / sqrt, a Newton step behind the approximation: within a unit in the last place (the correctly rounded function takes five times the
+// instructions, in every thread of a row)
+__device__ __forceinline__ float root(float v)
+{
+    const float y = rsqrtf(v);
+    return __fmaf_rn(y * 0.5f, __fmaf_rn(-v * y, y, 1.f), y);
+}
+
 // A row's runs first(k) = 8 (k THREADS + warp's first thread), all loads before the first use.
 template <typename T, int THREADS, int CHUNKS, bool OCTETS> struct Row {
     Octet<T> o[OCTETS ? CHUNKS : 1];
@@ -131,12 +139,13 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
         }
     }
     float ss = 0.f;
+    const PackRow<OCTETS> kept(a.kept8, lay, r, lane), out(a.y8, lay, r, lane);
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
         const uint32_t first = (k * THREADS + (t & ~31)) * 8;
         if (first >= cols) break;                           // the same for a warp
         if (a.h) store_run<OCTETS>(static_cast<T*>(a.h) + r * a.h_stride, first, cols, v[k], lane);
-        if (a.kept8) store_scales(static_cast<char*>(a.kept8), lay, r, first, pack_run<OCTETS>(static_cast<char*>(a.kept8), lay, r, first, v[k], lane), lane);
+        if (a.kept8) store_scales(a.kept8, lay, r, first, kept.run(first, v[k], lane), lane);
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = __fmaf_rn(v[k][e], v[k][e], ss);
     }
@@ -150,7 +159,7 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
             for (int e = 0; e < 8; ++e) wide += static_cast<double>(v[k][e]) * v[k][e];
         s = static_cast<float>(1.0 / sqrt(row_sum<THREADS>(wide, s_part64, t) / cols + a.eps));
     } else {
-        s = __frsqrt_rn(ss / cols + a.eps);
+        s = root(__fmaf_rn(ss, a.per_col, a.eps));
     }
     if (a.rstd && t == 0) a.rstd[r] = s;
     if (!a.y && !a.y8) return;
@@ -161,31 +170,30 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
         float w[8];
         load_gain<OCTETS>(a.gain, a.gain_bf16, first, cols, lane, w);
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) {
-            w[e] = v[k][e] * s * w[e];
-            if (first + 256 > cols && first + (OCTETS ? 8 * lane + e : 32 * e + lane) >= cols) w[e] = 0.f;      // (0 * NaN behind the row's end would spoil the block)
+        for (uint32_t e = 0; e < 8; ++e) w[e] = v[k][e] * s * w[e];
+        if (first + 256 > cols) {
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                if (first + (OCTETS ? 8 * lane + e : 32 * e + lane) >= cols) w[e] = 0.f;      // (0 * NaN behind the row's end would spoil the block)
         }
         if (a.y) store_run<OCTETS>(static_cast<T*>(a.y) + r * a.y_stride, first, cols, w, lane);
-        if (a.y8) store_scales(static_cast<char*>(a.y8), lay, r, first, pack_run<OCTETS>(static_cast<char*>(a.y8), lay, r, first, w, lane), lane);
+        if (a.y8) store_scales(a.y8, lay, r, first, out.run(first, w, lane), lane);
     }
 }
 
-// A CTA walks rows and keeps its share of dgain in registers; the shares of all CTAs are added in a fixed order by a second kernel.
+// Backward: a CTA walks rows and keeps its share of dgain in registers; the shares of all CTAs are added in a fixed order by a second
+// kernel. This form takes rows of more than 8192 columns.
 template <typename T, int THREADS, int CHUNKS, bool OCTETS>
-__global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_grad_kernel(const NormGradArgs a)
+__global__ void __launch_bounds__(THREADS) norm_grad_kernel(const NormGradArgs a)
 {
-    constexpr int kWarps = THREADS * kRowsPerCta<THREADS> / 32;
-    constexpr int kSum = THREADS == 32 ? 256 * CHUNKS : 1;
-    __shared__ float s_part[2][THREADS == 32 ? 1 : kWarps];
-    __shared__ float s_sum[kSum];
-    const int t = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x, lane = t & 31;
+    __shared__ float s_part[2][THREADS / 32];
+    const int t = threadIdx.x, lane = t & 31;
     const uint32_t cols = a.cols;
     const Packed8Layout lay(a.rows, cols);
-    const uint32_t step = gridDim.x * kRowsPerCta<THREADS>;
     auto column = [&](int k, uint32_t e) { return (k * THREADS + (t & ~31)) * 8 + (OCTETS ? 8 * lane + e : 32 * e + lane); };
     float sum[CHUNKS][8] = {};
     uint32_t turn = 0;
-    for (uint32_t r = blockIdx.x * kRowsPerCta<THREADS> + (THREADS == 32 ? threadIdx.x >> 5 : 0); r < a.rows; r += step, turn ^= 1) {
+    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
         float n[CHUNKS][8], g[CHUNKS][8];
         const float s = __ldg(a.rstd + r);
         if (a.kept8) {
@@ -267,188 +275,249 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_grad_kerne
     }
     if (!a.dgain) return;
     float* out = a.partial + static_cast<size_t>(blockIdx.x) * cols;
-    if (THREADS == 32) {                                    // the warps of a CTA, one after the other
-        for (int w = 0; w < kWarps; ++w) {
-            __syncthreads();
-            if (static_cast<int>(threadIdx.x >> 5) != w) continue;
 #pragma unroll
-            for (int k = 0; k < CHUNKS; ++k)
+    for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float& to = s_sum[(e * CHUNKS + k) * 32 + lane];
-                    to = w ? to + sum[k][e] : sum[k][e];
-                }
-        }
-        __syncthreads();
-        for (uint32_t c = threadIdx.x; c < cols; c += THREADS * kRowsPerCta<THREADS>) {
-            const uint32_t k = c >> 8, e = OCTETS ? c & 7 : (c >> 5) & 7, l = OCTETS ? (c >> 3) & 31 : c & 31;
-            out[c] = s_sum[(e * CHUNKS + k) * 32 + l];
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (column(k, e) < cols) out[column(k, e)] = sum[k][e];
-    }
+        for (int e = 0; e < 8; ++e)
+            if (column(k, e) < cols) out[column(k, e)] = sum[k][e];
 }
 
-// The same where rows start on 16-byte boundaries and have up to 8192 columns. What bounds the form above is that a row's loads, its
-// sum and its stores follow one another; here the rows to come are on their way into shared memory meanwhile, each thread copying
-// what it will read itself (so that nothing has to be waited for but its own copies): 16 columns of dy, h and dh, the scales
-// and the root of the row. TEAM threads to a row.
+// The same for rows of up to 8192 columns. What bounds the form above is that a row's loads, its sum and its stores follow one
+// another; here the rows to come are on their way into shared memory meanwhile. TEAM threads to a row, 16 columns to a thread.
+// A row is copied as it lies in memory, in 16-byte words from the boundary below its first element to its last (a word that holds
+// an element of the row is memory of the caller's), neighbours by neighbours: 32 bytes between lanes took 30 times the passes
+// through shared memory. OCTETS, where rows start on the boundary: a thread reads back only what it copied itself, CPL
+// columns t CPL + w TEAM CPL, and waits for nothing else; otherwise element by element, columns 32 apart, after the team has met.
 template <typename T, int TEAM> struct GradRing {
     static constexpr int kThreads = TEAM < 256 ? 256 : TEAM, kRows = kThreads / TEAM;
-    static constexpr int kWords = sizeof(T);                                    // 16-byte words of 16 columns
-    static constexpr uint32_t kSlot = kThreads * 16;
-    static constexpr uint32_t kStage = 3 * kWords * kSlot + 2 * kThreads * 4;   // dy, h, dh; scales, rstd
+    static constexpr int CPL = 16 / sizeof(T), kWords = sizeof(T);              // columns in a 16-byte word, words to a thread
+    static constexpr uint32_t kRow = TEAM * kWords * 16 + 16;                   // bytes of a row of dy, h or dh
+    static constexpr uint32_t kScalesAt = 3 * kRow, kRootAt = kScalesAt + TEAM * kWords * 4;
+    static constexpr uint32_t kTeam = kRootAt + 16, kStage = kRows * kTeam;     // scale words of a thread's columns; rstd
     static constexpr int kPerSm = kThreads == 256 ? 2 : 1;
     static constexpr uint32_t kDepth = 220 * 1024 / kPerSm / kStage > 4 ? 4 : 220 * 1024 / kPerSm / kStage;
     static constexpr size_t kSmem = kDepth * kStage;
+    static_assert(kDepth >= 2, "a row on its way while one is worked on");
 };
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, uint32_t bytes)      // the rest of the 16 bytes reads zero
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+template <int N> __device__ __forceinline__ void copy_small(uint32_t to, const void* from)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(N) : "memory");
 }
-__device__ __forceinline__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ uint32_t lds_u8(uint32_t saddr)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(saddr));
+    return v;
+}
+template <int TEAM> __device__ __forceinline__ void team_sync(int team)
+{
+    if (TEAM == 32) __syncwarp();
+    else if (TEAM >= 256) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(TEAM) : "memory");
+}
 
-template <typename T, int TEAM>
+template <typename T, int TEAM, bool OCTETS>
 __global__ void __launch_bounds__(GradRing<T, TEAM>::kThreads, GradRing<T, TEAM>::kPerSm) norm_grad_ring_kernel(const NormGradArgs a)
 {
     typedef GradRing<T, TEAM> G;
-    constexpr int kWarps = G::kThreads / 32;
+    constexpr int kWarps = G::kThreads / 32, CPL = G::CPL, W = G::kWords;
     extern __shared__ __align__(16) unsigned char s_ring[];
     __shared__ float s_part[2][kWarps];
-    const int tid = threadIdx.x, t = tid % TEAM, team = tid / TEAM;
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring));
-    const uint32_t cols = a.cols, c = t * 16, kb = c >> 7;
+    const int tid = threadIdx.x, t = tid % TEAM, team = tid / TEAM, lane = tid & 31;
+    const uint32_t cols = a.cols;
     const Packed8Layout lay(a.rows, cols);
-    const bool kept = a.kept8 != nullptr, in = kb < lay.col_blocks;
+    const bool kept = a.kept8 != nullptr;
     const uint32_t step = gridDim.x * G::kRows;
-    auto bytes_at = [&](int w) {      // of a 16-byte word of the lane's columns, how many exist
-        const uint32_t at = c + w * (16 / sizeof(T));
-        return at < cols ? min(16u, (cols - at) * static_cast<uint32_t>(sizeof(T))) : 0u;
-    };
+    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + team * G::kTeam;
+    // column of this thread's element e (0 .. 15), and the block it lies in
+    auto column = [&](uint32_t e) { return OCTETS ? (e / CPL * TEAM + t) * CPL + e % CPL : (t & ~31) * 16 + 32 * e + lane; };
+    auto offset = [&](const void* p, uint32_t r, uint64_t stride) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(static_cast<const T*>(p) + r * stride) & 15); };
+
     auto fetch = [&](uint32_t r, uint32_t slot) {
         if (r < a.rows) {
-            const uint32_t at = ring + slot * G::kStage + tid * 16;
-            auto row = [&](const void* p, uint64_t stride, uint32_t first) {
-                const T* from = static_cast<const T*>(p) + r * stride;
+            const uint32_t at = mine + slot * G::kStage;
+            auto row = [&](const void* p, uint64_t stride, uint32_t to) {
+                const char* from = reinterpret_cast<const char*>(static_cast<const T*>(p) + r * stride);
+                const uint32_t off = OCTETS ? 0 : offset(p, r, stride);
+                from -= off;
+                const uint32_t n = (off + cols * static_cast<uint32_t>(sizeof(T)) + 15) / 16;      // words that hold elements of the row
 #pragma unroll
-                for (int w = 0; w < G::kWords; ++w) {
-                    const uint32_t n = bytes_at(w);
-                    copy16(at + (first + w) * G::kSlot, n ? from + c + w * (16 / sizeof(T)) : from, n);
+                for (int w = 0; w < W; ++w) {
+                    const uint32_t i = w * TEAM + t;
+                    if (i < n) copy16(to + i * 16, from + i * 16);
                 }
+                if (!OCTETS && t == 0 && n > W * TEAM) copy16(to + W * TEAM * 16, from + W * TEAM * 16);
             };
-            row(a.dy, a.dy_stride, 0);
-            if (a.dh) row(a.dh, a.dh_stride, 2 * G::kWords);
-            const uint32_t word = ring + slot * G::kStage + 3 * G::kWords * G::kSlot + tid * 4;
+            row(a.dy, a.dy_stride, at);
+            if (a.dh) row(a.dh, a.dh_stride, at + 2 * G::kRow);
             if (kept) {
                 const char* src = static_cast<const char*>(a.kept8);
-                copy16(at + G::kWords * G::kSlot, in ? src + lay.tile(r >> 7, kb) + code_at(r, c) : src, in ? 16u : 0u);
-                if (in) copy4(word, src + lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r));
+                const char* scales = src + lay.scales(r >> 7, 0) + Packed8Layout::scale_word(r);
+                if (OCTETS) {
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        const uint32_t i = w * TEAM + t, c = i * CPL;
+                        if (c >> 7 >= lay.col_blocks) continue;
+                        copy_small<CPL>(at + G::kRow + i * CPL, src + lay.tile(r >> 7, c >> 7) + code_at(r, c & ~7u) + (c & 7));
+                        copy_small<4>(at + G::kScalesAt + i * 4, scales + (c >> 9) * 512);
+                    }
+                } else if (t * 16u >> 7 < lay.col_blocks) {
+                    copy16(at + G::kRow + t * 16, src + lay.tile(r >> 7, t * 16 >> 7) + code_at(r, t * 16));
+                    copy_small<4>(at + G::kScalesAt + t * 4, scales + (t * 16 >> 9) * 512);
+                }
             } else {
-                row(a.h, a.h_stride, G::kWords);
+                row(a.h, a.h_stride, at + G::kRow);
             }
-            copy4(word + G::kThreads * 4, a.rstd + r);
+            if (OCTETS || t == 0) copy_small<4>(at + G::kRootAt, a.rstd + r);
         }
         cp_async_commit();
     };
-    auto words = [&](uint32_t slot, uint32_t first, float (&v)[16]) {
-        const uint32_t at = ring + slot * G::kStage + first * G::kSlot + tid * 16;
+    // this thread's 16 elements of a copied row, zero behind the row's end
+    auto read = [&](uint32_t from, uint32_t off, float (&v)[16]) {
+        if (OCTETS) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            Octet<T> o;
+            for (int w = 0; w < W; ++w) {
+                float u[CPL];
+                Store<T>::widen(lds128(from + (w * TEAM + t) * 16), u);
 #pragma unroll
-            for (int w = 0; w < G::kWords / 2; ++w) o.w[w] = lds128(at + (h * (G::kWords / 2) + w) * G::kSlot);
-            float u[8];
-            widen(o, u);
+                for (int e = 0; e < CPL; ++e) v[w * CPL + e] = u[e];
+            }
+        } else {
+            const uint32_t at = from + off + column(0) * sizeof(T);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[8 * h + e] = u[e];
+            for (int e = 0; e < 16; ++e)
+                v[e] = sizeof(T) == 4 ? __uint_as_float(lds_u32(at + 32 * e * sizeof(T))) : __uint_as_float(lds_u16(at + 32 * e * sizeof(T)) << 16);
+        }
+        if (column(15) >= cols) {
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e)
+                if (column(e) >= cols) v[e] = 0.f;
         }
     };
 
     float gain[16], sum[16] = {};
 #pragma unroll
-    for (uint32_t e = 0; e < 16; ++e) gain[e] = a.gain && c + e < cols ? gain_at(a.gain, a.gain_bf16, c + e) : 1.f;
+    for (uint32_t e = 0; e < 16; ++e) gain[e] = a.gain && column(e) < cols ? gain_at(a.gain, a.gain_bf16, column(e)) : 1.f;
+    const float per_col = 1.f / cols;
     uint32_t r = blockIdx.x * G::kRows + team, slot = 0, turn = 0;
 #pragma unroll
     for (uint32_t i = 0; i + 1 < G::kDepth; ++i) fetch(r + i * step, i);
-    // the rows of a CTA's teams end together or one apart: all teams of a CTA take part in its last round
-    for (uint32_t r0 = blockIdx.x * G::kRows; r0 < a.rows; r0 += step, r += step, turn ^= 1) {
-        fetch(r + (G::kDepth - 1) * step, slot == 0 ? G::kDepth - 1 : slot - 1);
-        cp_async_wait<static_cast<int>(G::kDepth) - 1>();
-        float n[16], g[16], inner = 0.f, s = 0.f;
-        if (r < a.rows) {
-            const uint32_t word = ring + slot * G::kStage + 3 * G::kWords * G::kSlot + tid * 4;
-            s = __uint_as_float(lds_u32(word + G::kThreads * 4));
-            if (kept) {
-                const uint4 w = lds128(ring + slot * G::kStage + G::kWords * G::kSlot + tid * 16);
-                const float unit = in ? block_unit((lds_u32(word) >> (8 * (kb & 3))) & 0xFFu) : 0.f;
-                values4(w.x, unit, n);
-                values4(w.y, unit, n + 4);
-                values4(w.z, unit, n + 8);
-                values4(w.w, unit, n + 12);
-                if (c + 16 > cols)
+    for (; r < a.rows; r += step, turn ^= 1) {
+        if (OCTETS) {
+            fetch(r + (G::kDepth - 1) * step, slot == 0 ? G::kDepth - 1 : slot - 1);
+            cp_async_wait<static_cast<int>(G::kDepth) - 1>();
+        } else {
+            cp_async_wait<static_cast<int>(G::kDepth) - 2>();
+            team_sync<TEAM>(team);      // the row is there, and the one before has been read by all
+            fetch(r + (G::kDepth - 1) * step, slot == 0 ? G::kDepth - 1 : slot - 1);
+        }
+        const uint32_t at = mine + slot * G::kStage;
+        float n[16], g[16], inner = 0.f;
+        const float s = __uint_as_float(lds_u32(at + G::kRootAt));
+        if (kept) {
+            if (OCTETS) {
 #pragma unroll
-                    for (uint32_t e = 0; e < 16; ++e) n[e] = c + e < cols ? n[e] : 0.f;      // (codes behind the row's end may be NaN)
+                for (int w = 0; w < W; ++w) {
+                    const uint32_t i = w * TEAM + t, c = i * CPL, from = at + G::kRow + i * CPL;
+                    const float unit = block_unit((lds_u32(at + G::kScalesAt + i * 4) >> (8 * ((c >> 7) & 3))) & 0xFFu);
+                    float u[8];
+                    values4(lds_u32(from), unit, u);
+                    if (CPL == 8) values4(lds_u32(from + 4), unit, u + 4);
+#pragma unroll
+                    for (int e = 0; e < CPL; ++e) n[w * CPL + e] = u[e];
+                }
             } else {
-                words(slot, G::kWords, n);
-            }
-            words(slot, 0, g);
+                const uint32_t from = at + G::kRow + column(0), word = lds_u32(at + G::kScalesAt + (t & ~31) * 4);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                n[e] *= s;
-                sum[e] = __fmaf_rn(g[e], n[e], sum[e]);
-                g[e] *= gain[e];
-                inner = __fmaf_rn(g[e], n[e], inner);
+                for (int b = 0; b < 4; ++b) {
+                    uint32_t w = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w |= lds_u8(from + 128 * b + 32 * e) << (8 * e);
+                    float u[4];
+                    values4(w, block_unit((word >> (8 * b)) & 0xFFu), u);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) n[4 * b + e] = u[e];
+                }
             }
+            if (column(15) >= cols) {
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e)
+                    if (column(e) >= cols) n[e] = 0.f;      // (codes behind the row's end may be NaN)
+            }
+        } else {
+            read(at + G::kRow, OCTETS ? 0 : offset(a.h, r, a.h_stride), n);
+        }
+        read(at, OCTETS ? 0 : offset(a.dy, r, a.dy_stride), g);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            n[e] *= s;
+            sum[e] = __fmaf_rn(g[e], n[e], sum[e]);
+            g[e] *= gain[e];
+            inner = __fmaf_rn(g[e], n[e], inner);
         }
         inner = warp_sum(inner);
         if (TEAM > 32) {
-            if ((tid & 31) == 0) s_part[turn][tid >> 5] = inner;
-            __syncthreads();
+            if (lane == 0) s_part[turn][tid >> 5] = inner;
+            team_sync<TEAM>(team);
             inner = 0.f;
 #pragma unroll
             for (int w = 0; w < TEAM / 32; ++w) inner += s_part[turn][team * (TEAM / 32) + w];
         }
-        inner /= cols;
-        if (r < a.rows) {
-            float d[16];
-            if (a.dh) words(slot, 2 * G::kWords, d);
-            T* row = static_cast<T*>(a.dx) + r * a.dx_stride;
+        inner *= per_col;
+        float d[16];
+        if (a.dh) read(at + 2 * G::kRow, OCTETS ? 0 : offset(a.dh, r, a.dh_stride), d);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float u[8];
+        for (int e = 0; e < 16; ++e) {
+            const float v = s * __fmaf_rn(-n[e], inner, g[e]);
+            d[e] = a.dh ? v + d[e] : v;
+        }
+        T* row = static_cast<T*>(a.dx) + r * a.dx_stride;
+        if (OCTETS) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = s * __fmaf_rn(-n[8 * h + e], inner, g[8 * h + e]);
-                    u[e] = a.dh ? v + d[8 * h + e] : v;
+            for (int w = 0; w < W; ++w) {
+                const uint32_t c = column(w * CPL);
+                if (c + CPL <= cols) {
+                    uint4 o;
+                    if (sizeof(T) == 4) o = make_uint4(__float_as_uint(d[w * CPL]), __float_as_uint(d[w * CPL + 1]), __float_as_uint(d[w * CPL + 2]), __float_as_uint(d[w * CPL + 3]));
+                    else o = make_uint4(Out<bf16>::pack(d[w * CPL], d[w * CPL + 1]), Out<bf16>::pack(d[w * CPL + 2], d[w * CPL + 3]),
+                                        Out<bf16>::pack(d[w * CPL + 4 % CPL], d[w * CPL + 5 % CPL]), Out<bf16>::pack(d[w * CPL + 6 % CPL], d[w * CPL + 7 % CPL]));
+                    *reinterpret_cast<uint4*>(row + c) = o;
+                } else {
+#pragma unroll
+                    for (uint32_t e = 0; e < CPL; ++e)
+                        if (c + e < cols) Out<T>::store1(row + c + e, d[w * CPL + e]);
                 }
-                if (c + 8 * h < cols) store_octet(row, c + 8 * h, cols, u);
             }
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e)
+                if (column(e) < cols) Out<T>::store1(row + column(e), d[e]);
         }
         slot = slot + 1 == G::kDepth ? 0 : slot + 1;
     }
     if (!a.dgain) return;
     cp_async_wait<0>();
     float* out = a.partial + static_cast<size_t>(blockIdx.x) * cols;
-    float* shares = reinterpret_cast<float*>(s_ring);      // [team][column], 17 words to 16 columns
-    if (G::kRows > 1) {
+    if (G::kRows > 1) {      // the teams of a CTA, one behind the other
+        float* shares = reinterpret_cast<float*>(s_ring);
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) shares[tid * 17 + e] = sum[e];
+        for (int e = 0; e < 16; ++e) shares[(team * 16 + e) * TEAM + t] = sum[e];
         __syncthreads();
-        for (uint32_t at = tid; at < cols; at += G::kThreads) {
-            float v = 0.f;
+        if (team == 0) {
 #pragma unroll
-            for (int k = 0; k < G::kRows; ++k) v += shares[(k * TEAM + (at >> 4)) * 17 + (at & 15)];
-            out[at] = v;
+            for (uint32_t e = 0; e < 16; ++e) {
+                float v = 0.f;
+#pragma unroll
+                for (int k = 0; k < G::kRows; ++k) v += shares[(k * 16 + e) * TEAM + t];
+                if (column(e) < cols) out[column(e)] = v;
+            }
         }
     } else {
 #pragma unroll
         for (uint32_t e = 0; e < 16; ++e)
-            if (c + e < cols) out[c + e] = sum[e];
+            if (column(e) < cols) out[column(e)] = sum[e];
     }
 }
 
@@ -476,8 +545,8 @@ template <typename F> int by_width(uint32_t cols, F&& f)
     if (cols <= 256) return f(Const<32>(), Const<1>());
     if (cols <= 512) return f(Const<32>(), Const<2>());
     if (cols <= 1024) return f(Const<32>(), Const<4>());
-    if (cols <= 2048) return f(Const<256>(), Const<1>());
-    if (cols <= 4096) return f(Const<256>(), Const<2>());
+    if (cols <= 2048) return f(Const<128>(), Const<2>());
+    if (cols <= 4096) return f(Const<128>(), Const<4>());
     if (cols <= 8192) return f(Const<256>(), Const<4>());
     if (cols <= 16384) return f(Const<512>(), Const<4>());
     return f(Const<1024>(), Const<4>());
@@ -485,11 +554,6 @@ template <typename F> int by_width(uint32_t cols, F&& f)
 // CTAs that walk the rows of a backward pass: the rows, or what the 148 SMs hold at a time (a constant, so that sums are the same
 // on every device and the workspace is known without one).
 constexpr uint32_t kSms = 148;
-uint32_t grad_ctas(uint32_t rows, uint32_t cols)
-{
-    const uint32_t per_sm = cols <= 1024 ? 8 : (cols <= 4096 ? 4 : (cols <= 8192 ? 2 : 1));
-    return std::min(cols <= 1024 ? (rows + 3) / 4 : rows, per_sm * kSms);
-}
 constexpr uint32_t kRingCols = 8192;
 template <typename T, int TEAM> uint32_t ring_ctas(uint32_t rows)
 {
@@ -498,7 +562,7 @@ template <typename T, int TEAM> uint32_t ring_ctas(uint32_t rows)
 }
 
 constexpr int kDevices = 64;
-template <typename T, int TEAM> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
+template <typename T, int TEAM, bool OCTETS> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
 {
     typedef GradRing<T, TEAM> G;
     static std::atomic<bool> granted[kDevices];
@@ -506,21 +570,21 @@ template <typename T, int TEAM> int run_ring(const NormGradArgs& a, uint32_t* ct
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return static_cast<int>(e);
     if (device >= kDevices || !granted[device].load(std::memory_order_relaxed)) {
-        e = cudaFuncSetAttribute(norm_grad_ring_kernel<T, TEAM>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(G::kSmem));
+        e = cudaFuncSetAttribute(norm_grad_ring_kernel<T, TEAM, OCTETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(G::kSmem));
         if (e != cudaSuccess) return static_cast<int>(e);
         if (device < kDevices) granted[device].store(true, std::memory_order_relaxed);
     }
     *ctas = ring_ctas<T, TEAM>(a.rows);
-    norm_grad_ring_kernel<T, TEAM><<<*ctas, G::kThreads, G::kSmem, stream>>>(a);
+    norm_grad_ring_kernel<T, TEAM, OCTETS><<<*ctas, G::kThreads, G::kSmem, stream>>>(a);
     return static_cast<int>(cudaGetLastError());
 }
-template <typename T> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
+template <typename T, bool OCTETS> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
 {
-    if (a.cols <= 512) return run_ring<T, 32>(a, ctas, stream);
-    if (a.cols <= 1024) return run_ring<T, 64>(a, ctas, stream);
-    if (a.cols <= 2048) return run_ring<T, 128>(a, ctas, stream);
-    if (a.cols <= 4096) return run_ring<T, 256>(a, ctas, stream);
-    return run_ring<T, 512>(a, ctas, stream);
+    if (a.cols <= 512) return run_ring<T, 32, OCTETS>(a, ctas, stream);
+    if (a.cols <= 1024) return run_ring<T, 64, OCTETS>(a, ctas, stream);
+    if (a.cols <= 2048) return run_ring<T, 128, OCTETS>(a, ctas, stream);
+    if (a.cols <= 4096) return run_ring<T, 256, OCTETS>(a, ctas, stream);
+    return run_ring<T, 512, OCTETS>(a, ctas, stream);
 }
 
 template <bool OCTETS> int run_norm(int dtype, const NormArgs& a, cudaStream_t stream)
@@ -533,16 +597,17 @@ template <bool OCTETS> int run_norm(int dtype, const NormArgs& a, cudaStream_t s
         return static_cast<int>(cudaGetLastError());
     });
 }
-template <bool OCTETS> int run_grad(int dtype, const NormGradArgs& a, uint32_t ctas, cudaStream_t stream)
+template <bool OCTETS> int run_grad(int dtype, const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
 {
-    return by_width(a.cols, [&](auto threads, auto chunks) {
-        constexpr int T = decltype(threads)::value, C = decltype(chunks)::value;
-        if constexpr (!OCTETS || T >= 512) {      // (narrower rows on 16-byte boundaries take the ring)
-            if (dtype) norm_grad_kernel<bf16, T, C, OCTETS><<<ctas, T * kRowsPerCta<T>, 0, stream>>>(a);
-            else norm_grad_kernel<float, T, C, OCTETS><<<ctas, T * kRowsPerCta<T>, 0, stream>>>(a);
-        }
+    if (a.cols <= kRingCols) return dtype ? run_ring<bf16, OCTETS>(a, ctas, stream) : run_ring<float, OCTETS>(a, ctas, stream);
+    *ctas = std::min(a.rows, kSms);
+    auto run = [&](auto threads) {
+        constexpr int T = decltype(threads)::value;
+        if (dtype) norm_grad_kernel<bf16, T, 4, OCTETS><<<*ctas, T, 0, stream>>>(a);
+        else norm_grad_kernel<float, T, 4, OCTETS><<<*ctas, T, 0, stream>>>(a);
         return static_cast<int>(cudaGetLastError());
-    });
+    };
+    return a.cols <= 16384 ? run(Const<512>()) : run(Const<1024>());
 }
 
 }  // namespace
@@ -554,16 +619,15 @@ int launch_norm(int dtype, const NormArgs& a, void* stream)
 
 size_t norm_grad_workspace(uint32_t rows, uint32_t cols)
 {
-    return static_cast<size_t>(std::max(grad_ctas(rows, cols), std::min(rows, 2 * kSms))) * cols * sizeof(float);
+    return static_cast<size_t>(std::min(rows, 2 * kSms)) * cols * sizeof(float);
 }
 
 int launch_norm_grad(int dtype, const NormGradArgs& a, int* launched, void* stream)
 {
     *launched = 0;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    uint32_t ctas = grad_ctas(a.rows, a.cols);
-    const int e = a.vec && a.cols <= kRingCols ? (dtype ? run_ring<bf16>(a, &ctas, s) : run_ring<float>(a, &ctas, s))
-                                               : (a.vec ? run_grad<true>(dtype, a, ctas, s) : run_grad<false>(dtype, a, ctas, s));
+    uint32_t ctas = 0;
+    const int e = a.vec ? run_grad<true>(dtype, a, &ctas, s) : run_grad<false>(dtype, a, &ctas, s);
     if (e) return e;
     *launched = 1;
     if (!a.dgain) return 0;

@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
 #pragma unroll
                 for (uint32_t k = 0; k < 8; ++k) v[k] = __fmaf_rn(a.lambda, flip(e[k], (bits >> k) << 31), v[k]);
             }
-            word[i] |= pack_run<OCTETS>(dst, lay, r0 + i, first, v, lane) << (16 * half);
+            word[i] |= PackRow<OCTETS>(dst, lay, r0 + i, lane).run(first, v, lane) << (16 * half);
         }
     }
 #pragma unroll
@@ -230,7 +230,7 @@ constexpr int kTurnThreads = 256;
 
 template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(kTurnThreads, 2) turn8_kernel(const Turn8Args a)
 {
-    __shared__ __align__(16) uint32_t s_max[kTurnThreads / 32][128];
+    __shared__ __align__(16) float s_max[kTurnThreads / 32][128];
     __shared__ __align__(16) unsigned char s_tile[128 * 128];
     __shared__ __align__(16) unsigned char s_rows[BOTH && !OCTETS ? 128 * 128 : 16];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -240,29 +240,27 @@ template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(
     float v[8][8];
     load_sub<T, OCTETS>(a, r0, c0, l, v);
 
-    uint32_t top[8] = {};
+    float top[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top[e] = max_bits(top[e], magnitude(v[i][e]));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top[e] = max_bits(top[e], __shfl_xor_sync(~0u, top[e], 16));
+    for (int e = 0; e < 8; ++e) {
+        const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
+        top[e] = top8(col);
+        top[e] = top2(top[e], __shfl_xor_sync(~0u, top[e], 16));
+    }
     if (lane < 16) {      // kept by lane, so that a lane reads its own columns back in two pieces
-        reinterpret_cast<uint4*>(s_max[warp])[l] = make_uint4(top[0], top[1], top[2], top[3]);
-        reinterpret_cast<uint4*>(s_max[warp])[16 + l] = make_uint4(top[4], top[5], top[6], top[7]);
+        reinterpret_cast<float4*>(s_max[warp])[l] = make_float4(top[0], top[1], top[2], top[3]);
+        reinterpret_cast<float4*>(s_max[warp])[16 + l] = make_float4(top[4], top[5], top[6], top[7]);
     }
     if (BOTH) {
         const Packed8Layout lay(a.rows, a.cols);
         char* dst = static_cast<char*>(a.dst);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            uint32_t amax = 0;
+            float most = top8(v[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) amax = max_bits(amax, magnitude(v[i][e]));
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) amax = max_bits(amax, __shfl_xor_sync(~0u, amax, o));
-            const uint32_t e = block_scale(amax), r = r0 + i;
-            const uint2 w = codes8(v[i], amax, e);
+            for (int o = 1; o < 16; o <<= 1) most = top2(most, __shfl_xor_sync(~0u, most, o));
+            const uint32_t e = block_scale(most), r = r0 + i;
+            const uint2 w = codes8(v[i], most, e);
             if (!OCTETS) {
 #pragma unroll
                 for (uint32_t k = 0; k < 8; ++k) s_rows[(rg * 8 + i) * 128 + ((k ^ (r & 7)) << 4) + l] = static_cast<unsigned char>((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
@@ -275,10 +273,11 @@ template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(
     }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kTurnThreads / 32; ++w) {
-        const uint4 p = reinterpret_cast<const uint4*>(s_max[w])[l], q = reinterpret_cast<const uint4*>(s_max[w])[16 + l];
-        top[0] = max_bits(top[0], p.x); top[1] = max_bits(top[1], p.y); top[2] = max_bits(top[2], p.z); top[3] = max_bits(top[3], p.w);
-        top[4] = max_bits(top[4], q.x); top[5] = max_bits(top[5], q.y); top[6] = max_bits(top[6], q.z); top[7] = max_bits(top[7], q.w);
+    for (int w = 0; w < kTurnThreads / 32; w += 2) {
+        const float4 p = reinterpret_cast<const float4*>(s_max[w])[l], q = reinterpret_cast<const float4*>(s_max[w])[16 + l];
+        const float4 x = reinterpret_cast<const float4*>(s_max[w + 1])[l], y = reinterpret_cast<const float4*>(s_max[w + 1])[16 + l];
+        top[0] = top3(top[0], p.x, x.x); top[1] = top3(top[1], p.y, x.y); top[2] = top3(top[2], p.z, x.z); top[3] = top3(top[3], p.w, x.w);
+        top[4] = top3(top[4], q.x, y.x); top[5] = top3(top[5], q.y, y.y); top[6] = top3(top[6], q.z, y.z); top[7] = top3(top[7], q.w, y.w);
     }
     const Packed8Layout lay(a.cols, a.rows);
     char* turned = static_cast<char*>(a.turned);

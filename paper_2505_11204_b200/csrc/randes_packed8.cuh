@@ -10,13 +10,26 @@ namespace device {
 
 constexpr uint32_t kNotFinite = 0x7F800000u;      // a greatest magnitude (as bits) from here on: the block holds a NaN or an infinity
 
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-__device__ __forceinline__ uint32_t max_bits(uint32_t a, uint32_t b) { return a > b ? a : b; }
+// The greatest of magnitudes; a NaN wins.
+__device__ __forceinline__ float top2(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+__device__ __forceinline__ float top3(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+    return r;
+}
+__device__ __forceinline__ float top8(const float (&v)[8]) { return top3(top3(v[0], v[1], v[2]), top3(v[3], v[4], v[5]), top2(v[6], v[7])); }
 
 // Exponent + 127 of the least power of two, 2^-100 at least, that takes the block's greatest magnitude to 448 = 1.75 * 2^8 or below:
 // the carry out of the mantissa says whether that lies above 1.75. A block that holds a NaN or an infinity: 1 (its codes are NaN).
-__device__ __forceinline__ uint32_t block_scale(uint32_t amax)
+__device__ __forceinline__ uint32_t block_scale(float top)
 {
+    const uint32_t amax = __float_as_uint(top) & 0x7FFFFFFFu;
     const uint32_t e = ((amax + 0x1FFFFFu) >> 23) - 8;
     return amax >= kNotFinite ? 127u : (amax < (27u + 8u) << 23 ? 27u : e);
 }
@@ -33,11 +46,23 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
     return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
 }
 constexpr uint32_t kNanCodes = 0x7F7F7F7Fu;
-__device__ __forceinline__ uint2 codes8(const float (&v)[8], uint32_t amax, uint32_t e)
+__device__ __forceinline__ bool not_finite(float top) { return (__float_as_uint(top) & 0x7FFFFFFFu) >= kNotFinite; }
+// four elements (pairs) of a block whose inverse is twice in `inv`
+__device__ __forceinline__ uint32_t codes4(f32x2 ab, f32x2 cd, f32x2 inv)
+{
+    float a, b, c, d;
+    unpack2(mul2(ab, inv), a, b);
+    unpack2(mul2(cd, inv), c, d);
+    return codes4(a, b, c, d);
+}
+__device__ __forceinline__ f32x2 pair_of(float a, float b) { return pack2(__float_as_uint(a), __float_as_uint(b)); }
+// (a block that holds a NaN or an infinity: NaN in every code)
+__device__ __forceinline__ uint2 codes8(const float (&v)[8], float top, uint32_t e)
 {
     const float s = block_inverse(e);
-    if (amax >= kNotFinite) return make_uint2(kNanCodes, kNanCodes);
-    return make_uint2(codes4(v[0] * s, v[1] * s, v[2] * s, v[3] * s), codes4(v[4] * s, v[5] * s, v[6] * s, v[7] * s));
+    const f32x2 inv = pair_of(s, s);
+    const uint2 w = make_uint2(codes4(pair_of(v[0], v[1]), pair_of(v[2], v[3]), inv), codes4(pair_of(v[4], v[5]), pair_of(v[6], v[7]), inv));
+    return not_finite(top) ? make_uint2(kNanCodes, kNanCodes) : w;
 }
 // The four values behind a word of codes, exact (an e4m3 value is a half), times the block's unit.
 __device__ __forceinline__ void values4(uint32_t w, float unit, float* v)
@@ -110,59 +135,78 @@ template <typename T> __device__ __forceinline__ void store_octet(T* row, uint32
 // written by neighbours together, one element to a lane and instruction.
 template <typename T> __device__ __forceinline__ void load_strided(const T* row, uint32_t first, uint32_t cols, int lane, float (&v)[8])
 {
+    const T* p = row + first + lane;
+    if (first + 256 <= cols) {
 #pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) {
-        const uint32_t at = first + 32 * k + lane;
-        v[k] = at < cols ? Store<T>::load1(row + at) : 0.f;
+        for (int k = 0; k < 8; ++k) v[k] = Store<T>::load1(p + 32 * k);
+    } else {
+        const int left = static_cast<int>(cols) - static_cast<int>(first) - lane;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = 32 * k < left ? Store<T>::load1(p + 32 * k) : 0.f;
     }
 }
 template <typename T> __device__ __forceinline__ void store_strided(T* row, uint32_t first, uint32_t cols, int lane, const float (&v)[8])
 {
+    T* p = row + first + lane;
+    if (first + 256 <= cols) {
 #pragma unroll
-    for (uint32_t k = 0; k < 8; ++k) {
-        const uint32_t at = first + 32 * k + lane;
-        if (at < cols) Out<T>::store1(row + at, v[k]);
+        for (int k = 0; k < 8; ++k) Out<T>::store1(p + 32 * k, v[k]);
+    } else {
+        const int left = static_cast<int>(cols) - static_cast<int>(first) - lane;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (32 * k < left) Out<T>::store1(p + 32 * k, v[k]);
     }
 }
 
-// A warp's 256 columns of row r, from column `first` on, into eight bits; returns the scales of its two blocks (the second in bits 8-15).
-// OCTETS: lane l holds columns 8 l .. 8 l + 7; otherwise l, l + 32 ...
-template <bool OCTETS> __device__ __forceinline__ uint32_t pack_run(char* dst, const Packed8Layout& lay, uint32_t r, uint32_t first, const float (&v)[8], int lane)
-{
-    if (OCTETS) {
-        uint32_t amax = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) amax = max_bits(amax, magnitude(v[e]));
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) amax = max_bits(amax, __shfl_xor_sync(~0u, amax, o));
-        const uint32_t c = first + 8 * lane, kb = c >> 7, e = block_scale(amax);
-        if (kb < lay.col_blocks) *reinterpret_cast<uint2*>(dst + lay.tile(r >> 7, kb) + code_at(r, c)) = codes8(v, amax, e);
-        return __shfl_sync(~0u, e, 0) | (__shfl_sync(~0u, e, 16) << 8);
+// A warp's runs of 256 columns of one row on their way into eight bits. OCTETS: lane l holds columns 8 l .. 8 l + 7 of a run; otherwise
+// l, l + 32 ... (A run starts on a multiple of 256, so a lane's place inside a tile is the same for all of them.)
+template <bool OCTETS> struct PackRow {
+    char* codes;              // of this lane in the row's first two blocks
+    uint32_t flip, blocks;
+    __device__ __forceinline__ PackRow(void* dst, const Packed8Layout& lay, uint32_t r, int lane)
+    {
+        codes = static_cast<char*>(dst) + lay.tile(r >> 7, 0) + (r & 127) * 128;
+        if (OCTETS) codes += (lane >> 4) * 16384 + ((((lane >> 1) & 7) ^ (r & 7)) << 4) + (lane & 1) * 8;
+        else codes += lane & 15;
+        flip = (r ^ (lane >> 4)) & 7;
+        blocks = lay.col_blocks;
     }
-    uint32_t scales = 0;
+    // returns the scales of the run's two blocks (the second in bits 8-15)
+    __device__ __forceinline__ uint32_t run(uint32_t first, const float (&v)[8], int lane) const
+    {
+        const uint32_t kb = first >> 7;
+        char* to = codes + static_cast<size_t>(kb) * 16384;
+        if (OCTETS) {
+            float top = top8(v);
 #pragma unroll
-    for (uint32_t b = 0; b < 2; ++b) {
-        const uint32_t kb = (first >> 7) + b;
-        if (kb >= lay.col_blocks) break;
-        uint32_t amax = 0;
+            for (int o = 1; o < 16; o <<= 1) top = top2(top, __shfl_xor_sync(~0u, top, o));
+            const uint32_t e = block_scale(top);
+            if (kb + (lane >> 4) < blocks) *reinterpret_cast<uint2*>(to) = codes8(v, top, e);
+            return __shfl_sync(~0u, e, 0) | (__shfl_sync(~0u, e, 16) << 8);
+        }
+        uint32_t scales = 0;
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) amax = max_bits(amax, magnitude(v[4 * b + e]));
-        amax = __reduce_max_sync(~0u, amax);
-        const uint32_t s = block_scale(amax);
-        const float inv = block_inverse(s);
-        const uint32_t w = amax >= kNotFinite ? kNanCodes : codes4(v[4 * b] * inv, v[4 * b + 1] * inv, v[4 * b + 2] * inv, v[4 * b + 3] * inv);
-        char* to = dst + lay.tile(r >> 7, kb) + (r & 127) * 128 + (lane & 15);
+        for (uint32_t b = 0; b < 2; ++b) {
+            if (kb + b >= blocks) break;
+            const float* u = v + 4 * b;
+            const float top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top3(u[0], u[1], top2(u[2], u[3])))));      // (as bits: none is negative)
+            const uint32_t s = block_scale(top);
+            const f32x2 inv = pair_of(block_inverse(s), block_inverse(s));
+            const uint32_t w = not_finite(top) ? kNanCodes : codes4(pair_of(u[0], u[1]), pair_of(u[2], u[3]), inv);
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) to[((2 * e + (lane >> 4)) ^ (r & 7)) << 4] = static_cast<char>(w >> (8 * e));
-        scales |= s << (8 * b);
+            for (uint32_t e = 0; e < 4; ++e) to[b * 16384 + (((2 * e) ^ flip) << 4)] = static_cast<char>(w >> (8 * e));
+            scales |= s << (8 * b);
+        }
+        return scales;
     }
-    return scales;
-}
+};
 // and its scales, where no word of four blocks is at hand
-__device__ __forceinline__ void store_scales(char* dst, const Packed8Layout& lay, uint32_t r, uint32_t first, uint32_t scales, int lane)
+__device__ __forceinline__ void store_scales(void* dst, const Packed8Layout& lay, uint32_t r, uint32_t first, uint32_t scales, int lane)
 {
     const uint32_t kb = (first >> 7) + lane;
-    if (lane < 2 && kb < lay.col_blocks) dst[lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)] = static_cast<char>(scales >> (8 * lane));
+    if (lane < 2 && kb < lay.col_blocks)
+        static_cast<char*>(dst)[lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)] = static_cast<char>(scales >> (8 * lane));
 }
 
 }  // namespace device
