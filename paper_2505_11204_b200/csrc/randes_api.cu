@@ -2085,7 +2085,7 @@ int randes_packed_eight_linear_impl(const void* w, uint32_t rows, uint32_t cols,
         ++g_launches;
     }
     Linear8Args a{w, need ? workspace : x, y, x_stride, y_stride, rows, cols, n_tokens, vec ? 1u : 0u, y_dtype == RANDES_BF16 ? 1u : 0u, 0};
-    const int e = launch_linear8(a, packed || need ? -1 : x_dtype, dev.sms, dev.index, stream);
+    const int e = launch_linear8(a, packed || need ? -1 : x_dtype, dev.sms, stream);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit product");
     ++g_launches;
     return RANDES_OK;

@@ -373,7 +373,7 @@ struct Linear8Args {
     uint32_t log_ranks;           // set by the launcher: CTAs of a cluster that share a tile's columns
 };
 bool linear8_packs(uint32_t n_tokens);      // whether so few tokens go into eight bits inside the product
-int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, int device, void* stream);      // x_dtype -1: eight bits
+int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, void* stream);      // x_dtype -1: eight bits
 int linear8_giveups(unsigned int* count);
 
 // randes_norm.cu: root-mean-square norm with the residual's addition, and its gradient

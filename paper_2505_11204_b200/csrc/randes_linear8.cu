@@ -13,7 +13,6 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "randes_packed.cuh"
 #include "randes_packed8.cuh"
@@ -623,17 +622,11 @@ linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     }
 }
 
-constexpr int kDevices8 = 64;
-
-template <int N, typename X> int run_linear8(Linear8Args& a, int sm_count, int device, cudaStream_t stream)
+template <int N, typename X> int run_linear8(Linear8Args& a, int sm_count, cudaStream_t stream)
 {
     typedef Geom8<N> G;
-    static std::atomic<bool> granted[kDevices8];
-    if (device >= kDevices8 || !granted[device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(linear8_kernel<N, X>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(G::kSmem));
-        if (e != cudaSuccess) return static_cast<int>(e);
-        if (device < kDevices8) granted[device].store(true, std::memory_order_relaxed);
-    }
+    const cudaError_t e = opt_in<linear8_kernel<N, X>>(G::kSmem);
+    if (e != cudaSuccess) return static_cast<int>(e);
     const Packed8Layout lw(a.rows, a.cols);
     const uint64_t tiles = static_cast<uint64_t>(lw.row_tiles) * ((a.n_tokens + N - 1) / N);
     if (tiles > 0x7FFFFFFFu) return static_cast<int>(cudaErrorInvalidValue);
@@ -677,14 +670,10 @@ bool map_rows(EncodeTiled enc, CUtensorMap* map, const void* p, uint32_t words, 
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int run_pairs(const Linear8Args& a, int sm_count, int device, cudaStream_t stream)
+int run_pairs(const Linear8Args& a, int sm_count, cudaStream_t stream)
 {
-    static std::atomic<bool> granted[kDevices8];
-    if (device >= kDevices8 || !granted[device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(linear8_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Pair8::kSmem));
-        if (e != cudaSuccess) return static_cast<int>(e);
-        if (device < kDevices8) granted[device].store(true, std::memory_order_relaxed);
-    }
+    const cudaError_t e = opt_in<linear8_pair_kernel>(Pair8::kSmem);
+    if (e != cudaSuccess) return static_cast<int>(e);
     const EncodeTiled enc = encode_tiled();
     if (!enc) return static_cast<int>(cudaErrorNotSupported);
     const Packed8Layout lw(a.rows, a.cols), lx(a.n_tokens, a.cols);
@@ -703,16 +692,16 @@ int run_pairs(const Linear8Args& a, int sm_count, int device, cudaStream_t strea
 
 bool linear8_packs(uint32_t n_tokens) { return n_tokens <= 16; }
 
-int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, int device, void* stream)
+int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, void* stream)
 {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (x_dtype == 0) return run_linear8<16, float>(a, sm_count, device, s);
-    if (x_dtype == 1) return run_linear8<16, bf16>(a, sm_count, device, s);
-    if (a.n_tokens <= 16) return run_linear8<16, uint8_t>(a, sm_count, device, s);
-    if (a.n_tokens <= 32) return run_linear8<32, uint8_t>(a, sm_count, device, s);
-    if (a.n_tokens <= 64) return run_linear8<64, uint8_t>(a, sm_count, device, s);
-    if (a.n_tokens > 128) return run_pairs(a, sm_count, device, s);
-    return run_linear8<128, uint8_t>(a, sm_count, device, s);
+    if (x_dtype == 0) return run_linear8<16, float>(a, sm_count, s);
+    if (x_dtype == 1) return run_linear8<16, bf16>(a, sm_count, s);
+    if (a.n_tokens <= 16) return run_linear8<16, uint8_t>(a, sm_count, s);
+    if (a.n_tokens <= 32) return run_linear8<32, uint8_t>(a, sm_count, s);
+    if (a.n_tokens <= 64) return run_linear8<64, uint8_t>(a, sm_count, s);
+    if (a.n_tokens > 128) return run_pairs(a, sm_count, s);
+    return run_linear8<128, uint8_t>(a, sm_count, s);
 }
 
 int linear8_giveups(unsigned int* count)

@@ -13,7 +13,6 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <type_traits>
 
 #include "randes_packed8.cuh"
@@ -292,8 +291,7 @@ template <typename T, int TEAM> struct GradRing {
     static constexpr int kThreads = TEAM < 256 ? 256 : TEAM, kRows = kThreads / TEAM;
     static constexpr int CPL = 16 / sizeof(T), kWords = sizeof(T);              // columns in a 16-byte word, words to a thread
     static constexpr uint32_t kRow = TEAM * kWords * 16 + 16;                   // bytes of a row of dy, h or dh
-    static constexpr uint32_t kScalesAt = 3 * kRow, kRootAt = kScalesAt + TEAM * kWords * 4;
-    static constexpr uint32_t kTeam = kRootAt + 16, kStage = kRows * kTeam;     // scale words of a thread's columns; rstd
+    static constexpr uint32_t kTeam = 3 * kRow, kStage = kRows * kTeam;
     static constexpr int kPerSm = kThreads == 256 ? 2 : 1;
     static constexpr uint32_t kDepth = 220 * 1024 / kPerSm / kStage > 4 ? 4 : 220 * 1024 / kPerSm / kStage;
     static constexpr size_t kSmem = kDepth * kStage;
@@ -303,6 +301,12 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm vola
 template <int N> __device__ __forceinline__ void copy_small(uint32_t to, const void* from)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(N) : "memory");
+}
+__device__ __forceinline__ uint2 lds64(uint32_t saddr)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(saddr));
+    return v;
 }
 __device__ __forceinline__ uint32_t lds_u8(uint32_t saddr)
 {
@@ -352,26 +356,37 @@ __global__ void __launch_bounds__(GradRing<T, TEAM>::kThreads, GradRing<T, TEAM>
             row(a.dy, a.dy_stride, at);
             if (a.dh) row(a.dh, a.dh_stride, at + 2 * G::kRow);
             if (kept) {
-                const char* src = static_cast<const char*>(a.kept8);
-                const char* scales = src + lay.scales(r >> 7, 0) + Packed8Layout::scale_word(r);
+                const char* src = static_cast<const char*>(a.kept8) + lay.tile(r >> 7, 0);
                 if (OCTETS) {
 #pragma unroll
                     for (int w = 0; w < W; ++w) {
                         const uint32_t i = w * TEAM + t, c = i * CPL;
-                        if (c >> 7 >= lay.col_blocks) continue;
-                        copy_small<CPL>(at + G::kRow + i * CPL, src + lay.tile(r >> 7, c >> 7) + code_at(r, c & ~7u) + (c & 7));
-                        copy_small<4>(at + G::kScalesAt + i * 4, scales + (c >> 9) * 512);
+                        if (c >> 7 < lay.col_blocks) copy_small<CPL>(at + G::kRow + i * CPL, src + (c >> 7) * 16384 + code_at(r, c & ~7u) + (c & 7));
                     }
                 } else if (t * 16u >> 7 < lay.col_blocks) {
-                    copy16(at + G::kRow + t * 16, src + lay.tile(r >> 7, t * 16 >> 7) + code_at(r, t * 16));
-                    copy_small<4>(at + G::kScalesAt + t * 4, scales + (t * 16 >> 9) * 512);
+                    copy16(at + G::kRow + t * 16, src + (t * 16u >> 7) * 16384 + code_at(r, t * 16));
                 }
             } else {
                 row(a.h, a.h_stride, at + G::kRow);
             }
-            if (OCTETS || t == 0) copy_small<4>(at + G::kRootAt, a.rstd + r);
         }
         cp_async_commit();
+    };
+    // the scale words of this thread's columns and the root of the row, a row ahead (copied like the rest, one word for 32 lanes, they
+    // took 32 passes through shared memory)
+    constexpr int kScaleWords = OCTETS ? W : 1;
+    uint32_t scale[kScaleWords], scale_next[kScaleWords] = {};
+    float root_next = 0.f;
+    auto fetch_scalars = [&](uint32_t r) {
+        if (r >= a.rows) return;
+        root_next = __ldg(a.rstd + r);
+        if (!kept) return;
+        const char* words = static_cast<const char*>(a.kept8) + lay.scales(r >> 7, 0) + Packed8Layout::scale_word(r);
+#pragma unroll
+        for (int w = 0; w < kScaleWords; ++w) {
+            const uint32_t c = OCTETS ? (w * TEAM + t) * CPL : (t & ~31) * 16;
+            if (c >> 7 < lay.col_blocks) scale_next[w] = __ldg(reinterpret_cast<const uint32_t*>(words + (c >> 9) * 512));
+        }
     };
     // this thread's 16 elements of a copied row, zero behind the row's end
     auto read = [&](uint32_t from, uint32_t off, float (&v)[16]) {
@@ -403,7 +418,12 @@ __global__ void __launch_bounds__(GradRing<T, TEAM>::kThreads, GradRing<T, TEAM>
     uint32_t r = blockIdx.x * G::kRows + team, slot = 0, turn = 0;
 #pragma unroll
     for (uint32_t i = 0; i + 1 < G::kDepth; ++i) fetch(r + i * step, i);
+    fetch_scalars(r);
     for (; r < a.rows; r += step, turn ^= 1) {
+        const float s = root_next;
+#pragma unroll
+        for (int w = 0; w < kScaleWords; ++w) scale[w] = scale_next[w];
+        fetch_scalars(r + step);
         if (OCTETS) {
             fetch(r + (G::kDepth - 1) * step, slot == 0 ? G::kDepth - 1 : slot - 1);
             cp_async_wait<static_cast<int>(G::kDepth) - 1>();
@@ -414,21 +434,25 @@ __global__ void __launch_bounds__(GradRing<T, TEAM>::kThreads, GradRing<T, TEAM>
         }
         const uint32_t at = mine + slot * G::kStage;
         float n[16], g[16], inner = 0.f;
-        const float s = __uint_as_float(lds_u32(at + G::kRootAt));
         if (kept) {
             if (OCTETS) {
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     const uint32_t i = w * TEAM + t, c = i * CPL, from = at + G::kRow + i * CPL;
-                    const float unit = block_unit((lds_u32(at + G::kScalesAt + i * 4) >> (8 * ((c >> 7) & 3))) & 0xFFu);
+                    const float unit = block_unit((scale[w] >> (8 * ((c >> 7) & 3))) & 0xFFu);
                     float u[8];
-                    values4(lds_u32(from), unit, u);
-                    if (CPL == 8) values4(lds_u32(from + 4), unit, u + 4);
+                    if (CPL == 8) {
+                        const uint2 x = lds64(from);
+                        values4(x.x, unit, u);
+                        values4(x.y, unit, u + 4);
+                    } else {
+                        values4(lds_u32(from), unit, u);
+                    }
 #pragma unroll
                     for (int e = 0; e < CPL; ++e) n[w * CPL + e] = u[e];
                 }
             } else {
-                const uint32_t from = at + G::kRow + column(0), word = lds_u32(at + G::kScalesAt + (t & ~31) * 4);
+                const uint32_t from = at + G::kRow + column(0), word = scale[0];
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     uint32_t w = 0;
@@ -561,19 +585,11 @@ template <typename T, int TEAM> uint32_t ring_ctas(uint32_t rows)
     return std::min<uint32_t>((rows + G::kRows - 1) / G::kRows, G::kPerSm * kSms);
 }
 
-constexpr int kDevices = 64;
 template <typename T, int TEAM, bool OCTETS> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
 {
     typedef GradRing<T, TEAM> G;
-    static std::atomic<bool> granted[kDevices];
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
+    const cudaError_t e = opt_in<norm_grad_ring_kernel<T, TEAM, OCTETS>>(G::kSmem);
     if (e != cudaSuccess) return static_cast<int>(e);
-    if (device >= kDevices || !granted[device].load(std::memory_order_relaxed)) {
-        e = cudaFuncSetAttribute(norm_grad_ring_kernel<T, TEAM, OCTETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(G::kSmem));
-        if (e != cudaSuccess) return static_cast<int>(e);
-        if (device < kDevices) granted[device].store(true, std::memory_order_relaxed);
-    }
     *ctas = ring_ctas<T, TEAM>(a.rows);
     norm_grad_ring_kernel<T, TEAM, OCTETS><<<*ctas, G::kThreads, G::kSmem, stream>>>(a);
     return static_cast<int>(cudaGetLastError());

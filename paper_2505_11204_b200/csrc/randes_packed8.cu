@@ -121,8 +121,11 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
             *reinterpret_cast<uint32_t*>(dst + lay.scales(r0 >> 7, g) + Packed8Layout::scale_word(r0 + i)) = word[i];
 }
 
-template <typename T, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 * 32) unpack8_kernel(const __grid_constant__ Unpack8Batch<BATCH> a)
+// A lane takes CPL neighbouring columns at a time, 16 bytes of the output, so that a warp writes whole lines; where rows do not start
+// on 16-byte boundaries single columns, 32 apart.
+template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 * 32) unpack8_kernel(const __grid_constant__ Unpack8Batch<BATCH> a)
 {
+    constexpr uint32_t CPL = OCTETS ? Store<T>::CPL : 8, kSteps = 512 / 32 / CPL;      // columns to a lane and step
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Unpack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
     const Packed8Layout lay(m.rows, m.cols);
@@ -130,18 +133,25 @@ template <typename T, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 
     const uint32_t r0 = rb * kCtaRows8 + warp * kRows8, cols = m.cols;
     if (r0 >= m.rows) return;
     const uint32_t n = min(kRows8, m.rows - r0);
-    const char* src = static_cast<const char*>(m.src);
-    uint2 codes[2][kRows8];
-    uint32_t word[kRows8];
+    const char* src = static_cast<const char*>(m.src) + lay.tile(r0 >> 7, g * 4);
+    const char* scales = static_cast<const char*>(m.src) + lay.scales(r0 >> 7, g) + Packed8Layout::scale_word(r0);      // (four rows from a multiple of 4)
+    uint32_t codes[kRows8][kSteps][CPL / 4], word[kRows8];
 #pragma unroll
     for (uint32_t i = 0; i < kRows8; ++i) {
         if (i >= n) break;
-        const uint32_t r = r0 + i;
-        word[i] = __ldg(reinterpret_cast<const uint32_t*>(src + lay.scales(r >> 7, g) + Packed8Layout::scale_word(r)));
+        word[i] = __ldg(reinterpret_cast<const uint32_t*>(scales + 16 * i));
 #pragma unroll
-        for (uint32_t half = 0; half < 2; ++half) {
-            const uint32_t c = g * 512 + half * 256 + lane * 8;
-            if (c >> 7 < lay.col_blocks) codes[half][i] = __ldcs(reinterpret_cast<const uint2*>(src + lay.tile(r >> 7, c >> 7) + code_at(r, c)));
+        for (uint32_t k = 0; k < kSteps; ++k) {
+            const uint32_t c = k * 32 * CPL + lane * CPL;      // inside the group
+            if (g * 4 + (c >> 7) >= lay.col_blocks) continue;
+            const char* p = src + (c >> 7) * 16384 + code_at(r0 + i, c & ~7u) + (c & 7);
+            if (CPL == 8) {
+                const uint2 w = __ldcs(reinterpret_cast<const uint2*>(p));
+                codes[i][k][0] = w.x;
+                codes[i][k][CPL / 4 - 1] = w.y;
+            } else {
+                codes[i][k][0] = __ldcs(reinterpret_cast<const uint32_t*>(p));
+            }
         }
     }
 #pragma unroll
@@ -149,24 +159,32 @@ template <typename T, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 
         if (i >= n) break;
         T* row = static_cast<T*>(m.dst) + (r0 + i) * m.stride;
 #pragma unroll
-        for (uint32_t half = 0; half < 2; ++half) {
-            const uint32_t first = g * 512 + half * 256, c = first + lane * 8;
+        for (uint32_t k = 0; k < kSteps; ++k) {
+            const uint32_t first = g * 512 + k * 32 * CPL, c = first + lane * CPL;
             if (first >= cols) break;
-            float v[8];
-            if (m.vec) {
+            if (OCTETS) {
                 const float unit = block_unit((word[i] >> (8 * ((c >> 7) & 3))) & 0xFFu);
-                values4(codes[half][i].x, unit, v);
-                values4(codes[half][i].y, unit, v + 4);
-                store_octet(row, c, cols, v);
-            } else {
-                // column l + 32 k lies in lane 4 k + l / 8, whose eight codes are 8 (l / 8) .. + 7 of that run
+                float v[8];
+                values4(codes[i][k][0], unit, v);
+                if (CPL == 8) values4(codes[i][k][CPL / 4 - 1], unit, v + 4);
+                if (c + CPL <= cols) {
+                    const Octet<T> o = narrow<T>(v);      // (of four fp32 columns the first word)
+                    *reinterpret_cast<uint4*>(row + c) = o.w[0];
+                } else {
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) {
-                    const uint32_t from = 4 * k + (lane >> 3);
-                    const uint32_t x = __shfl_sync(~0u, codes[half][i].x, from), y = __shfl_sync(~0u, codes[half][i].y, from);
+                    for (uint32_t e = 0; e < CPL; ++e)
+                        if (c + e < cols) Out<T>::store1(row + c + e, v[e]);
+                }
+            } else {
+                // column l + 32 j lies in lane 4 j + l / 8, whose eight codes are 8 (l / 8) .. + 7 of that run
+                float v[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) {
+                    const uint32_t from = 4 * j + (lane >> 3);
+                    const uint32_t x = __shfl_sync(~0u, codes[i][k][0], from), y = __shfl_sync(~0u, codes[i][k][CPL / 4 - 1], from);
                     float u[4];
-                    values4((lane & 4 ? y : x) >> (8 * (lane & 3)), block_unit((word[i] >> (16 * half + 8 * (k >> 2))) & 0xFFu), u);
-                    v[k] = u[0];
+                    values4((lane & 4 ? y : x) >> (8 * (lane & 3)), block_unit((word[i] >> (16 * k + 8 * (j >> 2))) & 0xFFu), u);
+                    v[j] = u[0];
                 }
                 store_strided(row, first, cols, lane, v);
             }
@@ -176,38 +194,150 @@ template <typename T, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 
 
 // A tile of 128 x 128 in blocks along its columns, and with BOTH in blocks along its rows too, out of one read. A thread holds rows
 // 8 rg .. 8 rg + 7 of eight columns: 8 l .. 8 l + 7 where rows start on 16-byte boundaries (OCTETS), else l, l + 16 ..
-// l + 112. The greatest magnitudes of the columns meet in shared memory; the codes of a column are turned there, 8-byte pieces
-// exchanged by a number that differs between the 16 lanes that write at a time, so that they do not meet in a bank.
-template <typename T, bool OCTETS> __device__ __forceinline__ void load_sub(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, float (&v)[8][8])
+// l + 112, out of rows that are copied into shared memory as they lie, in 16-byte words from the boundary below their first element
+// (loads of single bf16 elements took three times as long: too few bytes under way). Elements that have 8 bits or fewer behind
+// the leading one stay pairs of bf16. The greatest magnitudes of the columns meet in shared memory; the codes of a column
+// are turned there, 8-byte pieces exchanged by a number that differs between the 16 lanes that write at a time, so that they
+// do not meet in a bank.
+__device__ __forceinline__ uint32_t top_bf16x2(uint32_t a, uint32_t b)      // magnitudes; the result's signs mean nothing
+{
+    uint32_t r;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+template <typename T> struct Block8;      // a thread's 8 x 8 elements
+template <> struct Block8<float> {
+    typedef float4 Top;                   // of four columns
+    float v[8][8];
+    __device__ __forceinline__ void set(int i, int e, float x) { v[i][e] = x; }
+    __device__ __forceinline__ void set(int i, const float (&x)[8])
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = x[e];
+    }
+    __device__ __forceinline__ float get(int i, int e) const { return v[i][e]; }
+    __device__ __forceinline__ void column_tops(float (&top)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
+            top[e] = top8(col);
+            top[e] = top2(top[e], __shfl_xor_sync(~0u, top[e], 16));
+        }
+    }
+    // of every row, over the 16 lanes that hold it
+    __device__ __forceinline__ void row_tops(float (&top)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            top[i] = top8(v[i]);
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) top[i] = top2(top[i], __shfl_xor_sync(~0u, top[i], o));
+        }
+    }
+};
+template <> struct Block8<bf16> {
+    uint32_t w[8][4];
+    __device__ __forceinline__ void set(int i, const float (&x)[8])      // (exact: at most 8 bits each)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[i][j] = Out<bf16>::pack(x[2 * j], x[2 * j + 1]);
+    }
+    __device__ __forceinline__ float get(int i, int e) const { return e & 1 ? high_half(w[i][e / 2]) : low_half(w[i][e / 2]); }
+    __device__ __forceinline__ void column_tops(float (&top)[8]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t m = top_bf16x2(w[0][j], w[1][j]);
+#pragma unroll
+            for (int i = 2; i < 8; ++i) m = top_bf16x2(m, w[i][j]);
+            m = top_bf16x2(m, __shfl_xor_sync(~0u, m, 16));
+            top[2 * j] = fabsf(low_half(m));
+            top[2 * j + 1] = fabsf(high_half(m));
+        }
+    }
+    __device__ __forceinline__ void row_tops(float (&top)[8]) const      // two rows to a word
+    {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const uint32_t a = top_bf16x2(top_bf16x2(w[i][0], w[i][1]), top_bf16x2(w[i][2], w[i][3]));
+            const uint32_t b = top_bf16x2(top_bf16x2(w[i + 1][0], w[i + 1][1]), top_bf16x2(w[i + 1][2], w[i + 1][3]));
+            uint32_t m = top_bf16x2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) m = top_bf16x2(m, __shfl_xor_sync(~0u, m, o));
+            top[i] = fabsf(low_half(m));
+            top[i + 1] = fabsf(high_half(m));
+        }
+    }
+};
+template <typename T> struct Held { typedef T type; };
+template <> struct Held<uint8_t> { typedef bf16 type; };
+
+constexpr int kTurnThreads = 256;
+// shared memory of an unaligned tile's rows: a row's words, one more than it has itself
+template <typename T> constexpr uint32_t kTurnPitch = 128 * sizeof(T) + 16;
+
+template <typename T, bool OCTETS>
+__device__ __forceinline__ void load_block(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, unsigned char* staged, Block8<T>& v)
 {
     const T* src = static_cast<const T*>(a.src);
     if (OCTETS) {
         Octet<T> o[8];
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
-            if (r0 + i < a.rows) o[i] = load_octet(src + (r0 + i) * a.stride, c0 + 8 * l, a.cols);
-#pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
-            if (r0 + i < a.rows) widen(o[i], v[i]);
+            if (r0 + i < a.rows) o[i] = load_octet(src + (r0 + i) * a.stride, c0 + 8 * l, a.cols);
             else
 #pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) v[i][e] = 0.f;
+                for (int h = 0; h < static_cast<int>(sizeof(T)) / 2; ++h) o[i].w[h] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            float x[8];
+            widen(o[i], x);
+            v.set(i, x);
         }
     } else {
+        constexpr uint32_t kWords = kTurnPitch<T> / 16;
+        const uint32_t first = r0 & ~127u, to = static_cast<uint32_t>(__cvta_generic_to_shared(staged)), width = min(128u, a.cols - c0);
+        auto begins = [&](uint32_t r) { return reinterpret_cast<const char*>(src + r * a.stride + c0); };
+        for (uint32_t i = threadIdx.x; i < 128 * kWords; i += kTurnThreads) {
+            const uint32_t row = i / kWords, word = i - row * kWords;
+            if (first + row >= a.rows) break;
+            const char* p = begins(first + row);
+            const uint32_t off = reinterpret_cast<uintptr_t>(p) & 15;
+            if (word * 16 < off + width * sizeof(T)) cp_async16(to + row * kTurnPitch<T> + word * 16, p - off + word * 16);      // (it holds an element of the row)
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncthreads();
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i)
+        for (uint32_t i = 0; i < 8; ++i) {
+            const unsigned char* p = staged + ((r0 & 127) + i) * kTurnPitch<T> + (reinterpret_cast<uintptr_t>(begins(r0 + i)) & 15);
+            float x[8];
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e) {
-                const uint32_t at = c0 + 16 * e + l;
-                v[i][e] = r0 + i < a.rows && at < a.cols ? Store<T>::load1(src + (r0 + i) * a.stride + at) : 0.f;
+                const uint32_t at = 16 * e + l;
+                x[e] = 0.f;
+                if (r0 + i < a.rows && at < width) {
+                    if (sizeof(T) == 4) x[e] = reinterpret_cast<const float*>(p)[at];
+                    else x[e] = __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const unsigned short*>(p)[at]) << 16);
+                }
             }
+            v.set(i, x);
+        }
     }
 }
-template <> __device__ __forceinline__ void load_sub<uint8_t, true>(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, float (&v)[8][8])
+// a matrix that is in eight bits already
+__device__ __forceinline__ void load_block8(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, Block8<bf16>& v)
 {
     const Packed8Layout lay(a.rows, a.cols);
     const char* src = static_cast<const char*>(a.src);
     const uint32_t rt = r0 >> 7, kb = c0 >> 7;
+    const char* codes = src + lay.tile(rt, kb);
+    const unsigned char* scales = reinterpret_cast<const unsigned char*>(src) + lay.scales(rt, kb >> 2) + Packed8Layout::scale_word(r0) + (kb & 3);
     uint2 w[8];
     uint32_t e[8];
 #pragma unroll
@@ -215,59 +345,58 @@ template <> __device__ __forceinline__ void load_sub<uint8_t, true>(const Turn8A
         w[i] = make_uint2(0, 0);
         e[i] = 0;
         if (r0 + i < a.rows) {
-            w[i] = __ldcs(reinterpret_cast<const uint2*>(src + lay.tile(rt, kb) + code_at(r0 + i, c0 + 8 * l)));
-            e[i] = __ldg(reinterpret_cast<const unsigned char*>(src + lay.scales(rt, kb >> 2) + Packed8Layout::scale_word(r0 + i) + (kb & 3)));
+            w[i] = __ldcs(reinterpret_cast<const uint2*>(codes + code_at(r0 + i, c0 + 8 * l)));
+            e[i] = __ldg(scales + 16 * i);      // (eight rows from a multiple of 8: neighbours in the tile of scales)
         }
     }
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
-        values4(w[i].x, block_unit(e[i]), v[i]);
-        values4(w[i].y, block_unit(e[i]), v[i] + 4);
+        float x[8];
+        values4(w[i].x, block_unit(e[i]), x);
+        values4(w[i].y, block_unit(e[i]), x + 4);
+        v.set(i, x);
     }
 }
 
-constexpr int kTurnThreads = 256;
-
-template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(kTurnThreads, 2) turn8_kernel(const Turn8Args a)
+template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(kTurnThreads, sizeof(T) == 4 ? 2 : 3) turn8_kernel(const Turn8Args a)
 {
+    typedef typename Held<T>::type H;
     __shared__ __align__(16) float s_max[kTurnThreads / 32][128];
     __shared__ __align__(16) unsigned char s_tile[128 * 128];
-    __shared__ __align__(16) unsigned char s_rows[BOTH && !OCTETS ? 128 * 128 : 16];
+    extern __shared__ __align__(16) unsigned char s_more[];      // unaligned rows, and with BOTH their codes
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t blocks = (a.cols + 127) / 128, rt = blockIdx.x / blocks, kb = blockIdx.x - rt * blocks;
     const uint32_t l = tid & 15, rg = tid >> 4, r0 = rt * 128 + rg * 8, c0 = kb * 128;
     auto column = [&](uint32_t e) { return OCTETS ? 8 * l + e : l + 16 * e; };
-    float v[8][8];
-    load_sub<T, OCTETS>(a, r0, c0, l, v);
+    Block8<H> v;
+    if constexpr (sizeof(T) == 1) load_block8(a, r0, c0, l, v);
+    else load_block<T, OCTETS>(a, r0, c0, l, s_more, v);
 
     float top[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
-        top[e] = top8(col);
-        top[e] = top2(top[e], __shfl_xor_sync(~0u, top[e], 16));
-    }
+    v.column_tops(top);
     if (lane < 16) {      // kept by lane, so that a lane reads its own columns back in two pieces
         reinterpret_cast<float4*>(s_max[warp])[l] = make_float4(top[0], top[1], top[2], top[3]);
         reinterpret_cast<float4*>(s_max[warp])[16 + l] = make_float4(top[4], top[5], top[6], top[7]);
     }
+    if (!OCTETS && BOTH) __syncthreads();      // (the codes of the rows go where the rows were)
     if (BOTH) {
         const Packed8Layout lay(a.rows, a.cols);
-        char* dst = static_cast<char*>(a.dst);
+        char* dst = static_cast<char*>(a.dst) + lay.tile(rt, kb);
+        char* scales = static_cast<char*>(a.dst) + lay.scales(rt, kb >> 2) + (kb & 3);
+        float most[8];
+        v.row_tops(most);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float most = top8(v[i]);
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) most = top2(most, __shfl_xor_sync(~0u, most, o));
-            const uint32_t e = block_scale(most), r = r0 + i;
-            const uint2 w = codes8(v[i], most, e);
+            const uint32_t e = block_scale(most[i]), r = rg * 8 + i;
+            const float row[8] = {v.get(i, 0), v.get(i, 1), v.get(i, 2), v.get(i, 3), v.get(i, 4), v.get(i, 5), v.get(i, 6), v.get(i, 7)};
+            const uint2 w = codes8(row, most[i], e);
             if (!OCTETS) {
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) s_rows[(rg * 8 + i) * 128 + ((k ^ (r & 7)) << 4) + l] = static_cast<unsigned char>((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
+                for (uint32_t k = 0; k < 8; ++k) s_more[r * 128 + ((k ^ (r & 7)) << 4) + l] = static_cast<unsigned char>((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
             }
-            if (r < a.rows) {
-                if (OCTETS) *reinterpret_cast<uint2*>(dst + lay.tile(rt, kb) + code_at(r, c0 + 8 * l)) = w;
-                if (l == 0) dst[lay.scales(rt, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)] = static_cast<char>(e);
+            if (rt * 128 + r < a.rows) {
+                if (OCTETS) *reinterpret_cast<uint2*>(dst + code_at(r, 8 * l)) = w;
+                if (l == 0) scales[Packed8Layout::scale_word(r)] = static_cast<char>(e);
             }
         }
     }
@@ -280,27 +409,28 @@ template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(
         top[4] = top3(top[4], q.x, y.x); top[5] = top3(top[5], q.y, y.y); top[6] = top3(top[6], q.z, y.z); top[7] = top3(top[7], q.w, y.w);
     }
     const Packed8Layout lay(a.cols, a.rows);
-    char* turned = static_cast<char*>(a.turned);
+    char* turned = static_cast<char*>(a.turned) + lay.tile(kb, rt);
+    char* scales = static_cast<char*>(a.turned) + lay.scales(kb, rt >> 2) + (rt & 3);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const uint32_t s = block_scale(top[e]);
-        const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
-        *reinterpret_cast<uint2*>(s_tile + column(e) * 128 + ((rg ^ l) << 3)) = codes8(col, top[e], s);
-        if (rg == 0 && c0 + column(e) < a.cols) turned[lay.scales(kb, rt >> 2) + Packed8Layout::scale_word(column(e)) + (rt & 3)] = static_cast<char>(s);
+        const float inv = block_inverse(s);
+        uint2 w = make_uint2(codes4(v.get(0, e) * inv, v.get(1, e) * inv, v.get(2, e) * inv, v.get(3, e) * inv),
+                             codes4(v.get(4, e) * inv, v.get(5, e) * inv, v.get(6, e) * inv, v.get(7, e) * inv));
+        if (not_finite(top[e])) w = make_uint2(kNanCodes, kNanCodes);
+        *reinterpret_cast<uint2*>(s_tile + column(e) * 128 + ((rg ^ l) << 3)) = w;
+        if (rg == 0 && c0 + column(e) < a.cols) scales[Packed8Layout::scale_word(column(e))] = static_cast<char>(s);
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const uint32_t at = k * kTurnThreads + tid, row = at >> 3, piece = at & 7, f = OCTETS ? row >> 3 : row & 15;      // f: the lane that wrote the row
-        if (BOTH && !OCTETS) {
-            const Packed8Layout to(a.rows, a.cols);
-            if (rt * 128 + row < a.rows)
-                *reinterpret_cast<uint4*>(static_cast<char*>(a.dst) + to.tile(rt, kb) + at * 16) = *reinterpret_cast<const uint4*>(s_rows + at * 16);
-        }
+        if (BOTH && !OCTETS && rt * 128 + row < a.rows)
+            *reinterpret_cast<uint4*>(static_cast<char*>(a.dst) + Packed8Layout(a.rows, a.cols).tile(rt, kb) + at * 16) = *reinterpret_cast<const uint4*>(s_more + at * 16);
         if (c0 + row < a.cols) {
             const uint4 w = *reinterpret_cast<const uint4*>(s_tile + row * 128 + ((piece ^ (f >> 1)) << 4));
             const uint4 o = f & 1 ? make_uint4(w.z, w.w, w.x, w.y) : w;
-            *reinterpret_cast<uint4*>(turned + lay.tile(kb, rt) + row * 128 + ((piece ^ (row & 7)) << 4)) = o;
+            *reinterpret_cast<uint4*>(turned + row * 128 + ((piece ^ (row & 7)) << 4)) = o;
         }
     }
 }
@@ -334,14 +464,26 @@ template <typename T> int run_unpack8(Unpack8Args& a, void* stream)
 {
     const uint32_t ctas = count_ctas(a);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a.n == 1) unpack8_kernel<T, 1><<<ctas, kWarps8 * 32, 0, s>>>(Unpack8Batch<1>{{a.mat[0]}, 1});
-    else unpack8_kernel<T, kPackBatch><<<ctas, kWarps8 * 32, 0, s>>>(a);
+    bool octets = true;
+    for (uint32_t i = 0; i < a.n; ++i) octets = octets && a.mat[i].vec;
+    auto run = [&](const auto& args, auto batch) {
+        constexpr uint32_t B = decltype(batch)::value;
+        if (octets) unpack8_kernel<T, true, B><<<ctas, kWarps8 * 32, 0, s>>>(args);
+        else unpack8_kernel<T, false, B><<<ctas, kWarps8 * 32, 0, s>>>(args);
+    };
+    if (a.n == 1) run(Unpack8Batch<1>{{a.mat[0]}, 1}, std::integral_constant<uint32_t, 1>());
+    else run(a, std::integral_constant<uint32_t, kPackBatch>());
     return static_cast<int>(cudaGetLastError());
 }
 template <typename T, bool BOTH, bool OCTETS> int run_turn8(const Turn8Args& a, void* stream)
 {
+    constexpr int kMore = OCTETS ? 0 : 128 * kTurnPitch<T>;
+    if (kMore) {
+        const cudaError_t e = opt_in<turn8_kernel<T, BOTH, OCTETS>>(kMore);
+        if (e != cudaSuccess) return static_cast<int>(e);
+    }
     const uint32_t ctas = ((a.rows + 127) / 128) * ((a.cols + 127) / 128);
-    turn8_kernel<T, BOTH, OCTETS><<<ctas, kTurnThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    turn8_kernel<T, BOTH, OCTETS><<<ctas, kTurnThreads, kMore, static_cast<cudaStream_t>(stream)>>>(a);
     return static_cast<int>(cudaGetLastError());
 }
 template <typename T> int run_turn8(const Turn8Args& a, void* stream)

@@ -3,9 +3,25 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "randes_device.cuh"
 
 namespace randes {
+
+// A kernel has to opt in to more than 48 KiB of shared memory, once per device.
+template <auto KERNEL> cudaError_t opt_in(size_t bytes)
+{
+    constexpr int kDevices = 64;
+    static std::atomic<bool> granted[kDevices];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess || (device < kDevices && granted[device].load(std::memory_order_relaxed))) return e;
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == cudaSuccess && device < kDevices) granted[device].store(true, std::memory_order_relaxed);
+    return e;
+}
+
 namespace device {
 
 constexpr uint32_t kNotFinite = 0x7F800000u;      // a greatest magnitude (as bits) from here on: the block holds a NaN or an infinity
