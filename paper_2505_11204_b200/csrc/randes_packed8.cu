@@ -192,13 +192,14 @@ template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_boun
     }
 }
 
-// A tile of 128 x 128 in blocks along its columns, and with BOTH in blocks along its rows too, out of one read. A thread holds rows
-// 8 rg .. 8 rg + 7 of eight columns: 8 l .. 8 l + 7 where rows start on 16-byte boundaries (OCTETS), else l, l + 16 ..
-// l + 112, out of rows that are copied into shared memory as they lie, in 16-byte words from the boundary below their first element
-// (loads of single bf16 elements took three times as long: too few bytes under way). Elements that have 8 bits or fewer behind
-// the leading one stay pairs of bf16. The greatest magnitudes of the columns meet in shared memory; the codes of a column
-// are turned there, 8-byte pieces exchanged by a number that differs between the 16 lanes that write at a time, so that they
-// do not meet in a bank.
+// A tile of 128 x 128 in blocks along its columns, and with BOTH in blocks along its rows too, out of one read. A thread holds eight
+// rows of CPL columns, a row's lanes being neighbours: columns CPL l .. where rows start on 16-byte boundaries (OCTETS: 16 bytes a
+// load), else l, l + L .. out of rows that are copied into shared memory as they lie, in 16-byte words from the boundary below their
+// first element (loads of single bf16 elements took four times as long: too few bytes under way). Elements that have 8 bits or
+// fewer behind the leading one stay pairs of bf16. The greatest magnitudes of the columns meet in shared memory; the codes of
+// a column are turned there, 8-byte pieces exchanged by a number that differs between the 16 lanes that write at a time, so
+// that they do not meet in a bank. (Measured at 8192 x 4096: bf16 with four columns to a thread 26 us instead of 22.5, fp32 with eight
+// 54 instead of 32.)
 __device__ __forceinline__ uint32_t top_bf16x2(uint32_t a, uint32_t b)      // magnitudes; the result's signs mean nothing
 {
     uint32_t r;
@@ -208,39 +209,34 @@ __device__ __forceinline__ uint32_t top_bf16x2(uint32_t a, uint32_t b)      // m
 __device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-template <typename T> struct Block8;      // a thread's 8 x 8 elements
-template <> struct Block8<float> {
-    typedef float4 Top;                   // of four columns
-    float v[8][8];
-    __device__ __forceinline__ void set(int i, int e, float x) { v[i][e] = x; }
-    __device__ __forceinline__ void set(int i, const float (&x)[8])
+template <typename T> struct Part;      // a thread's 8 rows x CPL columns; `set` takes a row as 16 bytes
+template <> struct Part<float> {
+    float v[8][4];
+    __device__ __forceinline__ void set(int i, const uint4& x) { Store<float>::widen(x, v[i]); }
+    __device__ __forceinline__ void set(int i, const float (&x)[4])
     {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = x[e];
+        for (int e = 0; e < 4; ++e) v[i][e] = x[e];
     }
     __device__ __forceinline__ float get(int i, int e) const { return v[i][e]; }
-    __device__ __forceinline__ void column_tops(float (&top)[8]) const
+    __device__ __forceinline__ void column_tops(float (&top)[4]) const
     {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4; ++e) {
             const float col[8] = {v[0][e], v[1][e], v[2][e], v[3][e], v[4][e], v[5][e], v[6][e], v[7][e]};
             top[e] = top8(col);
-            top[e] = top2(top[e], __shfl_xor_sync(~0u, top[e], 16));
         }
     }
-    // of every row, over the 16 lanes that hold it
     __device__ __forceinline__ void row_tops(float (&top)[8]) const
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            top[i] = top8(v[i]);
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) top[i] = top2(top[i], __shfl_xor_sync(~0u, top[i], o));
-        }
+        for (int i = 0; i < 8; ++i)      // (as bits: none is negative)
+            top[i] = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top3(v[i][0], v[i][1], top2(v[i][2], v[i][3])))));
     }
 };
-template <> struct Block8<bf16> {
+template <> struct Part<bf16> {
     uint32_t w[8][4];
+    __device__ __forceinline__ void set(int i, const uint4& x) { w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w; }
     __device__ __forceinline__ void set(int i, const float (&x)[8])      // (exact: at most 8 bits each)
     {
 #pragma unroll
@@ -254,12 +250,12 @@ template <> struct Block8<bf16> {
             uint32_t m = top_bf16x2(w[0][j], w[1][j]);
 #pragma unroll
             for (int i = 2; i < 8; ++i) m = top_bf16x2(m, w[i][j]);
-            m = top_bf16x2(m, __shfl_xor_sync(~0u, m, 16));
+            m = top_bf16x2(m, __shfl_xor_sync(~0u, m, 16));      // the other rows of the warp
             top[2 * j] = fabsf(low_half(m));
             top[2 * j + 1] = fabsf(high_half(m));
         }
     }
-    __device__ __forceinline__ void row_tops(float (&top)[8]) const      // two rows to a word
+    __device__ __forceinline__ void row_tops(float (&top)[8]) const      // over 16 lanes, two rows to a word
     {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
@@ -273,53 +269,59 @@ template <> struct Block8<bf16> {
         }
     }
 };
-template <typename T> struct Held { typedef T type; };
-template <> struct Held<uint8_t> { typedef bf16 type; };
-
-constexpr int kTurnThreads = 256;
-// shared memory of an unaligned tile's rows: a row's words, one more than it has itself
-template <typename T> constexpr uint32_t kTurnPitch = 128 * sizeof(T) + 16;
+// what a source's elements are held as, columns to a thread, threads to a row and to a CTA
+template <typename T> struct Turn {
+    typedef T Held;
+    static constexpr int CPL = 16 / sizeof(T), L = 128 / CPL, kThreads = 16 * L;
+    static constexpr uint32_t kPitch = 128 * sizeof(T) + 16;      // shared memory of an unaligned row: its words, one more than it has itself
+};
+template <> struct Turn<uint8_t> : Turn<bf16> {};
 
 template <typename T, bool OCTETS>
-__device__ __forceinline__ void load_block(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, unsigned char* staged, Block8<T>& v)
+__device__ __forceinline__ void load_part(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, unsigned char* staged, Part<T>& v)
 {
+    typedef Turn<T> U;
+    constexpr uint32_t CPL = U::CPL;
     const T* src = static_cast<const T*>(a.src);
     if (OCTETS) {
-        Octet<T> o[8];
+        const uint32_t c = c0 + CPL * l;
+        const T* p = src + r0 * a.stride + c;
+        if (r0 + 8 <= a.rows && c + CPL <= a.cols) {
+            uint4 x[8];
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            if (r0 + i < a.rows) o[i] = load_octet(src + (r0 + i) * a.stride, c0 + 8 * l, a.cols);
-            else
+            for (int i = 0; i < 8; ++i) x[i] = __ldcs(reinterpret_cast<const uint4*>(p + i * a.stride));
 #pragma unroll
-                for (int h = 0; h < static_cast<int>(sizeof(T)) / 2; ++h) o[i].w[h] = make_uint4(0, 0, 0, 0);
-        }
+            for (int i = 0; i < 8; ++i) v.set(i, x[i]);
+        } else {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            float x[8];
-            widen(o[i], x);
-            v.set(i, x);
+            for (uint32_t i = 0; i < 8; ++i) {
+                float x[CPL];
+#pragma unroll
+                for (uint32_t e = 0; e < CPL; ++e) x[e] = r0 + i < a.rows && c + e < a.cols ? Store<T>::load1(p + i * a.stride + e) : 0.f;
+                v.set(i, x);
+            }
         }
     } else {
-        constexpr uint32_t kWords = kTurnPitch<T> / 16;
+        constexpr uint32_t kWords = U::kPitch / 16;
         const uint32_t first = r0 & ~127u, to = static_cast<uint32_t>(__cvta_generic_to_shared(staged)), width = min(128u, a.cols - c0);
         auto begins = [&](uint32_t r) { return reinterpret_cast<const char*>(src + r * a.stride + c0); };
-        for (uint32_t i = threadIdx.x; i < 128 * kWords; i += kTurnThreads) {
+        for (uint32_t i = threadIdx.x; i < 128 * kWords; i += U::kThreads) {
             const uint32_t row = i / kWords, word = i - row * kWords;
             if (first + row >= a.rows) break;
             const char* p = begins(first + row);
             const uint32_t off = reinterpret_cast<uintptr_t>(p) & 15;
-            if (word * 16 < off + width * sizeof(T)) cp_async16(to + row * kTurnPitch<T> + word * 16, p - off + word * 16);      // (it holds an element of the row)
+            if (word * 16 < off + width * sizeof(T)) cp_async16(to + row * U::kPitch + word * 16, p - off + word * 16);      // (it holds an element of the row)
         }
         cp_async_commit();
         cp_async_wait<0>();
         __syncthreads();
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
-            const unsigned char* p = staged + ((r0 & 127) + i) * kTurnPitch<T> + (reinterpret_cast<uintptr_t>(begins(r0 + i)) & 15);
-            float x[8];
+            const unsigned char* p = staged + ((r0 & 127) + i) * U::kPitch + (reinterpret_cast<uintptr_t>(begins(r0 + i)) & 15);
+            float x[CPL];
 #pragma unroll
-            for (uint32_t e = 0; e < 8; ++e) {
-                const uint32_t at = 16 * e + l;
+            for (uint32_t e = 0; e < CPL; ++e) {
+                const uint32_t at = U::L * e + l;
                 x[e] = 0.f;
                 if (r0 + i < a.rows && at < width) {
                     if (sizeof(T) == 4) x[e] = reinterpret_cast<const float*>(p)[at];
@@ -331,13 +333,12 @@ __device__ __forceinline__ void load_block(const Turn8Args& a, uint32_t r0, uint
     }
 }
 // a matrix that is in eight bits already
-__device__ __forceinline__ void load_block8(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, Block8<bf16>& v)
+__device__ __forceinline__ void load_part8(const Turn8Args& a, uint32_t r0, uint32_t c0, uint32_t l, Part<bf16>& v)
 {
     const Packed8Layout lay(a.rows, a.cols);
-    const char* src = static_cast<const char*>(a.src);
     const uint32_t rt = r0 >> 7, kb = c0 >> 7;
-    const char* codes = src + lay.tile(rt, kb);
-    const unsigned char* scales = reinterpret_cast<const unsigned char*>(src) + lay.scales(rt, kb >> 2) + Packed8Layout::scale_word(r0) + (kb & 3);
+    const char* codes = static_cast<const char*>(a.src) + lay.tile(rt, kb);
+    const unsigned char* scales = static_cast<const unsigned char*>(a.src) + lay.scales(rt, kb >> 2) + Packed8Layout::scale_word(r0) + (kb & 3);
     uint2 w[8];
     uint32_t e[8];
 #pragma unroll
@@ -345,7 +346,7 @@ __device__ __forceinline__ void load_block8(const Turn8Args& a, uint32_t r0, uin
         w[i] = make_uint2(0, 0);
         e[i] = 0;
         if (r0 + i < a.rows) {
-            w[i] = __ldcs(reinterpret_cast<const uint2*>(codes + code_at(r0 + i, c0 + 8 * l)));
+            w[i] = __ldcs(reinterpret_cast<const uint2*>(codes + code_at(r0 + i, 8 * l)));
             e[i] = __ldg(scales + 16 * i);      // (eight rows from a multiple of 8: neighbours in the tile of scales)
         }
     }
@@ -358,25 +359,29 @@ __device__ __forceinline__ void load_block8(const Turn8Args& a, uint32_t r0, uin
     }
 }
 
-template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(kTurnThreads, sizeof(T) == 4 ? 2 : 3) turn8_kernel(const Turn8Args a)
+template <typename T, bool BOTH, bool OCTETS>
+__global__ void __launch_bounds__(Turn<T>::kThreads, sizeof(T) == 4 ? 2 : (BOTH ? 3 : 4)) turn8_kernel(const Turn8Args a)
 {
-    typedef typename Held<T>::type H;
-    __shared__ __align__(16) float s_max[kTurnThreads / 32][128];
+    typedef Turn<T> U;
+    typedef typename U::Held H;
+    constexpr int kWarps = U::kThreads / 32, CPL = U::CPL;
+    constexpr uint32_t L = U::L;
+    __shared__ __align__(16) float s_max[kWarps][128];
     __shared__ __align__(16) unsigned char s_tile[128 * 128];
     extern __shared__ __align__(16) unsigned char s_more[];      // unaligned rows, and with BOTH their codes
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t blocks = (a.cols + 127) / 128, rt = blockIdx.x / blocks, kb = blockIdx.x - rt * blocks;
-    const uint32_t l = tid & 15, rg = tid >> 4, r0 = rt * 128 + rg * 8, c0 = kb * 128;
-    auto column = [&](uint32_t e) { return OCTETS ? 8 * l + e : l + 16 * e; };
-    Block8<H> v;
-    if constexpr (sizeof(T) == 1) load_block8(a, r0, c0, l, v);
-    else load_block<T, OCTETS>(a, r0, c0, l, s_more, v);
+    const uint32_t l = tid % L, rg = tid / L, r0 = rt * 128 + rg * 8, c0 = kb * 128;
+    auto column = [&](uint32_t e) { return OCTETS ? CPL * l + e : l + L * e; };
+    Part<H> v;
+    if constexpr (sizeof(T) == 1) load_part8(a, r0, c0, l, v);
+    else load_part<T, OCTETS>(a, r0, c0, l, s_more, v);
 
-    float top[8];
+    float top[CPL];
     v.column_tops(top);
-    if (lane < 16) {      // kept by lane, so that a lane reads its own columns back in two pieces
-        reinterpret_cast<float4*>(s_max[warp])[l] = make_float4(top[0], top[1], top[2], top[3]);
-        reinterpret_cast<float4*>(s_max[warp])[16 + l] = make_float4(top[4], top[5], top[6], top[7]);
+    if (lane < static_cast<int>(L)) {      // by lane: it reads its own columns back
+#pragma unroll
+        for (int h = 0; h < CPL / 4; ++h) reinterpret_cast<float4*>(s_max[warp])[h * L + l] = make_float4(top[4 * h], top[4 * h + 1], top[4 * h + 2], top[4 * h + 3]);
     }
     if (!OCTETS && BOTH) __syncthreads();      // (the codes of the rows go where the rows were)
     if (BOTH) {
@@ -388,43 +393,55 @@ template <typename T, bool BOTH, bool OCTETS> __global__ void __launch_bounds__(
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t e = block_scale(most[i]), r = rg * 8 + i;
-            const float row[8] = {v.get(i, 0), v.get(i, 1), v.get(i, 2), v.get(i, 3), v.get(i, 4), v.get(i, 5), v.get(i, 6), v.get(i, 7)};
-            const uint2 w = codes8(row, most[i], e);
+            const float inv = block_inverse(e);
+            uint32_t w[CPL / 4];
+#pragma unroll
+            for (int h = 0; h < CPL / 4; ++h) {
+                w[h] = codes4(v.get(i, 4 * h) * inv, v.get(i, 4 * h + 1) * inv, v.get(i, 4 * h + 2) * inv, v.get(i, 4 * h + 3) * inv);
+                if (not_finite(most[i])) w[h] = kNanCodes;
+            }
             if (!OCTETS) {
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) s_more[r * 128 + ((k ^ (r & 7)) << 4) + l] = static_cast<unsigned char>((k < 4 ? w.x : w.y) >> (8 * (k & 3)));
+                for (uint32_t k = 0; k < CPL; ++k) s_more[r * 128 + ((column(k) >> 4 ^ (r & 7)) << 4) + (column(k) & 15)] = static_cast<unsigned char>(w[k / 4] >> (8 * (k & 3)));
             }
             if (rt * 128 + r < a.rows) {
-                if (OCTETS) *reinterpret_cast<uint2*>(dst + code_at(r, 8 * l)) = w;
+                if (OCTETS) {
+                    char* to = dst + code_at(r, CPL * l & ~7u) + (CPL * l & 7);
+                    if (CPL == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[CPL / 4 - 1]);
+                    else *reinterpret_cast<uint32_t*>(to) = w[0];
+                }
                 if (l == 0) scales[Packed8Layout::scale_word(r)] = static_cast<char>(e);
             }
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kTurnThreads / 32; w += 2) {
-        const float4 p = reinterpret_cast<const float4*>(s_max[w])[l], q = reinterpret_cast<const float4*>(s_max[w])[16 + l];
-        const float4 x = reinterpret_cast<const float4*>(s_max[w + 1])[l], y = reinterpret_cast<const float4*>(s_max[w + 1])[16 + l];
-        top[0] = top3(top[0], p.x, x.x); top[1] = top3(top[1], p.y, x.y); top[2] = top3(top[2], p.z, x.z); top[3] = top3(top[3], p.w, x.w);
-        top[4] = top3(top[4], q.x, y.x); top[5] = top3(top[5], q.y, y.y); top[6] = top3(top[6], q.z, y.z); top[7] = top3(top[7], q.w, y.w);
-    }
+    for (int w = 0; w < kWarps; w += 2)
+#pragma unroll
+        for (int h = 0; h < CPL / 4; ++h) {
+            const float4 p = reinterpret_cast<const float4*>(s_max[w])[h * L + l], x = reinterpret_cast<const float4*>(s_max[w + 1])[h * L + l];
+            top[4 * h] = top3(top[4 * h], p.x, x.x);
+            top[4 * h + 1] = top3(top[4 * h + 1], p.y, x.y);
+            top[4 * h + 2] = top3(top[4 * h + 2], p.z, x.z);
+            top[4 * h + 3] = top3(top[4 * h + 3], p.w, x.w);
+        }
     const Packed8Layout lay(a.cols, a.rows);
     char* turned = static_cast<char*>(a.turned) + lay.tile(kb, rt);
     char* scales = static_cast<char*>(a.turned) + lay.scales(kb, rt >> 2) + (rt & 3);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < CPL; ++e) {
         const uint32_t s = block_scale(top[e]);
         const float inv = block_inverse(s);
         uint2 w = make_uint2(codes4(v.get(0, e) * inv, v.get(1, e) * inv, v.get(2, e) * inv, v.get(3, e) * inv),
                              codes4(v.get(4, e) * inv, v.get(5, e) * inv, v.get(6, e) * inv, v.get(7, e) * inv));
         if (not_finite(top[e])) w = make_uint2(kNanCodes, kNanCodes);
-        *reinterpret_cast<uint2*>(s_tile + column(e) * 128 + ((rg ^ l) << 3)) = w;
+        *reinterpret_cast<uint2*>(s_tile + column(e) * 128 + ((rg ^ (l & 15)) << 3)) = w;
         if (rg == 0 && c0 + column(e) < a.cols) scales[Packed8Layout::scale_word(column(e))] = static_cast<char>(s);
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const uint32_t at = k * kTurnThreads + tid, row = at >> 3, piece = at & 7, f = OCTETS ? row >> 3 : row & 15;      // f: the lane that wrote the row
+    for (int k = 0; k < 1024 / U::kThreads; ++k) {
+        const uint32_t at = k * U::kThreads + tid, row = at >> 3, piece = at & 7, f = (OCTETS ? row / CPL : row) & 15;      // f: of the lane that wrote the row
         if (BOTH && !OCTETS && rt * 128 + row < a.rows)
             *reinterpret_cast<uint4*>(static_cast<char*>(a.dst) + Packed8Layout(a.rows, a.cols).tile(rt, kb) + at * 16) = *reinterpret_cast<const uint4*>(s_more + at * 16);
         if (c0 + row < a.cols) {
@@ -477,13 +494,13 @@ template <typename T> int run_unpack8(Unpack8Args& a, void* stream)
 }
 template <typename T, bool BOTH, bool OCTETS> int run_turn8(const Turn8Args& a, void* stream)
 {
-    constexpr int kMore = OCTETS ? 0 : 128 * kTurnPitch<T>;
+    constexpr int kMore = OCTETS ? 0 : 128 * Turn<T>::kPitch;
     if (kMore) {
         const cudaError_t e = opt_in<turn8_kernel<T, BOTH, OCTETS>>(kMore);
         if (e != cudaSuccess) return static_cast<int>(e);
     }
     const uint32_t ctas = ((a.rows + 127) / 128) * ((a.cols + 127) / 128);
-    turn8_kernel<T, BOTH, OCTETS><<<ctas, kTurnThreads, kMore, static_cast<cudaStream_t>(stream)>>>(a);
+    turn8_kernel<T, BOTH, OCTETS><<<ctas, Turn<T>::kThreads, kMore, static_cast<cudaStream_t>(stream)>>>(a);
     return static_cast<int>(cudaGetLastError());
 }
 template <typename T> int run_turn8(const Turn8Args& a, void* stream)
