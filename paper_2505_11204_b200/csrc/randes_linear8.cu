@@ -84,7 +84,9 @@ __device__ __forceinline__ uint32_t of_rank(uint32_t saddr, uint32_t rank)      
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ void cluster_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// (Relaxed: what is handed over is tensor memory, whose loads have been waited for; a release would wait for the stores of the tile
+// before as well.)
+__device__ __forceinline__ void cluster_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void tc_load32(uint32_t t, uint32_t (&v)[32])
 {
     asm volatile(
@@ -280,6 +282,7 @@ template <int N, typename X> __global__ void __launch_bounds__(kThreads8, 1) lin
     __syncthreads();
     tc_after();
     const uint32_t tmem = words[0];
+    after_last();
 
     if (warp == 0) {
         const char *w = static_cast<const char*>(a.w), *x = static_cast<const char*>(a.x);
@@ -459,7 +462,7 @@ struct Pair8 {
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Pair8::kThreads, 1)
+__global__ void __launch_bounds__(Pair8::kThreads, 1)
 linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
                     const __grid_constant__ CUtensorMap map_xs, const Linear8Args a)
 {
@@ -505,6 +508,7 @@ linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     cluster.sync();
     tc_after();
     const uint32_t tmem = words[0];
+    after_last();
 
     if (warp == 0) {
         Ring<S> at;
@@ -632,18 +636,8 @@ template <int N, typename X> int run_linear8(Linear8Args& a, int sm_count, cudaS
     if (tiles > 0x7FFFFFFFu) return static_cast<int>(cudaErrorInvalidValue);
     a.log_ranks = 0;      // CTAs share a tile's columns as long as all fit the SMs at once
     while (a.log_ranks < 3 && (tiles << (a.log_ranks + 1)) <= static_cast<uint64_t>(sm_count) && (2u << a.log_ranks) <= lw.col_blocks) ++a.log_ranks;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(a.log_ranks ? tiles << a.log_ranks : std::min<uint64_t>(tiles, sm_count)));
-    cfg.blockDim = dim3(kThreads8);
-    cfg.dynamicSmemBytes = G::kSmem;
-    cfg.stream = stream;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 1u << a.log_ranks;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = a.log_ranks ? 1 : 0;
-    return static_cast<int>(cudaLaunchKernelEx(&cfg, linear8_kernel<N, X>, a));
+    const uint32_t ctas = static_cast<uint32_t>(a.log_ranks ? tiles << a.log_ranks : std::min<uint64_t>(tiles, sm_count));
+    return static_cast<int>(launch_early(linear8_kernel<N, X>, ctas, kThreads8, G::kSmem, stream, 1u << a.log_ranks, a));
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -684,8 +678,7 @@ int run_pairs(const Linear8Args& a, int sm_count, cudaStream_t stream)
         return static_cast<int>(cudaErrorInvalidValue);
     const uint64_t tiles = static_cast<uint64_t>((lw.row_tiles + 1) / 2) * ((lx.row_tiles + 1) / 2);
     const unsigned grid = static_cast<unsigned>(std::min<uint64_t>(tiles, sm_count / 2) * 2);
-    linear8_pair_kernel<<<grid, Pair8::kThreads, Pair8::kSmem, stream>>>(mw, mws, mx, mxs, a);
-    return static_cast<int>(cudaGetLastError());
+    return static_cast<int>(launch_early(linear8_pair_kernel, grid, Pair8::kThreads, Pair8::kSmem, stream, 2, mw, mws, mx, mxs, a));
 }
 
 }  // namespace

@@ -119,6 +119,7 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
     if (THREADS == 32 && r >= a.rows) return;
     const uint32_t cols = a.cols;
     const Packed8Layout lay(a.rows, cols);
+    after_last();
 
     float v[CHUNKS][8];
     {
@@ -192,6 +193,7 @@ __global__ void __launch_bounds__(THREADS) norm_grad_kernel(const NormGradArgs a
     auto column = [&](int k, uint32_t e) { return (k * THREADS + (t & ~31)) * 8 + (OCTETS ? 8 * lane + e : 32 * e + lane); };
     float sum[CHUNKS][8] = {};
     uint32_t turn = 0;
+    after_last();
     for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
         float n[CHUNKS][8], g[CHUNKS][8];
         const float s = __ldg(a.rstd + r);
@@ -411,6 +413,7 @@ __global__ void __launch_bounds__(GradRing<T, TEAM>::kThreads, GradRing<T, TEAM>
         }
     };
 
+    after_last();
     float gain[16], sum[16] = {};
 #pragma unroll
     for (uint32_t e = 0; e < 16; ++e) gain[e] = a.gain && column(e) < cols ? gain_at(a.gain, a.gain_bf16, column(e)) : 1.f;
@@ -551,6 +554,7 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_gain_kernel(const float* p
     __shared__ float s[kSumRows][33];
     const uint32_t x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     float v = 0.f;
+    after_last();
     if (c < cols)
         for (uint32_t i = y; i < n; i += kSumRows) v += partial[static_cast<size_t>(i) * cols + c];
     s[y][x] = v;
@@ -591,8 +595,7 @@ template <typename T, int TEAM, bool OCTETS> int run_ring(const NormGradArgs& a,
     const cudaError_t e = opt_in<norm_grad_ring_kernel<T, TEAM, OCTETS>>(G::kSmem);
     if (e != cudaSuccess) return static_cast<int>(e);
     *ctas = ring_ctas<T, TEAM>(a.rows);
-    norm_grad_ring_kernel<T, TEAM, OCTETS><<<*ctas, G::kThreads, G::kSmem, stream>>>(a);
-    return static_cast<int>(cudaGetLastError());
+    return static_cast<int>(launch_early(norm_grad_ring_kernel<T, TEAM, OCTETS>, *ctas, G::kThreads, G::kSmem, stream, 1, a));
 }
 template <typename T, bool OCTETS> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
 {
@@ -608,9 +611,7 @@ template <bool OCTETS> int run_norm(int dtype, const NormArgs& a, cudaStream_t s
     return by_width(a.cols, [&](auto threads, auto chunks) {
         constexpr int T = decltype(threads)::value, C = decltype(chunks)::value, R = kRowsPerCta<T>;
         const uint32_t ctas = a.rows / R + (a.rows % R != 0);
-        if (dtype) norm_kernel<bf16, T, C, OCTETS><<<ctas, T * R, 0, stream>>>(a);
-        else norm_kernel<float, T, C, OCTETS><<<ctas, T * R, 0, stream>>>(a);
-        return static_cast<int>(cudaGetLastError());
+        return static_cast<int>(launch_early(dtype ? norm_kernel<bf16, T, C, OCTETS> : norm_kernel<float, T, C, OCTETS>, ctas, T * R, 0, stream, 1, a));
     });
 }
 template <bool OCTETS> int run_grad(int dtype, const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
@@ -619,9 +620,7 @@ template <bool OCTETS> int run_grad(int dtype, const NormGradArgs& a, uint32_t* 
     *ctas = std::min(a.rows, kSms);
     auto run = [&](auto threads) {
         constexpr int T = decltype(threads)::value;
-        if (dtype) norm_grad_kernel<bf16, T, 4, OCTETS><<<*ctas, T, 0, stream>>>(a);
-        else norm_grad_kernel<float, T, 4, OCTETS><<<*ctas, T, 0, stream>>>(a);
-        return static_cast<int>(cudaGetLastError());
+        return static_cast<int>(launch_early(dtype ? norm_grad_kernel<bf16, T, 4, OCTETS> : norm_grad_kernel<float, T, 4, OCTETS>, *ctas, T, 0, stream, 1, a));
     };
     return a.cols <= 16384 ? run(Const<512>()) : run(Const<1024>());
 }
@@ -647,8 +646,7 @@ int launch_norm_grad(int dtype, const NormGradArgs& a, int* launched, void* stre
     if (e) return e;
     *launched = 1;
     if (!a.dgain) return 0;
-    norm_gain_kernel<<<(a.cols + 31) / 32, 32 * kSumRows, 0, s>>>(a.partial, ctas, a.cols, a.dgain);
-    const int e2 = static_cast<int>(cudaGetLastError());
+    const int e2 = static_cast<int>(launch_early(norm_gain_kernel, (a.cols + 31) / 32, 32 * kSumRows, 0, s, 1, static_cast<const float*>(a.partial), ctas, a.cols, a.dgain));
     if (!e2) *launched = 2;
     return e2;
 }

@@ -62,6 +62,7 @@ template <typename T, typename M, bool RETRIEVE, bool OCTETS, uint32_t BATCH>
 __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_constant__ Pack8Batch<BATCH> a)
 {
     constexpr bool kBoth = OCTETS && sizeof(T) + (RETRIEVE ? sizeof(M) : 0) <= 4;
+    after_last();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Pack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
     const Packed8Layout lay(m.rows, m.cols);
@@ -126,6 +127,7 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
 template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 * 32) unpack8_kernel(const __grid_constant__ Unpack8Batch<BATCH> a)
 {
     constexpr uint32_t CPL = OCTETS ? Store<T>::CPL : 8, kSteps = 512 / 32 / CPL;      // columns to a lane and step
+    after_last();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Unpack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
     const Packed8Layout lay(m.rows, m.cols);
@@ -373,6 +375,7 @@ __global__ void __launch_bounds__(Turn<T>::kThreads, sizeof(T) == 4 ? 2 : (BOTH 
     const uint32_t blocks = (a.cols + 127) / 128, rt = blockIdx.x / blocks, kb = blockIdx.x - rt * blocks;
     const uint32_t l = tid % L, rg = tid / L, r0 = rt * 128 + rg * 8, c0 = kb * 128;
     auto column = [&](uint32_t e) { return OCTETS ? CPL * l + e : l + L * e; };
+    after_last();
     Part<H> v;
     if constexpr (sizeof(T) == 1) load_part8(a, r0, c0, l, v);
     else load_part<T, OCTETS>(a, r0, c0, l, s_more, v);
@@ -470,12 +473,10 @@ template <typename T, typename M, bool RETRIEVE> int run_pack8(Pack8Args& a, voi
     for (uint32_t i = 0; i < a.n; ++i) octets = octets && a.mat[i].vec == (RETRIEVE ? 3u : 1u);
     auto run = [&](const auto& args, auto batch) {
         constexpr uint32_t B = decltype(batch)::value;
-        if (octets) pack8_kernel<T, M, RETRIEVE, true, B><<<ctas, kWarps8 * 32, 0, s>>>(args);
-        else pack8_kernel<T, M, RETRIEVE, false, B><<<ctas, kWarps8 * 32, 0, s>>>(args);
+        return launch_early(octets ? pack8_kernel<T, M, RETRIEVE, true, B> : pack8_kernel<T, M, RETRIEVE, false, B>, ctas, kWarps8 * 32, 0, s, 1, args);
     };
-    if (a.n == 1) run(Pack8Batch<1>{{a.mat[0]}, 1, a.lambda, a.task}, std::integral_constant<uint32_t, 1>());
-    else run(a, std::integral_constant<uint32_t, kPackBatch>());
-    return static_cast<int>(cudaGetLastError());
+    return static_cast<int>(a.n == 1 ? run(Pack8Batch<1>{{a.mat[0]}, 1, a.lambda, a.task}, std::integral_constant<uint32_t, 1>())
+                                     : run(a, std::integral_constant<uint32_t, kPackBatch>()));
 }
 template <typename T> int run_unpack8(Unpack8Args& a, void* stream)
 {
@@ -485,12 +486,10 @@ template <typename T> int run_unpack8(Unpack8Args& a, void* stream)
     for (uint32_t i = 0; i < a.n; ++i) octets = octets && a.mat[i].vec;
     auto run = [&](const auto& args, auto batch) {
         constexpr uint32_t B = decltype(batch)::value;
-        if (octets) unpack8_kernel<T, true, B><<<ctas, kWarps8 * 32, 0, s>>>(args);
-        else unpack8_kernel<T, false, B><<<ctas, kWarps8 * 32, 0, s>>>(args);
+        return launch_early(octets ? unpack8_kernel<T, true, B> : unpack8_kernel<T, false, B>, ctas, kWarps8 * 32, 0, s, 1, args);
     };
-    if (a.n == 1) run(Unpack8Batch<1>{{a.mat[0]}, 1}, std::integral_constant<uint32_t, 1>());
-    else run(a, std::integral_constant<uint32_t, kPackBatch>());
-    return static_cast<int>(cudaGetLastError());
+    return static_cast<int>(a.n == 1 ? run(Unpack8Batch<1>{{a.mat[0]}, 1}, std::integral_constant<uint32_t, 1>())
+                                     : run(a, std::integral_constant<uint32_t, kPackBatch>()));
 }
 template <typename T, bool BOTH, bool OCTETS> int run_turn8(const Turn8Args& a, void* stream)
 {
@@ -500,8 +499,7 @@ template <typename T, bool BOTH, bool OCTETS> int run_turn8(const Turn8Args& a, 
         if (e != cudaSuccess) return static_cast<int>(e);
     }
     const uint32_t ctas = ((a.rows + 127) / 128) * ((a.cols + 127) / 128);
-    turn8_kernel<T, BOTH, OCTETS><<<ctas, Turn<T>::kThreads, kMore, static_cast<cudaStream_t>(stream)>>>(a);
-    return static_cast<int>(cudaGetLastError());
+    return static_cast<int>(launch_early(turn8_kernel<T, BOTH, OCTETS>, ctas, Turn<T>::kThreads, kMore, static_cast<cudaStream_t>(stream), 1, a));
 }
 template <typename T> int run_turn8(const Turn8Args& a, void* stream)
 {

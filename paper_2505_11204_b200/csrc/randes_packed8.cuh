@@ -4,6 +4,7 @@
 #include <cuda_fp16.h>
 
 #include <atomic>
+#include <utility>
 
 #include "randes_device.cuh"
 
@@ -22,7 +23,36 @@ template <auto KERNEL> cudaError_t opt_in(size_t bytes)
     return e;
 }
 
+// Launch in stream order, except that the kernel's CTAs may take their places while the kernel before it still runs: each of its
+// threads calls after_last() before it touches memory of the caller's. (A chain of small kernels then does not pay for a launch
+// between them: 2 to 3 us each.)
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), uint32_t ctas, uint32_t threads, size_t smem, cudaStream_t stream, uint32_t cluster, Args&&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
 namespace device {
+
+// Waits until what ran before in the stream has written its results; and lets what runs next take its places once every CTA has said so.
+__device__ __forceinline__ void after_last()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 constexpr uint32_t kNotFinite = 0x7F800000u;      // a greatest magnitude (as bits) from here on: the block holds a NaN or an infinity
 

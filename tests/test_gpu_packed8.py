@@ -284,3 +284,37 @@ def test_refusals():
         assert e.value.code == code, (i, e.value)
     again = randes.Packed8Matrix(8, 256, w.data.clone())
     assert torch.equal(again.unpack(), w.unpack())
+
+
+def test_chains_of_calls_in_graphs_that_fork_and_join():
+    """Kernels take their places early: what they read has to be complete all the same, in a captured chain too."""
+    n, cols = 64, 1024
+    w = [randes.pack8(weight(cols, cols, torch.bfloat16, i)) for i in range(4)]
+    x, gain = weight(n, cols, torch.bfloat16, 9, 1.0), torch.ones(cols, device="cuda")
+
+    def chain(x, join):
+        h = x
+        for q in w:
+            f = randes.rms_norm(randes.packed8_linear(h, q, y_dtype=randes.BF16), gain, h, packed=True)
+            h = f.h + 0                                    # another library's kernel in between
+            if join is not None:
+                join[0].wait_stream(torch.cuda.current_stream())
+                with torch.cuda.stream(join[0]):
+                    side = randes.packed8_linear(f.y, q, y_dtype=randes.BF16)
+                torch.cuda.current_stream().wait_stream(join[0])
+            else:
+                side = randes.packed8_linear(f.y, q, y_dtype=randes.BF16)
+            h = randes.rms_norm(h, gain, side).h
+        return h
+
+    want = chain(x, None)
+    torch.cuda.synchronize()
+    assert torch.isfinite(want.float()).all()
+    for join in (None, [torch.cuda.Stream()]):
+        buf, g = x.clone(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = chain(buf, join)
+        for _ in range(5):
+            out.zero_()
+            g.replay()
+            assert torch.equal(out, want)
