@@ -6,8 +6,10 @@ A stack of square layers and a vocabulary head stands in for a language model.  
 one superposition; base and superposition are then packed into four bits.  A batch of sequences, each of its own task, is
 decoded token by token: every layer is one call for the whole batch (the base read once, each slot of the superposition
 once), the head's logits are scored, the best token goes on.  The same sequences are also decoded with the retrieved fp32
-weights, and the log probabilities are compared.  Last, one more task learns: a few steps on its head with the gradient of
-the token log probabilities, and the result is added to the superposition.
+weights, and the log probabilities are compared.  Prompts of many tokens are read with each task's weights retrieved into eight
+bits: products on the tensor core, the last residual and the norm in front of the head in one pass.  Last, one more task learns: a
+few steps on its head with the gradient of the token log probabilities, a few on a layer with activations kept in eight bits, and
+the results are added to the superposition.
 """
 from __future__ import annotations
 
@@ -18,6 +20,7 @@ import torch
 
 from . import randes
 from .scoring import token_log_probs
+from .training import norm_linear
 
 
 def build(width: int, blocks: int, vocab: int, n_tasks: int, seed: int = 0):
@@ -77,6 +80,56 @@ def serve(width=1024, blocks=6, vocab=32128, n_tasks=4, n_tokens=8, steps=16, gr
     return {"tokens": tokens, "packed": packed_lp, "full": full, "bytes": (2 * full_bytes, 2 * packed_bytes)}
 
 
+def read_prompts(width=1024, blocks=6, vocab=32128, n_tasks=4, n_tokens=512, lam=0.5, seed=0):
+    """Scores every next token of a prompt per task, with the task's weights in eight bits and in their own type; returns both sets of
+    log probabilities [n_tasks, n_tokens - 1] and the bytes of a model in either form."""
+    plan, base, models, M = build(width, blocks, vocab, n_tasks, seed)
+    gen = torch.Generator(device="cuda").manual_seed(seed + 3)
+    angles = torch.arange(1, width + 1, device="cuda").float()[None] * 0.37
+    eight = torch.empty(n_tasks, n_tokens - 1, device="cuda")
+    full = torch.empty_like(eight)
+    for t in range(n_tasks):
+        prompt = torch.randint(0, vocab, (n_tokens,), generator=gen, device="cuda")
+        x = torch.sin(prompt[:-1].float()[:, None] * angles)       # the pseudo-embedding that decoding uses
+        w8 = plan.retrieve_packed8(t, lam, base, M)
+        h, delta = x, None
+        for l in range(blocks):
+            h = h if delta is None else h + delta
+            delta = torch.tanh(randes.packed8_linear(h, w8[l]))
+        f = randes.rms_norm(delta, None, h, packed=True)
+        eight[t] = randes.token_scores(randes.packed8_linear(f.y, w8[blocks]), prompt[1:]).logprob
+        w, h = plan.retrieve(t, lam, base, M), x
+        for l in range(blocks):
+            h = h + torch.tanh(h @ w[l].t())
+        full[t] = randes.token_scores((h / h.pow(2).mean(1, keepdim=True).sqrt()) @ w[blocks].t(), prompt[1:]).logprob
+    sizes = (sum(r * c * 4 for r, c in zip(plan.rows, plan.cols)), sum(p.nbytes for p in w8))
+    plan.close()
+    return {"eight": eight, "full": full, "bytes": sizes}
+
+
+def tune(width=256, rows=256, steps=3, rate=20.0, seed=0):
+    """A few steps on a normed layer of a new task, its activations kept in eight bits; returns the mean squared error before and after, and
+    whether adding the task changed the superposition."""
+    plan, base, models, M = build(width, 2, 4 * width, 2, seed)
+    gen = torch.Generator(device="cuda").manual_seed(seed + 4)
+    x, residual, target = (torch.randn(rows, width, generator=gen, device="cuda") for _ in range(3))
+    gain, weight = torch.ones(width, device="cuda", requires_grad=True), base[0].clone().requires_grad_(True)
+    seen = []
+    for _ in range(steps + 1):
+        y, h = norm_linear(x, gain, weight, residual)
+        loss = (y - target).pow(2).mean()
+        seen.append(float(loss.detach()))
+        d_gain, d_weight = torch.autograd.grad(loss, (gain, weight))
+        with torch.no_grad():
+            gain -= rate * d_gain
+            weight -= rate * d_weight
+    before = M.clone()
+    plan.add_model(2, 98, base, [weight.detach(), base[1], base[2]], M)
+    changed = not torch.equal(M, before)
+    plan.close()
+    return seen[0], seen[-1], changed
+
+
 def learn(width=256, vocab=4096, rows=64, steps=5, rate=50.0, seed=0):
     """A new task's head learns to name given tokens; returns the mean log probability before and after, by its own weights."""
     plan, base, models, M = build(width, 2, vocab, 2, seed)
@@ -101,7 +154,7 @@ def learn(width=256, vocab=4096, rows=64, steps=5, rate=50.0, seed=0):
 
 def main(argv=None) -> int:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    for name, value in (("width", 1024), ("blocks", 6), ("vocab", 32128), ("tasks", 4), ("tokens", 8), ("steps", 16), ("group", 64)):
+    for name, value in (("width", 1024), ("blocks", 6), ("vocab", 32128), ("tasks", 4), ("tokens", 8), ("steps", 16), ("group", 64), ("prompt", 512)):
         ap.add_argument("--" + name, type=int, default=value)
     a = ap.parse_args(argv)
     r = serve(a.width, a.blocks, a.vocab, a.tasks, a.tokens, a.steps, a.group)
@@ -110,9 +163,16 @@ def main(argv=None) -> int:
           % (a.tokens, a.tasks, a.steps, r["bytes"][1] / 2**20, r["bytes"][0] / 2**20))
     print("mean log probability of the tokens: packed %.3f, retrieved fp32 weights %.3f; largest difference %.3f"
           % (float(r["packed"].mean()), float(r["full"].mean()), float(off.max())))
+    if a.prompt > 1:
+        r = read_prompts(a.width, a.blocks, a.vocab, a.tasks, a.prompt)
+        print("%d prompts of %d tokens, each through its task's weights in eight bits, %.1f MiB (%.1f MiB in fp32): mean log probability %.3f, in fp32 %.3f; "
+              "largest difference %.3f" % (a.tasks, a.prompt, r["bytes"][1] / 2**20, r["bytes"][0] / 2**20, float(r["eight"].mean()), float(r["full"].mean()),
+                                           float((r["eight"] - r["full"]).abs().max())))
     first, last, added = learn()
     print("a new task's head: mean log probability of its tokens %.3f before, %.3f after five steps; added to the superposition: %s"
           % (first, last, "yes" if added else "no"))
+    first, last, added = tune()
+    print("a new task's layer, activations kept in eight bits: mean squared error %.3f before, %.3f after three steps; added: %s" % (first, last, "yes" if added else "no"))
     return 0
 
 
