@@ -2194,7 +2194,7 @@ int randes_rms_norm_backward_impl(const randes_rms_norm_backward_t* p, void* wor
             return fail(RANDES_WORKSPACE_TOO_SMALL, "the gradient of the gain needs a workspace of %zu bytes, got %zu", need, workspace ? workspace_bytes : 0);
         if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(RANDES_MISALIGNED, "workspace = %p is not 16-byte aligned", workspace);
     }
-    const NormGradArgs n{a.dy, a.h, a.kept8, a.rstd, a.gain, a.dh, a.dx, a.dgain, static_cast<float*>(workspace), a.dy_stride, a.h_stride, a.dh_stride,
+    const NormGradArgs n{a.dy, a.h, a.kept8, a.rstd, a.gain, a.dh, a.dx, a.dgain, need ? static_cast<float*>(workspace) : nullptr, a.dy_stride, a.h_stride, a.dh_stride,
                          a.dx_stride, a.rows, a.cols, vec ? 1u : 0u, a.gain && a.gain_dtype == RANDES_BF16 ? 1u : 0u};
     int launched = 0;
     const int e = launch_norm_grad(a.dtype, n, &launched, stream);

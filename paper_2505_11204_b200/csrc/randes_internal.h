@@ -401,7 +401,7 @@ struct NormGradArgs {
     const void* dh;               // or NULL
     void* dx;
     float* dgain;                 // or NULL
-    float* partial;               // [ctas][cols], in the caller's workspace
+    float* partial;               // [ctas][cols], in the caller's workspace; NULL where a call needs none
     uint64_t dy_stride, h_stride, dh_stride, dx_stride;
     uint32_t rows, cols, vec, gain_bf16;
 };

@@ -68,7 +68,7 @@ def test_forward(n, cols, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("kept", [False, True])
-@pytest.mark.parametrize("n,cols", SHAPES + [(2000, 64), (1500, 1024), (700, 2050)])
+@pytest.mark.parametrize("n,cols", SHAPES + [(2000, 64), (1500, 1024), (700, 2050), (256, 1024), (200, 768), (40, 5000), (32, 8192)])
 def test_backward(n, cols, kept, dtype):
     x, r, gain = rows_of(n, cols, dtype, 1), rows_of(n, cols, dtype, 2, 3.0), 1 + 0.3 * rows_of(1, cols, torch.float32, 3)[0]
     g, gh = rows_of(n, cols, dtype, 4), rows_of(n, cols, dtype, 5)
@@ -198,7 +198,10 @@ def test_refusals():
     s = torch.cuda.current_stream().cuda_stream
     back = dict(dy=x.data_ptr(), h=x.data_ptr(), rstd=f.rstd.data_ptr(), gain=gain.data_ptr(), dx=f.y.data_ptr(), dgain=gain.data_ptr(), dy_stride=256, h_stride=256,
                 dx_stride=256, rows=4, cols=256)
-    ws = torch.empty(randes.randes_rms_norm_backward_workspace(4, 256) + 16, dtype=torch.uint8, device="cuda")
+    need = randes.randes_rms_norm_backward_workspace(2000, 256)      # (few rows need none)
+    big, bigs = torch.zeros(4, 2000, 256, device="cuda"), torch.ones(2000, device="cuda")
+    many = dict(rows=2000, dy=big[0].data_ptr(), h=big[1].data_ptr(), dx=big[2].data_ptr(), rstd=bigs.data_ptr())
+    ws = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
     call = lambda at=ws.data_ptr(), n=ws.numel(), **kw: randes.randes_rms_norm_backward(randes.RmsNormBackward(**{**back, **kw}), at, n, s)
     cases = [(lambda: randes.rms_norm(x, gain[:100]), inv), (lambda: randes.rms_norm(x, gain.double()), inv), (lambda: randes.rms_norm(x, gain, x[:, :100]), inv),
              (lambda: randes.rms_norm(x, gain, x.bfloat16()), inv), (lambda: randes.rms_norm(x, gain, eps=0.0), inv), (lambda: randes.rms_norm(x, gain, eps=float("nan")), inv),
@@ -207,8 +210,8 @@ def test_refusals():
              (lambda: randes.rms_norm(x[1:], gain, h=x[:3]), inv), (lambda: randes.rms_norm(x.half(), gain), randes.UNSUPPORTED_DTYPE),
              (lambda: randes.rms_norm_backward(x, randes.pack8(x[:, :100]), f.rstd, gain), inv), (lambda: randes.rms_norm_backward(x, x, f.rstd[:2], gain), inv),
              (lambda: randes.rms_norm_backward(x, x.bfloat16(), f.rstd, gain), inv), (lambda: call(h=None), inv), (lambda: call(kept8=f.kept.address), inv),
-             (lambda: call(rstd=None), inv), (lambda: call(dx=None), inv), (lambda: call(at=None, n=0), randes.WORKSPACE_TOO_SMALL),
-             (lambda: call(n=randes.randes_rms_norm_backward_workspace(4, 256) - 1), randes.WORKSPACE_TOO_SMALL), (lambda: call(at=ws.data_ptr() + 8), randes.MISALIGNED),
+             (lambda: call(rstd=None), inv), (lambda: call(dx=None), inv), (lambda: call(at=None, n=0, **many), randes.WORKSPACE_TOO_SMALL),
+             (lambda: call(n=need - 1, **many), randes.WORKSPACE_TOO_SMALL), (lambda: call(at=ws.data_ptr() + 8, **many), randes.MISALIGNED),
              (lambda: call(dgain=gain.data_ptr() + 2), randes.MISALIGNED), (lambda: call(dtype=5), randes.UNSUPPORTED_DTYPE)]
     for i, (g, code) in enumerate(cases):
         with pytest.raises(randes.RandesError) as e:

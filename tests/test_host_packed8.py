@@ -27,7 +27,8 @@ def test_sizes():
     assert randes.randes_packed_eight_linear_workspace(700, randes.EIGHT_BITS, 10000) == 0
     assert randes.randes_packed_eight_linear_workspace(700, randes.BF16, 16) == 0
     assert randes.randes_packed_eight_linear_workspace(700, randes.F32, 17) == size(17, 700)
-    for rows, cols in ((1, 1), (1000, 768), (10 ** 6, 4096), (3, 32768)):
+    assert randes.randes_rms_norm_backward_workspace(1, 1) == randes.randes_rms_norm_backward_workspace(256, 1024) == 0
+    for rows, cols in ((257, 1024), (1000, 768), (10 ** 6, 4096), (3, 32768)):
         assert randes.randes_rms_norm_backward_workspace(rows, cols) >= 4 * cols
 
 
@@ -96,10 +97,11 @@ def test_norm_refusals():
     norm(rows=0, x=None, y=None)
     refused(inv, lambda: randes._check(randes.lib().randes_rms_norm(None, None)))
     ok2 = dict(dy=1 << 12, h=1 << 14, rstd=1 << 16, dx=1 << 18, dy_stride=256, h_stride=256, dx_stride=256, rows=4, cols=256)
+    many = dict(rows=2000, dy=1 << 30, h=1 << 31, dx=1 << 32)
     back = lambda at=None, n=0, **kw: randes.randes_rms_norm_backward(randes.RmsNormBackward(**{**ok2, **kw}), at, n, None)
     for kw, code in ((dict(h=None), inv), (dict(kept8=1 << 20), inv), (dict(h=None, kept8=(1 << 20) + 4), mis), (dict(rstd=None), inv), (dict(rstd=5), mis), (dict(dx=None), inv),
-                     (dict(dy=None), inv), (dict(dx=(1 << 12) + 64), inv), (dict(h=None, kept8=1 << 18), inv), (dict(dgain=1 << 24), randes.WORKSPACE_TOO_SMALL),
-                     (dict(dgain=1 << 24, at=(1 << 25) + 8, n=1 << 24), mis), (dict(dgain=3), mis), (dict(dtype=9), randes.UNSUPPORTED_DTYPE)):
+                     (dict(dy=None), inv), (dict(dx=(1 << 12) + 64), inv), (dict(h=None, kept8=1 << 18), inv), (dict(many, dgain=1 << 34), randes.WORKSPACE_TOO_SMALL),
+                     (dict(many, dgain=1 << 34, at=(1 << 35) + 8, n=1 << 24), mis), (dict(dgain=3), mis), (dict(dtype=9), randes.UNSUPPORTED_DTYPE)):
         refused(code, lambda: back(**kw))
     back(rows=0, dx=None, h=None)
 
