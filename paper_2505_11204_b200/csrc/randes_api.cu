@@ -2084,7 +2084,8 @@ int randes_packed_eight_linear_impl(const void* w, uint32_t rows, uint32_t cols,
         if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit pack kernel");
         ++g_launches;
     }
-    Linear8Args a{w, need ? workspace : x, y, x_stride, y_stride, rows, cols, n_tokens, vec ? 1u : 0u, y_dtype == RANDES_BF16 ? 1u : 0u, 0};
+    Linear8Args a{w, need ? workspace : x, y, x_stride, y_stride, rows, cols, n_tokens, vec ? 1u : 0u, y_dtype == RANDES_BF16 ? 1u : 0u,
+                  rows_aligned(y, n_tokens, y_stride, ye, 4 * ye) ? 1u : 0u, 0};
     const int e = launch_linear8(a, packed || need ? -1 : x_dtype, dev.sms, stream);
     if (e) return fail_cuda(static_cast<cudaError_t>(e), "launch of the eight-bit product");
     ++g_launches;

@@ -370,6 +370,7 @@ struct Linear8Args {
     uint64_t x_stride, y_stride;
     uint32_t rows, cols, n_tokens;
     uint32_t x_vec, y_bf16;
+    uint32_t y_vec;               // four neighbouring outputs from a multiple of four on start on a boundary of their size
     uint32_t log_ranks;           // set by the launcher: CTAs of a cluster that share a tile's columns
 };
 bool linear8_packs(uint32_t n_tokens);      // whether so few tokens go into eight bits inside the product

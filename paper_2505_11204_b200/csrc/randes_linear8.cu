@@ -167,6 +167,29 @@ template <uint32_t S> struct Ring {
 
 __device__ __forceinline__ void store_y(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_y(bf16* p, float v) { *p = __float2bfloat16_rn(v); }
+// four neighbouring outputs of a token, of which n exist
+__device__ __forceinline__ void store_four(float* p, const float4& y, bool whole, uint32_t n)
+{
+    if (whole) {
+        *reinterpret_cast<float4*>(p) = y;
+        return;
+    }
+    if (n > 0) p[0] = y.x;
+    if (n > 1) p[1] = y.y;
+    if (n > 2) p[2] = y.z;
+    if (n > 3) p[3] = y.w;
+}
+__device__ __forceinline__ void store_four(bf16* p, const float4& y, bool whole, uint32_t n)
+{
+    if (whole) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(Out<bf16>::pack(y.x, y.y), Out<bf16>::pack(y.z, y.w));
+        return;
+    }
+    if (n > 0) store_y(p, y.x);
+    if (n > 1) store_y(p + 1, y.y);
+    if (n > 2) store_y(p + 2, y.z);
+    if (n > 3) store_y(p + 3, y.w);
+}
 // One row's sums of N neighbouring tokens, of which n exist: a warp writes 32 neighbouring outputs of a token at a time.
 // (No branch between the stores: with one per output this took three times as long.)
 template <int N, typename T> __device__ __forceinline__ void store_tokens(const Linear8Args& a, uint32_t token, uint32_t n, uint32_t row, const uint32_t (&v)[N])
@@ -201,6 +224,50 @@ template <int N> struct Geom8 {
     static constexpr size_t kSmem = 1024 + static_cast<size_t>(kStages) * kStage + 8 * kBars + 16;
     static_assert(kStage % 1024 == 0 && 8 * kBars + 16 <= 512, "stages on the swizzle's boundary");
 };
+
+// Each CTA of a cluster adds its share of the tokens over all CTAs, in their order: a warp takes a token's 128 rows, four to a lane, several
+// tokens at a time so that loads from the other CTAs are under way together (one after the other they took half the time of
+// a product of one token with 4096 x 4096, and nine tenths of one of 128).
+template <int N, int RANKS>
+__device__ __forceinline__ void add_shares(const Linear8Args& a, cg::cluster_group& cluster, unsigned char* gen, volatile uint32_t* aborted, uint32_t n0, uint32_t row0,
+                                           uint32_t rank)
+{
+    constexpr uint32_t kWarps = kThreads8 / 32, kBatch = N / RANKS / kWarps >= 4 ? 16 / RANKS : (N / RANKS / kWarps >= 2 ? 2 : 1);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = row0 + 4 * lane, end = min(static_cast<uint32_t>(N), a.n_tokens - n0);
+    const float4* part[RANKS];
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < RANKS; ++k) {
+        part[k] = cluster.map_shared_rank(reinterpret_cast<const float4*>(gen), k) + lane;
+        bad = bad || *cluster.map_shared_rank(const_cast<const uint32_t*>(aborted), k);
+    }
+    for (uint32_t j0 = rank + RANKS * warp; j0 < end; j0 += RANKS * kWarps * kBatch) {
+        float4 v[kBatch][RANKS];
+#pragma unroll
+        for (uint32_t i = 0; i < kBatch; ++i) {
+            const uint32_t j = j0 + i * RANKS * kWarps;
+#pragma unroll
+            for (int k = 0; k < RANKS; ++k)
+                if (j < end) v[i][k] = part[k][j * 32];
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kBatch; ++i) {
+            const uint32_t j = j0 + i * RANKS * kWarps;
+            if (j >= end) break;
+            float4 y = v[i][0];
+#pragma unroll
+            for (int k = 1; k < RANKS; ++k) {
+                y.x += v[i][k].x;
+                y.y += v[i][k].y;
+                y.z += v[i][k].z;
+                y.w += v[i][k].w;
+            }
+            if (bad) y.x = y.y = y.z = y.w = __uint_as_float(0x7FFFFFFFu);
+            if (a.y_bf16) store_four(static_cast<bf16*>(a.y) + static_cast<size_t>(n0 + j) * a.y_stride + row, y, a.y_vec && row + 4 <= a.rows, a.rows - min(row, a.rows));
+            else store_four(static_cast<float*>(a.y) + static_cast<size_t>(n0 + j) * a.y_stride + row, y, a.y_vec && row + 4 <= a.rows, a.rows - min(row, a.rows));
+        }
+    }
+}
 
 // Few tokens that are not in eight bits yet: a thread holds 16 columns of one token, eight threads a block, four blocks ahead.
 template <typename X> struct Sixteen {
@@ -422,21 +489,11 @@ template <int N, typename X> __global__ void __launch_bounds__(kThreads8, 1) lin
         }
     }
     if (ranks > 1) {
-        // each CTA adds its share of the tokens over all CTAs, in their order
         cluster.sync();
         const uint32_t rt = tile0 / token_tiles, n0 = (tile0 - rt * token_tiles) * N;
-        const uint32_t row = rt * 128 + (threadIdx.x & 127);
-        if (threadIdx.x < 128 && row < a.rows) {
-            const float* part = reinterpret_cast<const float*>(gen);
-            bool bad = false;
-            for (uint32_t k = 0; k < ranks; ++k) bad = bad || *cluster.map_shared_rank(const_cast<uint32_t*>(aborted), k);
-            for (uint32_t j = rank; j < N && n0 + j < a.n_tokens; j += ranks) {
-                float y = 0.f;
-                for (uint32_t k = 0; k < ranks; ++k) y += cluster.map_shared_rank(part, k)[j * 128 + threadIdx.x];
-                const uint32_t one[1] = {bad ? 0x7FFFFFFFu : __float_as_uint(y)};
-                store_tokens<1>(a, n0 + j, row, one);
-            }
-        }
+        if (ranks == 2) add_shares<N, 2>(a, cluster, gen, aborted, n0, rt * 128, rank);
+        else if (ranks == 4) add_shares<N, 4>(a, cluster, gen, aborted, n0, rt * 128, rank);
+        else add_shares<N, 8>(a, cluster, gen, aborted, n0, rt * 128, rank);
         cluster.sync();      // nobody leaves while its sums may still be read
     }
     tc_before();
