@@ -13,6 +13,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "randes_packed.cuh"
 #include "randes_packed8.cuh"
@@ -683,6 +684,45 @@ linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     }
 }
 
+// Clusters of 2^log CTAs that run at once (an SM holds one CTA, and a cluster lies inside one part of the device: of eight, fewer than an
+// eighth of the SMs). Asked once per device.
+template <int N, typename X> uint32_t clusters_at_once(int log)
+{
+    constexpr int kDevices = 64;
+    static std::atomic<uint32_t> known[kDevices][4];
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return 0;
+    uint32_t n = device < kDevices ? known[device][log].load(std::memory_order_relaxed) : 0;
+    if (n) return n - 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1u << log);
+    cfg.blockDim = dim3(kThreads8);
+    cfg.dynamicSmemBytes = Geom8<N>::kSmem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 1u << log;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int most = 0;
+    if (cudaOccupancyMaxActiveClusters(&most, linear8_kernel<N, X>, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        most = 0;
+    }
+    if (device < kDevices) known[device][log].store(static_cast<uint32_t>(most) + 1, std::memory_order_relaxed);
+    return static_cast<uint32_t>(most);
+}
+// CTAs (as a power of two) that share a tile's columns: as many as fit the device at once. Adding up their sums takes 0.7 us with 16
+// tokens, 1.5 with 128, a block of columns 0.25 us, so short rows are not shared. (1 token, 1024 x 4096: 11.2 us with one CTA
+// to a tile, 7.2, 5.2 and 4.8 with 2, 4 and 8; 128 tokens, 1024 x 1024: 6.0, 6.6, 6.5 and 7.0.)
+template <int N, typename X> uint32_t ranks_of(uint64_t tiles, uint32_t col_blocks)
+{
+    if (col_blocks < (N == 16 ? 4u : 10u)) return 0;
+    uint32_t log = 0;
+    while (log < 3 && (2u << log) <= col_blocks && tiles <= clusters_at_once<N, X>(log + 1)) ++log;
+    return log;
+}
+
 template <int N, typename X> int run_linear8(Linear8Args& a, int sm_count, cudaStream_t stream)
 {
     typedef Geom8<N> G;
@@ -690,9 +730,7 @@ template <int N, typename X> int run_linear8(Linear8Args& a, int sm_count, cudaS
     if (e != cudaSuccess) return static_cast<int>(e);
     const Packed8Layout lw(a.rows, a.cols);
     const uint64_t tiles = static_cast<uint64_t>(lw.row_tiles) * ((a.n_tokens + N - 1) / N);
-    if (tiles > 0x7FFFFFFFu) return static_cast<int>(cudaErrorInvalidValue);
-    a.log_ranks = 0;      // CTAs share a tile's columns as long as all fit the SMs at once
-    while (a.log_ranks < 3 && (tiles << (a.log_ranks + 1)) <= static_cast<uint64_t>(sm_count) && (2u << a.log_ranks) <= lw.col_blocks) ++a.log_ranks;
+    a.log_ranks = ranks_of<N, X>(tiles, lw.col_blocks);
     const uint32_t ctas = static_cast<uint32_t>(a.log_ranks ? tiles << a.log_ranks : std::min<uint64_t>(tiles, sm_count));
     return static_cast<int>(launch_early(linear8_kernel<N, X>, ctas, kThreads8, G::kSmem, stream, 1u << a.log_ranks, a));
 }
@@ -750,8 +788,19 @@ int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, void* stream)
     if (a.n_tokens <= 16) return run_linear8<16, uint8_t>(a, sm_count, s);
     if (a.n_tokens <= 32) return run_linear8<32, uint8_t>(a, sm_count, s);
     if (a.n_tokens <= 64) return run_linear8<64, uint8_t>(a, sm_count, s);
-    if (a.n_tokens > 128) return run_pairs(a, sm_count, s);
-    return run_linear8<128, uint8_t>(a, sm_count, s);
+    if (a.n_tokens <= 128) return run_linear8<128, uint8_t>(a, sm_count, s);
+    // Pairs, or tiles of 128 tokens whose columns CTAs may share? By the time either takes, in hundredths of a microsecond as measured:
+    // rounds over the SMs times blocks of columns, and what does not depend on them. (256 tokens, 1024 x 4096: 13.6 us in
+    // pairs, 8.7 in shared tiles; 256 tokens, 16384 x 4096: 18.5 and 26.7.)
+    const Packed8Layout lw(a.rows, a.cols), lx(a.n_tokens, a.cols);
+    const uint64_t tiles = static_cast<uint64_t>(lw.row_tiles) * lx.row_tiles, pairs = static_cast<uint64_t>((lw.row_tiles + 1) / 2) * ((lx.row_tiles + 1) / 2);
+    const uint64_t sms = sm_count, kb = lw.col_blocks;
+    if (tiles <= 2 * sms && opt_in<linear8_kernel<128, uint8_t>>(Geom8<128>::kSmem) == cudaSuccess) {
+        const uint32_t log = ranks_of<128, uint8_t>(tiles, lw.col_blocks);
+        const uint64_t single = 400 + (((tiles << log) + sms - 1) / sms * kb * 32 >> log) + (log ? 150 + 30 * log : 0);
+        if (single < 500 + (pairs + sms / 2 - 1) / (sms / 2) * kb * 28) return run_linear8<128, uint8_t>(a, sm_count, s);
+    }
+    return run_pairs(a, sm_count, s);
 }
 
 int linear8_giveups(unsigned int* count)
