@@ -195,6 +195,7 @@ __device__ __forceinline__ void store_four(bf16* p, const float4& y, bool whole,
 // (No branch between the stores: with one per output this took three times as long.)
 template <int N, typename T> __device__ __forceinline__ void store_tokens(const Linear8Args& a, uint32_t token, uint32_t n, uint32_t row, const uint32_t (&v)[N])
 {
+    static_assert(N % 4 == 0, "by fours");
     if (row >= a.rows) return;
     T* p = static_cast<T*>(a.y) + static_cast<size_t>(token) * a.y_stride + row;
     if (n >= N) {
@@ -202,8 +203,17 @@ template <int N, typename T> __device__ __forceinline__ void store_tokens(const 
         for (int j = 0; j < N; ++j) store_y(p + j * a.y_stride, __uint_as_float(v[j]));
     } else {
 #pragma unroll
-        for (int j = 0; j < N - 1; ++j)
-            if (j < n) store_y(p + j * a.y_stride, __uint_as_float(v[j]));
+        for (int j = 0; j < N; j += 4) {
+            if (j + 4 <= n) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) store_y(p + (j + e) * a.y_stride, __uint_as_float(v[j + e]));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (j + e < n) store_y(p + (j + e) * a.y_stride, __uint_as_float(v[j + e]));
+                break;
+            }
+        }
     }
 }
 template <int N> __device__ __forceinline__ void store_tokens(const Linear8Args& a, uint32_t token, uint32_t row, const uint32_t (&v)[N])
@@ -211,6 +221,48 @@ template <int N> __device__ __forceinline__ void store_tokens(const Linear8Args&
     if (token >= a.n_tokens) return;
     if (a.y_bf16) store_tokens<N, bf16>(a, token, a.n_tokens - token, row, v);
     else store_tokens<N, float>(a, token, a.n_tokens - token, row, v);
+}
+
+// The other way round: a token's sums of 32 neighbouring rows of w, each lane a token of its own. `out` starts on a 32-byte boundary.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+__device__ __forceinline__ void store_rows(const Linear8Args& a, uint32_t token, uint32_t row, const uint32_t (&v)[32])
+{
+    if (token >= a.n_tokens || row >= a.rows) return;
+    const size_t at = static_cast<size_t>(token) * a.y_stride + row;
+    const bool whole = row + 32 <= a.rows;
+    if (a.y_bf16) {
+        bf16* p = static_cast<bf16*>(a.y) + at;
+        if (whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = Out<bf16>::pack(__uint_as_float(v[16 * h + 2 * e]), __uint_as_float(v[16 * h + 2 * e + 1]));
+                store32(p + 16 * h, w);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 31; ++e)
+                if (row + e < a.rows) store_y(p + e, __uint_as_float(v[e]));
+        }
+    } else {
+        float* p = static_cast<float*>(a.y) + at;
+        if (whole) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const uint32_t w[8] = {v[8 * h], v[8 * h + 1], v[8 * h + 2], v[8 * h + 3], v[8 * h + 4], v[8 * h + 5], v[8 * h + 6], v[8 * h + 7]};
+                store32(p + 8 * h, w);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 31; ++e)
+                if (row + e < a.rows) store_y(p + e, __uint_as_float(v[e]));
+        }
+    }
 }
 
 // N tokens to a tile.
@@ -520,9 +572,11 @@ struct Pair8 {
     static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 
-__global__ void __launch_bounds__(Pair8::kThreads, 1)
-linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
-                    const __grid_constant__ CUtensorMap map_xs, const Linear8Args a)
+// TURNED: the tokens are operand A, a lane of tensor memory holds a token and its neighbouring rows of w: the form for outputs whose
+// tokens start on 32-byte boundaries, since a lane then writes whole sectors (two or four stores for 32 sums in place of 32).
+template <bool TURNED> __global__ void __launch_bounds__(Pair8::kThreads, 1)
+linear8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_as, const __grid_constant__ CUtensorMap map_b,
+                    const __grid_constant__ CUtensorMap map_bs, const Linear8Args a)
 {
     typedef Pair8 G;
     constexpr int S = G::kStages;
@@ -540,7 +594,7 @@ linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster.block_rank();
-    const Packed8Layout lw(a.rows, a.cols), lx(a.n_tokens, a.cols);
+    const Packed8Layout lw(TURNED ? a.n_tokens : a.rows, a.cols), lx(TURNED ? a.rows : a.n_tokens, a.cols);      // of operands A and B
     const uint32_t n_kb = lw.col_blocks, row_pairs = (lw.row_tiles + 1) / 2, token_pairs = (lx.row_tiles + 1) / 2, tiles = row_pairs * token_pairs;
     const uint32_t tile0 = blockIdx.x >> 1, tile_step = gridDim.x >> 1;
     // bands of 8 pairs of row tiles: the CTAs that run at a time share what they read
@@ -583,13 +637,13 @@ linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                 const bool first = (kb & 3u) == 0;
                 if (elected()) {
                     if (rank == 0) bar_expect(full(at.s), 2 * (G::kStage + (first ? G::kScaleSlot : 0)));
-                    pair_load(st, &map_w, bar, (w0 + kb) * 128);
-                    pair_load(st + kTile, &map_x, bar, (x0 + kb) * 128);
+                    pair_load(st, &map_a, bar, (w0 + kb) * 128);
+                    pair_load(st + kTile, &map_b, bar, (x0 + kb) * 128);
                     if (first) {
                         const uint32_t sc = scales + at.s * G::kScaleSlot, g = kb >> 2;
-                        pair_load(sc, &map_ws, bar, (rp * 2 + rank) * lw.groups + g);
-                        pair_load(sc + kScales, &map_xs, bar, tp * 2 * lx.groups + g);
-                        pair_load(sc + 2 * kScales, &map_xs, bar, (tp * 2 + 1) * lx.groups + g);
+                        pair_load(sc, &map_as, bar, (rp * 2 + rank) * lw.groups + g);
+                        pair_load(sc + kScales, &map_bs, bar, tp * 2 * lx.groups + g);
+                        pair_load(sc + 2 * kScales, &map_bs, bar, (tp * 2 + 1) * lx.groups + g);
                     }
                 }
                 __syncwarp();
@@ -672,7 +726,8 @@ linear8_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                     __syncwarp();
                     if (lane == 0) cluster_arrive(next0);
                 }
-                store_tokens<32>(a, n0 + j0, row, v);
+                if (TURNED) store_rows(a, row, n0 + j0, v);
+                else store_tokens<32>(a, n0 + j0, row, v);
             }
         }
         tc_before();
@@ -759,21 +814,23 @@ bool map_rows(EncodeTiled enc, CUtensorMap* map, const void* p, uint32_t words, 
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int run_pairs(const Linear8Args& a, int sm_count, cudaStream_t stream)
+template <bool TURNED> int run_pairs(const Linear8Args& a, int sm_count, cudaStream_t stream)
 {
-    const cudaError_t e = opt_in<linear8_pair_kernel>(Pair8::kSmem);
+    constexpr auto kernel = linear8_pair_kernel<TURNED>;
+    const cudaError_t e = opt_in<kernel>(Pair8::kSmem);
     if (e != cudaSuccess) return static_cast<int>(e);
     const EncodeTiled enc = encode_tiled();
     if (!enc) return static_cast<int>(cudaErrorNotSupported);
-    const Packed8Layout lw(a.rows, a.cols), lx(a.n_tokens, a.cols);
-    CUtensorMap mw, mws, mx, mxs;
-    if (!map_rows(enc, &mw, a.w, 32, lw.codes / 128, 128) || !map_rows(enc, &mx, a.x, 32, lx.codes / 128, 128) ||
-        !map_rows(enc, &mws, static_cast<const char*>(a.w) + lw.codes, 128, static_cast<uint64_t>(lw.row_tiles) * lw.groups, 1) ||
-        !map_rows(enc, &mxs, static_cast<const char*>(a.x) + lx.codes, 128, static_cast<uint64_t>(lx.row_tiles) * lx.groups, 1))
+    const Packed8Layout la(TURNED ? a.n_tokens : a.rows, a.cols), lb(TURNED ? a.rows : a.n_tokens, a.cols);
+    const char *pa = static_cast<const char*>(TURNED ? a.x : a.w), *pb = static_cast<const char*>(TURNED ? a.w : a.x);
+    CUtensorMap ma, mas, mb, mbs;
+    if (!map_rows(enc, &ma, pa, 32, la.codes / 128, 128) || !map_rows(enc, &mb, pb, 32, lb.codes / 128, 128) ||
+        !map_rows(enc, &mas, pa + la.codes, 128, static_cast<uint64_t>(la.row_tiles) * la.groups, 1) ||
+        !map_rows(enc, &mbs, pb + lb.codes, 128, static_cast<uint64_t>(lb.row_tiles) * lb.groups, 1))
         return static_cast<int>(cudaErrorInvalidValue);
-    const uint64_t tiles = static_cast<uint64_t>((lw.row_tiles + 1) / 2) * ((lx.row_tiles + 1) / 2);
+    const uint64_t tiles = static_cast<uint64_t>((la.row_tiles + 1) / 2) * ((lb.row_tiles + 1) / 2);
     const unsigned grid = static_cast<unsigned>(std::min<uint64_t>(tiles, sm_count / 2) * 2);
-    return static_cast<int>(launch_early(linear8_pair_kernel, grid, Pair8::kThreads, Pair8::kSmem, stream, 2, mw, mws, mx, mxs, a));
+    return static_cast<int>(launch_early(kernel, grid, Pair8::kThreads, Pair8::kSmem, stream, 2, ma, mas, mb, mbs, a));
 }
 
 }  // namespace
@@ -800,7 +857,10 @@ int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, void* stream)
         const uint64_t single = 400 + (((tiles << log) + sms - 1) / sms * kb * 32 >> log) + (log ? 150 + 30 * log : 0);
         if (single < 500 + (pairs + sms / 2 - 1) / (sms / 2) * kb * 28) return run_linear8<128, uint8_t>(a, sm_count, s);
     }
-    return run_pairs(a, sm_count, s);
+    // (4096^3: 64.0 us with w as operand A, 60.6 turned, where results go out while the next tile is worked on; one round of 1024 x 4096 x
+    // 4096: 16.7 and 17.4)
+    const bool turned = pairs > sms / 2 && (reinterpret_cast<uintptr_t>(a.y) | a.y_stride * (a.y_bf16 ? 2 : 4)) % 32 == 0;
+    return turned ? run_pairs<true>(a, sm_count, s) : run_pairs<false>(a, sm_count, s);
 }
 
 int linear8_giveups(unsigned int* count)
