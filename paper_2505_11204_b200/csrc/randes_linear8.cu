@@ -224,11 +224,6 @@ template <int N> __device__ __forceinline__ void store_tokens(const Linear8Args&
 }
 
 // The other way round: a token's sums of 32 neighbouring rows of w, each lane a token of its own. `out` starts on a 32-byte boundary.
-__device__ __forceinline__ void store32(void* p, const uint32_t (&v)[8])
-{
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                 ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-}
 __device__ __forceinline__ void store_rows(const Linear8Args& a, uint32_t token, uint32_t row, const uint32_t (&v)[32])
 {
     if (token >= a.n_tokens || row >= a.rows) return;
@@ -242,7 +237,7 @@ __device__ __forceinline__ void store_rows(const Linear8Args& a, uint32_t token,
                 uint32_t w[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) w[e] = Out<bf16>::pack(__uint_as_float(v[16 * h + 2 * e]), __uint_as_float(v[16 * h + 2 * e + 1]));
-                store32(p + 16 * h, w);
+                store32(p + 16 * h, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
             }
         } else {
 #pragma unroll
@@ -254,8 +249,7 @@ __device__ __forceinline__ void store_rows(const Linear8Args& a, uint32_t token,
         if (whole) {
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                const uint32_t w[8] = {v[8 * h], v[8 * h + 1], v[8 * h + 2], v[8 * h + 3], v[8 * h + 4], v[8 * h + 5], v[8 * h + 6], v[8 * h + 7]};
-                store32(p + 8 * h, w);
+                store32(p + 8 * h, make_uint4(v[8 * h], v[8 * h + 1], v[8 * h + 2], v[8 * h + 3]), make_uint4(v[8 * h + 4], v[8 * h + 5], v[8 * h + 6], v[8 * h + 7]));
             }
         } else {
 #pragma unroll

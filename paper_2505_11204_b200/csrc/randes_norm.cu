@@ -6,9 +6,9 @@
 // gradient of x and of r alike, dh what reaches h past the norm. Sums run in fp32; a sum of squares that leaves fp32 is taken
 // again in fp64.
 //
-// Forward: a row stays in registers between the loads and the sum's return, eight columns to a thread and run -- neighbours
-// where rows start on 16-byte boundaries (OCTETS), so that 16 lanes hold a block of 128 columns; else 32 apart, so that a warp's
-// accesses are whole whatever the row's alignment.
+// Forward: a row stays in registers between the loads and the sum's return. Where rows start on 16-byte boundaries (OCTETS) a
+// thread holds 16 neighbouring columns of a run, so that eight lanes hold a block of 128; else columns 32 apart, so that a
+// warp's accesses are whole whatever the row's alignment.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -32,10 +32,18 @@ __device__ __forceinline__ float gain_at(const void* gain, bool bf, uint32_t c)
 {
     return bf ? Store<bf16>::load1(static_cast<const bf16*>(gain) + c) : __ldg(static_cast<const float*>(gain) + c);
 }
-// the gain of a lane's columns of a run that starts at `first`; ones without a gain
-template <bool OCTETS> __device__ __forceinline__ void load_gain(const void* gain, bool bf, uint32_t first, uint32_t cols, int lane, float (&v)[8])
+// The columns of a thread's octet k: OCTETS: eight neighbours from base(k) on, octets 2 j and 2 j + 1 side by side; otherwise base(k), 32
+// further and so on. (A warp's octets k start together behind the row's end or not at all, but for the second of a pair.)
+template <int THREADS, bool OCTETS> struct Place {
+    int t;
+    __device__ __forceinline__ uint32_t run(int k) const { return OCTETS ? (k / 2 * THREADS + (t & ~31)) * 16 : (k * THREADS + (t & ~31)) * 8; }      // the warp's first
+    __device__ __forceinline__ uint32_t base(int k) const { return run(k) + (OCTETS ? 16 * (t & 31) + 8 * (k & 1) : (t & 31)); }
+    __device__ __forceinline__ uint32_t column(int k, uint32_t e) const { return base(k) + (OCTETS ? e : 32 * e); }
+};
+// the gain of an octet's columns; ones without a gain
+template <int THREADS, bool OCTETS> __device__ __forceinline__ void load_gain(const void* gain, bool bf, const Place<THREADS, OCTETS>& at, int k, uint32_t cols, float (&v)[8])
 {
-    const uint32_t c = first + 8 * lane;
+    const uint32_t c = at.base(k);
     if (OCTETS && gain && c + 8 <= cols) {
         if (bf) {
             Octet<bf16> o;
@@ -50,10 +58,7 @@ template <bool OCTETS> __device__ __forceinline__ void load_gain(const void* gai
         return;
     }
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) {
-        const uint32_t at = OCTETS ? c + e : first + 32 * e + lane;
-        v[e] = gain && at < cols ? gain_at(gain, bf, at) : 1.f;
-    }
+    for (uint32_t e = 0; e < 8; ++e) v[e] = gain && at.column(k, e) < cols ? gain_at(gain, bf, at.column(k, e)) : 1.f;
 }
 
 template <typename V> __device__ __forceinline__ V warp_sum(V v)
@@ -84,17 +89,20 @@ __device__ __forceinline__ float root(float v)
     return __fmaf_rn(y * 0.5f, __fmaf_rn(-v * y, y, 1.f), y);
 }
 
-// A row's runs first(k) = 8 (k THREADS + warp's first thread), all loads before the first use.
+// A row's octets, all loads before the first use.
 template <typename T, int THREADS, int CHUNKS, bool OCTETS> struct Row {
     Octet<T> o[OCTETS ? CHUNKS : 1];
     float f[OCTETS ? 1 : CHUNKS][8];
-    __device__ __forceinline__ void load(const T* row, uint32_t cols, int t)
+    __device__ __forceinline__ void load(const T* row, uint32_t cols, const Place<THREADS, OCTETS>& at, int from = 0)      // octets `from` on
     {
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            const uint32_t first = (k * THREADS + (t & ~31)) * 8;
-            if (OCTETS) o[OCTETS ? k : 0] = load_octet(row, first + 8 * (t & 31), cols);
-            else load_strided(row, first, cols, t & 31, f[OCTETS ? 0 : k]);
+        for (int k = 0; k < CHUNKS; k += 2) {
+            if (OCTETS) {
+                load_two(row, at.base(from + k), cols, o[OCTETS ? k : 0], o[OCTETS ? k + 1 : 0]);
+            } else {
+                load_strided(row, at.run(from + k), cols, at.t & 31, f[OCTETS ? 0 : k]);
+                load_strided(row, at.run(from + k + 1), cols, at.t & 31, f[OCTETS ? 0 : k + 1]);
+            }
         }
     }
     __device__ __forceinline__ void get(int k, float (&v)[8]) const
@@ -105,16 +113,22 @@ template <typename T, int THREADS, int CHUNKS, bool OCTETS> struct Row {
             for (int e = 0; e < 8; ++e) v[e] = f[OCTETS ? 0 : k][e];
     }
 };
-template <bool OCTETS, typename T> __device__ __forceinline__ void store_run(T* row, uint32_t first, uint32_t cols, const float (&v)[8], int lane)
+template <int THREADS, bool OCTETS, typename T>
+__device__ __forceinline__ void store_octets(T* row, const Place<THREADS, OCTETS>& at, int k, uint32_t cols, const float (&lo)[8], const float (&hi)[8])
 {
-    if (OCTETS) store_octet(row, first + 8 * lane, cols, v);
-    else store_strided(row, first, cols, lane, v);
+    if (OCTETS) {
+        store_two(row, at.base(k), cols, lo, hi);
+    } else {
+        store_strided(row, at.run(k), cols, at.t & 31, lo);
+        store_strided(row, at.run(k + 1), cols, at.t & 31, hi);
+    }
 }
 
 template <typename T, int THREADS, int CHUNKS, bool OCTETS>
 __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(const NormArgs a)
 {
     constexpr int kWarps = THREADS * kRowsPerCta<THREADS> / 32;
+    static_assert(CHUNKS % 2 == 0, "pairs of octets");
     __shared__ float s_part[THREADS == 32 ? 1 : kWarps];
     __shared__ double s_part64[THREADS == 32 ? 1 : kWarps];
     const int t = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x, lane = t & 31;
@@ -122,13 +136,14 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
     if (THREADS == 32 && r >= a.rows) return;
     const uint32_t cols = a.cols;
     const Packed8Layout lay(a.rows, cols);
+    const Place<THREADS, OCTETS> at{t};
     after_last();
 
     float v[CHUNKS][8];
     {
         Row<T, THREADS, CHUNKS, OCTETS> x, d;
-        x.load(static_cast<const T*>(a.x) + r * a.x_stride, cols, t);
-        if (a.residual) d.load(static_cast<const T*>(a.residual) + r * a.residual_stride, cols, t);
+        x.load(static_cast<const T*>(a.x) + r * a.x_stride, cols, at);
+        if (a.residual) d.load(static_cast<const T*>(a.residual) + r * a.residual_stride, cols, at);
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
             x.get(k, v[k]);
@@ -141,16 +156,25 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
             }
         }
     }
+    // a pair of octets into eight bits
+    auto pack = [&](const PackRow<OCTETS>& to, int k, const float (&lo)[8], const float (&hi)[8]) {
+        if (OCTETS) {
+            to.run(at.run(k), lo, hi, lane);
+        } else {
+            to.run(at.run(k), lo, lane);
+            if (at.run(k + 1) < cols) to.run(at.run(k + 1), hi, lane);
+        }
+    };
     float ss = 0.f;
-    const PackRow<OCTETS> kept(a.kept8, lay, r, lane), out(a.y8, lay, r, lane);
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-        const uint32_t first = (k * THREADS + (t & ~31)) * 8;
-        if (first >= cols) break;                           // the same for a warp
-        if (a.h) store_run<OCTETS>(static_cast<T*>(a.h) + r * a.h_stride, first, cols, v[k], lane);
-        if (a.kept8) store_scales(a.kept8, lay, r, first, kept.run(first, v[k], lane), lane);
+    for (int k = 0; k < CHUNKS; k += 2) {
+        if (at.run(k) >= cols) break;                       // the same for a warp
+        if (a.h) store_octets(static_cast<T*>(a.h) + r * a.h_stride, at, k, cols, v[k], v[k + 1]);
+        if (a.kept8) pack(PackRow<OCTETS>(a.kept8, lay, r, lane), k, v[k], v[k + 1]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = __fmaf_rn(v[k][e], v[k][e], ss);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = __fmaf_rn(v[k + i][e], v[k + i][e], ss);
     }
     ss = row_sum<THREADS>(ss, s_part, t);
     float s;
@@ -167,20 +191,22 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
     if (a.rstd && t == 0) a.rstd[r] = s;
     if (!a.y && !a.y8) return;
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-        const uint32_t first = (k * THREADS + (t & ~31)) * 8;
-        if (first >= cols) break;
-        float w[8];
-        load_gain<OCTETS>(a.gain, a.gain_bf16, first, cols, lane, w);
+    for (int k = 0; k < CHUNKS; k += 2) {
+        if (at.run(k) >= cols) break;
+        float w[2][8];
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e) w[e] = v[k][e] * s * w[e];
-        if (first + 256 > cols) {
+        for (int i = 0; i < 2; ++i) {
+            load_gain(a.gain, a.gain_bf16, at, k + i, cols, w[i]);
 #pragma unroll
-            for (uint32_t e = 0; e < 8; ++e)
-                if (first + (OCTETS ? 8 * lane + e : 32 * e + lane) >= cols) w[e] = 0.f;      // (0 * NaN behind the row's end would spoil the block)
+            for (uint32_t e = 0; e < 8; ++e) w[i][e] = v[k + i][e] * s * w[i][e];
+            if (at.run(k + i) + 512 > cols) {
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e)
+                    if (at.column(k + i, e) >= cols) w[i][e] = 0.f;      // (0 * NaN behind the row's end would spoil the block)
+            }
         }
-        if (a.y) store_run<OCTETS>(static_cast<T*>(a.y) + r * a.y_stride, first, cols, w, lane);
-        if (a.y8) store_scales(a.y8, lay, r, first, out.run(first, w, lane), lane);
+        if (a.y) store_octets(static_cast<T*>(a.y) + r * a.y_stride, at, k, cols, w[0], w[1]);
+        if (a.y8) pack(PackRow<OCTETS>(a.y8, lay, r, lane), k, w[0], w[1]);
     }
 }
 
@@ -193,7 +219,7 @@ __global__ void __launch_bounds__(THREADS) norm_grad_kernel(const NormGradArgs a
     const int t = threadIdx.x, lane = t & 31;
     const uint32_t cols = a.cols;
     const Packed8Layout lay(a.rows, cols);
-    auto column = [&](int k, uint32_t e) { return (k * THREADS + (t & ~31)) * 8 + (OCTETS ? 8 * lane + e : 32 * e + lane); };
+    const Place<THREADS, OCTETS> at{t};
     float sum[CHUNKS][8] = {};
     uint32_t turn = 0;
     after_last();
@@ -201,47 +227,44 @@ __global__ void __launch_bounds__(THREADS) norm_grad_kernel(const NormGradArgs a
         float n[CHUNKS][8], g[CHUNKS][8];
         const float s = __ldg(a.rstd + r);
         if (a.kept8) {
-            const char* src = static_cast<const char*>(a.kept8);
+            const unsigned char* codes = static_cast<const unsigned char*>(a.kept8) + lay.tile(r >> 7, 0) + (r & 127) * 128;
+            const unsigned char* scales = static_cast<const unsigned char*>(a.kept8) + lay.scales(r >> 7, 0) + Packed8Layout::scale_word(r);
+            auto unit = [&](uint32_t kb) { return block_unit(__ldg(scales + (kb >> 2) * 512 + (kb & 3))); };
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
-                const uint32_t first = (k * THREADS + (t & ~31)) * 8;
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) n[k][e] = 0.f;
                 if (OCTETS) {
-                    const uint32_t c = first + 8 * lane, kb = c >> 7;
-                    uint2 w = make_uint2(0, 0);
-                    uint32_t e = 0;
+                    const uint32_t c = at.base(k), kb = c >> 7;
                     if (kb < lay.col_blocks) {
-                        w = __ldcs(reinterpret_cast<const uint2*>(src + lay.tile(r >> 7, kb) + code_at(r, c)));
-                        e = __ldg(reinterpret_cast<const unsigned char*>(src + lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)));
+                        const uint2 w = __ldcs(reinterpret_cast<const uint2*>(codes + kb * 16384 + ((((c >> 4) ^ r) & 7) << 4) + (c & 8)));
+                        values4(w.x, unit(kb), n[k]);
+                        values4(w.y, unit(kb), n[k] + 4);
                     }
-                    values4(w.x, block_unit(e), n[k]);
-                    values4(w.y, block_unit(e), n[k] + 4);
                 } else {
 #pragma unroll
                     for (uint32_t b = 0; b < 2; ++b) {
-                        const uint32_t kb = (first >> 7) + b;
-                        uint32_t w = 0, e = 0;
-                        if (kb < lay.col_blocks) {
-                            const unsigned char* from = reinterpret_cast<const unsigned char*>(src) + lay.tile(r >> 7, kb) + (r & 127) * 128 + (lane & 15);
+                        const uint32_t kb = (at.run(k) >> 7) + b;
+                        if (kb >= lay.col_blocks) break;
+                        uint32_t w = 0;
 #pragma unroll
-                            for (uint32_t j = 0; j < 4; ++j) w |= static_cast<uint32_t>(__ldg(from + (((2 * j + (lane >> 4)) ^ (r & 7)) << 4))) << (8 * j);
-                            e = __ldg(reinterpret_cast<const unsigned char*>(src + lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)));
-                        }
-                        values4(w, block_unit(e), n[k] + 4 * b);
+                        for (uint32_t j = 0; j < 4; ++j) w |= static_cast<uint32_t>(__ldg(codes + kb * 16384 + (((2 * j + (lane >> 4)) ^ (r & 7)) << 4) + (lane & 15))) << (8 * j);
+                        values4(w, unit(kb), n[k] + 4 * b);
                     }
                 }
 #pragma unroll
                 for (uint32_t e = 0; e < 8; ++e)
-                    if (first + 256 > cols && column(k, e) >= cols) n[k][e] = 0.f;      // (codes behind the row's end may be NaN)
+                    if (at.run(k) + 512 > cols && at.column(k, e) >= cols) n[k][e] = 0.f;      // (codes behind the row's end may be NaN)
             }
         } else {
             Row<T, THREADS, CHUNKS, OCTETS> h;
-            h.load(static_cast<const T*>(a.h) + r * a.h_stride, cols, t);
+            h.load(static_cast<const T*>(a.h) + r * a.h_stride, cols, at);
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) h.get(k, n[k]);
         }
         {
             Row<T, THREADS, CHUNKS, OCTETS> dy;
-            dy.load(static_cast<const T*>(a.dy) + r * a.dy_stride, cols, t);
+            dy.load(static_cast<const T*>(a.dy) + r * a.dy_stride, cols, at);
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) dy.get(k, g[k]);
         }
@@ -249,7 +272,7 @@ __global__ void __launch_bounds__(THREADS) norm_grad_kernel(const NormGradArgs a
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
             float w[8];
-            load_gain<OCTETS>(a.gain, a.gain_bf16, (k * THREADS + (t & ~31)) * 8, cols, lane, w);
+            load_gain(a.gain, a.gain_bf16, at, k, cols, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 n[k][e] *= s;
@@ -260,21 +283,21 @@ __global__ void __launch_bounds__(THREADS) norm_grad_kernel(const NormGradArgs a
         }
         inner = row_sum<THREADS>(inner, s_part[turn], t) / cols;
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            const uint32_t first = (k * THREADS + (t & ~31)) * 8;
-            if (first >= cols) break;
-            float d[8];
-            if (a.dh) {
-                const T* row = static_cast<const T*>(a.dh) + r * a.dh_stride;
-                if (OCTETS) widen(load_octet(row, first + 8 * lane, cols), d);
-                else load_strided(row, first, cols, lane, d);
-            }
+        for (int k = 0; k < CHUNKS; k += 2) {
+            if (at.run(k) >= cols) break;
+            Row<T, THREADS, 2, OCTETS> dh;
+            if (a.dh) dh.load(static_cast<const T*>(a.dh) + r * a.dh_stride, cols, at, k);
+            float d[2][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = s * __fmaf_rn(-n[k][e], inner, g[k][e]);
-                d[e] = a.dh ? v + d[e] : v;
+            for (int i = 0; i < 2; ++i) {
+                if (a.dh) dh.get(i, d[i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = s * __fmaf_rn(-n[k + i][e], inner, g[k + i][e]);
+                    d[i][e] = a.dh ? v + d[i][e] : v;
+                }
             }
-            store_run<OCTETS>(static_cast<T*>(a.dx) + r * a.dx_stride, first, cols, d, lane);
+            store_octets(static_cast<T*>(a.dx) + r * a.dx_stride, at, k, cols, d[0], d[1]);
         }
     }
     if (!a.dgain) return;
@@ -283,7 +306,7 @@ __global__ void __launch_bounds__(THREADS) norm_grad_kernel(const NormGradArgs a
     for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (column(k, e) < cols) out[column(k, e)] = sum[k][e];
+            if (at.column(k, e) < cols) out[at.column(k, e)] = sum[k][e];
 }
 
 // The same for rows of up to 8192 columns. What bounds the form above is that a row's loads, its sum and its stores follow one
@@ -617,7 +640,6 @@ template <int V> using Const = std::integral_constant<int, V>;
 // Calls f with the row's form: threads to a row and runs of 8 columns per thread.
 template <typename F> int by_width(uint32_t cols, F&& f)
 {
-    if (cols <= 256) return f(Const<32>(), Const<1>());
     if (cols <= 512) return f(Const<32>(), Const<2>());
     if (cols <= 1024) return f(Const<32>(), Const<4>());
     if (cols <= 2048) return f(Const<128>(), Const<2>());

@@ -35,33 +35,14 @@ template <typename Args> __device__ __forceinline__ uint32_t matrix_of(const Arg
     return i;
 }
 
-// Four rows of a warp's run of 256 columns, every load before the first use. OCTETS: the rows start on 16-byte boundaries.
-template <typename T, bool OCTETS> struct Rows8 {
-    Octet<T> o[OCTETS ? kRows8 : 1];
-    float f[OCTETS ? 1 : kRows8][8];
-    __device__ __forceinline__ void load(const T* p, uint64_t stride, uint32_t n, uint32_t first, uint32_t cols, int lane)
-    {
-#pragma unroll
-        for (uint32_t i = 0; i < kRows8; ++i)
-            if (i < n) {
-                if (OCTETS) o[OCTETS ? i : 0] = load_octet(p + i * stride, first + 8 * lane, cols);
-                else load_strided(p + i * stride, first, cols, lane, f[OCTETS ? 0 : i]);
-            }
-    }
-    __device__ __forceinline__ void get(uint32_t i, float (&v)[8]) const
-    {
-        if (OCTETS) widen(o[OCTETS ? i : 0], v);
-        else
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = f[OCTETS ? 0 : i][e];
-    }
-};
-
-// A warp takes rows r0 .. r0 + 3 of 512 columns, two runs of 256; both are loaded at once where that takes 32 to 64 registers.
-template <typename T, typename M, bool RETRIEVE, bool OCTETS, uint32_t BATCH>
+// A warp takes four rows of 512 columns. WIDE, where rows start on 16-byte boundaries: a lane holds 16 neighbours of each, every load
+// (two rows' where that would take more than 64 registers) before the first use. Otherwise two runs of 256, a lane's columns 32 apart.
+// (With eight neighbours to a lane the scales and places of half as many elements were worked out at a time: 20.0 us for 8192 x 4096
+// bf16.)
+template <typename T, typename M, bool RETRIEVE, bool WIDE, uint32_t BATCH>
 __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_constant__ Pack8Batch<BATCH> a)
 {
-    constexpr bool kBoth = OCTETS && sizeof(T) + (RETRIEVE ? sizeof(M) : 0) <= 4;
+    constexpr uint32_t kAhead = sizeof(T) + (RETRIEVE ? sizeof(M) : 0) <= 4 ? 4 : 2;      // rows loaded at a time
     after_last();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Pack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
@@ -69,57 +50,74 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
     const uint32_t cta = blockIdx.x - m.first_cta, rb = cta / lay.groups, g = cta - rb * lay.groups, r0 = rb * kCtaRows8 + warp * kRows8;
     if (r0 >= m.rows) return;
     const uint32_t n = min(kRows8, m.rows - r0), cols = m.cols;
-    char* dst = static_cast<char*>(m.dst);
     const T* src = static_cast<const T*>(m.src) + r0 * m.stride;
     const M* add = RETRIEVE ? static_cast<const M*>(m.m) + static_cast<uint64_t>(r0) * cols : nullptr;
-    uint32_t word[kRows8] = {};
-    Rows8<T, OCTETS> w[kBoth ? 2 : 1];
-    Rows8<M, OCTETS> d[RETRIEVE && kBoth ? 2 : 1];
-    auto load = [&](uint32_t half) {
-        const uint32_t first = g * 512 + half * 256;
-        if (first >= cols) return;
-        w[kBoth ? half : 0].load(src, m.stride, n, first, cols, lane);
-        if (RETRIEVE) d[kBoth ? half : 0].load(add, cols, n, first, cols, lane);
-    };
-    load(0);
-    if (kBoth) load(1);
+    auto retrieve = [&](float (&v)[8], const float (&d)[8], uint32_t bits) {
 #pragma unroll
-    for (uint32_t half = 0; half < 2; ++half) {
-        const uint32_t first = g * 512 + half * 256;
-        if (first >= cols) break;
-        if (!kBoth && half) load(1);
-        uint32_t bits = 0;      // of the lane's eight columns
+        for (uint32_t k = 0; k < 8; ++k) v[k] = __fmaf_rn(a.lambda, flip(d[k], (bits >> k) << 31), v[k]);
+    };
+    auto signs = [&](uint32_t block) { return philox4x32_10(block, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1); };
+    if (WIDE) {
+        const uint32_t c = g * 512 + 16 * lane;
+        uint32_t bits = 0;      // of the lane's 16 columns
         if (RETRIEVE && m.flip) {
-            if (OCTETS) {
-                const uint32_t c = first + 8 * lane, q = (c >> 5) & 3;
-                const uint4 blk = philox4x32_10(c >> 7, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1);
-                bits = (q == 0 ? blk.x : (q == 1 ? blk.y : (q == 2 ? blk.z : blk.w))) >> (c & 31);
-            } else {
+            const uint4 blk = signs(c >> 7);
+            const uint32_t q = (c >> 5) & 3;
+            bits = (q == 0 ? blk.x : (q == 1 ? blk.y : (q == 2 ? blk.z : blk.w))) >> (c & 31);
+        }
+#pragma unroll
+        for (uint32_t i0 = 0; i0 < kRows8; i0 += kAhead) {
+            Octet<T> w[kAhead][2];
+            Octet<M> d[RETRIEVE ? kAhead : 1][2];
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i)
+                if (i0 + i < n) {
+                    load_two(src + (i0 + i) * m.stride, c, cols, w[i][0], w[i][1]);
+                    if (RETRIEVE) load_two(add + static_cast<uint64_t>(i0 + i) * cols, c, cols, d[RETRIEVE ? i : 0][0], d[RETRIEVE ? i : 0][1]);
+                }
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) {
+                if (i0 + i >= n) break;
+                float v[2][8];
+#pragma unroll
+                for (uint32_t h = 0; h < 2; ++h) {
+                    widen(w[i][h], v[h]);
+                    if (RETRIEVE) {
+                        float e[8];
+                        widen(d[RETRIEVE ? i : 0][h], e);
+                        retrieve(v[h], e, bits >> (8 * h));
+                    }
+                }
+                PackRow<true>(m.dst, lay, r0 + i0 + i, lane).run(g * 512, v[0], v[1], lane);
+            }
+        }
+    } else {
+#pragma unroll
+        for (uint32_t half = 0; half < 2; ++half) {
+            const uint32_t first = g * 512 + half * 256;
+            if (first >= cols) break;
+            float v[kRows8][8], d[RETRIEVE ? kRows8 : 1][8];
+#pragma unroll
+            for (uint32_t i = 0; i < kRows8; ++i)
+                if (i < n) {
+                    load_strided(src + i * m.stride, first, cols, lane, v[i]);
+                    if (RETRIEVE) load_strided(add + static_cast<uint64_t>(i) * cols, first, cols, lane, d[RETRIEVE ? i : 0]);
+                }
+            uint32_t bits = 0;
+            if (RETRIEVE && m.flip)
 #pragma unroll
                 for (uint32_t b = 0; b < 2; ++b) {
-                    const uint4 blk = philox4x32_10((first >> 7) + b, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1);
+                    const uint4 blk = signs((first >> 7) + b);
                     bits |= ((blk.x >> lane & 1u) | (blk.y >> lane & 1u) << 1 | (blk.z >> lane & 1u) << 2 | (blk.w >> lane & 1u) << 3) << (4 * b);
                 }
-            }
-        }
 #pragma unroll
-        for (uint32_t i = 0; i < kRows8; ++i) {
-            if (i >= n) break;
-            float v[8];
-            w[kBoth ? half : 0].get(i, v);
-            if (RETRIEVE) {
-                float e[8];
-                d[RETRIEVE && kBoth ? half : 0].get(i, e);
-#pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) v[k] = __fmaf_rn(a.lambda, flip(e[k], (bits >> k) << 31), v[k]);
+            for (uint32_t i = 0; i < kRows8; ++i) {
+                if (i >= n) break;
+                if (RETRIEVE) retrieve(v[i], d[RETRIEVE ? i : 0], bits);
+                PackRow<false>(m.dst, lay, r0 + i, lane).run(first, v[i], lane);
             }
-            word[i] |= PackRow<OCTETS>(dst, lay, r0 + i, lane).run(first, v, lane) << (16 * half);
         }
     }
-#pragma unroll
-    for (uint32_t i = 0; i < kRows8; ++i)
-        if (i < n && lane == static_cast<int>(i))
-            *reinterpret_cast<uint32_t*>(dst + lay.scales(r0 >> 7, g) + Packed8Layout::scale_word(r0 + i)) = word[i];
 }
 
 // A lane takes CPL neighbouring columns at a time, 16 bytes of the output, so that a warp writes whole lines; where rows do not start
@@ -469,11 +467,11 @@ template <typename T, typename M, bool RETRIEVE> int run_pack8(Pack8Args& a, voi
 {
     const uint32_t ctas = count_ctas(a);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    bool octets = true;
-    for (uint32_t i = 0; i < a.n; ++i) octets = octets && a.mat[i].vec == (RETRIEVE ? 3u : 1u);
+    bool wide = true;
+    for (uint32_t i = 0; i < a.n; ++i) wide = wide && a.mat[i].vec == (RETRIEVE ? 3u : 1u);
     auto run = [&](const auto& args, auto batch) {
         constexpr uint32_t B = decltype(batch)::value;
-        return launch_early(octets ? pack8_kernel<T, M, RETRIEVE, true, B> : pack8_kernel<T, M, RETRIEVE, false, B>, ctas, kWarps8 * 32, 0, s, 1, args);
+        return launch_early(wide ? pack8_kernel<T, M, RETRIEVE, true, B> : pack8_kernel<T, M, RETRIEVE, false, B>, ctas, kWarps8 * 32, 0, s, 1, args);
     };
     return static_cast<int>(a.n == 1 ? run(Pack8Batch<1>{{a.mat[0]}, 1, a.lambda, a.task}, std::integral_constant<uint32_t, 1>())
                                      : run(a, std::integral_constant<uint32_t, kPackBatch>()));

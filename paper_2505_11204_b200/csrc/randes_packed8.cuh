@@ -177,6 +177,51 @@ template <typename T> __device__ __forceinline__ void store_octet(T* row, uint32
             if (c + e < cols) Out<T>::store1(row + c + e, v[e]);
     }
 }
+// 16 neighbouring columns, c a multiple of 16: whole 32-byte sectors at a time where the row starts on such a boundary (two 16-byte
+// accesses with 32 bytes between lanes take a fifth longer, stores above all).
+__device__ __forceinline__ void load32(const void* p, uint4& a, uint4& b)
+{
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
+template <typename T> __device__ __forceinline__ bool whole_sectors(const T* row, uint32_t c, uint32_t cols)
+{
+    return c + 16 <= cols && (reinterpret_cast<uintptr_t>(row) & 31) == 0;
+}
+template <typename T> __device__ __forceinline__ void load_two(const T* row, uint32_t c, uint32_t cols, Octet<T>& a, Octet<T>& b)
+{
+    if (whole_sectors(row, c, cols)) {
+        if constexpr (sizeof(T) == 2) {
+            load32(row + c, a.w[0], b.w[0]);
+        } else {
+            load32(row + c, a.w[0], a.w[1]);
+            load32(row + c + 8, b.w[0], b.w[1]);
+        }
+    } else {
+        a = load_octet(row, c, cols);
+        b = load_octet(row, c + 8, cols);
+    }
+}
+template <typename T> __device__ __forceinline__ void store_two(T* row, uint32_t c, uint32_t cols, const float (&lo)[8], const float (&hi)[8])
+{
+    if (whole_sectors(row, c, cols)) {
+        const Octet<T> a = narrow<T>(lo), b = narrow<T>(hi);
+        if constexpr (sizeof(T) == 2) {
+            store32(row + c, a.w[0], b.w[0]);
+        } else {
+            store32(row + c, a.w[0], a.w[1]);
+            store32(row + c + 8, b.w[0], b.w[1]);
+        }
+    } else {
+        store_octet(row, c, cols, lo);
+        store_octet(row, c + 8, cols, hi);
+    }
+}
 // Rows that start anywhere: a warp's run of 256 columns, lane l holding columns l, l + 32 .. l + 224, so that memory is read and
 // written by neighbours together, one element to a lane and instruction.
 template <typename T> __device__ __forceinline__ void load_strided(const T* row, uint32_t first, uint32_t cols, int lane, float (&v)[8])
@@ -205,33 +250,41 @@ template <typename T> __device__ __forceinline__ void store_strided(T* row, uint
     }
 }
 
-// A warp's runs of 256 columns of one row on their way into eight bits. OCTETS: lane l holds columns 8 l .. 8 l + 7 of a run; otherwise
-// l, l + 32 ... (A run starts on a multiple of 256, so a lane's place inside a tile is the same for all of them.)
-template <bool OCTETS> struct PackRow {
-    char* codes;              // of this lane in the row's first two blocks
+// A warp's runs of columns of one row on their way into eight bits, the place of this lane in the row's first blocks and their scales.
+// WIDE: runs of 512, lane l holding 16 neighbours from 16 l on, a 16-byte piece of a tile; otherwise runs of 256, columns l, l + 32 ...
+// (A run starts on a multiple of its length, so a lane's place is the same in all of them.)
+template <bool WIDE> struct PackRow {
+    char *codes, *scales;
     uint32_t flip, blocks;
     __device__ __forceinline__ PackRow(void* dst, const Packed8Layout& lay, uint32_t r, int lane)
     {
         codes = static_cast<char*>(dst) + lay.tile(r >> 7, 0) + (r & 127) * 128;
-        if (OCTETS) codes += (lane >> 4) * 16384 + ((((lane >> 1) & 7) ^ (r & 7)) << 4) + (lane & 1) * 8;
-        else codes += lane & 15;
+        scales = static_cast<char*>(dst) + lay.scales(r >> 7, 0) + Packed8Layout::scale_word(r);
         flip = (r ^ (lane >> 4)) & 7;
         blocks = lay.col_blocks;
+        if (WIDE) {
+            codes += (lane >> 3) * 16384 + (((lane ^ r) & 7) << 4);
+            scales += lane >> 3;
+        } else {
+            codes += lane & 15;
+        }
     }
-    // returns the scales of the run's two blocks (the second in bits 8-15)
-    __device__ __forceinline__ uint32_t run(uint32_t first, const float (&v)[8], int lane) const
+    __device__ __forceinline__ void run(uint32_t first, const float (&lo)[8], const float (&hi)[8], int lane) const
+    {
+        const uint32_t kb = (first >> 7) + (lane >> 3);
+        float top = top2(top8(lo), top8(hi));
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) top = top2(top, __shfl_xor_sync(~0u, top, o));
+        if (kb >= blocks) return;
+        const uint32_t e = block_scale(top);
+        const uint2 a = codes8(lo, top, e), b = codes8(hi, top, e);
+        *reinterpret_cast<uint4*>(codes + static_cast<size_t>(first >> 7) * 16384) = make_uint4(a.x, a.y, b.x, b.y);
+        if ((lane & 7) == 0) scales[static_cast<size_t>(first >> 9) * 512] = static_cast<char>(e);
+    }
+    __device__ __forceinline__ void run(uint32_t first, const float (&v)[8], int lane) const
     {
         const uint32_t kb = first >> 7;
         char* to = codes + static_cast<size_t>(kb) * 16384;
-        if (OCTETS) {
-            float top = top8(v);
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) top = top2(top, __shfl_xor_sync(~0u, top, o));
-            const uint32_t e = block_scale(top);
-            if (kb + (lane >> 4) < blocks) *reinterpret_cast<uint2*>(to) = codes8(v, top, e);
-            return __shfl_sync(~0u, e, 0) | (__shfl_sync(~0u, e, 16) << 8);
-        }
-        uint32_t scales = 0;
 #pragma unroll
         for (uint32_t b = 0; b < 2; ++b) {
             if (kb + b >= blocks) break;
@@ -242,18 +295,10 @@ template <bool OCTETS> struct PackRow {
             const uint32_t w = not_finite(top) ? kNanCodes : codes4(pair_of(u[0], u[1]), pair_of(u[2], u[3]), inv);
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) to[b * 16384 + (((2 * e) ^ flip) << 4)] = static_cast<char>(w >> (8 * e));
-            scales |= s << (8 * b);
+            if (lane == 0) scales[static_cast<size_t>(kb >> 2) * 512 + (kb & 3) + b] = static_cast<char>(s);
         }
-        return scales;
     }
 };
-// and its scales, where no word of four blocks is at hand
-__device__ __forceinline__ void store_scales(void* dst, const Packed8Layout& lay, uint32_t r, uint32_t first, uint32_t scales, int lane)
-{
-    const uint32_t kb = (first >> 7) + lane;
-    if (lane < 2 && kb < lay.col_blocks)
-        static_cast<char*>(dst)[lay.scales(r >> 7, kb >> 2) + Packed8Layout::scale_word(r) + (kb & 3)] = static_cast<char>(scales >> (8 * lane));
-}
 
 }  // namespace device
 }  // namespace randes
