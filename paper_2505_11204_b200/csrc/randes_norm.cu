@@ -25,8 +25,9 @@ namespace {
 
 using namespace device;
 
-// Threads to a row, columns of a row per thread (8 CHUNKS), rows to a CTA: warps take rows of their own up to 1024 columns.
-template <int THREADS> constexpr int kRowsPerCta = THREADS == 32 ? 4 : 1;
+// Threads to a row, columns of a row per thread (8 CHUNKS), rows to a CTA: up to 1024 columns warps, or halves of them, take rows of
+// their own.
+template <int THREADS> constexpr int kRowsPerCta = THREADS <= 32 ? 128 / THREADS : 1;
 
 __device__ __forceinline__ float gain_at(const void* gain, bool bf, uint32_t c)
 {
@@ -36,8 +37,10 @@ __device__ __forceinline__ float gain_at(const void* gain, bool bf, uint32_t c)
 // further and so on. (A warp's octets k start together behind the row's end or not at all, but for the second of a pair.)
 template <int THREADS, bool OCTETS> struct Place {
     int t;
-    __device__ __forceinline__ uint32_t run(int k) const { return OCTETS ? (k / 2 * THREADS + (t & ~31)) * 16 : (k * THREADS + (t & ~31)) * 8; }      // the warp's first
-    __device__ __forceinline__ uint32_t base(int k) const { return run(k) + (OCTETS ? 16 * (t & 31) + 8 * (k & 1) : (t & 31)); }
+    static constexpr int kLanes = THREADS < 32 ? THREADS : 32;
+    __device__ __forceinline__ int lane() const { return t & (kLanes - 1); }
+    __device__ __forceinline__ uint32_t run(int k) const { return OCTETS ? (k / 2 * THREADS + (t - lane())) * 16 : (k * THREADS + (t - lane())) * 8; }      // the warp's first
+    __device__ __forceinline__ uint32_t base(int k) const { return run(k) + (OCTETS ? 16 * lane() + 8 * (k & 1) : lane()); }
     __device__ __forceinline__ uint32_t column(int k, uint32_t e) const { return base(k) + (OCTETS ? e : 32 * e); }
 };
 // the gain of an octet's columns; ones without a gain
@@ -61,18 +64,18 @@ template <int THREADS, bool OCTETS> __device__ __forceinline__ void load_gain(co
     for (uint32_t e = 0; e < 8; ++e) v[e] = gain && at.column(k, e) < cols ? gain_at(gain, bf, at.column(k, e)) : 1.f;
 }
 
-template <typename V> __device__ __forceinline__ V warp_sum(V v)
+template <int LANES = 32, typename V> __device__ __forceinline__ V warp_sum(V v, uint32_t mask = ~0u)
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(mask, v, o);
     return v;
 }
 // The sum over the threads of a row, in every one of them, always in the same order. `part`: a word per warp, not touched again
 // before the row's threads have met once more.
-template <int THREADS, typename V> __device__ __forceinline__ V row_sum(V v, V* part, int tid)
+template <int THREADS, typename V> __device__ __forceinline__ V row_sum(V v, V* part, int tid, uint32_t mask = ~0u)
 {
-    v = warp_sum(v);
-    if (THREADS == 32) return v;
+    v = warp_sum<THREADS < 32 ? THREADS : 32>(v, mask);
+    if (THREADS <= 32) return v;
     if ((tid & 31) == 0) part[tid >> 5] = v;
     __syncthreads();
     V all = 0;
@@ -129,11 +132,13 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
 {
     constexpr int kWarps = THREADS * kRowsPerCta<THREADS> / 32;
     static_assert(CHUNKS % 2 == 0, "pairs of octets");
-    __shared__ float s_part[THREADS == 32 ? 1 : kWarps];
-    __shared__ double s_part64[THREADS == 32 ? 1 : kWarps];
-    const int t = THREADS == 32 ? threadIdx.x & 31 : threadIdx.x, lane = t & 31;
-    const uint32_t r = THREADS == 32 ? blockIdx.x * kRowsPerCta<THREADS> + (threadIdx.x >> 5) : blockIdx.x;
-    if (THREADS == 32 && r >= a.rows) return;
+    static_assert(OCTETS || THREADS >= 32, "runs of 256");
+    __shared__ float s_part[THREADS <= 32 ? 1 : kWarps];
+    __shared__ double s_part64[THREADS <= 32 ? 1 : kWarps];
+    const int t = threadIdx.x % THREADS, lane = t & 31;
+    const uint32_t r = blockIdx.x * kRowsPerCta<THREADS> + threadIdx.x / THREADS;
+    if (THREADS <= 32 && r >= a.rows) return;               // (the rest of the warp goes on by its own mask)
+    const uint32_t mask = THREADS == 16 ? 0xFFFFu << (threadIdx.x & 16) : ~0u;
     const uint32_t cols = a.cols;
     const Packed8Layout lay(a.rows, cols);
     const Place<THREADS, OCTETS> at{t};
@@ -159,7 +164,7 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
     // a pair of octets into eight bits
     auto pack = [&](const PackRow<OCTETS>& to, int k, const float (&lo)[8], const float (&hi)[8]) {
         if (OCTETS) {
-            to.run(at.run(k), lo, hi, lane);
+            to.run(at.run(k), lo, hi, lane, mask);
         } else {
             to.run(at.run(k), lo, lane);
             if (at.run(k + 1) < cols) to.run(at.run(k + 1), hi, lane);
@@ -176,7 +181,7 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss = __fmaf_rn(v[k + i][e], v[k + i][e], ss);
     }
-    ss = row_sum<THREADS>(ss, s_part, t);
+    ss = row_sum<THREADS>(ss, s_part, t, mask);
     float s;
     if (ss == INFINITY) {                                   // the same for all threads of the row
         double wide = 0;
@@ -184,7 +189,7 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
         for (int k = 0; k < CHUNKS; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) wide += static_cast<double>(v[k][e]) * v[k][e];
-        s = static_cast<float>(1.0 / sqrt(row_sum<THREADS>(wide, s_part64, t) / cols + a.eps));
+        s = static_cast<float>(1.0 / sqrt(row_sum<THREADS>(wide, s_part64, t, mask) / cols + a.eps));
     } else {
         s = root(__fmaf_rn(ss, a.per_col, a.eps));
     }
@@ -637,9 +642,14 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_gain_kernel(const float* p
 }
 
 template <int V> using Const = std::integral_constant<int, V>;
-// Calls f with the row's form: threads to a row and runs of 8 columns per thread.
-template <typename F> int by_width(uint32_t cols, F&& f)
+// Calls f with the row's form: threads to a row and runs of 8 columns per thread. (768 bf16 columns, 32768 rows: 45 us with 16 columns of
+// 512 lanes' worth to a warp, the second run half empty; 35 with half a warp to a row.)
+template <bool OCTETS, typename F> int by_width(uint32_t cols, F&& f)
 {
+    if constexpr (OCTETS) {
+        if (cols <= 256) return f(Const<16>(), Const<2>());
+        if (cols > 512 && cols <= 768) return f(Const<16>(), Const<6>());
+    }
     if (cols <= 512) return f(Const<32>(), Const<2>());
     if (cols <= 1024) return f(Const<32>(), Const<4>());
     if (cols <= 2048) return f(Const<128>(), Const<2>());
@@ -684,7 +694,7 @@ template <typename T, bool OCTETS> int run_ring(const NormGradArgs& a, uint32_t*
 
 template <bool OCTETS> int run_norm(int dtype, const NormArgs& a, cudaStream_t stream)
 {
-    return by_width(a.cols, [&](auto threads, auto chunks) {
+    return by_width<OCTETS>(a.cols, [&](auto threads, auto chunks) {
         constexpr int T = decltype(threads)::value, C = decltype(chunks)::value, R = kRowsPerCta<T>;
         const uint32_t ctas = a.rows / R + (a.rows % R != 0);
         return static_cast<int>(launch_early(dtype ? norm_kernel<bf16, T, C, OCTETS> : norm_kernel<float, T, C, OCTETS>, ctas, T * R, 0, stream, 1, a));

@@ -269,17 +269,18 @@ template <bool WIDE> struct PackRow {
             codes += lane & 15;
         }
     }
-    __device__ __forceinline__ void run(uint32_t first, const float (&lo)[8], const float (&hi)[8], int lane) const
+    // (half a warp may take a run of 256 likewise, with its own mask and its lanes counted from 0)
+    __device__ __forceinline__ void run(uint32_t first, const float (&lo)[8], const float (&hi)[8], int lane, uint32_t mask = ~0u) const
     {
         const uint32_t kb = (first >> 7) + (lane >> 3);
         float top = top2(top8(lo), top8(hi));
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) top = top2(top, __shfl_xor_sync(~0u, top, o));
+        for (int o = 1; o < 8; o <<= 1) top = top2(top, __shfl_xor_sync(mask, top, o));
         if (kb >= blocks) return;
         const uint32_t e = block_scale(top);
         const uint2 a = codes8(lo, top, e), b = codes8(hi, top, e);
         *reinterpret_cast<uint4*>(codes + static_cast<size_t>(first >> 7) * 16384) = make_uint4(a.x, a.y, b.x, b.y);
-        if ((lane & 7) == 0) scales[static_cast<size_t>(first >> 9) * 512] = static_cast<char>(e);
+        if ((lane & 7) == 0) scales[static_cast<size_t>(first >> 9) * 512 + (first >> 7 & 3)] = static_cast<char>(e);
     }
     __device__ __forceinline__ void run(uint32_t first, const float (&v)[8], int lane) const
     {
