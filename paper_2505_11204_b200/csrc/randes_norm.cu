@@ -6,9 +6,9 @@
 // gradient of x and of r alike, dh what reaches h past the norm. Sums run in fp32; a sum of squares that leaves fp32 is taken
 // again in fp64.
 //
-// Forward: a row stays in registers between the loads and the sum's return. Where rows start on 16-byte boundaries (OCTETS) a
-// thread holds 16 neighbouring columns of a run, so that eight lanes hold a block of 128; else columns 32 apart, so that a
-// warp's accesses are whole whatever the row's alignment.
+// Forward: a row stays in registers between the loads and the sum's return. A thread holds 16 neighbouring columns of a run (OCTETS), so
+// that eight lanes hold a block of 128, of rows that start on 16-byte boundaries or of bf16 rows that start anywhere (LOOSE);
+// of other rows columns 32 apart, so that a warp's accesses are whole whatever the row's alignment.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -47,7 +47,7 @@ template <int THREADS, bool OCTETS> struct Place {
 template <int THREADS, bool OCTETS> __device__ __forceinline__ void load_gain(const void* gain, bool bf, const Place<THREADS, OCTETS>& at, int k, uint32_t cols, float (&v)[8])
 {
     const uint32_t c = at.base(k);
-    if (OCTETS && gain && c + 8 <= cols) {
+    if (OCTETS && gain && c + 8 <= cols && (reinterpret_cast<uintptr_t>(gain) & 15) == 0) {
         if (bf) {
             Octet<bf16> o;
             o.w[0] = __ldg(reinterpret_cast<const uint4*>(static_cast<const bf16*>(gain) + c));
@@ -93,6 +93,21 @@ __device__ __forceinline__ float root(float v)
 }
 
 // A row's octets, all loads before the first use.
+template <int THREADS, int CHUNKS> struct LooseRow {
+    Loose w[CHUNKS / 2];
+    __device__ __forceinline__ void load(const bf16* row, uint32_t cols, const Place<THREADS, true>& at)
+    {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; k += 2) w[k / 2].load(row, at.base(k), cols);
+    }
+    __device__ __forceinline__ void get(const bf16* row, uint32_t cols, const Place<THREADS, true>& at, int k, float (&lo)[8], float (&hi)[8]) const
+    {
+        Octet<bf16> a, b;
+        w[k / 2].get(row, at.base(k), cols, a, b);
+        widen(a, lo);
+        widen(b, hi);
+    }
+};
 template <typename T, int THREADS, int CHUNKS, bool OCTETS> struct Row {
     Octet<T> o[OCTETS ? CHUNKS : 1];
     float f[OCTETS ? 1 : CHUNKS][8];
@@ -127,9 +142,10 @@ __device__ __forceinline__ void store_octets(T* row, const Place<THREADS, OCTETS
     }
 }
 
-template <typename T, int THREADS, int CHUNKS, bool OCTETS>
+template <typename T, int THREADS, int CHUNKS, bool OCTETS, bool LOOSE>
 __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(const NormArgs a)
 {
+    __shared__ __align__(16) uint4 s_scratch[LOOSE ? THREADS * kRowsPerCta<THREADS> / 32 : 1][64];
     constexpr int kWarps = THREADS * kRowsPerCta<THREADS> / 32;
     static_assert(CHUNKS % 2 == 0, "pairs of octets");
     static_assert(OCTETS || THREADS >= 32, "runs of 256");
@@ -146,21 +162,46 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
 
     float v[CHUNKS][8];
     {
-        Row<T, THREADS, CHUNKS, OCTETS> x, d;
-        x.load(static_cast<const T*>(a.x) + r * a.x_stride, cols, at);
-        if (a.residual) d.load(static_cast<const T*>(a.residual) + r * a.residual_stride, cols, at);
+        auto add = [&](int k, const float (&u)[8]) {
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            x.get(k, v[k]);
-            if (a.residual) {
-                float u[8];
-                d.get(k, u);
+            for (int e = 0; e < 8; ++e) v[k][e] += u[e];
+            if (sizeof(T) == 2) widen(narrow<T>(v[k]), v[k]);          // what is stored is what is normed
+        };
+        const T *from = static_cast<const T*>(a.x) + r * a.x_stride, *more = static_cast<const T*>(a.residual) + r * a.residual_stride;
+        if constexpr (LOOSE) {
+            LooseRow<THREADS, CHUNKS> x, d;
+            x.load(from, cols, at);
+            if (a.residual) d.load(more, cols, at);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[k][e] += u[e];
-                if (sizeof(T) == 2) widen(narrow<T>(v[k]), v[k]);      // what is stored is what is normed
+            for (int k = 0; k < CHUNKS; k += 2) {
+                x.get(from, cols, at, k, v[k], v[k + 1]);
+                if (a.residual) {
+                    float u[2][8];
+                    d.get(more, cols, at, k, u[0], u[1]);
+                    add(k, u[0]);
+                    add(k + 1, u[1]);
+                }
+            }
+        } else {
+            Row<T, THREADS, CHUNKS, OCTETS> x, d;
+            x.load(from, cols, at);
+            if (a.residual) d.load(more, cols, at);
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) {
+                x.get(k, v[k]);
+                if (a.residual) {
+                    float u[8];
+                    d.get(k, u);
+                    add(k, u);
+                }
             }
         }
     }
+    auto store = [&](void* p, uint64_t stride, int k, const float (&lo)[8], const float (&hi)[8]) {
+        T* row = static_cast<T*>(p) + r * stride;
+        if constexpr (LOOSE) store_loose(row, at.run(k), cols, lo, hi, s_scratch[threadIdx.x >> 5], lane);
+        else store_octets(row, at, k, cols, lo, hi);
+    };
     // a pair of octets into eight bits
     auto pack = [&](const PackRow<OCTETS>& to, int k, const float (&lo)[8], const float (&hi)[8]) {
         if (OCTETS) {
@@ -174,7 +215,7 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
 #pragma unroll
     for (int k = 0; k < CHUNKS; k += 2) {
         if (at.run(k) >= cols) break;                       // the same for a warp
-        if (a.h) store_octets(static_cast<T*>(a.h) + r * a.h_stride, at, k, cols, v[k], v[k + 1]);
+        if (a.h) store(a.h, a.h_stride, k, v[k], v[k + 1]);
         if (a.kept8) pack(PackRow<OCTETS>(a.kept8, lay, r, lane), k, v[k], v[k + 1]);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -210,7 +251,7 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
                     if (at.column(k + i, e) >= cols) w[i][e] = 0.f;      // (0 * NaN behind the row's end would spoil the block)
             }
         }
-        if (a.y) store_octets(static_cast<T*>(a.y) + r * a.y_stride, at, k, cols, w[0], w[1]);
+        if (a.y) store(a.y, a.y_stride, k, w[0], w[1]);
         if (a.y8) pack(PackRow<OCTETS>(a.y8, lay, r, lane), k, w[0], w[1]);
     }
 }
@@ -642,11 +683,11 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_gain_kernel(const float* p
 }
 
 template <int V> using Const = std::integral_constant<int, V>;
-// Calls f with the row's form: threads to a row and runs of 8 columns per thread. (768 bf16 columns, 32768 rows: 45 us with 16 columns of
-// 512 lanes' worth to a warp, the second run half empty; 35 with half a warp to a row.)
-template <bool OCTETS, typename F> int by_width(uint32_t cols, F&& f)
+// Calls f with the row's form: threads to a row and runs of 8 columns per thread. (768 bf16 columns, 32768 rows: 45 us with runs
+// of 512, the second half empty; 37 with half a warp to a row.)
+template <bool ALIGNED, typename F> int by_width(uint32_t cols, F&& f)
 {
-    if constexpr (OCTETS) {
+    if constexpr (ALIGNED) {
         if (cols <= 256) return f(Const<16>(), Const<2>());
         if (cols > 512 && cols <= 768) return f(Const<16>(), Const<6>());
     }
@@ -692,12 +733,13 @@ template <typename T, bool OCTETS> int run_ring(const NormGradArgs& a, uint32_t*
     return run_ring<T, 512, OCTETS>(a, ctas, stream);
 }
 
-template <bool OCTETS> int run_norm(int dtype, const NormArgs& a, cudaStream_t stream)
+template <typename E, bool ALIGNED> int run_norm(const NormArgs& a, cudaStream_t stream)
 {
-    return by_width<OCTETS>(a.cols, [&](auto threads, auto chunks) {
+    return by_width<ALIGNED>(a.cols, [&](auto threads, auto chunks) {
         constexpr int T = decltype(threads)::value, C = decltype(chunks)::value, R = kRowsPerCta<T>;
+        constexpr bool kLoose = !ALIGNED && sizeof(E) == 2;
         const uint32_t ctas = a.rows / R + (a.rows % R != 0);
-        return static_cast<int>(launch_early(dtype ? norm_kernel<bf16, T, C, OCTETS> : norm_kernel<float, T, C, OCTETS>, ctas, T * R, 0, stream, 1, a));
+        return static_cast<int>(launch_early(norm_kernel<E, T, C, ALIGNED || kLoose, kLoose>, ctas, T * R, 0, stream, 1, a));
     });
 }
 template <bool OCTETS> int run_grad(int dtype, const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
@@ -715,7 +757,9 @@ template <bool OCTETS> int run_grad(int dtype, const NormGradArgs& a, uint32_t* 
 
 int launch_norm(int dtype, const NormArgs& a, void* stream)
 {
-    return a.vec ? run_norm<true>(dtype, a, static_cast<cudaStream_t>(stream)) : run_norm<false>(dtype, a, static_cast<cudaStream_t>(stream));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (dtype) return a.vec ? run_norm<bf16, true>(a, s) : run_norm<bf16, false>(a, s);
+    return a.vec ? run_norm<float, true>(a, s) : run_norm<float, false>(a, s);
 }
 
 size_t norm_grad_workspace(uint32_t rows, uint32_t cols)

@@ -35,11 +35,13 @@ template <typename Args> __device__ __forceinline__ uint32_t matrix_of(const Arg
     return i;
 }
 
-// A warp takes four rows of 512 columns. WIDE, where rows start on 16-byte boundaries: a lane holds 16 neighbours of each, every load
-// (two rows' where that would take more than 64 registers) before the first use. Otherwise two runs of 256, a lane's columns 32 apart.
+// A warp takes four rows of 512 columns. A lane holds 16 neighbours of each, every load (two rows' where that would take more than 64
+// registers) before the first use: of rows that start on 16-byte boundaries, or (LOOSE) of bf16 rows that start anywhere. Other rows
+// (STRIDED): two runs of 256, a lane's columns 32 apart.
 // (With eight neighbours to a lane the scales and places of half as many elements were worked out at a time: 20.0 us for 8192 x 4096
 // bf16.)
-template <typename T, typename M, bool RETRIEVE, bool WIDE, uint32_t BATCH>
+enum { kAligned, kLoose, kStrided };
+template <typename T, typename M, bool RETRIEVE, int MODE, uint32_t BATCH>
 __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_constant__ Pack8Batch<BATCH> a)
 {
     constexpr uint32_t kAhead = sizeof(T) + (RETRIEVE ? sizeof(M) : 0) <= 4 ? 4 : 2;      // rows loaded at a time
@@ -57,7 +59,7 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
         for (uint32_t k = 0; k < 8; ++k) v[k] = __fmaf_rn(a.lambda, flip(d[k], (bits >> k) << 31), v[k]);
     };
     auto signs = [&](uint32_t block) { return philox4x32_10(block, m.slot, kTagSign, a.task.id, a.task.key0, a.task.key1); };
-    if (WIDE) {
+    if (MODE != kStrided) {
         const uint32_t c = g * 512 + 16 * lane;
         uint32_t bits = 0;      // of the lane's 16 columns
         if (RETRIEVE && m.flip) {
@@ -69,12 +71,28 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
         for (uint32_t i0 = 0; i0 < kRows8; i0 += kAhead) {
             Octet<T> w[kAhead][2];
             Octet<M> d[RETRIEVE ? kAhead : 1][2];
+            if constexpr (MODE == kAligned) {
 #pragma unroll
-            for (uint32_t i = 0; i < kAhead; ++i)
-                if (i0 + i < n) {
-                    load_two(src + (i0 + i) * m.stride, c, cols, w[i][0], w[i][1]);
-                    if (RETRIEVE) load_two(add + static_cast<uint64_t>(i0 + i) * cols, c, cols, d[RETRIEVE ? i : 0][0], d[RETRIEVE ? i : 0][1]);
-                }
+                for (uint32_t i = 0; i < kAhead; ++i)
+                    if (i0 + i < n) {
+                        load_two(src + (i0 + i) * m.stride, c, cols, w[i][0], w[i][1]);
+                        if (RETRIEVE) load_two(add + static_cast<uint64_t>(i0 + i) * cols, c, cols, d[RETRIEVE ? i : 0][0], d[RETRIEVE ? i : 0][1]);
+                    }
+            } else if constexpr (MODE == kLoose) {
+                Loose x[kAhead], y[RETRIEVE ? kAhead : 1];
+#pragma unroll
+                for (uint32_t i = 0; i < kAhead; ++i)
+                    if (i0 + i < n) {
+                        x[i].load(src + (i0 + i) * m.stride, c, cols);
+                        if (RETRIEVE) y[RETRIEVE ? i : 0].load(add + static_cast<uint64_t>(i0 + i) * cols, c, cols);
+                    }
+#pragma unroll
+                for (uint32_t i = 0; i < kAhead; ++i)
+                    if (i0 + i < n) {
+                        x[i].get(src + (i0 + i) * m.stride, c, cols, w[i][0], w[i][1]);
+                        if (RETRIEVE) y[RETRIEVE ? i : 0].get(add + static_cast<uint64_t>(i0 + i) * cols, c, cols, d[RETRIEVE ? i : 0][0], d[RETRIEVE ? i : 0][1]);
+                    }
+            }
 #pragma unroll
             for (uint32_t i = 0; i < kAhead; ++i) {
                 if (i0 + i >= n) break;
@@ -471,7 +489,8 @@ template <typename T, typename M, bool RETRIEVE> int run_pack8(Pack8Args& a, voi
     for (uint32_t i = 0; i < a.n; ++i) wide = wide && a.mat[i].vec == (RETRIEVE ? 3u : 1u);
     auto run = [&](const auto& args, auto batch) {
         constexpr uint32_t B = decltype(batch)::value;
-        return launch_early(wide ? pack8_kernel<T, M, RETRIEVE, true, B> : pack8_kernel<T, M, RETRIEVE, false, B>, ctas, kWarps8 * 32, 0, s, 1, args);
+        constexpr int kElse = sizeof(T) == 2 && (!RETRIEVE || sizeof(M) == 2) ? kLoose : kStrided;
+        return launch_early(wide ? pack8_kernel<T, M, RETRIEVE, kAligned, B> : pack8_kernel<T, M, RETRIEVE, kElse, B>, ctas, kWarps8 * 32, 0, s, 1, args);
     };
     return static_cast<int>(a.n == 1 ? run(Pack8Batch<1>{{a.mat[0]}, 1, a.lambda, a.task}, std::integral_constant<uint32_t, 1>())
                                      : run(a, std::integral_constant<uint32_t, kPackBatch>()));

@@ -222,6 +222,63 @@ template <typename T> __device__ __forceinline__ void store_two(T* row, uint32_t
         store_octet(row, c + 8, cols, hi);
     }
 }
+// The same where a bf16 row starts anywhere, a lane's 16 columns out of the two or three 16-byte words that hold them, moved into place by
+// what the row's start lies behind a boundary (the same for all lanes). A word that holds an element of the row is memory of
+// the caller's. (Element by element, 32 columns apart, the norm of 4096 x 4001 took 50 us and its packing 18; so 31 and 10.6.)
+template <int SHIFT> __device__ __forceinline__ void moved(const uint32_t (&w)[12], uint4& a, uint4& b)      // SHIFT elements on
+{
+    uint32_t o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = SHIFT & 1 ? __byte_perm(w[i + SHIFT / 2], w[i + SHIFT / 2 + 1], 0x5432) : w[i + SHIFT / 2];
+    a = make_uint4(o[0], o[1], o[2], o[3]);
+    b = make_uint4(o[4], o[5], o[6], o[7]);
+}
+struct Loose {      // loaded, not yet moved
+    uint4 w[3];
+    __device__ __forceinline__ void load(const bf16* row, uint32_t c, uint32_t cols)
+    {
+        const char* p = reinterpret_cast<const char*>(row + c);
+        const uint32_t off = reinterpret_cast<uintptr_t>(p) & 15;
+        w[0] = w[1] = w[2] = make_uint4(0, 0, 0, 0);
+        if (c < cols) w[0] = __ldg(reinterpret_cast<const uint4*>(p - off));
+        if (c + (16 - off) / 2 < cols) w[1] = __ldg(reinterpret_cast<const uint4*>(p - off) + 1);
+        if (off && c + (32 - off) / 2 < cols) w[2] = __ldg(reinterpret_cast<const uint4*>(p - off) + 2);
+    }
+    __device__ __forceinline__ void get(const bf16* row, uint32_t c, uint32_t cols, Octet<bf16>& a, Octet<bf16>& b) const
+    {
+        const uint32_t u[12] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w, w[2].x, w[2].y, w[2].z, w[2].w};
+        switch ((reinterpret_cast<uintptr_t>(row) & 15) / 2) {
+        case 0: moved<0>(u, a.w[0], b.w[0]); break;
+        case 1: moved<1>(u, a.w[0], b.w[0]); break;
+        case 2: moved<2>(u, a.w[0], b.w[0]); break;
+        case 3: moved<3>(u, a.w[0], b.w[0]); break;
+        case 4: moved<4>(u, a.w[0], b.w[0]); break;
+        case 5: moved<5>(u, a.w[0], b.w[0]); break;
+        case 6: moved<6>(u, a.w[0], b.w[0]); break;
+        default: moved<7>(u, a.w[0], b.w[0]); break;
+        }
+        if (c + 16 > cols) {      // what lies behind the row's end
+            uint32_t* words[8] = {&a.w[0].x, &a.w[0].y, &a.w[0].z, &a.w[0].w, &b.w[0].x, &b.w[0].y, &b.w[0].z, &b.w[0].w};
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) *words[i] &= (c + 2 * i < cols ? 0xFFFFu : 0u) | (c + 2 * i + 1 < cols ? 0xFFFF0000u : 0u);
+        }
+    }
+};
+// A warp's 512 columns from `first` on (lane l holding 16 from 16 l on) to a bf16 row that starts anywhere, through 1 KiB of shared memory
+// of the warp's own: neighbours write neighbours.
+__device__ __forceinline__ void store_loose(bf16* row, uint32_t first, uint32_t cols, const float (&lo)[8], const float (&hi)[8], uint4* scratch, int lane)
+{
+    scratch[2 * lane] = narrow<bf16>(lo).w[0];
+    scratch[2 * lane + 1] = narrow<bf16>(hi).w[0];
+    __syncwarp();
+    const unsigned short* from = reinterpret_cast<const unsigned short*>(scratch) + lane;
+    unsigned short* to = reinterpret_cast<unsigned short*>(row) + first + lane;
+    const int left = static_cast<int>(cols) - static_cast<int>(first) - lane;
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+        if (32 * k < left) to[32 * k] = from[32 * k];
+    __syncwarp();
+}
 // Rows that start anywhere: a warp's run of 256 columns, lane l holding columns l, l + 32 .. l + 224, so that memory is read and
 // written by neighbours together, one element to a lane and instruction.
 template <typename T> __device__ __forceinline__ void load_strided(const T* row, uint32_t first, uint32_t cols, int lane, float (&v)[8])

@@ -43,7 +43,7 @@ def check_eight(p, y, rel):
 
 
 SHAPES = [(1, 1), (1, 1024), (3, 7), (5, 127), (130, 128), (9, 129), (6, 256), (33, 300), (7, 513), (4, 1000), (4, 1024), (5, 1025), (3, 2048), (2, 2056), (3, 4001),
-          (2, 4096), (3, 6000), (2, 8192), (2, 9001), (1, 16384), (2, 16392), (1, 32768), (500, 64)]
+          (2, 4096), (3, 6000), (2, 8192), (2, 9001), (1, 16384), (2, 16392), (1, 32768), (500, 64), (7, 64), (5, 768), (3, 640), (9, 256), (3, 12345)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
