@@ -195,7 +195,6 @@ __device__ __forceinline__ void store_four(bf16* p, const float4& y, bool whole,
 // (No branch between the stores: with one per output this took three times as long.)
 template <int N, typename T> __device__ __forceinline__ void store_tokens(const Linear8Args& a, uint32_t token, uint32_t n, uint32_t row, const uint32_t (&v)[N])
 {
-    static_assert(N % 4 == 0, "by fours");
     if (row >= a.rows) return;
     T* p = static_cast<T*>(a.y) + static_cast<size_t>(token) * a.y_stride + row;
     if (n >= N) {
@@ -203,17 +202,8 @@ template <int N, typename T> __device__ __forceinline__ void store_tokens(const 
         for (int j = 0; j < N; ++j) store_y(p + j * a.y_stride, __uint_as_float(v[j]));
     } else {
 #pragma unroll
-        for (int j = 0; j < N; j += 4) {
-            if (j + 4 <= n) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) store_y(p + (j + e) * a.y_stride, __uint_as_float(v[j + e]));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 3; ++e)
-                    if (j + e < n) store_y(p + (j + e) * a.y_stride, __uint_as_float(v[j + e]));
-                break;
-            }
-        }
+        for (int j = 0; j < N - 1; ++j)
+            if (j < n) store_y(p + j * a.y_stride, __uint_as_float(v[j]));
     }
 }
 template <int N> __device__ __forceinline__ void store_tokens(const Linear8Args& a, uint32_t token, uint32_t row, const uint32_t (&v)[N])
