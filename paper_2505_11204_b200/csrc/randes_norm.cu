@@ -672,6 +672,7 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_gain_kernel(const float* p
     float v = 0.f;
     after_last();
     if (c < cols)
+#pragma unroll 10
         for (uint32_t i = y; i < n; i += kSumRows) v += partial[static_cast<size_t>(i) * cols + c];
     s[y][x] = v;
     __syncthreads();
