@@ -649,7 +649,7 @@ int randes_rms_norm(const randes_rms_norm_t* norm, void* stream);
  *   rstd              of the forward call
  *   dgain             device fp32 [cols] or NULL
  *   workspace         device memory, 16-byte aligned, at least randes_rms_norm_backward_workspace(rows, cols) bytes with dgain (none
- *                     for up to 2^18 elements)
+ *                     for up to 2^18 elements in rows of up to 8192 columns)
  * Sums in fp32 in a fixed order; one kernel launch, two where a workspace is needed.  Errors: as above, WORKSPACE_TOO_SMALL.
  */
 typedef struct {

@@ -405,6 +405,7 @@ struct NormGradArgs {
     float* partial;               // [ctas][cols], in the caller's workspace; NULL where a call needs none
     uint64_t dy_stride, h_stride, dh_stride, dx_stride;
     uint32_t rows, cols, vec, gain_bf16;
+    uint32_t parts, part;         // of a row, one to a CTA of a cluster, and their columns
 };
 constexpr uint32_t kNormMaxCols = 32768;
 int launch_norm(int dtype, const NormArgs& a, void* stream);

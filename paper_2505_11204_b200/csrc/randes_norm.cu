@@ -111,15 +111,15 @@ template <int THREADS, int CHUNKS> struct LooseRow {
 template <typename T, int THREADS, int CHUNKS, bool OCTETS> struct Row {
     Octet<T> o[OCTETS ? CHUNKS : 1];
     float f[OCTETS ? 1 : CHUNKS][8];
-    __device__ __forceinline__ void load(const T* row, uint32_t cols, const Place<THREADS, OCTETS>& at, int from = 0)      // octets `from` on
+    __device__ __forceinline__ void load(const T* row, uint32_t cols, const Place<THREADS, OCTETS>& at)
     {
 #pragma unroll
         for (int k = 0; k < CHUNKS; k += 2) {
             if (OCTETS) {
-                load_two(row, at.base(from + k), cols, o[OCTETS ? k : 0], o[OCTETS ? k + 1 : 0]);
+                load_two(row, at.base(k), cols, o[OCTETS ? k : 0], o[OCTETS ? k + 1 : 0]);
             } else {
-                load_strided(row, at.run(from + k), cols, at.t & 31, f[OCTETS ? 0 : k]);
-                load_strided(row, at.run(from + k + 1), cols, at.t & 31, f[OCTETS ? 0 : k + 1]);
+                load_strided(row, at.run(k), cols, at.t & 31, f[OCTETS ? 0 : k]);
+                load_strided(row, at.run(k + 1), cols, at.t & 31, f[OCTETS ? 0 : k + 1]);
             }
         }
     }
@@ -257,110 +257,18 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
 }
 
 // Backward: a CTA walks rows and keeps its share of dgain in registers; the shares of all CTAs are added in a fixed order by a second
-// kernel. This form takes rows of more than 8192 columns.
-template <typename T, int THREADS, int CHUNKS, bool OCTETS>
-__global__ void __launch_bounds__(THREADS) norm_grad_kernel(const NormGradArgs a)
-{
-    __shared__ float s_part[2][THREADS / 32];
-    const int t = threadIdx.x, lane = t & 31;
-    const uint32_t cols = a.cols;
-    const Packed8Layout lay(a.rows, cols);
-    const Place<THREADS, OCTETS> at{t};
-    float sum[CHUNKS][8] = {};
-    uint32_t turn = 0;
-    after_last();
-    for (uint32_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
-        float n[CHUNKS][8], g[CHUNKS][8];
-        const float s = __ldg(a.rstd + r);
-        if (a.kept8) {
-            const unsigned char* codes = static_cast<const unsigned char*>(a.kept8) + lay.tile(r >> 7, 0) + (r & 127) * 128;
-            const unsigned char* scales = static_cast<const unsigned char*>(a.kept8) + lay.scales(r >> 7, 0) + Packed8Layout::scale_word(r);
-            auto unit = [&](uint32_t kb) { return block_unit(__ldg(scales + (kb >> 2) * 512 + (kb & 3))); };
-#pragma unroll
-            for (int k = 0; k < CHUNKS; ++k) {
-#pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) n[k][e] = 0.f;
-                if (OCTETS) {
-                    const uint32_t c = at.base(k), kb = c >> 7;
-                    if (kb < lay.col_blocks) {
-                        const uint2 w = __ldcs(reinterpret_cast<const uint2*>(codes + kb * 16384 + ((((c >> 4) ^ r) & 7) << 4) + (c & 8)));
-                        values4(w.x, unit(kb), n[k]);
-                        values4(w.y, unit(kb), n[k] + 4);
-                    }
-                } else {
-#pragma unroll
-                    for (uint32_t b = 0; b < 2; ++b) {
-                        const uint32_t kb = (at.run(k) >> 7) + b;
-                        if (kb >= lay.col_blocks) break;
-                        uint32_t w = 0;
-#pragma unroll
-                        for (uint32_t j = 0; j < 4; ++j) w |= static_cast<uint32_t>(__ldg(codes + kb * 16384 + (((2 * j + (lane >> 4)) ^ (r & 7)) << 4) + (lane & 15))) << (8 * j);
-                        values4(w, unit(kb), n[k] + 4 * b);
-                    }
-                }
-#pragma unroll
-                for (uint32_t e = 0; e < 8; ++e)
-                    if (at.run(k) + 512 > cols && at.column(k, e) >= cols) n[k][e] = 0.f;      // (codes behind the row's end may be NaN)
-            }
-        } else {
-            Row<T, THREADS, CHUNKS, OCTETS> h;
-            h.load(static_cast<const T*>(a.h) + r * a.h_stride, cols, at);
-#pragma unroll
-            for (int k = 0; k < CHUNKS; ++k) h.get(k, n[k]);
-        }
-        {
-            Row<T, THREADS, CHUNKS, OCTETS> dy;
-            dy.load(static_cast<const T*>(a.dy) + r * a.dy_stride, cols, at);
-#pragma unroll
-            for (int k = 0; k < CHUNKS; ++k) dy.get(k, g[k]);
-        }
-        float inner = 0.f;
-#pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            float w[8];
-            load_gain(a.gain, a.gain_bf16, at, k, cols, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                n[k][e] *= s;
-                sum[k][e] = __fmaf_rn(g[k][e], n[k][e], sum[k][e]);
-                g[k][e] *= w[e];
-                inner = __fmaf_rn(g[k][e], n[k][e], inner);
-            }
-        }
-        inner = row_sum<THREADS>(inner, s_part[turn], t) / cols;
-#pragma unroll
-        for (int k = 0; k < CHUNKS; k += 2) {
-            if (at.run(k) >= cols) break;
-            Row<T, THREADS, 2, OCTETS> dh;
-            if (a.dh) dh.load(static_cast<const T*>(a.dh) + r * a.dh_stride, cols, at, k);
-            float d[2][8];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (a.dh) dh.get(i, d[i]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = s * __fmaf_rn(-n[k + i][e], inner, g[k + i][e]);
-                    d[i][e] = a.dh ? v + d[i][e] : v;
-                }
-            }
-            store_octets(static_cast<T*>(a.dx) + r * a.dx_stride, at, k, cols, d[0], d[1]);
-        }
-    }
-    if (!a.dgain) return;
-    float* out = a.partial + static_cast<size_t>(blockIdx.x) * cols;
-#pragma unroll
-    for (int k = 0; k < CHUNKS; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (at.column(k, e) < cols) out[at.column(k, e)] = sum[k][e];
-}
-
-// The same for rows of up to 8192 columns. What bounds the form above is that a row's loads, its sum and its stores follow one
-// another; here the rows to come are on their way into shared memory meanwhile. TEAM threads to a row, 16 columns to a thread.
+// kernel. While a row's sum and its stores follow one another, the rows to come are on their way into shared memory. TEAM threads to a
+// row, 16 columns to a thread.
 // A row is copied as it lies in memory, in 16-byte words from the boundary below its first element to its last (a word that holds
 // an element of the row is memory of the caller's), neighbours by neighbours: 32 bytes between lanes took 30 times the passes
 // through shared memory. OCTETS, where rows start on the boundary: a thread reads back only what it copied itself, CPL
 // columns t CPL + w TEAM CPL, and waits for nothing else; otherwise element by element, columns 32 apart, after the team has met.
+// PARTS, for rows of more than 8192 columns: a cluster takes a row, part columns to a CTA (a multiple of 512, so that a part's
+// codes and scales are whole words of their own), and every warp leaves its share of the row's sum in every CTA's memory. The
+// cluster meets once a row; two buffers for the shares are enough, since nobody is a row ahead of a CTA that still reads.
+// What bounds it: instructions, as much as memory: 8192 x 4096 bf16 from the eight-bit checkpoint 47.5 us (4900 GB/s), half the issue
+// slots taken; with a meeting of the cluster in every row 80 us at 2048 x 16384 (3000 GB/s).
+constexpr uint32_t kPartCols = 4096, kMostParts = kNormMaxCols / kPartCols;
 template <typename T, int TEAM, int THREADS, int PER_SM> struct GradRing {
     static constexpr int kThreads = THREADS, kRows = kThreads / TEAM;
     static constexpr int CPL = 16 / sizeof(T), kWords = sizeof(T);              // columns in a 16-byte word, words to a thread
@@ -393,18 +301,33 @@ template <int TEAM> __device__ __forceinline__ void team_sync(int team)
     else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(TEAM) : "memory");
 }
 
-template <typename T, int TEAM, int THREADS, int PER_SM, bool OCTETS>
-__global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const NormGradArgs a)
+template <typename T, int TEAM, int THREADS, int PER_SM, bool OCTETS, bool PARTS>
+__global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const __grid_constant__ NormGradArgs whole)
 {
     typedef GradRing<T, TEAM, THREADS, PER_SM> G;
+    static_assert(!PARTS || TEAM == THREADS, "a row to a cluster");
+    std::conditional_t<PARTS, NormGradArgs, const NormGradArgs&> a = whole;
+    uint32_t rank = 0, first = 0;      // of the columns
+    if constexpr (PARTS) {
+        cg::cluster_group cluster = cg::this_cluster();
+        rank = cluster.block_rank();
+        first = rank * a.part;
+        a.dy = static_cast<const T*>(a.dy) + first;
+        if (a.h) a.h = static_cast<const T*>(a.h) + first;
+        if (a.dh) a.dh = static_cast<const T*>(a.dh) + first;
+        a.dx = static_cast<T*>(a.dx) + first;
+        a.cols = min(a.cols - first, a.part);
+        cluster.sync();      // all are there before anyone writes into another's memory
+    }
     constexpr int kWarps = G::kThreads / 32, CPL = G::CPL, W = G::kWords;
     extern __shared__ __align__(16) unsigned char s_ring[];
-    __shared__ __align__(16) float s_part[2][kWarps];
+    __shared__ __align__(16) float s_part[2][PARTS ? kMostParts * kWarps : kWarps];
     const int tid = threadIdx.x, t = tid % TEAM, team = tid / TEAM, lane = tid & 31;
-    const uint32_t cols = a.cols;
-    const Packed8Layout lay(a.rows, cols);
+    const uint32_t cols = a.cols, parts = PARTS ? a.parts : 1;
+    const Packed8Layout lay(a.rows, whole.cols);
+    const uint32_t blocks = (cols + 127) / 128;
     const bool kept = a.kept8 != nullptr;
-    const uint32_t step = gridDim.x * G::kRows;
+    const uint32_t walker = blockIdx.x / parts, step = gridDim.x / parts * G::kRows;
     const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + team * G::kTeam;
     // column of this thread's element e (0 .. 15), and the block it lies in
     auto column = [&](uint32_t e) { return OCTETS ? (e / CPL * TEAM + t) * CPL + e % CPL : (t & ~31) * 16 + 32 * e + lane; };
@@ -428,14 +351,14 @@ __global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const N
             row(a.dy, a.dy_stride, at);
             if (a.dh) row(a.dh, a.dh_stride, at + 2 * G::kRow);
             if (kept) {
-                const char* src = static_cast<const char*>(a.kept8) + lay.tile(r >> 7, 0);
+                const char* src = static_cast<const char*>(a.kept8) + lay.tile(r >> 7, first >> 7);
                 if (OCTETS) {
 #pragma unroll
                     for (int w = 0; w < W; ++w) {
                         const uint32_t i = w * TEAM + t, c = i * CPL;
-                        if (c >> 7 < lay.col_blocks) copy_small<CPL>(at + G::kRow + i * CPL, src + (c >> 7) * 16384 + code_at(r, c & ~7u) + (c & 7));
+                        if (c >> 7 < blocks) copy_small<CPL>(at + G::kRow + i * CPL, src + (c >> 7) * 16384 + code_at(r, c & ~7u) + (c & 7));
                     }
-                } else if (t * 16u >> 7 < lay.col_blocks) {
+                } else if (t * 16u >> 7 < blocks) {
                     copy16(at + G::kRow + t * 16, src + (t * 16u >> 7) * 16384 + code_at(r, t * 16));
                 }
             } else {
@@ -455,11 +378,11 @@ __global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const N
         if (r >= a.rows) return;
         to.root = __ldg(a.rstd + r);
         if (!kept) return;
-        const char* words = static_cast<const char*>(a.kept8) + lay.scales(r >> 7, 0) + Packed8Layout::scale_word(r);
+        const char* words = static_cast<const char*>(a.kept8) + lay.scales(r >> 7, first >> 9) + Packed8Layout::scale_word(r);
 #pragma unroll
         for (int w = 0; w < kScaleWords; ++w) {
             const uint32_t c = OCTETS ? (w * TEAM + t) * CPL : (t & ~31) * 16;
-            if (c >> 7 < lay.col_blocks) to.scale[w] = __ldg(reinterpret_cast<const uint32_t*>(words + (c >> 9) * 512));
+            if (c >> 7 < blocks) to.scale[w] = __ldg(reinterpret_cast<const uint32_t*>(words + (c >> 9) * 512));
         }
     };
     // this thread's 16 elements of a copied row as pairs, zero behind the row's end
@@ -504,12 +427,12 @@ __global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const N
     f32x2 gain[8], sum[8];
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e) {
-        auto at = [&](uint32_t c) { return a.gain && c < cols ? gain_at(a.gain, a.gain_bf16, c) : 1.f; };
+        auto at = [&](uint32_t c) { return a.gain && c < cols ? gain_at(a.gain, a.gain_bf16, first + c) : 1.f; };
         gain[e] = pair_of(at(column(2 * e)), at(column(2 * e + 1)));
         sum[e] = 0;
     }
-    const float per_col = 1.f / cols;
-    uint32_t r = blockIdx.x * G::kRows + team, slot = 0, turn = 0;
+    const float per_col = 1.f / whole.cols;
+    uint32_t r = walker * G::kRows + team, slot = 0, turn = 0;
 #pragma unroll
     for (uint32_t i = 0; i + 1 < G::kDepth; ++i) fetch(r + i * step, i);
     Scalars now = {}, next = {}, later = {};
@@ -570,7 +493,13 @@ __global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const N
         float inner, odd;
         unpack2(inner2, inner, odd);
         inner = warp_sum(inner + odd);
-        if (TEAM > 32) {
+        if (PARTS) {
+            // every warp's share to every part of the row; the rest of the step's reads go on while they are under way
+            cg::cluster_group cluster = cg::this_cluster();
+            if (lane < parts) *cluster.map_shared_rank(&s_part[turn][rank * kWarps + (tid >> 5)], lane) = inner;
+            __syncwarp();
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        } else if (TEAM > 32) {
             constexpr int kTeamWarps = TEAM / 32;
             if (lane == 0) s_part[turn][tid >> 5] = inner;
             team_sync<TEAM>(team);
@@ -586,10 +515,22 @@ __global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const N
                 for (int w = 0; w < kTeamWarps; ++w) inner += s_part[turn][team * kTeamWarps + w];
             }
         }
-        const f32x2 minus = twice(-inner * per_col), root2 = twice(s);
         f32x2 d[8];
+        auto read_dh = [&] {
+            if (a.dh) read(at + 2 * G::kRow, OCTETS ? 0 : offset(a.dh, r, a.dh_stride), d);
+        };
+        if (PARTS) {
+            read_dh();
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            inner = 0.f;
+            for (uint32_t w = 0; w < parts * (kWarps / 4); ++w) {
+                const float4 x = *reinterpret_cast<const float4*>(&s_part[turn][4 * w]);
+                inner += (x.x + x.y) + (x.z + x.w);
+            }
+        }
+        const f32x2 minus = twice(-inner * per_col), root2 = twice(s);
+        if (!PARTS) read_dh();
         if (a.dh) {
-            read(at + 2 * G::kRow, OCTETS ? 0 : offset(a.dh, r, a.dh_stride), d);
 #pragma unroll
             for (int e = 0; e < 8; ++e) d[e] = fma2(root2, fma2(n[e], minus, g[e]), d[e]);
         } else {
@@ -634,7 +575,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const N
     // own memory for them to read
     float* shares = reinterpret_cast<float*>(s_ring);
     float* own = shares + (G::kRows > 1 ? 16 * G::kThreads : 0);
-    float* out = a.partial ? a.partial + static_cast<size_t>(blockIdx.x) * cols : own;
+    float* out = a.partial ? a.partial + static_cast<size_t>(walker) * whole.cols + first : own;
     float mysum[16];
 #pragma unroll
     for (int e = 0; e < 8; ++e) unpack2(sum[e], mysum[2 * e], mysum[2 * e + 1]);
@@ -653,7 +594,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const N
             if (column(e) < cols) out[column(e)] = v;
         }
     }
-    if (a.partial) return;
+    if (PARTS || a.partial) return;
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
     for (uint32_t c = blockIdx.x * G::kThreads + tid; c < cols; c += gridDim.x * G::kThreads) {
@@ -672,7 +613,6 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_gain_kernel(const float* p
     float v = 0.f;
     after_last();
     if (c < cols)
-#pragma unroll 10
         for (uint32_t i = y; i < n; i += kSumRows) v += partial[static_cast<size_t>(i) * cols + c];
     s[y][x] = v;
     __syncthreads();
@@ -703,7 +643,11 @@ template <bool ALIGNED, typename F> int by_width(uint32_t cols, F&& f)
 // CTAs that walk the rows of a backward pass: the rows, or what the 148 SMs hold at a time (a constant, so that sums are the same
 // on every device and the workspace is known without one).
 constexpr uint32_t kSms = 148;
-constexpr uint32_t kRingCols = 8192;
+// Clusters for rows in parts: two CTAs to an SM, and what clusters of up to eight leave free of 296 places, so that all of them run at
+// once (2048 x 16384 bf16: 70 to 64 clusters 77 to 80 us, 74 clusters 117; up to 8192 columns a CTA takes a row by itself: 52 us at
+// 4096 x 8192, 70 in two parts).
+constexpr uint32_t kRingCols = 8192, kPartPlaces = 256;
+uint32_t parts_of(uint32_t cols) { return (cols + kPartCols - 1) / kPartCols; }
 // Few rows go to one cluster, whose CTAs add their shares themselves: no second kernel and no workspace. (200 x 768 fp32: 15.5 -> 11.8 us
 // a call, most of it the host's.)
 constexpr uint32_t kCluster = 8;
@@ -712,7 +656,7 @@ bool one_cluster(uint32_t rows, uint32_t cols) { return cols <= kRingCols && sta
 template <typename T, int TEAM, int THREADS, int PER_SM, bool OCTETS> int run_ring(const NormGradArgs& a, bool cluster, uint32_t* ctas, cudaStream_t stream)
 {
     typedef GradRing<T, TEAM, THREADS, PER_SM> G;
-    constexpr auto kernel = norm_grad_ring_kernel<T, TEAM, THREADS, PER_SM, OCTETS>;
+    constexpr auto kernel = norm_grad_ring_kernel<T, TEAM, THREADS, PER_SM, OCTETS, false>;
     const cudaError_t e = opt_in<kernel>(G::kSmem);
     if (e != cudaSuccess) return static_cast<int>(e);
     *ctas = cluster ? kCluster : std::min<uint32_t>((a.rows + G::kRows - 1) / G::kRows, PER_SM * kSms);
@@ -725,8 +669,21 @@ template <typename T, int TEAM, bool OCTETS> int run_ring(const NormGradArgs& a,
     if (TEAM == 512 || cluster) return run_ring<T, TEAM, kThreads, 1, OCTETS>(a, cluster, ctas, stream);
     return run_ring<T, TEAM, kThreads, TEAM == 512 ? 1 : 2, OCTETS>(a, false, ctas, stream);
 }
+template <typename T, bool OCTETS> int run_parts(NormGradArgs a, uint32_t* ctas, cudaStream_t stream)
+{
+    constexpr int kThreads = kPartCols / 16;
+    typedef GradRing<T, kThreads, kThreads, 2> G;
+    constexpr auto kernel = norm_grad_ring_kernel<T, kThreads, kThreads, 2, OCTETS, true>;
+    const cudaError_t e = opt_in<kernel>(G::kSmem);
+    if (e != cudaSuccess) return static_cast<int>(e);
+    a.parts = parts_of(a.cols);
+    a.part = ((a.cols + a.parts - 1) / a.parts + 511) & ~511u;
+    *ctas = std::min(a.rows, kPartPlaces / a.parts);
+    return static_cast<int>(launch_early(kernel, *ctas * a.parts, kThreads, G::kSmem, stream, a.parts, a));
+}
 template <typename T, bool OCTETS> int run_ring(const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
 {
+    if (a.cols > kRingCols) return run_parts<T, OCTETS>(a, ctas, stream);
     if (a.cols <= 512) return run_ring<T, 32, OCTETS>(a, ctas, stream);
     if (a.cols <= 1024) return run_ring<T, 64, OCTETS>(a, ctas, stream);
     if (a.cols <= 2048) return run_ring<T, 128, OCTETS>(a, ctas, stream);
@@ -745,13 +702,7 @@ template <typename E, bool ALIGNED> int run_norm(const NormArgs& a, cudaStream_t
 }
 template <bool OCTETS> int run_grad(int dtype, const NormGradArgs& a, uint32_t* ctas, cudaStream_t stream)
 {
-    if (a.cols <= kRingCols) return dtype ? run_ring<bf16, OCTETS>(a, ctas, stream) : run_ring<float, OCTETS>(a, ctas, stream);
-    *ctas = std::min(a.rows, kSms);
-    auto run = [&](auto threads) {
-        constexpr int T = decltype(threads)::value;
-        return static_cast<int>(launch_early(dtype ? norm_grad_kernel<bf16, T, 4, OCTETS> : norm_grad_kernel<float, T, 4, OCTETS>, *ctas, T, 0, stream, 1, a));
-    };
-    return a.cols <= 16384 ? run(Const<512>()) : run(Const<1024>());
+    return dtype ? run_ring<bf16, OCTETS>(a, ctas, stream) : run_ring<float, OCTETS>(a, ctas, stream);
 }
 
 }  // namespace
@@ -765,7 +716,8 @@ int launch_norm(int dtype, const NormArgs& a, void* stream)
 
 size_t norm_grad_workspace(uint32_t rows, uint32_t cols)
 {
-    return one_cluster(rows, cols) ? 0 : static_cast<size_t>(std::min(rows, 2 * kSms)) * cols * sizeof(float);
+    if (one_cluster(rows, cols)) return 0;
+    return static_cast<size_t>(std::min(rows, cols > kRingCols ? kPartPlaces / parts_of(cols) : 2 * kSms)) * cols * sizeof(float);
 }
 
 int launch_norm_grad(int dtype, const NormGradArgs& a, int* launched, void* stream)

@@ -93,6 +93,30 @@ def test_backward(n, cols, kept, dtype):
     assert torch.equal(again[0], dx) and torch.equal(again[1], dgain)
 
 
+# rows in several parts, more of them than there are clusters for; a last part of one column, of one block, of a whole part
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("n,cols", [(200, 8193), (180, 9216), (90, 12289), (130, 16384), (60, 20481), (50, 28672), (70, 32768)])
+def test_backward_of_wide_rows(n, cols, pad, dtype):
+    view = lambda seed: rows_of(n, cols + pad, dtype, seed)[:, pad:]
+    x, g, gh, gain = view(1), view(2), view(3), 1 + 0.3 * rows_of(1, cols, torch.float32, 4)[0]
+    f = randes.rms_norm(x, gain, eps=EPS, checkpoint=True)
+    for kept in (False, True):
+        hd = (f.kept.unpack() if kept else f.h).double()
+        rstd, gd = f.rstd.double()[:, None], g.double()
+        nd, gg = hd * rstd, gd * gain.double()
+        want = rstd * (gg - nd * (gg * nd).mean(1, keepdim=True)) + gh.double()
+        size = rstd * (gg.abs() + nd.abs() * (gg * nd).abs().mean(1, keepdim=True)) + gh.double().abs()
+        tol = (2 * FP32 + 4 * 2.0 ** -24) * size + (step(dtype) * want.abs() if dtype is torch.bfloat16 else 0)
+        dx, dgain = randes.rms_norm_backward(g, f.kept if kept else f.h, f.rstd, gain, dh=gh)
+        assert ((dx.double() - want).abs() <= tol).all()
+        # at most n rows one after the other, then the clusters' shares
+        assert ((dgain.double() - (gd * nd).sum(0)).abs() <= (n + 100) * 2.0 ** -24 * (gd * nd).abs().sum(0)).all()
+        base = rows_of(n, cols + pad, dtype, 2)
+        into, _ = randes.rms_norm_backward(base[:, pad:], f.kept if kept else f.h, f.rstd, gain, dh=gh, out=base[:, pad:])
+        assert torch.equal(into, dx) and torch.equal(base[:, :pad], rows_of(n, cols + pad, dtype, 2)[:, :pad])
+
+
 def test_gradient_against_differences():
     n, cols, d = 3, 200, 1e-4
     x, gain, g = rows_of(n, cols, torch.float32, 1), 1 + 0.3 * rows_of(1, cols, torch.float32, 2)[0], rows_of(n, cols, torch.float32, 3)
