@@ -648,8 +648,8 @@ int randes_rms_norm(const randes_rms_norm_t* norm, void* stream);
  *   kept8             in place of h (which is NULL then): h in eight bits
  *   rstd              of the forward call
  *   dgain             device fp32 [cols] or NULL
- *   workspace         device memory, 16-byte aligned, at least randes_rms_norm_backward_workspace(rows, cols) bytes with dgain (none
- *                     for up to 2^18 elements in rows of up to 8192 columns)
+ *   workspace         device memory, 16-byte aligned, at least randes_rms_norm_backward_workspace(rows, cols) bytes with dgain (0 for
+ *                     few rows: NULL will do)
  * Sums in fp32 in a fixed order; one kernel launch, two where a workspace is needed.  Errors: as above, WORKSPACE_TOO_SMALL.
  */
 typedef struct {

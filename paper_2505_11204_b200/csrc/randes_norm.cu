@@ -266,8 +266,9 @@ __global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(con
 // PARTS, for rows of more than 8192 columns: a cluster takes a row, part columns to a CTA (a multiple of 512, so that a part's
 // codes and scales are whole words of their own), and every warp leaves its share of the row's sum in every CTA's memory. The
 // cluster meets once a row; two buffers for the shares are enough, since nobody is a row ahead of a CTA that still reads.
-// What bounds it: instructions, as much as memory: 8192 x 4096 bf16 from the eight-bit checkpoint 47.5 us (4900 GB/s), half the issue
+// What bounds it: instructions, as much as memory: 8192 x 4096 bf16 from the eight-bit checkpoint 46.9 us (5000 GB/s), half the issue
 // slots taken; with a meeting of the cluster in every row 80 us at 2048 x 16384 (3000 GB/s).
+constexpr uint32_t kCluster = 16;
 constexpr uint32_t kPartCols = 4096, kMostParts = kNormMaxCols / kPartCols;
 template <typename T, int TEAM, int THREADS, int PER_SM> struct GradRing {
     static constexpr int kThreads = THREADS, kRows = kThreads / TEAM;
@@ -597,15 +598,19 @@ __global__ void __launch_bounds__(THREADS, PER_SM) norm_grad_ring_kernel(const _
     if (PARTS || a.partial) return;
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
-    for (uint32_t c = blockIdx.x * G::kThreads + tid; c < cols; c += gridDim.x * G::kThreads) {
-        float v = 0.f;
-        for (uint32_t k = 0; k < gridDim.x; ++k) v += cluster.map_shared_rank(own, k)[c];
-        a.dgain[c] = v;
+    for (uint32_t c = blockIdx.x * G::kThreads + tid; c < cols; c += kCluster * G::kThreads) {
+        float v[kCluster];
+#pragma unroll
+        for (uint32_t k = 0; k < kCluster; ++k) v[k] = cluster.map_shared_rank(own, k)[c];
+#pragma unroll
+        for (uint32_t k = 1; k < kCluster; ++k) v[0] += v[k];
+        a.dgain[c] = v[0];
     }
     cluster.sync();      // nobody leaves while its shares may still be read
 }
 
-constexpr int kSumRows = 16;
+// (Eight, 16 or 32 sums side by side: 48.9, 47.7, 46.9 us with the gradient in front, 8192 x 4096 bf16.)
+constexpr int kSumRows = 32;
 __global__ void __launch_bounds__(32 * kSumRows) norm_gain_kernel(const float* partial, uint32_t n, uint32_t cols, float* dgain)
 {
     __shared__ float s[kSumRows][33];
@@ -648,16 +653,22 @@ constexpr uint32_t kSms = 148;
 // 4096 x 8192, 70 in two parts).
 constexpr uint32_t kRingCols = 8192, kPartPlaces = 256;
 uint32_t parts_of(uint32_t cols) { return (cols + kPartCols - 1) / kPartCols; }
-// Few rows go to one cluster, whose CTAs add their shares themselves: no second kernel and no workspace. (200 x 768 fp32: 15.5 -> 11.8 us
-// a call, most of it the host's.)
-constexpr uint32_t kCluster = 8;
-bool one_cluster(uint32_t rows, uint32_t cols) { return cols <= kRingCols && static_cast<uint64_t>(rows) * cols <= 1u << 18; }
+// Few rows go to one cluster, whose CTAs add their shares themselves: no second kernel and no workspace, whose allocation and launch
+// cost the host 4 us a call. The device takes 1 us for every step of 16 CTAs x 4096 columns on top of 4, so this holds up to four steps.
+// (200 x 768 fp32, four steps: 7.7 us on the device and 11.6 a call, against 5.7 and 15.5 with two kernels; with eight CTAs 10.7;
+// 4000 x 64, sixteen steps of rows that fill an eighth of a team: 26.)
+bool one_cluster(uint32_t rows, uint32_t cols)
+{
+    uint32_t width = 512;      // what a team takes
+    while (width < cols) width *= 2;
+    return cols <= kRingCols && static_cast<uint64_t>(rows) * width <= 4 * kCluster * 4096;
+}
 
 template <typename T, int TEAM, int THREADS, int PER_SM, bool OCTETS> int run_ring(const NormGradArgs& a, bool cluster, uint32_t* ctas, cudaStream_t stream)
 {
     typedef GradRing<T, TEAM, THREADS, PER_SM> G;
     constexpr auto kernel = norm_grad_ring_kernel<T, TEAM, THREADS, PER_SM, OCTETS, false>;
-    const cudaError_t e = opt_in<kernel>(G::kSmem);
+    const cudaError_t e = opt_in<kernel, PER_SM == 1>(G::kSmem);
     if (e != cudaSuccess) return static_cast<int>(e);
     *ctas = cluster ? kCluster : std::min<uint32_t>((a.rows + G::kRows - 1) / G::kRows, PER_SM * kSms);
     return static_cast<int>(launch_early(kernel, *ctas, THREADS, G::kSmem, stream, cluster ? kCluster : 1, a));

@@ -10,8 +10,8 @@
 
 namespace randes {
 
-// A kernel has to opt in to more than 48 KiB of shared memory, once per device.
-template <auto KERNEL> cudaError_t opt_in(size_t bytes)
+// A kernel has to opt in to more than 48 KiB of shared memory, and to clusters of more than eight CTAs, once per device.
+template <auto KERNEL, bool CLUSTERS = false> cudaError_t opt_in(size_t bytes)
 {
     constexpr int kDevices = 64;
     static std::atomic<bool> granted[kDevices];
@@ -19,6 +19,7 @@ template <auto KERNEL> cudaError_t opt_in(size_t bytes)
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess || (device < kDevices && granted[device].load(std::memory_order_relaxed))) return e;
     e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (CLUSTERS && e == cudaSuccess) e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess && device < kDevices) granted[device].store(true, std::memory_order_relaxed);
     return e;
 }
