@@ -64,6 +64,9 @@ class _NormLinear(torch.autograd.Function):
 def norm_linear(x, gain, weight, residual=None, eps: float = 1e-6):
     """(y, h): h = x + residual (x itself without one), y = (norm of h, times gain) weight^T, differentiable in all of them.
 
-    x, residual: [n, cols] fp32 or bf16 CUDA tensors; gain: [cols] or None; weight: [rows, cols]; y: [n, rows] of x's type."""
+    x, residual: [n, cols] fp32 or bf16 CUDA tensors; gain: [cols] or None; weight: [rows, cols]; y: [n, rows] of x's type.
+
+    A step may be captured into a graph. As with every torch function, warm it up on a side stream and let go of all results of
+    eager calls on the same leaves before: a backward pass under capture must not meet an eager graph that still lives."""
     out = _NormLinear.apply(x, gain, weight, residual, float(eps))
     return out if residual is not None else (out, x)

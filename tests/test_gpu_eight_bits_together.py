@@ -120,6 +120,63 @@ def test_a_step_is_captured_and_replayed():
         assert all(torch.equal(a, b) for a, b in zip(out, step()))
 
 
+def test_autograd_is_captured_and_replayed():
+    made = make(200, 512, 256, torch.bfloat16)
+    x, r, gain, w, g, gh = [t.clone() for t in made]
+    leaves = [t.requires_grad_(True) for t in (x, gain, w, r)]
+
+    def step():
+        y, h = norm_linear(x, gain, w, r)
+        return torch.autograd.grad([y, h], leaves, [g, gh])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in (1, 2):
+        with torch.no_grad():
+            for to, new in zip((x, r, gain, w, g, gh), make(200, 512, 256, torch.bfloat16, seed)):
+                to.copy_(new)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(out, step()))
+
+
+def test_two_threads_with_streams_of_their_own():
+    import threading
+
+    made = [make(150 + 100 * i, 512 + 256 * i, 256, torch.bfloat16, i) for i in range(2)]
+
+    def step(x, r, gain, w, g, gh):
+        f = randes.rms_norm(x, gain, r, packed=True, checkpoint=True)
+        p, pt = randes.pack8_both(w)
+        q, qt = randes.pack8_both(g)
+        dx, dgain = randes.rms_norm_backward(randes.packed8_linear(q, pt, y_dtype=randes.BF16), f.kept, f.rstd, gain, dh=gh)
+        return randes.packed8_linear(f.y, p), randes.packed8_linear(x[:7], p), randes.packed8_linear(qt, randes.pack8_transposed(f.y)), dx, dgain
+
+    want, wrong = [step(*m) for m in made], []
+    torch.cuda.synchronize()
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                got = step(*made[i])
+                stream.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                    wrong.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 def test_prompts_in_eight_bits_agree_with_the_retrieved_models():
     r = serve.read_prompts(width=256, blocks=3, vocab=2003, n_tasks=3, n_tokens=131)
     assert torch.isfinite(r["eight"]).all() and r["eight"].shape == (3, 130)
