@@ -6,7 +6,13 @@
 // scales are copied to tensor memory once per 512 columns.
 //
 // w is operand A (128 rows: tensor memory lanes), x operand B (16 to 128 tokens: columns): few tokens waste nothing, and a warp of
-// the epilogue writes 32 neighbouring outputs of a token whatever the row's alignment.
+// the epilogue writes 32 neighbouring outputs of a token whatever the row's alignment. More than 128 tokens: pairs of CTAs, below.
+//
+// What bounds it. Few tokens on small matrices: a chain of latencies (tensor memory, the first copies, the sums of the CTAs that share
+// a tile): 1 token, 1024 x 4096 4.6 us in a graph, of which the bytes are 0.7. Up to 128 tokens on large ones: bytes, 8192 x 8192 with 1,
+// 64, 128 tokens 15.5, 16.4, 18.6 us (4.3 TB/s). Many tokens: the tensor cores; 8192^3 397 us (2.77 PFLOP/s, their pipe taken 89 % of
+// the time and the clock held down by the power limit), 4096^3 54 to 62 us. One round of tiles, 4096 tokens of 4096 x 1024: 16.3 us, of which the
+// products are 12; the rest is the first stage's way and the last tile's.
 #include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -841,8 +847,8 @@ int launch_linear8(Linear8Args& a, int x_dtype, int sm_count, void* stream)
         const uint64_t single = 400 + (((tiles << log) + sms - 1) / sms * kb * 32 >> log) + (log ? 150 + 30 * log : 0);
         if (single < 500 + (pairs + sms / 2 - 1) / (sms / 2) * kb * 28) return run_linear8<128, uint8_t>(a, sm_count, s);
     }
-    // (4096^3: 64.0 us with w as operand A, 60.6 turned, where results go out while the next tile is worked on; one round of 1024 x 4096 x
-    // 4096: 16.7 and 17.4)
+    // (With w as operand A and turned, where results go out while the next tile is worked on: 8192^3 405 and 397 us, 4096 x 4096 x 1024 19.4
+    // and 18.6. One round, 4096 x 1024 x 4096: 16.3 and 17.6.)
     const bool turned = pairs > sms / 2 && (reinterpret_cast<uintptr_t>(a.y) | a.y_stride * (a.y_bf16 ? 2 : 4)) % 32 == 0;
     return turned ? run_pairs<true>(a, sm_count, s) : run_pairs<false>(a, sm_count, s);
 }

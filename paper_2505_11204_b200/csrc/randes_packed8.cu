@@ -38,8 +38,9 @@ template <typename Args> __device__ __forceinline__ uint32_t matrix_of(const Arg
 // A warp takes four rows of 512 columns. A lane holds 16 neighbours of each, every load (two rows' where that would take more than 64
 // registers) before the first use: of rows that start on 16-byte boundaries, or (LOOSE) of bf16 rows that start anywhere. Other rows
 // (STRIDED): two runs of 256, a lane's columns 32 apart.
+// What bounds it: memory; 8192 x 4096 bf16 15.8 us, fp32 26.7 (6.3 TB/s), out of base and superposition 28.5 and 47.5 (5.9, 6.35).
 // (With eight neighbours to a lane the scales and places of half as many elements were worked out at a time: 20.0 us for 8192 x 4096
-// bf16.)
+// bf16. Rows that start anywhere, 4096 x 4001 bf16: 10.7 us, 4.6 TB/s.)
 enum { kAligned, kLoose, kStrided };
 template <typename T, typename M, bool RETRIEVE, int MODE, uint32_t BATCH>
 __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_constant__ Pack8Batch<BATCH> a)
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
 }
 
 // A lane takes CPL neighbouring columns at a time, 16 bytes of the output, so that a warp writes whole lines; where rows do not start
-// on 16-byte boundaries single columns, 32 apart.
+// on 16-byte boundaries single columns, 32 apart. Memory bounds it: 8192 x 4096 into bf16 17.5 us, fp32 29.2 (5.7 TB/s).
 template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 * 32) unpack8_kernel(const __grid_constant__ Unpack8Batch<BATCH> a)
 {
     constexpr uint32_t CPL = OCTETS ? Store<T>::CPL : 8, kSteps = 512 / 32 / CPL;      // columns to a lane and step
@@ -216,8 +217,10 @@ template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_boun
 // first element (loads of single bf16 elements took four times as long: too few bytes under way). Elements that have 8 bits or
 // fewer behind the leading one stay pairs of bf16. The greatest magnitudes of the columns meet in shared memory; the codes of
 // a column are turned there, 8-byte pieces exchanged by a number that differs between the 16 lanes that write at a time, so
-// that they do not meet in a bank. (Measured at 8192 x 4096: bf16 with four columns to a thread 26 us instead of 22.5, fp32 with eight
-// 54 instead of 32.)
+// that they do not meet in a bank.
+// What bounds it: instructions (65 to 73 % of the issue slots; the codes of either form, and single bytes put together along the columns).
+// 8192 x 4096 bf16 20.0 us (5.0 TB/s), with BOTH 31.8 (4.2), fp32 29.8 (5.6), of a matrix in eight bits 20.6 (3.3). (bf16 with four
+// columns to a thread 26 us where eight took 22.5, fp32 with eight 54 where four took 32.)
 __device__ __forceinline__ uint32_t top_bf16x2(uint32_t a, uint32_t b)      // magnitudes; the result's signs mean nothing
 {
     uint32_t r;
