@@ -218,9 +218,10 @@ template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_boun
 // fewer behind the leading one stay pairs of bf16. The greatest magnitudes of the columns meet in shared memory; the codes of
 // a column are turned there, 8-byte pieces exchanged by a number that differs between the 16 lanes that write at a time, so
 // that they do not meet in a bank.
-// What bounds it: instructions (65 to 73 % of the issue slots; the codes of either form, and single bytes put together along the columns).
-// 8192 x 4096 bf16 20.0 us (5.0 TB/s), with BOTH 31.8 (4.2), fp32 29.8 (5.6), of a matrix in eight bits 20.6 (3.3). (bf16 with four
-// columns to a thread 26 us where eight took 22.5, fp32 with eight 54 where four took 32.)
+// What bounds it: memory, and with BOTH or of a matrix in eight bits the instructions that make codes. 8192 x 4096 bf16 14.1 us (7.1 TB/s; some of
+// it stays in L2), with BOTH 23.6 (5.7), fp32 25.7 and 36.6 (6.5, 5.5), of a matrix in eight bits 15.9. (With every thread working out
+// the scales of its own columns and rows, and products in fp32: 20.0, 31.8, 29.8, 46.2, 20.6. bf16 with four columns to a thread took
+// 26 us where eight took 22.5, fp32 with eight 54 where four took 32.)
 __device__ __forceinline__ uint32_t top_bf16x2(uint32_t a, uint32_t b)      // magnitudes; the result's signs mean nothing
 {
     uint32_t r;
@@ -230,7 +231,12 @@ __device__ __forceinline__ uint32_t top_bf16x2(uint32_t a, uint32_t b)      // m
 __device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-template <typename T> struct Part;      // a thread's 8 rows x CPL columns; `set` takes a row as 16 bytes
+// What a block's elements are multiplied by: NaN (and with it every code) where its greatest magnitude is not finite.
+__device__ __forceinline__ float factor_of(float top, uint32_t e) { return not_finite(top) ? __uint_as_float(0x7FC00000u) : block_inverse(e); }
+
+// A thread's 8 rows x CPL columns. `set` takes a row as 16 bytes; row_codes hands on the codes of each row and its exponent, the
+// latter in one lane; column_codes those of each column, by factors that lie in shared memory four columns to a word of them.
+template <typename T> struct Part;
 template <> struct Part<float> {
     float v[8][4];
     __device__ __forceinline__ void set(int i, const uint4& x) { Store<float>::widen(x, v[i]); }
@@ -248,12 +254,26 @@ template <> struct Part<float> {
             top[e] = top8(col);
         }
     }
-    __device__ __forceinline__ void row_tops(float (&top)[8]) const
+    template <typename F, typename G> __device__ __forceinline__ void row_codes(uint32_t l, F&& codes, G&& exponent) const
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)      // (as bits: none is negative)
-            top[i] = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top3(v[i][0], v[i][1], top2(v[i][2], v[i][3])))));
+        for (int i = 0; i < 8; ++i) {      // (as bits: none is negative)
+            const float top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top3(v[i][0], v[i][1], top2(v[i][2], v[i][3])))));
+            const uint32_t e = block_scale(top), w[1] = {codes_of(v[i][0], v[i][1], v[i][2], v[i][3], factor_of(top, e))};
+            codes(i, w);
+            if (l == 0) exponent(i, e);
+        }
     }
+    typedef float4 Factors;
+    static __device__ __forceinline__ float store_factor(float f) { return f; }
+    template <typename F> __device__ __forceinline__ void column_codes(const Factors (&f)[1], F&& codes) const
+    {
+        const float by[4] = {f[0].x, f[0].y, f[0].z, f[0].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            codes(e, make_uint2(codes_of(v[0][e], v[1][e], v[2][e], v[3][e], by[e]), codes_of(v[4][e], v[5][e], v[6][e], v[7][e], by[e])));
+    }
+    static __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d, float f) { return codes4(a * f, b * f, c * f, d * f); }
 };
 template <> struct Part<bf16> {
     uint32_t w[8][4];
@@ -276,19 +296,63 @@ template <> struct Part<bf16> {
             top[2 * j + 1] = fabsf(high_half(m));
         }
     }
-    __device__ __forceinline__ void row_tops(float (&top)[8]) const      // over 16 lanes, two rows to a word
+    // Over 16 lanes, two rows to a word: half the words go to the other half of the lanes first, so that four lanes end with each and work
+    // out its two rows' scales for all (every lane for all rows: a sixth of the kernel's instructions).
+    template <typename F, typename G> __device__ __forceinline__ void row_codes(uint32_t l, F&& codes, G&& exponent) const
     {
+        uint32_t m[4];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const uint32_t a = top_bf16x2(top_bf16x2(w[i][0], w[i][1]), top_bf16x2(w[i][2], w[i][3]));
-            const uint32_t b = top_bf16x2(top_bf16x2(w[i + 1][0], w[i + 1][1]), top_bf16x2(w[i + 1][2], w[i + 1][3]));
-            uint32_t m = top_bf16x2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t a = top_bf16x2(top_bf16x2(w[2 * j][0], w[2 * j][1]), top_bf16x2(w[2 * j][2], w[2 * j][3]));
+            const uint32_t b = top_bf16x2(top_bf16x2(w[2 * j + 1][0], w[2 * j + 1][1]), top_bf16x2(w[2 * j + 1][2], w[2 * j + 1][3]));
+            m[j] = top_bf16x2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+        }
+        const bool upper = l & 8, odd = l & 4;
+        const uint32_t m0 = top_bf16x2(upper ? m[2] : m[0], __shfl_xor_sync(~0u, upper ? m[0] : m[2], 8));
+        const uint32_t m1 = top_bf16x2(upper ? m[3] : m[1], __shfl_xor_sync(~0u, upper ? m[1] : m[3], 8));
+        uint32_t mine = top_bf16x2(odd ? m1 : m0, __shfl_xor_sync(~0u, odd ? m0 : m1, 4));
+        mine = top_bf16x2(mine, __shfl_xor_sync(~0u, mine, 2));
+        mine = top_bf16x2(mine, __shfl_xor_sync(~0u, mine, 1));
+        const float lo = fabsf(low_half(mine)), hi = fabsf(high_half(mine));      // of rows 2 (l / 4) and the next
+        const uint32_t elo = block_scale(lo), ehi = block_scale(hi);
+        if ((l & 3) < 2) exponent(l / 4 * 2 + (l & 1), l & 1 ? ehi : elo);
+        const uint32_t factors = __byte_perm(__float_as_uint(factor_of(lo, elo)), __float_as_uint(factor_of(hi, ehi)), 0x7632);      // (powers of two: exact)
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) m = top_bf16x2(m, __shfl_xor_sync(~0u, m, o));
-            top[i] = fabsf(low_half(m));
-            top[i + 1] = fabsf(high_half(m));
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t f = __shfl_sync(~0u, factors, 4 * j, 16);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t twice = __byte_perm(f, f, i ? 0x3232 : 0x1010);
+                const uint32_t* x = w[2 * j + i];
+                const uint32_t c[2] = {codes_of(times(x[0], twice), times(x[1], twice)), codes_of(times(x[2], twice), times(x[3], twice))};
+                codes(2 * j + i, c);
+            }
         }
     }
+    typedef uint2 Factors;
+    static __device__ __forceinline__ unsigned short store_factor(float f) { return static_cast<unsigned short>(__float_as_uint(f) >> 16); }
+    template <typename F> __device__ __forceinline__ void column_codes(const Factors (&f)[2], F&& codes) const
+    {
+        const uint32_t by[4] = {f[0].x, f[0].y, f[1].x, f[1].y};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = times(w[i][j], by[j]);
+            codes(2 * j, make_uint2(codes4(low_half(x[0]), low_half(x[1]), low_half(x[2]), low_half(x[3])),
+                                    codes4(low_half(x[4]), low_half(x[5]), low_half(x[6]), low_half(x[7]))));
+            codes(2 * j + 1, make_uint2(codes4(high_half(x[0]), high_half(x[1]), high_half(x[2]), high_half(x[3])),
+                                        codes4(high_half(x[4]), high_half(x[5]), high_half(x[6]), high_half(x[7]))));
+        }
+    }
+    // by powers of two: exact, but for what is far below a code's least step
+    static __device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b)
+    {
+        uint32_t r;
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t codes_of(uint32_t a, uint32_t b) { return codes4(low_half(a), high_half(a), low_half(b), high_half(b)); }
 };
 // what a source's elements are held as, columns to a thread, threads to a row and to a CTA
 template <typename T> struct Turn {
@@ -374,9 +438,12 @@ __device__ __forceinline__ void load_part8(const Turn8Args& a, uint32_t r0, uint
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) {
         float x[8];
-        values4(w[i].x, block_unit(e[i]), x);
-        values4(w[i].y, block_unit(e[i]), x + 4);
+        values4(w[i].x, 1.f, x);
+        values4(w[i].y, 1.f, x + 4);
         v.set(i, x);
+        const uint32_t unit = __float_as_uint(block_unit(e[i])), twice = __byte_perm(unit, unit, 0x3232);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v.w[i][j] = Part<bf16>::times(v.w[i][j], twice);
     }
 }
 
@@ -388,6 +455,7 @@ __global__ void __launch_bounds__(Turn<T>::kThreads, sizeof(T) == 4 ? 2 : (BOTH 
     constexpr int kWarps = U::kThreads / 32, CPL = U::CPL;
     constexpr uint32_t L = U::L;
     __shared__ __align__(16) float s_max[kWarps][128];
+    __shared__ __align__(16) decltype(Part<H>::store_factor(0.f)) s_factor[128];
     __shared__ __align__(16) unsigned char s_tile[128 * 128];
     extern __shared__ __align__(16) unsigned char s_more[];      // unaligned rows, and with BOTH their codes
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -399,66 +467,52 @@ __global__ void __launch_bounds__(Turn<T>::kThreads, sizeof(T) == 4 ? 2 : (BOTH 
     if constexpr (sizeof(T) == 1) load_part8(a, r0, c0, l, v);
     else load_part<T, OCTETS>(a, r0, c0, l, s_more, v);
 
-    float top[CPL];
-    v.column_tops(top);
-    if (lane < static_cast<int>(L)) {      // by lane: it reads its own columns back
+    {
+        float top[CPL];
+        v.column_tops(top);
+        if (lane < static_cast<int>(L)) {      // by lane: it reads its own columns back
 #pragma unroll
-        for (int h = 0; h < CPL / 4; ++h) reinterpret_cast<float4*>(s_max[warp])[h * L + l] = make_float4(top[4 * h], top[4 * h + 1], top[4 * h + 2], top[4 * h + 3]);
+            for (int h = 0; h < CPL / 4; ++h) reinterpret_cast<float4*>(s_max[warp])[h * L + l] = make_float4(top[4 * h], top[4 * h + 1], top[4 * h + 2], top[4 * h + 3]);
+        }
     }
-    if (!OCTETS && BOTH) __syncthreads();      // (the codes of the rows go where the rows were)
+    __syncthreads();      // (and the codes of unaligned rows go where the rows were)
+    if (tid < 128) {      // a column's scale, by one thread for all
+        const uint32_t e = tid / (4 * L) * 4 + (tid & 3), of = tid / 4 % L, c = OCTETS ? CPL * of + e : of + L * e;
+        uint32_t most = 0;      // (as bits: none is negative, and a NaN is the greatest)
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) most = max(most, __float_as_uint(s_max[w][tid]));
+        const uint32_t s = block_scale(__uint_as_float(most));
+        s_factor[tid] = Part<H>::store_factor(factor_of(__uint_as_float(most), s));
+        const Packed8Layout lay(a.cols, a.rows);
+        if (c0 + c < a.cols) static_cast<char*>(a.turned)[lay.scales(kb, rt >> 2) + (rt & 3) + Packed8Layout::scale_word(c)] = static_cast<char>(s);
+    }
     if (BOTH) {
         const Packed8Layout lay(a.rows, a.cols);
         char* dst = static_cast<char*>(a.dst) + lay.tile(rt, kb);
         char* scales = static_cast<char*>(a.dst) + lay.scales(rt, kb >> 2) + (kb & 3);
-        float most[8];
-        v.row_tops(most);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t e = block_scale(most[i]), r = rg * 8 + i;
-            const float inv = block_inverse(e);
-            uint32_t w[CPL / 4];
-#pragma unroll
-            for (int h = 0; h < CPL / 4; ++h) {
-                w[h] = codes4(v.get(i, 4 * h) * inv, v.get(i, 4 * h + 1) * inv, v.get(i, 4 * h + 2) * inv, v.get(i, 4 * h + 3) * inv);
-                if (not_finite(most[i])) w[h] = kNanCodes;
-            }
+        v.row_codes(l, [&](uint32_t i, const uint32_t (&w)[CPL / 4]) {
+            const uint32_t r = rg * 8 + i;
             if (!OCTETS) {
 #pragma unroll
                 for (uint32_t k = 0; k < CPL; ++k) s_more[r * 128 + ((column(k) >> 4 ^ (r & 7)) << 4) + (column(k) & 15)] = static_cast<unsigned char>(w[k / 4] >> (8 * (k & 3)));
+            } else if (rt * 128 + r < a.rows) {
+                char* to = dst + code_at(r, CPL * l & ~7u) + (CPL * l & 7);
+                if (CPL == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[CPL / 4 - 1]);
+                else *reinterpret_cast<uint32_t*>(to) = w[0];
             }
-            if (rt * 128 + r < a.rows) {
-                if (OCTETS) {
-                    char* to = dst + code_at(r, CPL * l & ~7u) + (CPL * l & 7);
-                    if (CPL == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[CPL / 4 - 1]);
-                    else *reinterpret_cast<uint32_t*>(to) = w[0];
-                }
-                if (l == 0) scales[Packed8Layout::scale_word(r)] = static_cast<char>(e);
-            }
-        }
+        }, [&](uint32_t i, uint32_t e) {
+            const uint32_t r = rg * 8 + i;
+            if (rt * 128 + r < a.rows) scales[Packed8Layout::scale_word(r)] = static_cast<char>(e);
+        });
     }
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWarps; w += 2)
-#pragma unroll
-        for (int h = 0; h < CPL / 4; ++h) {
-            const float4 p = reinterpret_cast<const float4*>(s_max[w])[h * L + l], x = reinterpret_cast<const float4*>(s_max[w + 1])[h * L + l];
-            top[4 * h] = top3(top[4 * h], p.x, x.x);
-            top[4 * h + 1] = top3(top[4 * h + 1], p.y, x.y);
-            top[4 * h + 2] = top3(top[4 * h + 2], p.z, x.z);
-            top[4 * h + 3] = top3(top[4 * h + 3], p.w, x.w);
-        }
     const Packed8Layout lay(a.cols, a.rows);
     char* turned = static_cast<char*>(a.turned) + lay.tile(kb, rt);
-    char* scales = static_cast<char*>(a.turned) + lay.scales(kb, rt >> 2) + (rt & 3);
+    {
+        typename Part<H>::Factors f[CPL / 4];
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) {
-        const uint32_t s = block_scale(top[e]);
-        const float inv = block_inverse(s);
-        uint2 w = make_uint2(codes4(v.get(0, e) * inv, v.get(1, e) * inv, v.get(2, e) * inv, v.get(3, e) * inv),
-                             codes4(v.get(4, e) * inv, v.get(5, e) * inv, v.get(6, e) * inv, v.get(7, e) * inv));
-        if (not_finite(top[e])) w = make_uint2(kNanCodes, kNanCodes);
-        *reinterpret_cast<uint2*>(s_tile + column(e) * 128 + ((rg ^ (l & 15)) << 3)) = w;
-        if (rg == 0 && c0 + column(e) < a.cols) scales[Packed8Layout::scale_word(column(e))] = static_cast<char>(s);
+        for (int h = 0; h < CPL / 4; ++h) f[h] = reinterpret_cast<const typename Part<H>::Factors*>(s_factor)[h * L + l];
+        v.column_codes(f, [&](uint32_t e, uint2 w) { *reinterpret_cast<uint2*>(s_tile + column(e) * 128 + ((rg ^ (l & 15)) << 3)) = w; });
     }
     __syncthreads();
 #pragma unroll
