@@ -139,11 +139,11 @@ __global__ void __launch_bounds__(kWarps8 * 32) pack8_kernel(const __grid_consta
     }
 }
 
-// A lane takes CPL neighbouring columns at a time, 16 bytes of the output, so that a warp writes whole lines; where rows do not start
-// on 16-byte boundaries single columns, 32 apart. Memory bounds it: 8192 x 4096 into bf16 17.5 us, fp32 29.2 (5.7 TB/s).
+// A warp takes four rows of 512 columns, a lane 16 neighbours of each (a piece of a tile, and whole sectors of the output); where rows do
+// not start on 16-byte boundaries single columns, 32 apart. Memory bounds it: 8192 x 4096 into bf16 17.1 us, fp32 26.3 (5.9, 6.4 TB/s; fp32
+// with 16 bytes to a lane 28.9).
 template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_bounds__(kWarps8 * 32) unpack8_kernel(const __grid_constant__ Unpack8Batch<BATCH> a)
 {
-    constexpr uint32_t CPL = OCTETS ? Store<T>::CPL : 8, kSteps = 512 / 32 / CPL;      // columns to a lane and step
     after_last();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Unpack8Matrix& m = a.mat[BATCH == 1 ? 0 : matrix_of(a, blockIdx.x)];
@@ -154,58 +154,60 @@ template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_boun
     const uint32_t n = min(kRows8, m.rows - r0);
     const char* src = static_cast<const char*>(m.src) + lay.tile(r0 >> 7, g * 4);
     const char* scales = static_cast<const char*>(m.src) + lay.scales(r0 >> 7, g) + Packed8Layout::scale_word(r0);      // (four rows from a multiple of 4)
-    uint32_t codes[kRows8][kSteps][CPL / 4], word[kRows8];
+    T* to = static_cast<T*>(m.dst) + r0 * m.stride;
+    if constexpr (OCTETS) {
+        const uint32_t c = g * 512 + lane * 16, block = lane >> 3;
+        if (g * 4 + block >= lay.col_blocks) return;
+        uint4 w[kRows8];
+        uint32_t e[kRows8];
 #pragma unroll
-    for (uint32_t i = 0; i < kRows8; ++i) {
-        if (i >= n) break;
-        word[i] = __ldg(reinterpret_cast<const uint32_t*>(scales + 16 * i));
+        for (uint32_t i = 0; i < kRows8; ++i) {
+            if (i >= n) break;
+            e[i] = __ldg(reinterpret_cast<const unsigned char*>(scales) + 16 * i + block);
+            w[i] = __ldcs(reinterpret_cast<const uint4*>(src + block * 16384 + code_at(r0 + i, lane * 16)));
+        }
 #pragma unroll
-        for (uint32_t k = 0; k < kSteps; ++k) {
-            const uint32_t c = k * 32 * CPL + lane * CPL;      // inside the group
-            if (g * 4 + (c >> 7) >= lay.col_blocks) continue;
-            const char* p = src + (c >> 7) * 16384 + code_at(r0 + i, c & ~7u) + (c & 7);
-            if (CPL == 8) {
-                const uint2 w = __ldcs(reinterpret_cast<const uint2*>(p));
-                codes[i][k][0] = w.x;
-                codes[i][k][CPL / 4 - 1] = w.y;
-            } else {
-                codes[i][k][0] = __ldcs(reinterpret_cast<const uint32_t*>(p));
+        for (uint32_t i = 0; i < kRows8; ++i) {
+            if (i >= n) break;
+            const float unit = block_unit(e[i]);
+            float lo[8], hi[8];
+            values4(w[i].x, unit, lo);
+            values4(w[i].y, unit, lo + 4);
+            values4(w[i].z, unit, hi);
+            values4(w[i].w, unit, hi + 4);
+            store_two(to + i * m.stride, c, cols, lo, hi);
+        }
+    } else {
+        uint2 codes[kRows8][2];      // of two runs of 256 columns
+        uint32_t word[kRows8];
+#pragma unroll
+        for (uint32_t i = 0; i < kRows8; ++i) {
+            if (i >= n) break;
+            word[i] = __ldg(reinterpret_cast<const uint32_t*>(scales + 16 * i));
+#pragma unroll
+            for (uint32_t k = 0; k < 2; ++k) {
+                const uint32_t c = k * 256 + lane * 8, block = c >> 7;      // inside the group
+                if (g * 4 + block < lay.col_blocks) codes[i][k] = __ldcs(reinterpret_cast<const uint2*>(src + block * 16384 + code_at(r0 + i, c)));
             }
         }
-    }
 #pragma unroll
-    for (uint32_t i = 0; i < kRows8; ++i) {
-        if (i >= n) break;
-        T* row = static_cast<T*>(m.dst) + (r0 + i) * m.stride;
+        for (uint32_t i = 0; i < kRows8; ++i) {
+            if (i >= n) break;
 #pragma unroll
-        for (uint32_t k = 0; k < kSteps; ++k) {
-            const uint32_t first = g * 512 + k * 32 * CPL, c = first + lane * CPL;
-            if (first >= cols) break;
-            if (OCTETS) {
-                const float unit = block_unit((word[i] >> (8 * ((c >> 7) & 3))) & 0xFFu);
-                float v[8];
-                values4(codes[i][k][0], unit, v);
-                if (CPL == 8) values4(codes[i][k][CPL / 4 - 1], unit, v + 4);
-                if (c + CPL <= cols) {
-                    const Octet<T> o = narrow<T>(v);      // (of four fp32 columns the first word)
-                    *reinterpret_cast<uint4*>(row + c) = o.w[0];
-                } else {
-#pragma unroll
-                    for (uint32_t e = 0; e < CPL; ++e)
-                        if (c + e < cols) Out<T>::store1(row + c + e, v[e]);
-                }
-            } else {
+            for (uint32_t k = 0; k < 2; ++k) {
+                const uint32_t first = g * 512 + k * 256;
+                if (first >= cols) break;
                 // column l + 32 j lies in lane 4 j + l / 8, whose eight codes are 8 (l / 8) .. + 7 of that run
                 float v[8];
 #pragma unroll
                 for (uint32_t j = 0; j < 8; ++j) {
                     const uint32_t from = 4 * j + (lane >> 3);
-                    const uint32_t x = __shfl_sync(~0u, codes[i][k][0], from), y = __shfl_sync(~0u, codes[i][k][CPL / 4 - 1], from);
+                    const uint32_t x = __shfl_sync(~0u, codes[i][k].x, from), y = __shfl_sync(~0u, codes[i][k].y, from);
                     float u[4];
                     values4((lane & 4 ? y : x) >> (8 * (lane & 3)), block_unit((word[i] >> (16 * k + 8 * (j >> 2))) & 0xFFu), u);
                     v[j] = u[0];
                 }
-                store_strided(row, first, cols, lane, v);
+                store_strided(to + i * m.stride, first, cols, lane, v);
             }
         }
     }
