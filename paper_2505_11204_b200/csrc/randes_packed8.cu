@@ -180,14 +180,15 @@ template <typename T, bool OCTETS, uint32_t BATCH> __global__ void __launch_boun
     } else {
         uint2 codes[kRows8][2];      // of two runs of 256 columns
         uint32_t word[kRows8];
+        const uint32_t last = lay.col_blocks - 1 - g * 4;
 #pragma unroll
         for (uint32_t i = 0; i < kRows8; ++i) {
             if (i >= n) break;
             word[i] = __ldg(reinterpret_cast<const uint32_t*>(scales + 16 * i));
 #pragma unroll
             for (uint32_t k = 0; k < 2; ++k) {
-                const uint32_t c = k * 256 + lane * 8, block = c >> 7;      // inside the group
-                if (g * 4 + block < lay.col_blocks) codes[i][k] = __ldcs(reinterpret_cast<const uint2*>(src + block * 16384 + code_at(r0 + i, c)));
+                const uint32_t c = k * 256 + lane * 8, block = min(c >> 7, last);      // inside the group
+                codes[i][k] = __ldcs(reinterpret_cast<const uint2*>(src + block * 16384 + code_at(r0 + i, c)));
             }
         }
 #pragma unroll
