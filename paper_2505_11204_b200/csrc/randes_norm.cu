@@ -145,8 +145,12 @@ __device__ __forceinline__ void store_octets(T* row, const Place<THREADS, OCTETS
     }
 }
 
+// CTAs an SM has to hold, where the compiler would otherwise take so many registers that it holds one less. (2048 x 16001 fp32 124 us
+// with one row at a time, 95 with two; 4096 x 8101 bf16 76 with two, 64 with three. The same cap on narrower forms made them slower.)
+template <int THREADS, bool LOOSE> constexpr int kHeld = THREADS == 448 || THREADS == 512 ? 2 : (LOOSE && THREADS == 256 ? 3 : 0);      // (0: as the compiler likes)
+
 template <typename T, int THREADS, int CHUNKS, bool OCTETS, bool LOOSE>
-__global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>) norm_kernel(const NormArgs a)
+__global__ void __launch_bounds__(THREADS* kRowsPerCta<THREADS>, kHeld<THREADS, LOOSE>) norm_kernel(const NormArgs a)
 {
     __shared__ __align__(16) uint4 s_scratch[LOOSE ? THREADS * kRowsPerCta<THREADS> / 32 : 1][64];
     constexpr int kWarps = THREADS * kRowsPerCta<THREADS> / 32;
@@ -632,8 +636,9 @@ __global__ void __launch_bounds__(32 * kSumRows) norm_gain_kernel(const float* p
 }
 
 template <int V> using Const = std::integral_constant<int, V>;
-// Calls f with the row's form: threads to a row and runs of 8 columns per thread. (768 bf16 columns, 32768 rows: 45 us with runs
-// of 512, the second half empty; 37 with half a warp to a row.)
+// Calls f with the row's form: threads to a row and runs of 8 columns per thread. Empty threads hold registers that rows under way could
+// have, so widths come in steps of an eighth to a half. (768 bf16 columns, 32768 rows: 45 us with runs of 512, the second half empty; 37
+// with half a warp to a row. 3702 x 4352 and 4358: 34 and 61 us with 256 threads, 27 and 33 with 160. 8192 x 2560: 33 with 128, 28 with 96.)
 template <bool ALIGNED, typename F> int by_width(uint32_t cols, F&& f)
 {
     if constexpr (ALIGNED) {
@@ -642,9 +647,17 @@ template <bool ALIGNED, typename F> int by_width(uint32_t cols, F&& f)
     }
     if (cols <= 512) return f(Const<32>(), Const<2>());
     if (cols <= 1024) return f(Const<32>(), Const<4>());
+    if (cols <= 1536) return f(Const<96>(), Const<2>());
     if (cols <= 2048) return f(Const<128>(), Const<2>());
+    if (cols <= 3072) return f(Const<96>(), Const<4>());
     if (cols <= 4096) return f(Const<128>(), Const<4>());
+    if (cols <= 5120) return f(Const<160>(), Const<4>());
+    if (cols <= 6144) return f(Const<192>(), Const<4>());
+    if (cols <= 7168) return f(Const<224>(), Const<4>());
     if (cols <= 8192) return f(Const<256>(), Const<4>());
+    if (cols <= 10240) return f(Const<320>(), Const<4>());
+    if (cols <= 12288) return f(Const<384>(), Const<4>());
+    if (cols <= 14336) return f(Const<448>(), Const<4>());
     if (cols <= 16384) return f(Const<512>(), Const<4>());
     return f(Const<1024>(), Const<4>());
 }

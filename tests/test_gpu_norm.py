@@ -117,6 +117,23 @@ def test_backward_of_wide_rows(n, cols, pad, dtype):
         assert torch.equal(into, dx) and torch.equal(base[:, :pad], rows_of(n, cols + pad, dtype, 2)[:, :pad])
 
 
+# one width of every number of threads to a row, on 16-byte boundaries and off them
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [1281, 1536, 2500, 3064, 4097, 5120, 5121, 6000, 6145, 7168, 7169, 8200, 10241, 12288, 12289, 14336, 14337])
+def test_forward_of_every_width(cols, dtype):
+    n = 5
+    x, r, gain = rows_of(n, cols, dtype, 1), rows_of(n, cols, dtype, 2, 3.0), 1 + 0.3 * rows_of(1, cols, torch.float32, 3)[0]
+    p = randes.rms_norm(x, gain, r, eps=EPS, packed=True, checkpoint=True)
+    f = randes.rms_norm(x, gain, r, eps=EPS)
+    h = (x.float() + r.float()).to(dtype)
+    rstd, y = norm64(h, gain)
+    assert torch.equal(p.h, h) and torch.equal(f.h, h) and torch.equal(p.rstd, f.rstd)
+    assert ((f.rstd.double() - rstd).abs() <= FP32 * rstd).all()
+    assert ((f.y.double() - y).abs() <= (FP32 + (step(dtype) if dtype is torch.bfloat16 else 0)) * y.abs()).all()
+    check_eight(p.y, y, FP32)
+    assert torch.equal(p.kept.unpack(), randes.pack8(h).unpack())
+
+
 def test_gradient_against_differences():
     n, cols, d = 3, 200, 1e-4
     x, gain, g = rows_of(n, cols, torch.float32, 1), 1 + 0.3 * rows_of(1, cols, torch.float32, 2)[0], rows_of(n, cols, torch.float32, 3)
