@@ -822,7 +822,7 @@ def _new_packed8(rows: int, cols: int, device) -> Packed8Matrix:
     import torch
 
     p = Packed8Matrix.__new__(Packed8Matrix)      # (the size is right)
-    p._hold(rows, cols, torch.empty(_packed8_size(rows, cols), dtype=_torch.uint8, device=device))
+    p._hold(rows, cols, torch.empty(_packed8_size(rows, cols), dtype=torch.uint8, device=device))
     return p
 
 

@@ -319,3 +319,18 @@ def test_chains_of_calls_in_graphs_that_fork_and_join():
             out.zero_()
             g.replay()
             assert torch.equal(out, want)
+
+
+def test_retrieving_or_turning_may_be_the_first_call(monkeypatch):
+    w = torch.randn(130, 300, device="cuda")
+    p, t = randes.pack8_both(w)
+    plan = randes.Plan([130], [300], [0], [0], task_ids=[0], seeds=[1])
+    M = plan.new_superposition()
+    M.zero_()
+    for first in (lambda: randes.pack8_transposed(randes.Packed8Matrix(130, 300, p.data)), lambda: plan.retrieve_packed8(0, 0.3, [w], M)[0], lambda: p,
+                  lambda: randes.packed8_linear(p, p)):
+        monkeypatch.setattr(randes, "_torch", None)
+        got = first()
+        if isinstance(got, randes.Packed8Matrix):
+            assert torch.equal(got.unpack(), (t if got.rows == 300 else p).unpack())
+    plan.close()

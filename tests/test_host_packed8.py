@@ -118,3 +118,10 @@ def test_product_refusals():
         refused(code, lambda: call(**kw))
     call(n_tokens=0, x=None, y=None)
     call(rows=0, w=None, y=None)
+
+
+def test_the_first_call_of_a_process_may_be_any(monkeypatch):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(randes, "_torch", None)      # as a process that has made no call on tensors finds it
+    p = randes._new_packed8(3, 200, torch.device("cpu"))
+    assert (p.rows, p.cols, p.nbytes) == (3, 200, randes.randes_packed_eight_bytes(3, 200)) and p.data.dtype is torch.uint8
