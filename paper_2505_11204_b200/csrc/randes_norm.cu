@@ -645,20 +645,21 @@ template <bool ALIGNED, typename F> int by_width(uint32_t cols, F&& f)
         if (cols <= 256) return f(Const<16>(), Const<2>());
         if (cols > 512 && cols <= 768) return f(Const<16>(), Const<6>());
     }
-    if (cols <= 512) return f(Const<32>(), Const<2>());
-    if (cols <= 1024) return f(Const<32>(), Const<4>());
-    if (cols <= 1536) return f(Const<96>(), Const<2>());
-    if (cols <= 2048) return f(Const<128>(), Const<2>());
-    if (cols <= 3072) return f(Const<96>(), Const<4>());
-    if (cols <= 4096) return f(Const<128>(), Const<4>());
-    if (cols <= 5120) return f(Const<160>(), Const<4>());
-    if (cols <= 6144) return f(Const<192>(), Const<4>());
-    if (cols <= 7168) return f(Const<224>(), Const<4>());
-    if (cols <= 8192) return f(Const<256>(), Const<4>());
-    if (cols <= 10240) return f(Const<320>(), Const<4>());
-    if (cols <= 12288) return f(Const<384>(), Const<4>());
-    if (cols <= 14336) return f(Const<448>(), Const<4>());
-    if (cols <= 16384) return f(Const<512>(), Const<4>());
+    auto fits = [&](uint32_t threads, uint32_t chunks) { return cols <= 8 * threads * chunks; };
+    if (fits(32, 2)) return f(Const<32>(), Const<2>());
+    if (fits(32, 4)) return f(Const<32>(), Const<4>());
+    if (fits(96, 2)) return f(Const<96>(), Const<2>());
+    if (fits(128, 2)) return f(Const<128>(), Const<2>());
+    if (fits(96, 4)) return f(Const<96>(), Const<4>());
+    if (fits(128, 4)) return f(Const<128>(), Const<4>());
+    if (fits(160, 4)) return f(Const<160>(), Const<4>());
+    if (fits(192, 4)) return f(Const<192>(), Const<4>());
+    if (fits(224, 4)) return f(Const<224>(), Const<4>());
+    if (fits(256, 4)) return f(Const<256>(), Const<4>());
+    if (fits(320, 4)) return f(Const<320>(), Const<4>());
+    if (fits(384, 4)) return f(Const<384>(), Const<4>());
+    if (fits(448, 4)) return f(Const<448>(), Const<4>());
+    if (fits(512, 4)) return f(Const<512>(), Const<4>());
     return f(Const<1024>(), Const<4>());
 }
 // CTAs that walk the rows of a backward pass: the rows, or what the 148 SMs hold at a time (a constant, so that sums are the same
